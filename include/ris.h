@@ -320,7 +320,7 @@ int32_t ris_attention_design(ris_mask_t mask, int32_t dtype, int32_t head_dim);
 
 /* Synchronise `stream` and report (then clear) the device error words: RIS_ERR_DEVICE_TIMEOUT
  * if a kernel's bounded wait gave up since the last call, RIS_ERR_INVALID if a decode step
- * read a position outside [t0, cache_len) from device memory, else RIS_OK. A kernel that sets
+ * read a position outside [t0, cache_len) from device memory or tokens did not fit a 4-bit cache, else RIS_OK. A kernel that sets
  * a word skips the rest of its work, so outputs of that launch are undefined. Blocks.
  * Errors: RIS_ERR_CUDA. */
 ris_status ris_device_status(void *stream);
@@ -405,6 +405,117 @@ ris_status ris_decode_step(ris_anchor_t anchor, const void *q, const void *k, co
                            int64_t cache_len, int64_t t, int64_t *t_dev, int32_t advance, int32_t window,
                            int32_t heads, int32_t kv_heads, int32_t head_dim, int32_t dtype, int32_t out_dtype,
                            int64_t n_ctx, const ris_rope_cfg *rope, void *out, float *lse, void *stream);
+
+/* ---- Packed prompts and a 4-bit cache ---------------------------------------------------------
+ * The serving path of a batch of sequences (the paper has no counterpart): positions given per
+ * token, causal attention over prompts of different lengths in one call, a K/V cache held in 4
+ * bits, and its eviction by accumulated attention weight.
+ *
+ * Pack: the plan of a call over n_seqs sequences whose tokens lie one after another. Sequence s has
+ * q_lens[s] rows (new tokens) and k_lens[s] keys (HOST arrays; k_lens NULL: the same lengths). The rows
+ * are the last of the sequence's positions: row i sees keys j <= i + k_lens[s] - q_lens[s], and a row that sees none
+ * gets zeros and a log-sum-exp of -infinity. Lengths may be 0. Built once per batch
+ * and kept for all layers and all calls of it, on any stream ordered after `stream`. Blocks (the
+ * plan's copy); not during stream capture. Errors: RIS_ERR_INVALID (n_seqs outside [1, 65535], a negative length,
+ * more than 2^31 - 65537 tokens), RIS_ERR_OOM, RIS_ERR_CUDA. On error *out is NULL.
+ * ris_pack_info: any output may be NULL. ris_pack_free: ordered on the stream it was built on. */
+typedef struct ris_pack_s *ris_pack_t;
+ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t n_seqs, ris_pack_t *out, void *stream);
+ris_status ris_pack_info(ris_pack_t pack, int32_t *n_seqs, int64_t *q_total, int64_t *k_total, int64_t *q_longest,
+                         int64_t *k_longest);
+ris_status ris_pack_free(ris_pack_t pack);
+
+/* Rotate q [n][heads][head_dim] and k [n][kv_heads][head_dim] (k may be NULL with kv_heads 0) at given
+ * positions, rotate-half pairs (c, c + D/2), then scale by the rope's mscale. Token i's heads start at
+ * q + i * q_stride (elements, a multiple of 16 bytes, at least heads * head_dim: the rows of a fused
+ * projection); q_out and k_out are contiguous, and may be q and k where those are contiguous.
+ * positions: DEVICE int32 [axes][n], of either sign. sections: HOST [axes], 1 <= axes <= 4: how many of the
+ * head_dim / 2 frequencies follow each axis (time, height, width), sections[0] first, or with
+ * interleaved = 1 frequency c follows axis c mod axes while c / axes < sections[that axis], else axis 0. One
+ * axis with sections[0] = head_dim / 2 is ordinary RoPE at any positions (packed prompts, a batch's next tokens). The
+ * extension factor is resolved for n_ctx tokens. inverse = 1 turns backwards: the transposed
+ * map, which takes the gradient of q_out and k_out to that of q and k. Angles as in
+ * ris_attention_masked's own rotation; fp32 arithmetic, bf16 results rounded to nearest even.
+ * Errors: RIS_ERR_INVALID (rope NULL or NONE, head_dim not 64 or 128, sections that do not sum to head_dim / 2). */
+ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out, int32_t dtype, int64_t n, int32_t heads,
+                         int32_t kv_heads, int32_t head_dim, int64_t q_stride, int64_t k_stride, const int32_t *positions,
+                         int32_t axes, const int32_t *sections, int32_t interleaved, int64_t n_ctx, const ris_rope_cfg *rope,
+                         int32_t inverse, void *stream);
+
+/* Causal attention over the sequences of a pack: q [q_total][heads][head_dim], k and v [k_total][kv_heads]
+ * [head_dim] as given (rotated by the caller), token strides in elements as in ris_rope_axes;
+ * out [q_total][heads][head_dim] contiguous; scores scaled by 1 / sqrt(head_dim).
+ * lse: optional [heads][q_total] natural-log sum of exp of the scaled scores.
+ * weight_rows W > 0 with key_weight [kv_heads][k_total]: the attention weight that each key got from the
+ * last W rows of its sequence (all rows where there are fewer), summed over the query heads of its KV head: what
+ * ris_cache4_append takes as the first of a slot's accumulated weight. W = 0: key_weight NULL.
+ * head_dim in {64, 128}, any heads / kv_heads, fp32 or bf16. fp32 inputs never use a narrower product.
+ * A key that a row does not see takes no part in it, whatever it holds.
+ * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (more row tiles x heads than a grid holds), RIS_ERR_OOM, RIS_ERR_CUDA. */
+ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, const void *v, void *out, int32_t heads,
+                                int32_t kv_heads, int32_t head_dim, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                                int32_t dtype, int32_t out_dtype, float *lse, int32_t weight_rows, float *key_weight,
+                                void *stream);
+
+/* A K/V cache held in 4 bits: caller-owned DEVICE arrays, each 16-byte aligned. Sequence b holds the
+ * slots 0 .. length[b] - 1 of every KV head; the slots of a head need not be in the order of their
+ * positions, and after an eviction differ from head to head.
+ *   A row of head_dim values is cut into groups of 32. A group's scale is bf16(max |x| * fl32(1/6)) (NaN where a
+ *   value is not finite: the group then stands for NaN); a value is stored as the e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6, sign in bit 3)
+ *   nearest to x / scale in fp32, ties to the even code, at most 6. Two codes make a byte, the even element in the
+ *   low half. With i the byte's number in natural order, n = head_dim / 32 and m = head_dim / 16, it lies at
+ *     keys    4 (((i / 4) mod 4) n + i / 16) + i mod 4,      values  (i mod 8) m + i / 8.
+ * capacity is a multiple of 16; slots at and past length[b] may hold anything. `sync` is zeroed by the
+ * caller once; every call leaves it zero. Calls on one cache must be ordered on the GPU. */
+typedef struct {
+    int32_t batch;     /* sequences, 1 .. 65535 */
+    int32_t kv_heads;  /* 1 .. 4096 */
+    int32_t head_dim;  /* 64 or 128 */
+    int32_t reserved;  /* must be 0 */
+    int64_t capacity;  /* slots of a sequence and head, a multiple of 16, at most 2^30 */
+    uint8_t *k, *v;            /* [batch][kv_heads][capacity][head_dim / 2] codes */
+    void *k_scale, *v_scale;   /* bf16 [batch][kv_heads][capacity][head_dim / 32] */
+    int32_t *pos;              /* [batch][kv_heads][capacity] position of the slot's token */
+    float *weight;             /* [batch][kv_heads][capacity] accumulated attention weight */
+    int32_t *length;           /* [batch] slots in use */
+    uint32_t *sync;            /* 4 words */
+} ris_cache4;
+
+/* Append the rows of a pack (its q side; sequence s to row s of the batch) to the cache: k and v
+ * [q_total][kv_heads][head_dim], rotated, token strides in elements; positions: DEVICE int32 [q_total]; weight: optional
+ * DEVICE [kv_heads][q_total] (else 0). Token i of sequence b goes to slot start[b] + i and length[b] becomes start[b] + q_lens[b];
+ * start NULL: after the slots in use. start (DEVICE int32 [batch]) must not be the cache's length.
+ * Tokens past the capacity (or at a negative slot) are left out and reported by ris_device_status as
+ * RIS_ERR_INVALID. A pack of ones is a decode step's append. Errors: RIS_ERR_INVALID, RIS_ERR_CUDA. */
+ris_status ris_cache4_append(const ris_cache4 *cache, ris_pack_t pack, const void *k, const void *v, int64_t k_stride,
+                             int64_t v_stride, int32_t dtype, const int32_t *positions, const float *weight,
+                             const int32_t *start, void *stream);
+
+/* The values that slots first[b] .. first[b] + count - 1 stand for (first NULL: 0; DEVICE int32 [batch]), exactly:
+ * k and v fp32 [batch][kv_heads][count][head_dim]; zeros for slots that are not in use. */
+ris_status ris_cache4_read(const ris_cache4 *cache, const int32_t *first, int64_t count, float *k, float *v, void *stream);
+
+/* One token's attention per sequence over every slot in use: q [batch][heads][head_dim] (rotated), out the
+ * same shape (out_dtype), lse optional [batch][heads]. A sequence without slots gets zeros and -infinity.
+ * longest: an upper bound of the lengths that the caller knows (slots past it take no part), 0 for the
+ * capacity: it sizes the grid and the scratch, so nothing in the launch depends on the lengths and a
+ * captured graph can be replayed as they grow.
+ * weight_out (optional, [batch][kv_heads][capacity]): weight_in + the weights of this token, summed over the query
+ * heads of the KV head, for every slot in use (others untouched); weight_in NULL counts as 0 and may be weight_out
+ * (the cache's own weight array, to add up in place). fp32 outputs take the query (fp32 inputs) and the weights in two fp16 parts each, bf16
+ * outputs the weights in one. Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
+ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t heads, int32_t dtype, int32_t out_dtype,
+                             int64_t longest, void *out, float *lse, const float *weight_in, float *weight_out, void *stream);
+
+/* Cut every (sequence, KV head) of src with more than `budget` slots back to `budget`, into dst (another cache
+ * of the same batch, kv_heads and head_dim with capacity >= budget, or src itself). Kept are the first `budget`
+ * slots in this order: those with a position above the newest of the head - `recent`, then by weight
+ * (NaN last), then by slot. A kept slot below the budget keeps its place; the i-th kept one at or above it
+ * takes the i-th freed place below it. kept: DEVICE int32 [batch][kv_heads][budget], the source slot of each
+ * place, -1 where there is none. dst's lengths become min(length, budget); its slots past that are untouched.
+ * 0 <= recent < budget. Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
+ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_t budget, int32_t recent, int32_t *kept,
+                            void *stream);
 
 /* ---- Measurement support (the paper has no counterpart) -------------------------------------
  * Small kernels that measure the ceilings the attention kernels are compared against, for the

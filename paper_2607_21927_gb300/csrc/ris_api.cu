@@ -18,6 +18,7 @@
 #include <vector>
 
 #include "ris_internal.h"
+#include "serve.h"
 
 namespace ris {
 
@@ -386,6 +387,11 @@ ris_status validate_attention(const void *q, const void *k, const void *v, void 
 
 namespace ris {
 void set_error_text(const char *msg) { t_err = msg; }
+cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s)
+{
+    prepare_pool_once();
+    return pool_alloc(p, bytes < 16 ? 16 : bytes, s);
+}
 }  // namespace ris
 
 extern "C" {
@@ -913,11 +919,12 @@ ris_status ris_device_status(void *stream)
     unsigned int word = 0, tile_word = 0;
     RIS_CUDA(cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)));
     RIS_CUDA(read_tile_error(&tile_word));
-    const unsigned int decode_word = read_decode_error();
-    word |= tile_word;
+    const unsigned int decode_word = read_decode_error(), cache_word = read_cache4_error();
+    word |= tile_word | (cache_word & 4u);
     if (word != 0u) return fail(RIS_ERR_DEVICE_TIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
     if (decode_word != 0u)
         return fail(RIS_ERR_INVALID, "a decode step read a position outside [t0, cache_len) from t_dev");
+    if (cache_word != 0u) return fail(RIS_ERR_INVALID, "tokens were appended outside a 4-bit cache's slots and left out");
     return RIS_OK;
 }
 

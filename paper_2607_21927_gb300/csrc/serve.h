@@ -1,0 +1,127 @@
+// Internal declarations of the serving operators: packed prompts, positions on several axes and
+// the 4-bit cache (not part of the ABI).
+#pragma once
+
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "../../include/ris.h"
+#include "ris_internal.h"
+
+namespace ris {
+
+constexpr int kPackRows = 128;      // query rows of a work item of a pack (one TMEM tile)
+constexpr int kPackKeys = 128;      // keys of a key item
+constexpr int kMaxAxes = 4;
+constexpr int kCacheGroup = 32;     // elements that share a scale
+constexpr int kMaxPackSeqs = 65535;
+
+// A work item: rows row .. row + kPackRows - 1 (or keys) of a sequence. The sequence's own sizes ride
+// along, so that a CTA needs one 32-byte load to know everything about its item.
+struct alignas(32) PackItem {
+    int32_t seq;
+    int32_t row;     // first row (or key) of the item within its sequence
+    int32_t q_base;  // first row of the sequence in q / out
+    int32_t q_len;
+    int32_t k_base;  // first key of the sequence in k / v
+    int32_t k_len;
+    int32_t pad[2];
+};
+
+struct RopeAxesArgs {
+    const void *x[2];          // q and k (k may be null: heads[1] = 0)
+    void *y[2];
+    int64_t stride[2];         // elements from one token's heads to the next's
+    int32_t heads[2];
+    int64_t n;
+    int32_t D;
+    const int32_t *pos;        // [axes][n]
+    uint8_t axis[kMaxHeadDimHalf];   // axis of each frequency
+    uint64_t turn[kMaxHeadDimHalf];  // rotation frequencies as fractions of a turn, in 2^-64
+    float mscale;
+    int32_t inverse;
+};
+cudaError_t launch_rope_axes(const RopeAxesArgs &a, int dtype, cudaStream_t s);
+
+struct PackedArgs {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;  // elements from token to token
+    void *out;                 // [q_total][Hq][D]
+    float *lse;                // [Hq][q_total] or null
+    int64_t q_total, k_total;
+    const PackItem *items;     // query items, the longest key range first
+    int32_t n_items;
+    const PackItem *key_items;
+    int32_t n_key_items;
+    int32_t Hq, Hkv, G;
+    float scale_log2;          // log2(e) / sqrt(D)
+    // key weights: of the last weight_rows rows of each sequence
+    int32_t weight_rows;       // 0: none
+    float *key_weight;         // [Hkv][k_total]
+    float2 *row_stat;          // scratch [Hq][q_total]: each row's (maximum in log2, 1 / sum); null without weights
+    const void *v16;           // bf16 calls: the values as fp16, scaled by 2^-E, [k_total][Hkv][D]
+    const float *v_absmax;     // device: max |v|
+};
+cudaError_t launch_packed_f32(const PackedArgs &a, int D, int dtype, int out_dtype, cudaStream_t s);
+cudaError_t launch_packed_weights(const PackedArgs &a, int D, int dtype, cudaStream_t s);
+
+struct Cache4Args {
+    uint8_t *k, *v;              // [B][Hkv][cap][D / 2]
+    uint16_t *k_scale, *v_scale; // bf16 [B][Hkv][cap][D / 32]
+    int32_t *pos;                // [B][Hkv][cap]
+    float *weight;               // [B][Hkv][cap]
+    int32_t *length;             // [B]
+    int32_t B, Hkv, D;
+    int64_t cap;
+};
+
+struct Cache4AppendArgs {
+    Cache4Args c;
+    const void *k, *v;
+    int64_t k_stride, v_stride;
+    const int32_t *positions;    // [total]
+    const float *weight;         // [Hkv][total] or null (zero)
+    const int32_t *start;        // [B] or null: the cache's lengths
+    const int32_t *off;          // the pack's row offsets [B + 1]
+    const int32_t *seq_of;       // sequence of each row [total]
+    int64_t total;
+    unsigned int *ticket;        // start null: CTAs done (0 between calls)
+};
+cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStream_t s);
+cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_t count, float *k, float *v, cudaStream_t s);
+
+struct Cache4AttendArgs {
+    Cache4Args c;
+    const void *q;               // [B][Hq][D]
+    void *out;
+    float *lse;                  // [B][Hq] or null
+    const float *weight_in;      // [B][Hkv][cap] or null
+    float *weight_out;           // or null
+    int32_t Hq, G;
+    float scale_log2;
+    int64_t reach;               // slots that a sequence can hold: cap, or less where the caller knows better
+    int32_t chunk;               // slots of a CTA, a multiple of 16
+    int32_t n_chunks;            // CTAs of a (sequence, KV head)
+    float *part_o;               // [B][Hq][n_chunks][D]
+    float2 *part_ml;             // [B][Hq][n_chunks]
+    float *scores;               // weights: [B][Hq][cap] scores in log2
+    float2 *row_stat;            // weights: [B][Hq] (maximum in log2, 1 / sum)
+};
+cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s);
+
+struct Cache4EvictArgs {
+    Cache4Args src, dst;
+    int32_t in_place;
+    int32_t budget, recent;
+    int32_t *kept;               // [B][Hkv][budget]
+};
+// holes: scratch [B * Hkv][budget]
+cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaStream_t s);
+
+// Reads and clears the error word of the cache's kernels (bit 1: tokens appended past the capacity).
+unsigned int read_cache4_error();
+
+// Stream-ordered pool memory, as every allocation of the library (ris_api.cu).
+cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s);
+
+}  // namespace ris

@@ -121,6 +121,21 @@ _SIGS = {
                         ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                         ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                         ctypes.c_void_p],
+    "ris_pack_create": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p],
+    "ris_pack_info": [ctypes.c_void_p] * 6,
+    "ris_pack_free": [ctypes.c_void_p],
+    "ris_rope_axes": [ctypes.c_void_p] * 4 + [ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
+                      ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                      ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p],
+    "ris_attention_packed": [ctypes.c_void_p] * 5 + [ctypes.c_int32] * 3 + [ctypes.c_int64] * 3 +
+                            [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p,
+                             ctypes.c_void_p],
+    "ris_cache4_append": [ctypes.c_void_p] * 4 + [ctypes.c_int64, ctypes.c_int64, ctypes.c_int32] + [ctypes.c_void_p] * 4,
+    "ris_cache4_read": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64] + [ctypes.c_void_p] * 3,
+    "ris_cache4_attend": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                          ctypes.c_int64] + [ctypes.c_void_p] * 5,
+    "ris_cache4_evict": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
+                         ctypes.c_void_p],
     "ris_probe_l2_read": [ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p],
     "ris_probe_ffma": [ctypes.c_void_p, ctypes.c_void_p],
     "ris_probe_l2_bytes": [ctypes.c_void_p],
@@ -578,3 +593,189 @@ def ris_mask_row_split(mask: Mask, parts: int):
     _check("ris_mask_row_split", lib().ris_mask_row_split(mask.handle, int(parts), b))
     return list(b)
 
+
+# ----------------------------------------------------------------------------- packed prompts
+class Pack:
+    """The plan of a batch of sequences (ris_pack_create); freed by ``free()`` or when garbage collected."""
+
+    def __init__(self, handle: ctypes.c_void_p):
+        self.handle = handle
+        n, t = ctypes.c_int32(), [ctypes.c_int64() for _ in range(4)]
+        _check("ris_pack_info", lib().ris_pack_info(handle, ctypes.byref(n), *(ctypes.byref(x) for x in t)))
+        self.n_seqs = n.value
+        self.q_total, self.k_total, self.q_longest, self.k_longest = (x.value for x in t)
+
+    def free(self) -> None:
+        if self.handle:
+            _check("ris_pack_free", lib().ris_pack_free(self.handle))
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.free()
+
+
+def ris_pack_create(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, stream=None) -> Pack:
+    """Sequences of q_lens rows and k_lens keys each (k_lens None: the same)."""
+    n = len(q_lens)
+    if k_lens is not None and len(k_lens) != n:
+        raise ValueError(f"{n} row lengths, {len(k_lens)} key lengths")
+    q = (ctypes.c_int64 * max(n, 1))(*[int(x) for x in q_lens])
+    k = None if k_lens is None else (ctypes.c_int64 * max(n, 1))(*[int(x) for x in k_lens])
+    h = ctypes.c_void_p()
+    _check("ris_pack_create", lib().ris_pack_create(q, k, n, ctypes.byref(h), _stream(stream)))
+    return Pack(h)
+
+
+def _token_stride(x: torch.Tensor, name: str) -> int:
+    """Elements from token to token of x [n, H, D] whose heads lie side by side."""
+    n, H, D = x.shape
+    if not x.is_cuda or (x.numel() > 0 and ((D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D))):
+        raise ValueError(f"{name}: [n, H, D] on the GPU, each token's heads side by side")
+    return x.stride(0) if n > 1 else H * D
+
+
+def ris_rope_axes(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, sections: Sequence[int], n_ctx: int,
+                  rope: RopeCfg, interleaved: bool = False, inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """q [n, Hq, D] and k [n, Hkv, D] (or None) rotated at positions [axes, n] (int32): (q_out, k_out)."""
+    n, Hq, D = q.shape
+    Hkv = 0 if k is None else k.shape[1]
+    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32
+    assert tuple(positions.shape) == (len(sections), n), "positions: [axes, n]"
+    assert k is None or (k.shape[0] == n and k.shape[2] == D and k.dtype == q.dtype)
+    q_out = _alloc_out(q_out, (n, Hq, D), q.dtype, q.device)
+    k_out = None if k is None else _alloc_out(k_out, (n, Hkv, D), q.dtype, q.device)
+    assert q_out.dtype == q.dtype and (k is None or k_out.dtype == q.dtype)
+    sec = (ctypes.c_int32 * len(sections))(*[int(x) for x in sections])
+    _check("ris_rope_axes", lib().ris_rope_axes(
+        _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _dtype(q), n, Hq, Hkv, D, _token_stride(q, "q"),
+        0 if k is None else _token_stride(k, "k"), _ptr(positions), len(sections), sec, int(bool(interleaved)), int(n_ctx),
+        _ref(rope), int(bool(inverse)), _stream(stream)))
+    return q_out, k_out
+
+
+def ris_attention_packed(pack: Pack, q, k, v, out: Optional[torch.Tensor] = None, out_dtype=None, return_lse: bool = False,
+                         weight_rows: int = 0, stream=None):
+    """Causal attention over a pack's sequences, always a tuple: out [q_total, Hq, D], then lse [Hq, q_total]
+    (return_lse) and key_weight [Hkv, k_total] (weight_rows > 0). q, k, v may be views into a fused projection's rows."""
+    (n, Hq, D), (m, Hkv, _) = q.shape, k.shape
+    if n != pack.q_total or m != pack.k_total:
+        raise ValueError(f"q has {n} tokens and k {m}, the pack {pack.q_total} and {pack.k_total}")
+    assert k.shape == v.shape and k.shape[2] == D and q.dtype == k.dtype == v.dtype
+    out = _alloc_out(out, (n, Hq, D), out_dtype or q.dtype, q.device)
+    lse = torch.empty((Hq, n), dtype=torch.float32, device=q.device) if return_lse else None
+    kw = torch.empty((Hkv, m), dtype=torch.float32, device=q.device) if weight_rows > 0 else None
+    _check("ris_attention_packed", lib().ris_attention_packed(
+        pack.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), Hq, Hkv, D, _token_stride(q, "q"), _token_stride(k, "k"),
+        _token_stride(v, "v"), _dtype(q), _dtype(out), _ptr(lse), int(weight_rows), _ptr(kw), _stream(stream)))
+    return (out,) + ((lse,) if return_lse else ()) + ((kw,) if weight_rows > 0 else ())
+
+
+# ----------------------------------------------------------------------------- the 4-bit cache
+class _Cache4Desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("capacity", ctypes.c_int64)] + \
+               [(name, ctypes.c_void_p) for name in ("k", "v", "k_scale", "v_scale", "pos", "weight", "length", "sync")]
+
+
+class Cache4:
+    """A K/V cache held in 4 bits (ris_cache4): the tensors, which the caller may read and set, and their
+    descriptor. k, v uint8 [B, Hkv, capacity, D/2]; k_scale, v_scale bf16 [.., D/32]; pos int32 and weight fp32
+    [B, Hkv, capacity]; length int32 [B]."""
+
+    _TYPES = dict(k=torch.uint8, v=torch.uint8, k_scale=torch.bfloat16, v_scale=torch.bfloat16, pos=torch.int32,
+                  weight=torch.float32, length=torch.int32)
+
+    def __init__(self, k, v, k_scale, v_scale, pos, weight, length):
+        B, H, cap, half = k.shape
+        shapes = dict(k=(B, H, cap, half), v=(B, H, cap, half), k_scale=(B, H, cap, half // 16),
+                      v_scale=(B, H, cap, half // 16), pos=(B, H, cap), weight=(B, H, cap), length=(B,))
+        given = dict(k=k, v=v, k_scale=k_scale, v_scale=v_scale, pos=pos, weight=weight, length=length)
+        for name, x in given.items():
+            if x.dtype != self._TYPES[name] or tuple(x.shape) != shapes[name] or not x.is_contiguous() or not x.is_cuda:
+                raise ValueError(f"{name}: contiguous {self._TYPES[name]} {shapes[name]} on the GPU")
+            setattr(self, name, x)
+        self.batch, self.kv_heads, self.capacity, self.head_dim = B, H, cap, 2 * half
+        self.sync = torch.zeros(4, dtype=torch.int32, device=k.device)
+        self.desc = _Cache4Desc(B, H, 2 * half, 0, cap, *(getattr(self, n).data_ptr() for n in
+                                                          ("k", "v", "k_scale", "v_scale", "pos", "weight", "length", "sync")))
+
+    @classmethod
+    def empty(cls, batch: int, kv_heads: int, head_dim: int, capacity: int, device="cuda") -> "Cache4":
+        """A cache with no token in it; capacity is rounded up to a multiple of 16 slots."""
+        cap = (int(capacity) + 15) // 16 * 16
+
+        def z(*shape, dtype):
+            return torch.zeros(batch, *shape, dtype=dtype, device=device)
+
+        return cls(z(kv_heads, cap, head_dim // 2, dtype=torch.uint8), z(kv_heads, cap, head_dim // 2, dtype=torch.uint8),
+                   z(kv_heads, cap, head_dim // 32, dtype=torch.bfloat16), z(kv_heads, cap, head_dim // 32, dtype=torch.bfloat16),
+                   z(kv_heads, cap, dtype=torch.int32), z(kv_heads, cap, dtype=torch.float32), z(dtype=torch.int32))
+
+
+def ris_cache4_append(cache: Cache4, pack: Pack, k, v, positions: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                      start: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The pack's rows k, v [q_total, Hkv, D] into the cache, after the slots in use or at start [B] (int32)."""
+    n, H, D = k.shape
+    if n != pack.q_total or (H, D) != (cache.kv_heads, cache.head_dim):
+        raise ValueError(f"k is {tuple(k.shape)}, the pack has {pack.q_total} rows, the cache heads "
+                         f"{cache.kv_heads} x {cache.head_dim}")
+    assert k.shape == v.shape and k.dtype == v.dtype
+    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.numel() == n
+    if weight is not None:
+        assert weight.is_cuda and weight.is_contiguous() and weight.dtype == torch.float32 and tuple(weight.shape) == (H, n)
+    if start is not None:
+        assert start.is_cuda and start.is_contiguous() and start.dtype == torch.int32 and start.numel() == cache.batch
+    _check("ris_cache4_append", lib().ris_cache4_append(
+        ctypes.byref(cache.desc), pack.handle, _ptr(k), _ptr(v), _token_stride(k, "k"), _token_stride(v, "v"), _dtype(k),
+        _ptr(positions), _ptr(weight), _ptr(start), _stream(stream)))
+
+
+def ris_cache4_read(cache: Cache4, first: Optional[torch.Tensor] = None, count: Optional[int] = None, stream=None):
+    """The values of slots first[b] .. first[b] + count - 1 (zeros past the length): k, v fp32 [B, Hkv, count, D]."""
+    count = cache.capacity if count is None else int(count)
+    if first is not None:
+        assert first.is_cuda and first.is_contiguous() and first.dtype == torch.int32 and first.numel() == cache.batch
+    shape = (cache.batch, cache.kv_heads, count, cache.head_dim)
+    k, v = (torch.empty(shape, dtype=torch.float32, device=cache.k.device) for _ in range(2))
+    _check("ris_cache4_read", lib().ris_cache4_read(ctypes.byref(cache.desc), _ptr(first), count, _ptr(k), _ptr(v),
+                                                    _stream(stream)))
+    return k, v
+
+
+def ris_cache4_attend(cache: Cache4, q: torch.Tensor, out=None, out_dtype=None, return_lse: bool = False,
+                      weight_in: Optional[torch.Tensor] = None, weight_out: Optional[torch.Tensor] = None,
+                      longest: int = 0, stream=None):
+    """q [B, Hq, D], one token per sequence, over every slot in use: out [B, Hq, D] (and lse [B, Hq]).
+    weight_out [B, Hkv, capacity] gets weight_in (or 0) plus this token's weights; pass cache.weight as both to add up."""
+    B, Hq, D = q.shape
+    if (B, D) != (cache.batch, cache.head_dim):
+        raise ValueError(f"q is {tuple(q.shape)}, the cache has {cache.batch} sequences of head dim {cache.head_dim}")
+    assert q.is_cuda and q.is_contiguous()
+    out = _alloc_out(out, (B, Hq, D), out_dtype or q.dtype, q.device)
+    lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if return_lse else None
+    for w in (weight_in, weight_out):
+        if w is not None:
+            assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.shape == cache.weight.shape
+    _check("ris_cache4_attend", lib().ris_cache4_attend(
+        ctypes.byref(cache.desc), _ptr(q), Hq, _dtype(q), _dtype(out), int(longest), _ptr(out), _ptr(lse), _ptr(weight_in),
+        _ptr(weight_out), _stream(stream)))
+    return (out, lse) if return_lse else out
+
+
+def ris_cache4_evict(src: Cache4, dst: Cache4, budget: int, recent: int, kept: Optional[torch.Tensor] = None, stream=None):
+    """Cut src back to `budget` slots per sequence and head into dst (src itself: in place); returns the source
+    slots kept [B, Hkv, budget] (int32, -1 where there is none)."""
+    kept = _alloc_out(kept, (src.batch, src.kv_heads, int(budget)), torch.int32, src.k.device)
+    assert kept.dtype == torch.int32
+    _check("ris_cache4_evict", lib().ris_cache4_evict(ctypes.byref(src.desc), ctypes.byref(dst.desc), int(budget),
+                                                      int(recent), _ptr(kept), _stream(stream)))
+    return kept
