@@ -1,0 +1,1303 @@
+// Causal attention over packed prompts on the 5th-generation tensor cores, bf16 inputs.
+//
+// S = Q K^T with bf16 operands (exact products, fp32 sums), one online softmax per row over the keys j <= i +
+// k_len - q_len of its own sequence, O = P V with P as fp16 (11 bits; a bf16 P would add as much error
+// again as the bf16 output's own rounding) against the values as fp16 scaled by a power of two (a
+// bf16 value is exact there), the row's sum from the fp32 weights before they are rounded. The values
+// are converted by two passes over V ahead of the attention (its largest magnitude, then the values):
+// a few percent of a call at most, as V is read once per 128 rows of it anyway.
+//
+// A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two layouts:
+//   head dim 128  k_packed128, two CTAs of a cluster share every key and value tile, see there
+//   head dim 64   k_packed64, a CTA carries two row tiles at once, see there
+//
+// Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls
+// through to the end, TMEM is released and the CTA returns.
+//
+// Values that are not finite take a slow path (0 times an infinity is not 0, and a product over a tile
+// multiplies keys that a row does not see by 0): one warp per row over exactly the keys it sees.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <mutex>
+#include <type_traits>
+
+#include "attn_common.cuh"
+#include "serve.h"
+#include "tcgen05.cuh"
+
+namespace ris {
+
+// Device error word of this file (bit 1: a bounded wait gave up); read by read_packed_error.
+__device__ unsigned int g_ris_packed_error;
+
+namespace {
+
+using namespace tc;
+
+constexpr int BM = 128, BN = 128;  // query rows and keys of a tile
+static_assert(kPackRows == BM, "an item is a row tile");
+constexpr int kGroupWarps = 4;     // of a softmax group: one thread per row
+constexpr int kSoftmaxWarps = 2 * kGroupWarps;
+constexpr int kTmaWarp = kSoftmaxWarps, kScoreWarp = kSoftmaxWarps + 1, kValueWarp = kSoftmaxWarps + 2,
+              kRelayWarp = kSoftmaxWarps + 3;
+constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
+// registers per thread: at launch, then after setmaxnreg of a softmax and of a loader / MMA thread
+constexpr int kRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
+static_assert(2 * kSoftmaxRegs + kOtherRegs == 3 * kRegs, "the shares of the three warpgroups add up to the launch's");
+// The reference maximum of a row moves only when its maximum grows by more than this (log2), so P
+// stays below 2^8.
+constexpr float kLazyLog2 = 8.f;
+constexpr uint32_t kTmemCols = 512;
+
+// Exponent E of the values' scale 2^-E: the largest magnitude lands in [2^13, 2^14).
+__device__ __forceinline__ int value_exp(float vmax)
+{
+    return min(max((int)((__float_as_uint(vmax) >> 23) & 0xFF) - 127 - 13, -100), 114);
+}
+
+// kept keys of word e of a tile, as bits: those up to the row's last one (counted from the tile's start)
+__device__ __forceinline__ uint32_t causal_word(int last, int e)
+{
+    const int lim = min(31, max(-1, last - 32 * e));
+    return lim < 0 ? 0u : 0xFFFFFFFFu >> (31 - lim);
+}
+// x = -infinity unless the word has the bit: a predicated move
+__device__ __forceinline__ void drop_unless(float &x, uint32_t word, uint32_t bit)
+{
+    asm("{\n\t.reg .pred p;\n\t.reg .b32 t;\n\t"
+        "and.b32 t, %1, %2;\n\tsetp.eq.u32 p, t, 0;\n\t@p mov.b32 %0, 0xFF800000;\n\t}"
+        : "+f"(x)
+        : "r"(word), "r"(bit));
+}
+__device__ __forceinline__ float row_max(const float (&sv)[BN])
+{
+    float mx8[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        mx8[e] = fmaxf(sv[e], sv[e + 8]);
+#pragma unroll
+        for (int c = 16; c < BN; c += 16) mx8[e] = fmax3(mx8[e], sv[c + e], sv[c + 8 + e]);
+    }
+    return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
+}
+// P = 2^(s sc - mu) as fp16, two keys to a word, and the sum of the weights before they are rounded
+__device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, float mu, uint32_t (&hw)[BN / 2])
+{
+    const uint64_t sc2 = f2_pack(sc, sc), nmu2 = f2_pack(-mu, -mu);
+    uint64_t sum[2] = {0, 0};
+#pragma unroll
+    for (int w = 0; w < BN / 2; ++w) {
+        float x0, x1;
+        f2_unpack(f2_fma(f2_pack(sv[2 * w], sv[2 * w + 1]), sc2, nmu2), x0, x1);
+        x0 = ex2(x0);
+        x1 = ex2(x1);
+        const __half2 hp = __floats2half2_rn(x0, x1);
+        sum[w & 1] = f2_add(sum[w & 1], f2_pack(x0, x1));
+        hw[w] = *reinterpret_cast<const uint32_t *>(&hp);
+    }
+    float a, b;
+    f2_unpack(f2_add(sum[0], sum[1]), a, b);
+    return a + b;
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+// 16 bytes of outputs (four fp32 or eight bf16 values)
+template <typename TOut>
+__device__ __forceinline__ void store16(void *dst, const float *x)
+{
+    if constexpr (sizeof(TOut) == 4)
+        *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+    else
+        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// A row's softmax as the other outputs: log-sum-exp, and (maximum, 1 / sum) for the key weights.
+__device__ __forceinline__ void store_row(const PackedArgs &a, int h, int64_t row, float m, float l)
+{
+    if (a.lse != nullptr) a.lse[h * a.q_total + row] = (m + log2f(l)) * kLn2;
+    if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l);
+}
+
+// The slow path: rows row .. row + BM - 1 of the item, warp `warp` of `warps` taking every warps-th, over the keys that each sees.
+template <int DT, typename TOut>
+__device__ __noinline__ void rows_one_by_one(const PackedArgs &a, const PackItem &it, int row, int h, int warp, int warps)
+{
+    constexpr int C = DT / 32;
+    const int lane = threadIdx.x & 31, g = h / a.G;
+    const __nv_bfloat16 *k = reinterpret_cast<const __nv_bfloat16 *>(a.k) + (int64_t)it.k_base * a.k_stride + g * DT;
+    const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(a.v) + (int64_t)it.k_base * a.v_stride + g * DT;
+    for (int i = row + warp; i < min(row + BM, it.q_len); i += warps) {
+        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) + (int64_t)(it.q_base + i) * a.q_stride + h * DT;
+        const int n = min(it.k_len, i + it.k_len - it.q_len + 1);
+        float m = -INFINITY, l = 0.f, o[C] = {};
+        for (int j0 = 0; j0 < n; j0 += 32) {
+            const int j = j0 + lane;
+            float s = -INFINITY;
+            if (j < n) {
+                s = 0.f;
+                for (int d = 0; d < DT; ++d) s = fmaf(__bfloat162float(q[d]), __bfloat162float(k[j * a.k_stride + d]), s);
+                s *= a.scale_log2;
+            }
+            const float nm = fmaxf(m, warp_max(s)), ref = nm == -INFINITY ? 0.f : nm;
+            const float p = exp2f(s - ref), al = exp2f(m - ref);
+            m = nm;
+            l = fmaf(l, al, warp_sum(j < n ? p : 0.f));
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] *= al;
+            for (int e = 0; e < min(32, n - j0); ++e) {
+                const float pe = __shfl_sync(0xFFFFFFFFu, p, e);
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[c] = fmaf(pe, __bfloat162float(v[(j0 + e) * a.v_stride + lane + 32 * c]), o[c]);
+            }
+        }
+        const int64_t r = it.q_base + i;
+        TOut *out = reinterpret_cast<TOut *>(a.out) + (r * a.Hq + h) * DT;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const float x = l == 0.f ? 0.f : o[c] / l;
+            if constexpr (sizeof(TOut) == 4)
+                out[lane + 32 * c] = x;
+            else
+                out[lane + 32 * c] = __float2bfloat16_rn(x);
+        }
+        if (lane == 0) store_row(a, h, r, m, l);
+    }
+}
+
+struct PackedMaps {
+    CUtensorMap q, k, v;
+};
+
+// O of 32 rows (a warp's) x OC columns from column c_from on of TMEM at t_o, normalised, through the
+// warp's part of shared memory so that neighbouring lanes store neighbouring pieces of a row; 16-byte
+// pieces swizzled by the row. Rows with no weight (inv 0) become zeros whatever the columns hold.
+template <int OC, typename TOut>
+__device__ __forceinline__ void store_out(unsigned char *stage, uint32_t t_o, float inv, TOut *out, int64_t pitch, int rows)
+{
+    constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;  // bytes and pieces of a row's part
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c0 = 0; c0 < OC; c0 += 32) {
+        float ov[32];
+        tmem_ld32(t_o + c0, ov);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) ov[c] = inv == 0.f ? 0.f : ov[c] * inv;
+#pragma unroll
+        for (int e = 0; e < 32 * (int)sizeof(TOut) / 16; ++e) {
+            const int piece = c0 * (int)sizeof(TOut) / 16 + e;
+            store16<TOut>(stage + lane * RB + ((piece ^ (lane & (NP - 1))) << 4), ov + e * (16 / (int)sizeof(TOut)));
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < NP; ++e) {
+        const int rr = e * (32 / NP) + lane / NP, piece = lane & (NP - 1);
+        const uint4 x = *reinterpret_cast<const uint4 *>(stage + rr * RB + ((piece ^ (rr & (NP - 1))) << 4));
+        if (rr < rows) *reinterpret_cast<uint4 *>(out + rr * pitch + piece * (16 / (int)sizeof(TOut))) = x;
+    }
+    __syncwarp();
+}
+
+// What the warps of a cluster leave in each of its CTAs for the end of the kernel.
+struct ClosingNotes {
+    uint32_t bad;        // a wait gave up in either CTA
+    uint32_t scored;     // tiles whose score products were issued and committed
+    uint32_t valued;     // tiles whose value products were
+    uint32_t keys[2], values[2];  // tiles whose keys / values each CTA requested (in the first CTA)
+};
+
+// ---------------------------------------------------------------- head dim 128
+// Shared memory (bytes, from a 1024-aligned base).
+struct Lay128 {
+    static constexpr int DT = 128, NSK = 4, NSV = 4;  // stages of the key and of the value ring
+    static constexpr int KROWS = BN / 2;           // keys of a tile held by one CTA
+    static constexpr int K_BLK = KROWS * 128;      // one 64-column block
+    static constexpr int K_STAGE = 2 * K_BLK;
+    static constexpr int V_STAGE = BN * 128;       // 64 of the 128 value columns
+    static constexpr int Q_BLK = BM * 128;
+    static constexpr int OFF_K = 0;
+    static constexpr int OFF_V = NSK * K_STAGE;
+    static constexpr int OFF_Q = OFF_V + NSV * V_STAGE;
+    static constexpr int OFF_BARS = OFF_Q + 2 * Q_BLK;
+    static constexpr int OFF_TMEM = OFF_BARS + 224;  // after the barriers
+    static constexpr int OFF_END = OFF_TMEM + 4;     // ClosingNotes
+    static constexpr int OFF_M = OFF_BARS + 256;     // float [BM]
+    static constexpr int OFF_ML = OFF_M + BM * 4;    // float2 [2][BM]
+    static constexpr int BYTES = OFF_ML + 2 * BM * 8;
+    static_assert(BYTES <= 232448 && OFF_END + (int)sizeof(ClosingNotes) <= OFF_M, "shared memory of a CTA");
+    // Barriers, one of each kind per ring stage or buffer, so that no waiter can fall two phases behind a
+    // barrier it polls by parity:
+    //   Q_FULL          the query tiles have landed (relayed with the first keys)
+    //   K_FULL, V_FULL  a tile's keys / values have landed (relayed to S_GO / P_GO)
+    //   S_GO            the score products of a tile may start: its keys have landed and the scores
+    //                   of the tile two before (if any) have been read out of their buffer
+    //   S_FULL          they are done (and the key stage is free)
+    //   P_GO            the value product may start: P is written and the values have landed
+    //   PV_DONE         it is done (P's buffer and the value stage are free, O has settled)
+    // S_FULL and PV_DONE of each CTA get the products' completion. The others are used in the
+    // cluster's first CTA, whose warps issue the products: the loaders of both CTAs announce
+    // their copies there and the copies complete there, and the softmax warps of both arrive there.
+    static constexpr int B_Q_FULL = 0, B_K_FULL = 1, B_S_GO = B_K_FULL + NSK, B_S_FULL = B_S_GO + NSK,
+                         B_V_FULL = B_S_FULL + NSK, B_P_GO = B_V_FULL + NSV, B_PV_DONE = B_P_GO + NSV,
+                         NBAR = B_PV_DONE + NSV;
+    static_assert(NBAR * 8 <= 224 && NBAR <= 32, "barriers below the TMEM base word, a lane each");
+};
+
+// Two CTAs of a cluster share their key and value tiles (tcgen05 cta_group::2, one 256 x 128 product over
+// both SMs, each holding half of the B operand: 64 of a tile's keys, 64 of the value columns): two heads of a
+// KV group on the same 128 rows or, where a group has an odd number of heads, two consecutive row
+// tiles of a head. That halves what an SM reads of shared memory per product, which one CTA alone
+// would need all of (128 B a clock), and the L2 traffic of the tiles.
+//
+//   warp 8 (TMA)    loads the query tile, then streams 128-key tiles of the keys and of the values
+//                   into two rings, each CTA its half;
+//   warp 11 (relay) (first CTA) passes what has landed on to the barriers of the issuing warps;
+//   warps 9, 10     (first CTA) issue tcgen05.mma: the score tile S into a double-buffered TMEM score
+//                   tile, and O += P V (A = P in TMEM, double-buffered) into the TMEM output tile;
+//   warps 0-7       two groups of four warps, one thread per row in each, on alternate key tiles:
+//                   scores from TMEM, causal cut (only where a warp's rows end inside the tile), maximum, fp32 online
+//                   softmax from the reference maximum that the other group hands over, O rescaled in
+//                   TMEM only when the maximum grew by more than 2^8, P into TMEM.
+// TMEM: S 2 x 128 columns, O 128, P 2 x 64: all 512.
+//
+// Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles.
+template <typename TOut>
+__global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+{
+    using L = Lay128;
+    constexpr int NSK = L::NSK, NSV = L::NSV, DT = 128;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    uint64_t *const bars = reinterpret_cast<uint64_t *>(smem + L::OFF_BARS);
+    uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
+    float *const m_sh = reinterpret_cast<float *>(smem + L::OFF_M);
+    float2(*const ml_sh)[BM] = reinterpret_cast<float2(*)[BM]>(smem + L::OFF_ML);
+    volatile ClosingNotes *const notes = reinterpret_cast<ClosingNotes *>(smem + L::OFF_END);
+    const uint32_t sbase = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned int *const gave_up = &g_ris_packed_error;
+
+    // ---- the cluster's item: with an even group 128 rows of two heads, else 256 rows of one (rank 1 the second half,
+    // which may hold no rows)
+    const int rank = (int)(blockIdx.x & 1);
+    const bool head_pair = (a.G & 1) == 0;
+    const unsigned n_h = (unsigned)(head_pair ? a.Hq / 2 : a.Hq), c = blockIdx.x / 2, r2 = c / n_h;
+    const int h = head_pair ? 2 * (int)(c - r2 * n_h) + rank : (int)(c - r2 * n_h);
+    const PackItem it = a.items[r2];
+    const int q0 = it.row + (head_pair ? 0 : rank * BM);  // first row of this CTA, in its sequence
+    const int g = h / a.G, shift = it.k_len - it.q_len;
+    // keys that the last of the cluster's rows sees
+    const int n_keys = max(0, min(it.k_len, min(it.q_len, it.row + (head_pair ? BM : 2 * BM)) + shift));
+    const int n_kt = (n_keys + BN - 1) / BN;
+
+    constexpr auto BAR = [](int i) { return (uint32_t)(L::OFF_BARS + 8 * i); };
+    const bool first_loads = (sbase & 1023u) == 0u && n_kt > 0;
+    if (warp == kTmaWarp) {
+        if (lane < L::NBAR) {
+            // S_GO, P_GO: the group's warps of each CTA and the relay; S_FULL, PV_DONE: the commit; the
+            // copies' barriers: the loader of each CTA
+            const bool go = (lane >= L::B_S_GO && lane < L::B_S_GO + NSK) || (lane >= L::B_P_GO && lane < L::B_P_GO + NSV);
+            const bool done = (lane >= L::B_S_FULL && lane < L::B_S_FULL + NSK) || lane >= L::B_PV_DONE;
+            mbar_init(smem_u32(&bars[lane]), go ? kGroupWarps * 2 + 1 : done ? 1 : 2);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        if (lane < (int)(sizeof(ClosingNotes) / 4)) reinterpret_cast<volatile uint32_t *>(smem + L::OFF_END)[lane] = 0u;
+        __syncwarp();
+        cluster_sync();  // the barriers of both CTAs are initialised once this is passed
+        // the query tile and the first keys at once, under the rest of the start-up
+        if (lane == 0 && first_loads) {
+            const uint32_t lead = cluster_addr(sbase, 0);
+            const uint32_t bq = lead + BAR(L::B_Q_FULL), bk = lead + BAR(L::B_K_FULL);
+            const int key = it.k_base + L::KROWS * rank, row = it.q_base + q0;
+            mbar_arrive_expect_tx<2>(bq, 2 * L::Q_BLK);
+            mbar_arrive_expect_tx<2>(bk, L::K_STAGE);
+            for (int blk = 0; blk < 2; ++blk) {
+                tma_load_3d<2>(sbase + L::OFF_Q + blk * L::Q_BLK, &maps.q, 64 * blk, h, row, bq);
+                tma_load_3d<2>(sbase + L::OFF_K + blk * L::K_BLK, &maps.k, 64 * blk, g, key, bk);
+            }
+        }
+    } else {
+        cluster_arrive();
+        if (warp == kScoreWarp) tmem_alloc<2, kTmemCols>(smem_u32(&tmem_base_sh));  // by one full warp (of each CTA)
+        cluster_wait();
+    }
+    const uint32_t lead = cluster_addr(sbase, 0);  // the issuing CTA's shared memory
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    // all 512 columns: the allocation starts at TMEM address 0, so every address below is a
+    // constant (anything else ends the CTA as a failed wait does, below)
+    constexpr uint32_t T_S0 = 0, T_O = T_S0 + 2 * BN, T_P0 = T_O + DT;
+    static_assert(T_P0 + BN <= kTmemCols, "TMEM columns");
+    const uint32_t tmem = tmem_base_sh;
+    auto arrive_lead = [&](int bar) { mbar_arrive_cluster(lead + BAR(bar)); };
+    bool ok = tmem == 0u && (sbase & 1023u) == 0u;  // (the swizzled boxes need the alignment)
+
+    if (warp >= kSoftmaxWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+    if (warp == kTmaWarp) {
+        // =============================== TMA producer
+        if (lane == 0 && first_loads) {
+            // (The query tile and the first keys were requested above.) Keys of tile j once the score
+            // products of tile j - NSK are done, values of tile j once the value product of tile j - NSV is: the loader
+            // waits on the barriers that announce those products (S_FULL, PV_DONE). The score
+            // products of tile t + 1 finish before the value product of tile t, so in this order no
+            // wait holds up a load that could go before it.
+            int nk = 1, nv = 0;  // tiles whose keys / values were requested
+            auto load_k = [&](int j) -> bool {
+                if (j >= n_kt) return true;
+                const int st = j % NSK;
+                if (j >= NSK && !mbar_wait<2>(sbase + BAR(L::B_S_FULL + st), (j / NSK - 1) & 1, gave_up)) return false;
+                const uint32_t bk = lead + BAR(L::B_K_FULL + st);
+                const uint32_t dk = sbase + L::OFF_K + st * L::K_STAGE;
+                mbar_arrive_expect_tx<2>(bk, L::K_STAGE);
+                for (int blk = 0; blk < 2; ++blk)
+                    tma_load_3d<2>(dk + blk * L::K_BLK, &maps.k, 64 * blk, g, it.k_base + j * BN + L::KROWS * rank, bk);
+                nk = j + 1;
+                return true;
+            };
+            auto load_v = [&](int j) -> bool {
+                if (j >= n_kt) return true;
+                const int st = j % NSV;
+                if (j >= NSV && !mbar_wait<2>(sbase + BAR(L::B_PV_DONE + st), (j / NSV - 1) & 1, gave_up)) return false;
+                const uint32_t bv = lead + BAR(L::B_V_FULL + st);
+                mbar_arrive_expect_tx<2>(bv, L::V_STAGE);
+                tma_load_3d<2>(sbase + L::OFF_V + st * L::V_STAGE, &maps.v, 64 * rank, g, it.k_base + j * BN, bv);
+                nv = j + 1;
+                return true;
+            };
+            ok = ok && load_v(0) && load_k(1) && load_v(1) && load_k(2) && load_v(2) && load_k(3) && load_v(3) && load_k(4);
+            for (int t = 0; t < n_kt && ok; ++t) ok = load_k(t + 5) && load_v(t + 4);
+            // (that the copies requested last have landed before a CTA leaves: see the end)
+            st_cluster(sbase + L::OFF_END + offsetof(ClosingNotes, keys) + 4 * rank, 0, (uint32_t)nk);
+            st_cluster(sbase + L::OFF_END + offsetof(ClosingNotes, values) + 4 * rank, 0, (uint32_t)nv);
+            static_assert(NSK == 4 && NSV == 4, "the order of the loads and of the relay");
+        }
+    } else if (!ok || rank != 0) {
+        // an unexpected base: straight to the common end; and the second CTA has nothing to issue
+    } else if (warp == kRelayWarp) {
+        // =============================== relay: what has landed, to the barriers that the issuing
+        // warps wait on, in the order of the loads; so each of them waits on one barrier per tile
+        if (lane == 0 && n_kt > 0) {
+            auto relay_k = [&](int j) -> bool {
+                if (j >= n_kt) return true;
+                if (!mbar_wait<2>(sbase + BAR(L::B_K_FULL + j % NSK), (j / NSK) & 1, gave_up)) return false;
+                mbar_arrive(sbase + BAR(L::B_S_GO + j % NSK));
+                return true;
+            };
+            auto relay_v = [&](int j) -> bool {
+                if (j >= n_kt) return true;
+                if (!mbar_wait<2>(sbase + BAR(L::B_V_FULL + j % NSV), (j / NSV) & 1, gave_up)) return false;
+                mbar_arrive(sbase + BAR(L::B_P_GO + j % NSV));
+                return true;
+            };
+            ok = mbar_wait<2>(sbase + BAR(L::B_Q_FULL), 0, gave_up) && relay_k(0) && relay_v(0) && relay_k(1) && relay_v(1) &&
+                 relay_k(2) && relay_v(2) && relay_k(3) && relay_v(3) && relay_k(4);
+            for (int t = 0; t < n_kt && ok; ++t) ok = relay_k(t + 5) && relay_v(t + 4);
+        }
+    } else {
+        // =============================== product issuers (of the cluster's first CTA, for both): one
+        // warp for the scores, one for the value products. The whole warp runs this code, so that every operand
+        // is warp-uniform, and one elected lane issues.
+        constexpr uint32_t ID_S = idesc_bf16(2 * BM, BN, false);  // S[128 x 128] = Q K^T, both K-major
+        constexpr uint32_t ID_O = idesc_f16(2 * BM, DT, true);    // O[128 x 128] += P V, fp16, V MN-major
+        // score products of a tile of ring stage ST: a k-step of 16 columns 32 B further in a 128 B row
+        auto issue_s = [&](auto st_c) {
+            constexpr int ST = decltype(st_c)::value;
+            const uint32_t kd = desc_lo(sbase + L::OFF_K + ST * L::K_STAGE, 16);
+            const uint32_t qd = desc_lo(sbase + L::OFF_Q, 16);
+            constexpr uint32_t dt = T_S0 + (ST & 1) * BN;
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < DT / 16; ++ks)
+                    tc_mma_ss<2>(dt, qd + dstep((ks >> 2) * L::Q_BLK + (ks & 3) * 32), kd + dstep((ks >> 2) * L::K_BLK + (ks & 3) * 32), ID_S,
+                                 ks > 0);
+                tc_commit<2>(sbase + BAR(L::B_S_FULL + ST));
+            }
+            __syncwarp();
+        };
+        // value product of a tile of ring stage ST: P (in TMEM, the buffer of the tile's parity), 128
+        // keys packed two per column, times V, 128 keys x 128 B rows: 16 keys = two 8-row atoms (SBO 1024)
+        auto issue_o = [&](auto st_c, uint32_t acc) {
+            constexpr int ST = decltype(st_c)::value;
+            const uint32_t vd = desc_lo(sbase + L::OFF_V + ST * L::V_STAGE, L::V_STAGE);
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < BN / 16; ++ks)
+                    tc_mma_ts<2>(T_O, T_P0 + (ST & 1) * (BN / 2) + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 ? 1u : acc);
+                tc_commit<2>(sbase + BAR(L::B_PV_DONE + ST));
+            }
+            __syncwarp();
+        };
+        auto wait_all = [&](int bar, int parity) -> bool {
+            const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<2>(sbase + BAR(bar), parity, gave_up));
+            tc_fence_after();
+            return got;
+        };
+        int issued = 0;  // tiles whose products this warp committed
+        auto score_step = [&](auto st_c, int j) {
+            if (!ok || j >= n_kt) return;
+            ok = wait_all(L::B_S_GO + decltype(st_c)::value, (j / NSK) & 1);
+            if (!ok) return;
+            issue_s(st_c);
+            issued = j + 1;
+        };
+        auto value_step = [&](auto st_c, int j) {
+            if (!ok || j >= n_kt) return;
+            ok = wait_all(L::B_P_GO + decltype(st_c)::value, (j / NSV) & 1);
+            if (!ok) return;
+            issue_o(st_c, j > 0 ? 1u : 0u);
+            issued = j + 1;
+        };
+        using I0 = std::integral_constant<int, 0>;
+        using I1 = std::integral_constant<int, 1>;
+        using I2 = std::integral_constant<int, 2>;
+        using I3 = std::integral_constant<int, 3>;
+        if (warp == kScoreWarp) {
+            for (int j = 0; j < n_kt && ok; j += 4) {
+                score_step(I0{}, j);
+                score_step(I1{}, j + 1);
+                score_step(I2{}, j + 2);
+                score_step(I3{}, j + 3);
+            }
+        } else {
+            for (int j = 0; j < n_kt && ok; j += 4) {
+                value_step(I0{}, j);
+                value_step(I1{}, j + 1);
+                value_step(I2{}, j + 2);
+                value_step(I3{}, j + 3);
+            }
+        }
+        if (lane < 2) {
+            const int off = L::OFF_END + (warp == kValueWarp ? offsetof(ClosingNotes, valued) : offsetof(ClosingNotes, scored));
+            st_cluster(sbase + off, lane, (uint32_t)issued);
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        // =============================== softmax: group grp of four warps takes the tiles of parity
+        // grp, one thread per row q0 + r; at the end a thread owns half of its row's columns
+        constexpr int OC = DT / 2;
+        const int wq = warp & 3, grp = warp >> 2;
+        const int r = wq * 32 + lane;  // TMEM lane
+        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        const float sc = a.scale_log2, v_absmax = *a.v_absmax;
+        // the group's score buffer is free for its first tile
+        if (lane == 0 && grp < n_kt) arrive_lead(L::B_S_GO + grp);
+        const int last_key = q0 + r + shift;          // last key that the row sees
+        const int warp_sees = q0 + wq * 32 + shift;   // that every row of the warp sees (and those past the sequence's end)
+        float l = 0.f, m_own = -INFINITY;  // row sum over this thread's tiles, relative to 2^m_own
+        bool s_full = false;  // seen at the end of the last tile: a poll takes 200 cycles even if it succeeds
+        for (int j = grp; j < n_kt; j += 2) {
+            if (ok) {
+                const uint32_t bar = sbase + BAR(L::B_S_FULL + j % NSK);
+                ok = __all_sync(0xFFFFFFFFu, s_full || mbar_wait<2, true>(bar, (j / NSK) & 1, gave_up));
+            }
+            tc_fence_after();
+            uint32_t su[2][64];
+            tmem_issue64(T_S0 + grp * BN + lane_off, su[0]);
+            tmem_issue64(T_S0 + grp * BN + lane_off + 64, su[1]);
+            tmem_wait_ld();
+            pin64(su[0]);
+            pin64(su[1]);
+            tc_fence_before();
+            __syncwarp();
+            tc_fence_before();
+            if (lane == 0 && j + 2 < n_kt) arrive_lead(L::B_S_GO + (j + 2) % NSK);
+            float sv[BN];
+#pragma unroll
+            for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
+            if (warp_sees < j * BN + BN - 1) {
+                uint32_t cw[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cw[e] = causal_word(last_key - j * BN, e);
+#pragma unroll
+                for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
+            }
+            const float mx = row_max(sv) * sc;  // (the scale is positive)
+            // The row's reference maximum moves on from tile to tile, handed to the other group. It moves, and
+            // O is rescaled, only when the row max grows by more than kLazyLog2. The TMEM loads / stores are
+            // warp-collective, so the whole warp runs them when any of its rows needs it.
+            float m_prev = -INFINITY;
+            if (j > 0) {
+                pair_sync(1 + 2 * wq + (grp ^ 1));
+                m_prev = m_sh[r];
+            }
+            const bool upd = mx > m_prev + kLazyLog2;
+            const float m_ref = upd ? mx : m_prev;
+            // the value product of tile t is done (t < 0: nothing to wait for)
+            auto pv_done = [&](int t) -> bool {
+                const uint32_t bar = sbase + BAR(L::B_PV_DONE + t % NSV);
+                return t < 0 || __all_sync(0xFFFFFFFFu, mbar_wait<2, true>(bar, (t / NSV) & 1, gave_up));
+            };
+            const bool scale_o = upd && m_prev != -INFINITY;
+            const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
+            const float al = scale_o ? exp2f(m_prev - m_ref) : 1.f;
+            if (m_ref != m_own) {
+                l *= m_own == -INFINITY ? 0.f : exp2f(m_own - m_ref);
+                m_own = m_ref;
+            }
+            uint32_t hw[BN / 2];
+            const float lsum = weights_of(sv, sc, m_ref == -INFINITY ? 0.f : m_ref, hw);
+            // Only now on to the other group: its exponentials (the other warp of this scheduler) run
+            // while this warp stores P and takes the next tile's scores and maximum, and not
+            // against this warp's own
+            if (j + 1 < n_kt) {
+                m_sh[r] = m_ref;
+                __threadfence_block();
+                pair_arrive(1 + 2 * wq + grp);
+            }
+            if (!ok) continue;
+            ok = pv_done(j - 2);  // P's buffer is free
+            if (!ok) continue;
+            tc_fence_after();
+            if (any_scale) {
+                // O has settled once the value product of tile j - 1 is done (that of tile j - 2 first,
+                // above, so that the barrier is not polled a phase early); nothing adds to it before
+                // this warp's P is announced below, and the other group's warp of these rows scales it next
+                // only after that product.
+                ok = pv_done(j - 1);
+                if (!ok) continue;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c0 = 0; c0 < DT; c0 += 32) {
+                    float ov[32];
+                    uint32_t ow[32];
+                    tmem_ld32(T_O + lane_off + c0, ov);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) ow[e] = __float_as_uint(ov[e] * al);
+                    tmem_st32(T_O + lane_off + c0, ow);
+                }
+                tmem_wait_st();
+            }
+            const uint32_t tp = T_P0 + grp * (BN / 2) + lane_off;
+            tmem_st32(tp, hw);
+            tmem_st32(tp + 32, hw + 32);
+            s_full = j + 2 < n_kt && mbar_test<2, true>(sbase + BAR(L::B_S_FULL + (j + 2) % NSK), ((j + 2) / NSK) & 1);
+            l += lsum;
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            tc_fence_before();
+            if (lane == 0) arrive_lead(L::B_P_GO + j % NSV);
+        }
+        // the row's maximum and sum from both threads
+        ml_sh[grp][r] = make_float2(m_own, l);
+        ok = !pair_or(9 + wq, !ok);
+        for (int t = max(0, n_kt - 2); t < n_kt && ok; ++t)  // in order, as above
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait<2>(sbase + BAR(L::B_PV_DONE + t % NSV), (t / NSV) & 1, gave_up));
+        if (ok) {
+            tc_fence_after();
+            const float2 ma = ml_sh[0][r], mb = ml_sh[1][r];
+            // the group of the last tile holds the final maximum; a group without tiles has l = 0
+            const float m_fin = n_kt == 0 ? -INFINITY : ((n_kt - 1) & 1) ? mb.x : ma.x;
+            const float lt = (ma.x == m_fin ? ma.y : ma.y * exp2f(ma.x - m_fin)) +
+                             (mb.x == m_fin ? mb.y : mb.y * exp2f(mb.x - m_fin));
+            // fp16 values were scaled by 2^-E for the value product
+            if (v_absmax < INFINITY) {
+                const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / lt;
+                const int w0 = q0 + 32 * wq;  // the warp's first row
+                TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT + OC * grp;
+                store_out<OC, TOut>(smem + warp * (32 * OC * (int)sizeof(TOut)), T_O + lane_off + OC * grp, inv, out,
+                                    (int64_t)a.Hq * DT, it.q_len - w0);
+                if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin, lt);
+            } else {
+                rows_one_by_one<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps);
+            }
+        }
+    }
+
+    if (!ok) {
+        atomicOr(&g_ris_packed_error, 2u);
+        for (int x = 0; x < 2; ++x) st_cluster(sbase + L::OFF_END + offsetof(ClosingNotes, bad), x, 1u);
+    }
+    __syncwarp();
+    tc_fence_before();
+    // Neither CTA of a cluster may leave, or release TMEM, while a product is running or anything can
+    // still reach its shared memory. The softmax warps of each CTA have seen, in their own
+    // barriers, every commit (S_FULL of every tile, PV_DONE of every tile), and so the end of every copy:
+    // nothing is under way unless a wait gave up. Then the copies and commits still to come, as the
+    // loaders and the issuing warps counted them, are waited for before both CTAs leave. (What one
+    // loader requested and the other did not is announced here in its place.)
+    cluster_sync();
+    __syncthreads();
+    tc_fence_after();
+    if (notes->bad != 0u) {
+        if (warp == kTmaWarp && lane == 0) {
+            auto landed = [&](int bar, int stages, int n0, int n1) {
+                const int n = max(n0, n1);
+                for (int j = max(0, n - stages); j < n; ++j) {
+                    if (j >= min(n0, n1)) mbar_arrive(sbase + BAR(bar + j % stages));
+                    mbar_wait_own<2>(sbase + BAR(bar + j % stages), (j / stages) & 1);
+                }
+            };
+            if (rank == 0) {
+                if (notes->keys[0] > 0u) mbar_wait_own<2>(sbase + BAR(L::B_Q_FULL), 0);
+                landed(L::B_K_FULL, NSK, (int)notes->keys[0], (int)notes->keys[1]);
+                landed(L::B_V_FULL, NSV, (int)notes->values[0], (int)notes->values[1]);
+            }
+            const int ns = (int)notes->scored, nv = (int)notes->valued;
+            for (int j = max(0, ns - NSK); j < ns; ++j) mbar_wait_own<2>(sbase + BAR(L::B_S_FULL + j % NSK), (j / NSK) & 1);
+            for (int j = max(0, nv - NSV); j < nv; ++j) mbar_wait_own<2>(sbase + BAR(L::B_PV_DONE + j % NSV), (j / NSV) & 1);
+        }
+        __syncwarp();
+        cluster_sync();
+        __syncthreads();
+        tc_fence_after();
+    }
+    if (warp == kScoreWarp) tmem_dealloc<2, kTmemCols>(tmem);
+}
+
+// ---------------------------------------------------------------- head dim 64
+struct Lay64 {
+    static constexpr int DT = 64, NSK = 4, NSV = 4;
+    static constexpr int TILE = 128 * 128;  // 128 rows or keys of 64 16-bit values
+    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_BARS = OFF_Q + 2 * TILE;
+    static constexpr int OFF_TMEM = OFF_BARS + 256, BYTES = OFF_TMEM + 16;
+    // Barriers, of a stage:
+    //   K_FULL, V_FULL    its keys / values have landed
+    //   K_FREE, V_FREE    the products that read it are done
+    // and of a row tile t, one phase per key tile:
+    //   S_GO    its scores have been read out of their buffer
+    //   S_FULL  they are there
+    //   P_GO    P is written (and O rescaled where needed)
+    //   PV_DONE O has settled, P's buffer is free
+    static constexpr int B_Q_FULL = 0, B_K_FULL = 1, B_V_FULL = B_K_FULL + NSK, B_K_FREE = B_V_FULL + NSV, B_V_FREE = B_K_FREE + NSK,
+                         B_S_GO = B_V_FREE + NSV, B_S_FULL = B_S_GO + 2, B_P_GO = B_S_FULL + 2, B_PV_DONE = B_P_GO + 2,
+                         NBAR = B_PV_DONE + 2;
+    static_assert(NBAR <= 32 && BYTES <= 232448, "a lane per barrier; shared memory of a CTA");
+};
+
+// One CTA carries two row tiles over the same key tiles: two heads of a KV group on the same 128 rows or, where a
+// group has an odd number of heads, 256 rows of a head. Each softmax group owns one of them, so neither waits for
+// the other: at head dim 64 a key tile takes 512 cycles of the tensor pipe per row tile and its 16,384
+// exponentials as long or longer, and the softmax is what has to be kept busy. (Two groups on
+// alternate tiles of one row tile pass the reference maximum from hand to hand, one tile's exponentials after the other's.)
+//
+//   warp 8 (TMA)  both query tiles, then key and value tiles into two rings;
+//   warp 9        scores S_t = Q_t K^T of both row tiles, each as soon as its group has read the last ones;
+//   warp 10       O_t += P_t V;
+//   warps 0-3, 4-7  the softmax of row tile 0, 1: one thread per row.
+// TMEM: S 2 x 128 columns, P 2 x 64, O 2 x 64: all 512. P has columns of its own, so the next scores are computed
+// under the exponentials.
+template <typename TOut>
+__global__ void __launch_bounds__(kThreads, 1) k_packed64(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+{
+    using L = Lay64;
+    constexpr int NSK = L::NSK, NSV = L::NSV, DT = 64, TILE = L::TILE;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
+    const uint32_t sbase = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned int *const gave_up = &g_ris_packed_error;
+    const bool head_pair = (a.G & 1) == 0;
+    const unsigned n_h = (unsigned)(head_pair ? a.Hq / 2 : a.Hq), r2 = blockIdx.x / n_h;
+    const int h0 = (int)(blockIdx.x - r2 * n_h) * (head_pair ? 2 : 1);
+    const PackItem it = a.items[r2];
+    const int g = h0 / a.G, shift = it.k_len - it.q_len;
+    // first row and key tiles of row tile t (a second half without rows has none)
+    auto row_of = [&](int t) { return it.row + (head_pair ? 0 : t * BM); };
+    auto tiles_of = [&](int t) {
+        const int q0 = row_of(t), keys = q0 < it.q_len ? max(0, min(it.k_len, min(it.q_len, q0 + BM) + shift)) : 0;
+        return (keys + BN - 1) / BN;
+    };
+    const int n0 = tiles_of(0), n1 = tiles_of(1), n_kt = max(n0, n1);
+    auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
+
+    if (warp == kTmaWarp) {
+        if (lane < L::NBAR) {
+            const bool by_group = (lane >= L::B_S_GO && lane < L::B_S_GO + 2) || (lane >= L::B_P_GO && lane < L::B_P_GO + 2);
+            mbar_init(bar(lane), by_group ? kGroupWarps : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+    } else if (warp == kScoreWarp) {
+        tmem_alloc<1, kTmemCols>(smem_u32(&tmem_base_sh));
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    constexpr uint32_t T_S = 0, T_P = T_S + 2 * BN, T_O = T_P + BN;
+    static_assert(T_O + 2 * DT <= kTmemCols, "TMEM columns");
+    const uint32_t tmem = tmem_base_sh;
+    bool ok = tmem == 0u && (sbase & 1023u) == 0u;
+
+    if (warp >= kSoftmaxWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+        if (warp == kTmaWarp) {
+            if (lane == 0 && ok && n_kt > 0) {
+                int nk = 0, nv = 0;
+                mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL), 2 * TILE);
+                for (int t = 0; t < 2; ++t)
+                    tma_load_3d<1>(sbase + L::OFF_Q + t * TILE, &maps.q, 0, head_pair ? h0 + t : h0, it.q_base + row_of(t), bar(L::B_Q_FULL));
+                for (int j = 0; j < n_kt && ok; ++j) {
+                    const int sk = j % NSK, sv = j % NSV;
+                    if (j >= NSK) ok = mbar_wait<1>(bar(L::B_K_FREE + sk), (j / NSK - 1) & 1, gave_up);
+                    if (!ok) break;
+                    mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + sk), TILE);
+                    tma_load_3d<1>(sbase + L::OFF_K + sk * TILE, &maps.k, 0, g, it.k_base + j * BN, bar(L::B_K_FULL + sk));
+                    nk = j + 1;
+                    if (j >= NSV) ok = mbar_wait<1>(bar(L::B_V_FREE + sv), (j / NSV - 1) & 1, gave_up);
+                    if (!ok) break;
+                    mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + sv), TILE);
+                    tma_load_3d<1>(sbase + L::OFF_V + sv * TILE, &maps.v, 0, g, it.k_base + j * BN, bar(L::B_V_FULL + sv));
+                    nv = j + 1;
+                }
+                // nothing of this thread's may still be on its way to shared memory when the CTA ends
+                mbar_wait_own<1>(bar(L::B_Q_FULL), 0);
+                for (int j = max(0, nk - NSK); j < nk; ++j) mbar_wait_own<1>(bar(L::B_K_FULL + j % NSK), (j / NSK) & 1);
+                for (int j = max(0, nv - NSV); j < nv; ++j) mbar_wait_own<1>(bar(L::B_V_FULL + j % NSV), (j / NSV) & 1);
+            }
+        } else if (warp == kScoreWarp && ok && n_kt > 0) {
+            constexpr uint32_t ID_S = idesc_bf16(BM, BN, false);
+            auto wait_all = [&](int i, int parity) -> bool {
+                const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+                tc_fence_after();
+                return got;
+            };
+            int done0 = 0, done1 = 0, freed = 0;
+            ok = wait_all(L::B_Q_FULL, 0);
+            for (int j = 0; j < n_kt && ok; ++j) {
+                const int st = j % NSK;
+                ok = wait_all(L::B_K_FULL + st, (j / NSK) & 1);
+                const uint32_t kd = desc_lo(sbase + L::OFF_K + st * TILE, 16);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!ok || j >= (t ? n1 : n0)) continue;
+                    ok = wait_all(L::B_S_GO + t, j & 1);
+                    if (!ok) continue;
+                    const uint32_t qd = desc_lo(sbase + L::OFF_Q + t * TILE, 16);
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < DT / 16; ++ks)
+                            tc_mma_ss<1>(T_S + t * BN, qd + dstep(ks * 32), kd + dstep(ks * 32), ID_S, ks > 0);
+                        tc_commit<1>(bar(L::B_S_FULL + t));
+                    }
+                    __syncwarp();
+                    (t ? done1 : done0) = j + 1;
+                }
+                if (!ok) break;
+                if (elect_one()) tc_commit<1>(bar(L::B_K_FREE + st));
+                __syncwarp();
+                freed = j + 1;
+            }
+            // every commit of this warp has arrived before the CTA ends
+            if (lane == 0) {
+                if (done0 > 0) mbar_wait_own<1>(bar(L::B_S_FULL), (done0 - 1) & 1);
+                if (done1 > 0) mbar_wait_own<1>(bar(L::B_S_FULL + 1), (done1 - 1) & 1);
+                for (int j = max(0, freed - NSK); j < freed; ++j) mbar_wait_own<1>(bar(L::B_K_FREE + j % NSK), (j / NSK) & 1);
+            }
+        } else if (warp == kValueWarp && ok && n_kt > 0) {
+            constexpr uint32_t ID_O = idesc_f16(BM, DT, true);
+            auto wait_all = [&](int i, int parity) -> bool {
+                const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+                tc_fence_after();
+                return got;
+            };
+            int done0 = 0, done1 = 0, freed = 0;
+            for (int j = 0; j < n_kt && ok; ++j) {
+                const int st = j % NSV;
+                ok = wait_all(L::B_V_FULL + st, (j / NSV) & 1);
+                const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, TILE);
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!ok || j >= (t ? n1 : n0)) continue;
+                    ok = wait_all(L::B_P_GO + t, j & 1);
+                    if (!ok) continue;
+                    if (elect_one()) {
+#pragma unroll
+                        for (int ks = 0; ks < BN / 16; ++ks)
+                            tc_mma_ts<1>(T_O + t * DT, T_P + t * (BN / 2) + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
+                        tc_commit<1>(bar(L::B_PV_DONE + t));
+                    }
+                    __syncwarp();
+                    (t ? done1 : done0) = j + 1;
+                }
+                if (!ok) break;
+                if (elect_one()) tc_commit<1>(bar(L::B_V_FREE + st));
+                __syncwarp();
+                freed = j + 1;
+            }
+            if (lane == 0) {
+                if (done0 > 0) mbar_wait_own<1>(bar(L::B_PV_DONE), (done0 - 1) & 1);
+                if (done1 > 0) mbar_wait_own<1>(bar(L::B_PV_DONE + 1), (done1 - 1) & 1);
+                for (int j = max(0, freed - NSV); j < freed; ++j) mbar_wait_own<1>(bar(L::B_V_FREE + j % NSV), (j / NSV) & 1);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        const int wq = warp & 3, grp = warp >> 2, h = head_pair ? h0 + grp : h0;
+        const int r = wq * 32 + lane, q0 = row_of(grp), n = grp ? n1 : n0;
+        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        const float sc = a.scale_log2, v_absmax = *a.v_absmax;
+        const uint32_t t_s = T_S + grp * BN + lane_off, t_p = T_P + grp * (BN / 2) + lane_off, t_o = T_O + grp * DT + lane_off;
+        if (lane == 0 && n > 0) mbar_arrive(bar(L::B_S_GO + grp));
+        const int last_key = q0 + r + shift, warp_sees = q0 + wq * 32 + shift;
+        float l = 0.f, m = -INFINITY;
+        for (int j = 0; j < n && ok; ++j) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_S_FULL + grp), j & 1, gave_up));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t su[2][64];
+            tmem_issue64(t_s, su[0]);
+            tmem_issue64(t_s + 64, su[1]);
+            tmem_wait_ld();
+            pin64(su[0]);
+            pin64(su[1]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && j + 1 < n) mbar_arrive(bar(L::B_S_GO + grp));
+            float sv[BN];
+#pragma unroll
+            for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
+            if (warp_sees < j * BN + BN - 1) {
+                uint32_t cw[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) cw[e] = causal_word(last_key - j * BN, e);
+#pragma unroll
+                for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
+            }
+            const float mx = row_max(sv) * sc;
+            const bool upd = mx > m + kLazyLog2;
+            const bool scale_o = upd && m != -INFINITY;
+            const float al = scale_o ? exp2f(m - mx) : 1.f;
+            if (upd) {
+                l *= al;
+                m = mx;
+            }
+            const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
+            uint32_t hw[BN / 2];
+            l += weights_of(sv, sc, m == -INFINITY ? 0.f : m, hw);
+            if (j > 0) {  // P's buffer is free, and O has settled
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_PV_DONE + grp), (j - 1) & 1, gave_up));
+                if (!ok) break;
+                tc_fence_after();
+                if (any_scale) {
+#pragma unroll 1
+                    for (int c0 = 0; c0 < DT; c0 += 32) {
+                        float ov[32];
+                        uint32_t ow[32];
+                        tmem_ld32(t_o + c0, ov);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) ow[e] = __float_as_uint(ov[e] * al);
+                        tmem_st32(t_o + c0, ow);
+                    }
+                    tmem_wait_st();
+                }
+            }
+            tmem_st32(t_p, hw);
+            tmem_st32(t_p + 32, hw + 32);
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(L::B_P_GO + grp));
+        }
+        if (ok && n > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_PV_DONE + grp), (n - 1) & 1, gave_up));
+        // (rows without a key: the query's copy, whose place the zeros pass through, must have landed)
+        if (ok && n == 0 && n_kt > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FULL), 0, gave_up));
+        if (ok) {
+            tc_fence_after();
+            if (v_absmax < INFINITY) {
+                const float inv = l == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / l;
+                const int w0 = q0 + 32 * wq;
+                TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT;
+                // through the row tile's query, whose products are done: 4 KB a warp
+                unsigned char *stage = smem + L::OFF_Q + warp * (TILE / kGroupWarps);
+                constexpr int OC = 128 / (int)sizeof(TOut);
+#pragma unroll
+                for (int c0 = 0; c0 < DT; c0 += OC)
+                    store_out<OC, TOut>(stage, t_o + c0, inv, out + c0, (int64_t)a.Hq * DT, it.q_len - w0);
+                if (q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m, l);
+            } else {
+                rows_one_by_one<DT, TOut>(a, it, q0, h, wq, kGroupWarps);
+            }
+        }
+    }
+    if (!ok) atomicOr(&g_ris_packed_error, 2u);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kScoreWarp) tmem_dealloc<1, kTmemCols>(tmem);
+}
+
+// ---------------------------------------------------------------- values as fp16
+// The largest magnitude of each CTA's share of V (as bits without the sign, so that an infinity or NaN wins).
+constexpr int kPrepThreads = 256, kPrepBlocks = 304;
+__global__ void __launch_bounds__(kPrepThreads) k_values_absmax(const PackedArgs a, int row_pieces, float *part)
+{
+    const int64_t n = a.k_total * row_pieces, step = (int64_t)gridDim.x * kPrepThreads;
+    uint32_t m = 0;
+#pragma unroll 4
+    for (int64_t t = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t < n; t += step) {
+        const int64_t r = t / row_pieces;
+        const uint4 x = *reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.v) + r * a.v_stride + (t - r * row_pieces) * 8);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, max((w[e] << 16) & 0x7FFFFFFFu, w[e] & 0x7FFF0000u));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    __shared__ uint32_t red[kPrepThreads / 32];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kPrepThreads / 32; ++w) m = max(m, red[w]);
+        part[blockIdx.x] = __uint_as_float(m);
+    }
+}
+// part[0 .. n_part - 1] -> *absmax; v16 = fp16(v 2^-E)
+__global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a, int row_pieces, const float *part, int n_part, float *absmax,
+                                                             __half *v16)
+{
+    uint32_t m = 0;
+    for (int i = threadIdx.x; i < n_part; i += kPrepThreads) m = max(m, __float_as_uint(part[i]));
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    __shared__ uint32_t red[kPrepThreads / 32];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kPrepThreads / 32; ++w) m = max(m, red[w]);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *absmax = __uint_as_float(m);
+    const float s = pow2i(-value_exp(__uint_as_float(m)));
+    const int64_t n = a.k_total * row_pieces, step = (int64_t)gridDim.x * kPrepThreads;
+#pragma unroll 2
+    for (int64_t t = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t < n; t += step) {
+        const int64_t r = t / row_pieces;
+        const uint4 x = *reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.v) + r * a.v_stride + (t - r * row_pieces) * 8);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const __half2 hv = __floats2half2_rn(__uint_as_float(w[e] << 16) * s, __uint_as_float(w[e] & 0xFFFF0000u) * s);
+            y[e] = *reinterpret_cast<const uint32_t *>(&hv);
+        }
+        reinterpret_cast<uint4 *>(v16)[t] = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+}
+
+// ---------------------------------------------------------------- key weights
+// What each key got from the last weight_rows rows of its sequence: w_j = sum over those rows i and the heads of its
+// KV head of 2^(s_ij - m_i) / l_i, with the maxima and sums that the attention left. One CTA per (128 keys,
+// KV head) holds the keys as the A operand and runs S^T = K Q^T over the group's heads and chunks of 64 rows: a
+// thread owns a key (a TMEM lane), so the sum over rows stays in its register. Bounded by the
+// exponentials, one per pair and head.
+//
+//   warps 0-3  one thread per key; warp 4 (TMA) the keys, then chunks of rows into a ring; warp 5 the products
+template <int DT>
+struct LayW {
+    static constexpr int RC = 64, NQ = 3, NB = DT / 64;    // rows of a chunk, ring stages, 64-column blocks
+    static constexpr int K_BLK = BN * 128, Q_BLK = RC * 128, Q_STAGE = NB * Q_BLK;
+    static constexpr int OFF_K = 0, OFF_Q = OFF_K + NB * K_BLK, OFF_STAT = OFF_Q + NQ * Q_STAGE;  // float2 [4][RC]
+    static constexpr int OFF_BARS = OFF_STAT + 4 * RC * 8, OFF_TMEM = OFF_BARS + 128, BYTES = OFF_TMEM + 16;
+    static constexpr int B_K_FULL = 0, B_Q_FULL = 1, B_Q_FREE = B_Q_FULL + NQ, B_S_FULL = B_Q_FREE + NQ, B_S_FREE = B_S_FULL + 2,
+                         NBAR = B_S_FREE + 2;
+    static constexpr uint32_t COLS = 2 * RC;
+};
+constexpr int kWeightThreads = 192;
+
+template <int DT>
+__global__ void __launch_bounds__(kWeightThreads) k_packed_weights_tc(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+{
+    using L = LayW<DT>;
+    constexpr int RC = L::RC, NQ = L::NQ, NB = L::NB;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
+    const uint32_t sbase = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned int *const gave_up = &g_ris_packed_error;
+    const PackItem it = a.key_items[blockIdx.x];
+    const int g = blockIdx.y, shift = it.k_len - it.q_len;
+    // rows that count and see the item's first key
+    const int first = max(max(0, it.q_len - a.weight_rows), it.row - shift);
+    const int chunks = first < it.q_len ? (it.q_len - first + RC - 1) / RC : 0, steps = chunks * a.G;
+    const int j = it.row + (int)threadIdx.x;  // this thread's key (warps 0-3)
+    if (steps == 0) {
+        if (threadIdx.x < BN && j < it.k_len) a.key_weight[(int64_t)g * a.k_total + it.k_base + j] = 0.f;
+        return;
+    }
+    auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
+    if (warp == 4) {
+        if (lane < L::NBAR) {
+            mbar_init(bar(lane), lane >= L::B_S_FREE ? 4 : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+    } else if (warp == 5) {
+        tmem_alloc<1, L::COLS>(smem_u32(&tmem_base_sh));
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_sh;
+    bool ok = (sbase & 1023u) == 0u;
+    if (warp == 4) {
+        if (lane == 0 && ok) {
+            mbar_arrive_expect_tx<1>(bar(L::B_K_FULL), NB * L::K_BLK);
+            for (int blk = 0; blk < NB; ++blk)
+                tma_load_3d<1>(sbase + L::OFF_K + blk * L::K_BLK, &maps.k, 64 * blk, g, it.k_base + it.row, bar(L::B_K_FULL));
+            int n = 0;
+            for (int s = 0; s < steps && ok; ++s) {
+                const int st = s % NQ, h = g * a.G + s / chunks, row = it.q_base + first + s % chunks * RC;
+                if (s >= NQ) ok = mbar_wait<1>(bar(L::B_Q_FREE + st), (s / NQ - 1) & 1, gave_up);
+                if (!ok) break;
+                mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL + st), L::Q_STAGE);
+                for (int blk = 0; blk < NB; ++blk)
+                    tma_load_3d<1>(sbase + L::OFF_Q + st * L::Q_STAGE + blk * L::Q_BLK, &maps.q, 64 * blk, h, row, bar(L::B_Q_FULL + st));
+                n = s + 1;
+            }
+            mbar_wait_own<1>(bar(L::B_K_FULL), 0);
+            for (int s = max(0, n - NQ); s < n; ++s) mbar_wait_own<1>(bar(L::B_Q_FULL + s % NQ), (s / NQ) & 1);
+        }
+    } else if (warp == 5) {
+        constexpr uint32_t ID = idesc_bf16(BN, RC, false);
+        auto wait_all = [&](int i, int parity) -> bool {
+            const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+            tc_fence_after();
+            return got;
+        };
+        if (ok) ok = wait_all(L::B_K_FULL, 0);
+        int n = 0;
+        for (int s = 0; s < steps && ok; ++s) {
+            const int st = s % NQ, b = s & 1;
+            ok = wait_all(L::B_Q_FULL + st, (s / NQ) & 1);
+            if (ok && s >= 2) ok = wait_all(L::B_S_FREE + b, (s / 2 - 1) & 1);
+            if (!ok) break;
+            const uint32_t kd = desc_lo(sbase + L::OFF_K, 16), qd = desc_lo(sbase + L::OFF_Q + st * L::Q_STAGE, 16);
+            if (elect_one()) {
+#pragma unroll
+                for (int ks = 0; ks < DT / 16; ++ks)
+                    tc_mma_ss<1>(tmem + b * RC, kd + dstep((ks >> 2) * L::K_BLK + (ks & 3) * 32), qd + dstep((ks >> 2) * L::Q_BLK + (ks & 3) * 32),
+                                 ID, ks > 0);
+                tc_commit<1>(bar(L::B_S_FULL + b));
+                tc_commit<1>(bar(L::B_Q_FREE + st));
+            }
+            __syncwarp();
+            n = s + 1;
+        }
+        // every commit has arrived before the CTA ends
+        if (lane == 0) {
+            for (int s = max(0, n - 2); s < n; ++s) mbar_wait_own<1>(bar(L::B_S_FULL + (s & 1)), (s / 2) & 1);
+            for (int s = max(0, n - NQ); s < n; ++s) mbar_wait_own<1>(bar(L::B_Q_FREE + s % NQ), (s / NQ) & 1);
+        }
+    } else {
+        float2 *const st_sh = reinterpret_cast<float2 *>(smem + L::OFF_STAT) + warp * RC;
+        const float sc = a.scale_log2;
+        const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+        float w = 0.f;
+        auto stats = [&](int s, float2 (&x)[RC / 32]) {
+            const int i0 = first + s % chunks * RC;
+            const float2 *p = a.row_stat + (int64_t)(g * a.G + s / chunks) * a.q_total + it.q_base;
+#pragma unroll
+            for (int e = 0; e < RC / 32; ++e) {
+                const int i = i0 + lane + 32 * e;
+                x[e] = s < steps && i < it.q_len ? p[i] : make_float2(0.f, 0.f);
+            }
+        };
+        float2 next[RC / 32];
+        stats(0, next);
+        for (int s = 0; s < steps && ok; ++s) {
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < RC / 32; ++e) st_sh[lane + 32 * e] = next[e];
+            stats(s + 1, next);
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_S_FULL + (s & 1)), (s / 2) & 1, gave_up));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t sv[RC];
+            tmem_issue64(tmem + (s & 1) * RC + lane_off, sv);
+            tmem_wait_ld();
+            pin64(sv);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && s + 2 < steps) mbar_arrive(bar(L::B_S_FREE + (s & 1)));
+            const int i0 = first + s % chunks * RC;
+            const int from = j - shift - i0;   // first row of the chunk that sees this thread's key
+            const int rows = it.q_len - i0;    // rows of the chunk
+            float part[4] = {};
+            if (it.row + warp * 32 + 31 - shift <= i0 && rows >= RC) {
+#pragma unroll
+                for (int e = 0; e < RC; e += 2) {
+                    const float4 ml = *reinterpret_cast<const float4 *>(&st_sh[e]);
+                    part[e & 2] = fmaf(ex2(fmaf(__uint_as_float(sv[e]), sc, -ml.x)), ml.y, part[e & 2]);
+                    part[(e & 2) + 1] = fmaf(ex2(fmaf(__uint_as_float(sv[e + 1]), sc, -ml.z)), ml.w, part[(e & 2) + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < RC; ++e) {
+                    const float2 ml = st_sh[e];
+                    const float p = ex2(fmaf(__uint_as_float(sv[e]), sc, -ml.x));
+                    if (e >= from && e < rows) part[e & 3] = fmaf(p, ml.y, part[e & 3]);
+                }
+            }
+            w += (part[0] + part[1]) + (part[2] + part[3]);
+        }
+        if (ok && j < it.k_len) a.key_weight[(int64_t)g * a.k_total + it.k_base + j] = w;
+    }
+    if (!ok) atomicOr(&g_ris_packed_error, 2u);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 5) tmem_dealloc<1, L::COLS>(tmem);
+}
+
+// ---------------------------------------------------------------- host side
+PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
+{
+    static std::once_flag once;
+    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+            q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
+    });
+    return fn;
+}
+
+// n tokens of H heads of D 16-bit values, `stride` elements from token to token, viewed as 3D (d, head,
+// token); box = 64 d x 1 head x `rows` tokens.
+bool make_map(CUtensorMap *m, const void *base, int64_t n, int H, int64_t stride, int rows, int D, bool f16 = false)
+{
+    auto fn = encode_fn();
+    if (fn == nullptr) return false;
+    cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)n};
+    cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
+    cuuint32_t box[3] = {64, 1, (cuuint32_t)rows};
+    cuuint32_t estr[3] = {1, 1, 1};
+    return fn(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
+              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DT, typename TOut>
+cudaError_t launch_tiles(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
+{
+    constexpr int CG = DT == 128 ? 2 : 1;
+    // at least the 128 layout's: one CTA per SM, as a CTA holds all TMEM columns
+    constexpr int bytes = DT == 128 ? Lay128::BYTES : Lay64::BYTES;
+    static_assert(bytes > 232448 / 2, "one CTA per SM, as it holds all TMEM columns");
+    void (*kern)(PackedArgs, PackedMaps);
+    if constexpr (DT == 128)
+        kern = k_packed128<TOut>;
+    else
+        kern = k_packed64<TOut>;
+    static std::once_flag once;
+    static cudaError_t ready = cudaSuccess;
+    std::call_once(once, [&] {
+        ready = cudaFuncSetAttribute(reinterpret_cast<const void *>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        // the softmax threads' setmaxnreg would wait for registers that a smaller launch lacks
+        cudaFuncAttributes fa;
+        if (ready == cudaSuccess) ready = cudaFuncGetAttributes(&fa, reinterpret_cast<const void *>(kern));
+        if (ready == cudaSuccess && (fa.numRegs + 7) / 8 * 8 < kRegs) ready = cudaErrorInvalidConfiguration;
+    });
+    if (ready != cudaSuccess) return ready;
+    const int64_t heads = (a.G & 1) == 0 ? a.Hq / 2 : a.Hq;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.n_items * heads * CG));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a, maps);
+    note_launch();
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace
+
+size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim)
+{
+    return 256 + sizeof(float) * kPrepBlocks + 256 + (size_t)k_total * kv_heads * head_dim * 2;
+}
+
+cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, void *scratch, cudaStream_t s)
+{
+    // scratch: the largest magnitude, the parts it comes from, the values
+    float *absmax = static_cast<float *>(scratch), *part = absmax + 64;
+    __half *v16 = reinterpret_cast<__half *>((reinterpret_cast<uintptr_t>(part + kPrepBlocks) + 255) & ~uintptr_t(255));
+    a.v_absmax = absmax;
+    const int row_pieces = a.Hkv * D / 8;
+    const int64_t pieces = a.k_total * row_pieces, blocks = (pieces + 4 * kPrepThreads - 1) / (4 * kPrepThreads);
+    if (pieces > 0) {
+        const int n_part = (int)(blocks < kPrepBlocks ? blocks : kPrepBlocks);
+        k_values_absmax<<<n_part, kPrepThreads, 0, s>>>(a, row_pieces, part);
+        k_values_f16<<<(unsigned)(blocks < 2432 ? blocks : 2432), kPrepThreads, 0, s>>>(a, row_pieces, part, n_part, absmax, v16);
+        note_launch(2);
+    } else {
+        const cudaError_t e = cudaMemsetAsync(absmax, 0, sizeof(float), s);
+        if (e != cudaSuccess) return e;
+    }
+    alignas(64) PackedMaps maps;
+    const int krows = D == 128 ? Lay128::KROWS : BN;
+    // (without keys no box of k or v is ever asked for: any valid map does)
+    const bool keys = a.k_total > 0;
+    if (!make_map(&maps.q, a.q, a.q_total, a.Hq, a.q_stride, BM, D)) return cudaErrorInvalidValue;
+    if (!keys)
+        maps.k = maps.v = maps.q;
+    else if (!make_map(&maps.k, a.k, a.k_total, a.Hkv, a.k_stride, krows, D) ||
+             !make_map(&maps.v, v16, a.k_total, a.Hkv, (int64_t)a.Hkv * D, BN, D, true))
+        return cudaErrorInvalidValue;
+    if (D == 128) return out_dtype == RIS_F32 ? launch_tiles<128, float>(a, maps, s) : launch_tiles<128, __nv_bfloat16>(a, maps, s);
+    return out_dtype == RIS_F32 ? launch_tiles<64, float>(a, maps, s) : launch_tiles<64, __nv_bfloat16>(a, maps, s);
+}
+
+cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
+{
+    alignas(64) PackedMaps maps;
+    if (a.q_total == 0)
+        maps = PackedMaps{};  // no rows: every CTA writes zeros
+    else if (!make_map(&maps.q, a.q, a.q_total, a.Hq, a.q_stride, LayW<128>::RC, D) ||
+             !make_map(&maps.k, a.k, a.k_total, a.Hkv, a.k_stride, BN, D))
+        return cudaErrorInvalidValue;
+    else
+        maps.v = maps.k;
+    const dim3 grid((unsigned)a.n_key_items, (unsigned)a.Hkv);
+    cudaError_t e;
+    if (D == 128) {
+        e = cudaFuncSetAttribute(k_packed_weights_tc<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, LayW<128>::BYTES);
+        if (e != cudaSuccess) return e;
+        k_packed_weights_tc<128><<<grid, kWeightThreads, LayW<128>::BYTES, s>>>(a, maps);
+    } else {
+        // 60 KB where 40 would do: five CTAs of an SM would ask for more TMEM columns than there are
+        constexpr int bytes = 60 << 10;
+        static_assert(bytes >= LayW<64>::BYTES, "");
+        e = cudaFuncSetAttribute(k_packed_weights_tc<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != cudaSuccess) return e;
+        k_packed_weights_tc<64><<<grid, kWeightThreads, bytes, s>>>(a, maps);
+    }
+    note_launch();
+    return cudaGetLastError();
+}
+
+// Read and clear this file's device error word (the caller has synchronised).
+unsigned int read_packed_error()
+{
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_ris_packed_error, sizeof(v)) != cudaSuccess) return 0;
+    if (v != 0) cudaMemcpyToSymbol(g_ris_packed_error, &zero, sizeof(zero));
+    return v;
+}
+
+}  // namespace ris

@@ -24,17 +24,7 @@ constexpr int BM = 64, BN = 64, LD = BM + 4;  // rows and keys of a tile, pitch 
 constexpr int kThreads = 256;
 constexpr int kHalves = kPackRows / BM;
 
-template <typename T>
-__device__ __forceinline__ float4 load4(const T *p);
-template <>
-__device__ __forceinline__ float4 load4<float>(const float *p) { return *reinterpret_cast<const float4 *>(p); }
-template <>
-__device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16 *p)
-{
-    const uint2 w = *reinterpret_cast<const uint2 *>(p);
-    return make_float4(__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
-                       __uint_as_float(w.y & 0xFFFF0000u));
-}
+__device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
 __device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
 {
@@ -69,12 +59,12 @@ __device__ __forceinline__ float2 f2_get(uint64_t v)
 }
 
 // x[row][d] of up to 64 rows of one head, d-major into dst[d][row]; rows past `rows` as zeros
-template <typename T, int D>
-__device__ __forceinline__ void stage_t(float *dst, const T *x, int64_t stride, int rows)
+template <int D>
+__device__ __forceinline__ void stage_t(float *dst, const float *x, int64_t stride, int rows)
 {
     for (int t = threadIdx.x; t < BM * (D / 4); t += kThreads) {
         const int r = t % BM, d = t / BM * 4;
-        const float4 v = r < rows ? load4<T>(x + r * stride + d) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float4 v = r < rows ? load4(x + r * stride + d) : make_float4(0.f, 0.f, 0.f, 0.f);
         dst[d * LD + r] = v.x;
         dst[(d + 1) * LD + r] = v.y;
         dst[(d + 2) * LD + r] = v.z;
@@ -82,7 +72,7 @@ __device__ __forceinline__ void stage_t(float *dst, const T *x, int64_t stride, 
     }
 }
 
-template <typename T, typename TO, int D>
+template <typename TO, int D>
 __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
 {
     extern __shared__ __align__(16) float sm[];
@@ -94,11 +84,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
     const int g = h / a.G;
     const int shift = it.k_len - it.q_len;              // row i sees keys j <= i + shift
     const int keys = max(0, min(it.k_len, r0 + rows + shift));  // that the last of the rows sees
-    const T *q = reinterpret_cast<const T *>(a.q) + (int64_t)(it.q_base + r0) * a.q_stride + h * D;
-    const T *k = reinterpret_cast<const T *>(a.k) + (int64_t)it.k_base * a.k_stride + g * D;
-    const T *v = reinterpret_cast<const T *>(a.v) + (int64_t)it.k_base * a.v_stride + g * D;
+    const float *q = reinterpret_cast<const float *>(a.q) + (int64_t)(it.q_base + r0) * a.q_stride + h * D;
+    const float *k = reinterpret_cast<const float *>(a.k) + (int64_t)it.k_base * a.k_stride + g * D;
+    const float *v = reinterpret_cast<const float *>(a.v) + (int64_t)it.k_base * a.v_stride + g * D;
     const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    stage_t<T, D>(qs, q, a.q_stride, rows);
+    stage_t<D>(qs, q, a.q_stride, rows);
     constexpr int C = D / 16;  // columns of O of a thread: 4 tx + 64 x ..
     uint64_t o[4][C / 2] = {};
     float m[4], l[4];
@@ -107,11 +97,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
     for (int k0 = 0; k0 < keys; k0 += BN) {
         const int kn = min(BN, keys - k0);
         __syncthreads();  // the tiles of the last step are done with
-        stage_t<T, D>(ks, k + (int64_t)k0 * a.k_stride, a.k_stride, kn);
+        stage_t<D>(ks, k + (int64_t)k0 * a.k_stride, a.k_stride, kn);
         for (int t = threadIdx.x; t < BN * (D / 4); t += kThreads) {
             const int r = t / (D / 4), d = t % (D / 4) * 4;
             // a key that is not there weighs nothing, whatever lies in its place
-            store4(vs + r * D + d, r < kn ? load4<T>(v + (int64_t)(k0 + r) * a.v_stride + d) : make_float4(0.f, 0.f, 0.f, 0.f));
+            store4(vs + r * D + d, r < kn ? load4(v + (int64_t)(k0 + r) * a.v_stride + d) : make_float4(0.f, 0.f, 0.f, 0.f));
         }
         __syncthreads();
         uint64_t s2[4][2] = {};
@@ -210,7 +200,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
 // Threads are keys; rows of q in shared memory, kRows at a time.
 constexpr int kWeightRows = 32;
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kPackKeys) k_packed_weights(const PackedArgs a)
 {
     __shared__ __align__(16) float qs[kWeightRows][D];
@@ -219,9 +209,9 @@ __global__ void __launch_bounds__(kPackKeys) k_packed_weights(const PackedArgs a
     const int g = blockIdx.y, j = it.row + threadIdx.x, shift = it.k_len - it.q_len;
     const bool there = j < it.k_len;
     float4 kr[D / 4];
-    const T *k = reinterpret_cast<const T *>(a.k) + (int64_t)(it.k_base + (there ? j : it.row)) * a.k_stride + g * D;
+    const float *k = reinterpret_cast<const float *>(a.k) + (int64_t)(it.k_base + (there ? j : it.row)) * a.k_stride + g * D;
 #pragma unroll
-    for (int d = 0; d < D / 4; ++d) kr[d] = load4<T>(k + 4 * d);
+    for (int d = 0; d < D / 4; ++d) kr[d] = load4(k + 4 * d);
     // rows that see the item's first key, of those that count
     const int first = max(max(0, it.q_len - a.weight_rows), it.row - shift);
     float w = 0.f;
@@ -231,7 +221,7 @@ __global__ void __launch_bounds__(kPackKeys) k_packed_weights(const PackedArgs a
             __syncthreads();
             for (int t = threadIdx.x; t < n * (D / 4); t += kPackKeys) {
                 const int r = t / (D / 4), d = t % (D / 4) * 4;
-                store4(&qs[r][d], load4<T>(reinterpret_cast<const T *>(a.q) + (int64_t)(it.q_base + i0 + r) * a.q_stride + h * D + d));
+                store4(&qs[r][d], load4(reinterpret_cast<const float *>(a.q) + (int64_t)(it.q_base + i0 + r) * a.q_stride + h * D + d));
             }
             if (threadIdx.x < n) st[threadIdx.x] = a.row_stat[(int64_t)h * a.q_total + it.q_base + i0 + threadIdx.x];
             __syncthreads();
@@ -253,10 +243,10 @@ __global__ void __launch_bounds__(kPackKeys) k_packed_weights(const PackedArgs a
     if (there) a.key_weight[(int64_t)g * a.k_total + it.k_base + j] = w;
 }
 
-template <typename T, typename TO, int D>
+template <typename TO, int D>
 cudaError_t launch(const PackedArgs &a, cudaStream_t s)
 {
-    auto kern = k_packed_f32<T, TO, D>;
+    auto kern = k_packed_f32<TO, D>;
     constexpr int bytes = (2 * D * LD + BN * D) * (int)sizeof(float);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
@@ -265,35 +255,23 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t s)
     return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t launch_weights(const PackedArgs &a, int D, cudaStream_t s)
+}  // namespace
+
+cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStream_t s)
+{
+    if (out_dtype == RIS_F32) return D == 128 ? launch<float, 128>(a, s) : launch<float, 64>(a, s);
+    return D == 128 ? launch<__nv_bfloat16, 128>(a, s) : launch<__nv_bfloat16, 64>(a, s);
+}
+
+cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s)
 {
     const dim3 grid((unsigned)a.n_key_items, (unsigned)a.Hkv);
     if (D == 128)
-        k_packed_weights<T, 128><<<grid, kPackKeys, 0, s>>>(a);
+        k_packed_weights<128><<<grid, kPackKeys, 0, s>>>(a);
     else
-        k_packed_weights<T, 64><<<grid, kPackKeys, 0, s>>>(a);
+        k_packed_weights<64><<<grid, kPackKeys, 0, s>>>(a);
     note_launch();
     return cudaGetLastError();
-}
-
-template <typename T, typename TO>
-cudaError_t launch_d(const PackedArgs &a, int D, cudaStream_t s)
-{
-    return D == 128 ? launch<T, TO, 128>(a, s) : launch<T, TO, 64>(a, s);
-}
-
-}  // namespace
-
-cudaError_t launch_packed_f32(const PackedArgs &a, int D, int dtype, int out_dtype, cudaStream_t s)
-{
-    if (dtype == RIS_F32) return out_dtype == RIS_F32 ? launch_d<float, float>(a, D, s) : launch_d<float, __nv_bfloat16>(a, D, s);
-    return out_dtype == RIS_F32 ? launch_d<__nv_bfloat16, float>(a, D, s) : launch_d<__nv_bfloat16, __nv_bfloat16>(a, D, s);
-}
-
-cudaError_t launch_packed_weights(const PackedArgs &a, int D, int dtype, cudaStream_t s)
-{
-    return dtype == RIS_F32 ? launch_weights<float>(a, D, s) : launch_weights<__nv_bfloat16>(a, D, s);
 }
 
 }  // namespace ris

@@ -920,7 +920,7 @@ ris_status ris_device_status(void *stream)
     RIS_CUDA(cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)));
     RIS_CUDA(read_tile_error(&tile_word));
     const unsigned int decode_word = read_decode_error(), cache_word = read_cache4_error();
-    word |= tile_word | (cache_word & 4u);
+    word |= tile_word | (cache_word & 4u) | read_packed_error();
     if (word != 0u) return fail(RIS_ERR_DEVICE_TIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
     if (decode_word != 0u)
         return fail(RIS_ERR_INVALID, "a decode step read a position outside [t0, cache_len) from t_dev");

@@ -59,11 +59,16 @@ struct PackedArgs {
     int32_t weight_rows;       // 0: none
     float *key_weight;         // [Hkv][k_total]
     float2 *row_stat;          // scratch [Hq][q_total]: each row's (maximum in log2, 1 / sum); null without weights
-    const void *v16;           // bf16 calls: the values as fp16, scaled by 2^-E, [k_total][Hkv][D]
-    const float *v_absmax;     // device: max |v|
+    const float *v_absmax;     // device, tile kernels: max |v|
 };
-cudaError_t launch_packed_f32(const PackedArgs &a, int D, int dtype, int out_dtype, cudaStream_t s);
-cudaError_t launch_packed_weights(const PackedArgs &a, int D, int dtype, cudaStream_t s);
+// fp32 inputs: items of kPackRows rows.
+cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStream_t s);
+cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s);
+// bf16 inputs: items of kPackRows rows with an even group, of 2 kPackRows with an odd one; scratch of
+// packed_scratch_bytes, 256-byte aligned.
+size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim);
+cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, void *scratch, cudaStream_t s);
+cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s);
 
 struct Cache4Args {
     uint8_t *k, *v;              // [B][Hkv][cap][D / 2]
@@ -120,6 +125,8 @@ cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaSt
 
 // Reads and clears the error word of the cache's kernels (bit 1: tokens appended past the capacity).
 unsigned int read_cache4_error();
+// Reads and clears the error word of the packed attention's tile kernels (a bounded wait gave up).
+unsigned int read_packed_error();
 
 // Stream-ordered pool memory, as every allocation of the library (ris_api.cu).
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s);

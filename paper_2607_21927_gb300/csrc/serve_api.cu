@@ -1,6 +1,6 @@
 // C ABI of the serving operators: packed prompts, positions on several axes and the 4-bit cache.
 // Argument checks, the plan of a pack, scratch and the launches; the work is in rope_axes.cu,
-// attn_packed_f32.cu, cache4.cu and cache4_evict.cu.
+// attn_packed.cu, attn_packed_f32.cu, cache4.cu and cache4_evict.cu.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -20,8 +20,8 @@ struct ris_pack_s {
     int64_t q_total = 0, k_total = 0, q_longest = 0, k_longest = 0;
     void *mem = nullptr;  // device: everything below
     int32_t *q_off = nullptr, *seq_of = nullptr;
-    PackItem *items = nullptr, *key_items = nullptr;
-    int32_t n_items = 0, n_key_items = 0;
+    PackItem *items = nullptr, *pairs = nullptr, *key_items = nullptr;  // of 128 rows, 256 rows, 128 keys
+    int32_t n_items = 0, n_pairs = 0, n_key_items = 0;
     cudaStream_t stream = nullptr;
 };
 
@@ -141,11 +141,11 @@ Cache4Args cache_args(const ris_cache4 *c)
 
 double log2e_over_sqrt(int32_t head_dim) { return 1.4426950408889634074 / std::sqrt((double)head_dim); }
 
-// The items of lengths n (rows, or keys) of every sequence.
-std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vector<int32_t> &k_off, bool keys)
+// The items of `step` rows (or keys) of every sequence; of rows, those with the most keys first, so that the
+// short ones fill the tail of the grid.
+std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vector<int32_t> &k_off, bool keys, int step)
 {
     std::vector<PackItem> v;
-    const int step = keys ? kPackKeys : kPackRows;
     for (size_t s = 0; s + 1 < q_off.size(); ++s) {
         PackItem it{};
         it.seq = (int32_t)s;
@@ -159,6 +159,11 @@ std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vec
             v.push_back(it);
         }
     }
+    auto cost = [step](const PackItem &it) {
+        const int64_t last = std::min<int64_t>((int64_t)it.row + step, it.q_len) + it.k_len - it.q_len;
+        return std::max<int64_t>(0, std::min<int64_t>(last, it.k_len));
+    };
+    if (!keys) std::stable_sort(v.begin(), v.end(), [&](const PackItem &x, const PackItem &y) { return cost(x) > cost(y); });
     return v;
 }
 
@@ -197,20 +202,17 @@ ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t
         }
         p->q_total = nq;
         p->k_total = nk;
-        std::vector<PackItem> items = items_of(q_off, k_off, false), keys = items_of(q_off, k_off, true);
-        // the items with the most keys first, so that the short ones fill the tail of the grid
-        auto cost = [](const PackItem &it) {
-            const int64_t last = std::min<int64_t>(it.row + kPackRows, it.q_len) + it.k_len - it.q_len;
-            return std::max<int64_t>(0, std::min<int64_t>(last, it.k_len));
-        };
-        std::stable_sort(items.begin(), items.end(), [&](const PackItem &x, const PackItem &y) { return cost(x) > cost(y); });
+        const std::vector<PackItem> items = items_of(q_off, k_off, false, kPackRows), pairs = items_of(q_off, k_off, false, 2 * kPackRows),
+                                    keys = items_of(q_off, k_off, true, kPackKeys);
         p->n_items = (int32_t)items.size();
+        p->n_pairs = (int32_t)pairs.size();
         p->n_key_items = (int32_t)keys.size();
         cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
         p->stream = s;
         const size_t off_b = room(sizeof(int32_t) * q_off.size()), seq_b = room(sizeof(int32_t) * seq_of.size()),
-                     item_b = room(sizeof(PackItem) * items.size()), key_b = room(sizeof(PackItem) * keys.size());
-        cudaError_t e = library_alloc(&p->mem, off_b + seq_b + item_b + key_b, s);
+                     item_b = room(sizeof(PackItem) * items.size()), pair_b = room(sizeof(PackItem) * pairs.size()),
+                     key_b = room(sizeof(PackItem) * keys.size());
+        cudaError_t e = library_alloc(&p->mem, off_b + seq_b + item_b + pair_b + key_b, s);
         char *d = static_cast<char *>(p->mem);
         auto put = [&](const void *src, size_t bytes) {
             if (e == cudaSuccess && bytes > 0) e = cudaMemcpyAsync(d, src, bytes, cudaMemcpyHostToDevice, s);
@@ -224,6 +226,9 @@ ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t
         p->items = reinterpret_cast<PackItem *>(d);
         put(items.data(), sizeof(PackItem) * items.size());
         d += item_b;
+        p->pairs = reinterpret_cast<PackItem *>(d);
+        put(pairs.data(), sizeof(PackItem) * pairs.size());
+        d += pair_b;
         p->key_items = reinterpret_cast<PackItem *>(d);
         put(keys.data(), sizeof(PackItem) * keys.size());
         // the host arrays end with this call: the copies out of them must have been taken
@@ -372,13 +377,21 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     a.scale_log2 = (float)log2e_over_sqrt(head_dim);
     a.weight_rows = weight_rows;
     a.key_weight = key_weight;
-    Scratch stat;
-    if (weight_rows > 0 && pack->q_total > 0) {
-        RIS_CUDA(stat.alloc(sizeof(float2) * (size_t)heads * pack->q_total, s));
-        a.row_stat = static_cast<float2 *>(stat.p);
+    const bool tiles = dtype == RIS_BF16;
+    if (tiles && (a.G & 1) != 0) {
+        a.items = pack->pairs;
+        a.n_items = pack->n_pairs;
     }
-    if (pack->n_items > 0) RIS_CUDA(launch_packed_f32(a, head_dim, dtype, out_dtype, s));
-    if (weight_rows > 0 && pack->n_key_items > 0) RIS_CUDA(launch_packed_weights(a, head_dim, dtype, s));
+    const size_t stat_b = weight_rows > 0 ? room(sizeof(float2) * (size_t)heads * pack->q_total) : 0;
+    const size_t tile_b = tiles ? packed_scratch_bytes(pack->k_total, kv_heads, head_dim) : 0;
+    Scratch mem;
+    if (stat_b + tile_b > 0) RIS_CUDA(mem.alloc(stat_b + tile_b, s));
+    if (weight_rows > 0) a.row_stat = static_cast<float2 *>(mem.p);
+    if (pack->n_items > 0)
+        RIS_CUDA(tiles ? launch_packed_tiles(a, head_dim, out_dtype, static_cast<char *>(mem.p) + stat_b, s)
+                       : launch_packed_f32(a, head_dim, out_dtype, s));
+    if (weight_rows > 0 && pack->n_key_items > 0)
+        RIS_CUDA(tiles ? launch_packed_weights_tc(a, head_dim, s) : launch_packed_weights_f32(a, head_dim, s));
     return RIS_OK;
 }
 
