@@ -14,6 +14,8 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <mutex>
+#include <type_traits>
 
 #include "attn_common.cuh"
 #include "serve.h"
@@ -71,13 +73,31 @@ __device__ __forceinline__ __nv_bfloat16 scale_of(uint32_t top)
 }
 
 // the codes of a and b (a in the low half)
-__device__ __forceinline__ uint32_t code2(float a, float b, float s)
+__device__ __forceinline__ uint32_t code2(float a, float b)
 {
-    const float x = s > 0.f ? __fdiv_rn(a, s) : 0.f, y = s > 0.f ? __fdiv_rn(b, s) : 0.f;
     uint16_t r;
-    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u16.u8 %0, t;\n\t}" : "=h"(r) : "f"(y), "f"(x));
+    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u16.u8 %0, t;\n\t}" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
+// The codes of x / s rounded to fp32 first, as the format has it, without a division per value: the code is a
+// monotone function, so where x / s (1 - 2^-21) and x / s (1 + 2^-21), each good to 2^-22, have the same
+// code, the quotient between them has it too. Else (a value next to a limit) the division itself.
+struct Scale {
+    float s, lo, hi;  // the scale; 1 / s pulled down and up, or lo > hi where it is not to be used
+    __device__ __forceinline__ explicit Scale(float scale) : s(scale)
+    {
+        const float r = __frcp_rn(scale);
+        lo = r * (1.f - 0x1p-21f);
+        hi = r * (1.f + 0x1p-21f);
+        if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) lo = 1.f, hi = 0.f;
+    }
+    __device__ __forceinline__ uint32_t codes(float a, float b) const
+    {
+        const uint32_t c = code2(a * lo, b * lo);
+        if (c == code2(a * hi, b * hi) && lo <= hi) return c;
+        return s > 0.f ? code2(__fdiv_rn(a, s), __fdiv_rn(b, s)) : 0u;
+    }
+};
 
 constexpr int kAppendThreads = 256;
 
@@ -93,8 +113,9 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4Ap
     const int64_t r = (int64_t)blockIdx.x * (kAppendThreads / lanes) + threadIdx.x / lanes;  // token and head
     const int64_t n_rows = a.total * a.c.Hkv;
     const bool in = r < n_rows;
-    const int64_t tok = (in ? r : n_rows - 1) / a.c.Hkv;
-    const int head = (int)((in ? r : n_rows - 1) - tok * a.c.Hkv);
+    const int64_t r_in = in ? r : n_rows - 1;
+    const int64_t tok = n_rows <= 0xFFFFFFFFLL ? (int64_t)((uint32_t)r_in / (uint32_t)a.c.Hkv) : r_in / a.c.Hkv;
+    const int head = (int)(r_in - tok * a.c.Hkv);
     const int b = a.seq_of[tok], i = (int)tok - a.off[b];
     const int64_t slot = (int64_t)(a.start != nullptr ? a.start[b] : a.c.length[b]) + i;
     const bool ok = slot >= 0 && slot < a.c.cap;
@@ -115,10 +136,10 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4Ap
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             const __nv_bfloat16 s = scale_of(top);
             sc[g] = __bfloat16_as_ushort(s);
-            const float sf = __bfloat162float(s);
+            const Scale sf(__bfloat162float(s));
             w[g] = 0;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[g] |= code2(x[g][2 * e], x[g][2 * e + 1], sf) << (8 * e);
+            for (int e = 0; e < 4; ++e) w[g] |= sf.codes(x[g][2 * e], x[g][2 * e + 1]) << (8 * e);
         }
         if (in && ok) {
             uint8_t *dst = a.c.k + row * (D / 2) + u * (4 * NG);
@@ -150,9 +171,9 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4Ap
             for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
             const __nv_bfloat16 s = scale_of(top);
             sc[g] = __bfloat16_as_ushort(s);
-            const float sf = __bfloat162float(s);
+            const Scale sf(__bfloat162float(s));
 #pragma unroll
-            for (int e = 2 * g; e < 2 * g + 2; ++e) w[e / 4] |= code2(x[e][0], x[e][1], sf) << (8 * (e & 3));
+            for (int e = 2 * g; e < 2 * g + 2; ++e) w[e / 4] |= sf.codes(x[e][0], x[e][1]) << (8 * (e & 3));
         }
         if (in && ok) {
             uint8_t *dst = a.c.v + row * (D / 2) + u * NM;
@@ -196,60 +217,61 @@ __device__ __forceinline__ __half2 values2(uint32_t byte)
     return *reinterpret_cast<const __half2 *>(&r);
 }
 
-// One thread per four elements of a row of the output: two bytes in, 16 bytes out. Bound by the fp32
-// rows that it writes.
-constexpr int kReadThreads = 256;
+// One thread per four elements of a row of the output, kReadRows rows of a list to a CTA: two bytes in, 16 bytes out.
+// Bound by the fp32 rows that it writes.
+constexpr int kReadThreads = 256, kReadRows = 64;
 template <int D>
-__global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c, const int32_t *first, int64_t count, float *ko,
-                                                              float *vo)
+__global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c, const int32_t *first, int64_t count, int blocks,
+                                                              float *ko, float *vo)
 {
-    constexpr int Q = D / 4, NG = D / kCacheGroup, NM = D / 16;
-    const int64_t t = (int64_t)blockIdx.x * kReadThreads + threadIdx.x;
-    const int64_t n = (int64_t)c.B * c.Hkv * count * Q;
-    if (t >= n) return;
-    const int e = (int)(t % Q);  // elements 4 e .. 4 e + 3: bytes 2 e, 2 e + 1 in natural order
-    const int64_t r = t / Q, bh = r / count, i = r % count;
+    constexpr int Q = D / 4, NG = D / kCacheGroup, NM = D / 16, STEP = kReadThreads / Q;
+    const int64_t bh = blockIdx.x / blocks;
+    const int64_t i0 = (int64_t)(blockIdx.x - bh * blocks) * kReadRows + threadIdx.x / Q;
+    const int e = threadIdx.x % Q;  // elements 4 e .. 4 e + 3: bytes 2 e, 2 e + 1 in natural order
     const int b = (int)(bh / c.Hkv);
-    const int64_t slot = i + (first != nullptr ? first[b] : 0);
-    const bool there = slot >= 0 && slot < min((int64_t)c.length[b], c.cap);
+    const int64_t s0 = first != nullptr ? first[b] : 0, len = min((int64_t)c.length[b], c.cap);
     const bool values = blockIdx.y != 0;
-    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (there) {
-        const int64_t row = bh * c.cap + slot;
-        uint32_t b0, b1;
-        if (!values) {
-            const int word = e / 2;  // 8 elements
-            const uint8_t *p = c.k + row * (D / 2) + ((word & 3) * NG + (word >> 2)) * 4 + (e & 1) * 2;
-            const uint32_t w = *reinterpret_cast<const uint16_t *>(p);
-            b0 = w & 0xFFu, b1 = w >> 8;
-        } else {
-            const int tile = e / 4, col = 2 * (e & 3);
-            const uint8_t *p = c.v + row * (D / 2) + tile;
-            b0 = p[col * NM], b1 = p[(col + 1) * NM];
+    const int word = e / 2, tile = e / 4, col = 2 * (e & 3);
+    const uint8_t *codes = (values ? c.v : c.k) + bh * c.cap * (D / 2) +
+                           (values ? tile + col * NM : ((word & 3) * NG + (word >> 2)) * 4 + (e & 1) * 2);
+    const uint16_t *scales = (values ? c.v_scale : c.k_scale) + bh * c.cap * NG + e / 8;
+    float4 *out = reinterpret_cast<float4 *>(values ? vo : ko) + bh * count * Q + e;
+#pragma unroll 4
+    for (int64_t i = i0; i < min(count, i0 + kReadRows - (int)threadIdx.x / Q); i += STEP) {
+        const int64_t slot = i + s0;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (slot >= 0 && slot < len) {
+            const uint8_t *p = codes + slot * (D / 2);
+            uint32_t b0, b1;
+            if (values) {
+                b0 = p[0], b1 = p[NM];
+            } else {
+                const uint32_t w = *reinterpret_cast<const uint16_t *>(p);
+                b0 = w & 0xFFu, b1 = w >> 8;
+            }
+            const float sf = __uint_as_float((uint32_t)scales[slot * NG] << 16);
+            const float2 lo = __half22float2(values2(b0)), hi = __half22float2(values2(b1));
+            x = make_float4(lo.x * sf, lo.y * sf, hi.x * sf, hi.y * sf);
         }
-        const uint32_t s = (values ? c.v_scale : c.k_scale)[row * NG + e / 8];
-        const float sf = __uint_as_float(s << 16);
-        const float2 lo = __half22float2(values2(b0)), hi = __half22float2(values2(b1));
-        x = make_float4(lo.x * sf, lo.y * sf, hi.x * sf, hi.y * sf);
+        out[i * Q] = x;
     }
-    reinterpret_cast<float4 *>(values ? vo : ko)[t] = x;
 }
 
 // ---------------------------------------------------------------- attention of one token
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kTile = 16;                      // slots of a warp's product
-constexpr int kWarpTiles = 4;                  // tiles of a warp in a stage
-constexpr int kStageSlots = kWarps * kWarpTiles * kTile;  // 256
-constexpr int kStages = 2;
-constexpr int kMinExp = -114;                  // smallest exponent of a value scale that counts as such
+constexpr int kUnit = kCacheUnit;              // slots by which the work is shared out
+constexpr int kMinExp = -100;                  // smallest exponent of a value scale that counts as such: sums stay finite
 
-template <int D>
+template <int D, bool SPLIT>
 struct Lay {
+    static constexpr int TILES = SPLIT ? 2 : 4, SLOTS = TILES * kTile, STAGES = 8 / TILES;  // of a warp's stage; of its ring
     static constexpr int NG = D / kCacheGroup, NM = D / 16;
     static constexpr int CODES = D / 2, SCALES = 2 * NG;  // bytes of a slot
-    static constexpr int OFF_K = 0, OFF_V = OFF_K + kStageSlots * CODES, OFF_KS = OFF_V + kStageSlots * CODES,
-                         OFF_VS = OFF_KS + kStageSlots * SCALES, STAGE = OFF_VS + kStageSlots * SCALES;
-    static constexpr int OFF_BARS = kStages * STAGE, BYTES = OFF_BARS + 8 * kStages;
+    static constexpr int OFF_K = 0, OFF_V = OFF_K + SLOTS * CODES, OFF_KS = OFF_V + SLOTS * CODES, OFF_VS = OFF_KS + SLOTS * SCALES,
+                         STAGE = OFF_VS + SLOTS * SCALES;
+    static constexpr int OFF_BARS = kWarps * STAGES * STAGE, BYTES = OFF_BARS + 8 * kWarps * STAGES;
+    static_assert(kWarps * 8 * (D * 4 + 8) <= OFF_BARS, "the warps' parts of a list pass through the rings");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -276,9 +298,16 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 
 __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// the product alone (no registers to clear for it)
+__device__ __forceinline__ void mma0(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 {
@@ -319,142 +348,207 @@ __device__ __forceinline__ float bf16_at(uint32_t w, int e) { return __uint_as_f
 // neighbouring rows of the values.
 __device__ __forceinline__ int tile_slot(int r) { return ((r & 7) >> 1) + 4 * (r & 1) + (r & 8); }
 
-// One CTA per (range of slots, KV head, sequence). Its four warps take tiles of 16 slots in turn, each with
-// a softmax of its own over the slots that it saw; bulk copies bring stages of 256 slots (codes and
-// scales, contiguous per KV head) into a ring of two. A tile:
+// How the slots in use are shared out. A list is a (sequence, KV head, block of 8 query heads) and holds
+// ceil(length / kUnit) units; the units of all lists, one list after another, are cut into as many equal runs as there are CTAs, whatever
+// the lengths are. CTA i's part of list l has partial number i + l: runs and lists advance together, so no two parts
+// share a number. Lists of a sequence are neighbours: list = b * per_seq + y.
+struct Shares {
+    int64_t total;  // units of all lists
+
+    __device__ __forceinline__ int64_t begin(int cta, int ctas) const { return total * cta / ctas; }
+    // the CTA whose run holds unit u
+    __device__ __forceinline__ int cta_of(int64_t u, int ctas) const
+    {
+        int i = (int)(u * ctas / total);
+        while (i + 1 < ctas && begin(i + 1, ctas) <= u) ++i;
+        while (begin(i, ctas) > u) --i;
+        return i;
+    }
+};
+__device__ __forceinline__ int64_t slots_of(const Cache4AttendArgs &a, int b)
+{
+    return max((int64_t)0, min((int64_t)a.c.length[b], a.reach));
+}
+__device__ __forceinline__ int64_t units_of(const Cache4AttendArgs &a, int b) { return (slots_of(a, b) + kUnit - 1) / kUnit; }
+
+// Sum over the block's threads of x; every thread gets it. `red`: a word per warp.
+__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *red)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) x += red[w];
+    return x;
+}
+
+// Persistent CTAs of four warps; each CTA takes a run of units and the lists that it touches one after another. Its warps
+// take stages of 64 slots (32 for fp32 outputs, whose accumulators double; fewer where that leaves warps without any) in turn, each
+// with a softmax of its own over the slots that it saw and a ring of its own, filled by bulk copies (codes and scales are contiguous per KV head): no warp waits for another before a list's
+// end. A tile of 16 slots:
 //   S^T = K q^T  rows are slots, columns up to 8 query heads: the codes as fp16 (exact) straight from
 //                the lane's word, one accumulator per group of 32, which the group's scale then multiplies in
-//                fp32 (so the products are exact up to fp32 sums); the query as fp16 scaled by a power of two, with a second fp16 of
-//                what that leaves for fp32 inputs;
-//   O^T += V^T P^T  the weights times the slot's scale, per group of 32, as fp16 scaled by 2^12 over the
-//                largest scale so far (a weight of 2^-26 of the largest is still normal), transposed by movmatrix; with SPLIT a second fp16
-//                of what the first leaves, for fp32 outputs; values as fp16 pairs of slots by byte permutes.
+//                fp32 (so the products are exact up to fp32 sums); the query as fp16 scaled by a power of
+//                two, with a second fp16 of what that leaves for fp32 inputs;
+//   O^T += V^T P^T  the weights times the slot's scale, per group of 32, as fp16, transposed by
+//                movmatrix; with SPLIT a second fp16 of what the first leaves, for fp32 outputs; values as
+//                fp16 pairs of slots by byte permutes.
+// The weights are 2^(s - m + 4 - ev), ev the exponent of the largest value scale so far and m a reference that
+// moves only when a score exceeds it by more than 2^8: weight times scale stays below 2^13, and what a
+// weight of 2^-18 of the reference's or more loses to fp16 is its 11 bits' rounding. Sums and O carry the same factor, which cancels.
 // Slots past the length enter with score -infinity and scale 0, whatever lies there.
-// G query heads of a KV head: 8 of them per product; QB products of a CTA share the unpacked codes' loads.
-template <typename T, bool SPLIT, int D, int QB>
-__global__ void __launch_bounds__(kThreads) k_cache4_attend(const Cache4AttendArgs a)
+// A list takes 8 query heads of its KV head, a product's columns.
+constexpr float kLazyLog2 = 8.f;
+
+template <typename T, bool SPLIT, int D>
+__global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4AttendArgs a)
 {
-    using L = Lay<D>;
-    constexpr int NG = L::NG, NM = L::NM;
+    using L = Lay<D, SPLIT>;
+    constexpr int NG = L::NG, NM = L::NM, kWarpTiles = L::TILES, kStageSlots = L::SLOTS, kStages = L::STAGES;
     constexpr bool LO = sizeof(T) == 4;  // the query needs a second part
     extern __shared__ __align__(128) unsigned char smem[];
-    const uint32_t sbase = smem_u32(smem);
+    __shared__ int64_t red[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
-    const int b = blockIdx.z, kvh = blockIdx.y % a.c.Hkv, h0 = blockIdx.y / a.c.Hkv * (8 * QB);  // first head of the group
-    const int nh = min(8 * QB, a.G - h0);
-    const int64_t len = max(0, min(a.c.length[b], (int)min(a.reach, (int64_t)INT32_MAX)));
-    const int64_t first = (int64_t)blockIdx.x * a.chunk;
-    const int n = (int)max((int64_t)0, min((int64_t)a.chunk, len - first));  // slots of this CTA
-    const int64_t head0 = (int64_t)b * a.Hq + kvh * a.G + h0;                 // its first query head
-    if (n == 0 && blockIdx.x != 0) return;
-    const int64_t row0 = ((int64_t)b * a.c.Hkv + kvh) * a.c.cap + first;
-    const int n_stages = (n + kStageSlots - 1) / kStageSlots;
-    auto fetch = [&](int st) {  // by one thread
-        const int s0 = st * kStageSlots, rows = min(kStageSlots, (n - s0 + 15) / 16 * 16);
-        const uint32_t bar = sbase + L::OFF_BARS + 8 * (st % kStages), dst = sbase + st % kStages * L::STAGE;
-        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(rows * 2 * (L::CODES + L::SCALES))
-                     : "memory");
-        bulk_load(dst + L::OFF_K, a.c.k + (row0 + s0) * L::CODES, rows * L::CODES, bar);
-        bulk_load(dst + L::OFF_KS, a.c.k_scale + (row0 + s0) * NG, rows * L::SCALES, bar);
-        bulk_load(dst + L::OFF_V, a.c.v + (row0 + s0) * L::CODES, rows * L::CODES, bar);
-        bulk_load(dst + L::OFF_VS, a.c.v_scale + (row0 + s0) * NG, rows * L::SCALES, bar);
-    };
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < kStages; ++i)
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(sbase + L::OFF_BARS + 8 * i) : "memory");
+    const int per_seq = a.lists / a.c.B;
+    unsigned char *const ring = smem + warp * (kStages * L::STAGE);
+    const uint32_t ring_at = smem_u32(ring), bars = smem_u32(smem) + L::OFF_BARS + 8 * kStages * warp;
+    if (lane == 0) {
+        for (int i = 0; i < kStages; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bars + 8 * i) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        for (int st = 0; st < min(kStages, n_stages); ++st) fetch(st);
     }
-    // the queries: lane (g8, t4) holds elements 32 g + 8 t4 .. + 7 of head g8 of each block, scaled by 2^-e
-    uint32_t qh[QB][NG][4], ql[LO ? QB : 1][LO ? NG : 1][4];
-    float unscale[QB][2];  // of heads 2 t4, 2 t4 + 1: log2(e) / sqrt(D) 2^e
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        const int h = 8 * qb + g8;
-        const bool have = h < nh;
-        const T *q = reinterpret_cast<const T *>(a.q) + (head0 + (have ? h : 0)) * D + 8 * t4;
-        float x[NG][8];
-        uint32_t top = 0;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            load_row<T, 8>(q + kCacheGroup * g, x[g]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, mag(x[g][e]));
-        }
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        // |q| 2^-e below 2^13; the exponent stays where both factors are normal numbers
-        const int e2 = min(max((int)(top >> 23) - 127 - 12, -100), 100);
-        const float down = pow2i(-e2), up = have ? pow2i(e2) * a.scale_log2 : 0.f;
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float u = have ? x[g][2 * e] * down : 0.f, v = have ? x[g][2 * e + 1] * down : 0.f;
-                qh[qb][g][e] = pack_half(u, v);
-                if constexpr (LO) ql[qb][g][e] = pack_rest(u, v, qh[qb][g][e]);
-            }
-        unscale[qb][0] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4);
-        unscale[qb][1] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4 + 4);
+    __syncwarp();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    Shares sh;
+    {
+        int64_t n = 0;
+        for (int b = threadIdx.x; b < a.c.B; b += kThreads) n += units_of(a, b);
+        sh.total = block_sum(n, red) * per_seq;
     }
-    float m[QB][2], l[QB][2], o[QB][NM][4];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-        m[qb][0] = m[qb][1] = -INFINITY;
-        l[qb][0] = l[qb][1] = 0.f;
-#pragma unroll
-        for (int e = 0; e < NM; ++e) o[qb][e][0] = o[qb][e][1] = o[qb][e][2] = o[qb][e][3] = 0.f;
+    const int ctas = (int)min((int64_t)gridDim.x, sh.total);  // no run is empty
+    if ((int)blockIdx.x >= ctas) return;
+    int64_t at = sh.begin(blockIdx.x, ctas);
+    const int64_t end = sh.begin(blockIdx.x + 1, ctas);
+    // the list that holds unit `at`, and its first unit
+    int b = 0;
+    int64_t base = 0;
+    while (b < a.c.B && at < end) {
+        // whole sequences before the run, a block's worth at a time
+        int64_t n = 0;
+        for (int e = b + threadIdx.x; e < min(b + kThreads, a.c.B); e += kThreads) n += units_of(a, e);
+        n = block_sum(n, red) * per_seq;
+        if (base + n > at) break;
+        base += n;
+        b += kThreads;
     }
-    int ev = kMinExp;  // O is in units of 2^(ev - 12), ev the exponent of the largest value scale so far
+    int used = 0, phase = 0;  // the warp's next stage of its ring, and the phase of its barrier
     bool ok = true;
-    __syncthreads();
-    for (int st = 0; st < n_stages; ++st) {
-        // (a warp whose wait gave up only skips the work: every warp meets the others at each barrier)
-        if (ok) ok = mbar_wait(sbase + L::OFF_BARS + 8 * (st % kStages), (st / kStages) & 1);
-        const unsigned char *sm = smem + st % kStages * L::STAGE;
-        const int s0 = st * kStageSlots, ns = min(kStageSlots, n - s0);  // slots of the stage
-        const int n_tiles = (ns + kTile - 1) / kTile;
-        if (ok && warp < n_tiles) {
-            // the value scales of this lane's slots, and the largest of the warp's
+    for (; b < a.c.B && at < end; ++b) {
+        const int64_t len = slots_of(a, b), units = (len + kUnit - 1) / kUnit;
+        if (base + units * per_seq <= at) {
+            base += units * per_seq;
+            continue;
+        }
+        for (int y = 0; y < per_seq && at < end; ++y, base += units) {
+        if (base + units <= at) continue;
+        const int64_t u1 = min(end, base + units);
+        const int64_t first = (at - base) * kUnit;
+        const int n = (int)(min(len, (u1 - base) * kUnit) - first);  // slots of this part
+        at = u1;
+        const int kvh = y % a.c.Hkv, h0 = y / a.c.Hkv * 8;  // first head of the block
+        const int nh = min(8, a.G - h0);
+        const int64_t head0 = (int64_t)b * a.Hq + kvh * a.G + h0;
+        const int64_t row0 = ((int64_t)b * a.c.Hkv + kvh) * a.c.cap + first;
+        // the warp's stages: `per` slots from per (warp + 4 i) on
+        const int per = min(kStageSlots, (n + kWarps * kTile - 1) / (kWarps * kTile) * kTile), s_step = kWarps * per;
+        auto fetch = [&](int s0, int slot) {  // by one lane
+            const int rows = min(per, (n - s0 + 15) / 16 * 16);
+            const uint32_t bar = bars + 8 * slot, dst = ring_at + slot * L::STAGE;
+            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(rows * 2 * (L::CODES + L::SCALES))
+                         : "memory");
+            bulk_load(dst + L::OFF_K, a.c.k + (row0 + s0) * L::CODES, rows * L::CODES, bar);
+            bulk_load(dst + L::OFF_KS, a.c.k_scale + (row0 + s0) * NG, rows * L::SCALES, bar);
+            bulk_load(dst + L::OFF_V, a.c.v + (row0 + s0) * L::CODES, rows * L::CODES, bar);
+            bulk_load(dst + L::OFF_VS, a.c.v_scale + (row0 + s0) * NG, rows * L::SCALES, bar);
+        };
+        // (the ring is empty here: the last part's stages were waited for, and its outputs have left it)
+        if (lane == 0 && ok)
+            for (int i = 0, s0 = warp * per, slot = used; i < kStages && s0 < n; ++i, s0 += s_step) {
+                fetch(s0, slot);
+                slot = slot + 1 == kStages ? 0 : slot + 1;
+            }
+        // the queries: lane (g8, t4) holds elements 32 g + 8 t4 .. + 7 of head g8 of each block, scaled by 2^-e
+        uint32_t qh[NG][4], ql[LO ? NG : 1][4];
+        float unscale[2];  // of heads 2 t4, 2 t4 + 1: log2(e) / sqrt(D) 2^e
+        {
+            const int h = g8;
+            const bool have = h < nh;
+            const T *q = reinterpret_cast<const T *>(a.q) + (head0 + (have ? h : 0)) * D + 8 * t4;
+            float x[NG][8];
+            uint32_t top = 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+                load_row<T, 8>(q + kCacheGroup * g, x[g]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, mag(x[g][e]));
+            }
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // |q| 2^-e below 2^13; the exponent stays where both factors are normal numbers
+            const int e2 = min(max((int)(top >> 23) - 127 - 12, -100), 100);
+            const float down = pow2i(-e2), up = pow2i(e2) * a.scale_log2;
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float u = have ? x[g][2 * e] * down : 0.f, v = have ? x[g][2 * e + 1] * down : 0.f;
+                    qh[g][e] = pack_half(u, v);
+                    if constexpr (LO) ql[g][e] = pack_rest(u, v, qh[g][e]);
+                }
+            unscale[0] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4);
+            unscale[1] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4 + 4);
+        }
+        float m[2], l[2], o[NM][4];
+        {
+            m[0] = m[1] = -INFINITY;
+            l[0] = l[1] = 0.f;
+#pragma unroll
+            for (int e = 0; e < NM; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
+        }
+        int ev = kMinExp;  // exponent of the largest value scale so far
+        // a stage of ns slots at s0; FULL: ns == kStageSlots
+        auto stage = [&](auto full_c, const unsigned char *sm, int s0, int ns) {
+            constexpr bool FULL = decltype(full_c)::value;
+            // the value scales of this lane's slots, and the largest of the stage
             uint32_t vsc[kWarpTiles][2][NG / 2], top = 0;
 #pragma unroll
             for (int i = 0; i < kWarpTiles; ++i)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int slot = (warp + kWarps * i) * kTile + tile_slot(g8 + 8 * r);
-                    const bool there = slot < ns;
-                    const uint32_t *p = reinterpret_cast<const uint32_t *>(sm + L::OFF_VS + (there ? slot : 0) * L::SCALES);
+                    const int slot = i * kTile + tile_slot(g8 + 8 * r);
+                    const uint32_t *p = reinterpret_cast<const uint32_t *>(sm + L::OFF_VS + slot * L::SCALES);
 #pragma unroll
                     for (int g = 0; g < NG / 2; ++g) {
-                        vsc[i][r][g] = there ? p[g] : 0u;
+                        vsc[i][r][g] = FULL || slot < ns ? p[g] : 0u;
                         top = __vmaxu2(top, vsc[i][r][g]);
                     }
                 }
-            top = max(top & 0xFFFFu, top >> 16);
-#pragma unroll
-            for (int x = 4; x < 32; x <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
+            top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
             const int e_new = max(ev, min((int)(top >> 7) - 127, 127));
-            const float ov = e_new - ev > 126 ? 0.f : pow2i(ev - e_new);  // O in the new units
-            ev = e_new;
-            const float to16 = pow2i(12 - ev);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
+            {
                 float s[kWarpTiles][4];
 #pragma unroll
                 for (int i = 0; i < kWarpTiles; ++i) {
-                    const int tile = warp + kWarps * i;
-                    if (tile >= n_tiles) {
+                    if (!FULL && i * kTile >= ns) {
                         s[i][0] = s[i][1] = s[i][2] = s[i][3] = -INFINITY;
                         continue;
                     }
-                    uint32_t kw[2][NG];
-                    float ks[2][NG];
-                    bool there[2];
+                    uint32_t kw[2][NG], ksw[2][NG / 2];
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const int slot = tile * kTile + tile_slot(g8 + 8 * r);
-                        there[r] = slot < ns;
+                        const int slot = i * kTile + tile_slot(g8 + 8 * r);
                         const unsigned char *p = sm + L::OFF_K + slot * L::CODES + t4 * (4 * NG);
                         const uint32_t *ps = reinterpret_cast<const uint32_t *>(sm + L::OFF_KS + slot * L::SCALES);
                         if constexpr (NG == 4) {
@@ -465,71 +559,83 @@ __global__ void __launch_bounds__(kThreads) k_cache4_attend(const Cache4AttendAr
                             kw[r][0] = w.x, kw[r][1] = w.y;
                         }
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) ks[r][g] = bf16_at(ps[g / 2], g);
+                        for (int g = 0; g < NG / 2; ++g) ksw[r][g] = ps[g];
                     }
                     float acc[4] = {};
 #pragma unroll
                     for (int g = 0; g < NG; ++g) {
-                        uint32_t x[4], y[4];
+                        uint32_t x[4], z[4];
                         unpack4(kw[0][g], x);
-                        unpack4(kw[1][g], y);
-                        float d[4] = {};
-                        const uint32_t f0[4] = {x[0], y[0], x[1], y[1]}, f1[4] = {x[2], y[2], x[3], y[3]};
-                        mma(d, f0, qh[qb][g][0], qh[qb][g][1]);
-                        mma(d, f1, qh[qb][g][2], qh[qb][g][3]);
+                        unpack4(kw[1][g], z);
+                        float d[4];
+                        const uint32_t f0[4] = {x[0], z[0], x[1], z[1]}, f1[4] = {x[2], z[2], x[3], z[3]};
+                        mma0(d, f0, qh[g][0], qh[g][1]);
+                        mma(d, f1, qh[g][2], qh[g][3]);
                         if constexpr (LO) {
-                            mma(d, f0, ql[qb][g][0], ql[qb][g][1]);
-                            mma(d, f1, ql[qb][g][2], ql[qb][g][3]);
+                            mma(d, f0, ql[g][0], ql[g][1]);
+                            mma(d, f1, ql[g][2], ql[g][3]);
                         }
-                        acc[0] = fmaf(d[0], ks[0][g], acc[0]);
-                        acc[1] = fmaf(d[1], ks[0][g], acc[1]);
-                        acc[2] = fmaf(d[2], ks[1][g], acc[2]);
-                        acc[3] = fmaf(d[3], ks[1][g], acc[3]);
+                        const float k0 = bf16_at(ksw[0][g / 2], g), k1 = bf16_at(ksw[1][g / 2], g);
+                        acc[0] = g == 0 ? d[0] * k0 : fmaf(d[0], k0, acc[0]);
+                        acc[1] = g == 0 ? d[1] * k0 : fmaf(d[1], k0, acc[1]);
+                        acc[2] = g == 0 ? d[2] * k1 : fmaf(d[2], k1, acc[2]);
+                        acc[3] = g == 0 ? d[3] * k1 : fmaf(d[3], k1, acc[3]);
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[i][e] = there[e >> 1] ? acc[e] * unscale[qb][e & 1] : -INFINITY;
+                    for (int e = 0; e < 4; ++e) {
+                        s[i][e] = acc[e];
+                        if (!FULL && i * kTile + tile_slot(g8 + 8 * (e >> 1)) >= ns) s[i][e] = -INFINITY;
+                    }
                     if (a.scores != nullptr) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const int h = 8 * qb + 2 * t4 + (e & 1);
-                            if (there[e >> 1] && h < nh)
-                                a.scores[(head0 + h) * a.c.cap + first + s0 + tile * kTile + tile_slot(g8 + 8 * (e >> 1))] = s[i][e];
+                            const int h = 2 * t4 + (e & 1), slot = i * kTile + tile_slot(g8 + 8 * (e >> 1));
+                            if ((FULL || slot < ns) && h < nh)
+                                a.scores[(head0 + h) * a.c.cap + first + s0 + slot] = s[i][e] * unscale[e & 1];
                         }
                     }
                 }
-                float nm[2], al[2], ref[2];
+                float x[2];
+                bool moves = e_new != ev;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float x = fmaxf(s[0][e], s[0][e + 2]);
+                    x[e] = fmaxf(s[0][e], s[0][e + 2]);
 #pragma unroll
-                    for (int i = 1; i < kWarpTiles; ++i) x = fmaxf(x, fmaxf(s[i][e], s[i][e + 2]));
-#pragma unroll
-                    for (int y = 4; y < 32; y <<= 1) x = fmaxf(x, __shfl_xor_sync(0xFFFFFFFFu, x, y));
-                    nm[e] = fmaxf(m[qb][e], x);
-                    ref[e] = nm[e] == -INFINITY ? 0.f : nm[e];
-                    al[e] = ex2(m[qb][e] - ref[e]);
-                    m[qb][e] = nm[e];
-                    l[qb][e] *= al[e];
+                    for (int i = 1; i < kWarpTiles; ++i) x[e] = fmaxf(x[e], fmaxf(s[i][e], s[i][e + 2]));
+                    x[e] *= unscale[e];
+                    moves = moves || x[e] > m[e] + kLazyLog2;
                 }
-                // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor pipe's
-                // additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
-                float part[SPLIT ? NM : 1][4] = {};
-                if constexpr (!SPLIT) {
+                if (__any_sync(0xFFFFFFFFu, moves)) {  // (in the first stages of a list, mostly)
+                    const float ov = e_new - ev > 126 ? 0.f : pow2i(ev - e_new);
+                    float al[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int w = 4; w < 32; w <<= 1) x[e] = fmaxf(x[e], __shfl_xor_sync(0xFFFFFFFFu, x[e], w));
+                        const float nm = x[e] > m[e] + kLazyLog2 ? x[e] : m[e];
+                        al[e] = m[e] == -INFINITY ? 0.f : ex2(m[e] - nm) * ov;
+                        m[e] = nm;
+                        l[e] *= al[e];
+                    }
 #pragma unroll
                     for (int e = 0; e < NM; ++e)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) o[qb][e][c] *= al[c & 1] * ov;
+                        for (int c = 0; c < 4; ++c) o[e][c] *= al[c & 1];
                 }
+                // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor pipe's
+                // additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
+                float part[SPLIT ? NM : 1][4];
+                float to[2];  // exponent of a weight: s unscale + to
+#pragma unroll
+                for (int e = 0; e < 2; ++e) to[e] = (float)(4 - e_new) - (m[e] == -INFINITY ? 0.f : m[e]);
 #pragma unroll
                 for (int i = 0; i < kWarpTiles; ++i) {
-                    const int tile = warp + kWarps * i;
-                    if (tile >= n_tiles) continue;
+                    if (!FULL && i * kTile >= ns) continue;
                     float p[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        p[e] = ex2(s[i][e] - ref[e & 1]);
-                        l[qb][e & 1] += p[e];
-                        p[e] *= to16;
+                        p[e] = ex2(fmaf(s[i][e], unscale[e & 1], to[e & 1]));
+                        l[e & 1] += p[e];
                     }
                     uint32_t bh[NG][2], bl[SPLIT ? NG : 1][2];
 #pragma unroll
@@ -537,15 +643,15 @@ __global__ void __launch_bounds__(kThreads) k_cache4_attend(const Cache4AttendAr
 #pragma unroll
                         for (int r = 0; r < 2; ++r) {
                             const float sc = bf16_at(vsc[i][r][g / 2], g);
-                            const float x = p[2 * r] * sc, y = p[2 * r + 1] * sc;
-                            const uint32_t hi = pack_half(x, y);
-                            if constexpr (SPLIT) bl[g][r] = transpose8(pack_rest(x, y, hi));
+                            const float u = p[2 * r] * sc, v = p[2 * r + 1] * sc;
+                            const uint32_t hi = pack_half(u, v);
+                            if constexpr (SPLIT) bl[g][r] = transpose8(pack_rest(u, v, hi));
                             bh[g][r] = transpose8(hi);
                         }
                     uint32_t vw[4][NM / 4];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const unsigned char *p8 = sm + L::OFF_V + (tile * kTile + 4 * r + t4) * L::CODES + g8 * NM;
+                        const unsigned char *p8 = sm + L::OFF_V + (i * kTile + 4 * r + t4) * L::CODES + g8 * NM;
                         if constexpr (NM == 8) {
                             const uint2 w = *reinterpret_cast<const uint2 *>(p8);
                             vw[r][0] = w.x, vw[r][1] = w.y;
@@ -555,19 +661,22 @@ __global__ void __launch_bounds__(kThreads) k_cache4_attend(const Cache4AttendAr
                     }
 #pragma unroll
                     for (int q4 = 0; q4 < NM / 4; ++q4) {
-                        uint32_t x[4][4];
+                        uint32_t w[4][4];
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) unpack4(vw[r][q4], x[r]);
+                        for (int r = 0; r < 4; ++r) unpack4(vw[r][q4], w[r]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int tl = 4 * q4 + e;
-                            const uint32_t f[4] = {__byte_perm(x[0][e], x[1][e], 0x5410), __byte_perm(x[0][e], x[1][e], 0x7632),
-                                                   __byte_perm(x[2][e], x[3][e], 0x5410), __byte_perm(x[2][e], x[3][e], 0x7632)};
+                            const uint32_t f[4] = {__byte_perm(w[0][e], w[1][e], 0x5410), __byte_perm(w[0][e], w[1][e], 0x7632),
+                                                   __byte_perm(w[2][e], w[3][e], 0x5410), __byte_perm(w[2][e], w[3][e], 0x7632)};
                             if constexpr (SPLIT) {
-                                mma(part[tl], f, bl[tl / 2][0], bl[tl / 2][1]);
+                                if (i == 0)
+                                    mma0(part[tl], f, bl[tl / 2][0], bl[tl / 2][1]);
+                                else
+                                    mma(part[tl], f, bl[tl / 2][0], bl[tl / 2][1]);
                                 mma(part[tl], f, bh[tl / 2][0], bh[tl / 2][1]);
                             } else {
-                                mma(o[qb][tl], f, bh[tl / 2][0], bh[tl / 2][1]);
+                                mma(o[tl], f, bh[tl / 2][0], bh[tl / 2][1]);
                             }
                         }
                     }
@@ -576,88 +685,155 @@ __global__ void __launch_bounds__(kThreads) k_cache4_attend(const Cache4AttendAr
 #pragma unroll
                     for (int e = 0; e < NM; ++e)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) o[qb][e][c] = fmaf(o[qb][e][c], al[c & 1] * ov, part[e][c]);
+                        for (int c = 0; c < 4; ++c) o[e][c] += part[e][c];
                 }
             }
+            ev = e_new;
+        };
+        for (int s0 = warp * per; s0 < n; s0 += s_step) {
+            ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(bars + 8 * used, phase));
+            if (ok) {
+                const unsigned char *sm = ring + used * L::STAGE;
+                if (min(per, n - s0) == kStageSlots)
+                    stage(std::true_type{}, sm, s0, kStageSlots);
+                else
+                    stage(std::false_type{}, sm, s0, min(per, n - s0));
+                __syncwarp();  // every lane is done with the stage
+                const int next = s0 + kStages * s_step;
+                if (lane == 0 && next < n) fetch(next, used);
+            }
+            if (++used == kStages) {
+                used = 0;
+                phase ^= 1;
+            }
         }
-        __syncthreads();  // every warp is done with the stage
-        if (threadIdx.x == 0 && ok && st + kStages < n_stages) fetch(st + kStages);
-    }
-    ok = __syncthreads_and(ok);
-    if (!ok) {  // (a copy that never landed: the outputs are undefined)
-        if (threadIdx.x == 0) atomicOr(&g_ris_cache4_error, 4u);
-        return;
-    }
-    // the four warps' parts of each head, through shared memory: [warp][head][D] and (maximum, sum)
-    float *const so = reinterpret_cast<float *>(smem);
-    float2 *const sml = reinterpret_cast<float2 *>(smem + kWarps * 8 * QB * D * 4);
-    const float back = pow2i(ev - 12);
+        // the four warps' parts of each head, through the rings: [warp][head][D] and (maximum, sum)
+        __syncthreads();
+        float *const so = reinterpret_cast<float *>(smem);
+        float2 *const sml = reinterpret_cast<float2 *>(smem + kWarps * 8 * D * 4);
+        const float back = pow2i(ev - 4);
+        {
 #pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
+            for (int e = 0; e < 2; ++e) {
+                float x = l[e] * back;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float x = l[qb][e];
+                for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, w);
+                const int h = 2 * t4 + e;
+                if (g8 == 0) sml[warp * 8 + h] = make_float2(m[e], x);
 #pragma unroll
-            for (int y = 4; y < 32; y <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, y);
-            const int h = 8 * qb + 2 * t4 + e;
-            if (g8 == 0) sml[warp * 8 * QB + h] = make_float2(m[qb][e], x);
+                for (int tl = 0; tl < NM; ++tl)
+                    *reinterpret_cast<float2 *>(so + (warp * 8 + h) * D + 16 * tl + 2 * g8) =
+                        make_float2(o[tl][e] * back, o[tl][e + 2] * back);
+            }
+        }
+        __syncthreads();
+        // one partial per head of the block: number cta + list
+        const int64_t part = ((int64_t)blockIdx.x + (int64_t)b * per_seq + y) * 8;
+        for (int t = threadIdx.x; t < nh * D; t += kThreads) {
+            const int h = t / D, d = t % D;
+            float M = -INFINITY, sum = 0.f, x = 0.f;
 #pragma unroll
-            for (int tl = 0; tl < NM; ++tl)
-                *reinterpret_cast<float2 *>(so + (warp * 8 * QB + h) * D + 16 * tl + 2 * g8) =
-                    make_float2(o[qb][tl][e] * back, o[qb][tl][e + 2] * back);
+            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sml[w * 8 + h].x);
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                const float2 ml = sml[w * 8 + h];
+                const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+                sum = fmaf(ml.y, f, sum);
+                x = fmaf(so[(w * 8 + h) * D + d], f, x);
+            }
+            a.part_o[(part + h) * D + d] = x;
+            if (d == 0) a.part_ml[part + h] = make_float2(M, sum);
+        }
+        // the rings take copies again: after every read of them, and ordered before them
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
         }
     }
-    __syncthreads();
-    for (int t = threadIdx.x; t < nh * D; t += kThreads) {
-        const int h = t / D, d = t % D;
-        float M = -INFINITY, sum = 0.f, x = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sml[w * 8 * QB + h].x);
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-            const float2 ml = sml[w * 8 * QB + h];
-            const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-            sum = fmaf(ml.y, f, sum);
-            x = fmaf(so[(w * 8 * QB + h) * D + d], f, x);
-        }
-        const int64_t part = (head0 + h) * a.n_chunks + blockIdx.x;
-        a.part_o[part * D + d] = x;
-        if (d == 0) a.part_ml[part] = make_float2(M, sum);
-    }
+    if (!ok) atomicOr(&g_ris_cache4_error, 4u);  // (a copy that never landed: the outputs are undefined)
 }
 
-// Joins the ranges of a sequence: one CTA per (query head, sequence), a thread per channel; then
-// (weights) CTAs that add up what each slot got from the heads of its KV head, from the scores that the first kernel left.
-constexpr int kJoinThreads = 128;
-constexpr int kWeightSlots = 1024;  // slots of a CTA
+// Joins the parts of a list. The first CTAs: one per (query head, sequence), warps over its parts, a lane per
+// channels; then (weights) CTAs that add up what each slot got from the heads of its KV head, from the scores that
+// the first kernel left. Launched as its programmatic dependent.
+constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
+constexpr int kWeightSlots = 512;  // slots of a CTA
 
 template <typename TO, int D>
 __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4AttendArgs a)
 {
-    const int b = blockIdx.z;
-    const int64_t len = max(0, min(a.c.length[b], (int)min(a.reach, (int64_t)INT32_MAX)));
-    const int na = max(1, (int)((len + a.chunk - 1) / a.chunk));  // ranges that hold slots
+    constexpr int C = D / 32, block_heads = 8;
+    __shared__ int64_t red[kJoinWarps];
+    __shared__ float so[kJoinWarps][D];
+    __shared__ float2 sml[kJoinWarps];
+    extern __shared__ float2 stat[];  // [G], weights
+    const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int per_seq = a.lists / a.c.B;
+    Shares sh;
+    int64_t before = 0;  // units of the sequences before this one
+    {
+        int64_t n = 0, m = 0;
+        for (int e = threadIdx.x; e < a.c.B; e += kJoinThreads) {
+            const int64_t u = units_of(a, e);
+            n += u;
+            m += e < b ? u : 0;
+        }
+        sh.total = block_sum(n, red) * per_seq;
+        before = block_sum(m, red) * per_seq;
+    }
+    const int64_t len = slots_of(a, b), units = (len + kUnit - 1) / kUnit;
+    const int ctas = (int)min((int64_t)a.ctas, sh.total);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // the parts of list y of this sequence: CTAs i0 .. i1, partial numbers i + list
+    auto parts = [&](int y, int &i0, int &i1) {
+        if (units == 0) {
+            i0 = 0, i1 = -1;
+            return;
+        }
+        const int64_t u0 = before + y * units;
+        i0 = sh.cta_of(u0, ctas);
+        i1 = sh.cta_of(u0 + units - 1, ctas);
+    };
     if ((int)blockIdx.x < a.Hq) {
-        const int64_t h = (int64_t)b * a.Hq + blockIdx.x;
-        const float2 *ml = a.part_ml + h * a.n_chunks;
-        float M = -INFINITY, sum = 0.f, x = 0.f;
-        for (int i = 0; i < na; ++i) M = fmaxf(M, ml[i].x);
+        const int h = blockIdx.x, kvh = h / a.G, hb = (h % a.G) / block_heads, y = hb * a.c.Hkv + kvh;
+        int i0, i1;
+        parts(y, i0, i1);
+        const int64_t p0 = ((int64_t)b * per_seq + y) * block_heads + h % a.G % block_heads;
+        float M = -INFINITY, sum = 0.f, x[C] = {};
+        for (int i = i0 + warp; i <= i1; i += kJoinWarps) {
+            const int64_t p = p0 + (int64_t)i * block_heads;
+            const float2 ml = a.part_ml[p];
+            float v[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) v[c] = a.part_o[p * D + lane + 32 * c];
+            const float nm = fmaxf(M, ml.x);
+            const float f0 = M == -INFINITY ? 0.f : exp2f(M - nm), f1 = ml.x == -INFINITY ? 0.f : exp2f(ml.x - nm);
+            M = nm;
+            sum = fmaf(sum, f0, ml.y * f1);
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[c] = fmaf(x[c], f0, v[c] * f1);
+        }
+        if (lane == 0) sml[warp] = make_float2(M, sum);
+#pragma unroll
+        for (int c = 0; c < C; ++c) so[warp][lane + 32 * c] = x[c];
+        __syncthreads();
+        const int64_t row = (int64_t)b * a.Hq + h;
         const int d = threadIdx.x;
         if (d < D) {
-            const float *po = a.part_o + h * a.n_chunks * D + d;
-#pragma unroll 8
-            for (int i = 0; i < na; ++i) {
-                const float2 y = ml[i];
-                const float f = y.x == -INFINITY ? 0.f : exp2f(y.x - M);
-                sum = fmaf(y.y, f, sum);
-                x = fmaf(po[(int64_t)i * D], f, x);
+            float tm = -INFINITY, ts = 0.f, to = 0.f;
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) tm = fmaxf(tm, sml[w].x);
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) {
+                const float f = sml[w].x == -INFINITY ? 0.f : exp2f(sml[w].x - tm);
+                ts = fmaf(sml[w].y, f, ts);
+                to = fmaf(so[w][d], f, to);
             }
-            x = sum == 0.f ? 0.f : x / sum;  // no slot: zeros
+            to = ts == 0.f ? 0.f : to / ts;  // no slot: zeros
             if constexpr (sizeof(TO) == 4)
-                reinterpret_cast<float *>(a.out)[h * D + d] = x;
+                reinterpret_cast<float *>(a.out)[row * D + d] = to;
             else
-                reinterpret_cast<__nv_bfloat16 *>(a.out)[h * D + d] = __float2bfloat16_rn(x);
-            if (d == 0 && a.lse != nullptr) a.lse[h] = (M + log2f(sum)) * kLn2;
+                reinterpret_cast<__nv_bfloat16 *>(a.out)[row * D + d] = __float2bfloat16_rn(to);
+            if (d == 0 && a.lse != nullptr) a.lse[row] = (tm + log2f(ts)) * kLn2;
         }
         return;
     }
@@ -665,54 +841,83 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
     const int w = blockIdx.x - a.Hq, blocks = (gridDim.x - a.Hq) / a.c.Hkv, kvh = w / blocks;
     const int64_t s0 = (int64_t)(w % blocks) * kWeightSlots;
     if (s0 >= len) return;
-    extern __shared__ float2 stat[];  // [G]
-    for (int h = threadIdx.x; h < a.G; h += kJoinThreads) {
-        const float2 *ml = a.part_ml + ((int64_t)b * a.Hq + kvh * a.G + h) * a.n_chunks;
+    for (int h = warp; h < a.G; h += kJoinWarps) {  // a warp per head, a lane per part
+        const int y = h / block_heads * a.c.Hkv + kvh;
+        int i0, i1;
+        parts(y, i0, i1);
+        const int64_t p0 = ((int64_t)b * per_seq + y) * block_heads + h % block_heads;
         float M = -INFINITY, sum = 0.f;
-        for (int i = 0; i < na; ++i) M = fmaxf(M, ml[i].x);
-        for (int i = 0; i < na; ++i) sum = fmaf(ml[i].y, exp2f(ml[i].x - M), sum);
-        stat[h] = make_float2(M, 1.f / sum);
+        for (int i = i0 + lane; i <= i1; i += 32) {
+            const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
+            const float nm = fmaxf(M, ml.x);
+            sum = nm == -INFINITY ? sum : sum * exp2f(M - nm) + ml.y * exp2f(ml.x - nm);
+            M = nm;
+        }
+        const float tm = warp_max(M);
+        sum = warp_sum(M == -INFINITY ? 0.f : sum * exp2f(M - tm));
+        if (lane == 0) stat[h] = make_float2(tm, 1.f / sum);
     }
     __syncthreads();
     const int64_t row = ((int64_t)b * a.c.Hkv + kvh) * a.c.cap;
     const float *sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.c.cap;
-    for (int64_t s = s0 + threadIdx.x; s < min(s0 + kWeightSlots, len); s += kJoinThreads) {
-        float x = 0.f;
-        for (int h = 0; h < a.G; ++h) x = fmaf(ex2(sc[h * a.c.cap + s] - stat[h].x), stat[h].y, x);
-        a.weight_out[row + s] = (a.weight_in != nullptr ? a.weight_in[row + s] : 0.f) + x;
+    constexpr int P = kWeightSlots / kJoinThreads;
+    float x[P] = {};
+#pragma unroll 2
+    for (int h = 0; h < a.G; ++h) {
+        const float2 ml = stat[h];
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+            const int64_t s = s0 + threadIdx.x + e * kJoinThreads;
+            if (s < len) x[e] = fmaf(ex2(sc[h * a.c.cap + s] - ml.x), ml.y, x[e]);
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+        const int64_t s = s0 + threadIdx.x + e * kJoinThreads;
+        if (s < len) a.weight_out[row + s] = (a.weight_in != nullptr ? a.weight_in[row + s] : 0.f) + x[e];
     }
 }
 
-template <typename T, bool SPLIT, int D, int QB>
+template <typename T, bool SPLIT, int D>
 cudaError_t launch_part(const Cache4AttendArgs &a, cudaStream_t s)
 {
-    auto kern = k_cache4_attend<T, SPLIT, D, QB>;
-    constexpr int bytes = std::max(Lay<D>::BYTES, kWarps * 8 * QB * (D * 4 + 8));
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
-    const int blocks = (a.G + 8 * QB - 1) / (8 * QB);
-    kern<<<dim3((unsigned)a.n_chunks, (unsigned)(a.c.Hkv * blocks), (unsigned)a.c.B), kThreads, bytes, s>>>(a);
+    auto kern = k_cache4_attend<T, SPLIT, D>;
+    constexpr int bytes = Lay<D, SPLIT>::BYTES;
+    static std::once_flag once;
+    static cudaError_t ready = cudaSuccess;
+    std::call_once(once, [&] { ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    if (ready != cudaSuccess) return ready;
+    kern<<<(unsigned)a.ctas, kThreads, bytes, s>>>(a);
     note_launch();
     return cudaGetLastError();
 }
 template <typename T, bool SPLIT>
 cudaError_t launch_part_d(const Cache4AttendArgs &a, cudaStream_t s)
 {
-    if (a.G > 8) return a.c.D == 128 ? launch_part<T, SPLIT, 128, 2>(a, s) : launch_part<T, SPLIT, 64, 2>(a, s);
-    return a.c.D == 128 ? launch_part<T, SPLIT, 128, 1>(a, s) : launch_part<T, SPLIT, 64, 1>(a, s);
+    return a.c.D == 128 ? launch_part<T, SPLIT, 128>(a, s) : launch_part<T, SPLIT, 64>(a, s);
+}
+template <typename TO, int D>
+cudaError_t launch_join_d(const Cache4AttendArgs &a, cudaStream_t s)
+{
+    const int64_t blocks = a.weight_out != nullptr ? (a.reach + kWeightSlots - 1) / kWeightSlots * a.c.Hkv : 0;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.Hq + blocks), (unsigned)a.c.B);
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = a.weight_out != nullptr ? a.G * sizeof(float2) : 0;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_cache4_join<TO, D>, a);
+    note_launch();
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 template <typename TO>
 cudaError_t launch_join(const Cache4AttendArgs &a, cudaStream_t s)
 {
-    const int64_t blocks = a.weight_out != nullptr ? (a.reach + kWeightSlots - 1) / kWeightSlots * a.c.Hkv : 0;
-    const dim3 grid((unsigned)(a.Hq + blocks), 1, (unsigned)a.c.B);
-    const size_t bytes = a.weight_out != nullptr ? a.G * sizeof(float2) : 0;
-    if (a.c.D == 128)
-        k_cache4_join<TO, 128><<<grid, kJoinThreads, bytes, s>>>(a);
-    else
-        k_cache4_join<TO, 64><<<grid, kJoinThreads, bytes, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    return a.c.D == 128 ? launch_join_d<TO, 128>(a, s) : launch_join_d<TO, 64>(a, s);
 }
 
 }  // namespace
@@ -738,12 +943,12 @@ cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStrea
 
 cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_t count, float *k, float *v, cudaStream_t s)
 {
-    const int64_t n = (int64_t)c.B * c.Hkv * count * (c.D / 4);
-    const dim3 grid((unsigned)((n + kReadThreads - 1) / kReadThreads), 2);
+    const int blocks = (int)((count + kReadRows - 1) / kReadRows);
+    const dim3 grid((unsigned)((int64_t)c.B * c.Hkv * blocks), 2);
     if (c.D == 128)
-        k_cache4_read<128><<<grid, kReadThreads, 0, s>>>(c, first, count, k, v);
+        k_cache4_read<128><<<grid, kReadThreads, 0, s>>>(c, first, count, blocks, k, v);
     else
-        k_cache4_read<64><<<grid, kReadThreads, 0, s>>>(c, first, count, k, v);
+        k_cache4_read<64><<<grid, kReadThreads, 0, s>>>(c, first, count, blocks, k, v);
     note_launch();
     return cudaGetLastError();
 }

@@ -22,38 +22,77 @@ __device__ __forceinline__ uint32_t order_of(float w)
 }
 
 constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kMaxCluster = 8;
+constexpr int kBins = 2048, kPasses = 3;  // digits of 11, 11 and 10 bits, from the top
+constexpr int kCachedSlots = 20480;       // slots of a CTA whose order and position fit its shared memory
 
-// Sum over the block of x, and this thread's exclusive prefix.
-__device__ __forceinline__ int block_scan(int x, int &total)
+struct Exchange {  // what the CTAs of a cluster read of one another
+    int newest, recent, holes, movers;
+    uint32_t hist[kPasses][kBins];
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void cluster_sync()
 {
-    __shared__ int part[kWarps];
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the word at `p` (of this CTA's shared memory) in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t ld_cluster(const void *p, int rank)
+{
+    uint32_t at, x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+    return x;
+}
+
+// Sums of (x, y) over the block, and this thread's exclusive prefixes.
+struct Pair {
+    int x, y;
+};
+__device__ __forceinline__ Pair block_scan(Pair v, Pair &total, Pair *part)
+{
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = x;
+    Pair inc = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xFFFFFFFFu, inc, o);
-        if (lane >= o) inc += y;
+        const int a = __shfl_up_sync(0xFFFFFFFFu, inc.x, o), b = __shfl_up_sync(0xFFFFFFFFu, inc.y, o);
+        if (lane >= o) {
+            inc.x += a;
+            inc.y += b;
+        }
     }
     __syncthreads();
     if (lane == 31) part[warp] = inc;
     __syncthreads();
-    int before = 0, all = 0;
+    Pair w = part[lane];  // (kWarps == 32)
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        before += w < warp ? part[w] : 0;
-        all += part[w];
+    for (int o = 1; o < 32; o <<= 1) {
+        const int a = __shfl_up_sync(0xFFFFFFFFu, w.x, o), b = __shfl_up_sync(0xFFFFFFFFu, w.y, o);
+        if (lane >= o) {
+            w.x += a;
+            w.y += b;
+        }
     }
-    total = all;
-    return before + inc - x;
+    total = {__shfl_sync(0xFFFFFFFFu, w.x, 31), __shfl_sync(0xFFFFFFFFu, w.y, 31)};
+    const int bx = __shfl_sync(0xFFFFFFFFu, w.x, (warp + 31) & 31), by = __shfl_sync(0xFFFFFFFFu, w.y, (warp + 31) & 31);
+    return {(warp ? bx : 0) + inc.x - v.x, (warp ? by : 0) + inc.y - v.y};
 }
 
-// One CTA per (sequence, KV head): the newest position, the threshold weight by four passes over
-// eight bits each, then the lists in slot order. holes: [B * Hkv][budget] scratch.
-__global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs a, int32_t *holes)
+// One cluster of `size` CTAs per (sequence, KV head), each with a run of its slots: the newest position, then the
+// threshold weight by three passes of a radix select (histograms in shared memory, summed over the cluster
+// by every CTA for itself), then the lists. A slot's order and position are read from memory once and
+// stay in shared memory (CACHED). Ties at the threshold go to the lowest slots: the last histogram says how many of
+// them each CTA holds. holes: [B * Hkv][budget] scratch, the freed slots in order. Bound by latency: seven
+// cluster barriers and about as many block scans.
+template <bool CACHED>
+__global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs a, int32_t *holes, int size)
 {
-    __shared__ int hist[256];
-    __shared__ int sh_max, sh_digit, sh_need;
-    const int bh = blockIdx.x, b = bh / a.src.Hkv, tid = threadIdx.x;
+    extern __shared__ uint2 slots[];  // CACHED: (order, position)
+    __shared__ Exchange ex;
+    __shared__ Pair part[kWarps];
+    __shared__ int sh_digit, sh_need;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int bh = blockIdx.x / size, rank = blockIdx.x % size, b = bh / a.src.Hkv, tid = threadIdx.x;
     const int len = max(0, (int)min((int64_t)a.src.length[b], a.src.cap));
     const int left = min(len, a.budget);
     const float *weight = a.src.weight + bh * a.src.cap;
@@ -61,128 +100,264 @@ __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs
     int32_t *kept = a.kept + (int64_t)bh * a.budget;
     holes += (int64_t)bh * a.budget;
     if (len <= a.budget) {
-        for (int j = tid; j < a.budget; j += kThreads) kept[j] = j < len ? j : -1;
+        for (int j = rank * kThreads + tid; j < a.budget; j += size * kThreads) kept[j] = j < len ? j : -1;
         return;
     }
-    if (tid == 0) sh_max = INT32_MIN;
+    // this CTA's slots: c0 .. c0 + n - 1
+    const int per = (len + size - 1) / size, c0 = min(len, rank * per), n = min(len, c0 + per) - c0;
+    for (int i = tid; i < kPasses * kBins; i += kThreads) (&ex.hist[0][0])[i] = 0u;
+    if (tid == 0) {
+        ex.newest = INT32_MIN;
+        ex.recent = 0;
+    }
     __syncthreads();
     int newest = INT32_MIN;
-    for (int j = tid; j < len; j += kThreads) newest = max(newest, pos[j]);
-    atomicMax(&sh_max, newest);
-    __syncthreads();
-    const int64_t line = (int64_t)sh_max - a.recent;  // newer than this: recent
-    int mine = 0, n_recent;
-    for (int j = tid; j < len; j += kThreads) mine += pos[j] > line;
-    block_scan(mine, n_recent);
-    // the threshold lies among the recent slots (all of the budget goes to them) or among the others
+    for (int i = tid; i < n; i += kThreads) {
+        const int p = pos[c0 + i];
+        if (CACHED) slots[i] = make_uint2(order_of(weight[c0 + i]), (uint32_t)p);
+        newest = max(newest, p);
+    }
+    newest = __reduce_max_sync(0xFFFFFFFFu, newest);
+    if ((tid & 31) == 0) atomicMax(&ex.newest, newest);
+    auto slot_at = [&](int i) -> uint2 { return CACHED ? slots[i] : make_uint2(order_of(weight[c0 + i]), (uint32_t)pos[c0 + i]); };
+    cluster_sync();
+    newest = INT32_MIN;
+    for (int r = 0; r < size; ++r) newest = max(newest, (int)ld_cluster(&ex.newest, r));
+    const int64_t line = (int64_t)newest - a.recent;  // newer than this: recent
+    auto is_recent = [&](uint2 s) { return (int64_t)(int32_t)s.y > line; };
+
+    // the first histogram, of the slots that are not recent, and how many are
+    int mine = 0;
+    for (int i = tid; i < n; i += kThreads) {
+        const uint2 s = slot_at(i);
+        if (is_recent(s))
+            ++mine;
+        else
+            atomicAdd(&ex.hist[0][s.x >> 21], 1u);
+    }
+    mine = __reduce_add_sync(0xFFFFFFFFu, mine);
+    if ((tid & 31) == 0 && mine > 0) atomicAdd(&ex.recent, mine);
+    cluster_sync();
+    int n_recent = 0;
+    for (int r = 0; r < size; ++r) n_recent += (int)ld_cluster(&ex.recent, r);
+    // the threshold lies among the others (recent slots all stay), or where those are too many among the recent
     const bool among_recent = n_recent >= a.budget;
     int need = among_recent ? a.budget : a.budget - n_recent;  // slots to take of that class
-    uint32_t prefix = 0, mask = 0;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
+    if (among_recent) {
+        cluster_sync();  // (the histogram is built again: nobody reads the first one any more)
+        for (int i = tid; i < kBins; i += kThreads) ex.hist[0][i] = 0u;
         __syncthreads();
-        for (int j = tid; j < len; j += kThreads) {
-            if ((pos[j] > line) != among_recent) continue;
-            const uint32_t u = order_of(weight[j]);
-            if ((u & mask) == prefix) atomicAdd(&hist[(u >> shift) & 255], 1);
+        for (int i = tid; i < n; i += kThreads) {
+            const uint2 s = slot_at(i);
+            if (is_recent(s)) atomicAdd(&ex.hist[0][s.x >> 21], 1u);
         }
-        __syncthreads();
-        if (tid == 0) {
-            int d = 255, n = need;
-            while (d > 0 && hist[d] < n) n -= hist[d--];
-            sh_digit = d;
-            sh_need = n;
+        cluster_sync();
+    }
+    uint32_t prefix = 0;
+    int ties_before = 0;  // ties in the CTAs before this one
+#pragma unroll 1
+    for (int pass = 0; pass < kPasses; ++pass) {
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+        if (pass > 0) {
+            const int above = pass == 1 ? 21 : 10, bits = pass == 1 ? 0x7FF : 0x3FF;
+            for (int i = tid; i < n; i += kThreads) {
+                const uint2 s = slot_at(i);
+                if (is_recent(s) == among_recent && s.x >> above == prefix >> above) atomicAdd(&ex.hist[pass][(s.x >> shift) & bits], 1u);
+            }
+            cluster_sync();
+        }
+        // bins from the top: thread t takes bins top - 2 t and the one below
+        constexpr int PB = kBins / kThreads;
+        int cnt[PB] = {}, sum = 0;
+#pragma unroll
+        for (int e = 0; e < PB; ++e) {
+            const int bin = kBins - 1 - PB * tid - e;
+            uint32_t x[kMaxCluster];
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) x[r] = r < size ? ld_cluster(&ex.hist[pass][bin], r) : 0u;
+#pragma unroll
+            for (int r = 0; r < kMaxCluster; ++r) cnt[e] += (int)x[r];
+            sum += cnt[e];
+        }
+        Pair total;
+        int before = block_scan({sum, 0}, total, part).x;
+#pragma unroll
+        for (int e = 0; e < PB; ++e) {
+            if (before < need && need <= before + cnt[e]) {
+                sh_digit = kBins - 1 - PB * tid - e;
+                sh_need = need - before;
+            }
+            before += cnt[e];
         }
         __syncthreads();
         prefix |= (uint32_t)sh_digit << shift;
-        mask |= 255u << shift;
         need = sh_need;
+        if (pass == kPasses - 1)
+            for (int r = 0; r < rank; ++r) ties_before += (int)ld_cluster(&ex.hist[pass][sh_digit], r);
         __syncthreads();
     }
-    // slots above the threshold stay, and of those at it the first `need`
-    int ties = 0, n_holes = 0, n_moved = 0;
-    for (int j0 = 0; j0 < len; j0 += kThreads) {
-        const int j = j0 + tid;
-        bool keep = false, tie = false;
-        if (j < len) {
-            const bool rec = pos[j] > line;
-            const uint32_t u = order_of(weight[j]);
-            if (rec != among_recent)
-                keep = rec;
-            else {
-                keep = u > prefix;
-                tie = u == prefix;
-            }
-        }
-        int n;
-        const int before = block_scan(tie, n);
-        if (tie && ties + before < need) keep = true;
-        ties += n;
-        const bool hole = j < left && !keep;
-        const int h = block_scan(hole, n);
-        if (hole) holes[n_holes + h] = j;
-        if (j < left && keep) kept[j] = j;
-        n_holes += n;
-        // movers are met after every slot below the budget, so after every hole (which the scans'
-        // barriers order within the block)
-        const bool moved = j < len && j >= left && keep;
-        const int r = block_scan(moved, n);
-        if (moved) kept[holes[n_moved + r]] = j;
-        n_moved += n;
+
+    // Slots above the threshold stay, and of those at it the first `need`. A thread takes a run of slots.
+    const int run = (n + kThreads - 1) / kThreads, i0 = min(n, tid * run), i1 = min(n, i0 + run);
+    auto state = [&](uint2 s) { return is_recent(s) != among_recent ? (is_recent(s) ? 2 : 0) : s.x > prefix ? 2 : s.x == prefix ? 1 : 0; };
+    Pair total;
+    int ties = 0;
+    for (int i = i0; i < i1; ++i) ties += state(slot_at(i)) == 1;
+    const int ties_at = ties_before + block_scan({ties, 0}, total, part).x;
+    Pair own = {0, 0};
+    int t = ties_at;
+    for (int i = i0; i < i1; ++i) {
+        const int st = state(slot_at(i));
+        const bool keep = st == 2 || (st == 1 && t++ < need);
+        if (c0 + i < left)
+            own.x += !keep;
+        else
+            own.y += keep;
+    }
+    Pair at = block_scan(own, total, part);
+    if (tid == 0) {
+        ex.holes = total.x;
+        ex.movers = total.y;
+    }
+    cluster_sync();
+    for (int r = 0; r < rank; ++r) {
+        at.x += (int)ld_cluster(&ex.holes, r);
+        at.y += (int)ld_cluster(&ex.movers, r);
+    }
+    t = ties_at;
+    int hole = at.x;
+    for (int i = i0; i < i1 && c0 + i < left; ++i) {
+        const int st = state(slot_at(i));
+        if (st == 2 || (st == 1 && t++ < need))
+            kept[c0 + i] = c0 + i;
+        else
+            holes[hole++] = c0 + i;
+    }
+    cluster_sync();  // every freed slot of the list is written
+    t = ties_at;
+    int mover = at.y;
+    for (int i = i0; i < i1; ++i) {
+        const int st = state(slot_at(i));
+        const bool keep = st == 2 || (st == 1 && t++ < need);
+        if (keep && c0 + i >= left) kept[__ldcg(&holes[mover++])] = c0 + i;
     }
 }
 
-// Moves the rows: 16 lanes to a slot of the target. Codes 16 bytes at a time; scales, position and weight by single
-// lanes. In place only what moves.
-constexpr int kMoveThreads = 256;
+// Moves the rows: four lanes to a slot of the target, kRows of them at once. In place only what moves. Bound by HBM: a row's codes,
+// scales, position and weight are read once and written once.
+constexpr int kMoveThreads = 256, kMoveRows = 2;
 template <int D>
-__global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictArgs a)
+__global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictArgs a, int blocks)
 {
-    constexpr int P = D / 32, LANES = 16;  // 16-byte pieces of a row's codes
-    const int64_t t = (int64_t)blockIdx.x * (kMoveThreads / LANES) + threadIdx.x / LANES;
-    const int u = threadIdx.x % LANES;
-    const int64_t n = (int64_t)a.src.B * a.src.Hkv * a.budget;
-    if (t < n) {
-        const int64_t bh = t / a.budget, j = t - bh * a.budget;
-        const int from = a.kept[t];
-        if (from >= 0 && !(a.in_place && from == j)) {
-            const int64_t rs = bh * a.src.cap + from, rd = bh * a.dst.cap + j;
-            if (u < P)
-                reinterpret_cast<uint4 *>(a.dst.k)[rd * P + u] = reinterpret_cast<const uint4 *>(a.src.k)[rs * P + u];
-            else if (u < 2 * P)
-                reinterpret_cast<uint4 *>(a.dst.v)[rd * P + u - P] = reinterpret_cast<const uint4 *>(a.src.v)[rs * P + u - P];
-            else if (u < 2 * P + P / 2)
-                reinterpret_cast<uint32_t *>(a.dst.k_scale)[rd * (P / 2) + u - 2 * P] =
-                    reinterpret_cast<const uint32_t *>(a.src.k_scale)[rs * (P / 2) + u - 2 * P];
-            else if (u < 3 * P)
-                reinterpret_cast<uint32_t *>(a.dst.v_scale)[rd * (P / 2) + u - 2 * P - P / 2] =
-                    reinterpret_cast<const uint32_t *>(a.src.v_scale)[rs * (P / 2) + u - 2 * P - P / 2];
-            else if (u == 3 * P)
-                a.dst.pos[rd] = a.src.pos[rs];
-            else if (u == 3 * P + 1)
-                a.dst.weight[rd] = a.src.weight[rs];
+    constexpr int PIECES = D / 32 / 2;  // 16-byte pieces of a row's codes, two lanes for the keys, two for the values
+    const int bh = blockIdx.x / blocks, u = threadIdx.x & 3;
+    const int first = (blockIdx.x - bh * blocks) * (kMoveThreads / 4 * kMoveRows) + threadIdx.x / 4;
+    // (nothing that the select kernel reads or writes is touched before it has finished)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool values = u >= 2;
+    const uint4 *sc = reinterpret_cast<const uint4 *>(values ? a.src.v : a.src.k);
+    uint4 *dc = reinterpret_cast<uint4 *>(values ? a.dst.v : a.dst.k);
+    int64_t rs[kMoveRows], rd[kMoveRows];
+    uint4 x[kMoveRows][PIECES];
+    uint32_t y[kMoveRows][D / 64];
+    bool go[kMoveRows];
+#pragma unroll
+    for (int e = 0; e < kMoveRows; ++e) {
+        const int j = first + e * (kMoveThreads / 4);
+        const int from = j < a.budget ? a.kept[(int64_t)bh * a.budget + j] : -1;
+        go[e] = from >= 0 && !(a.in_place && from == j);
+        rs[e] = bh * a.src.cap + max(from, 0);
+        rd[e] = bh * a.dst.cap + j;
+    }
+#pragma unroll
+    for (int e = 0; e < kMoveRows; ++e) {
+        if (!go[e]) continue;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) x[e][p] = sc[rs[e] * (2 * PIECES) + (u & 1) * PIECES + p];
+        // lane 0: position and key scales; 1: weight; 2: value scales
+        if (u == 0 || u == 2) {
+            const uint32_t *p = reinterpret_cast<const uint32_t *>(values ? a.src.v_scale : a.src.k_scale) + rs[e] * (D / 64);
+#pragma unroll
+            for (int g = 0; g < D / 64; ++g) y[e][g] = p[g];
+        } else {
+            y[e][0] = u == 1 ? reinterpret_cast<const uint32_t *>(a.src.weight)[rs[e]] : (uint32_t)a.src.pos[rs[e]];
         }
     }
-    if (blockIdx.x == 0)
+#pragma unroll
+    for (int e = 0; e < kMoveRows; ++e) {
+        if (!go[e]) continue;
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) dc[rd[e] * (2 * PIECES) + (u & 1) * PIECES + p] = x[e][p];
+        if (u == 0 || u == 2) {
+            uint32_t *p = reinterpret_cast<uint32_t *>(values ? a.dst.v_scale : a.dst.k_scale) + rd[e] * (D / 64);
+#pragma unroll
+            for (int g = 0; g < D / 64; ++g) p[g] = y[e][g];
+        } else if (u == 1) {
+            reinterpret_cast<uint32_t *>(a.dst.weight)[rd[e]] = y[e][0];
+        } else {
+            a.dst.pos[rd[e]] = (int32_t)y[e][0];
+        }
+    }
+    if (blockIdx.x == 0)  // (nobody reads the lengths any more)
         for (int b = threadIdx.x; b < a.src.B; b += kMoveThreads)
             a.dst.length[b] = max(0, min((int)min((int64_t)a.src.length[b], a.src.cap), a.budget));
+}
+
+template <bool CACHED>
+cudaError_t launch_select(const Cache4EvictArgs &a, int32_t *holes, int size, size_t bytes, cudaStream_t s)
+{
+    if (bytes > 0) {
+        const cudaError_t e = cudaFuncSetAttribute(k_evict_select<CACHED>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != cudaSuccess) return e;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(a.src.B * a.src.Hkv * size));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = size;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_evict_select<CACHED>, a, holes, size);
+    note_launch();
+    return e;
+}
+
+template <int D>
+cudaError_t launch_move(const Cache4EvictArgs &a, cudaStream_t s)
+{
+    const int blocks = (a.budget + kMoveThreads / 4 * kMoveRows - 1) / (kMoveThreads / 4 * kMoveRows);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((int64_t)blocks * a.src.B * a.src.Hkv));
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_evict_move<D>, a, blocks);
+    note_launch();
+    return e;
 }
 
 }  // namespace
 
 cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaStream_t s)
 {
-    k_evict_select<<<(unsigned)(a.src.B * a.src.Hkv), kThreads, 0, s>>>(a, holes);
-    cudaError_t e = cudaGetLastError();
-    note_launch();
+    // CTAs of a list: so many that a thread has about four slots, and all of them fit the cluster
+    int size = 1;
+    while (size < kMaxCluster && (int64_t)size * kThreads * 2 < a.src.cap) size *= 2;
+    const int64_t per = (a.src.cap + size - 1) / size;
+    cudaError_t e = per <= kCachedSlots ? launch_select<true>(a, holes, size, (size_t)per * sizeof(uint2), s)
+                                        : launch_select<false>(a, holes, size, 0, s);
     if (e != cudaSuccess) return e;
-    const int64_t n = (int64_t)a.src.B * a.src.Hkv * a.budget, per = kMoveThreads / 16;
-    if (a.src.D == 128)
-        k_evict_move<128><<<(unsigned)((n + per - 1) / per), kMoveThreads, 0, s>>>(a);
-    else
-        k_evict_move<64><<<(unsigned)((n + per - 1) / per), kMoveThreads, 0, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    e = a.src.D == 128 ? launch_move<128>(a, s) : launch_move<64>(a, s);
+    return e != cudaSuccess ? e : cudaGetLastError();
 }
 
 }  // namespace ris

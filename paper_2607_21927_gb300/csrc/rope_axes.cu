@@ -20,7 +20,7 @@
 namespace ris {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kBatch = 4;
 
 template <typename T>
 struct Vec;
@@ -94,18 +94,28 @@ __global__ void __launch_bounds__(kThreads) k_rope_axes(const RopeAxesArgs a)
         const int first = w == 0 ? 0 : a.heads[0], n = a.heads[w];
         const T *x = reinterpret_cast<const T *>(a.x[w]) + p * a.stride[w] + c;
         T *y = reinterpret_cast<T *>(a.y[w]) + p * (int64_t)n * a.D + c;
-#pragma unroll 4
-        for (int h = max(h0 - first, 0); h < min(h1 - first, n); ++h) {
-            float u[V], v[V], r[V], t[V];
-            Vec<T>::load(x + h * a.D, u);
-            Vec<T>::load(x + h * a.D + half, v);
+        // kBatch heads' loads ahead of their stores (which the compiler may not pass: they may be in place)
+        const int end = min(h1 - first, n);
+        for (int h = max(h0 - first, 0); h < end; h += kBatch) {
+            float u[kBatch][V], v[kBatch][V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                r[e] = fmaf(u[e], cs[e], -(v[e] * sn[e]));
-                t[e] = fmaf(v[e], cs[e], u[e] * sn[e]);
-            }
-            Vec<T>::store(y + h * a.D, r);
-            Vec<T>::store(y + h * a.D + half, t);
+            for (int i = 0; i < kBatch; ++i)
+                if (h + i < end) {
+                    Vec<T>::load(x + (h + i) * a.D, u[i]);
+                    Vec<T>::load(x + (h + i) * a.D + half, v[i]);
+                }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (h + i < end) {
+                    float r[V], t[V];
+#pragma unroll
+                    for (int e = 0; e < V; ++e) {
+                        r[e] = fmaf(u[i][e], cs[e], -(v[i][e] * sn[e]));
+                        t[e] = fmaf(v[i][e], cs[e], u[i][e] * sn[e]);
+                    }
+                    Vec<T>::store(y + (h + i) * a.D, r);
+                    Vec<T>::store(y + (h + i) * a.D + half, t);
+                }
         }
     }
 }

@@ -15,6 +15,7 @@ constexpr int kPackKeys = 128;      // keys of a key item
 constexpr int kMaxAxes = 4;
 constexpr int kCacheGroup = 32;     // elements that share a scale
 constexpr int kMaxPackSeqs = 65535;
+constexpr int kCacheUnit = 64;      // slots by which the attention over a 4-bit cache is shared out
 
 // A work item: rows row .. row + kPackRows - 1 (or keys) of a sequence. The sequence's own sizes ride
 // along, so that a CTA needs one 32-byte load to know everything about its item.
@@ -105,12 +106,11 @@ struct Cache4AttendArgs {
     int32_t Hq, G;
     float scale_log2;
     int64_t reach;               // slots that a sequence can hold: cap, or less where the caller knows better
-    int32_t chunk;               // slots of a CTA, a multiple of 16
-    int32_t n_chunks;            // CTAs of a (sequence, KV head)
-    float *part_o;               // [B][Hq][n_chunks][D]
-    float2 *part_ml;             // [B][Hq][n_chunks]
+    int32_t lists;               // (sequence, KV head, block of 8 query heads)
+    int32_t ctas;                // among which the slots are shared out
+    float *part_o;               // [ctas + lists][heads of a block][D]
+    float2 *part_ml;             // [ctas + lists][heads of a block]
     float *scores;               // weights: [B][Hq][cap] scores in log2
-    float2 *row_stat;            // weights: [B][Hq] (maximum in log2, 1 / sum)
 };
 cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s);
 

@@ -139,6 +139,37 @@ Cache4Args cache_args(const ris_cache4 *c)
     return a;
 }
 
+// The rotation frequencies of a configuration as fractions of a turn in 2^-64. A prefill's layers and a
+// generation's steps ask for the same ones again and again (64 powers, 3 us of host time): the calling thread's last ones are
+// kept, by value.
+ris_status rope_turns(const ris_rope_cfg *rope, int64_t n_ctx, int32_t head_dim, const uint64_t **turn, double *mscale)
+{
+    struct Last {
+        ris_rope_cfg cfg{};
+        int64_t n_ctx = -1;
+        int32_t head_dim = 0;
+        double mscale = 1.0;
+        uint64_t turn[kMaxHeadDimHalf] = {};
+    };
+    static thread_local Last last;
+    const ris_rope_cfg &c = last.cfg;
+    if (last.n_ctx != n_ctx || last.head_dim != head_dim || c.kind != rope->kind || c.reserved != rope->reserved ||
+        c.theta != rope->theta || c.native_len != rope->native_len || c.factor != rope->factor || c.yarn_alpha != rope->yarn_alpha ||
+        c.yarn_beta != rope->yarn_beta) {
+        double f[kMaxHeadDimHalf], ms = 1.0;
+        last.n_ctx = -1;
+        RIS_TRY(ris_rope_freqs(rope, n_ctx, head_dim, f, &ms));
+        for (int i = 0; i < head_dim / 2; ++i) last.turn[i] = (uint64_t)(f[i] * (18446744073709551616.0 / 6.283185307179586476925286766559));
+        last.cfg = *rope;
+        last.head_dim = head_dim;
+        last.mscale = ms;
+        last.n_ctx = n_ctx;
+    }
+    *turn = last.turn;
+    *mscale = last.mscale;
+    return RIS_OK;
+}
+
 double log2e_over_sqrt(int32_t head_dim) { return 1.4426950408889634074 / std::sqrt((double)head_dim); }
 
 // The items of `step` rows (or keys) of every sequence; of rows, those with the most keys first, so that the
@@ -291,8 +322,9 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
         return fail(RIS_ERR_INVALID, "the sections hold %lld frequencies, not head_dim / 2 = %d", (long long)sum, head_dim / 2);
     if (rope == nullptr || rope->kind == RIS_ROPE_NONE) return fail(RIS_ERR_INVALID, "rope is NULL or of kind NONE");
     RopeAxesArgs a{};
-    double f[kMaxHeadDimHalf], ms = 1.0;
-    RIS_TRY(ris_rope_freqs(rope, n_ctx, head_dim, f, &ms));
+    const uint64_t *turn = nullptr;
+    double ms = 1.0;
+    RIS_TRY(rope_turns(rope, n_ctx, head_dim, &turn, &ms));
     if (n > 0) {
         RIS_TRY(check_ptr(q, "q"));
         RIS_TRY(check_ptr(q_out, "q_out"));
@@ -308,7 +340,7 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
             return fail(RIS_ERR_INVALID, "in place only where the heads of a token follow the last one's");
     }
     if (n == 0) return RIS_OK;
-    for (int c = 0; c < head_dim / 2; ++c) a.turn[c] = (uint64_t)(f[c] * (18446744073709551616.0 / 6.283185307179586476925286766559));
+    std::copy(turn, turn + head_dim / 2, a.turn);
     if (interleaved) {
         // frequency c goes to axis c mod axes while that axis has any left, else to the first axis
         for (int c = 0; c < head_dim / 2; ++c) {
@@ -441,8 +473,7 @@ ris_status ris_cache4_read(const ris_cache4 *cache, const int32_t *first, int64_
     if (count == 0) return RIS_OK;
     RIS_TRY(check_ptr(k, "k"));
     RIS_TRY(check_ptr(v, "v"));
-    const int64_t threads = (int64_t)cache->batch * cache->kv_heads * count * (cache->head_dim / 4);
-    if (threads / 256 >= 2147483647LL) return fail(RIS_ERR_UNSUPPORTED, "too many rows for one call");
+    if ((int64_t)cache->batch * cache->kv_heads * ((count + 63) / 64) > 2147483647LL) return fail(RIS_ERR_UNSUPPORTED, "too many rows for one call");
     RIS_CUDA(launch_cache4_read(cache_args(cache), first, count, k, v, reinterpret_cast<cudaStream_t>(stream)));
     return RIS_OK;
 }
@@ -474,12 +505,14 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
     a.G = heads / cache->kv_heads;
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
     a.reach = longest > 0 ? longest : cache->capacity;
-    // ranges: three CTAs per SM, of at least 64 slots
-    const int64_t lists = (int64_t)cache->batch * cache->kv_heads * ((a.G + 15) / 16);
-    const int64_t per = (a.reach * lists + 455) / 456;
-    a.chunk = (int32_t)std::min<int64_t>(std::max<int64_t>(64, (per + 63) / 64 * 64), (a.reach + 63) / 64 * 64);
-    a.n_chunks = (int32_t)((a.reach + a.chunk - 1) / a.chunk);
-    const size_t parts = (size_t)cache->batch * heads * a.n_chunks;
+    constexpr int32_t block = 8;
+    const int64_t lists = (int64_t)cache->batch * cache->kv_heads * ((a.G + block - 1) / block);
+    if (lists > (int64_t(1) << 24)) return fail(RIS_ERR_UNSUPPORTED, "batch x kv_heads = %lld lists", (long long)lists);
+    a.lists = (int32_t)lists;
+    // as many CTAs as are resident at once (cache4.cu's launch bounds), fewer where there are not as many units
+    constexpr int per_sm = 3;
+    a.ctas = (int32_t)std::min<int64_t>(152 * per_sm, lists * ((a.reach + kCacheUnit - 1) / kCacheUnit));
+    const size_t parts = ((size_t)a.ctas + (size_t)lists) * block;
     const size_t o_b = room(sizeof(float) * parts * cache->head_dim), ml_b = room(sizeof(float2) * parts);
     const size_t score_b = weight_out != nullptr ? sizeof(float) * (size_t)cache->batch * heads * cache->capacity : 0;
     Scratch mem;
@@ -509,6 +542,9 @@ ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_
         if ((x[i] == y[i]) != same) return fail(RIS_ERR_INVALID, "src and dst share some of their arrays");
     if (same && src->capacity != dst->capacity) return fail(RIS_ERR_INVALID, "in place, but the capacities differ");
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const int64_t lists = (int64_t)src->batch * src->kv_heads;
+    if (lists > (int64_t(1) << 24) || lists * (budget / 128 + 1) > 2147483647LL)
+        return fail(RIS_ERR_UNSUPPORTED, "batch x kv_heads = %lld lists of %d slots", (long long)lists, budget);
     Cache4EvictArgs a{};
     a.src = cache_args(src);
     a.dst = cache_args(dst);

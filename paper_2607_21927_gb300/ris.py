@@ -7,6 +7,7 @@ if ``libris.so`` is missing or no CUDA device is present the call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import threading
 from typing import Optional, Sequence
@@ -146,6 +147,8 @@ _SIGS = {
 def lib():
     """Load libris.so (raises if it was not built; there is no fallback)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -159,7 +162,7 @@ def lib():
             L.ris_last_error.restype = ctypes.c_char_p
             L.ris_launch_count.restype = ctypes.c_int64
             L.ris_version.restype = ctypes.c_char_p
-            _lib = L
+            _lib = L  # (published last: complete for a thread that does not take the lock)
     return _lib
 
 
@@ -635,30 +638,76 @@ def ris_pack_create(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = Non
     return Pack(h)
 
 
-def _token_stride(x: torch.Tensor, name: str) -> int:
-    """Elements from token to token of x [n, H, D] whose heads lie side by side."""
+# The calls below are made per layer and per generated token, some of them for a few microseconds of GPU work:
+# checks first, then plain integers into the C call.
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(stream, x: torch.Tensor) -> int:
+    return torch._C._cuda_getCurrentRawStream(x.get_device()) if stream is None else stream.cuda_stream
+
+
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _code(t: torch.Tensor) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
+
+
+def _heads(x: torch.Tensor, name: str):
+    """(n, H, D, elements from token to token) of x [n, H, D] whose heads lie side by side."""
     n, H, D = x.shape
-    if not x.is_cuda or (x.numel() > 0 and ((D > 1 and x.stride(2) != 1) or (H > 1 and x.stride(1) != D))):
+    st = x.stride()
+    if not x.is_cuda or (n > 0 and ((D > 1 and st[2] != 1) or (H > 1 and st[1] != D))):
         raise ValueError(f"{name}: [n, H, D] on the GPU, each token's heads side by side")
-    return x.stride(0) if n > 1 else H * D
+    return n, H, D, st[0] if n > 1 else H * D
+
+
+def _out(out, shape, dtype, device):
+    if out is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    assert out.is_cuda and out.is_contiguous() and tuple(out.shape) == tuple(shape)
+    return out
+
+
+def _ints(x: torch.Tensor, n: int, name: str) -> int:
+    if x.dtype != torch.int32 or not x.is_cuda or not x.is_contiguous() or x.numel() != n:
+        raise ValueError(f"{name}: {n} contiguous int32 on the GPU")
+    return x.data_ptr()
+
+
+@functools.lru_cache(maxsize=64)
+def _sections(sections: tuple):
+    return (ctypes.c_int32 * len(sections))(*sections)
 
 
 def ris_rope_axes(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, sections: Sequence[int], n_ctx: int,
                   rope: RopeCfg, interleaved: bool = False, inverse: bool = False, q_out=None, k_out=None, stream=None):
     """q [n, Hq, D] and k [n, Hkv, D] (or None) rotated at positions [axes, n] (int32): (q_out, k_out)."""
-    n, Hq, D = q.shape
-    Hkv = 0 if k is None else k.shape[1]
-    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32
-    assert tuple(positions.shape) == (len(sections), n), "positions: [axes, n]"
-    assert k is None or (k.shape[0] == n and k.shape[2] == D and k.dtype == q.dtype)
-    q_out = _alloc_out(q_out, (n, Hq, D), q.dtype, q.device)
-    k_out = None if k is None else _alloc_out(k_out, (n, Hkv, D), q.dtype, q.device)
-    assert q_out.dtype == q.dtype and (k is None or k_out.dtype == q.dtype)
-    sec = (ctypes.c_int32 * len(sections))(*[int(x) for x in sections])
-    _check("ris_rope_axes", lib().ris_rope_axes(
-        _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), _dtype(q), n, Hq, Hkv, D, _token_stride(q, "q"),
-        0 if k is None else _token_stride(k, "k"), _ptr(positions), len(sections), sec, int(bool(interleaved)), int(n_ctx),
-        _ref(rope), int(bool(inverse)), _stream(stream)))
+    n, Hq, D, qs = _heads(q, "q")
+    axes = len(sections)
+    if positions.dim() != 2 or positions.shape[0] != axes:
+        raise ValueError("positions: [axes, n]")
+    pos = _ints(positions, axes * n, "positions")
+    q_out = _out(q_out, (n, Hq, D), q.dtype, q.device)
+    Hkv = ks = 0
+    if k is not None:
+        m, Hkv, Dk, ks = _heads(k, "k")
+        assert m == n and Dk == D and k.dtype == q.dtype, "k: the tokens, head dim and type of q"
+        k_out = _out(k_out, (n, Hkv, D), q.dtype, q.device)
+        assert k_out.dtype == q.dtype
+    else:
+        k_out = None
+    assert q_out.dtype == q.dtype
+    st = lib().ris_rope_axes(q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), _code(q), n, Hq, Hkv, D, qs, ks, pos, axes,
+                             _sections(tuple(sections)), int(interleaved), int(n_ctx), _ref(rope), int(inverse),
+                             _raw_stream(stream, q))
+    if st:
+        _check("ris_rope_axes", st)
     return q_out, k_out
 
 
@@ -666,16 +715,17 @@ def ris_attention_packed(pack: Pack, q, k, v, out: Optional[torch.Tensor] = None
                          weight_rows: int = 0, stream=None):
     """Causal attention over a pack's sequences, always a tuple: out [q_total, Hq, D], then lse [Hq, q_total]
     (return_lse) and key_weight [Hkv, k_total] (weight_rows > 0). q, k, v may be views into a fused projection's rows."""
-    (n, Hq, D), (m, Hkv, _) = q.shape, k.shape
+    (n, Hq, D, qs), (m, Hkv, Dk, ks), (mv, Hv, Dv, vs) = _heads(q, "q"), _heads(k, "k"), _heads(v, "v")
     if n != pack.q_total or m != pack.k_total:
         raise ValueError(f"q has {n} tokens and k {m}, the pack {pack.q_total} and {pack.k_total}")
-    assert k.shape == v.shape and k.shape[2] == D and q.dtype == k.dtype == v.dtype
-    out = _alloc_out(out, (n, Hq, D), out_dtype or q.dtype, q.device)
+    assert (m, Hkv, Dk) == (mv, Hv, Dv) and Dk == D and q.dtype == k.dtype == v.dtype, "k and v alike, of q's head dim and type"
+    out = _out(out, (n, Hq, D), out_dtype or q.dtype, q.device)
     lse = torch.empty((Hq, n), dtype=torch.float32, device=q.device) if return_lse else None
     kw = torch.empty((Hkv, m), dtype=torch.float32, device=q.device) if weight_rows > 0 else None
-    _check("ris_attention_packed", lib().ris_attention_packed(
-        pack.handle, _ptr(q), _ptr(k), _ptr(v), _ptr(out), Hq, Hkv, D, _token_stride(q, "q"), _token_stride(k, "k"),
-        _token_stride(v, "v"), _dtype(q), _dtype(out), _ptr(lse), int(weight_rows), _ptr(kw), _stream(stream)))
+    st = lib().ris_attention_packed(pack.handle, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), Hq, Hkv, D, qs, ks, vs,
+                                    _code(q), _code(out), _addr(lse), int(weight_rows), _addr(kw), _raw_stream(stream, q))
+    if st:
+        _check("ris_attention_packed", st)
     return (out,) + ((lse,) if return_lse else ()) + ((kw,) if weight_rows > 0 else ())
 
 
@@ -687,7 +737,7 @@ class _Cache4Desc(ctypes.Structure):
 
 
 class Cache4:
-    """A K/V cache held in 4 bits (ris_cache4): the tensors, which the caller may read and set, and their
+    """A K/V cache held in 4 bits (ris_cache4): the tensors, which the caller may read and set (in place), and their
     descriptor. k, v uint8 [B, Hkv, capacity, D/2]; k_scale, v_scale bf16 [.., D/32]; pos int32 and weight fp32
     [B, Hkv, capacity]; length int32 [B]."""
 
@@ -707,6 +757,7 @@ class Cache4:
         self.sync = torch.zeros(4, dtype=torch.int32, device=k.device)
         self.desc = _Cache4Desc(B, H, 2 * half, 0, cap, *(getattr(self, n).data_ptr() for n in
                                                           ("k", "v", "k_scale", "v_scale", "pos", "weight", "length", "sync")))
+        self._ref = ctypes.byref(self.desc)
 
     @classmethod
     def empty(cls, batch: int, kv_heads: int, head_dim: int, capacity: int, device="cuda") -> "Cache4":
@@ -724,30 +775,29 @@ class Cache4:
 def ris_cache4_append(cache: Cache4, pack: Pack, k, v, positions: torch.Tensor, weight: Optional[torch.Tensor] = None,
                       start: Optional[torch.Tensor] = None, stream=None) -> None:
     """The pack's rows k, v [q_total, Hkv, D] into the cache, after the slots in use or at start [B] (int32)."""
-    n, H, D = k.shape
-    if n != pack.q_total or (H, D) != (cache.kv_heads, cache.head_dim):
-        raise ValueError(f"k is {tuple(k.shape)}, the pack has {pack.q_total} rows, the cache heads "
+    (n, H, D, ks), (nv, Hv, Dv, vs) = _heads(k, "k"), _heads(v, "v")
+    if n != pack.q_total or H != cache.kv_heads or D != cache.head_dim or (nv, Hv, Dv) != (n, H, D):
+        raise ValueError(f"k is {tuple(k.shape)}, v {tuple(v.shape)}, the pack has {pack.q_total} rows, the cache heads "
                          f"{cache.kv_heads} x {cache.head_dim}")
-    assert k.shape == v.shape and k.dtype == v.dtype
-    assert positions.is_cuda and positions.is_contiguous() and positions.dtype == torch.int32 and positions.numel() == n
+    assert k.dtype == v.dtype
     if weight is not None:
         assert weight.is_cuda and weight.is_contiguous() and weight.dtype == torch.float32 and tuple(weight.shape) == (H, n)
-    if start is not None:
-        assert start.is_cuda and start.is_contiguous() and start.dtype == torch.int32 and start.numel() == cache.batch
-    _check("ris_cache4_append", lib().ris_cache4_append(
-        ctypes.byref(cache.desc), pack.handle, _ptr(k), _ptr(v), _token_stride(k, "k"), _token_stride(v, "v"), _dtype(k),
-        _ptr(positions), _ptr(weight), _ptr(start), _stream(stream)))
+    st = lib().ris_cache4_append(cache._ref, pack.handle, k.data_ptr(), v.data_ptr(), ks, vs, _code(k),
+                                 _ints(positions, n, "positions"), _addr(weight),
+                                 None if start is None else _ints(start, cache.batch, "start"), _raw_stream(stream, k))
+    if st:
+        _check("ris_cache4_append", st)
 
 
 def ris_cache4_read(cache: Cache4, first: Optional[torch.Tensor] = None, count: Optional[int] = None, stream=None):
     """The values of slots first[b] .. first[b] + count - 1 (zeros past the length): k, v fp32 [B, Hkv, count, D]."""
     count = cache.capacity if count is None else int(count)
-    if first is not None:
-        assert first.is_cuda and first.is_contiguous() and first.dtype == torch.int32 and first.numel() == cache.batch
-    shape = (cache.batch, cache.kv_heads, count, cache.head_dim)
-    k, v = (torch.empty(shape, dtype=torch.float32, device=cache.k.device) for _ in range(2))
-    _check("ris_cache4_read", lib().ris_cache4_read(ctypes.byref(cache.desc), _ptr(first), count, _ptr(k), _ptr(v),
-                                                    _stream(stream)))
+    both = torch.empty((2, cache.batch, cache.kv_heads, count, cache.head_dim), dtype=torch.float32, device=cache.k.device)
+    k, v = both.unbind(0)
+    st = lib().ris_cache4_read(cache._ref, None if first is None else _ints(first, cache.batch, "first"), count, k.data_ptr(),
+                               v.data_ptr(), _raw_stream(stream, cache.k))
+    if st:
+        _check("ris_cache4_read", st)
     return k, v
 
 
@@ -757,25 +807,26 @@ def ris_cache4_attend(cache: Cache4, q: torch.Tensor, out=None, out_dtype=None, 
     """q [B, Hq, D], one token per sequence, over every slot in use: out [B, Hq, D] (and lse [B, Hq]).
     weight_out [B, Hkv, capacity] gets weight_in (or 0) plus this token's weights; pass cache.weight as both to add up."""
     B, Hq, D = q.shape
-    if (B, D) != (cache.batch, cache.head_dim):
-        raise ValueError(f"q is {tuple(q.shape)}, the cache has {cache.batch} sequences of head dim {cache.head_dim}")
-    assert q.is_cuda and q.is_contiguous()
-    out = _alloc_out(out, (B, Hq, D), out_dtype or q.dtype, q.device)
+    if B != cache.batch or D != cache.head_dim or not q.is_cuda or not q.is_contiguous():
+        raise ValueError(f"q: contiguous [{cache.batch}, heads, {cache.head_dim}] on the GPU, not {tuple(q.shape)}")
+    out = _out(out, (B, Hq, D), out_dtype or q.dtype, q.device)
     lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device) if return_lse else None
     for w in (weight_in, weight_out):
         if w is not None:
             assert w.is_cuda and w.is_contiguous() and w.dtype == torch.float32 and w.shape == cache.weight.shape
-    _check("ris_cache4_attend", lib().ris_cache4_attend(
-        ctypes.byref(cache.desc), _ptr(q), Hq, _dtype(q), _dtype(out), int(longest), _ptr(out), _ptr(lse), _ptr(weight_in),
-        _ptr(weight_out), _stream(stream)))
+    st = lib().ris_cache4_attend(cache._ref, q.data_ptr(), Hq, _code(q), _code(out), int(longest), out.data_ptr(), _addr(lse),
+                                 _addr(weight_in), _addr(weight_out), _raw_stream(stream, q))
+    if st:
+        _check("ris_cache4_attend", st)
     return (out, lse) if return_lse else out
 
 
 def ris_cache4_evict(src: Cache4, dst: Cache4, budget: int, recent: int, kept: Optional[torch.Tensor] = None, stream=None):
     """Cut src back to `budget` slots per sequence and head into dst (src itself: in place); returns the source
     slots kept [B, Hkv, budget] (int32, -1 where there is none)."""
-    kept = _alloc_out(kept, (src.batch, src.kv_heads, int(budget)), torch.int32, src.k.device)
+    kept = _out(kept, (src.batch, src.kv_heads, int(budget)), torch.int32, src.k.device)
     assert kept.dtype == torch.int32
-    _check("ris_cache4_evict", lib().ris_cache4_evict(ctypes.byref(src.desc), ctypes.byref(dst.desc), int(budget),
-                                                      int(recent), _ptr(kept), _stream(stream)))
+    st = lib().ris_cache4_evict(src._ref, dst._ref, int(budget), int(recent), kept.data_ptr(), _raw_stream(stream, kept))
+    if st:
+        _check("ris_cache4_evict", st)
     return kept
