@@ -27,40 +27,35 @@ __device__ unsigned int g_ris_cache4_error;
 
 namespace {
 
-template <typename T>
-__device__ __forceinline__ float to_f(T x);
-template <>
-__device__ __forceinline__ float to_f<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ float to_f<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
-
-// x[0 .. N-1], N elements in a row, N * sizeof(T) a multiple of 4 and the address aligned to it (up to 16)
+// N elements in a row as they lie in memory, N * sizeof(T) a multiple of 4 and the address aligned to it (up to 16)
 template <typename T, int N>
-__device__ __forceinline__ void load_row(const T *p, float *x)
-{
-    constexpr int B = N * (int)sizeof(T), W = B >= 16 ? 16 : B;
+struct Raw {
+    static constexpr int B = N * (int)sizeof(T), W = B >= 16 ? 16 : B;
     uint32_t w[B / 4];
+    __device__ __forceinline__ void load(const T *p)
+    {
 #pragma unroll
-    for (int i = 0; i < B / W; ++i) {
-        const char *at = reinterpret_cast<const char *>(p) + i * W;
-        if constexpr (W == 16) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(at);
-            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-        } else if constexpr (W == 8) {
-            const uint2 v = *reinterpret_cast<const uint2 *>(at);
-            w[2 * i] = v.x, w[2 * i + 1] = v.y;
-        } else {
-            w[i] = *reinterpret_cast<const uint32_t *>(at);
+        for (int i = 0; i < B / W; ++i) {
+            const char *at = reinterpret_cast<const char *>(p) + i * W;
+            if constexpr (W == 16) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(at);
+                w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+            } else if constexpr (W == 8) {
+                const uint2 v = *reinterpret_cast<const uint2 *>(at);
+                w[2 * i] = v.x, w[2 * i + 1] = v.y;
+            } else {
+                w[i] = *reinterpret_cast<const uint32_t *>(at);
+            }
         }
     }
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
+    __device__ __forceinline__ float operator[](int e) const
+    {
         if constexpr (sizeof(T) == 4)
-            x[e] = __uint_as_float(w[e]);
+            return __uint_as_float(w[e]);
         else
-            x[e] = __uint_as_float((e & 1) ? (w[e >> 1] & 0xFFFF0000u) : (w[e >> 1] << 16));
+            return __uint_as_float((e & 1) ? (w[e >> 1] & 0xFFFF0000u) : (w[e >> 1] << 16));
     }
-}
+};
 
 // |x| for a maximum that a NaN or an infinity must win: the bits without the sign
 __device__ __forceinline__ uint32_t mag(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
@@ -79,124 +74,123 @@ __device__ __forceinline__ uint32_t code2(float a, float b)
     asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u16.u8 %0, t;\n\t}" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
-// The codes of x / s rounded to fp32 first, as the format has it, without a division per value: the code is a
-// monotone function, so where x / s (1 - 2^-21) and x / s (1 + 2^-21), each good to 2^-22, have the same
-// code, the quotient between them has it too. Else (a value next to a limit) the division itself.
+// The codes of x / s, rounded to fp32 first as the format has it, without a division per value: with r = fl(1 / s), q = fl(x r)
+// and the exact remainder x - q s, fl(q + r (x - q s)) is the quotient but for a relative 2^-46 before its one
+// rounding (Markstein, IBM J. Res. Dev. 34, 1990). As the scale has 8 significant bits, a quotient that is no
+// fp32 number is at least 2^-33 of itself away from the middle of two, so the rounding is the division's own.
 struct Scale {
-    float s, lo, hi;  // the scale; 1 / s pulled down and up, or lo > hi where it is not to be used
-    __device__ __forceinline__ explicit Scale(float scale) : s(scale)
+    float s, r;
+    bool plain;  // the scale is outside the range where no step over- or underflows
+    __device__ __forceinline__ explicit Scale(float scale)
     {
-        const float r = __frcp_rn(scale);
-        lo = r * (1.f - 0x1p-21f);
-        hi = r * (1.f + 0x1p-21f);
-        if (!(scale >= 0x1p-100f && scale <= 0x1p100f)) lo = 1.f, hi = 0.f;
+        s = scale;
+        r = 1.f / scale;
+        plain = !(scale >= 0x1p-100f && scale <= 0x1p100f);
+    }
+    __device__ __forceinline__ float quotient(float x) const
+    {
+        const float q = x * r;
+        return fmaf(fmaf(-q, s, x), r, q);
     }
     __device__ __forceinline__ uint32_t codes(float a, float b) const
     {
-        const uint32_t c = code2(a * lo, b * lo);
-        if (c == code2(a * hi, b * hi) && lo <= hi) return c;
-        return s > 0.f ? code2(__fdiv_rn(a, s), __fdiv_rn(b, s)) : 0u;
+        if (plain) return s > 0.f ? code2(__fdiv_rn(a, s), __fdiv_rn(b, s)) : 0u;
+        return code2(quotient(a), quotient(b));
     }
 };
 
-constexpr int kAppendThreads = 256;
+// Four lanes to a row of keys and its row of values; each lane loads what it stores (16 or 8 bytes of codes in one
+// piece each), so rows are read and written in whole sectors; a group's maximum comes from its four lanes by shuffles.
+// Bound by HBM (a row is read once and D / 2 + D / 16 bytes of it written) where there are rows enough, and
+// else by the latency of one pass.
+constexpr int kAppendThreads = 128;
 
-// blockIdx.y 0: keys, four lanes to a row; 1: values, eight lanes to a row. Each lane loads what it
-// stores, so rows are read and written in whole sectors; a group's maximum comes from its lanes by
-// shuffles. Bound by HBM: a row is read once (2 D bytes of bf16) and D / 2 + D / 16 bytes are written.
 template <typename T, int D>
 __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4AppendArgs a)
 {
-    constexpr int NG = D / kCacheGroup;
-    const bool values = blockIdx.y != 0;
-    const int lanes = values ? 8 : 4, u = threadIdx.x & (lanes - 1);
-    const int64_t r = (int64_t)blockIdx.x * (kAppendThreads / lanes) + threadIdx.x / lanes;  // token and head
+    constexpr int NG = D / kCacheGroup, NM = D / 16;
+    const int u = threadIdx.x & 3;
+    const int64_t r = (int64_t)blockIdx.x * (kAppendThreads / 4) + threadIdx.x / 4;  // token and head
     const int64_t n_rows = a.total * a.c.Hkv;
     const bool in = r < n_rows;
     const int64_t r_in = in ? r : n_rows - 1;
     const int64_t tok = n_rows <= 0xFFFFFFFFLL ? (int64_t)((uint32_t)r_in / (uint32_t)a.c.Hkv) : r_in / a.c.Hkv;
     const int head = (int)(r_in - tok * a.c.Hkv);
+    // lane u: the keys' elements 32 g + 8 u .. + 7 of every group, the values' 16 e + 4 u .. + 3 of every tile
+    Raw<T, 8> xk[NG];
+    Raw<T, 4> xv[NM];
+    const T *pk = reinterpret_cast<const T *>(a.k) + tok * a.k_stride + head * D + 8 * u;
+    const T *pv = reinterpret_cast<const T *>(a.v) + tok * a.v_stride + head * D + 4 * u;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) xk[g].load(pk + kCacheGroup * g);
+#pragma unroll
+    for (int e = 0; e < NM; ++e) xv[e].load(pv + 16 * e);
     const int b = a.seq_of[tok], i = (int)tok - a.off[b];
     const int64_t slot = (int64_t)(a.start != nullptr ? a.start[b] : a.c.length[b]) + i;
-    const bool ok = slot >= 0 && slot < a.c.cap;
+    const bool ok = in && slot >= 0 && slot < a.c.cap;
     if (in && !ok) atomicOr(&g_ris_cache4_error, 2u);
     const int64_t row = ((int64_t)b * a.c.Hkv + head) * a.c.cap + slot;
-    if (!values) {
-        float x[NG][8];
-        const T *p = reinterpret_cast<const T *>(a.k) + tok * a.k_stride + head * D + 8 * u;
+    auto of_lanes = [](uint32_t top) {
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        return max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+    };
+    uint32_t wk[NG], wv[NM / 2], sk[NG], sv[NG];
 #pragma unroll
-        for (int g = 0; g < NG; ++g) load_row<T, 8>(p + kCacheGroup * g, x[g]);
-        uint32_t w[NG], sc[NG];
+    for (int g = 0; g < NG; ++g) {
+        uint32_t top = 0;
 #pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            uint32_t top = 0;
+        for (int e = 0; e < 8; ++e) top = max(top, mag(xk[g][e]));
+        const __nv_bfloat16 s = scale_of(of_lanes(top));
+        sk[g] = __bfloat16_as_ushort(s);
+        const Scale sc(__bfloat162float(s));
+        wk[g] = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, mag(x[g][e]));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            const __nv_bfloat16 s = scale_of(top);
-            sc[g] = __bfloat16_as_ushort(s);
-            const Scale sf(__bfloat162float(s));
-            w[g] = 0;
+        for (int e = 0; e < 4; ++e) wk[g] |= sc.codes(xk[g][2 * e], xk[g][2 * e + 1]) << (8 * e);
+    }
+    // columns 2 u and 2 u + 1: NM bytes each, one per tile
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[g] |= sf.codes(x[g][2 * e], x[g][2 * e + 1]) << (8 * e);
+    for (int w = 0; w < NM / 2; ++w) wv[w] = 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = max(top, max(mag(xv[2 * g][e]), mag(xv[2 * g + 1][e])));
+        const __nv_bfloat16 s = scale_of(of_lanes(top));
+        sv[g] = __bfloat16_as_ushort(s);
+        const Scale sc(__bfloat162float(s));
+#pragma unroll
+        for (int e = 2 * g; e < 2 * g + 2; ++e)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) wv[(c * NM + e) / 4] |= sc.codes(xv[e][2 * c], xv[e][2 * c + 1]) << (8 * (e & 3));
+    }
+    if (ok) {
+        uint8_t *dk = a.c.k + row * (D / 2) + u * (4 * NG), *dv = a.c.v + row * (D / 2) + u * (2 * NM);
+        if constexpr (D == 128) {
+            *reinterpret_cast<uint4 *>(dk) = make_uint4(wk[0], wk[1], wk[2], wk[3]);
+            *reinterpret_cast<uint4 *>(dv) = make_uint4(wv[0], wv[1], wv[2], wv[3]);
+        } else {
+            *reinterpret_cast<uint2 *>(dk) = make_uint2(wk[0], wk[1]);
+            *reinterpret_cast<uint2 *>(dv) = make_uint2(wv[0], wv[1]);
         }
-        if (in && ok) {
-            uint8_t *dst = a.c.k + row * (D / 2) + u * (4 * NG);
-            if constexpr (NG == 4)
-                *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-            else
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
-            if (u == 0) {
-                uint32_t *ds = reinterpret_cast<uint32_t *>(a.c.k_scale + row * NG);
+        if (u < 2) {
+            uint32_t *ds = reinterpret_cast<uint32_t *>((u ? a.c.v_scale : a.c.k_scale) + row * NG);
 #pragma unroll
-                for (int g = 0; g < NG / 2; ++g) ds[g] = sc[2 * g] | (sc[2 * g + 1] << 16);
-            } else if (u == 1) {
-                a.c.pos[row] = a.positions[tok];
-            } else if (u == 2) {
-                a.c.weight[row] = a.weight != nullptr ? a.weight[(int64_t)head * a.total + tok] : 0.f;
-            }
-        }
-    } else {
-        constexpr int NM = D / 16;
-        float x[NM][2];
-        const T *p = reinterpret_cast<const T *>(a.v) + tok * a.v_stride + head * D + 2 * u;
-#pragma unroll
-        for (int m = 0; m < NM; ++m) load_row<T, 2>(p + 16 * m, x[m]);
-        uint32_t w[NM / 4] = {}, sc[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-            uint32_t top = max(max(mag(x[2 * g][0]), mag(x[2 * g][1])), max(mag(x[2 * g + 1][0]), mag(x[2 * g + 1][1])));
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const __nv_bfloat16 s = scale_of(top);
-            sc[g] = __bfloat16_as_ushort(s);
-            const Scale sf(__bfloat162float(s));
-#pragma unroll
-            for (int e = 2 * g; e < 2 * g + 2; ++e) w[e / 4] |= sf.codes(x[e][0], x[e][1]) << (8 * (e & 3));
-        }
-        if (in && ok) {
-            uint8_t *dst = a.c.v + row * (D / 2) + u * NM;
-            if constexpr (NM == 8)
-                *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
-            else
-                *reinterpret_cast<uint32_t *>(dst) = w[0];
-            if (u == 0) {
-                uint32_t *ds = reinterpret_cast<uint32_t *>(a.c.v_scale + row * NG);
-#pragma unroll
-                for (int g = 0; g < NG / 2; ++g) ds[g] = sc[2 * g] | (sc[2 * g + 1] << 16);
-            }
+            for (int g = 0; g < NG / 2; ++g) ds[g] = u ? sv[2 * g] | (sv[2 * g + 1] << 16) : sk[2 * g] | (sk[2 * g + 1] << 16);
+        } else if (u == 2) {
+            a.c.pos[row] = a.positions[tok];
+        } else {
+            a.c.weight[row] = a.weight != nullptr ? a.weight[(int64_t)head * a.total + tok] : 0.f;
         }
     }
     // the new lengths: written at once where the rows start at given slots, else by the last CTA,
     // once every CTA has read the old ones
-    bool last = a.start != nullptr && blockIdx.x == 0 && blockIdx.y == 0;
+    bool last = a.start != nullptr && blockIdx.x == 0;
     if (a.start == nullptr) {
         __shared__ bool done;
         __syncthreads();
         if (threadIdx.x == 0) {
             __threadfence();
-            done = atomicAdd(a.ticket, 1u) == gridDim.x * gridDim.y - 1;
+            done = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
             if (done) *a.ticket = 0u;
         }
         __syncthreads();
@@ -486,11 +480,11 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             const int h = g8;
             const bool have = h < nh;
             const T *q = reinterpret_cast<const T *>(a.q) + (head0 + (have ? h : 0)) * D + 8 * t4;
-            float x[NG][8];
+            Raw<T, 8> x[NG];
             uint32_t top = 0;
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-                load_row<T, 8>(q + kCacheGroup * g, x[g]);
+                x[g].load(q + kCacheGroup * g);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, mag(x[g][e]));
             }
@@ -624,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                 }
                 // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor pipe's
                 // additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
-                float part[SPLIT ? NM : 1][4];
+                [[maybe_unused]] float part[SPLIT ? NM : 1][4];
                 float to[2];  // exponent of a weight: s unscale + to
 #pragma unroll
                 for (int e = 0; e < 2; ++e) to[e] = (float)(4 - e_new) - (m[e] == -INFINITY ? 0.f : m[e]);
@@ -637,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                         p[e] = ex2(fmaf(s[i][e], unscale[e & 1], to[e & 1]));
                         l[e & 1] += p[e];
                     }
-                    uint32_t bh[NG][2], bl[SPLIT ? NG : 1][2];
+                    [[maybe_unused]] uint32_t bh[NG][2], bl[SPLIT ? NG : 1][2];
 #pragma unroll
                     for (int g = 0; g < NG; ++g)
 #pragma unroll
@@ -924,8 +918,8 @@ cudaError_t launch_join(const Cache4AttendArgs &a, cudaStream_t s)
 
 cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStream_t s)
 {
-    const int64_t rows = a.total * a.c.Hkv, per = kAppendThreads / 8;
-    const dim3 grid((unsigned)((rows + per - 1) / per), 2);
+    const int64_t rows = a.total * a.c.Hkv, per = kAppendThreads / 4;
+    const dim3 grid((unsigned)((rows + per - 1) / per));
     if (dtype == RIS_F32) {
         if (a.c.D == 128)
             k_cache4_append<float, 128><<<grid, kAppendThreads, 0, s>>>(a);

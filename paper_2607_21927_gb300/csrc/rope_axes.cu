@@ -20,43 +20,33 @@
 namespace ris {
 namespace {
 
-constexpr int kThreads = 256, kBatch = 4;
+constexpr int kThreads = 256, kBatch = 2;
 
+// 16 bytes of elements
 template <typename T>
-struct Vec;
-template <>
-struct Vec<float> {
-    static constexpr int V = 4;
-    static __device__ __forceinline__ void load(const float *p, float *x)
+struct Vec {
+    static constexpr int V = 16 / (int)sizeof(T);
+    uint4 raw;
+    __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const uint4 *>(p); }
+    __device__ __forceinline__ float operator[](int e) const
     {
-        const float4 v = *reinterpret_cast<const float4 *>(p);
-        x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+        if constexpr (V == 4)
+            return __uint_as_float(w[e]);
+        else
+            return __uint_as_float((e & 1) ? (w[e >> 1] & 0xFFFF0000u) : (w[e >> 1] << 16));
     }
-    static __device__ __forceinline__ void store(float *p, const float *x)
-    {
-        *reinterpret_cast<float4 *>(p) = make_float4(x[0], x[1], x[2], x[3]);
-    }
-};
-template <>
-struct Vec<__nv_bfloat16> {
-    static constexpr int V = 8;
-    static __device__ __forceinline__ void load(const __nv_bfloat16 *p, float *x)
-    {
-        const uint4 v = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(w[e] << 16);
-            x[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-        }
-    }
-    static __device__ __forceinline__ void store(__nv_bfloat16 *p, const float *x)
+    static __device__ __forceinline__ void store(T *p, const float *x)
     {
         uint32_t w[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
-            w[e] = *reinterpret_cast<const uint32_t *>(&b);
+            if constexpr (V == 4) {
+                w[e] = __float_as_uint(x[e]);
+            } else {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * e], x[2 * e + 1]);
+                w[e] = *reinterpret_cast<const uint32_t *>(&b);
+            }
         }
         *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     }
@@ -74,14 +64,33 @@ __device__ __forceinline__ void sincos_turns(int32_t p, uint64_t turn, float *sn
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_rope_axes(const RopeAxesArgs a)
+__global__ void __launch_bounds__(kThreads, 4) k_rope_axes(const RopeAxesArgs a)
 {
     constexpr int V = Vec<T>::V;
     const int half = a.D >> 1, c = V * threadIdx.x;  // blockDim.x == half / V
     const int64_t p = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     if (p >= a.n) return;
+    // heads h0 .. h1 - 1 of q and k, one after another
     const int heads = a.heads[0] + a.heads[1];
     const int h0 = (int)((int64_t)heads * blockIdx.y / gridDim.y), h1 = (int)((int64_t)heads * (blockIdx.y + 1) / gridDim.y);
+    auto of = [&](int h, bool out) -> T * {
+        const int w = h >= a.heads[0];
+        const int64_t at = p * (out ? (int64_t)a.heads[w] * a.D : a.stride[w]) + (h - w * a.heads[0]) * a.D + c;
+        return (out ? reinterpret_cast<T *>(a.y[w]) : reinterpret_cast<T *>(const_cast<void *>(a.x[w]))) + at;
+    };
+    // kBatch heads' loads ahead of what is stored before them in time (which the compiler may not reorder: they may
+    // be in place), the first ahead of the sines and cosines
+    Vec<T> u[kBatch], v[kBatch];
+    auto load = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            if (h + i < h1) {
+                const T *x = of(h + i, false);
+                u[i].load(x);
+                v[i].load(x + half);
+            }
+    };
+    load(h0);
     float cs[V], sn[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) {
@@ -89,34 +98,27 @@ __global__ void __launch_bounds__(kThreads) k_rope_axes(const RopeAxesArgs a)
         cs[e] *= a.mscale;
         sn[e] *= a.inverse ? -a.mscale : a.mscale;
     }
+    for (int h = h0; h < h1; h += kBatch) {
+        Vec<T> s[kBatch], t[kBatch];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int first = w == 0 ? 0 : a.heads[0], n = a.heads[w];
-        const T *x = reinterpret_cast<const T *>(a.x[w]) + p * a.stride[w] + c;
-        T *y = reinterpret_cast<T *>(a.y[w]) + p * (int64_t)n * a.D + c;
-        // kBatch heads' loads ahead of their stores (which the compiler may not pass: they may be in place)
-        const int end = min(h1 - first, n);
-        for (int h = max(h0 - first, 0); h < end; h += kBatch) {
-            float u[kBatch][V], v[kBatch][V];
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (h + i < end) {
-                    Vec<T>::load(x + (h + i) * a.D, u[i]);
-                    Vec<T>::load(x + (h + i) * a.D + half, v[i]);
-                }
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i)
-                if (h + i < end) {
-                    float r[V], t[V];
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        r[e] = fmaf(u[i][e], cs[e], -(v[i][e] * sn[e]));
-                        t[e] = fmaf(v[i][e], cs[e], u[i][e] * sn[e]);
-                    }
-                    Vec<T>::store(y + (h + i) * a.D, r);
-                    Vec<T>::store(y + (h + i) * a.D + half, t);
-                }
+        for (int i = 0; i < kBatch; ++i) {
+            s[i] = u[i];
+            t[i] = v[i];
         }
+        load(h + kBatch);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            if (h + i < h1) {
+                float x[V], y[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    x[e] = fmaf(s[i][e], cs[e], -(t[i][e] * sn[e]));
+                    y[e] = fmaf(t[i][e], cs[e], s[i][e] * sn[e]);
+                }
+                T *out = of(h + i, true);
+                Vec<T>::store(out, x);
+                Vec<T>::store(out + half, y);
+            }
     }
 }
 

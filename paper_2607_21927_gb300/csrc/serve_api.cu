@@ -449,6 +449,7 @@ ris_status ris_cache4_append(const ris_cache4 *cache, ris_pack_t pack, const voi
     RIS_TRY(check_stride(v_stride, (int64_t)cache->kv_heads * cache->head_dim, dtype, "v_stride"));
     if (positions == nullptr || !aligned(positions, 4)) return fail(RIS_ERR_INVALID, "positions is NULL or misaligned");
     if (weight != nullptr && !aligned(weight, 4)) return fail(RIS_ERR_INVALID, "weight is misaligned");
+    if (pack->q_total * cache->kv_heads > 32LL * 2147483647LL) return fail(RIS_ERR_UNSUPPORTED, "more rows than a grid holds");
     Cache4AppendArgs a{};
     a.c = cache_args(cache);
     a.k = k, a.v = v;
