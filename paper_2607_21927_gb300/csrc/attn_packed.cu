@@ -8,8 +8,9 @@
 // a few percent of a call at most, as V is read once per 128 rows of it anyway.
 //
 // A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two layouts:
-//   head dim 128  k_packed128, two CTAs of a cluster share every key and value tile, see there
-//   head dim 64   k_packed64, a CTA carries two row tiles at once, see there
+//   head dim 128  the same for short prompts, k_packed128 for long ones: two CTAs of a cluster share every key and
+//                 value tile
+//   head dim 64   k_packed_rows, persistent, two CTAs to an SM, each with a row tile at a time
 //
 // Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls
 // through to the end, TMEM is released and the CTA returns.
@@ -21,6 +22,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <algorithm>
 #include <cstddef>
 #include <cstdint>
 #include <mutex>
@@ -85,13 +87,14 @@ __device__ __forceinline__ float row_max(const float (&sv)[BN])
     }
     return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
 }
-// P = 2^(s sc - mu) as fp16, two keys to a word, and the sum of the weights before they are rounded
+// P = 2^(s sc - mu) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the weights before they are rounded
+template <int C0 = 0, int C1 = BN>
 __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, float mu, uint32_t (&hw)[BN / 2])
 {
     const uint64_t sc2 = f2_pack(sc, sc), nmu2 = f2_pack(-mu, -mu);
     uint64_t sum[2] = {0, 0};
 #pragma unroll
-    for (int w = 0; w < BN / 2; ++w) {
+    for (int w = C0 / 2; w < C1 / 2; ++w) {
         float x0, x1;
         f2_unpack(f2_fma(f2_pack(sv[2 * w], sv[2 * w + 1]), sc2, nmu2), x0, x1);
         x0 = ex2(x0);
@@ -174,14 +177,18 @@ __device__ __noinline__ void rows_one_by_one(const PackedArgs &a, const PackItem
 }
 
 struct PackedMaps {
-    CUtensorMap q, k, v;
+    CUtensorMap q, k, v, out;
 };
 
-// O of 32 rows (a warp's) x OC columns from column c_from on of TMEM at t_o, normalised, through the
-// warp's part of shared memory so that neighbouring lanes store neighbouring pieces of a row; 16-byte
-// pieces swizzled by the row. Rows with no weight (inv 0) become zeros whatever the columns hold.
+// The kernels that lay out the values (k_values_f16) have finished. Ahead of it run the start-up and, as nothing before this
+// call is still running (see there), the copies of queries and keys and the first scores.
+__device__ __forceinline__ void values_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// O of 32 rows (a warp's) x OC columns from TMEM, normalised, into the warp's part of shared memory, row by
+// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv 0) become zeros whatever
+// the columns hold.
 template <int OC, typename TOut>
-__device__ __forceinline__ void store_out(unsigned char *stage, uint32_t t_o, float inv, TOut *out, int64_t pitch, int rows)
+__device__ __forceinline__ void stage_out(unsigned char *stage, uint32_t t_o, float inv)
 {
     constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;  // bytes and pieces of a row's part
     const int lane = threadIdx.x & 31;
@@ -197,7 +204,13 @@ __device__ __forceinline__ void store_out(unsigned char *stage, uint32_t t_o, fl
             store16<TOut>(stage + lane * RB + ((piece ^ (lane & (NP - 1))) << 4), ov + e * (16 / (int)sizeof(TOut)));
         }
     }
-    __syncwarp();
+}
+// the first `rows` of those rows to memory, so that neighbouring lanes store neighbouring pieces of a row
+template <int OC, typename TOut>
+__device__ __forceinline__ void rows_out(const unsigned char *stage, TOut *out, int64_t pitch, int rows)
+{
+    constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;
+    const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
         const int rr = e * (32 / NP) + lane / NP, piece = lane & (NP - 1);
@@ -347,6 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == kTmaWarp) {
         // =============================== TMA producer
+        values_ready();
         if (lane == 0 && first_loads) {
             // (The query tile and the first keys were requested above.) Keys of tile j once the score
             // products of tile j - NSK are done, values of tile j once the value product of tile j - NSV is: the loader
@@ -491,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
         const int wq = warp & 3, grp = warp >> 2;
         const int r = wq * 32 + lane;  // TMEM lane
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
+        values_ready();
         const float sc = a.scale_log2, v_absmax = *a.v_absmax;
         // the group's score buffer is free for its first tile
         if (lane == 0 && grp < n_kt) arrive_lead(L::B_S_GO + grp);
@@ -608,8 +623,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
                 const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / lt;
                 const int w0 = q0 + 32 * wq;  // the warp's first row
                 TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT + OC * grp;
-                store_out<OC, TOut>(smem + warp * (32 * OC * (int)sizeof(TOut)), T_O + lane_off + OC * grp, inv, out,
-                                    (int64_t)a.Hq * DT, it.q_len - w0);
+                unsigned char *stage = smem + warp * (32 * OC * (int)sizeof(TOut));
+                stage_out<OC, TOut>(stage, T_O + lane_off + OC * grp, inv);
+                __syncwarp();
+                rows_out<OC, TOut>(stage, out, (int64_t)a.Hq * DT, it.q_len - w0);
                 if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin, lt);
             } else {
                 rows_one_by_one<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps);
@@ -658,234 +675,319 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
     if (warp == kScoreWarp) tmem_dealloc<2, kTmemCols>(tmem);
 }
 
-// ---------------------------------------------------------------- head dim 64
-struct Lay64 {
-    static constexpr int DT = 64, NSK = 4, NSV = 4;
-    static constexpr int TILE = 128 * 128;  // 128 rows or keys of 64 16-bit values
-    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_BARS = OFF_Q + 2 * TILE;
-    static constexpr int OFF_TMEM = OFF_BARS + 256, BYTES = OFF_TMEM + 16;
-    // Barriers, of a stage:
-    //   K_FULL, V_FULL    its keys / values have landed
-    //   K_FREE, V_FREE    the products that read it are done
-    // and of a row tile t, one phase per key tile:
-    //   S_GO    its scores have been read out of their buffer
-    //   S_FULL  they are there
+// ---------------------------------------------------------------- a row tile per CTA at a time
+template <int D>
+struct LayRows {
+    static constexpr int DT = D, NB = D / 64;              // 64-column blocks
+    static constexpr bool OVER = D == 128;                 // P takes the scores' columns
+    static constexpr int NSK = D == 64 ? 3 : 1, NSV = D == 64 ? 2 : 1, NI = 4;
+    static constexpr int BLK = 128 * 128, TILE = NB * BLK; // 128 rows or keys of D 16-bit values
+    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_OUT = OFF_Q + TILE,
+                         OFF_BARS = OFF_OUT + BLK, OFF_INFO = OFF_BARS + 192, OFF_TMEM = OFF_INFO + NI * 64, BYTES = OFF_TMEM + 16;
+    // Barriers, of a ring stage:
+    //   K_FULL, V_FULL, Q_FULL  its keys / values / the query tile have landed
+    //   K_FREE, V_FREE, Q_FREE  the products that read it are done
+    //   I_FULL, I_FREE          a unit's description is there / every role has read it
+    // and one phase per key tile:
+    //   S_GO    the last scores have been read out of their buffer (only where P has its own columns: else the value product
+    //           before has to be done, which says that too)
+    //   S_FULL  the next are there
     //   P_GO    P is written (and O rescaled where needed)
     //   PV_DONE O has settled, P's buffer is free
-    static constexpr int B_Q_FULL = 0, B_K_FULL = 1, B_V_FULL = B_K_FULL + NSK, B_K_FREE = B_V_FULL + NSV, B_V_FREE = B_K_FREE + NSK,
-                         B_S_GO = B_V_FREE + NSV, B_S_FULL = B_S_GO + 2, B_P_GO = B_S_FULL + 2, B_PV_DONE = B_P_GO + 2,
-                         NBAR = B_PV_DONE + 2;
-    static_assert(NBAR <= 32 && BYTES <= 232448, "a lane per barrier; shared memory of a CTA");
+    static constexpr int B_K_FULL = 0, B_V_FULL = B_K_FULL + NSK, B_Q_FULL = B_V_FULL + NSV, B_K_FREE = B_Q_FULL + 1,
+                         B_V_FREE = B_K_FREE + NSK, B_Q_FREE = B_V_FREE + NSV, B_I_FULL = B_Q_FREE + 1, B_I_FREE = B_I_FULL + NI,
+                         B_S_GO = B_I_FREE + NI, B_S_FULL = B_S_GO + 1, B_P_GO = B_S_FULL + 1, B_PV_DONE = B_P_GO + 1,
+                         NBAR = B_PV_DONE + 1;
+    static_assert(NBAR <= 24 && 2 * (BYTES + 1024) <= 228 * 1024, "barriers; two CTAs of an SM");
+    static constexpr uint32_t COLS = 256, T_P = OVER ? 0 : BN, T_O = OVER ? BN : BN + BN / 2;  // TMEM; S at 0
+    static_assert(T_O + DT <= COLS, "TMEM columns");
+    // registers per thread: at launch, then after setmaxnreg of a softmax and of another thread
+    static constexpr int THREADS = 256, REGS = 128, SOFTMAX_REGS = 200, OTHER_REGS = 56;
+    static_assert(SOFTMAX_REGS + OTHER_REGS == 2 * REGS, "the shares of the two warpgroups add up to the launch's");
 };
 
-// One CTA carries two row tiles over the same key tiles: two heads of a KV group on the same 128 rows or, where a
-// group has an odd number of heads, 256 rows of a head. Each softmax group owns one of them, so neither waits for
-// the other: at head dim 64 a key tile takes 512 cycles of the tensor pipe per row tile and its 16,384
-// exponentials as long or longer, and the softmax is what has to be kept busy. (Two groups on
-// alternate tiles of one row tile pass the reference maximum from hand to hand, one tile's exponentials after the other's.)
+// What the other roles need to know of a unit, a (work item, query head).
+struct UnitInfo {
+    int n;                  // key tiles, -1: no more units
+    int h, row, shift;      // head; first row; key j is seen by row i when j <= i + shift
+    int q_base, q_len, k_base, k_len;
+};
+static_assert(sizeof(UnitInfo) <= 64, "the ring's slots");
+
+// The units of one CTA after another, in the items' order; the CTAs take them in rounds, every second round
+// backwards, so that the long ones are dealt out evenly.
+struct Units {
+    int64_t total;
+    int round;
+    __device__ __forceinline__ bool next(const PackedArgs &a, PackItem &it, int &h)
+    {
+        for (;;) {
+            const int64_t base = (int64_t)++round * gridDim.x;
+            if (base >= total) return false;
+            const int64_t u = base + ((round & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+            if (u >= total) continue;
+            it = a.items[(int)u / a.Hq];
+            h = (int)u % a.Hq;
+            return true;
+        }
+    }
+};
+
+// Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
+// few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and the two CTAs
+// fill each other's; the loaders and issuing warps run on into the next unit while the last one is finished; the outputs
+// leave by TMA. With a CTA (head dim 128: a cluster) per unit, 64 prompts of 256 tokens took 96 us at 12 heads of 128,
+// 111 at 32 heads of 64. At head dim 64 a key tile takes 512 cycles of the tensor pipe and its 16,384 exponentials as
+// long, so it is the softmax that bounds it even over long prompts; at head dim 128 the products of a CTA
+// read as much shared memory as there is bandwidth, and long prompts go to k_packed128.
 //
-//   warp 8 (TMA)  both query tiles, then key and value tiles into two rings;
-//   warp 9        scores S_t = Q_t K^T of both row tiles, each as soon as its group has read the last ones;
-//   warp 10       O_t += P_t V;
-//   warps 0-3, 4-7  the softmax of row tile 0, 1: one thread per row.
-// TMEM: S 2 x 128 columns, P 2 x 64, O 2 x 64: all 512. P has columns of its own, so the next scores are computed
-// under the exponentials.
-template <typename TOut>
-__global__ void __launch_bounds__(kThreads, 1) k_packed64(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+//   warp 4  the units, query and key tiles, warp 5 value tiles (TMA);
+//   warp 6  S = Q K^T as soon as its columns are free, warp 7 O += P V;
+//   warps 0-3  the softmax, one thread per row.
+template <int D, typename TOut>
+__global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
-    using L = Lay64;
-    constexpr int NSK = L::NSK, NSV = L::NSV, DT = 64, TILE = L::TILE;
+    using L = LayRows<D>;
+    constexpr int NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
+    constexpr int kLoadQK = 4, kLoadV = 5, kScores = 6, kValues = 7;
     extern __shared__ __align__(1024) unsigned char smem[];
     uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned int *const gave_up = &g_ris_packed_error;
-    const bool head_pair = (a.G & 1) == 0;
-    const unsigned n_h = (unsigned)(head_pair ? a.Hq / 2 : a.Hq), r2 = blockIdx.x / n_h;
-    const int h0 = (int)(blockIdx.x - r2 * n_h) * (head_pair ? 2 : 1);
-    const PackItem it = a.items[r2];
-    const int g = h0 / a.G, shift = it.k_len - it.q_len;
-    // first row and key tiles of row tile t (a second half without rows has none)
-    auto row_of = [&](int t) { return it.row + (head_pair ? 0 : t * BM); };
-    auto tiles_of = [&](int t) {
-        const int q0 = row_of(t), keys = q0 < it.q_len ? max(0, min(it.k_len, min(it.q_len, q0 + BM) + shift)) : 0;
-        return (keys + BN - 1) / BN;
-    };
-    const int n0 = tiles_of(0), n1 = tiles_of(1), n_kt = max(n0, n1);
     auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
 
-    if (warp == kTmaWarp) {
+    if (warp == kLoadQK) {
         if (lane < L::NBAR) {
-            const bool by_group = (lane >= L::B_S_GO && lane < L::B_S_GO + 2) || (lane >= L::B_P_GO && lane < L::B_P_GO + 2);
-            mbar_init(bar(lane), by_group ? kGroupWarps : 1);
+            const bool by_group = lane == L::B_S_GO || lane == L::B_P_GO, free = lane >= L::B_I_FREE && lane < L::B_I_FREE + NI;
+            mbar_init(bar(lane), by_group ? kGroupWarps : free ? kGroupWarps + 3 : 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-    } else if (warp == kScoreWarp) {
-        tmem_alloc<1, kTmemCols>(smem_u32(&tmem_base_sh));
+    } else if (warp == kScores) {
+        tmem_alloc<1, L::COLS>(smem_u32(&tmem_base_sh));
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    constexpr uint32_t T_S = 0, T_P = T_S + 2 * BN, T_O = T_P + BN;
-    static_assert(T_O + 2 * DT <= kTmemCols, "TMEM columns");
     const uint32_t tmem = tmem_base_sh;
-    bool ok = tmem == 0u && (sbase & 1023u) == 0u;
+    bool ok = (sbase & 1023u) == 0u;
+    auto wait_all = [&](int i, int parity) -> bool {
+        const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+        tc_fence_after();
+        return got;
+    };
+    // description of unit u (a whole warp, or a loader's lane); its place is given back once every lane has it
+    auto unit = [&](int u, UnitInfo &x) -> bool {
+        if (!mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up)) return false;
+        x = *reinterpret_cast<const UnitInfo *>(smem + L::OFF_INFO + u % NI * 64);
+        return true;
+    };
+    auto unit_read = [&](int u, bool one) { mbar_arrive_if(one, bar(L::B_I_FREE + u % NI)); };
 
-    if (warp >= kSoftmaxWarps) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp == kTmaWarp) {
-            if (lane == 0 && ok && n_kt > 0) {
-                int nk = 0, nv = 0;
-                mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL), 2 * TILE);
-                for (int t = 0; t < 2; ++t)
-                    tma_load_3d<1>(sbase + L::OFF_Q + t * TILE, &maps.q, 0, head_pair ? h0 + t : h0, it.q_base + row_of(t), bar(L::B_Q_FULL));
-                for (int j = 0; j < n_kt && ok; ++j) {
-                    const int sk = j % NSK, sv = j % NSV;
-                    if (j >= NSK) ok = mbar_wait<1>(bar(L::B_K_FREE + sk), (j / NSK - 1) & 1, gave_up);
+    if (warp >= kGroupWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
+        if (warp == kLoadQK) {
+            if (lane == 0 && ok) {
+                Units units{(int64_t)a.n_items * a.Hq, -1};
+                int nq = 0, nk = 0;  // query and key tiles asked for
+                bool more = true;
+                for (int u = 0; more && ok; ++u) {
+                    PackItem it;
+                    int h = 0, n = -1;
+                    more = units.next(a, it, h);
+                    if (u >= NI) ok = mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up);
                     if (!ok) break;
-                    mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + sk), TILE);
-                    tma_load_3d<1>(sbase + L::OFF_K + sk * TILE, &maps.k, 0, g, it.k_base + j * BN, bar(L::B_K_FULL + sk));
-                    nk = j + 1;
-                    if (j >= NSV) ok = mbar_wait<1>(bar(L::B_V_FREE + sv), (j / NSV - 1) & 1, gave_up);
-                    if (!ok) break;
-                    mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + sv), TILE);
-                    tma_load_3d<1>(sbase + L::OFF_V + sv * TILE, &maps.v, 0, g, it.k_base + j * BN, bar(L::B_V_FULL + sv));
-                    nv = j + 1;
+                    UnitInfo &x = *reinterpret_cast<UnitInfo *>(smem + L::OFF_INFO + u % NI * 64);
+                    if (more) {
+                        const int shift = it.k_len - it.q_len;
+                        n = (max(0, min(it.k_len, min(it.q_len, it.row + BM) + shift)) + BN - 1) / BN;  // tiles that the rows see
+                        x = UnitInfo{n, h, it.row, shift, it.q_base, it.q_len, it.k_base, it.k_len};
+                    } else {
+                        x.n = -1;
+                    }
+                    mbar_arrive(bar(L::B_I_FULL + u % NI));
+                    const int g = h / a.G;
+                    for (int j = 0; j < n; ++j, ++nk) {
+                        const int st = nk % NSK;
+                        if (nk >= NSK) ok = mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + st), TILE);
+                        for (int blk = 0; blk < NB; ++blk)
+                            tma_load_3d<1>(sbase + L::OFF_K + st * TILE + blk * L::BLK, &maps.k, 64 * blk, g, it.k_base + j * BN,
+                                           bar(L::B_K_FULL + st));
+                        if (j > 0) continue;
+                        if (nq > 0) ok = mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL), TILE);
+                        for (int blk = 0; blk < NB; ++blk)
+                            tma_load_3d<1>(sbase + L::OFF_Q + blk * L::BLK, &maps.q, 64 * blk, h, it.q_base + it.row, bar(L::B_Q_FULL));
+                        ++nq;
+                    }
                 }
                 // nothing of this thread's may still be on its way to shared memory when the CTA ends
-                mbar_wait_own<1>(bar(L::B_Q_FULL), 0);
-                for (int j = max(0, nk - NSK); j < nk; ++j) mbar_wait_own<1>(bar(L::B_K_FULL + j % NSK), (j / NSK) & 1);
-                for (int j = max(0, nv - NSV); j < nv; ++j) mbar_wait_own<1>(bar(L::B_V_FULL + j % NSV), (j / NSV) & 1);
+                if (nq > 0) mbar_wait_own<1>(bar(L::B_Q_FULL), (nq - 1) & 1);
+                for (int i = max(0, nk - NSK); i < nk; ++i) mbar_wait_own<1>(bar(L::B_K_FULL + i % NSK), (i / NSK) & 1);
             }
-        } else if (warp == kScoreWarp && ok && n_kt > 0) {
-            constexpr uint32_t ID_S = idesc_bf16(BM, BN, false);
-            auto wait_all = [&](int i, int parity) -> bool {
-                const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
-                tc_fence_after();
-                return got;
-            };
-            int done0 = 0, done1 = 0, freed = 0;
-            ok = wait_all(L::B_Q_FULL, 0);
-            for (int j = 0; j < n_kt && ok; ++j) {
-                const int st = j % NSK;
-                ok = wait_all(L::B_K_FULL + st, (j / NSK) & 1);
-                const uint32_t kd = desc_lo(sbase + L::OFF_K + st * TILE, 16);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (!ok || j >= (t ? n1 : n0)) continue;
-                    ok = wait_all(L::B_S_GO + t, j & 1);
-                    if (!ok) continue;
-                    const uint32_t qd = desc_lo(sbase + L::OFF_Q + t * TILE, 16);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 0; ks < DT / 16; ++ks)
-                            tc_mma_ss<1>(T_S + t * BN, qd + dstep(ks * 32), kd + dstep(ks * 32), ID_S, ks > 0);
-                        tc_commit<1>(bar(L::B_S_FULL + t));
+        } else if (warp == kLoadV) {
+            values_ready();
+            if (lane == 0 && ok) {
+                int nv = 0;
+                for (int u = 0;; ++u) {
+                    UnitInfo x;
+                    ok = unit(u, x);
+                    if (!ok || x.n < 0) break;
+                    unit_read(u, true);
+                    const int g = x.h / a.G;
+                    for (int j = 0; j < x.n; ++j, ++nv) {
+                        const int st = nv % NSV;
+                        if (nv >= NSV) ok = mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + st), TILE);
+                        for (int blk = 0; blk < NB; ++blk)
+                            tma_load_3d<1>(sbase + L::OFF_V + st * TILE + blk * L::BLK, &maps.v, 64 * blk, g, x.k_base + j * BN,
+                                           bar(L::B_V_FULL + st));
                     }
-                    __syncwarp();
-                    (t ? done1 : done0) = j + 1;
+                    if (!ok) break;
+                }
+                for (int i = max(0, nv - NSV); i < nv; ++i) mbar_wait_own<1>(bar(L::B_V_FULL + i % NSV), (i / NSV) & 1);
+            }
+        } else if (ok) {
+            // The issuing warps, all lanes: trip counts and addresses come out of warp-wide reductions, which leave them in
+            // uniform registers; a product whose operands are in the lanes' registers costs more time to issue than to run.
+            const uint32_t tb = __reduce_max_sync(0xFFFFFFFFu, tmem);
+            int t = 0, nq = 0;  // tiles; units with keys
+            for (int u = 0;; ++u) {
+                UnitInfo x;
+                ok = __all_sync(0xFFFFFFFFu, unit(u, x));
+                if (!ok) break;
+                const int n = __reduce_max_sync(0xFFFFFFFFu, x.n);
+                __syncwarp();
+                unit_read(u, lane == 0);
+                if (n < 0) break;
+                if (n == 0) continue;
+                if (warp == kScores) {
+                    constexpr uint32_t ID_S = idesc_bf16(BM, BN, false);
+                    ok = wait_all(L::B_Q_FULL, nq & 1);
+                    const uint32_t qd = desc_lo(sbase + L::OFF_Q, 16);
+                    for (int j = 0; j < n && ok; ++j, ++t) {
+                        const int st = t % NSK;
+                        ok = wait_all(L::B_K_FULL + st, (t / NSK) & 1);
+                        if (!L::OVER)
+                            ok = ok && wait_all(L::B_S_GO, t & 1);
+                        else if (t > 0)
+                            ok = ok && wait_all(L::B_PV_DONE, (t - 1) & 1);
+                        if (!ok) break;
+                        const uint32_t kd = desc_lo(sbase + L::OFF_K + st * TILE, 16);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                tc_mma_ss<1>(tb, qd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), kd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), ID_S, ks > 0);
+                            tc_commit<1>(bar(L::B_S_FULL));
+                            tc_commit<1>(bar(L::B_K_FREE + st));
+                            if (j == n - 1) tc_commit<1>(bar(L::B_Q_FREE));
+                        }
+                        __syncwarp();
+                    }
+                } else {
+                    constexpr uint32_t ID_O = idesc_f16(BM, D, true);
+                    for (int j = 0; j < n && ok; ++j, ++t) {
+                        const int st = t % NSV;
+                        ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO, t & 1);
+                        if (!ok) break;
+                        const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, L::BLK);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < BN / 16; ++ks)
+                                tc_mma_ts<1>(tb + L::T_O, tb + L::T_P + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
+                            tc_commit<1>(bar(L::B_PV_DONE));
+                            tc_commit<1>(bar(L::B_V_FREE + st));
+                        }
+                        __syncwarp();
+                    }
                 }
                 if (!ok) break;
-                if (elect_one()) tc_commit<1>(bar(L::B_K_FREE + st));
-                __syncwarp();
-                freed = j + 1;
+                ++nq;
             }
-            // every commit of this warp has arrived before the CTA ends
-            if (lane == 0) {
-                if (done0 > 0) mbar_wait_own<1>(bar(L::B_S_FULL), (done0 - 1) & 1);
-                if (done1 > 0) mbar_wait_own<1>(bar(L::B_S_FULL + 1), (done1 - 1) & 1);
-                for (int j = max(0, freed - NSK); j < freed; ++j) mbar_wait_own<1>(bar(L::B_K_FREE + j % NSK), (j / NSK) & 1);
-            }
-        } else if (warp == kValueWarp && ok && n_kt > 0) {
-            constexpr uint32_t ID_O = idesc_f16(BM, DT, true);
-            auto wait_all = [&](int i, int parity) -> bool {
-                const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
-                tc_fence_after();
-                return got;
-            };
-            int done0 = 0, done1 = 0, freed = 0;
-            for (int j = 0; j < n_kt && ok; ++j) {
-                const int st = j % NSV;
-                ok = wait_all(L::B_V_FULL + st, (j / NSV) & 1);
-                const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, TILE);
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    if (!ok || j >= (t ? n1 : n0)) continue;
-                    ok = wait_all(L::B_P_GO + t, j & 1);
-                    if (!ok) continue;
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 0; ks < BN / 16; ++ks)
-                            tc_mma_ts<1>(T_O + t * DT, T_P + t * (BN / 2) + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
-                        tc_commit<1>(bar(L::B_PV_DONE + t));
-                    }
-                    __syncwarp();
-                    (t ? done1 : done0) = j + 1;
-                }
-                if (!ok) break;
-                if (elect_one()) tc_commit<1>(bar(L::B_V_FREE + st));
-                __syncwarp();
-                freed = j + 1;
-            }
-            if (lane == 0) {
-                if (done0 > 0) mbar_wait_own<1>(bar(L::B_PV_DONE), (done0 - 1) & 1);
-                if (done1 > 0) mbar_wait_own<1>(bar(L::B_PV_DONE + 1), (done1 - 1) & 1);
-                for (int j = max(0, freed - NSV); j < freed; ++j) mbar_wait_own<1>(bar(L::B_V_FREE + j % NSV), (j / NSV) & 1);
+            // every commit of this warp has arrived before the CTA ends (after a wait that gave up, those of the tiles issued)
+            if (lane == 0 && t > 0) {
+                const int done = warp == kScores ? L::B_S_FULL : L::B_PV_DONE, free = warp == kScores ? L::B_K_FREE : L::B_V_FREE;
+                const int ring = warp == kScores ? NSK : NSV;
+                mbar_wait_own<1>(bar(done), (t - 1) & 1);
+                for (int i = max(0, t - ring); i < t; ++i) mbar_wait_own<1>(bar(free + i % ring), (i / ring) & 1);
+                if (warp == kScores && nq > 0) mbar_wait_own<1>(bar(L::B_Q_FREE), (nq - 1) & 1);
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        const int wq = warp & 3, grp = warp >> 2, h = head_pair ? h0 + grp : h0;
-        const int r = wq * 32 + lane, q0 = row_of(grp), n = grp ? n1 : n0;
-        const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
-        const float sc = a.scale_log2, v_absmax = *a.v_absmax;
-        const uint32_t t_s = T_S + grp * BN + lane_off, t_p = T_P + grp * (BN / 2) + lane_off, t_o = T_O + grp * DT + lane_off;
-        if (lane == 0 && n > 0) mbar_arrive(bar(L::B_S_GO + grp));
-        const int last_key = q0 + r + shift, warp_sees = q0 + wq * 32 + shift;
-        float l = 0.f, m = -INFINITY;
-        for (int j = 0; j < n && ok; ++j) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_S_FULL + grp), j & 1, gave_up));
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t su[2][64];
-            tmem_issue64(t_s, su[0]);
-            tmem_issue64(t_s + 64, su[1]);
-            tmem_wait_ld();
-            pin64(su[0]);
-            pin64(su[1]);
-            tc_fence_before();
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
+        const int r = threadIdx.x;  // TMEM lane, row of the tile
+        const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+        const uint32_t t_s = tmem + lane_off, t_p = tmem + L::T_P + lane_off, t_o = tmem + L::T_O + lane_off;
+        unsigned char *const stage = smem + L::OFF_OUT + warp * (L::BLK / kGroupWarps);
+        const float sc = a.scale_log2;
+        int t = 0;           // tiles
+        bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
+        if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
+        values_ready();
+        const float v_absmax = *a.v_absmax;
+        for (int u = 0; ok; ++u) {
+            UnitInfo x;
+            ok = __all_sync(0xFFFFFFFFu, unit(u, x));
+            if (!ok || x.n < 0) break;
             __syncwarp();
-            if (lane == 0 && j + 1 < n) mbar_arrive(bar(L::B_S_GO + grp));
-            float sv[BN];
+            unit_read(u, lane == 0);
+            const int last_key = x.row + r + x.shift, warp_sees = x.row + warp * 32 + x.shift;
+            float l = 0.f, m = -INFINITY;
+            for (int j = 0; j < x.n; ++j, ++t) {
+                // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
+                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL, t & 1);
+                tc_fence_after();
+                uint32_t su[2][64];
+                tmem_issue64(t_s, su[0]);
+                tmem_issue64(t_s + 64, su[1]);
+                tmem_wait_ld();
+                pin64(su[0]);
+                pin64(su[1]);
+                if (!L::OVER) {
+                    tc_fence_before();
+                    __syncwarp();
+                    mbar_arrive_if(lane == 0, bar(L::B_S_GO));
+                }
+                float sv[BN];
 #pragma unroll
-            for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
-            if (warp_sees < j * BN + BN - 1) {
-                uint32_t cw[4];
+                for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
+                if (warp_sees < j * BN + BN - 1) {
+                    uint32_t cw[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) cw[e] = causal_word(last_key - j * BN, e);
+                    for (int e = 0; e < 4; ++e) cw[e] = causal_word(last_key - j * BN, e);
 #pragma unroll
-                for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
-            }
-            const float mx = row_max(sv) * sc;
-            const bool upd = mx > m + kLazyLog2;
-            const bool scale_o = upd && m != -INFINITY;
-            const float al = scale_o ? exp2f(m - mx) : 1.f;
-            if (upd) {
+                    for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
+                }
+                const float mx = row_max(sv) * sc;
+                const bool upd = mx > m + kLazyLog2;
+                const bool scale_o = upd && m != -INFINITY;
+                const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
+                const float al = scale_o ? exp2f(m - mx) : 1.f;
                 l *= al;
-                m = mx;
-            }
-            const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
-            uint32_t hw[BN / 2];
-            l += weights_of(sv, sc, m == -INFINITY ? 0.f : m, hw);
-            if (j > 0) {  // P's buffer is free, and O has settled
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_PV_DONE + grp), (j - 1) & 1, gave_up));
-                if (!ok) break;
+                m = upd ? mx : m;
+                const float mu = m == -INFINITY ? 0.f : m;
+                uint32_t hw[BN / 2];
+                float sum = weights_of<0, 96>(sv, sc, mu, hw);
+                // polled here, the answers are there when the weights are
+                bool settled = true;
+                if (!L::OVER) {
+                    settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
+                    there = mbar_test<1>(bar(L::B_S_FULL), (t + 1) & 1);
+                }
+                l += sum + weights_of<96, BN>(sv, sc, mu, hw);
+                // P's buffer is free and O has settled once the last value product is done (where P takes the scores'
+                // place, the scores were computed after that; a unit's first tile: waited for at the end of the last unit)
+                if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
                 tc_fence_after();
                 if (any_scale) {
 #pragma unroll 1
-                    for (int c0 = 0; c0 < DT; c0 += 32) {
+                    for (int c0 = 0; c0 < D; c0 += 32) {
                         float ov[32];
                         uint32_t ow[32];
                         tmem_ld32(t_o + c0, ov);
@@ -895,60 +997,107 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed64(const PackedArgs a, co
                     }
                     tmem_wait_st();
                 }
+                tmem_st32(t_p, hw);
+                tmem_st32(t_p + 32, hw + 32);
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_if(lane == 0, bar(L::B_P_GO));
             }
-            tmem_st32(t_p, hw);
-            tmem_st32(t_p + 32, hw + 32);
-            tmem_wait_st();
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(L::B_P_GO + grp));
-        }
-        if (ok && n > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_PV_DONE + grp), (n - 1) & 1, gave_up));
-        // (rows without a key: the query's copy, whose place the zeros pass through, must have landed)
-        if (ok && n == 0 && n_kt > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FULL), 0, gave_up));
-        if (ok) {
-            tc_fence_after();
-            if (v_absmax < INFINITY) {
-                const float inv = l == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / l;
-                const int w0 = q0 + 32 * wq;
-                TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT;
-                // through the row tile's query, whose products are done: 4 KB a warp
-                unsigned char *stage = smem + L::OFF_Q + warp * (TILE / kGroupWarps);
-                constexpr int OC = 128 / (int)sizeof(TOut);
+            if (ok && x.n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+            if (!ok) break;
+            if (!(v_absmax < INFINITY)) {  // (by all four warps, wherever the rows end)
+                PackItem it{};
+                it.q_base = x.q_base, it.q_len = x.q_len, it.k_base = x.k_base, it.k_len = x.q_len + x.shift;
+                rows_one_by_one<D, TOut>(a, it, x.row, x.h, warp, kGroupWarps);
+                continue;
+            }
+            const int w0 = x.row + 32 * warp, rows = x.q_len - w0;  // the warp's first row, and how many it has (or more than 32)
+            if (rows <= 0) continue;
+            TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(x.q_base + w0) * a.Hq + x.h) * D;
+            const float inv = l == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / l;
+            constexpr int OC = 128 / (int)sizeof(TOut);  // columns that pass through the warp's 4 KB at a time
 #pragma unroll
-                for (int c0 = 0; c0 < DT; c0 += OC)
-                    store_out<OC, TOut>(stage, t_o + c0, inv, out + c0, (int64_t)a.Hq * DT, it.q_len - w0);
-                if (q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m, l);
-            } else {
-                rows_one_by_one<DT, TOut>(a, it, q0, h, wq, kGroupWarps);
+            for (int c0 = 0; c0 < D; c0 += OC) {
+                // the last copy out of the place has read it
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+                __syncwarp();
+                if (x.n > 0) {
+                    stage_out<OC, TOut>(stage, t_o + c0, inv);
+                } else {  // rows without a key: zeros
+                    for (int e = lane; e < 256; e += 32) reinterpret_cast<uint4 *>(stage)[e] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                if (rows >= 32) {
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
+                                         reinterpret_cast<uint64_t>(&maps.out)),
+                                     "r"(c0), "r"(x.h), "r"(x.q_base + w0), "r"(smem_u32(stage))
+                                     : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                } else {
+                    __syncwarp();
+                    rows_out<OC, TOut>(stage, out + c0, (int64_t)a.Hq * D, rows);
+                }
             }
+            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m, l);
+            tc_fence_before();  // (O has been read before the next P is announced)
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) atomicOr(&g_ris_packed_error, 2u);
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == kScoreWarp) tmem_dealloc<1, kTmemCols>(tmem);
+    if (warp == kScores) tmem_dealloc<1, L::COLS>(tmem);
 }
 
 // ---------------------------------------------------------------- values as fp16
-// The largest magnitude of each CTA's share of V (as bits without the sign, so that an infinity or NaN wins).
+// 16-byte pieces of V by number, row_pieces to a row. (32-bit division: a 64-bit one takes longer than the load.)
 constexpr int kPrepThreads = 256, kPrepBlocks = 304;
+struct Pieces {
+    const __nv_bfloat16 *v;
+    int64_t stride, n;
+    uint32_t row_pieces;
+    bool wide;
+    __device__ __forceinline__ Pieces(const PackedArgs &a, int row_pieces_)
+        : v(reinterpret_cast<const __nv_bfloat16 *>(a.v)), stride(a.v_stride), n(a.k_total * row_pieces_), row_pieces(row_pieces_),
+          wide(n > 0xFFFFFFFFLL)
+    {
+        if (stride == (int64_t)row_pieces * 8) row_pieces = 0;  // rows without gaps: one long one
+    }
+    __device__ __forceinline__ uint4 load(int64_t t) const
+    {
+        int64_t at = t * 8;
+        if (row_pieces != 0) {
+            const int64_t r = wide ? t / row_pieces : (int64_t)((uint32_t)t / row_pieces);
+            at = r * stride + (t - r * row_pieces) * 8;
+        }
+        return *reinterpret_cast<const uint4 *>(v + at);
+    }
+};
+// The largest magnitude of each CTA's share of V (as bits without the sign, so that an infinity or NaN wins).
 __global__ void __launch_bounds__(kPrepThreads) k_values_absmax(const PackedArgs a, int row_pieces, float *part)
 {
-    const int64_t n = a.k_total * row_pieces, step = (int64_t)gridDim.x * kPrepThreads;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const Pieces p(a, row_pieces);
+    const int64_t step = (int64_t)gridDim.x * kPrepThreads;
     uint32_t m = 0;
-#pragma unroll 4
-    for (int64_t t = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t < n; t += step) {
-        const int64_t r = t / row_pieces;
-        const uint4 x = *reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.v) + r * a.v_stride + (t - r * row_pieces) * 8);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    for (int64_t t0 = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t0 < p.n; t0 += 4 * step) {
+        uint4 x[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) m = max(m, max((w[e] << 16) & 0x7FFFFFFFu, w[e] & 0x7FFF0000u));
+        for (int e = 0; e < 4; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) m = max(m, max((w[c] << 16) & 0x7FFFFFFFu, w[c] & 0x7FFF0000u));
+        }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
     __shared__ uint32_t red[kPrepThreads / 32];
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
@@ -957,14 +1106,22 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_absmax(const PackedArgs
         part[blockIdx.x] = __uint_as_float(m);
     }
 }
-// part[0 .. n_part - 1] -> *absmax; v16 = fp16(v 2^-E)
+// part[0 .. n_part - 1] -> *absmax; v16 = fp16(v 2^-E). A programmatic dependent of the kernel above; the attention is one of
+// this kernel, allowed to start once every CTA here knows that nothing before this call is still running.
 __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a, int row_pieces, const float *part, int n_part, float *absmax,
                                                              __half *v16)
 {
+    const Pieces p(a, row_pieces);
+    const int64_t step = (int64_t)gridDim.x * kPrepThreads;
+    int64_t t0 = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x;
+    uint4 x[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     uint32_t m = 0;
     for (int i = threadIdx.x; i < n_part; i += kPrepThreads) m = max(m, __float_as_uint(part[i]));
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+    m = __reduce_max_sync(0xFFFFFFFFu, m);
     __shared__ uint32_t red[kPrepThreads / 32];
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
     __syncthreads();
@@ -972,19 +1129,22 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a,
     for (int w = 0; w < kPrepThreads / 32; ++w) m = max(m, red[w]);
     if (blockIdx.x == 0 && threadIdx.x == 0) *absmax = __uint_as_float(m);
     const float s = pow2i(-value_exp(__uint_as_float(m)));
-    const int64_t n = a.k_total * row_pieces, step = (int64_t)gridDim.x * kPrepThreads;
-#pragma unroll 2
-    for (int64_t t = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t < n; t += step) {
-        const int64_t r = t / row_pieces;
-        const uint4 x = *reinterpret_cast<const uint4 *>(reinterpret_cast<const __nv_bfloat16 *>(a.v) + r * a.v_stride + (t - r * row_pieces) * 8);
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-        uint32_t y[4];
+    for (;;) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const __half2 hv = __floats2half2_rn(__uint_as_float(w[e] << 16) * s, __uint_as_float(w[e] & 0xFFFF0000u) * s);
-            y[e] = *reinterpret_cast<const uint32_t *>(&hv);
+        for (int e = 0; e < 2; ++e) {
+            const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+            uint32_t y[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const __half2 hv = __floats2half2_rn(__uint_as_float(w[c] << 16) * s, __uint_as_float(w[c] & 0xFFFF0000u) * s);
+                y[c] = *reinterpret_cast<const uint32_t *>(&hv);
+            }
+            if (t0 + e * step < p.n) reinterpret_cast<uint4 *>(v16)[t0 + e * step] = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        reinterpret_cast<uint4 *>(v16)[t] = make_uint4(y[0], y[1], y[2], y[3]);
+        t0 += 2 * step;
+        if (t0 >= p.n) break;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
@@ -1170,57 +1330,84 @@ PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
     return fn;
 }
 
-// n tokens of H heads of D 16-bit values, `stride` elements from token to token, viewed as 3D (d, head,
-// token); box = 64 d x 1 head x `rows` tokens.
-bool make_map(CUtensorMap *m, const void *base, int64_t n, int H, int64_t stride, int rows, int D, bool f16 = false)
+// n tokens of H heads of D values, `stride` elements from token to token, viewed as 3D (d, head, token); box =
+// 128 bytes of d x 1 head x `rows` tokens.
+bool make_map(CUtensorMap *m, CUtensorMapDataType type, const void *base, int64_t n, int H, int64_t stride, int rows, int D)
 {
     auto fn = encode_fn();
     if (fn == nullptr) return false;
+    const int size = type == CU_TENSOR_MAP_DATA_TYPE_FLOAT32 ? 4 : 2;
     cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)H, (cuuint64_t)n};
-    cuuint64_t strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)stride * 2};
-    cuuint32_t box[3] = {64, 1, (cuuint32_t)rows};
+    cuuint64_t strides[2] = {(cuuint64_t)D * size, (cuuint64_t)stride * size};
+    cuuint32_t box[3] = {(cuuint32_t)(128 / size), 1, (cuuint32_t)rows};
     cuuint32_t estr[3] = {1, 1, 1};
-    return fn(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims,
-              strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(m, type, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+constexpr CUtensorMapDataType kBf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, kF16 = CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                              kF32 = CU_TENSOR_MAP_DATA_TYPE_FLOAT32;
+
+using TileKernel = void (*)(PackedArgs, PackedMaps);
+
+// Once per kernel: its shared memory, and that its launch has the registers that the softmax threads' setmaxnreg would
+// wait for.
+cudaError_t prepare(TileKernel kern, int bytes, int regs)
+{
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    cudaFuncAttributes fa;
+    if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, kern);
+    return e != cudaSuccess ? e : (fa.numRegs + 7) / 8 * 8 < regs ? cudaErrorInvalidConfiguration : cudaSuccess;
 }
 
-template <int DT, typename TOut>
-cudaError_t launch_tiles(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
+// A programmatic dependent of the launch before it.
+cudaLaunchAttribute dependent()
 {
-    constexpr int CG = DT == 128 ? 2 : 1;
-    // at least the 128 layout's: one CTA per SM, as a CTA holds all TMEM columns
-    constexpr int bytes = DT == 128 ? Lay128::BYTES : Lay64::BYTES;
-    static_assert(bytes > 232448 / 2, "one CTA per SM, as it holds all TMEM columns");
-    void (*kern)(PackedArgs, PackedMaps);
-    if constexpr (DT == 128)
-        kern = k_packed128<TOut>;
-    else
-        kern = k_packed64<TOut>;
-    static std::once_flag once;
-    static cudaError_t ready = cudaSuccess;
-    std::call_once(once, [&] {
-        ready = cudaFuncSetAttribute(reinterpret_cast<const void *>(kern), cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        // the softmax threads' setmaxnreg would wait for registers that a smaller launch lacks
-        cudaFuncAttributes fa;
-        if (ready == cudaSuccess) ready = cudaFuncGetAttributes(&fa, reinterpret_cast<const void *>(kern));
-        if (ready == cudaSuccess && (fa.numRegs + 7) / 8 * 8 < kRegs) ready = cudaErrorInvalidConfiguration;
-    });
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    return at;
+}
+
+template <typename TOut>
+cudaError_t launch_clusters(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
+{
+    static_assert(Lay128::BYTES > 232448 / 2, "one CTA per SM, as it holds all TMEM columns");
+    static const cudaError_t ready = prepare(k_packed128<TOut>, Lay128::BYTES, kRegs);
     if (ready != cudaSuccess) return ready;
-    const int64_t heads = (a.G & 1) == 0 ? a.Hq / 2 : a.Hq;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.n_items * heads * CG));
+    cfg.gridDim = dim3((unsigned)((int64_t)a.n_items * ((a.G & 1) == 0 ? a.Hq / 2 : a.Hq) * 2));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = bytes;
+    cfg.dynamicSmemBytes = Lay128::BYTES;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
-    at[0].val.clusterDim.y = 1;
-    at[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute at[2];
+    at[0] = dependent();
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = 1;
+    at[1].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_packed128<TOut>, a, maps);
+    note_launch();
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+template <int D, typename TOut>
+cudaError_t launch_rows(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
+{
+    using L = LayRows<D>;
+    static const cudaError_t ready = prepare(k_packed_rows<D, TOut>, L::BYTES, L::REGS);
+    if (ready != cudaSuccess) return ready;
+    const int64_t units = (int64_t)a.n_items * a.Hq;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>(units, 2 * 152));
+    cfg.blockDim = dim3(L::THREADS);
+    cfg.dynamicSmemBytes = L::BYTES;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1] = {dependent()};
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a, maps);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_packed_rows<D, TOut>, a, maps);
     note_launch();
     return e != cudaSuccess ? e : cudaGetLastError();
 }
@@ -1232,7 +1419,7 @@ size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim)
     return 256 + sizeof(float) * kPrepBlocks + 256 + (size_t)k_total * kv_heads * head_dim * 2;
 }
 
-cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, void *scratch, cudaStream_t s)
+cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s)
 {
     // scratch: the largest magnitude, the parts it comes from, the values
     float *absmax = static_cast<float *>(scratch), *part = absmax + 64;
@@ -1243,24 +1430,34 @@ cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, void *scratc
     if (pieces > 0) {
         const int n_part = (int)(blocks < kPrepBlocks ? blocks : kPrepBlocks);
         k_values_absmax<<<n_part, kPrepThreads, 0, s>>>(a, row_pieces, part);
-        k_values_f16<<<(unsigned)(blocks < 2432 ? blocks : 2432), kPrepThreads, 0, s>>>(a, row_pieces, part, n_part, absmax, v16);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(blocks < 1216 ? blocks : 1216));
+        cfg.blockDim = dim3(kPrepThreads);
+        cfg.stream = s;
+        cudaLaunchAttribute at[1] = {dependent()};
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_values_f16, a, row_pieces, (const float *)part, n_part, absmax, v16);
         note_launch(2);
+        if (e != cudaSuccess) return e;
     } else {
         const cudaError_t e = cudaMemsetAsync(absmax, 0, sizeof(float), s);
         if (e != cudaSuccess) return e;
     }
     alignas(64) PackedMaps maps;
-    const int krows = D == 128 ? Lay128::KROWS : BN;
-    // (without keys no box of k or v is ever asked for: any valid map does)
-    const bool keys = a.k_total > 0;
-    if (!make_map(&maps.q, a.q, a.q_total, a.Hq, a.q_stride, BM, D)) return cudaErrorInvalidValue;
-    if (!keys)
-        maps.k = maps.v = maps.q;
-    else if (!make_map(&maps.k, a.k, a.k_total, a.Hkv, a.k_stride, krows, D) ||
-             !make_map(&maps.v, v16, a.k_total, a.Hkv, (int64_t)a.Hkv * D, BN, D, true))
+    const CUtensorMapDataType out_type = out_dtype == RIS_F32 ? kF32 : kBf16;
+    if (!make_map(&maps.q, kBf16, a.q, a.q_total, a.Hq, a.q_stride, BM, D) ||
+        !make_map(&maps.out, out_type, a.out, a.q_total, a.Hq, (int64_t)a.Hq * D, 32, D))
         return cudaErrorInvalidValue;
-    if (D == 128) return out_dtype == RIS_F32 ? launch_tiles<128, float>(a, maps, s) : launch_tiles<128, __nv_bfloat16>(a, maps, s);
-    return out_dtype == RIS_F32 ? launch_tiles<64, float>(a, maps, s) : launch_tiles<64, __nv_bfloat16>(a, maps, s);
+    // (without keys no box of k or v is ever asked for: any valid map does)
+    if (a.k_total == 0)
+        maps.k = maps.v = maps.q;
+    else if (!make_map(&maps.k, kBf16, a.k, a.k_total, a.Hkv, a.k_stride, clusters ? Lay128::KROWS : BN, D) ||
+             !make_map(&maps.v, kF16, v16, a.k_total, a.Hkv, (int64_t)a.Hkv * D, BN, D))
+        return cudaErrorInvalidValue;
+    if (clusters) return out_dtype == RIS_F32 ? launch_clusters<float>(a, maps, s) : launch_clusters<__nv_bfloat16>(a, maps, s);
+    if (D == 128) return out_dtype == RIS_F32 ? launch_rows<128, float>(a, maps, s) : launch_rows<128, __nv_bfloat16>(a, maps, s);
+    return out_dtype == RIS_F32 ? launch_rows<64, float>(a, maps, s) : launch_rows<64, __nv_bfloat16>(a, maps, s);
 }
 
 cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
@@ -1268,8 +1465,8 @@ cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
     alignas(64) PackedMaps maps;
     if (a.q_total == 0)
         maps = PackedMaps{};  // no rows: every CTA writes zeros
-    else if (!make_map(&maps.q, a.q, a.q_total, a.Hq, a.q_stride, LayW<128>::RC, D) ||
-             !make_map(&maps.k, a.k, a.k_total, a.Hkv, a.k_stride, BN, D))
+    else if (!make_map(&maps.q, kBf16, a.q, a.q_total, a.Hq, a.q_stride, LayW<128>::RC, D) ||
+             !make_map(&maps.k, kBf16, a.k, a.k_total, a.Hkv, a.k_stride, BN, D))
         return cudaErrorInvalidValue;
     else
         maps.v = maps.k;

@@ -65,10 +65,10 @@ struct PackedArgs {
 // fp32 inputs: items of kPackRows rows.
 cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStream_t s);
 cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s);
-// bf16 inputs: items of kPackRows rows with an even group, of 2 kPackRows with an odd one; scratch of
-// packed_scratch_bytes, 256-byte aligned.
+// bf16 inputs: items of kPackRows rows, or for clusters (head dim 128) with an odd group of 2 kPackRows; scratch
+// of packed_scratch_bytes, 256-byte aligned.
 size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim);
-cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, void *scratch, cudaStream_t s);
+cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s);
 cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s);
 
 struct Cache4Args {

@@ -22,6 +22,7 @@ struct ris_pack_s {
     int32_t *q_off = nullptr, *seq_of = nullptr;
     PackItem *items = nullptr, *pairs = nullptr, *key_items = nullptr;  // of 128 rows, 256 rows, 128 keys
     int32_t n_items = 0, n_pairs = 0, n_key_items = 0;
+    int64_t key_tiles = 0;  // of 128 x 128 that the items of 128 rows see
     cudaStream_t stream = nullptr;
 };
 
@@ -172,6 +173,20 @@ ris_status rope_turns(const ris_rope_cfg *rope, int64_t n_ctx, int32_t head_dim,
 
 double log2e_over_sqrt(int32_t head_dim) { return 1.4426950408889634074 / std::sqrt((double)head_dim); }
 
+// Keys that the last of an item's `step` rows sees.
+int64_t keys_of(const PackItem &it, int step)
+{
+    const int64_t last = std::min<int64_t>((int64_t)it.row + step, it.q_len) + it.k_len - it.q_len;
+    return std::max<int64_t>(0, std::min<int64_t>(last, it.k_len));
+}
+
+// Head dim 128, bf16: whether a pack's row tiles see so many key tiles (24 on average, about 6,000 tokens of one prompt)
+// that two CTAs sharing every key tile beat two independent ones on each SM, which finish a row tile and start the next
+// one with less delay. us a call of 16,384 to 18,432 tokens, clusters / rows: prompts of 256 tokens 86 / 41, of 1024 107 / 67,
+// of 4096 183 / 163, of 6144 254 / 259, of 8192 275 / 299, of 16384 465 / 565 (12 / 2 heads; 8 / 8 heads: of 4096 138 / 126, of
+// 8192 201 / 220).
+bool packed_by_clusters(const ris_pack_s *pack) { return pack->key_tiles >= 24LL * pack->n_items; }
+
 // The items of `step` rows (or keys) of every sequence; of rows, those with the most keys first, so that the
 // short ones fill the tail of the grid.
 std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vector<int32_t> &k_off, bool keys, int step)
@@ -190,11 +205,8 @@ std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vec
             v.push_back(it);
         }
     }
-    auto cost = [step](const PackItem &it) {
-        const int64_t last = std::min<int64_t>((int64_t)it.row + step, it.q_len) + it.k_len - it.q_len;
-        return std::max<int64_t>(0, std::min<int64_t>(last, it.k_len));
-    };
-    if (!keys) std::stable_sort(v.begin(), v.end(), [&](const PackItem &x, const PackItem &y) { return cost(x) > cost(y); });
+    if (!keys)
+        std::stable_sort(v.begin(), v.end(), [step](const PackItem &x, const PackItem &y) { return keys_of(x, step) > keys_of(y, step); });
     return v;
 }
 
@@ -235,6 +247,7 @@ ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t
         p->k_total = nk;
         const std::vector<PackItem> items = items_of(q_off, k_off, false, kPackRows), pairs = items_of(q_off, k_off, false, 2 * kPackRows),
                                     keys = items_of(q_off, k_off, true, kPackKeys);
+        for (const PackItem &it : items) p->key_tiles += (keys_of(it, kPackRows) + kPackKeys - 1) / kPackKeys;
         p->n_items = (int32_t)items.size();
         p->n_pairs = (int32_t)pairs.size();
         p->n_key_items = (int32_t)keys.size();
@@ -410,7 +423,8 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     a.weight_rows = weight_rows;
     a.key_weight = key_weight;
     const bool tiles = dtype == RIS_BF16;
-    if (tiles && (a.G & 1) != 0) {
+    const bool clusters = tiles && head_dim == 128 && packed_by_clusters(pack);
+    if (clusters && (a.G & 1) != 0) {
         a.items = pack->pairs;
         a.n_items = pack->n_pairs;
     }
@@ -420,7 +434,7 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     if (stat_b + tile_b > 0) RIS_CUDA(mem.alloc(stat_b + tile_b, s));
     if (weight_rows > 0) a.row_stat = static_cast<float2 *>(mem.p);
     if (pack->n_items > 0)
-        RIS_CUDA(tiles ? launch_packed_tiles(a, head_dim, out_dtype, static_cast<char *>(mem.p) + stat_b, s)
+        RIS_CUDA(tiles ? launch_packed_tiles(a, head_dim, out_dtype, clusters, static_cast<char *>(mem.p) + stat_b, s)
                        : launch_packed_f32(a, head_dim, out_dtype, s));
     if (weight_rows > 0 && pack->n_key_items > 0)
         RIS_CUDA(tiles ? launch_packed_weights_tc(a, head_dim, s) : launch_packed_weights_f32(a, head_dim, s));

@@ -21,6 +21,12 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// (predicated, without a branch)
+__device__ __forceinline__ void mbar_arrive_if(bool go, uint32_t bar)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %1, 0;\n\t@p mbarrier.arrive.shared::cta.b64 _, [%0];\n\t}" ::"r"(bar), "r"((uint32_t)go)
+                 : "memory");
+}
 // Arrival on a barrier of any CTA of the cluster (shared::cluster address, see cluster_addr). What
 // it announces is tensor memory that was read or written, which tcgen05.wait and the tcgen05 fences on
 // both sides order, and nothing that this thread read or wrote itself: relaxed.
@@ -141,8 +147,11 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const u
     if (mbar_try_wait<CG, TMEM>(bar, parity)) return true;
     const long long t0 = clock64();
     while (!mbar_try_wait<CG, TMEM>(bar, parity)) {
-        if (clock64() - t0 > (1LL << 31)) return false;
-        if (*reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u) return false;
+        // (the error word only once the wait is far beyond what it ever takes: a poll that reads it first sees the
+        // barrier a memory latency late)
+        const long long waited = clock64() - t0;
+        if (waited > (1LL << 31)) return false;
+        if (waited > (1LL << 20) && *reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u) return false;
     }
     return true;
 }
