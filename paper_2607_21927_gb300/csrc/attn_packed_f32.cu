@@ -1,11 +1,14 @@
 // Causal attention over packed prompts on the FP32 pipe: fp32 inputs, which never pass through a
 // narrower product, and the weight that each key got from a sequence's last rows.
 //
-// k_packed_f32: one CTA per (64 query rows, query head) walks the keys in tiles of 64 with a running
-// maximum and sum: S = Q K^T with a 4 x 4 patch per thread (Q and K d-major in shared memory), the softmax
-// over the 16 lanes that share a row, P d-major over the keys' place, O += P V with a 4 x D/16 patch in registers.
-// Bound by the FMA pipe (4 D flops per pair and head); per step of d a warp reads 3 wavefronts of shared
-// memory for 16 packed multiply-adds, so both pipes are near even.
+// k_packed_f32: one CTA per (32 query rows, query head) walks the keys in tiles of 64 with a running maximum and
+// sum. Keys and values come row by row by cp.async into a buffer each, so that the next keys travel under the
+// value product and the next values under the scores; rows of 4 more elements than the head dim keep 16-byte reads of
+// eight neighbouring rows apart. S: a 4 x 4 patch per thread, 4 elements of d at a time as packed pairs (which leaves
+// two partial sums per score); the softmax over the 16 lanes that share a row; O += P V with a 4 x D/16 patch.
+// Bound by the FMA pipe: 4 D flops per pair and head; shared memory reads fill three quarters of its
+// bandwidth beside it. Tiles of 32 rows, because a short prompt has few of them and the one with the most keys is
+// the last to end.
 //
 // k_packed_weights: one thread per key holds the key's row in registers and walks the last rows of the
 // group's heads, broadcast from shared memory: w_j = sum_i,h exp2(s_ij - m_i) / l_i.
@@ -20,9 +23,9 @@
 namespace ris {
 namespace {
 
-constexpr int BM = 64, BN = 64, LD = BM + 4;  // rows and keys of a tile, pitch of the d-major arrays
-constexpr int kThreads = 256;
-constexpr int kHalves = kPackRows / BM;
+constexpr int BM = 32, BN = 64, LP = BN + 4;  // rows and keys of a tile, pitch of P
+constexpr int kThreads = 4 * BM;
+constexpr int kParts = kPackRows / BM;
 
 __device__ __forceinline__ float4 load4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
@@ -58,27 +61,33 @@ __device__ __forceinline__ float2 f2_get(uint64_t v)
     return r;
 }
 
-// x[row][d] of up to 64 rows of one head, d-major into dst[d][row]; rows past `rows` as zeros
-template <int D>
-__device__ __forceinline__ void stage_t(float *dst, const float *x, int64_t stride, int rows)
+// R rows of one head from memory to rows of pitch D + 4 (PAD) or D in shared memory, asynchronously; rows past `rows` as zeros
+template <int R, int D, bool PAD>
+__device__ __forceinline__ void fetch_rows(float *dst, const float *x, int64_t stride, int rows)
 {
-    for (int t = threadIdx.x; t < BM * (D / 4); t += kThreads) {
-        const int r = t % BM, d = t / BM * 4;
-        const float4 v = r < rows ? load4(x + r * stride + d) : make_float4(0.f, 0.f, 0.f, 0.f);
-        dst[d * LD + r] = v.x;
-        dst[(d + 1) * LD + r] = v.y;
-        dst[(d + 2) * LD + r] = v.z;
-        dst[(d + 3) * LD + r] = v.w;
+#pragma unroll
+    for (int e = 0; e < R * (D / 4) / kThreads; ++e) {
+        const int t = threadIdx.x + e * kThreads, r = t / (D / 4), d = t % (D / 4) * 4;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst + r * (PAD ? D + 4 : D) + d);
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(x + (r < rows ? r : 0) * stride + d), "r"(r < rows ? 16 : 0)
+                     : "memory");
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void fetched_but()  // all but the last N groups
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 template <typename TO, int D>
 __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
 {
+    constexpr int LK = D + 4;
     extern __shared__ __align__(16) float sm[];
-    float *const qs = sm, *const ks = qs + D * LD, *const vs = ks + D * LD, *const ps = ks;
-    const int b = blockIdx.x, h = b % a.Hq, part = b / a.Hq % kHalves;
-    const PackItem it = a.items[b / a.Hq / kHalves];
+    float *const qs = sm, *const ks = qs + BM * LK, *const vs = ks + BN * LK, *const ps = vs + BN * D;
+    const int b = blockIdx.x, h = b % a.Hq, part = kParts - 1 - b / a.Hq % kParts;
+    const PackItem it = a.items[b / a.Hq / kParts];
     const int r0 = it.row + part * BM, rows = min(BM, it.q_len - r0);
     if (rows <= 0) return;
     const int g = h / a.G;
@@ -87,47 +96,52 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
     const float *q = reinterpret_cast<const float *>(a.q) + (int64_t)(it.q_base + r0) * a.q_stride + h * D;
     const float *k = reinterpret_cast<const float *>(a.k) + (int64_t)it.k_base * a.k_stride + g * D;
     const float *v = reinterpret_cast<const float *>(a.v) + (int64_t)it.k_base * a.v_stride + g * D;
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    stage_t<D>(qs, q, a.q_stride, rows);
-    constexpr int C = D / 16;  // columns of O of a thread: 4 tx + 64 x ..
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;  // rows 4 ty + i; keys tx + 16 j; columns 4 tx + 64 c
+    fetch_rows<BM, D, true>(qs, q, a.q_stride, rows);
+    if (keys > 0) {
+        fetch_rows<BN, D, true>(ks, k, a.k_stride, min(BN, keys));
+        fetch_rows<BN, D, false>(vs, v, a.v_stride, min(BN, keys));
+    }
+    constexpr int C = D / 16;  // columns of O of a thread
     uint64_t o[4][C / 2] = {};
     float m[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
     for (int k0 = 0; k0 < keys; k0 += BN) {
-        const int kn = min(BN, keys - k0);
-        __syncthreads();  // the tiles of the last step are done with
-        stage_t<D>(ks, k + (int64_t)k0 * a.k_stride, a.k_stride, kn);
-        for (int t = threadIdx.x; t < BN * (D / 4); t += kThreads) {
-            const int r = t / (D / 4), d = t % (D / 4) * 4;
-            // a key that is not there weighs nothing, whatever lies in its place
-            store4(vs + r * D + d, r < kn ? load4(v + (int64_t)(k0 + r) * a.v_stride + d) : make_float4(0.f, 0.f, 0.f, 0.f));
-        }
+        const int kn = min(BN, keys - k0), left = min(BN, keys - k0 - BN);  // keys of this tile and of the next one
+        fetched_but<1>();  // (the values' copy may still be on its way)
         __syncthreads();
-        uint64_t s2[4][2] = {};
-#pragma unroll 8
-        for (int d = 0; d < D; ++d) {
-            const float4 qa = *reinterpret_cast<const float4 *>(qs + d * LD + 4 * ty);
-            const ulonglong2 kb = *reinterpret_cast<const ulonglong2 *>(ks + d * LD + 4 * tx);
-            const float qr[4] = {qa.x, qa.y, qa.z, qa.w};
+        uint64_t s2[4][4] = {};  // two partial sums of each score: of the even and of the odd elements
+#pragma unroll 4
+        for (int d = 0; d < D; d += 4) {
+            ulonglong2 qa[4], kb[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint64_t qq = f2(qr[i], qr[i]);
-                s2[i][0] = f2_fma(qq, kb.x, s2[i][0]);
-                s2[i][1] = f2_fma(qq, kb.y, s2[i][1]);
-            }
+            for (int i = 0; i < 4; ++i) qa[i] = *reinterpret_cast<const ulonglong2 *>(qs + (4 * ty + i) * LK + d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const ulonglong2 *>(ks + (tx + 16 * j) * LK + d);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s2[i][j] = f2_fma(qa[i].x, kb[j].x, s2[i][j]);
+                    s2[i][j] = f2_fma(qa[i].y, kb[j].y, s2[i][j]);
+                }
         }
-        __syncthreads();  // the keys' place takes P
+        __syncthreads();  // the keys' buffer is free
+        if (left > 0)
+            fetch_rows<BN, D, true>(ks, k + (int64_t)(k0 + BN) * a.k_stride, a.k_stride, left);
+        else
+            asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 lo = f2_get(s2[i][0]), hi = f2_get(s2[i][1]);
-            float s[4] = {lo.x, lo.y, hi.x, hi.y};
-            const int last = r0 + 4 * ty + i + shift - k0 - 4 * tx;  // last key of the patch that the row sees
-            float mx = -INFINITY;
+            const int last = r0 + 4 * ty + i + shift - k0;  // last key of the tile that the row sees
+            float s[4], mx = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[e] = e <= last && 4 * tx + e < kn ? s[e] * a.scale_log2 : -INFINITY;
-                mx = fmaxf(mx, s[e]);
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = f2_get(s2[i][j]);
+                const int key = tx + 16 * j;
+                s[j] = key <= last && key < kn ? (x.x + x.y) * a.scale_log2 : -INFINITY;
+                mx = fmaxf(mx, s[j]);
             }
 #pragma unroll
             for (int x = 8; x > 0; x >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, x));
@@ -136,36 +150,42 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
             m[i] = nm;
             float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[e] = exp2f(s[e] - ref);
-                sum += s[e];
-                ps[(4 * tx + e) * LD + 4 * ty + i] = s[e];
+            for (int j = 0; j < 4; ++j) {
+                s[j] = exp2f(s[j] - ref);
+                sum += s[j];
+                ps[(4 * ty + i) * LP + tx + 16 * j] = s[j];
             }
             l[i] = fmaf(l[i], al, sum);  // this lane's part of the row's sum
             const uint64_t al2 = f2(al, al);
 #pragma unroll
             for (int c = 0; c < C / 2; ++c) o[i][c] = f2_mul(o[i][c], al2);
         }
+        fetched_but<1>();  // (the next keys' copy may still be on its way)
         __syncthreads();
         // O += P V; where some row does not see the whole tile, a row takes only the keys that it sees (0 times
         // an infinity or NaN in a key's place is not 0)
         const int seen = r0 + 4 * ty + shift - k0;  // last key of the tile that the first of the four rows sees
         auto values = [&](auto masked) {
-#pragma unroll 4
-            for (int j = 0; j < BN; ++j) {
-                const float4 pa = *reinterpret_cast<const float4 *>(ps + j * LD + 4 * ty);
-                const float pr[4] = {pa.x, pa.y, pa.z, pa.w};
-                ulonglong2 vb[C / 4];
+#pragma unroll 2
+            for (int j = 0; j < BN; j += 4) {
+                float4 pa[4];
 #pragma unroll
-                for (int c = 0; c < C / 4; ++c) vb[c] = *reinterpret_cast<const ulonglong2 *>(vs + j * D + 64 * c + 4 * tx);
+                for (int i = 0; i < 4; ++i) pa[i] = *reinterpret_cast<const float4 *>(ps + (4 * ty + i) * LP + j);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (decltype(masked)::value && j > seen + i) continue;
-                    const uint64_t pp = f2(pr[i], pr[i]);
+                for (int e = 0; e < 4; ++e) {
+                    ulonglong2 vb[C / 4];
 #pragma unroll
-                    for (int c = 0; c < C / 4; ++c) {
-                        o[i][2 * c] = f2_fma(pp, vb[c].x, o[i][2 * c]);
-                        o[i][2 * c + 1] = f2_fma(pp, vb[c].y, o[i][2 * c + 1]);
+                    for (int c = 0; c < C / 4; ++c) vb[c] = *reinterpret_cast<const ulonglong2 *>(vs + (j + e) * D + 64 * c + 4 * tx);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (decltype(masked)::value && j + e > seen + i) continue;
+                        const float p = e == 0 ? pa[i].x : e == 1 ? pa[i].y : e == 2 ? pa[i].z : pa[i].w;
+                        const uint64_t pp = f2(p, p);
+#pragma unroll
+                        for (int c = 0; c < C / 4; ++c) {
+                            o[i][2 * c] = f2_fma(pp, vb[c].x, o[i][2 * c]);
+                            o[i][2 * c + 1] = f2_fma(pp, vb[c].y, o[i][2 * c + 1]);
+                        }
                     }
                 }
             }
@@ -174,6 +194,11 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
             values(std::false_type{});
         else
             values(std::true_type{});
+        __syncthreads();  // the values' buffer and P's are free
+        if (left > 0)
+            fetch_rows<BN, D, false>(vs, v + (int64_t)(k0 + BN) * a.v_stride, a.v_stride, left);
+        else
+            asm volatile("cp.async.commit_group;" ::: "memory");
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -247,10 +272,10 @@ template <typename TO, int D>
 cudaError_t launch(const PackedArgs &a, cudaStream_t s)
 {
     auto kern = k_packed_f32<TO, D>;
-    constexpr int bytes = (2 * D * LD + BN * D) * (int)sizeof(float);
+    constexpr int bytes = ((BM + BN) * (D + 4) + BN * D + BM * LP) * (int)sizeof(float);
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != cudaSuccess) return e;
-    kern<<<(unsigned)((int64_t)a.n_items * kHalves * a.Hq), kThreads, bytes, s>>>(a);
+    kern<<<(unsigned)((int64_t)a.n_items * kParts * a.Hq), kThreads, bytes, s>>>(a);
     note_launch();
     return cudaGetLastError();
 }

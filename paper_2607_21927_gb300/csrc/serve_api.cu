@@ -402,7 +402,7 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
         RIS_TRY(check_stride(k_stride, (int64_t)kv_heads * head_dim, dtype, "k_stride"));
         RIS_TRY(check_stride(v_stride, (int64_t)kv_heads * head_dim, dtype, "v_stride"));
     }
-    if ((int64_t)pack->n_items * 2 * heads > 2147483647LL)
+    if ((int64_t)pack->n_items * 4 * heads > 2147483647LL)
         return fail(RIS_ERR_UNSUPPORTED, "%d row tiles x %d heads are more than a grid holds", pack->n_items, heads);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     PackedArgs a{};
