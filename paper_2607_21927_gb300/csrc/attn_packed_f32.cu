@@ -5,7 +5,8 @@
 // sum. Keys and values come row by row by cp.async into a buffer each, so that the next keys travel under the
 // value product and the next values under the scores; rows of 4 more elements than the head dim keep 16-byte reads of
 // eight neighbouring rows apart. S: a 4 x 4 patch per thread, 4 elements of d at a time as packed pairs (which leaves
-// two partial sums per score); the softmax over the 16 lanes that share a row; O += P V with a 4 x D/16 patch.
+// two partial sums per score); the softmax over the 16 lanes that share a row; O += P V with a 4 x D/16
+// patch, P as pairs of the same weight in shared memory (two moves a weight otherwise).
 // Bound by the FMA pipe: 4 D flops per pair and head; shared memory reads fill three quarters of its
 // bandwidth beside it. Tiles of 32 rows, because a short prompt has few of them and the one with the most keys is
 // the last to end.
@@ -23,7 +24,7 @@
 namespace ris {
 namespace {
 
-constexpr int BM = 32, BN = 64, LP = BN + 4;  // rows and keys of a tile, pitch of P
+constexpr int BM = 32, BN = 64, LP = 2 * BN + 4;  // rows and keys of a tile, pitch of P
 constexpr int kThreads = 4 * BM;
 constexpr int kParts = kPackRows / BM;
 
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
             for (int j = 0; j < 4; ++j) {
                 s[j] = exp2f(s[j] - ref);
                 sum += s[j];
-                ps[(4 * ty + i) * LP + tx + 16 * j] = s[j];
+                *reinterpret_cast<uint64_t *>(ps + (4 * ty + i) * LP + 2 * (tx + 16 * j)) = f2(s[j], s[j]);
             }
             l[i] = fmaf(l[i], al, sum);  // this lane's part of the row's sum
             const uint64_t al2 = f2(al, al);
@@ -166,21 +167,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
         // an infinity or NaN in a key's place is not 0)
         const int seen = r0 + 4 * ty + shift - k0;  // last key of the tile that the first of the four rows sees
         auto values = [&](auto masked) {
-#pragma unroll 2
-            for (int j = 0; j < BN; j += 4) {
-                float4 pa[4];
+#pragma unroll 4
+            for (int j = 0; j < BN; j += 2) {
+                ulonglong2 pa[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) pa[i] = *reinterpret_cast<const float4 *>(ps + (4 * ty + i) * LP + j);
+                for (int i = 0; i < 4; ++i) pa[i] = *reinterpret_cast<const ulonglong2 *>(ps + (4 * ty + i) * LP + 2 * j);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
+                for (int e = 0; e < 2; ++e) {
                     ulonglong2 vb[C / 4];
 #pragma unroll
                     for (int c = 0; c < C / 4; ++c) vb[c] = *reinterpret_cast<const ulonglong2 *>(vs + (j + e) * D + 64 * c + 4 * tx);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (decltype(masked)::value && j + e > seen + i) continue;
-                        const float p = e == 0 ? pa[i].x : e == 1 ? pa[i].y : e == 2 ? pa[i].z : pa[i].w;
-                        const uint64_t pp = f2(p, p);
+                        const uint64_t pp = e == 0 ? pa[i].x : pa[i].y;
 #pragma unroll
                         for (int c = 0; c < C / 4; ++c) {
                             o[i][2 * c] = f2_fma(pp, vb[c].x, o[i][2 * c]);
