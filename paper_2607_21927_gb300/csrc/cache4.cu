@@ -318,6 +318,9 @@ __device__ __forceinline__ void unpack4(uint32_t w, uint32_t (&h)[4])
         : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
         : "r"(w));
 }
+// the low (high) halves of every byte of a, and those of b as the high halves
+__device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) { return (a & 0x0F0F0F0Fu) | ((b << 4) & 0xF0F0F0F0u); }
+__device__ __forceinline__ uint32_t high_halves(uint32_t a, uint32_t b) { return ((a >> 4) & 0x0F0F0F0Fu) | (b & 0xF0F0F0F0u); }
 __device__ __forceinline__ float ex2(float x)
 {
     float y;
@@ -343,39 +346,28 @@ __device__ __forceinline__ float bf16_at(uint32_t w, int e) { return __uint_as_f
 __device__ __forceinline__ int tile_slot(int r) { return ((r & 7) >> 1) + 4 * (r & 1) + (r & 8); }
 
 // How the slots in use are shared out. A list is a (sequence, KV head, block of 8 query heads) and holds
-// ceil(length / kUnit) units; the units of all lists, one list after another, are cut into as many equal runs as there are CTAs, whatever
-// the lengths are. CTA i's part of list l has partial number i + l: runs and lists advance together, so no two parts
-// share a number. Lists of a sequence are neighbours: list = b * per_seq + y.
-struct Shares {
-    int64_t total;  // units of all lists
-
-    __device__ __forceinline__ int64_t begin(int cta, int ctas) const { return total * cta / ctas; }
-    // the CTA whose run holds unit u
-    __device__ __forceinline__ int cta_of(int64_t u, int ctas) const
-    {
-        int i = (int)(u * ctas / total);
-        while (i + 1 < ctas && begin(i + 1, ctas) <= u) ++i;
-        while (begin(i, ctas) > u) --i;
-        return i;
-    }
-};
+// ceil(length / kUnit) units; the units of all lists, one list after another, are cut into as many equal runs as there are CTAs,
+// whatever the lengths are. CTA i's part of list l has partial number i + l: runs and lists advance together, so no
+// two parts share a number. Lists of a sequence are neighbours: list = b * per_seq + y. Every warp works this out for
+// itself, 32 sequences at a time by shuffles (with the block's barriers and 64-bit divisions it took 4 us).
 __device__ __forceinline__ int64_t slots_of(const Cache4AttendArgs &a, int b)
 {
     return max((int64_t)0, min((int64_t)a.c.length[b], a.reach));
 }
-__device__ __forceinline__ int64_t units_of(const Cache4AttendArgs &a, int b) { return (slots_of(a, b) + kUnit - 1) / kUnit; }
-
-// Sum over the block's threads of x; every thread gets it. `red`: a word per warp.
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *red)
+__device__ __forceinline__ int64_t units_of(const Cache4AttendArgs &a, int b)
+{
+    return b < a.c.B ? (slots_of(a, b) + kUnit - 1) / kUnit : 0;
+}
+__device__ __forceinline__ int64_t warp_sum64(int64_t x)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = 0;
-    for (int w = 0; w < (int)(blockDim.x >> 5); ++w) x += red[w];
     return x;
+}
+// floor(x y / z)
+__device__ __forceinline__ int64_t mul_div(int64_t x, int y, int z)
+{
+    return x < (1 << 20) && y < (1 << 11) ? (int64_t)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
 }
 
 // Persistent CTAs of four warps; each CTA takes a run of units and the lists that it touches one after another. Its warps
@@ -388,7 +380,7 @@ __device__ __forceinline__ int64_t block_sum(int64_t x, int64_t *red)
 //                two, with a second fp16 of what that leaves for fp32 inputs;
 //   O^T += V^T P^T  the weights times the slot's scale, per group of 32, as fp16, transposed by
 //                movmatrix; with SPLIT a second fp16 of what the first leaves, for fp32 outputs; values as
-//                fp16 pairs of slots by byte permutes.
+//                fp16 pairs of slots, paired as codes (half the instructions of pairing them as fp16).
 // The weights are 2^(s - m + 4 - ev), ev the exponent of the largest value scale so far and m a reference that
 // moves only when a score exceeds it by more than 2^8: weight times scale stays below 2^13, and what a
 // weight of 2^-18 of the reference's or more loses to fp16 is its 11 bits' rounding. Sums and O carry the same factor, which cancels.
@@ -403,7 +395,6 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
     constexpr int NG = L::NG, NM = L::NM, kWarpTiles = L::TILES, kStageSlots = L::SLOTS, kStages = L::STAGES;
     constexpr bool LO = sizeof(T) == 4;  // the query needs a second part
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int64_t red[kWarps];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
     const int per_seq = a.lists / a.c.B;
     unsigned char *const ring = smem + warp * (kStages * L::STAGE);
@@ -415,40 +406,49 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
     }
     __syncwarp();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    Shares sh;
-    {
-        int64_t n = 0;
-        for (int b = threadIdx.x; b < a.c.B; b += kThreads) n += units_of(a, b);
-        sh.total = block_sum(n, red) * per_seq;
-    }
-    const int ctas = (int)min((int64_t)gridDim.x, sh.total);  // no run is empty
+    // this CTA's run of units, and the sequence that its first one is in
+    int64_t total = 0;
+    int64_t mine = units_of(a, lane);  // of the sequences that the search below looks at
+    for (int b0 = 0; b0 < a.c.B; b0 += 32) total += warp_sum64(b0 == 0 ? mine : units_of(a, b0 + lane));
+    total *= per_seq;
+    const int ctas = (int)min((int64_t)gridDim.x, total);  // no run is empty
     if ((int)blockIdx.x >= ctas) return;
-    int64_t at = sh.begin(blockIdx.x, ctas);
-    const int64_t end = sh.begin(blockIdx.x + 1, ctas);
-    // the list that holds unit `at`, and its first unit
+    int64_t at = mul_div(total, blockIdx.x, ctas);
+    const int64_t end = mul_div(total, blockIdx.x + 1, ctas);
     int b = 0;
-    int64_t base = 0;
-    while (b < a.c.B && at < end) {
-        // whole sequences before the run, a block's worth at a time
-        int64_t n = 0;
-        for (int e = b + threadIdx.x; e < min(b + kThreads, a.c.B); e += kThreads) n += units_of(a, e);
-        n = block_sum(n, red) * per_seq;
-        if (base + n > at) break;
-        base += n;
-        b += kThreads;
+    int64_t base = 0;  // first unit of sequence b
+    for (int b0 = 0;; b0 += 32) {
+        if (b0 > 0) mine = units_of(a, b0 + lane);
+        int64_t upto = mine * per_seq;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        const uint32_t past = __ballot_sync(0xFFFFFFFFu, base + upto > at);
+        if (past != 0u) {
+            const int first = __ffs(past) - 1;
+            b = b0 + first;
+            base += __shfl_sync(0xFFFFFFFFu, upto - mine * per_seq, first);
+            break;
+        }
+        base += __shfl_sync(0xFFFFFFFFu, upto, 31);  // (a sequence past `at` exists: at < total)
     }
     int used = 0, phase = 0;  // the warp's next stage of its ring, and the phase of its barrier
     bool ok = true;
     for (; b < a.c.B && at < end; ++b) {
         const int64_t len = slots_of(a, b), units = (len + kUnit - 1) / kUnit;
-        if (base + units * per_seq <= at) {
-            base += units * per_seq;
-            continue;
-        }
-        for (int y = 0; y < per_seq && at < end; ++y, base += units) {
-        if (base + units <= at) continue;
+        if (units == 0) continue;
+        // (below per_seq: at lies in this sequence)
+        const int y0 = at - base <= 0xFFFFFFFFLL ? (int)((uint32_t)(at - base) / (uint32_t)units) : (int)((at - base) / units);
+        base += y0 * units;
+        for (int y = y0; y < per_seq && at < end; ++y, base += units) {
         const int64_t u1 = min(end, base + units);
         const int64_t first = (at - base) * kUnit;
+        if (threadIdx.x == 0) {  // which CTAs' parts make up the list
+            if (first == 0) a.list_cta[2 * ((int64_t)b * per_seq + y)] = (int)blockIdx.x;
+            if (u1 == base + units) a.list_cta[2 * ((int64_t)b * per_seq + y) + 1] = (int)blockIdx.x;
+        }
         const int n = (int)(min(len, (u1 - base) * kUnit) - first);  // slots of this part
         at = u1;
         const int kvh = y % a.c.Hkv, h0 = y / a.c.Hkv * 8;  // first head of the block
@@ -467,12 +467,6 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             bulk_load(dst + L::OFF_V, a.c.v + (row0 + s0) * L::CODES, rows * L::CODES, bar);
             bulk_load(dst + L::OFF_VS, a.c.v_scale + (row0 + s0) * NG, rows * L::SCALES, bar);
         };
-        // (the ring is empty here: the last part's stages were waited for, and its outputs have left it)
-        if (lane == 0 && ok)
-            for (int i = 0, s0 = warp * per, slot = used; i < kStages && s0 < n; ++i, s0 += s_step) {
-                fetch(s0, slot);
-                slot = slot + 1 == kStages ? 0 : slot + 1;
-            }
         // the queries: lane (g8, t4) holds elements 32 g + 8 t4 .. + 7 of head g8 of each block, scaled by 2^-e
         uint32_t qh[NG][4], ql[LO ? NG : 1][4];
         float unscale[2];  // of heads 2 t4, 2 t4 + 1: log2(e) / sqrt(D) 2^e
@@ -481,13 +475,20 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             const bool have = h < nh;
             const T *q = reinterpret_cast<const T *>(a.q) + (head0 + (have ? h : 0)) * D + 8 * t4;
             Raw<T, 8> x[NG];
+#pragma unroll
+            for (int g = 0; g < NG; ++g) x[g].load(q + kCacheGroup * g);
+            // after the queries' loads: behind all the CTAs' copies, 30 MB at once, they would take 4 us
+            // (the ring is empty here: the last part's stages were waited for, and its outputs have left it)
+            if (lane == 0 && ok)
+                for (int i = 0, s0 = warp * per, slot = used; i < kStages && s0 < n; ++i, s0 += s_step) {
+                    fetch(s0, slot);
+                    slot = slot + 1 == kStages ? 0 : slot + 1;
+                }
             uint32_t top = 0;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) {
-                x[g].load(q + kCacheGroup * g);
+            for (int g = 0; g < NG; ++g)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = max(top, mag(x[g][e]));
-            }
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
             // |q| 2^-e below 2^13; the exponent stays where both factors are normal numbers
@@ -655,14 +656,17 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                     }
 #pragma unroll
                     for (int q4 = 0; q4 < NM / 4; ++q4) {
-                        uint32_t w[4][4];
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) unpack4(vw[r][q4], w[r]);
+                        // byte e of the words x (slots of rows 2 t, 2 t + 1) and y (2 t + 8, 2 t + 9): the pair of values
+                        // of element 2 g8 (index 0) or 2 g8 + 1 (1) of tile 4 q4 + e
+                        uint32_t x[2][4], y[2][4];
+                        unpack4(low_halves(vw[0][q4], vw[1][q4]), x[0]);
+                        unpack4(high_halves(vw[0][q4], vw[1][q4]), x[1]);
+                        unpack4(low_halves(vw[2][q4], vw[3][q4]), y[0]);
+                        unpack4(high_halves(vw[2][q4], vw[3][q4]), y[1]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int tl = 4 * q4 + e;
-                            const uint32_t f[4] = {__byte_perm(w[0][e], w[1][e], 0x5410), __byte_perm(w[0][e], w[1][e], 0x7632),
-                                                   __byte_perm(w[2][e], w[3][e], 0x5410), __byte_perm(w[2][e], w[3][e], 0x7632)};
+                            const uint32_t f[4] = {x[0][e], x[1][e], y[0][e], y[1][e]};
                             if constexpr (SPLIT) {
                                 if (i == 0)
                                     mma0(part[tl], f, bl[tl / 2][0], bl[tl / 2][1]);
@@ -756,36 +760,18 @@ template <typename TO, int D>
 __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4AttendArgs a)
 {
     constexpr int C = D / 32, block_heads = 8;
-    __shared__ int64_t red[kJoinWarps];
     __shared__ float so[kJoinWarps][D];
     __shared__ float2 sml[kJoinWarps];
     extern __shared__ float2 stat[];  // [G], weights
     const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_seq = a.lists / a.c.B;
-    Shares sh;
-    int64_t before = 0;  // units of the sequences before this one
-    {
-        int64_t n = 0, m = 0;
-        for (int e = threadIdx.x; e < a.c.B; e += kJoinThreads) {
-            const int64_t u = units_of(a, e);
-            n += u;
-            m += e < b ? u : 0;
-        }
-        sh.total = block_sum(n, red) * per_seq;
-        before = block_sum(m, red) * per_seq;
-    }
-    const int64_t len = slots_of(a, b), units = (len + kUnit - 1) / kUnit;
-    const int ctas = (int)min((int64_t)a.ctas, sh.total);
+    const int64_t len = slots_of(a, b);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // the parts of list y of this sequence: CTAs i0 .. i1, partial numbers i + list
     auto parts = [&](int y, int &i0, int &i1) {
-        if (units == 0) {
-            i0 = 0, i1 = -1;
-            return;
-        }
-        const int64_t u0 = before + y * units;
-        i0 = sh.cta_of(u0, ctas);
-        i1 = sh.cta_of(u0 + units - 1, ctas);
+        const int2 x = reinterpret_cast<const int2 *>(a.list_cta)[(int64_t)b * per_seq + y];
+        i0 = len > 0 ? x.x : 0;
+        i1 = len > 0 ? x.y : -1;
     };
     if ((int)blockIdx.x < a.Hq) {
         const int h = blockIdx.x, kvh = h / a.G, hb = (h % a.G) / block_heads, y = hb * a.c.Hkv + kvh;

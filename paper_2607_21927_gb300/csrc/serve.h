@@ -110,6 +110,7 @@ struct Cache4AttendArgs {
     int32_t ctas;                // among which the slots are shared out
     float *part_o;               // [ctas + lists][heads of a block][D]
     float2 *part_ml;             // [ctas + lists][heads of a block]
+    int32_t *list_cta;           // [lists][2] first and last CTA of each list that holds slots
     float *scores;               // weights: [B][Hq][cap] scores in log2
 };
 cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s);

@@ -531,10 +531,12 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
     const size_t o_b = room(sizeof(float) * parts * cache->head_dim), ml_b = room(sizeof(float2) * parts);
     const size_t score_b = weight_out != nullptr ? sizeof(float) * (size_t)cache->batch * heads * cache->capacity : 0;
     Scratch mem;
-    RIS_CUDA(mem.alloc(o_b + ml_b + score_b, s));
+    const size_t list_b = room(2 * sizeof(int32_t) * (size_t)lists);
+    RIS_CUDA(mem.alloc(o_b + ml_b + list_b + score_b, s));
     a.part_o = static_cast<float *>(mem.p);
     a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(mem.p) + o_b);
-    if (weight_out != nullptr) a.scores = reinterpret_cast<float *>(static_cast<char *>(mem.p) + o_b + ml_b);
+    a.list_cta = reinterpret_cast<int32_t *>(static_cast<char *>(mem.p) + o_b + ml_b);
+    if (weight_out != nullptr) a.scores = reinterpret_cast<float *>(static_cast<char *>(mem.p) + o_b + ml_b + list_b);
     RIS_CUDA(launch_cache4_attend(a, dtype, out_dtype, s));
     return RIS_OK;
 }
