@@ -265,7 +265,7 @@ struct Lay {
     static constexpr int OFF_K = 0, OFF_V = OFF_K + SLOTS * CODES, OFF_KS = OFF_V + SLOTS * CODES, OFF_VS = OFF_KS + SLOTS * SCALES,
                          STAGE = OFF_VS + SLOTS * SCALES;
     static constexpr int OFF_BARS = kWarps * STAGES * STAGE, BYTES = OFF_BARS + 8 * kWarps * STAGES;
-    static_assert(kWarps * 8 * (D * 4 + 8) <= OFF_BARS, "the warps' parts of a list pass through the rings");
+    static_assert(kWarps * 8 * ((D + 4) * 4 + 12) <= OFF_BARS, "the warps' parts of a list pass through the rings");
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -705,42 +705,49 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                 phase ^= 1;
             }
         }
-        // the four warps' parts of each head, through the rings: [warp][head][D] and (maximum, sum)
+        // the four warps' parts of each head, through the rings: [warp][head][D], (maximum, sum), factors
         __syncthreads();
+        constexpr int LO_ = D + 4;  // (the four lanes t4 write rows two apart)
         float *const so = reinterpret_cast<float *>(smem);
-        float2 *const sml = reinterpret_cast<float2 *>(smem + kWarps * 8 * D * 4);
+        float2 *const sml = reinterpret_cast<float2 *>(so + kWarps * 8 * LO_);
+        float *const sf = reinterpret_cast<float *>(sml + kWarps * 8);
         const float back = pow2i(ev - 4);
-        {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                float x = l[e] * back;
+        for (int e = 0; e < 2; ++e) {
+            float x = l[e] * back;
 #pragma unroll
-                for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, w);
-                const int h = 2 * t4 + e;
-                if (g8 == 0) sml[warp * 8 + h] = make_float2(m[e], x);
+            for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, w);
+            const int h = 2 * t4 + e;
+            if (g8 == 0) sml[warp * 8 + h] = make_float2(m[e], x);
 #pragma unroll
-                for (int tl = 0; tl < NM; ++tl)
-                    *reinterpret_cast<float2 *>(so + (warp * 8 + h) * D + 16 * tl + 2 * g8) =
-                        make_float2(o[tl][e] * back, o[tl][e + 2] * back);
-            }
+            for (int tl = 0; tl < NM; ++tl)
+                *reinterpret_cast<float2 *>(so + (warp * 8 + h) * LO_ + 16 * tl + 2 * g8) = make_float2(o[tl][e] * back, o[tl][e + 2] * back);
         }
         __syncthreads();
         // one partial per head of the block: number cta + list
         const int64_t part = ((int64_t)blockIdx.x + (int64_t)b * per_seq + y) * 8;
-        for (int t = threadIdx.x; t < nh * D; t += kThreads) {
-            const int h = t / D, d = t % D;
-            float M = -INFINITY, sum = 0.f, x = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sml[w * 8 + h].x);
+        if (warp == 0) {  // lane: warp lane / 8, head lane mod 8
+            const float2 ml = sml[lane];
+            float M = fmaxf(ml.x, __shfl_xor_sync(0xFFFFFFFFu, ml.x, 8));
+            M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, 16));
+            const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
+            float sum = ml.y * f;
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
+            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
+            sf[lane] = f;
+            if (lane < nh) a.part_ml[part + lane] = make_float2(M, sum);
+        }
+        __syncthreads();
+        for (int t = threadIdx.x; t < nh * (D / 4); t += kThreads) {
+            const int h = t / (D / 4), d = t % (D / 4) * 4;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                const float2 ml = sml[w * 8 + h];
-                const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-                sum = fmaf(ml.y, f, sum);
-                x = fmaf(so[(w * 8 + h) * D + d], f, x);
+                const float f = sf[w * 8 + h];
+                const float4 v = *reinterpret_cast<const float4 *>(so + (w * 8 + h) * LO_ + d);
+                x.x = fmaf(v.x, f, x.x), x.y = fmaf(v.y, f, x.y), x.z = fmaf(v.z, f, x.z), x.w = fmaf(v.w, f, x.w);
             }
-            a.part_o[(part + h) * D + d] = x;
-            if (d == 0) a.part_ml[part + h] = make_float2(M, sum);
+            *reinterpret_cast<float4 *>(a.part_o + (part + h) * D + d) = x;
         }
         // the rings take copies again: after every read of them, and ordered before them
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -754,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
 // channels; then (weights) CTAs that add up what each slot got from the heads of its KV head, from the scores that
 // the first kernel left. Launched as its programmatic dependent.
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
-constexpr int kWeightSlots = 512;  // slots of a CTA
+constexpr int kWeightSlots = 4 * kJoinThreads;  // slots of a CTA
 
 template <typename TO, int D>
 __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4AttendArgs a)
@@ -766,6 +773,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
     const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_seq = a.lists / a.c.B;
     const int64_t len = slots_of(a, b);
+    // a CTA of the weights: its KV head and this thread's four slots
+    const int w = (int)blockIdx.x - a.Hq, blocks = ((int)gridDim.x - a.Hq) / a.c.Hkv, kvh_w = w >= 0 ? w / blocks : 0;
+    const int64_t s0 = (int64_t)(w >= 0 ? w % blocks : 0) * kWeightSlots;
+    if (w >= 0 && s0 >= len) return;  // (the CTAs of the outputs wait for the first kernel in any case)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     // the parts of list y of this sequence: CTAs i0 .. i1, partial numbers i + list
     auto parts = [&](int y, int &i0, int &i1) {
@@ -817,15 +828,23 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         }
         return;
     }
-    // weights
-    const int w = blockIdx.x - a.Hq, blocks = (gridDim.x - a.Hq) / a.c.Hkv, kvh = w / blocks;
-    const int64_t s0 = (int64_t)(w % blocks) * kWeightSlots;
-    if (s0 >= len) return;
+    // weights: the scores of the first eight heads are on their way before the heads' sums are known
+    const int64_t s1 = s0 + 4 * threadIdx.x, row = ((int64_t)b * a.c.Hkv + kvh_w) * a.c.cap + s1;
+    const float *sc = a.scores + ((int64_t)b * a.Hq + kvh_w * a.G) * a.c.cap + s1;
+    const bool in = s1 < len;
+    float4 x[8], y = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto load = [&](int h0) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (in && h0 + e < a.G) x[e] = *reinterpret_cast<const float4 *>(sc + (h0 + e) * a.c.cap);
+    };
+    load(0);
+    if (in && a.weight_in != nullptr) y = *reinterpret_cast<const float4 *>(a.weight_in + row);
     for (int h = warp; h < a.G; h += kJoinWarps) {  // a warp per head, a lane per part
-        const int y = h / block_heads * a.c.Hkv + kvh;
+        const int yl = h / block_heads * a.c.Hkv + kvh_w;
         int i0, i1;
-        parts(y, i0, i1);
-        const int64_t p0 = ((int64_t)b * per_seq + y) * block_heads + h % block_heads;
+        parts(yl, i0, i1);
+        const int64_t p0 = ((int64_t)b * per_seq + yl) * block_heads + h % block_heads;
         float M = -INFINITY, sum = 0.f;
         for (int i = i0 + lane; i <= i1; i += 32) {
             const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
@@ -838,23 +857,23 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         if (lane == 0) stat[h] = make_float2(tm, 1.f / sum);
     }
     __syncthreads();
-    const int64_t row = ((int64_t)b * a.c.Hkv + kvh) * a.c.cap;
-    const float *sc = a.scores + ((int64_t)b * a.Hq + kvh * a.G) * a.c.cap;
-    constexpr int P = kWeightSlots / kJoinThreads;
-    float x[P] = {};
-#pragma unroll 2
-    for (int h = 0; h < a.G; ++h) {
-        const float2 ml = stat[h];
+    for (int h0 = 0; h0 < a.G; h0 += 8) {
+        if (h0 > 0) load(h0);
 #pragma unroll
-        for (int e = 0; e < P; ++e) {
-            const int64_t s = s0 + threadIdx.x + e * kJoinThreads;
-            if (s < len) x[e] = fmaf(ex2(sc[h * a.c.cap + s] - ml.x), ml.y, x[e]);
-        }
+        for (int e = 0; e < 8; ++e)
+            if (in && h0 + e < a.G) {
+                const float2 ml = stat[h0 + e];
+                y.x = fmaf(ex2(x[e].x - ml.x), ml.y, y.x);
+                y.y = fmaf(ex2(x[e].y - ml.x), ml.y, y.y);
+                y.z = fmaf(ex2(x[e].z - ml.x), ml.y, y.z);
+                y.w = fmaf(ex2(x[e].w - ml.x), ml.y, y.w);
+            }
     }
-#pragma unroll
-    for (int e = 0; e < P; ++e) {
-        const int64_t s = s0 + threadIdx.x + e * kJoinThreads;
-        if (s < len) a.weight_out[row + s] = (a.weight_in != nullptr ? a.weight_in[row + s] : 0.f) + x[e];
+    if (s1 + 4 <= len) {
+        *reinterpret_cast<float4 *>(a.weight_out + row) = y;
+    } else if (in) {  // slots past the length stay as they are
+        const float z[4] = {y.x, y.y, y.z, y.w};
+        for (int e = 0; e < (int)(len - s1); ++e) a.weight_out[row + e] = z[e];
     }
 }
 
