@@ -516,3 +516,118 @@ def test_serving_round_trip():
         for h in range(Hkv):
             have = sorted(cache.pos[b, h, :want[b]].tolist())
             assert have[-20:] == list(range(m + 4 - 20, m + 4)) and len(set(have)) == len(have)
+
+
+# ---------------------------------------------------------------- prompts behind many keys
+LONG_KEYS = ([200, 130, 3, 0, 40], [5000, 6000, 1, 7, 20])  # short rows behind long prompts: the rows' tiles see some 30 key tiles each
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(6, 2, 128), (8, 2, 128), (2, 2, 128), (5, 1, 64), (4, 2, 64)])
+@pytest.mark.parametrize("out_dtype", [F32, BF16])
+def test_attention_packed_behind_long_prompts(Hq, Hkv, D, out_dtype):
+    n, m = LONG_KEYS
+    q = randn(sum(n), Hq, D, seed=1, dtype=BF16, scale=2.0)
+    kv = randn(sum(m), 2 * Hkv, D, seed=2, dtype=BF16)
+    k, v = kv[:, :Hkv], kv[:, Hkv:]
+    with ris.ris_pack_create(n, m) as pack:
+        out, lse, w = ris.ris_attention_packed(pack, q, k, v, out_dtype=out_dtype, return_lse=True, weight_rows=150)
+        ris.ris_device_status()
+    ro, rl, rw = packed_plain(q, k, v, n, m, 150)
+    check_bf16_path(to_np(out), ro.numpy(), out_bf16=out_dtype == BF16)
+    empty = rl == -INF
+    assert empty.any() and (lse.double().cpu()[empty] == -INF).all() and (out.cpu()[empty.T] == 0).all()
+    assert ((lse.double().cpu() - rl)[~empty].abs() <= 2e-5 * (1 + rl[~empty].abs())).all()
+    assert (w.double().cpu() - rw).abs().max() <= 2e-5 * max(1.0, float(rw.max()))
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(3, 1), (4, 1)])
+@pytest.mark.parametrize("bad", [INF, -INF, float("nan")])
+def test_attention_packed_hidden_keys_behind_long_prompts(Hq, Hkv, bad):
+    """An infinity or NaN among the last keys of the first sequence reaches only its rows that see it."""
+    n, m = LONG_KEYS
+    q = randn(sum(n), Hq, 128, seed=1, dtype=BF16)
+    k, v = randn(sum(m), Hkv, 128, seed=2, dtype=BF16), randn(sum(m), Hkv, 128, seed=3, dtype=BF16)
+    with ris.ris_pack_create(n, m) as pack:
+        good, = ris.ris_attention_packed(pack, q, k, v)
+        for x in (k, v):
+            y = x.clone()
+            y[4900, 0, 5] = bad  # seen by rows 100 .. 199
+            y[4999, 0, 6] = bad
+            got, = ris.ris_attention_packed(pack, q, y if x is k else k, y if x is v else v)
+            ris.ris_device_status()
+            rows = torch.ones(sum(n), dtype=torch.bool, device="cuda")
+            rows[100:200] = False
+            tol = 0.0 if x is k else 2 ** -7
+            assert torch.isfinite(got[rows]).all()
+            assert ((got[rows].float() - good[rows].float()).abs() <= tol * good[rows].float().abs() + (tol > 0) * 1e-2).all()
+            if x is v:
+                assert not torch.isfinite(got[100:200, :, 5].float()).any()
+
+
+# ---------------------------------------------------------------- allocations that fail, streams, the example
+@pytest.fixture
+def allocations():
+    yield ris.ris_debug_fail_allocation
+    ris.ris_debug_fail_allocation(-1)
+
+
+def test_serving_allocation_failures(allocations):
+    """Every allocation of every call, failed in turn: the call reports it, nothing is kept, the next call is right."""
+    lens, Hq, Hkv, D = [70, 200], 4, 2, 128
+    q, k, v = (randn(270, h, D, seed=h, dtype=BF16) for h in (Hq, Hkv, Hkv))
+    cache = filled(2, Hkv, D, 256, [256, 199])
+    dst = ris.Cache4.empty(2, Hkv, D, 64)
+    pack = ris.ris_pack_create(lens)
+    qt = q[:2].contiguous()
+    calls = [lambda: ris.ris_pack_create(lens),
+             lambda: ris.ris_attention_packed(pack, q, k, v, return_lse=True, weight_rows=8),
+             lambda: ris.ris_cache4_attend(cache, qt, weight_out=dst_weight),
+             lambda: ris.ris_cache4_evict(cache, dst, 64, 8)]
+    dst_weight = torch.zeros_like(cache.weight)
+    for call in calls:
+        first = call()
+        torch.cuda.synchronize()
+        in_use = ris.ris_memory_stats()[0]
+        failed = 0
+        for n in range(8):
+            ris.ris_debug_fail_allocation(n)
+            try:
+                call()
+            except ris.RisError as e:
+                assert e.status == ris.RIS_ERR_OOM
+                failed += 1
+                torch.cuda.synchronize()
+                assert ris.ris_memory_stats()[0] == in_use
+            else:
+                break
+            finally:
+                ris.ris_debug_fail_allocation(-1)
+        assert failed >= 1 and n < 7
+        again = call()
+        ris.ris_device_status()
+        if isinstance(first, tuple):
+            assert all(torch.equal(a, b) for a, b in zip(first, again))
+        elif torch.is_tensor(first):
+            assert torch.equal(first, again)
+
+
+def test_example_serves_prompts():
+    import importlib.util
+    import os
+
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_prompts.py")
+    spec = importlib.util.spec_from_file_location("serve_prompts", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    lens, tokens, budget, slack = [300, 33, 150], 21, 128, 8
+    server, states = example.main(["--prompts", *map(str, lens), "--image", "4", "6", "--layers", "2", "--tokens", str(tokens),
+                                   "--budget", str(budget), "--recent", "32", "--slack", str(slack)])
+    assert states.shape == (tokens, 3, 12 * 128) and torch.isfinite(states.float()).all()
+    # cuts before steps 8 and 16; the second sequence grows from 33 to 54 without reaching the budget
+    assert server.layers[0].cache.length.tolist() == [128 + 5, 33 + 21, 128 + 5]
+    assert server.token.tolist() == [n + tokens for n in lens]
+    assert server.time.tolist() == [300 - 24 + 6 + tokens, 33 + tokens, 150 + tokens]
+    for layer in server.layers:
+        for b, n in enumerate(lens):
+            have = layer.cache.pos[b, 0, :int(layer.cache.length[b])].tolist()
+            assert len(set(have)) == len(have) and set(range(n + tokens - 32, n + tokens)) <= set(have)
