@@ -1160,8 +1160,9 @@ template <int DT>
 struct LayW {
     static constexpr int RC = 64, NQ = 3, NB = DT / 64;    // rows of a chunk, ring stages, 64-column blocks
     static constexpr int K_BLK = BN * 128, Q_BLK = RC * 128, Q_STAGE = NB * Q_BLK;
-    static constexpr int OFF_K = 0, OFF_Q = OFF_K + NB * K_BLK, OFF_STAT = OFF_Q + NQ * Q_STAGE;  // float2 [4][RC]
-    static constexpr int OFF_BARS = OFF_STAT + 4 * RC * 8, OFF_TMEM = OFF_BARS + 128, BYTES = OFF_TMEM + 16;
+    static constexpr int NST = 4;                          // chunks of row statistics, a warp's own, in flight or in use
+    static constexpr int OFF_K = 0, OFF_Q = OFF_K + NB * K_BLK, OFF_STAT = OFF_Q + NQ * Q_STAGE;  // float2 [4][NST][RC]
+    static constexpr int OFF_BARS = OFF_STAT + 4 * NST * RC * 8, OFF_TMEM = OFF_BARS + 128, BYTES = OFF_TMEM + 16;
     static constexpr int B_K_FULL = 0, B_Q_FULL = 1, B_Q_FREE = B_Q_FULL + NQ, B_S_FULL = B_Q_FREE + NQ, B_S_FREE = B_S_FULL + 2,
                          NBAR = B_S_FREE + 2;
     static constexpr uint32_t COLS = 2 * RC;
@@ -1169,10 +1170,10 @@ struct LayW {
 constexpr int kWeightThreads = 192;
 
 template <int DT>
-__global__ void __launch_bounds__(kWeightThreads) k_packed_weights_tc(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+__global__ void __launch_bounds__(kWeightThreads, DT == 64 ? 4 : 2) k_packed_weights_tc(const PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
     using L = LayW<DT>;
-    constexpr int RC = L::RC, NQ = L::NQ, NB = L::NB;
+    constexpr int RC = L::RC, NQ = L::NQ, NB = L::NB, NST = L::NST;
     extern __shared__ __align__(1024) unsigned char smem[];
     uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
     const uint32_t sbase = smem_u32(smem);
@@ -1224,6 +1225,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_packed_weights_tc(const Pack
         }
     } else if (warp == 5) {
         constexpr uint32_t ID = idesc_bf16(BN, RC, false);
+        const uint32_t tb = __reduce_max_sync(0xFFFFFFFFu, tmem);  // (into a uniform register)
         auto wait_all = [&](int i, int parity) -> bool {
             const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
             tc_fence_after();
@@ -1240,7 +1242,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_packed_weights_tc(const Pack
             if (elect_one()) {
 #pragma unroll
                 for (int ks = 0; ks < DT / 16; ++ks)
-                    tc_mma_ss<1>(tmem + b * RC, kd + dstep((ks >> 2) * L::K_BLK + (ks & 3) * 32), qd + dstep((ks >> 2) * L::Q_BLK + (ks & 3) * 32),
+                    tc_mma_ss<1>(tb + b * RC, kd + dstep((ks >> 2) * L::K_BLK + (ks & 3) * 32), qd + dstep((ks >> 2) * L::Q_BLK + (ks & 3) * 32),
                                  ID, ks > 0);
                 tc_commit<1>(bar(L::B_S_FULL + b));
                 tc_commit<1>(bar(L::B_Q_FREE + st));
@@ -1254,57 +1256,65 @@ __global__ void __launch_bounds__(kWeightThreads) k_packed_weights_tc(const Pack
             for (int s = max(0, n - NQ); s < n; ++s) mbar_wait_own<1>(bar(L::B_Q_FREE + s % NQ), (s / NQ) & 1);
         }
     } else {
-        float2 *const st_sh = reinterpret_cast<float2 *>(smem + L::OFF_STAT) + warp * RC;
+        float2 *const st_sh = reinterpret_cast<float2 *>(smem + L::OFF_STAT) + warp * NST * RC;
         const float sc = a.scale_log2;
         const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
         float w = 0.f;
-        auto stats = [&](int s, float2 (&x)[RC / 32]) {
-            const int i0 = first + s % chunks * RC;
-            const float2 *p = a.row_stat + (int64_t)(g * a.G + s / chunks) * a.q_total + it.q_base;
+        // the maxima and 1 / sums of step s's rows, zeros past the last row
+        auto stats = [&](int s) {
+            if (s < steps) {
+                const int i0 = first + s % chunks * RC;
+                const float2 *p = a.row_stat + (int64_t)(g * a.G + s / chunks) * a.q_total + it.q_base;
 #pragma unroll
-            for (int e = 0; e < RC / 32; ++e) {
-                const int i = i0 + lane + 32 * e;
-                x[e] = s < steps && i < it.q_len ? p[i] : make_float2(0.f, 0.f);
+                for (int e = lane; e < RC; e += 32)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(smem_u32(st_sh + s % NST * RC + e)),
+                                 "l"(p + min(i0 + e, it.q_len - 1)), "r"(i0 + e < it.q_len ? 8 : 0)
+                                 : "memory");
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        float2 next[RC / 32];
-        stats(0, next);
+        for (int s = 0; s < NST - 1; ++s) stats(s);
         for (int s = 0; s < steps && ok; ++s) {
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < RC / 32; ++e) st_sh[lane + 32 * e] = next[e];
-            stats(s + 1, next);
+            asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
+            __syncwarp();  // step s's are there for every lane, and every lane is done with those of step s - 1
+            stats(s + NST - 1);
+            const float2 *const st = st_sh + s % NST * RC;
             ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_S_FULL + (s & 1)), (s / 2) & 1, gave_up));
             if (!ok) break;
             tc_fence_after();
-            uint32_t sv[RC];
-            tmem_issue64(tmem + (s & 1) * RC + lane_off, sv);
-            tmem_wait_ld();
-            pin64(sv);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0 && s + 2 < steps) mbar_arrive(bar(L::B_S_FREE + (s & 1)));
             const int i0 = first + s % chunks * RC;
             const int from = j - shift - i0;   // first row of the chunk that sees this thread's key
             const int rows = it.q_len - i0;    // rows of the chunk
+            const bool whole = it.row + warp * 32 + 31 - shift <= i0 && rows >= RC;
             float part[4] = {};
-            if (it.row + warp * 32 + 31 - shift <= i0 && rows >= RC) {
 #pragma unroll
-                for (int e = 0; e < RC; e += 2) {
-                    const float4 ml = *reinterpret_cast<const float4 *>(&st_sh[e]);
-                    part[e & 2] = fmaf(ex2(fmaf(__uint_as_float(sv[e]), sc, -ml.x)), ml.y, part[e & 2]);
-                    part[(e & 2) + 1] = fmaf(ex2(fmaf(__uint_as_float(sv[e + 1]), sc, -ml.z)), ml.w, part[(e & 2) + 1]);
+            for (int half = 0; half < RC; half += 32) {
+                float sv[32];
+                tmem_ld32(tmem + (s & 1) * RC + lane_off + half, sv);
+                if (half == RC - 32) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0 && s + 2 < steps) mbar_arrive(bar(L::B_S_FREE + (s & 1)));
                 }
-            } else {
+                if (whole) {
 #pragma unroll
-                for (int e = 0; e < RC; ++e) {
-                    const float2 ml = st_sh[e];
-                    const float p = ex2(fmaf(__uint_as_float(sv[e]), sc, -ml.x));
-                    if (e >= from && e < rows) part[e & 3] = fmaf(p, ml.y, part[e & 3]);
+                    for (int e = 0; e < 32; e += 2) {
+                        const float4 ml = *reinterpret_cast<const float4 *>(&st[half + e]);
+                        part[e & 2] = fmaf(ex2(fmaf(sv[e], sc, -ml.x)), ml.y, part[e & 2]);
+                        part[(e & 2) + 1] = fmaf(ex2(fmaf(sv[e + 1], sc, -ml.z)), ml.w, part[(e & 2) + 1]);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float2 ml = st[half + e];
+                        const float p = ex2(fmaf(sv[e], sc, -ml.x));
+                        if (half + e >= from && half + e < rows) part[e & 3] = fmaf(p, ml.y, part[e & 3]);
+                    }
                 }
             }
             w += (part[0] + part[1]) + (part[2] + part[3]);
         }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
         if (ok && j < it.k_len) a.key_weight[(int64_t)g * a.k_total + it.k_base + j] = w;
     }
     if (!ok) atomicOr(&g_ris_packed_error, 2u);
@@ -1477,8 +1487,8 @@ cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
         if (e != cudaSuccess) return e;
         k_packed_weights_tc<128><<<grid, kWeightThreads, LayW<128>::BYTES, s>>>(a, maps);
     } else {
-        // 60 KB where 40 would do: five CTAs of an SM would ask for more TMEM columns than there are
-        constexpr int bytes = 60 << 10;
+        // 52 KB where 49 would do: four CTAs to an SM; five would ask for more TMEM columns than there are
+        constexpr int bytes = 52 << 10;
         static_assert(bytes >= LayW<64>::BYTES, "");
         e = cudaFuncSetAttribute(k_packed_weights_tc<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != cudaSuccess) return e;
