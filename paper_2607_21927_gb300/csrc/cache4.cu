@@ -116,6 +116,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4Ap
     const int64_t r_in = in ? r : n_rows - 1;
     const int64_t tok = n_rows <= 0xFFFFFFFFLL ? (int64_t)((uint32_t)r_in / (uint32_t)a.c.Hkv) : r_in / a.c.Hkv;
     const int head = (int)(r_in - tok * a.c.Hkv);
+    after_last();
     // lane u: the keys' elements 32 g + 8 u .. + 7 of every group, the values' 16 e + 4 u .. + 3 of every tile
     Raw<T, 8> xk[NG];
     Raw<T, 4> xv[NM];
@@ -220,6 +221,7 @@ __global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c
 {
     constexpr int Q = D / 4, NG = D / kCacheGroup, NM = D / 16, STEP = kReadThreads / Q;
     const int64_t bh = blockIdx.x / blocks;
+    after_last();
     const int64_t i0 = (int64_t)(blockIdx.x - bh * blocks) * kReadRows + threadIdx.x / Q;
     const int e = threadIdx.x % Q;  // elements 4 e .. 4 e + 3: bytes 2 e, 2 e + 1 in natural order
     const int b = (int)(bh / c.Hkv);
@@ -405,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     __syncwarp();
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    after_last();  // (the join reads the lengths before it waits for this kernel)
     // this CTA's run of units, and the sequence that its first one is in
     int64_t total = 0;
     int64_t mine = units_of(a, lane);  // of the sequences that the search below looks at
@@ -777,7 +779,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
     const int w = (int)blockIdx.x - a.Hq, blocks = ((int)gridDim.x - a.Hq) / a.c.Hkv, kvh_w = w >= 0 ? w / blocks : 0;
     const int64_t s0 = (int64_t)(w >= 0 ? w % blocks : 0) * kWeightSlots;
     if (w >= 0 && s0 >= len) return;  // (the CTAs of the outputs wait for the first kernel in any case)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_last();
     // the parts of list y of this sequence: CTAs i0 .. i1, partial numbers i + list
     auto parts = [&](int y, int &i0, int &i1) {
         const int2 x = reinterpret_cast<const int2 *>(a.list_cta)[(int64_t)b * per_seq + y];
@@ -886,9 +888,7 @@ cudaError_t launch_part(const Cache4AttendArgs &a, cudaStream_t s)
     static cudaError_t ready = cudaSuccess;
     std::call_once(once, [&] { ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
-    kern<<<(unsigned)a.ctas, kThreads, bytes, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    return launch_chained(kern, dim3((unsigned)a.ctas), dim3(kThreads), bytes, s, a);
 }
 template <typename T, bool SPLIT>
 cudaError_t launch_part_d(const Cache4AttendArgs &a, cudaStream_t s)
@@ -899,19 +899,8 @@ template <typename TO, int D>
 cudaError_t launch_join_d(const Cache4AttendArgs &a, cudaStream_t s)
 {
     const int64_t blocks = a.weight_out != nullptr ? (a.reach + kWeightSlots - 1) / kWeightSlots * a.c.Hkv : 0;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(a.Hq + blocks), (unsigned)a.c.B);
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = a.weight_out != nullptr ? a.G * sizeof(float2) : 0;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_cache4_join<TO, D>, a);
-    note_launch();
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return launch_chained(k_cache4_join<TO, D>, dim3((unsigned)(a.Hq + blocks), (unsigned)a.c.B), dim3(kJoinThreads),
+                          a.weight_out != nullptr ? a.G * sizeof(float2) : 0, s, a);
 }
 template <typename TO>
 cudaError_t launch_join(const Cache4AttendArgs &a, cudaStream_t s)
@@ -924,32 +913,20 @@ cudaError_t launch_join(const Cache4AttendArgs &a, cudaStream_t s)
 cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStream_t s)
 {
     const int64_t rows = a.total * a.c.Hkv, per = kAppendThreads / 4;
-    const dim3 grid((unsigned)((rows + per - 1) / per));
-    if (dtype == RIS_F32) {
-        if (a.c.D == 128)
-            k_cache4_append<float, 128><<<grid, kAppendThreads, 0, s>>>(a);
-        else
-            k_cache4_append<float, 64><<<grid, kAppendThreads, 0, s>>>(a);
-    } else {
-        if (a.c.D == 128)
-            k_cache4_append<__nv_bfloat16, 128><<<grid, kAppendThreads, 0, s>>>(a);
-        else
-            k_cache4_append<__nv_bfloat16, 64><<<grid, kAppendThreads, 0, s>>>(a);
-    }
-    note_launch();
-    return cudaGetLastError();
+    const dim3 grid((unsigned)((rows + per - 1) / per)), block(kAppendThreads);
+    if (dtype == RIS_F32)
+        return a.c.D == 128 ? launch_chained(k_cache4_append<float, 128>, grid, block, 0, s, a)
+                            : launch_chained(k_cache4_append<float, 64>, grid, block, 0, s, a);
+    return a.c.D == 128 ? launch_chained(k_cache4_append<__nv_bfloat16, 128>, grid, block, 0, s, a)
+                        : launch_chained(k_cache4_append<__nv_bfloat16, 64>, grid, block, 0, s, a);
 }
 
 cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_t count, float *k, float *v, cudaStream_t s)
 {
     const int blocks = (int)((count + kReadRows - 1) / kReadRows);
-    const dim3 grid((unsigned)((int64_t)c.B * c.Hkv * blocks), 2);
-    if (c.D == 128)
-        k_cache4_read<128><<<grid, kReadThreads, 0, s>>>(c, first, count, blocks, k, v);
-    else
-        k_cache4_read<64><<<grid, kReadThreads, 0, s>>>(c, first, count, blocks, k, v);
-    note_launch();
-    return cudaGetLastError();
+    const dim3 grid((unsigned)((int64_t)c.B * c.Hkv * blocks), 2), block(kReadThreads);
+    return c.D == 128 ? launch_chained(k_cache4_read<128>, grid, block, 0, s, c, first, count, blocks, k, v)
+                      : launch_chained(k_cache4_read<64>, grid, block, 0, s, c, first, count, blocks, k, v);
 }
 
 cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s)

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs
     __shared__ Exchange ex;
     __shared__ Pair part[kWarps];
     __shared__ int sh_digit, sh_need;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    after_last();
     const int bh = blockIdx.x / size, rank = blockIdx.x % size, b = bh / a.src.Hkv, tid = threadIdx.x;
     const int len = max(0, (int)min((int64_t)a.src.length[b], a.src.cap));
     const int left = min(len, a.budget);
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictAr
     const int bh = blockIdx.x / blocks, u = threadIdx.x & 3;
     const int first = (blockIdx.x - bh * blocks) * (kMoveThreads / 4 * kMoveRows) + threadIdx.x / 4;
     // (nothing that the select kernel reads or writes is touched before it has finished)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    after_last();
     const bool values = u >= 2;
     const uint4 *sc = reinterpret_cast<const uint4 *>(values ? a.src.v : a.src.k);
     uint4 *dc = reinterpret_cast<uint4 *>(values ? a.dst.v : a.dst.k);
@@ -329,13 +329,15 @@ cudaError_t launch_select(const Cache4EvictArgs &a, int32_t *holes, int size, si
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = bytes;
     cfg.stream = s;
-    cudaLaunchAttribute at[1];
+    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = size;
     at[0].val.clusterDim.y = 1;
     at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, k_evict_select<CACHED>, a, holes, size);
     note_launch();
     return e;
@@ -345,18 +347,7 @@ template <int D>
 cudaError_t launch_move(const Cache4EvictArgs &a, cudaStream_t s)
 {
     const int blocks = (a.budget + kMoveThreads / 4 * kMoveRows - 1) / (kMoveThreads / 4 * kMoveRows);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((int64_t)blocks * a.src.B * a.src.Hkv));
-    cfg.blockDim = dim3(kMoveThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_evict_move<D>, a, blocks);
-    note_launch();
-    return e;
+    return launch_chained(k_evict_move<D>, dim3((unsigned)((int64_t)blocks * a.src.B * a.src.Hkv)), dim3(kMoveThreads), 0, s, a, blocks);
 }
 
 }  // namespace

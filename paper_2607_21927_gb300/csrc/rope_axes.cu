@@ -69,6 +69,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_rope_axes(const RopeAxesArgs a)
     constexpr int V = Vec<T>::V;
     const int half = a.D >> 1, c = V * threadIdx.x;  // blockDim.x == half / V
     const int64_t p = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    after_last();
     if (p >= a.n) return;
     // heads h0 .. h1 - 1 of q and k, one after another
     const int heads = a.heads[0] + a.heads[1];
@@ -130,9 +131,7 @@ cudaError_t launch(const RopeAxesArgs &a, cudaStream_t s)
     const int heads = a.heads[0] + a.heads[1];
     // two CTAs per SM before a slice holds every head
     const int slices = (int)std::min<int64_t>(heads, std::max<int64_t>(1, 304 / blocks));
-    k_rope_axes<T><<<dim3((unsigned)blocks, (unsigned)slices), dim3(x, tokens), 0, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    return launch_chained(k_rope_axes<T>, dim3((unsigned)blocks, (unsigned)slices), dim3(x, tokens), 0, s, a);
 }
 
 }  // namespace

@@ -132,4 +132,32 @@ unsigned int read_packed_error();
 // Stream-ordered pool memory, as every allocation of the library (ris_api.cu).
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s);
 
+#ifdef __CUDACC__
+// The serving kernels are a few microseconds each, one after another: each is launched while the last one runs
+// (a programmatic dependent) and waits for it where it begins, so that only the launch itself overlaps: nothing is read
+// or written before `after_last` returns. Its own dependent may start from there on.
+__device__ __forceinline__ void after_last()
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... P, typename... A>
+cudaError_t launch_chained(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kern, P(args)...);
+    note_launch();
+    return e != cudaSuccess ? e : cudaGetLastError();
+}
+#endif
+
 }  // namespace ris

@@ -631,3 +631,56 @@ def test_example_serves_prompts():
         for b, n in enumerate(lens):
             have = layer.cache.pos[b, 0, :int(layer.cache.length[b])].tolist()
             assert len(set(have)) == len(have) and set(range(n + tokens - 32, n + tokens)) <= set(have)
+
+
+def test_serving_calls_after_other_work_in_a_graph():
+    """Each call right behind a memset, a copy, another stream's kernel and another library's, eagerly and as a replayed graph."""
+    B, Hq, Hkv, D, cap = 3, 4, 2, 64, 64
+    x = randn(B, Hq + 2 * Hkv, D, seed=1, dtype=BF16)
+    src = x.clone()
+    lens = torch.tensor([40, 7, 33], dtype=torch.int32, device="cuda")
+    base = filled(B, Hkv, D, cap, lens.tolist())
+    cache, small = filled(B, Hkv, D, cap, lens.tolist()), ris.Cache4.empty(B, Hkv, D, 32)
+    rope = ris.rope_cfg(ris.ROPE_PLAIN, 1e4, 2048)
+    ones, pos = ris.ris_pack_create([1] * B), torch.zeros(1, B, dtype=torch.int32, device="cuda")
+    side, main = torch.cuda.Stream(), torch.cuda.Stream()
+    big = randn(1024, 1024, seed=2)
+
+    def steps():
+        cache.length.zero_()                                   # memset
+        cache.weight.zero_()
+        cache.length.copy_(base.length)                        # copies
+        x.copy_(src)
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):                          # another stream's product, waited for
+            y = big @ big
+            pos.fill_(50)
+        torch.cuda.current_stream().wait_stream(side)
+        q, k = ris.ris_rope_axes(x[:, :Hq], x[:, Hq:Hq + Hkv], pos, [D // 2], 64, rope)
+        ris.ris_cache4_append(cache, ones, k, x[:, Hq + Hkv:], pos[0])
+        o = ris.ris_cache4_attend(cache, q, out_dtype=F32, weight_in=cache.weight, weight_out=cache.weight)
+        z = o * 2.0                                            # another library's kernel
+        pos.zero_()
+        kept = ris.ris_cache4_evict(cache, small, 32, 4)
+        small.weight.mul_(1.0)
+        rk, rv = ris.ris_cache4_read(small)
+        w, = ris.ris_attention_packed(ones, q, k, x[:, Hq + Hkv:])
+        return [q, k, o, z, kept, rk, rv, w, cache.length.clone(), cache.weight.clone(), y]
+
+    want = [t.clone() for t in steps()]
+    torch.cuda.synchronize()
+    ref, _, _ = attend_plain(cache, want[0], (lens + 1).tolist())
+    assert rel_l2(to_np(want[2]), ref.numpy()) <= 1e-5 and torch.equal(want[3], want[2] * 2.0)
+    main.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(main):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=main):
+            got = steps()
+        for _ in range(3):
+            for t in got:
+                t.zero_()
+            graph.replay()
+    torch.cuda.synchronize()
+    ris.ris_device_status()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
