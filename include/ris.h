@@ -503,7 +503,8 @@ ris_status ris_cache4_read(const ris_cache4 *cache, const int32_t *first, int64_
  * weight_out (optional, [batch][kv_heads][capacity]): weight_in + the weights of this token, summed over the query
  * heads of the KV head, for every slot in use (others untouched); weight_in NULL counts as 0 and may be weight_out
  * (the cache's own weight array, to add up in place). fp32 outputs take the query (fp32 inputs) and the weights in two fp16 parts each, bf16
- * outputs the weights in one. Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
+ * outputs the weights in one. Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (weights over more than 4096 query heads of a
+ * KV head, batch x kv_heads past 2^24), RIS_ERR_OOM, RIS_ERR_CUDA. */
 ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t heads, int32_t dtype, int32_t out_dtype,
                              int64_t longest, void *out, float *lse, const float *weight_in, float *weight_out, void *stream);
 

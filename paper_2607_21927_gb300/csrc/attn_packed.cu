@@ -756,6 +756,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned int *const gave_up = &g_ris_packed_error;
     auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     if (warp == kLoadQK) {
         if (lane < L::NBAR) {
@@ -1082,7 +1083,7 @@ struct Pieces {
 // The largest magnitude of each CTA's share of V (as bits without the sign, so that an infinity or NaN wins).
 __global__ void __launch_bounds__(kPrepThreads) k_values_absmax(const PackedArgs a, int row_pieces, float *part)
 {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    after_last();
     const Pieces p(a, row_pieces);
     const int64_t step = (int64_t)gridDim.x * kPrepThreads;
     uint32_t m = 0;
@@ -1179,6 +1180,7 @@ __global__ void __launch_bounds__(kWeightThreads, DT == 64 ? 4 : 2) k_packed_wei
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned int *const gave_up = &g_ris_packed_error;
+    after_last();
     const PackItem it = a.key_items[blockIdx.x];
     const int g = blockIdx.y, shift = it.k_len - it.q_len;
     // rows that count and see the item's first key
@@ -1359,23 +1361,14 @@ constexpr CUtensorMapDataType kBf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, kF16 = C
 
 using TileKernel = void (*)(PackedArgs, PackedMaps);
 
-// Once per kernel: its shared memory, and that its launch has the registers that the softmax threads' setmaxnreg would
-// wait for.
+// Once per kernel: its shared memory, and that its launch has the `regs` registers a thread that the softmax threads'
+// setmaxnreg would wait for.
 cudaError_t prepare(TileKernel kern, int bytes, int regs)
 {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     cudaFuncAttributes fa;
     if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, kern);
     return e != cudaSuccess ? e : (fa.numRegs + 7) / 8 * 8 < regs ? cudaErrorInvalidConfiguration : cudaSuccess;
-}
-
-// A programmatic dependent of the launch before it.
-cudaLaunchAttribute dependent()
-{
-    cudaLaunchAttribute at;
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    return at;
 }
 
 template <typename TOut>
@@ -1390,7 +1383,8 @@ cudaError_t launch_clusters(const PackedArgs &a, const PackedMaps &maps, cudaStr
     cfg.dynamicSmemBytes = Lay128::BYTES;
     cfg.stream = s;
     cudaLaunchAttribute at[2];
-    at[0] = dependent();
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = 2;
     at[1].val.clusterDim.y = 1;
@@ -1409,17 +1403,7 @@ cudaError_t launch_rows(const PackedArgs &a, const PackedMaps &maps, cudaStream_
     static const cudaError_t ready = prepare(k_packed_rows<D, TOut>, L::BYTES, L::REGS);
     if (ready != cudaSuccess) return ready;
     const int64_t units = (int64_t)a.n_items * a.Hq;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min<int64_t>(units, 2 * 152));
-    cfg.blockDim = dim3(L::THREADS);
-    cfg.dynamicSmemBytes = L::BYTES;
-    cfg.stream = s;
-    cudaLaunchAttribute at[1] = {dependent()};
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_packed_rows<D, TOut>, a, maps);
-    note_launch();
-    return e != cudaSuccess ? e : cudaGetLastError();
+    return launch_chained(k_packed_rows<D, TOut>, dim3((unsigned)std::min<int64_t>(units, 2 * 152)), dim3(L::THREADS), L::BYTES, s, a, maps);
 }
 
 }  // namespace
@@ -1439,16 +1423,10 @@ cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool cluster
     const int64_t pieces = a.k_total * row_pieces, blocks = (pieces + 4 * kPrepThreads - 1) / (4 * kPrepThreads);
     if (pieces > 0) {
         const int n_part = (int)(blocks < kPrepBlocks ? blocks : kPrepBlocks);
-        k_values_absmax<<<n_part, kPrepThreads, 0, s>>>(a, row_pieces, part);
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(blocks < 1216 ? blocks : 1216));
-        cfg.blockDim = dim3(kPrepThreads);
-        cfg.stream = s;
-        cudaLaunchAttribute at[1] = {dependent()};
-        cfg.attrs = at;
-        cfg.numAttrs = 1;
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_values_f16, a, row_pieces, (const float *)part, n_part, absmax, v16);
-        note_launch(2);
+        cudaError_t e = launch_chained(k_values_absmax, dim3(n_part), dim3(kPrepThreads), 0, s, a, row_pieces, part);
+        if (e != cudaSuccess) return e;
+        e = launch_chained(k_values_f16, dim3((unsigned)(blocks < 1216 ? blocks : 1216)), dim3(kPrepThreads), 0, s, a, row_pieces, part, n_part,
+                           absmax, v16);
         if (e != cudaSuccess) return e;
     } else {
         const cudaError_t e = cudaMemsetAsync(absmax, 0, sizeof(float), s);
@@ -1481,21 +1459,18 @@ cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
     else
         maps.v = maps.k;
     const dim3 grid((unsigned)a.n_key_items, (unsigned)a.Hkv);
-    cudaError_t e;
     if (D == 128) {
-        e = cudaFuncSetAttribute(k_packed_weights_tc<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, LayW<128>::BYTES);
-        if (e != cudaSuccess) return e;
-        k_packed_weights_tc<128><<<grid, kWeightThreads, LayW<128>::BYTES, s>>>(a, maps);
+        static const cudaError_t ready = prepare(k_packed_weights_tc<128>, LayW<128>::BYTES, 0);
+        if (ready != cudaSuccess) return ready;
+        return launch_chained(k_packed_weights_tc<128>, grid, dim3(kWeightThreads), LayW<128>::BYTES, s, a, maps);
     } else {
         // 52 KB where 49 would do: four CTAs to an SM; five would ask for more TMEM columns than there are
         constexpr int bytes = 52 << 10;
         static_assert(bytes >= LayW<64>::BYTES, "");
-        e = cudaFuncSetAttribute(k_packed_weights_tc<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-        if (e != cudaSuccess) return e;
-        k_packed_weights_tc<64><<<grid, kWeightThreads, bytes, s>>>(a, maps);
+        static const cudaError_t ready = prepare(k_packed_weights_tc<64>, bytes, 0);
+        if (ready != cudaSuccess) return ready;
+        return launch_chained(k_packed_weights_tc<64>, grid, dim3(kWeightThreads), bytes, s, a, maps);
     }
-    note_launch();
-    return cudaGetLastError();
 }
 
 // Read and clear this file's device error word (the caller has synchronised).

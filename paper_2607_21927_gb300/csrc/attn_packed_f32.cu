@@ -87,6 +87,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
     constexpr int LK = D + 4;
     extern __shared__ __align__(16) float sm[];
     float *const qs = sm, *const ks = qs + BM * LK, *const vs = ks + BN * LK, *const ps = vs + BN * D;
+    // (what follows is not let in early: its CTAs, in the places of those that end first, would upset the order by length of a
+    // next call's: 157 us instead of 135)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.x, h = b % a.Hq, part = kParts - 1 - b / a.Hq % kParts;
     const PackItem it = a.items[b / a.Hq / kParts];
     const int r0 = it.row + part * BM, rows = min(BM, it.q_len - r0);
@@ -230,6 +233,7 @@ __global__ void __launch_bounds__(kPackKeys) k_packed_weights(const PackedArgs a
 {
     __shared__ __align__(16) float qs[kWeightRows][D];
     __shared__ float2 st[kWeightRows];
+    after_last();
     const PackItem it = a.key_items[blockIdx.x];
     const int g = blockIdx.y, j = it.row + threadIdx.x, shift = it.k_len - it.q_len;
     const bool there = j < it.k_len;
@@ -273,11 +277,9 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t s)
 {
     auto kern = k_packed_f32<TO, D>;
     constexpr int bytes = ((BM + BN) * (D + 4) + BN * D + BM * LP) * (int)sizeof(float);
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e != cudaSuccess) return e;
-    kern<<<(unsigned)((int64_t)a.n_items * kParts * a.Hq), kThreads, bytes, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (ready != cudaSuccess) return ready;
+    return launch_chained(kern, dim3((unsigned)((int64_t)a.n_items * kParts * a.Hq)), dim3(kThreads), bytes, s, a);
 }
 
 }  // namespace
@@ -291,12 +293,7 @@ cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStr
 cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s)
 {
     const dim3 grid((unsigned)a.n_key_items, (unsigned)a.Hkv);
-    if (D == 128)
-        k_packed_weights<128><<<grid, kPackKeys, 0, s>>>(a);
-    else
-        k_packed_weights<64><<<grid, kPackKeys, 0, s>>>(a);
-    note_launch();
-    return cudaGetLastError();
+    return launch_chained(D == 128 ? k_packed_weights<128> : k_packed_weights<64>, grid, dim3(kPackKeys), 0, s, a);
 }
 
 }  // namespace ris

@@ -508,6 +508,8 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
     if (weight_in != nullptr && weight_out == nullptr) return fail(RIS_ERR_INVALID, "weight_in without weight_out");
     if (longest < 0 || longest > cache->capacity)
         return fail(RIS_ERR_INVALID, "longest %lld outside [0, %lld]", (long long)longest, (long long)cache->capacity);
+    if (weight_out != nullptr && heads / cache->kv_heads > 4096)
+        return fail(RIS_ERR_UNSUPPORTED, "weights over %d query heads of a KV head (4096 at most)", heads / cache->kv_heads);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     Cache4AttendArgs a{};
     a.c = cache_args(cache);

@@ -84,6 +84,8 @@ def test_cache4(ris, mem):
               dict(lse=p + 4), dict(wi=p), dict(wo=p + 4)]:
         a = dict(ok, **c)
         refused(ris, L.ris_cache4_attend(g, a["q"], a["heads"], a["dt"], a["odt"], a["longest"], a["out"], a["lse"], a["wi"], a["wo"], None))
+    one = ctypes.byref(desc(ris, p, kv_heads=1))
+    refused(ris, L.ris_cache4_attend(one, p, 4097, 1, 1, 0, p, None, None, p, None), ris.RIS_ERR_UNSUPPORTED)
     other = desc(ris, p + 16)
     for s, d, budget, recent, kept in ((good, good, 0, 0, p), (good, good, 33, 0, p), (good, good, 8, 8, p), (good, good, 8, -1, p),
                                        (good, good, 8, 0, None), (good, desc(ris, p, capacity=16), 8, 0, p),
