@@ -257,60 +257,43 @@ __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs
     }
 }
 
-// Moves the rows: four lanes to a slot of the target, kRows of them at once. In place only what moves. Bound by HBM: a row's codes,
-// scales, position and weight are read once and written once.
-constexpr int kMoveThreads = 256, kMoveRows = 2;
+// Moves the rows: four lanes to a slot of the target. In place only what moves. Bound by HBM: a row's codes, scales, position and
+// weight are read once and written once, though the pieces of a row that is not next to the last one are parts of 32-byte sectors
+// (256 bytes fetched for 152 at head dim 128). One slot to a thread, so that the launch has threads enough to keep
+// the loads in flight: 51 us an eviction of 16 x 2 lists of 20,000 to 32,768 slots to 8,192, with two slots 53, with four 60.
+constexpr int kMoveThreads = 256, kMoveSlots = kMoveThreads / 4;
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictArgs a, int blocks)
 {
     constexpr int PIECES = D / 32 / 2;  // 16-byte pieces of a row's codes, two lanes for the keys, two for the values
-    const int bh = blockIdx.x / blocks, u = threadIdx.x & 3;
-    const int first = (blockIdx.x - bh * blocks) * (kMoveThreads / 4 * kMoveRows) + threadIdx.x / 4;
+    const int bh = blockIdx.x / blocks, u = threadIdx.x & 3, j = (blockIdx.x - bh * blocks) * kMoveSlots + threadIdx.x / 4;
     // (nothing that the select kernel reads or writes is touched before it has finished)
     after_last();
-    const bool values = u >= 2;
-    const uint4 *sc = reinterpret_cast<const uint4 *>(values ? a.src.v : a.src.k);
-    uint4 *dc = reinterpret_cast<uint4 *>(values ? a.dst.v : a.dst.k);
-    int64_t rs[kMoveRows], rd[kMoveRows];
-    uint4 x[kMoveRows][PIECES];
-    uint32_t y[kMoveRows][D / 64];
-    bool go[kMoveRows];
+    const int from = j < a.budget ? a.kept[(int64_t)bh * a.budget + j] : -1;
+    if (from >= 0 && !(a.in_place && from == j)) {
+        const int64_t rs = bh * a.src.cap + from, rd = bh * a.dst.cap + j;
+        const bool values = u >= 2;
+        const uint4 *sc = reinterpret_cast<const uint4 *>(values ? a.src.v : a.src.k) + rs * (2 * PIECES) + (u & 1) * PIECES;
+        uint4 *dc = reinterpret_cast<uint4 *>(values ? a.dst.v : a.dst.k) + rd * (2 * PIECES) + (u & 1) * PIECES;
+        uint4 x[PIECES];
 #pragma unroll
-    for (int e = 0; e < kMoveRows; ++e) {
-        const int j = first + e * (kMoveThreads / 4);
-        const int from = j < a.budget ? a.kept[(int64_t)bh * a.budget + j] : -1;
-        go[e] = from >= 0 && !(a.in_place && from == j);
-        rs[e] = bh * a.src.cap + max(from, 0);
-        rd[e] = bh * a.dst.cap + j;
-    }
-#pragma unroll
-    for (int e = 0; e < kMoveRows; ++e) {
-        if (!go[e]) continue;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) x[e][p] = sc[rs[e] * (2 * PIECES) + (u & 1) * PIECES + p];
-        // lane 0: position and key scales; 1: weight; 2: value scales
+        for (int p = 0; p < PIECES; ++p) x[p] = sc[p];
+        // lane 0: key scales; 1: weight; 2: value scales; 3: position
         if (u == 0 || u == 2) {
-            const uint32_t *p = reinterpret_cast<const uint32_t *>(values ? a.src.v_scale : a.src.k_scale) + rs[e] * (D / 64);
+            const uint32_t *p = reinterpret_cast<const uint32_t *>(values ? a.src.v_scale : a.src.k_scale) + rs * (D / 64);
+            uint32_t *q = reinterpret_cast<uint32_t *>(values ? a.dst.v_scale : a.dst.k_scale) + rd * (D / 64);
+            uint32_t y[D / 64];
 #pragma unroll
-            for (int g = 0; g < D / 64; ++g) y[e][g] = p[g];
-        } else {
-            y[e][0] = u == 1 ? reinterpret_cast<const uint32_t *>(a.src.weight)[rs[e]] : (uint32_t)a.src.pos[rs[e]];
-        }
-    }
+            for (int g = 0; g < D / 64; ++g) y[g] = p[g];
 #pragma unroll
-    for (int e = 0; e < kMoveRows; ++e) {
-        if (!go[e]) continue;
-#pragma unroll
-        for (int p = 0; p < PIECES; ++p) dc[rd[e] * (2 * PIECES) + (u & 1) * PIECES + p] = x[e][p];
-        if (u == 0 || u == 2) {
-            uint32_t *p = reinterpret_cast<uint32_t *>(values ? a.dst.v_scale : a.dst.k_scale) + rd[e] * (D / 64);
-#pragma unroll
-            for (int g = 0; g < D / 64; ++g) p[g] = y[e][g];
+            for (int g = 0; g < D / 64; ++g) q[g] = y[g];
         } else if (u == 1) {
-            reinterpret_cast<uint32_t *>(a.dst.weight)[rd[e]] = y[e][0];
+            a.dst.weight[rd] = a.src.weight[rs];
         } else {
-            a.dst.pos[rd[e]] = (int32_t)y[e][0];
+            a.dst.pos[rd] = a.src.pos[rs];
         }
+#pragma unroll
+        for (int p = 0; p < PIECES; ++p) dc[p] = x[p];
     }
     if (blockIdx.x == 0)  // (nobody reads the lengths any more)
         for (int b = threadIdx.x; b < a.src.B; b += kMoveThreads)
@@ -346,7 +329,7 @@ cudaError_t launch_select(const Cache4EvictArgs &a, int32_t *holes, int size, si
 template <int D>
 cudaError_t launch_move(const Cache4EvictArgs &a, cudaStream_t s)
 {
-    const int blocks = (a.budget + kMoveThreads / 4 * kMoveRows - 1) / (kMoveThreads / 4 * kMoveRows);
+    const int blocks = (a.budget + kMoveSlots - 1) / kMoveSlots;
     return launch_chained(k_evict_move<D>, dim3((unsigned)((int64_t)blocks * a.src.B * a.src.Hkv)), dim3(kMoveThreads), 0, s, a, blocks);
 }
 

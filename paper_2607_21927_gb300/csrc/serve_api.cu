@@ -562,7 +562,7 @@ ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_
     if (same && src->capacity != dst->capacity) return fail(RIS_ERR_INVALID, "in place, but the capacities differ");
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const int64_t lists = (int64_t)src->batch * src->kv_heads;
-    if (lists > (int64_t(1) << 24) || lists * (budget / 128 + 1) > 2147483647LL)
+    if (lists > (int64_t(1) << 24) || lists * (budget / 64 + 1) > 2147483647LL)
         return fail(RIS_ERR_UNSUPPORTED, "batch x kv_heads = %lld lists of %d slots", (long long)lists, budget);
     Cache4EvictArgs a{};
     a.src = cache_args(src);
