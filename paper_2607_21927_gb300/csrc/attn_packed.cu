@@ -7,10 +7,9 @@
 // are converted by two passes over V ahead of the attention (its largest magnitude, then the values):
 // a few percent of a call at most, as V is read once per 128 rows of it anyway.
 //
-// A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two layouts:
-//   head dim 128  the same for short prompts, k_packed128 for long ones: two CTAs of a cluster share every key and
-//                 value tile
-//   head dim 64   k_packed_rows, persistent, two CTAs to an SM, each with a row tile at a time
+// A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two kernels:
+//   k_packed_rows  head dim 64, and short prompts at head dim 128: persistent, two CTAs to an SM, each with a row tile at a time
+//   k_packed128    long prompts at head dim 128: two CTAs of a cluster share every key and value tile
 //
 // Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls
 // through to the end, TMEM is released and the CTA returns.
@@ -282,7 +281,9 @@ struct Lay128 {
 //                   TMEM only when the maximum grew by more than 2^8, P into TMEM.
 // TMEM: S 2 x 128 columns, O 128, P 2 x 64: all 512.
 //
-// Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles.
+// Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles. One prompt of 32,768 tokens
+// at 12 / 2 heads: 1.96 ms, 1.68 PFLOP/s (cuBLAS 1.89 in a burst and 1.70 under the power limit), the pipe 87 % busy from the
+// first CTA to the last.
 template <typename TOut>
 __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
@@ -736,9 +737,11 @@ struct Units {
 // Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
 // few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and the two CTAs
 // fill each other's; the loaders and issuing warps run on into the next unit while the last one is finished; the outputs
-// leave by TMA. With a CTA (head dim 128: a cluster) per unit, 64 prompts of 256 tokens took 96 us at 12 heads of 128,
-// 111 at 32 heads of 64. At head dim 64 a key tile takes 512 cycles of the tensor pipe and its 16,384 exponentials as
-// long, so it is the softmax that bounds it even over long prompts; at head dim 128 the products of a CTA
+// leave by TMA. 64 prompts of 256 tokens take 40 us at 12 heads of 128, 57 at 32 heads of 64; with a CTA (head dim 128: a
+// cluster) per unit they took 96 and 111. At head dim 64 a key tile takes 512 cycles of the tensor pipe and its 16,384 exponentials as
+// long, so it is the softmax that bounds it even over long prompts: 1,050 cycles a tile and SM over 16,384 tokens (issue slots 57 %,
+// exponentials 49 %, tensor pipe 49 % busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). Two threads to a row,
+// sixteen softmax warps to an SM instead of eight, took 1,170 (a barrier a tile for the row's maximum). At head dim 128 the products of a CTA
 // read as much shared memory as there is bandwidth, and long prompts go to k_packed128.
 //
 //   warp 4  the units, query and key tiles, warp 5 value tiles (TMA);
@@ -1154,7 +1157,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a,
 // KV head of 2^(s_ij - m_i) / l_i, with the maxima and sums that the attention left. One CTA per (128 keys,
 // KV head) holds the keys as the A operand and runs S^T = K Q^T over the group's heads and chunks of 64 rows: a
 // thread owns a key (a TMEM lane), so the sum over rows stays in its register. Bounded by the
-// exponentials, one per pair and head.
+// latency of a few steps per CTA: 17 us for the last 64 rows of 9 prompts, 16,233 keys and 32 / 4 heads of 64, whose exponentials
+// alone take 3.6 (issue slots 34 % busy).
 //
 //   warps 0-3  one thread per key; warp 4 (TMA) the keys, then chunks of rows into a ring; warp 5 the products
 template <int DT>

@@ -85,7 +85,8 @@ __device__ __forceinline__ Pair block_scan(Pair v, Pair &total, Pair *part)
 // by every CTA for itself), then the lists. A slot's order and position are read from memory once and
 // stay in shared memory (CACHED). Ties at the threshold go to the lowest slots: the last histogram says how many of
 // them each CTA holds. holes: [B * Hkv][budget] scratch, the freed slots in order. Bound by latency: seven
-// cluster barriers and about as many block scans.
+// cluster barriers and about as many block scans, 31 us for 16 x 2 lists of 20,000 to 32,768 slots (7 MB). One
+// CTA to a list took 58 us (the atomics on one SM's shared memory).
 template <bool CACHED>
 __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs a, int32_t *holes, int size)
 {
