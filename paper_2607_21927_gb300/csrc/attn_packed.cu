@@ -738,10 +738,12 @@ struct Units {
 // few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and the two CTAs
 // fill each other's; the loaders and issuing warps run on into the next unit while the last one is finished; the outputs
 // leave by TMA. 64 prompts of 256 tokens take 40 us at 12 heads of 128, 57 at 32 heads of 64; with a CTA (head dim 128: a
-// cluster) per unit they took 96 and 111. At head dim 64 a key tile takes 512 cycles of the tensor pipe and its 16,384 exponentials as
-// long, so it is the softmax that bounds it even over long prompts: 1,050 cycles a tile and SM over 16,384 tokens (issue slots 57 %,
-// exponentials 49 %, tensor pipe 49 % busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). Two threads to a row,
-// sixteen softmax warps to an SM instead of eight, took 1,170 (a barrier a tile for the row's maximum). At head dim 128 the products of a CTA
+// cluster) per unit they took 96 and 111. At head dim 64 a key tile's products and its 16,384
+// exponentials each take 512 cycles; it takes 1,050 an SM over 16,384 tokens (issue slots 57 %, exponentials 49 %, tensor pipe 49 %
+// busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). What it waits for is shared memory: a score product reads all of its
+// bandwidth (8 KB of operands in 64 cycles), so the products' issue stalls (570 and 520 cycles from first to done) and a look at a
+// barrier takes 300 cycles. Sixteen softmax warps to an SM instead of eight took 1,170, no maximum ahead of the
+// weights 1,090. At head dim 128 the products of a CTA
 // read as much shared memory as there is bandwidth, and long prompts go to k_packed128.
 //
 //   warp 4  the units, query and key tiles, warp 5 value tiles (TMA);

@@ -684,3 +684,26 @@ def test_serving_calls_after_other_work_in_a_graph():
     ris.ris_device_status()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (3, 1, 128)])
+@pytest.mark.parametrize("step", [0.05, 0.4, 3.0, -0.4])
+@pytest.mark.parametrize("late", [0, 64, 127])
+def test_attention_packed_scores_that_grow_along_the_keys(Hq, Hkv, D, step, late):
+    """Scores that rise (or fall) by `step` a key, so that a row's maximum moves by less than 2^8, by up to 2^15 and by far more in a
+    tile, in its first half or its second; and one key of each tile far above the rest."""
+    lens = [300, 513, 70]
+    n = sum(lens)
+    q, k, v = randn(n, Hq, D, seed=1, dtype=BF16), randn(n, Hkv, D, seed=2, dtype=BF16, scale=0.1), randn(n, Hkv, D, seed=3, dtype=BF16)
+    q[..., 0], q[..., 1] = math.sqrt(D), math.sqrt(D)
+    at = torch.cat([torch.arange(m) for m in lens]).cuda()
+    k[..., 0] = (at * step).to(BF16)[:, None]
+    k[..., 1] = ((at % 128 == late) * (at // 128 + 1) * 12.0).to(BF16)[:, None]
+    with ris.ris_pack_create(lens) as pack:
+        out, lse, w = ris.ris_attention_packed(pack, q, k, v, out_dtype=F32, return_lse=True, weight_rows=40)
+        ris.ris_device_status()
+    ro, rl, rw = packed_plain(q, k, v, lens, lens, 40)
+    check_bf16_path(to_np(out), ro.numpy())
+    assert ((lse.double().cpu() - rl).abs() <= 2e-5 * (1 + rl.abs())).all()
+    # a score of magnitude S is a sum of fp32 additions that cut off, 2^-23 S each, eight of them: 1e-6 S
+    assert (w.double().cpu() - rw).abs().max() <= (2e-5 + 1e-6 * float(rl.abs().max())) * max(1.0, float(rw.max()))
