@@ -740,9 +740,10 @@ struct Units {
 // leave by TMA. 64 prompts of 256 tokens take 40 us at 12 heads of 128, 57 at 32 heads of 64; with a CTA (head dim 128: a
 // cluster) per unit they took 96 and 111. At head dim 64 a key tile's products and its 16,384
 // exponentials each take 512 cycles; it takes 1,050 an SM over 16,384 tokens (issue slots 57 %, exponentials 49 %, tensor pipe 49 %
-// busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). What it waits for is shared memory: a score product reads all of its
-// bandwidth (8 KB of operands in 64 cycles), so the products' issue stalls (570 and 520 cycles from first to done) and a look at a
-// barrier takes 300 cycles. Sixteen softmax warps to an SM instead of eight took 1,170, no maximum ahead of the
+// busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). It is the softmax warps' own chain at two warps
+// to a scheduler, 2,110 cycles a tile: 1,000 for the weights (512 of exponentials, the other warp's in between), 390 for the maximum, 310
+// for the tensor memory's loads and stores with their fences, 350 from the loop's end to the next scores; half the products' work would take
+// 1 % less time, no exponentials 18 %. Sixteen softmax warps to an SM instead of eight took 1,170, no maximum ahead of the
 // weights 1,090. At head dim 128 the products of a CTA
 // read as much shared memory as there is bandwidth, and long prompts go to k_packed128.
 //
