@@ -1382,7 +1382,8 @@ template <typename TOut>
 cudaError_t launch_clusters(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
 {
     static_assert(Lay128::BYTES > 232448 / 2, "one CTA per SM, as it holds all TMEM columns");
-    static const cudaError_t ready = prepare(k_packed128<TOut>, Lay128::BYTES, kRegs);
+    static Once once;
+    const cudaError_t ready = once([] { return prepare(k_packed128<TOut>, Lay128::BYTES, kRegs); });
     if (ready != cudaSuccess) return ready;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((int64_t)a.n_items * ((a.G & 1) == 0 ? a.Hq / 2 : a.Hq) * 2));
@@ -1407,7 +1408,8 @@ template <int D, typename TOut>
 cudaError_t launch_rows(const PackedArgs &a, const PackedMaps &maps, cudaStream_t s)
 {
     using L = LayRows<D>;
-    static const cudaError_t ready = prepare(k_packed_rows<D, TOut>, L::BYTES, L::REGS);
+    static Once once;
+    const cudaError_t ready = once([] { return prepare(k_packed_rows<D, TOut>, L::BYTES, L::REGS); });
     if (ready != cudaSuccess) return ready;
     const int64_t units = (int64_t)a.n_items * a.Hq;
     return launch_chained(k_packed_rows<D, TOut>, dim3((unsigned)std::min<int64_t>(units, 2 * 152)), dim3(L::THREADS), L::BYTES, s, a, maps);
@@ -1467,14 +1469,16 @@ cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
         maps.v = maps.k;
     const dim3 grid((unsigned)a.n_key_items, (unsigned)a.Hkv);
     if (D == 128) {
-        static const cudaError_t ready = prepare(k_packed_weights_tc<128>, LayW<128>::BYTES, 0);
+        static Once once;
+        const cudaError_t ready = once([] { return prepare(k_packed_weights_tc<128>, LayW<128>::BYTES, 0); });
         if (ready != cudaSuccess) return ready;
         return launch_chained(k_packed_weights_tc<128>, grid, dim3(kWeightThreads), LayW<128>::BYTES, s, a, maps);
     } else {
         // 52 KB where 49 would do: four CTAs to an SM; five would ask for more TMEM columns than there are
         constexpr int bytes = 52 << 10;
         static_assert(bytes >= LayW<64>::BYTES, "");
-        static const cudaError_t ready = prepare(k_packed_weights_tc<64>, bytes, 0);
+        static Once once;
+        const cudaError_t ready = once([] { return prepare(k_packed_weights_tc<64>, bytes, 0); });
         if (ready != cudaSuccess) return ready;
         return launch_chained(k_packed_weights_tc<64>, grid, dim3(kWeightThreads), bytes, s, a, maps);
     }

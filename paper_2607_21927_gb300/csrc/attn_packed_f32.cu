@@ -278,7 +278,8 @@ cudaError_t launch(const PackedArgs &a, cudaStream_t s)
 {
     auto kern = k_packed_f32<TO, D>;
     constexpr int bytes = ((BM + BN) * (D + 4) + BN * D + BM * LP) * (int)sizeof(float);
-    static const cudaError_t ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static Once once;
+    const cudaError_t ready = once([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
     return launch_chained(kern, dim3((unsigned)((int64_t)a.n_items * kParts * a.Hq)), dim3(kThreads), bytes, s, a);
 }

@@ -14,7 +14,6 @@
 
 #include <algorithm>
 #include <cstdint>
-#include <mutex>
 #include <type_traits>
 
 #include "attn_common.cuh"
@@ -890,9 +889,8 @@ cudaError_t launch_part(const Cache4AttendArgs &a, cudaStream_t s)
 {
     auto kern = k_cache4_attend<T, SPLIT, D>;
     constexpr int bytes = Lay<D, SPLIT>::BYTES;
-    static std::once_flag once;
-    static cudaError_t ready = cudaSuccess;
-    std::call_once(once, [&] { ready = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    static Once once;
+    const cudaError_t ready = once([&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
     return launch_chained(kern, dim3((unsigned)a.ctas), dim3(kThreads), bytes, s, a);
 }

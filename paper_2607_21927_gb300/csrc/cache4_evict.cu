@@ -304,9 +304,11 @@ __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictAr
 template <bool CACHED>
 cudaError_t launch_select(const Cache4EvictArgs &a, int32_t *holes, int size, size_t bytes, cudaStream_t s)
 {
-    static const cudaError_t ready =
-        CACHED ? cudaFuncSetAttribute(k_evict_select<CACHED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedSlots * (int)sizeof(uint2))
-               : cudaSuccess;
+    static Once once;
+    const cudaError_t ready = once([] {
+        return CACHED ? cudaFuncSetAttribute(k_evict_select<CACHED>, cudaFuncAttributeMaxDynamicSharedMemorySize, kCachedSlots * (int)sizeof(uint2))
+                      : cudaSuccess;
+    });
     if (ready != cudaSuccess) return ready;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(a.src.B * a.src.Hkv * size));
