@@ -707,3 +707,50 @@ def test_attention_packed_scores_that_grow_along_the_keys(Hq, Hkv, D, step, late
     assert ((lse.double().cpu() - rl).abs() <= 2e-5 * (1 + rl.abs())).all()
     # a score of magnitude S is a sum of fp32 additions that cut off, 2^-23 S each, eight of them: 1e-6 S
     assert (w.double().cpu() - rw).abs().max() <= (2e-5 + 1e-6 * float(rl.abs().max())) * max(1.0, float(rw.max()))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_serving_token_strides_past_32_bits(dtype):
+    """Tokens 2^20 elements apart: the last ones lie past 2^32 elements. The same bits as from contiguous copies."""
+    n, Hq, Hkv, D = 4200, 3, 1, 64
+    x = torch.empty(n, 1 << 20, dtype=dtype, device="cuda")
+    heads = x[:, :(Hq + 2 * Hkv) * D].unflatten(1, (-1, D))
+    heads.copy_(randn(n, Hq + 2 * Hkv, D, seed=1, dtype=dtype))
+    q, k, v = heads[:, :Hq], heads[:, Hq:Hq + Hkv], heads[:, Hq + Hkv:]
+    lens = [4000, 0, 200]
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    rope = ris.rope_cfg(ris.ROPE_PLAIN, 1e4, 2048)
+    got = []
+    for a, b, c in ((q, k, v), (q.contiguous(), k.contiguous(), v.contiguous())):
+        cache = ris.Cache4.empty(3, Hkv, D, 4000)
+        with ris.ris_pack_create(lens) as pack:
+            ris.ris_cache4_append(cache, pack, b, c, pos)
+            got.append([*ris.ris_rope_axes(a, b, pos[None], [D // 2], n, rope),
+                        *ris.ris_attention_packed(pack, a, b, c, return_lse=True, weight_rows=16), cache.k, cache.v, cache.k_scale, cache.pos])
+    ris.ris_device_status()
+    for s, t in zip(*got):
+        assert torch.equal(s, t)
+    assert torch.isfinite(got[0][2].float()).all()
+
+
+def test_attention_packed_outputs_past_31_bits():
+    """11,000 prompts of 128 tokens: 2.2 billion output elements. The last prompts by themselves give the same bits."""
+    S, m, Hq, Hkv, D, last = 11000, 128, 12, 2, 128, 3
+    n = S * m
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn(n, h, D, generator=g, device="cuda", dtype=BF16) for h in (Hq, Hkv, Hkv))
+    assert q.numel() > 2 ** 31
+    with ris.ris_pack_create([m] * S) as pack, ris.ris_pack_create([m] * last) as few:
+        out, lse, w = ris.ris_attention_packed(pack, q, k, v, return_lse=True, weight_rows=8)
+        t = n - last * m
+        # (values are scaled by the call's largest magnitude, a power of two: the same bits where both scales are in fp16's normal range)
+        o2, l2, w2 = ris.ris_attention_packed(few, q[t:], k[t:], v[t:], return_lse=True, weight_rows=8)
+        ris.ris_device_status()
+    assert rel_l2(to_np(out[t:]), to_np(o2)) <= 1e-4
+    assert torch.equal(lse[:, t:], l2) and torch.equal(w[:, t:], w2)
+    rows = torch.tensor([0, 127, 128, n // 2, n - 1], device="cuda")
+    for i in rows.tolist():
+        b = i // m * m
+        s = torch.einsum("hd,jd->hj", q[i, :6].double(), k[b:i + 1, 0].double()) / math.sqrt(D)
+        ref = torch.softmax(s, -1) @ v[b:i + 1, 0].double()
+        check_bf16_path(to_np(out[i, :6]), ref.cpu().numpy(), out_bf16=True)
