@@ -140,37 +140,6 @@ Cache4Args cache_args(const ris_cache4 *c)
     return a;
 }
 
-// The rotation frequencies of a configuration as fractions of a turn in 2^-64. A prefill's layers and a
-// generation's steps ask for the same ones again and again (64 powers, 3 us of host time): the calling thread's last ones are
-// kept, by value.
-ris_status rope_turns(const ris_rope_cfg *rope, int64_t n_ctx, int32_t head_dim, const uint64_t **turn, double *mscale)
-{
-    struct Last {
-        ris_rope_cfg cfg{};
-        int64_t n_ctx = -1;
-        int32_t head_dim = 0;
-        double mscale = 1.0;
-        uint64_t turn[kMaxHeadDimHalf] = {};
-    };
-    static thread_local Last last;
-    const ris_rope_cfg &c = last.cfg;
-    if (last.n_ctx != n_ctx || last.head_dim != head_dim || c.kind != rope->kind || c.reserved != rope->reserved ||
-        c.theta != rope->theta || c.native_len != rope->native_len || c.factor != rope->factor || c.yarn_alpha != rope->yarn_alpha ||
-        c.yarn_beta != rope->yarn_beta) {
-        double f[kMaxHeadDimHalf], ms = 1.0;
-        last.n_ctx = -1;
-        RIS_TRY(ris_rope_freqs(rope, n_ctx, head_dim, f, &ms));
-        for (int i = 0; i < head_dim / 2; ++i) last.turn[i] = (uint64_t)(f[i] * (18446744073709551616.0 / 6.283185307179586476925286766559));
-        last.cfg = *rope;
-        last.head_dim = head_dim;
-        last.mscale = ms;
-        last.n_ctx = n_ctx;
-    }
-    *turn = last.turn;
-    *mscale = last.mscale;
-    return RIS_OK;
-}
-
 double log2e_over_sqrt(int32_t head_dim) { return 1.4426950408889634074 / std::sqrt((double)head_dim); }
 
 // Keys that the last of an item's `step` rows sees.
@@ -335,9 +304,8 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
         return fail(RIS_ERR_INVALID, "the sections hold %lld frequencies, not head_dim / 2 = %d", (long long)sum, head_dim / 2);
     if (rope == nullptr || rope->kind == RIS_ROPE_NONE) return fail(RIS_ERR_INVALID, "rope is NULL or of kind NONE");
     RopeAxesArgs a{};
-    const uint64_t *turn = nullptr;
-    double ms = 1.0;
-    RIS_TRY(rope_turns(rope, n_ctx, head_dim, &turn, &ms));
+    double f[kMaxHeadDimHalf], ms = 1.0;
+    RIS_TRY(ris_rope_freqs(rope, n_ctx, head_dim, f, &ms));
     if (n > 0) {
         RIS_TRY(check_ptr(q, "q"));
         RIS_TRY(check_ptr(q_out, "q_out"));
@@ -353,7 +321,8 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
             return fail(RIS_ERR_INVALID, "in place only where the heads of a token follow the last one's");
     }
     if (n == 0) return RIS_OK;
-    std::copy(turn, turn + head_dim / 2, a.turn);
+    for (int c = 0; c < head_dim / 2; ++c)  // as fractions of a turn in 2^-64
+        a.turn[c] = (uint64_t)(f[c] * (18446744073709551616.0 / 6.283185307179586476925286766559));
     if (interleaved) {
         // frequency c goes to axis c mod axes while that axis has any left, else to the first axis
         for (int c = 0; c < head_dim / 2; ++c) {
