@@ -257,7 +257,8 @@ __global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kTile = 16;                      // slots of a warp's product
 constexpr int kUnit = kCacheUnit;              // slots by which the work is shared out
-constexpr int kMinExp = -100;                  // smallest exponent of a value scale that counts as such: sums stay finite
+constexpr float kMostFactor = 0x1p118f;        // largest factor of a weight times value scale (a weight is 2^8 at most)
+constexpr float kMostHalf = 0x1p15f;           // what weight, scale and factor may come to as fp16
 
 template <int D, bool SPLIT>
 struct Lay {
@@ -329,6 +330,20 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// two fp32 values in one register pair, and their product by halves
+__device__ __forceinline__ uint64_t f2_pack(float x, float y)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
+    return d;
+}
+__device__ __forceinline__ void f2_unpack(uint64_t v, float &x, float &y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(v)); }
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ uint32_t pack_half(float x, float y)
 {
     const __half2 h = __floats2half2_rn(x, y);
@@ -383,14 +398,17 @@ __device__ __forceinline__ int64_t mul_div(int64_t x, int y, int z)
 //   O^T += V^T P^T  the weights times the slot's scale, per group of 32, as fp16, transposed by
 //                movmatrix; with SPLIT a second fp16 of what the first leaves, for fp32 outputs; values as
 //                fp16 pairs of slots, paired as codes (half the instructions of pairing them as fp16).
-// The weights are 2^(s - m + 4 - ev), ev the exponent of the largest value scale so far and m a reference that
-// moves only when a score exceeds it by more than 2^8: weight times scale stays below 2^13, and what a
-// weight of 2^-18 of the reference's or more loses to fp16 is its 11 bits' rounding. Sums and O carry the same factor, which cancels.
+// The weights are p = 2^(s - m), m a whole number that moves only when a score exceeds it by more than 2^8; the row's sum is
+// that of p alone, whatever the values hold. fp16 gets u = f p scale with a factor f, a power of two, per query head and group
+// of 32 channels: it comes down when a u would pass 2^15, to where the largest of the stage is 16, and goes up with m, so
+// what a slot adds keeps fp16's 11 bits down to 2^-18 of the largest that any slot so far has added to that head and group,
+// and no group, slot or scale that is not finite takes bits from another group. O carries its group's f.
 // Slots past the length enter with score -infinity and scale 0, whatever lies there.
 // A list takes 8 query heads of its KV head, a product's columns.
-// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 49.8 us a call with the join, 5.2 of the 6.8 TB/s that a
-// copy reaches; unpacking keeps the ALU pipe 59 % and the issue slots half busy, so three CTAs' loads and
-// arithmetic do not overlap all the way. Smaller calls are latency: 24 sequences of 700 to 9,216 slots 12.5 us before the join, of which the
+// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 53.8 us a call with the join, 4.8 of the 6.8 TB/s that a
+// copy reaches (one exponent for all groups and heads, which a scale that is not finite or one large slot spoils, took 49.7; fp32
+// outputs 82 and 73); unpacking keeps the ALU pipe and the issue slots half busy, so three CTAs' loads and arithmetic do not
+// overlap all the way. Smaller calls are latency: 24 sequences of 700 to 9,216 slots 12.5 us before the join, of which the
 // copies' first arrival and a warp's two stages are most.
 constexpr float kLazyLog2 = 8.f;
 
@@ -511,19 +529,20 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             unscale[0] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4);
             unscale[1] = __shfl_sync(0xFFFFFFFFu, up, 8 * t4 + 4);
         }
-        float m[2], l[2], o[NM][4];
+        float m[2], l[2], fac[2][NG], o[NM][4];  // (index 0, 1: heads 2 t4, 2 t4 + 1)
         {
             m[0] = m[1] = -INFINITY;
             l[0] = l[1] = 0.f;
 #pragma unroll
+            for (int g = 0; g < NG; ++g) fac[0][g] = fac[1][g] = kMostFactor;
+#pragma unroll
             for (int e = 0; e < NM; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
         }
-        int ev = kMinExp;  // exponent of the largest value scale so far
         // a stage of ns slots at s0; FULL: ns == kStageSlots
         auto stage = [&](auto full_c, const unsigned char *sm, int s0, int ns) {
             constexpr bool FULL = decltype(full_c)::value;
-            // the value scales of this lane's slots, and the largest of the stage
-            uint32_t vsc[kWarpTiles][2][NG / 2], top = 0;
+            // the value scales of this lane's slots, two groups to a word, and the largest
+            uint32_t vsc[kWarpTiles][2][NG / 2], top[NG / 2] = {};
 #pragma unroll
             for (int i = 0; i < kWarpTiles; ++i)
 #pragma unroll
@@ -533,11 +552,9 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
 #pragma unroll
                     for (int g = 0; g < NG / 2; ++g) {
                         vsc[i][r][g] = FULL || slot < ns ? p[g] : 0u;
-                        top = __vmaxu2(top, vsc[i][r][g]);
+                        top[g] = __vmaxu2(top[g], vsc[i][r][g]);
                     }
                 }
-            top = __reduce_max_sync(0xFFFFFFFFu, max(top & 0xFFFFu, top >> 16));
-            const int e_new = max(ev, min((int)(top >> 7) - 127, 127));
             {
                 float s[kWarpTiles][4];
 #pragma unroll
@@ -597,38 +614,72 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                     }
                 }
                 float x[2];
-                bool moves = e_new != ev;
+                bool moves = false;
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     x[e] = fmaxf(s[0][e], s[0][e + 2]);
 #pragma unroll
                     for (int i = 1; i < kWarpTiles; ++i) x[e] = fmaxf(x[e], fmaxf(s[i][e], s[i][e + 2]));
                     x[e] *= unscale[e];
-                    moves = moves || x[e] > m[e] + kLazyLog2;
+                    // no u of this lane is larger than its largest weight times its largest scales, all groups' together (NaN: not
+                    // known to be small)
+                    float most = 0.f;
+#pragma unroll
+                    for (int g = 0; g < NG; ++g) most = fmaf(fac[e][g], bf16_at(top[g / 2], g), most);
+                    moves = moves || x[e] > m[e] + kLazyLog2 || !(ex2(x[e] - m[e]) * most <= kMostHalf);
                 }
                 if (__any_sync(0xFFFFFFFFu, moves)) {  // (in the first stages of a list, mostly)
-                    const float ov = e_new - ev > 126 ? 0.f : pow2i(ev - e_new);
-                    float al[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
                         for (int w = 4; w < 32; w <<= 1) x[e] = fmaxf(x[e], __shfl_xor_sync(0xFFFFFFFFu, x[e], w));
-                        const float nm = x[e] > m[e] + kLazyLog2 ? x[e] : m[e];
-                        al[e] = m[e] == -INFINITY ? 0.f : ex2(m[e] - nm) * ov;
-                        m[e] = nm;
-                        l[e] *= al[e];
+                        const bool begun = m[e] != -INFINITY;  // (else O and l are 0, or NaN)
+                        float up = 1.f;
+                        if (x[e] > m[e] + kLazyLog2) {
+                            const float nm = ceilf(x[e]);
+                            if (begun) {
+                                up = ex2(nm - m[e]);
+                                l[e] *= ex2(m[e] - nm);
+                            }
+                            m[e] = nm;
+                        }
+                        const float ref = m[e] == -INFINITY ? 0.f : m[e];
+                        float most[NG] = {};  // largest weight times scale, times 2^-8
+#pragma unroll
+                        for (int i = 0; i < kWarpTiles; ++i)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                const float p = ex2(fmaf(s[i][e + 2 * r], unscale[e], -ref)) * 0x1p-8f;
+#pragma unroll
+                                for (int g = 0; g < NG; ++g) {
+                                    const float u = p * bf16_at(vsc[i][r][g / 2], g);
+                                    if (u < INFINITY) most[g] = fmaxf(most[g], u);
+                                }
+                            }
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+#pragma unroll
+                            for (int w = 4; w < 32; w <<= 1) most[g] = fmaxf(most[g], __shfl_xor_sync(0xFFFFFFFFu, most[g], w));
+                            // O stays as it is where f goes up as the weights come down
+                            const float had = fac[e][g] * up;
+                            fac[e][g] = fminf(had, kMostFactor);
+                            if (most[g] * fac[e][g] > kMostHalf * 0x1p-8f)
+                                fac[e][g] = __uint_as_float((uint32_t)max(1, 127 - 4 - ((int)(__float_as_uint(most[g]) >> 23) - 127)) << 23);
+                            if (begun && fac[e][g] != had) {
+                                const float by = fac[e][g] / had;
+#pragma unroll
+                                for (int t = 2 * g; t < 2 * g + 2; ++t) {
+                                    o[t][e] *= by;
+                                    o[t][e + 2] *= by;
+                                }
+                            }
+                        }
                     }
-#pragma unroll
-                    for (int e = 0; e < NM; ++e)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) o[e][c] *= al[c & 1];
                 }
                 // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor pipe's
                 // additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
                 [[maybe_unused]] float part[SPLIT ? NM : 1][4];
-                float to[2];  // exponent of a weight: s unscale + to
-#pragma unroll
-                for (int e = 0; e < 2; ++e) to[e] = (float)(4 - e_new) - (m[e] == -INFINITY ? 0.f : m[e]);
+                const float to[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};  // exponent of a weight: s unscale + to
 #pragma unroll
                 for (int i = 0; i < kWarpTiles; ++i) {
                     if (!FULL && i * kTile >= ns) continue;
@@ -640,11 +691,12 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                     }
                     [[maybe_unused]] uint32_t bh[NG][2], bl[SPLIT ? NG : 1][2];
 #pragma unroll
-                    for (int g = 0; g < NG; ++g)
+                    for (int r = 0; r < 2; ++r)
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
+                        for (int g = 0; g < NG; ++g) {
                             const float sc = bf16_at(vsc[i][r][g / 2], g);
-                            const float u = p[2 * r] * sc, v = p[2 * r + 1] * sc;
+                            float u, v;
+                            f2_unpack(f2_mul(f2_mul(f2_pack(p[2 * r], p[2 * r + 1]), f2_pack(fac[0][g], fac[1][g])), f2_pack(sc, sc)), u, v);
                             const uint32_t hi = pack_half(u, v);
                             if constexpr (SPLIT) bl[g][r] = transpose8(pack_rest(u, v, hi));
                             bh[g][r] = transpose8(hi);
@@ -692,7 +744,6 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                         for (int c = 0; c < 4; ++c) o[e][c] += part[e][c];
                 }
             }
-            ev = e_new;
         };
         for (int s0 = warp * per; s0 < n; s0 += s_step) {
             ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(bars + 8 * used, phase));
@@ -717,17 +768,18 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
         float *const so = reinterpret_cast<float *>(smem);
         float2 *const sml = reinterpret_cast<float2 *>(so + kWarps * 8 * LO_);
         float *const sf = reinterpret_cast<float *>(sml + kWarps * 8);
-        const float back = pow2i(ev - 4);
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            float x = l[e] * back;
+            float x = l[e];
 #pragma unroll
             for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, w);
             const int h = 2 * t4 + e;
+            const float inv = x == 0.f ? 0.f : 1.f / x;  // (averages: sums of the largest values would pass fp32's range)
             if (g8 == 0) sml[warp * 8 + h] = make_float2(m[e], x);
 #pragma unroll
             for (int tl = 0; tl < NM; ++tl)
-                *reinterpret_cast<float2 *>(so + (warp * 8 + h) * LO_ + 16 * tl + 2 * g8) = make_float2(o[tl][e] * back, o[tl][e + 2] * back);
+                *reinterpret_cast<float2 *>(so + (warp * 8 + h) * LO_ + 16 * tl + 2 * g8) =
+                    make_float2(o[tl][e] * inv * (1.f / fac[e][tl / 2]), o[tl][e + 2] * inv * (1.f / fac[e][tl / 2]));
         }
         __syncthreads();
         // one partial per head of the block: number cta + list
@@ -736,11 +788,10 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             const float2 ml = sml[lane];
             float M = fmaxf(ml.x, __shfl_xor_sync(0xFFFFFFFFu, ml.x, 8));
             M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, 16));
-            const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - M);
-            float sum = ml.y * f;
-            sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 8);
+            const float part_sum = ml.y * (ml.x == -INFINITY ? 0.f : exp2f(ml.x - M));
+            float sum = part_sum + __shfl_xor_sync(0xFFFFFFFFu, part_sum, 8);
             sum += __shfl_xor_sync(0xFFFFFFFFu, sum, 16);
-            sf[lane] = f;
+            sf[lane] = sum == 0.f ? 0.f : part_sum / sum;  // the warp's share of the average
             if (lane < nh) a.part_ml[part + lane] = make_float2(M, sum);
         }
         __syncthreads();
@@ -775,7 +826,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
 {
     constexpr int C = D / 32, block_heads = 8;
     __shared__ float so[kJoinWarps][D];
-    __shared__ float2 sml[kJoinWarps];
     extern __shared__ float2 stat[];  // [G], weights
     const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_seq = a.lists / a.c.B;
@@ -791,47 +841,65 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         i0 = len > 0 ? x.x : 0;
         i1 = len > 0 ? x.y : -1;
     };
+    // the maximum and sum of the parts together, a lane per part
+    auto whole = [&](int64_t p0, int i0, int i1) -> float2 {
+        float M = -INFINITY, sum = 0.f;
+        for (int i = i0 + lane; i <= i1; i += 32) {
+            const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
+            const float nm = fmaxf(M, ml.x);
+            sum = nm == -INFINITY ? sum + ml.y : sum * exp2f(M - nm) + ml.y * exp2f(ml.x - nm);
+            M = nm;
+        }
+        const float tm = warp_max(M);
+        return make_float2(tm, warp_sum(tm == -INFINITY ? sum : sum * exp2f(M - tm)));
+    };
     if ((int)blockIdx.x < a.Hq) {
         const int h = blockIdx.x, kvh = h / a.G, hb = (h % a.G) / block_heads, y = hb * a.c.Hkv + kvh;
         int i0, i1;
         parts(y, i0, i1);
         const int64_t p0 = ((int64_t)b * per_seq + y) * block_heads + h % a.G % block_heads;
-        float M = -INFINITY, sum = 0.f, x[C] = {};
-        for (int i = i0 + warp; i <= i1; i += kJoinWarps) {
+        // (each warp's first three parts are on their way while the sums are joined)
+        constexpr int AHEAD = 3;
+        float2 at[AHEAD];
+        float v[AHEAD][C];
+        auto fetch = [&](int i, float2 &ml, float(&o)[C]) {
             const int64_t p = p0 + (int64_t)i * block_heads;
-            const float2 ml = a.part_ml[p];
-            float v[C];
+            ml = a.part_ml[p];
 #pragma unroll
-            for (int c = 0; c < C; ++c) v[c] = a.part_o[p * D + lane + 32 * c];
-            const float nm = fmaxf(M, ml.x);
-            const float f0 = M == -INFINITY ? 0.f : exp2f(M - nm), f1 = ml.x == -INFINITY ? 0.f : exp2f(ml.x - nm);
-            M = nm;
-            sum = fmaf(sum, f0, ml.y * f1);
+            for (int c = 0; c < C; ++c) o[c] = a.part_o[p * D + lane + 32 * c];
+        };
 #pragma unroll
-            for (int c = 0; c < C; ++c) x[c] = fmaf(x[c], f0, v[c] * f1);
+        for (int n = 0; n < AHEAD; ++n)
+            if (i0 + warp + kJoinWarps * n <= i1) fetch(i0 + warp + kJoinWarps * n, at[n], v[n]);
+        const float2 ml = whole(p0, i0, i1);
+        const float inv = 1.f / ml.y;
+        float x[C] = {};
+        auto add = [&](const float2 &part, const float(&o)[C]) {
+            const float share = part.y * (part.x == -INFINITY ? 0.f : exp2f(part.x - ml.x)) * inv;
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[c] = fmaf(o[c], share, x[c]);
+        };
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n)
+            if (i0 + warp + kJoinWarps * n <= i1) add(at[n], v[n]);
+        for (int i = i0 + warp + kJoinWarps * AHEAD; i <= i1; i += kJoinWarps) {
+            fetch(i, at[0], v[0]);
+            add(at[0], v[0]);
         }
-        if (lane == 0) sml[warp] = make_float2(M, sum);
 #pragma unroll
         for (int c = 0; c < C; ++c) so[warp][lane + 32 * c] = x[c];
         __syncthreads();
         const int64_t row = (int64_t)b * a.Hq + h;
         const int d = threadIdx.x;
         if (d < D) {
-            float tm = -INFINITY, ts = 0.f, to = 0.f;
+            float to = 0.f;  // (no slot: zeros)
 #pragma unroll
-            for (int w = 0; w < kJoinWarps; ++w) tm = fmaxf(tm, sml[w].x);
-#pragma unroll
-            for (int w = 0; w < kJoinWarps; ++w) {
-                const float f = sml[w].x == -INFINITY ? 0.f : exp2f(sml[w].x - tm);
-                ts = fmaf(sml[w].y, f, ts);
-                to = fmaf(so[w][d], f, to);
-            }
-            to = ts == 0.f ? 0.f : to / ts;  // no slot: zeros
+            for (int w = 0; w < kJoinWarps; ++w) to += so[w][d];
             if constexpr (sizeof(TO) == 4)
                 reinterpret_cast<float *>(a.out)[row * D + d] = to;
             else
                 reinterpret_cast<__nv_bfloat16 *>(a.out)[row * D + d] = __float2bfloat16_rn(to);
-            if (d == 0 && a.lse != nullptr) a.lse[row] = (tm + log2f(ts)) * kLn2;
+            if (d == 0 && a.lse != nullptr) a.lse[row] = (ml.x + log2f(ml.y)) * kLn2;
         }
         return;
     }
@@ -852,16 +920,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         int i0, i1;
         parts(yl, i0, i1);
         const int64_t p0 = ((int64_t)b * per_seq + yl) * block_heads + h % block_heads;
-        float M = -INFINITY, sum = 0.f;
-        for (int i = i0 + lane; i <= i1; i += 32) {
-            const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
-            const float nm = fmaxf(M, ml.x);
-            sum = nm == -INFINITY ? sum : sum * exp2f(M - nm) + ml.y * exp2f(ml.x - nm);
-            M = nm;
-        }
-        const float tm = warp_max(M);
-        sum = warp_sum(M == -INFINITY ? 0.f : sum * exp2f(M - tm));
-        if (lane == 0) stat[h] = make_float2(tm, 1.f / sum);
+        const float2 ml = whole(p0, i0, i1);
+        if (lane == 0) stat[h] = make_float2(ml.x, 1.f / ml.y);
     }
     __syncthreads();
     for (int h0 = 0; h0 < a.G; h0 += 8) {
