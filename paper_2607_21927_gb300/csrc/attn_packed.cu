@@ -2,10 +2,11 @@
 //
 // S = Q K^T with bf16 operands (exact products, fp32 sums), one online softmax per row over the keys j <= i +
 // k_len - q_len of its own sequence, O = P V with P as fp16 (11 bits; a bf16 P would add as much error
-// again as the bf16 output's own rounding) against the values as fp16 scaled by a power of two (a
-// bf16 value is exact there), the row's sum from the fp32 weights before they are rounded. The values
-// are converted by two passes over V ahead of the attention (its largest magnitude, then the values):
-// a few percent of a call at most, as V is read once per 128 rows of it anyway.
+// again as the bf16 output's own rounding) against the values as fp16 scaled by a power of two of their
+// sequence and KV head (a bf16 value is exact there down to 2^-30 of the largest), the row's sum from the fp32 weights before they
+// are rounded. The values are converted by two passes over V ahead of the attention (bounds, then the values): a few
+// percent of a call where there are as many rows as keys, as V is read once per 128 rows of it anyway; most of one of
+// few rows behind many keys.
 //
 // A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two kernels:
 //   k_packed_rows  head dim 64, and short prompts at head dim 128: persistent, two CTAs to an SM, each with a row tile at a time
@@ -14,8 +15,9 @@
 // Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls
 // through to the end, TMEM is released and the CTA returns.
 //
-// Values that are not finite take a slow path (0 times an infinity is not 0, and a product over a tile
-// multiplies keys that a row does not see by 0): one warp per row over exactly the keys it sees.
+// Where a sequence's values of a KV head are not all finite (0 times an infinity is not 0, and a product over a tile multiplies
+// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the values as given: one warp per row
+// over exactly the keys it sees.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -129,7 +131,8 @@ __device__ __forceinline__ void store_row(const PackedArgs &a, int h, int64_t ro
     if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l);
 }
 
-// The slow path: rows row .. row + BM - 1 of the item, warp `warp` of `warps` taking every warps-th, over the keys that each sees.
+// Rows from the values as given: rows row .. row + BM - 1 of the item, warp `warp` of `warps` taking every warps-th, over the
+// keys that each sees. Outputs only: a row's maximum and sum do not depend on the values.
 template <int DT, typename TOut>
 __device__ __noinline__ void rows_one_by_one(const PackedArgs &a, const PackItem &it, int row, int h, int warp, int warps)
 {
@@ -171,7 +174,6 @@ __device__ __noinline__ void rows_one_by_one(const PackedArgs &a, const PackItem
             else
                 out[lane + 32 * c] = __float2bfloat16_rn(x);
         }
-        if (lane == 0) store_row(a, h, r, m, l);
     }
 }
 
@@ -507,7 +509,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
         const int r = wq * 32 + lane;  // TMEM lane
         const uint32_t lane_off = (uint32_t)(wq * 32) << 16;
         values_ready();
-        const float sc = a.scale_log2, v_absmax = *a.v_absmax;
+        const float sc = a.scale_log2, v_top = it.k_len > 0 ? a.v_top[(int64_t)it.seq * a.Hkv + g] : 0.f;
         // the group's score buffer is free for its first tile
         if (lane == 0 && grp < n_kt) arrive_lead(L::B_S_GO + grp);
         const int last_key = q0 + r + shift;          // last key that the row sees
@@ -619,16 +621,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
             const float m_fin = n_kt == 0 ? -INFINITY : ((n_kt - 1) & 1) ? mb.x : ma.x;
             const float lt = (ma.x == m_fin ? ma.y : ma.y * exp2f(ma.x - m_fin)) +
                              (mb.x == m_fin ? mb.y : mb.y * exp2f(mb.x - m_fin));
+            if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin, lt);
             // fp16 values were scaled by 2^-E for the value product
-            if (v_absmax < INFINITY) {
-                const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / lt;
+            if (v_top < INFINITY) {
+                const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_top)) / lt;
                 const int w0 = q0 + 32 * wq;  // the warp's first row
                 TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT + OC * grp;
                 unsigned char *stage = smem + warp * (32 * OC * (int)sizeof(TOut));
                 stage_out<OC, TOut>(stage, T_O + lane_off + OC * grp, inv);
                 __syncwarp();
                 rows_out<OC, TOut>(stage, out, (int64_t)a.Hq * DT, it.q_len - w0);
-                if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin, lt);
             } else {
                 rows_one_by_one<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps);
             }
@@ -712,6 +714,7 @@ struct UnitInfo {
     int n;                  // key tiles, -1: no more units
     int h, row, shift;      // head; first row; key j is seen by row i when j <= i + shift
     int q_base, q_len, k_base, k_len;
+    int64_t top;            // its place in v_top
 };
 static_assert(sizeof(UnitInfo) <= 64, "the ring's slots");
 
@@ -733,6 +736,17 @@ struct Units {
         }
     }
 };
+
+// The units of this CTA whose rows are to be computed from the values as given.
+template <int D, typename TOut>
+__device__ __noinline__ void units_as_given(const PackedArgs &a, int warp)
+{
+    Units units{(int64_t)a.n_items * a.Hq, -1};
+    PackItem it;
+    int h;
+    while (units.next(a, it, h))
+        if (it.k_len > 0 && !(a.v_top[(int64_t)it.seq * a.Hkv + h / a.G] < INFINITY)) rows_one_by_one<D, TOut>(a, it, it.row, h, warp, kGroupWarps);
+}
 
 // Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
 // few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and the two CTAs
@@ -810,7 +824,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
                     if (more) {
                         const int shift = it.k_len - it.q_len;
                         n = (max(0, min(it.k_len, min(it.q_len, it.row + BM) + shift)) + BN - 1) / BN;  // tiles that the rows see
-                        x = UnitInfo{n, h, it.row, shift, it.q_base, it.q_len, it.k_base, it.k_len};
+                        x = UnitInfo{n, h, it.row, shift, it.q_base, it.q_len, it.k_base, it.k_len, (int64_t)it.seq * a.Hkv + h / a.G};
                     } else {
                         x.n = -1;
                     }
@@ -937,13 +951,15 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
         bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
         if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
         values_ready();
-        const float v_absmax = *a.v_absmax;
+        bool left = false;  // units whose rows are to be computed from the values as given
         for (int u = 0; ok; ++u) {
             UnitInfo x;
             ok = __all_sync(0xFFFFFFFFu, unit(u, x));
             if (!ok || x.n < 0) break;
             __syncwarp();
             unit_read(u, lane == 0);
+            float v_top;  // (on its way from here on: it is asked for at the unit's end; undefined without keys)
+            asm volatile("ld.global.f32 %0, [%1];" : "=f"(v_top) : "l"(a.v_top + x.top));
             const int last_key = x.row + r + x.shift, warp_sees = x.row + warp * 32 + x.shift;
             float l = 0.f, m = -INFINITY;
             for (int j = 0; j < x.n; ++j, ++t) {
@@ -1013,16 +1029,16 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
             }
             if (ok && x.n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
             if (!ok) break;
-            if (!(v_absmax < INFINITY)) {  // (by all four warps, wherever the rows end)
-                PackItem it{};
-                it.q_base = x.q_base, it.q_len = x.q_len, it.k_base = x.k_base, it.k_len = x.q_len + x.shift;
-                rows_one_by_one<D, TOut>(a, it, x.row, x.h, warp, kGroupWarps);
+            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m, l);
+            if (x.n > 0 && !(v_top < INFINITY)) {
+                left = true;
+                tc_fence_before();
                 continue;
             }
             const int w0 = x.row + 32 * warp, rows = x.q_len - w0;  // the warp's first row, and how many it has (or more than 32)
             if (rows <= 0) continue;
             TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(x.q_base + w0) * a.Hq + x.h) * D;
-            const float inv = l == 0.f ? 0.f : pow2i(value_exp(v_absmax)) / l;
+            const float inv = l == 0.f ? 0.f : pow2i(value_exp(v_top)) / l;
             constexpr int OC = 128 / (int)sizeof(TOut);  // columns that pass through the warp's 4 KB at a time
 #pragma unroll
             for (int c0 = 0; c0 < D; c0 += OC) {
@@ -1049,9 +1065,10 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
                     rows_out<OC, TOut>(stage, out + c0, (int64_t)a.Hq * D, rows);
                 }
             }
-            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m, l);
             tc_fence_before();  // (O has been read before the next P is announced)
         }
+        // (after everything else: they take far longer than a wait of another role may)
+        if (ok && left) units_as_given<D, TOut>(a, warp);
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) atomicOr(&g_ris_packed_error, 2u);
@@ -1063,95 +1080,119 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
 }
 
 // ---------------------------------------------------------------- values as fp16
-// 16-byte pieces of V by number, row_pieces to a row. (32-bit division: a 64-bit one takes longer than the load.)
-constexpr int kPrepThreads = 256, kPrepBlocks = 304;
-struct Pieces {
+// Two passes over V ahead of the attention, a CTA per (run of a sequence's keys, KV head). A row sees keys of its own
+// sequence and KV head only, so the scale is theirs: nothing that another prompt or head holds takes bits from these.
+// Within them fp16 holds a key's values to 2^-12 of its own largest (what P's rounding costs) where the keys' largest
+// values lie within 2^26 of one another. Where they do not (a key that most rows do not see may be that large), or are not
+// finite, the rows are computed from the values as given.
+constexpr int kPrepThreads = 256, kPrepWarps = kPrepThreads / 32, kMostSpan = 26;
+// the pieces (16 bytes) of one head of a run's keys: this thread's piece of every kRows-th key from its first one
+template <int D>
+struct HeadPieces {
+    static constexpr int P = D / 8, kRows = kPrepThreads / P, kAhead = kPackKeys / kRows;  // (a short run's pieces at once)
     const __nv_bfloat16 *v;
-    int64_t stride, n;
-    uint32_t row_pieces;
-    bool wide;
-    __device__ __forceinline__ Pieces(const PackedArgs &a, int row_pieces_)
-        : v(reinterpret_cast<const __nv_bfloat16 *>(a.v)), stride(a.v_stride), n(a.k_total * row_pieces_), row_pieces(row_pieces_),
-          wide(n > 0xFFFFFFFFLL)
+    int64_t stride;
+    int n, row;
+    __device__ __forceinline__ HeadPieces(const PackedArgs &a, const PackRun &run, int head)
+        : stride(a.v_stride), n(run.n), row(threadIdx.x / P)
     {
-        if (stride == (int64_t)row_pieces * 8) row_pieces = 0;  // rows without gaps: one long one
+        v = reinterpret_cast<const __nv_bfloat16 *>(a.v) + (int64_t)run.first * stride + head * D + (threadIdx.x % P) * 8;
     }
-    __device__ __forceinline__ uint4 load(int64_t t) const
+    __device__ __forceinline__ uint4 load(int i) const
     {
-        int64_t at = t * 8;
-        if (row_pieces != 0) {
-            const int64_t r = wide ? t / row_pieces : (int64_t)((uint32_t)t / row_pieces);
-            at = r * stride + (t - r * row_pieces) * 8;
-        }
-        return *reinterpret_cast<const uint4 *>(v + at);
+        return i + row < n ? *reinterpret_cast<const uint4 *>(v + (int64_t)(i + row) * stride) : make_uint4(0u, 0u, 0u, 0u);
     }
 };
-// The largest magnitude of each CTA's share of V (as bits without the sign, so that an infinity or NaN wins).
-__global__ void __launch_bounds__(kPrepThreads) k_values_absmax(const PackedArgs a, int row_pieces, float *part)
+// part[head][run] = the largest magnitude of the run's values (upper half, bf16 without the sign, so that an infinity or NaN wins)
+// and the smallest of its keys' largest ones that is not zero (lower half, 0xFFFF: every key is zero)
+template <int D>
+__global__ void __launch_bounds__(kPrepThreads) k_values_bounds(const PackedArgs a, uint32_t *part)
 {
+    using V = HeadPieces<D>;
+    const V p(a, a.runs[blockIdx.x], blockIdx.y);
     after_last();
-    const Pieces p(a, row_pieces);
-    const int64_t step = (int64_t)gridDim.x * kPrepThreads;
-    uint32_t m = 0;
-    for (int64_t t0 = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x; t0 < p.n; t0 += 4 * step) {
-        uint4 x[4];
+    uint32_t most = 0u, least = 0xFFFFFFFFu;
+    for (int i = 0; i < p.n; i += V::kAhead * V::kRows) {
+        uint4 x[V::kAhead];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
+        for (int e = 0; e < V::kAhead; ++e) x[e] = p.load(i + e * V::kRows);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < V::kAhead; ++e) {
             const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
+            uint32_t m = 0u;
 #pragma unroll
             for (int c = 0; c < 4; ++c) m = max(m, max((w[c] << 16) & 0x7FFFFFFFu, w[c] & 0x7FFF0000u));
+#pragma unroll
+            for (int o = 1; o < V::P; o <<= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+            most = max(most, m);
+            least = min(least, m == 0u ? 0xFFFFFFFFu : m);
         }
     }
-    m = __reduce_max_sync(0xFFFFFFFFu, m);
-    __shared__ uint32_t red[kPrepThreads / 32];
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    __shared__ uint2 red[kPrepWarps];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_uint2(most, least);
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < kPrepThreads / 32; ++w) m = max(m, red[w]);
-        part[blockIdx.x] = __uint_as_float(m);
+        for (int w = 1; w < kPrepWarps; ++w) {
+            most = max(most, red[w].x);
+            least = min(least, red[w].y);
+        }
+        part[(int64_t)blockIdx.y * a.n_runs + blockIdx.x] = most | (least >> 16);
     }
 }
-// part[0 .. n_part - 1] -> *absmax; v16 = fp16(v 2^-E). A programmatic dependent of the kernel above; the attention is one of
-// this kernel, allowed to start once every CTA here knows that nothing before this call is still running.
-__global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a, int row_pieces, const float *part, int n_part, float *absmax,
-                                                             __half *v16)
+// v16 = fp16(v 2^-E), E from the parts of the sequence's runs, and top[seq][head] as v_top. A programmatic dependent of the kernel
+// above; the attention is one of this kernel, allowed to start once every CTA here knows that nothing before this call is still running.
+template <int D>
+__global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a, const uint32_t *part, float *top, __half *v16)
 {
-    const Pieces p(a, row_pieces);
-    const int64_t step = (int64_t)gridDim.x * kPrepThreads;
-    int64_t t0 = (int64_t)blockIdx.x * kPrepThreads + threadIdx.x;
-    uint4 x[2];
+    using V = HeadPieces<D>;
+    const PackRun run = a.runs[blockIdx.x];
+    const int head = blockIdx.y;
+    const V p(a, run, head);
+    uint4 x[V::kAhead];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
+    for (int e = 0; e < V::kAhead; ++e) x[e] = p.load(e * V::kRows);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    uint32_t m = 0;
-    for (int i = threadIdx.x; i < n_part; i += kPrepThreads) m = max(m, __float_as_uint(part[i]));
-    m = __reduce_max_sync(0xFFFFFFFFu, m);
-    __shared__ uint32_t red[kPrepThreads / 32];
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = m;
+    uint32_t most = 0u, least = 0xFFFFu;
+    for (int i = run.run0 + (int)threadIdx.x; i < run.run1; i += kPrepThreads) {
+        const uint32_t w = part[(int64_t)head * a.n_runs + i];
+        most = max(most, w & 0xFFFF0000u);
+        least = min(least, w & 0xFFFFu);
+    }
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    least = __reduce_min_sync(0xFFFFFFFFu, least);
+    __shared__ uint2 red[kPrepWarps];
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = make_uint2(most, least);
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kPrepThreads / 32; ++w) m = max(m, red[w]);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *absmax = __uint_as_float(m);
-    const float s = pow2i(-value_exp(__uint_as_float(m)));
-    for (;;) {
+    for (int w = 0; w < kPrepWarps; ++w) {
+        most = max(most, red[w].x);
+        least = min(least, red[w].y);
+    }
+    const bool as_given = most >= 0x7F800000u || (least != 0xFFFFu && (int)(most >> 23) - (int)(least >> 7) > kMostSpan);
+    if ((int)blockIdx.x == run.run0 && threadIdx.x == 0) top[(int64_t)run.seq * a.Hkv + head] = as_given ? INFINITY : __uint_as_float(most);
+    // (zeros where v16 is not to be used: a tile at a sequence's end reaches into the next one's, under weights of 0)
+    const float s = as_given ? 0.f : pow2i(-value_exp(__uint_as_float(most)));
+    __half *out = v16 + ((int64_t)run.first * a.Hkv + head) * D + (threadIdx.x % V::P) * 8;
+    for (int i = 0;;) {
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < V::kAhead; ++e) {
             const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
             uint32_t y[4];
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const __half2 hv = __floats2half2_rn(__uint_as_float(w[c] << 16) * s, __uint_as_float(w[c] & 0xFFFF0000u) * s);
-                y[c] = *reinterpret_cast<const uint32_t *>(&hv);
+                y[c] = as_given ? 0u : *reinterpret_cast<const uint32_t *>(&hv);
             }
-            if (t0 + e * step < p.n) reinterpret_cast<uint4 *>(v16)[t0 + e * step] = make_uint4(y[0], y[1], y[2], y[3]);
+            const int r = i + e * V::kRows + p.row;
+            if (r < p.n) *reinterpret_cast<uint4 *>(out + (int64_t)r * a.Hkv * D) = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        t0 += 2 * step;
-        if (t0 >= p.n) break;
+        i += V::kAhead * V::kRows;
+        if (i >= p.n) break;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = t0 + e * step < p.n ? p.load(t0 + e * step) : make_uint4(0u, 0u, 0u, 0u);
+        for (int e = 0; e < V::kAhead; ++e) x[e] = p.load(i + e * V::kRows);
     }
 }
 
@@ -1417,28 +1458,26 @@ cudaError_t launch_rows(const PackedArgs &a, const PackedMaps &maps, cudaStream_
 
 }  // namespace
 
-size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim)
+// scratch: the bounds of the runs, the largest magnitudes, the values
+static size_t scratch_part(const PackedArgs &a) { return (sizeof(uint32_t) * a.n_runs * a.Hkv + 255) & ~size_t(255); }
+static size_t scratch_top(const PackedArgs &a) { return (sizeof(float) * a.n_seqs * a.Hkv + 255) & ~size_t(255); }
+size_t packed_scratch_bytes(const PackedArgs &a, int32_t head_dim)
 {
-    return 256 + sizeof(float) * kPrepBlocks + 256 + (size_t)k_total * kv_heads * head_dim * 2;
+    return scratch_part(a) + scratch_top(a) + (size_t)a.k_total * a.Hkv * head_dim * 2;
 }
 
 cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s)
 {
-    // scratch: the largest magnitude, the parts it comes from, the values
-    float *absmax = static_cast<float *>(scratch), *part = absmax + 64;
-    __half *v16 = reinterpret_cast<__half *>((reinterpret_cast<uintptr_t>(part + kPrepBlocks) + 255) & ~uintptr_t(255));
-    a.v_absmax = absmax;
-    const int row_pieces = a.Hkv * D / 8;
-    const int64_t pieces = a.k_total * row_pieces, blocks = (pieces + 4 * kPrepThreads - 1) / (4 * kPrepThreads);
-    if (pieces > 0) {
-        const int n_part = (int)(blocks < kPrepBlocks ? blocks : kPrepBlocks);
-        cudaError_t e = launch_chained(k_values_absmax, dim3(n_part), dim3(kPrepThreads), 0, s, a, row_pieces, part);
+    char *const mem = static_cast<char *>(scratch);
+    uint32_t *const part = reinterpret_cast<uint32_t *>(mem);
+    float *const top = reinterpret_cast<float *>(mem + scratch_part(a));
+    __half *const v16 = reinterpret_cast<__half *>(mem + scratch_part(a) + scratch_top(a));
+    a.v_top = top;
+    if (a.n_runs > 0) {
+        const dim3 grid((unsigned)a.n_runs, (unsigned)a.Hkv);
+        cudaError_t e = launch_chained(D == 128 ? k_values_bounds<128> : k_values_bounds<64>, grid, dim3(kPrepThreads), 0, s, a, part);
         if (e != cudaSuccess) return e;
-        e = launch_chained(k_values_f16, dim3((unsigned)(blocks < 1216 ? blocks : 1216)), dim3(kPrepThreads), 0, s, a, row_pieces, part, n_part,
-                           absmax, v16);
-        if (e != cudaSuccess) return e;
-    } else {
-        const cudaError_t e = cudaMemsetAsync(absmax, 0, sizeof(float), s);
+        e = launch_chained(D == 128 ? k_values_f16<128> : k_values_f16<64>, grid, dim3(kPrepThreads), 0, s, a, part, top, v16);
         if (e != cudaSuccess) return e;
     }
     alignas(64) PackedMaps maps;

@@ -14,6 +14,7 @@ namespace ris {
 
 constexpr int kPackRows = 128;      // query rows of a work item of a pack (one TMEM tile)
 constexpr int kPackKeys = 128;      // keys of a key item
+constexpr int kPackRuns = 304;      // runs of the keys of a long pack, about (two CTAs to an SM and head)
 constexpr int kMaxAxes = 4;
 constexpr int kCacheGroup = 32;     // elements that share a scale
 constexpr int kMaxPackSeqs = 65535;
@@ -29,6 +30,14 @@ struct alignas(32) PackItem {
     int32_t k_base;  // first key of the sequence in k / v
     int32_t k_len;
     int32_t pad[2];
+};
+
+// A run of the keys of a sequence, by which the values are looked through and laid out.
+struct alignas(32) PackRun {
+    int32_t seq;
+    int32_t first, n;    // its keys in k / v
+    int32_t run0, run1;  // the runs of the sequence
+    int32_t pad[3];
 };
 
 struct RopeAxesArgs {
@@ -62,14 +71,17 @@ struct PackedArgs {
     int32_t weight_rows;       // 0: none
     float *key_weight;         // [Hkv][k_total]
     float2 *row_stat;          // scratch [Hq][q_total]: each row's (maximum in log2, 1 / sum); null without weights
-    const float *v_absmax;     // device, tile kernels: max |v|
+    const PackRun *runs;
+    int32_t n_runs, n_seqs;
+    const float *v_top;        // tile kernels: [n_seqs][Hkv] the largest |v|, or infinity where the rows are to be computed from
+                               // the values as given (undefined for sequences without keys)
 };
 // fp32 inputs: items of kPackRows rows.
 cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStream_t s);
 cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s);
 // bf16 inputs: items of kPackRows rows, or for clusters (head dim 128) with an odd group of 2 kPackRows; scratch
 // of packed_scratch_bytes, 256-byte aligned.
-size_t packed_scratch_bytes(int64_t k_total, int32_t kv_heads, int32_t head_dim);
+size_t packed_scratch_bytes(const PackedArgs &a, int32_t head_dim);
 cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s);
 cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s);
 

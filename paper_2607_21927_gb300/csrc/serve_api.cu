@@ -21,7 +21,8 @@ struct ris_pack_s {
     void *mem = nullptr;  // device: everything below
     int32_t *q_off = nullptr, *seq_of = nullptr;
     PackItem *items = nullptr, *pairs = nullptr, *key_items = nullptr;  // of 128 rows, 256 rows, 128 keys
-    int32_t n_items = 0, n_pairs = 0, n_key_items = 0;
+    PackRun *runs = nullptr;
+    int32_t n_items = 0, n_pairs = 0, n_key_items = 0, n_runs = 0;
     int64_t key_tiles = 0;  // of 128 x 128 that the items of 128 rows see
     cudaStream_t stream = nullptr;
 };
@@ -179,6 +180,25 @@ std::vector<PackItem> items_of(const std::vector<int32_t> &q_off, const std::vec
     return v;
 }
 
+// Runs of the keys: whole key items, so long that there are about kPackRuns of them.
+std::vector<PackRun> runs_of(const std::vector<int32_t> &k_off)
+{
+    const int64_t total = k_off.back(), step = std::max<int64_t>(1, (total + (int64_t)kPackRuns * kPackKeys - 1) / ((int64_t)kPackRuns * kPackKeys)) * kPackKeys;
+    std::vector<PackRun> v;
+    for (size_t s = 0; s + 1 < k_off.size(); ++s) {
+        PackRun r{};
+        r.seq = (int32_t)s;
+        r.run0 = (int32_t)v.size();
+        r.run1 = (int32_t)(r.run0 + (k_off[s + 1] - k_off[s] + step - 1) / step);
+        for (int64_t k = k_off[s]; k < k_off[s + 1]; k += step) {
+            r.first = (int32_t)k;
+            r.n = (int32_t)std::min<int64_t>(step, k_off[s + 1] - k);
+            v.push_back(r);
+        }
+    }
+    return v;
+}
+
 }  // namespace
 
 extern "C" {
@@ -220,12 +240,14 @@ ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t
         p->n_items = (int32_t)items.size();
         p->n_pairs = (int32_t)pairs.size();
         p->n_key_items = (int32_t)keys.size();
+        const std::vector<PackRun> runs = runs_of(k_off);
+        p->n_runs = (int32_t)runs.size();
         cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
         p->stream = s;
         const size_t off_b = room(sizeof(int32_t) * q_off.size()), seq_b = room(sizeof(int32_t) * seq_of.size()),
                      item_b = room(sizeof(PackItem) * items.size()), pair_b = room(sizeof(PackItem) * pairs.size()),
-                     key_b = room(sizeof(PackItem) * keys.size());
-        cudaError_t e = library_alloc(&p->mem, off_b + seq_b + item_b + pair_b + key_b, s);
+                     key_b = room(sizeof(PackItem) * keys.size()), run_b = room(sizeof(PackRun) * runs.size());
+        cudaError_t e = library_alloc(&p->mem, off_b + seq_b + item_b + pair_b + key_b + run_b, s);
         char *d = static_cast<char *>(p->mem);
         auto put = [&](const void *src, size_t bytes) {
             if (e == cudaSuccess && bytes > 0) e = cudaMemcpyAsync(d, src, bytes, cudaMemcpyHostToDevice, s);
@@ -244,6 +266,9 @@ ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t
         d += pair_b;
         p->key_items = reinterpret_cast<PackItem *>(d);
         put(keys.data(), sizeof(PackItem) * keys.size());
+        d += key_b;
+        p->runs = reinterpret_cast<PackRun *>(d);
+        put(runs.data(), sizeof(PackRun) * runs.size());
         // the host arrays end with this call: the copies out of them must have been taken
         if (e == cudaSuccess) e = cudaStreamSynchronize(s);
         if (e != cudaSuccess) {
@@ -385,6 +410,9 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     a.n_items = pack->n_items;
     a.key_items = pack->key_items;
     a.n_key_items = pack->n_key_items;
+    a.runs = pack->runs;
+    a.n_runs = pack->n_runs;
+    a.n_seqs = pack->n_seqs;
     a.Hq = heads;
     a.Hkv = kv_heads;
     a.G = heads / kv_heads;
@@ -398,7 +426,7 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
         a.n_items = pack->n_pairs;
     }
     const size_t stat_b = weight_rows > 0 ? room(sizeof(float2) * (size_t)heads * pack->q_total) : 0;
-    const size_t tile_b = tiles ? packed_scratch_bytes(pack->k_total, kv_heads, head_dim) : 0;
+    const size_t tile_b = tiles ? packed_scratch_bytes(a, head_dim) : 0;
     Scratch mem;
     if (stat_b + tile_b > 0) RIS_CUDA(mem.alloc(stat_b + tile_b, s));
     if (weight_rows > 0) a.row_stat = static_cast<float2 *>(mem.p);
