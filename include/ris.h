@@ -415,10 +415,12 @@ ris_status ris_decode_step(ris_anchor_t anchor, const void *q, const void *k, co
  * q_lens[s] rows (new tokens) and k_lens[s] keys (HOST arrays; k_lens NULL: the same lengths). The rows
  * are the last of the sequence's positions: row i sees keys j <= i + k_lens[s] - q_lens[s], and a row that sees none
  * gets zeros and a log-sum-exp of -infinity. Lengths may be 0. Built once per batch
- * and kept for all layers and all calls of it, on any stream ordered after `stream`. Blocks (the
+ * and kept for all layers and all calls of it, on any stream. Blocks (the
  * plan's copy); not during stream capture. Errors: RIS_ERR_INVALID (n_seqs outside [1, 65535], a negative length,
  * more than 2^31 - 65537 tokens), RIS_ERR_OOM, RIS_ERR_CUDA. On error *out is NULL.
- * ris_pack_info: any output may be NULL. ris_pack_free: ordered on the stream it was built on. */
+ * ris_pack_info: any output may be NULL. ris_pack_free: gives the plan back on the stream it was built on, behind every call
+ * with the pack that was queued before, on whatever stream. Calls captured into a graph are not among them: a graph must not be
+ * replayed once a pack in it was freed, nor the pack freed before the last replay has finished. */
 typedef struct ris_pack_s *ris_pack_t;
 ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t n_seqs, ris_pack_t *out, void *stream);
 ris_status ris_pack_info(ris_pack_t pack, int32_t *n_seqs, int64_t *q_total, int64_t *k_total, int64_t *q_longest,

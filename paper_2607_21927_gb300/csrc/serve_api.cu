@@ -8,7 +8,9 @@
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
+#include <mutex>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "serve.h"
@@ -25,6 +27,11 @@ struct ris_pack_s {
     int32_t n_items = 0, n_pairs = 0, n_key_items = 0, n_runs = 0;
     int64_t key_tiles = 0;  // of 128 x 128 that the items of 128 rows see
     cudaStream_t stream = nullptr;
+    // Streams other than its own that calls with it were queued on, each with an event behind the last of them: its memory
+    // is given back behind these.
+    std::mutex mu;
+    std::vector<std::pair<cudaStream_t, cudaEvent_t>> used;
+    bool unknown = false;  // a use could not be noted: the device is waited for
 };
 
 namespace {
@@ -70,6 +77,39 @@ struct Scratch {
     ~Scratch()
     {
         if (p) cudaFreeAsync(p, s);
+    }
+};
+
+// Notes that a call queues work with the pack on `s`, behind that work: when the call returns, whether it succeeds or not.
+struct PackUse {
+    ris_pack_s *pack;
+    cudaStream_t s;
+    ~PackUse()
+    {
+        // (the per-thread default stream is another one in each thread: one handle says too little)
+        const bool one = s != cudaStreamPerThread;
+        if (s == pack->stream && one) return;
+        cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
+        cudaError_t e = cudaStreamIsCapturing(s, &st);
+        if (e == cudaSuccess && st != cudaStreamCaptureStatusNone) return;  // (a graph's uses are the caller's to order)
+        std::lock_guard<std::mutex> lk(pack->mu);
+        cudaEvent_t ev = nullptr;
+        for (const auto &u : pack->used)
+            if (u.first == s) ev = u.second;
+        if (e == cudaSuccess && one && ev == nullptr) {
+            e = cudaEventCreateWithFlags(&ev, cudaEventDisableTiming);
+            if (e == cudaSuccess) try {
+                    pack->used.emplace_back(s, ev);
+                } catch (...) {  // host memory
+                    cudaEventDestroy(ev);
+                    e = cudaErrorMemoryAllocation;
+                }
+        }
+        if (e == cudaSuccess && one) e = cudaEventRecord(ev, s);
+        if (e != cudaSuccess || !one) {
+            cudaGetLastError();
+            pack->unknown = true;
+        }
     }
 };
 
@@ -299,7 +339,18 @@ ris_status ris_pack_info(ris_pack_t pack, int32_t *n_seqs, int64_t *q_total, int
 ris_status ris_pack_free(ris_pack_t pack)
 {
     if (pack == nullptr) return RIS_OK;
-    const cudaError_t e = pack->mem ? cudaFreeAsync(pack->mem, pack->stream) : cudaSuccess;
+    cudaError_t e = cudaSuccess;
+    for (const auto &u : pack->used)
+        if (e == cudaSuccess) e = cudaStreamWaitEvent(pack->stream, u.second, 0);
+    if (pack->unknown || e != cudaSuccess) {
+        cudaGetLastError();
+        e = cudaDeviceSynchronize();
+    }
+    if (pack->mem) {
+        const cudaError_t e2 = cudaFreeAsync(pack->mem, pack->stream);
+        if (e == cudaSuccess) e = e2;
+    }
+    for (const auto &u : pack->used) cudaEventDestroy(u.second);
     delete pack;
     if (e != cudaSuccess) return cuda_fail(e, "cudaFreeAsync");
     return RIS_OK;
@@ -427,6 +478,7 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     }
     const size_t stat_b = weight_rows > 0 ? room(sizeof(float2) * (size_t)heads * pack->q_total) : 0;
     const size_t tile_b = tiles ? packed_scratch_bytes(a, head_dim) : 0;
+    const PackUse use{pack, s};
     Scratch mem;
     if (stat_b + tile_b > 0) RIS_CUDA(mem.alloc(stat_b + tile_b, s));
     if (weight_rows > 0) a.row_stat = static_cast<float2 *>(mem.p);
@@ -472,6 +524,7 @@ ris_status ris_cache4_append(const ris_cache4 *cache, ris_pack_t pack, const voi
     a.seq_of = pack->seq_of;
     a.total = pack->q_total;
     a.ticket = cache->sync;
+    const PackUse use{pack, reinterpret_cast<cudaStream_t>(stream)};
     RIS_CUDA(launch_cache4_append(a, dtype, reinterpret_cast<cudaStream_t>(stream)));
     return RIS_OK;
 }

@@ -599,7 +599,8 @@ def ris_mask_row_split(mask: Mask, parts: int):
 
 # ----------------------------------------------------------------------------- packed prompts
 class Pack:
-    """The plan of a batch of sequences (ris_pack_create); freed by ``free()`` or when garbage collected."""
+    """The plan of a batch of sequences (ris_pack_create); freed by ``free()`` or when garbage collected, behind the calls with
+    it that were queued on any stream, except those captured into a graph, which must not outlive its packs."""
 
     def __init__(self, handle: ctypes.c_void_p):
         self.handle = handle
