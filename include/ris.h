@@ -344,6 +344,7 @@ ris_status ris_shutdown(void);
  * first wait on them gives up after wait_limit_cycles (0 = the default, about 2^31 cycles):
  * the kernel sets its device error word, releases its tensor memory and returns, and
  * ris_device_status reports RIS_ERR_DEVICE_TIMEOUT (outputs of that launch are undefined).
+ * The copies of ris_cache4_attend are left out and waited for in the same way.
  * no_loads = 0 with a nonzero limit only shortens the waits. (0, 0) restores the defaults.
  * Both switches are process-wide. Errors: RIS_ERR_INVALID. */
 ris_status ris_debug_fail_allocation(int64_t n);

@@ -272,7 +272,8 @@ struct Lay {
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
+constexpr int64_t kWaitLimit = int64_t(1) << 31;  // cycles
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int64_t limit = kWaitLimit)
 {
     const long long t0 = clock64();
     for (;;) {
@@ -283,7 +284,7 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity)
             : "r"(bar), "r"(parity)
             : "memory");
         if (ok) return true;
-        if (clock64() - t0 > (1LL << 31)) return false;
+        if (clock64() - t0 > limit) return false;
     }
 }
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -405,7 +406,7 @@ __device__ __forceinline__ int64_t mul_div(int64_t x, int y, int z)
 // and no group, slot or scale that is not finite takes bits from another group. O carries its group's f.
 // Slots past the length enter with score -infinity and scale 0, whatever lies there.
 // A list takes 8 query heads of its KV head, a product's columns.
-// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 53.8 us a call with the join, 4.8 of the 6.8 TB/s that a
+// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 54.6 us a call with the join, 4.7 of the 6.8 TB/s that a
 // copy reaches (one exponent for all groups and heads, which a scale that is not finite or one large slot spoils, took 49.7; fp32
 // outputs 82 and 73); unpacking keeps the ALU pipe and the issue slots half busy, so three CTAs' loads and arithmetic do not
 // overlap all the way. Smaller calls are latency: 24 sequences of 700 to 9,216 slots 12.5 us before the join, of which the
@@ -503,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             for (int g = 0; g < NG; ++g) x[g].load(q + kCacheGroup * g);
             // after the queries' loads: behind all the CTAs' copies, 30 MB at once, they would take 4 us
             // (the ring is empty here: the last part's stages were waited for, and its outputs have left it)
-            if (lane == 0 && ok)
+            if (lane == 0 && ok && !a.debug_no_loads)
                 for (int i = 0, s0 = warp * per, slot = used; i < kStages && s0 < n; ++i, s0 += s_step) {
                     fetch(s0, slot);
                     slot = slot + 1 == kStages ? 0 : slot + 1;
@@ -745,23 +746,27 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                 }
             }
         };
-        for (int s0 = warp * per; s0 < n; s0 += s_step) {
-            ok = __all_sync(0xFFFFFFFFu, ok && mbar_wait(bars + 8 * used, phase));
-            if (ok) {
-                const unsigned char *sm = ring + used * L::STAGE;
-                if (min(per, n - s0) == kStageSlots)
-                    stage(std::true_type{}, sm, s0, kStageSlots);
-                else
-                    stage(std::false_type{}, sm, s0, min(per, n - s0));
-                __syncwarp();  // every lane is done with the stage
-                const int next = s0 + kStages * s_step;
-                if (lane == 0 && next < n) fetch(next, used);
+        for (int s0 = warp * per; ok && s0 < n; s0 += s_step) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bars + 8 * used, phase, a.wait_limit));
+            if (!ok) {
+                // the stages asked for, this one and the next of the ring, have landed before the ring is used for
+                // anything else, or the CTA ends
+                for (int i = 0; i < kStages && s0 < n && !a.debug_no_loads; ++i, s0 += s_step) {
+                    mbar_wait(bars + 8 * used, phase);
+                    if (++used == kStages) used = 0, phase ^= 1;
+                }
+                break;
             }
-            if (++used == kStages) {
-                used = 0;
-                phase ^= 1;
-            }
+            const unsigned char *sm = ring + used * L::STAGE;
+            if (min(per, n - s0) == kStageSlots)
+                stage(std::true_type{}, sm, s0, kStageSlots);
+            else
+                stage(std::false_type{}, sm, s0, min(per, n - s0));
+            __syncwarp();  // every lane is done with the stage
+            if (lane == 0 && s0 + kStages * s_step < n) fetch(s0 + kStages * s_step, used);
+            if (++used == kStages) used = 0, phase ^= 1;
         }
+        __syncwarp();
         // the four warps' parts of each head, through the rings: [warp][head][D], (maximum, sum), factors
         __syncthreads();
         constexpr int LO_ = D + 4;  // (the four lanes t4 write rows two apart)
@@ -811,7 +816,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
         __syncthreads();
         }
     }
-    if (!ok) atomicOr(&g_ris_cache4_error, 4u);  // (a copy that never landed: the outputs are undefined)
+    if (!ok) atomicOr(&g_ris_cache4_error, 4u);  // (a copy that was given up: the outputs are undefined)
 }
 
 // Joins the parts of a list. The first CTAs: one per (query head, sequence), warps over its parts, a lane per
@@ -993,8 +998,9 @@ cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_
                       : launch_chained(k_cache4_read<64>, grid, block, 0, s, c, first, count, blocks, k, v);
 }
 
-cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s)
+cudaError_t launch_cache4_attend(Cache4AttendArgs a, int dtype, int out_dtype, cudaStream_t s)
 {
+    if (a.wait_limit == 0) a.wait_limit = kWaitLimit;
     // fp32 outputs take the weights as two fp16 parts (22 bits), bf16 outputs as one (11 bits, against the
     // 8 that the output keeps)
     cudaError_t e;

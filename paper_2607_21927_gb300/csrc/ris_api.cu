@@ -387,6 +387,8 @@ ris_status validate_attention(const void *q, const void *k, const void *v, void 
 
 namespace ris {
 void set_error_text(const char *msg) { t_err = msg; }
+int64_t debug_wait_limit() { return g_wait_limit.load(); }
+int32_t debug_no_loads() { return g_tile_no_loads.load(); }
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s)
 {
     prepare_pool_once();

@@ -126,8 +126,10 @@ struct Cache4AttendArgs {
     float2 *part_ml;             // [ctas + lists][heads of a block]
     int32_t *list_cta;           // [lists][2] first and last CTA of each list that holds slots
     float *scores;               // weights: [B][Hq][cap] scores in log2
+    int64_t wait_limit;          // cycles a device-side wait may take (0: about 2^31)
+    int32_t debug_no_loads;      // tests only: no copies are issued, so the first wait on them gives up
 };
-cudaError_t launch_cache4_attend(const Cache4AttendArgs &a, int dtype, int out_dtype, cudaStream_t s);
+cudaError_t launch_cache4_attend(Cache4AttendArgs a, int dtype, int out_dtype, cudaStream_t s);
 
 struct Cache4EvictArgs {
     Cache4Args src, dst;
@@ -142,6 +144,10 @@ cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaSt
 unsigned int read_cache4_error();
 // Reads and clears the error word of the packed attention's tile kernels (a bounded wait gave up).
 unsigned int read_packed_error();
+
+// What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked; whether loads are left out.
+int64_t debug_wait_limit();
+int32_t debug_no_loads();
 
 // Stream-ordered pool memory, as every allocation of the library (ris_api.cu).
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s);

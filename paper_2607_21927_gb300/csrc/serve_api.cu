@@ -589,6 +589,8 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
     a.part_ml = reinterpret_cast<float2 *>(static_cast<char *>(mem.p) + o_b);
     a.list_cta = reinterpret_cast<int32_t *>(static_cast<char *>(mem.p) + o_b + ml_b);
     if (weight_out != nullptr) a.scores = reinterpret_cast<float *>(static_cast<char *>(mem.p) + o_b + ml_b + list_b);
+    a.wait_limit = debug_wait_limit();
+    a.debug_no_loads = debug_no_loads();
     RIS_CUDA(launch_cache4_attend(a, dtype, out_dtype, s));
     return RIS_OK;
 }
