@@ -4,10 +4,10 @@
 
 #include <cuda_runtime.h>
 
-#include <atomic>
 #include <cstdint>
 
 #include "../../include/ris.h"
+#include "once.h"
 #include "ris_internal.h"
 
 namespace ris {
@@ -161,18 +161,6 @@ __device__ __forceinline__ void after_last()
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
-// What a kernel needs once before its first launch; tried again where it failed.
-struct Once {
-    std::atomic<bool> done{false};
-    template <typename F>
-    cudaError_t operator()(F f)
-    {
-        if (done.load(std::memory_order_acquire)) return cudaSuccess;
-        const cudaError_t e = f();
-        if (e == cudaSuccess) done.store(true, std::memory_order_release);
-        return e;
-    }
-};
 template <typename... P, typename... A>
 cudaError_t launch_chained(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const A &...args)
 {
