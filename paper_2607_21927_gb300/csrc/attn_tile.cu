@@ -92,6 +92,7 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "once.h"
 
 namespace ris {
 
@@ -1280,17 +1281,17 @@ template <int DT, bool SPLIT, bool DENSE, typename TOut, bool SUFFIX = false>
 cudaError_t launch_t(const AttnArgs &a, const TileMaps &maps, cudaStream_t s)
 {
     auto kern = k_attn_tile<DT, SPLIT, DENSE, SUFFIX, TOut>;
-    static bool attr = false;
-    if (!attr) {
+    static Once once;
+    const cudaError_t ready = once([&] {
         cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES);
         if (e != cudaSuccess) return e;
         // the softmax threads' setmaxnreg would wait for registers that a smaller launch lacks
         cudaFuncAttributes fa;
         e = cudaFuncGetAttributes(&fa, kern);
         if (e != cudaSuccess) return e;
-        if (fa.numRegs < kRegs) return cudaErrorInvalidConfiguration;
-        attr = true;
-    }
+        return fa.numRegs < kRegs ? cudaErrorInvalidConfiguration : cudaSuccess;
+    });
+    if (ready != cudaSuccess) return ready;
     constexpr int CG = Lay<DT>::CG;
     const int64_t n_qt = (a.row1 + BM - 1) / BM - a.row0 / BM;  // tiles covering rows row0 .. row1-1
     const bool tile_pair = CG == 2 && (a.G & 1) != 0;

@@ -78,3 +78,9 @@ def test_calls_on_two_devices():
                 ris.ris_cache4_attend(cache, q[:2].contiguous())
                 ris.ris_cache4_evict(cache, cache, 16, 4)
             ris.ris_device_status()
+
+
+def test_tile_kernel_is_prepared_per_device():
+    text = open(os.path.join(ROOT, "paper_2607_21927_gb300", "csrc", "attn_tile.cu")).read()
+    assert text.count("cudaFuncSetAttribute(") == 1 and "static bool" not in text
+    assert text.index("static Once once;") < text.index("= once([") < text.index("cudaFuncSetAttribute(")
