@@ -610,7 +610,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                         for (int e = 0; e < 4; ++e) {
                             const int h = 2 * t4 + (e & 1), slot = i * kTile + tile_slot(g8 + 8 * (e >> 1));
                             if ((FULL || slot < ns) && h < nh)
-                                a.scores[(head0 + h) * a.c.cap + first + s0 + slot] = s[i][e] * unscale[e & 1];
+                                a.scores[(head0 + h) * a.score_pitch + first + s0 + slot] = s[i][e] * unscale[e & 1];
                         }
                     }
                 }
@@ -910,13 +910,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
     }
     // weights: the scores of the first eight heads are on their way before the heads' sums are known
     const int64_t s1 = s0 + 4 * threadIdx.x, row = ((int64_t)b * a.c.Hkv + kvh_w) * a.c.cap + s1;
-    const float *sc = a.scores + ((int64_t)b * a.Hq + kvh_w * a.G) * a.c.cap + s1;
+    const float *sc = a.scores + ((int64_t)b * a.Hq + kvh_w * a.G) * a.score_pitch + s1;
     const bool in = s1 < len;
     float4 x[8], y = make_float4(0.f, 0.f, 0.f, 0.f);
     auto load = [&](int h0) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            if (in && h0 + e < a.G) x[e] = *reinterpret_cast<const float4 *>(sc + (h0 + e) * a.c.cap);
+            if (in && h0 + e < a.G) x[e] = *reinterpret_cast<const float4 *>(sc + (h0 + e) * a.score_pitch);
     };
     load(0);
     if (in && a.weight_in != nullptr) y = *reinterpret_cast<const float4 *>(a.weight_in + row);

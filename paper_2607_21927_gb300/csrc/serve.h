@@ -125,7 +125,8 @@ struct Cache4AttendArgs {
     float *part_o;               // [ctas + lists][heads of a block][D]
     float2 *part_ml;             // [ctas + lists][heads of a block]
     int32_t *list_cta;           // [lists][2] first and last CTA of each list that holds slots
-    float *scores;               // weights: [B][Hq][cap] scores in log2
+    float *scores;               // weights: [B][Hq][score_pitch] scores in log2
+    int64_t score_pitch;         // reach, rounded up to a multiple of 4
     int64_t wait_limit;          // cycles a device-side wait may take (0: about 2^31)
     int32_t debug_no_loads;      // tests only: no copies are issued, so the first wait on them gives up
 };

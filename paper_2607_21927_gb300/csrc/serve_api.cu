@@ -581,7 +581,8 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
     a.ctas = (int32_t)std::min<int64_t>(152 * per_sm, lists * ((a.reach + kCacheUnit - 1) / kCacheUnit));
     const size_t parts = ((size_t)a.ctas + (size_t)lists) * block;
     const size_t o_b = room(sizeof(float) * parts * cache->head_dim), ml_b = room(sizeof(float2) * parts);
-    const size_t score_b = weight_out != nullptr ? sizeof(float) * (size_t)cache->batch * heads * cache->capacity : 0;
+    a.score_pitch = (a.reach + 3) & ~int64_t(3);
+    const size_t score_b = weight_out != nullptr ? sizeof(float) * (size_t)cache->batch * heads * a.score_pitch : 0;
     Scratch mem;
     const size_t list_b = room(2 * sizeof(int32_t) * (size_t)lists);
     RIS_CUDA(mem.alloc(o_b + ml_b + list_b + score_b, s));
