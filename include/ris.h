@@ -451,7 +451,7 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
  * lse: optional [heads][q_total] natural-log sum of exp of the scaled scores.
  * weight_rows W > 0 with key_weight [kv_heads][k_total]: the attention weight that each key got from the
  * last W rows of its sequence (all rows where there are fewer), summed over the query heads of its KV head: what
- * ris_cache4_append takes as the first of a slot's accumulated weight. W = 0: key_weight NULL.
+ * ris_cache4_append takes as the first of a slot's accumulated weight. W = 0: key_weight NULL; it may be NULL where no sequence has a key.
  * head_dim in {64, 128}, any heads / kv_heads, fp32 or bf16. fp32 inputs never use a narrower product.
  * A key that a row does not see takes no part in it, whatever it holds.
  * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (more row tiles x heads than a grid holds), RIS_ERR_OOM, RIS_ERR_CUDA. */

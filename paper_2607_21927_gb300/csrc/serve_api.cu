@@ -433,7 +433,8 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
     RIS_TRY(check_dtype(dtype, "dtype"));
     RIS_TRY(check_dtype(out_dtype, "out_dtype"));
     if (weight_rows < 0) return fail(RIS_ERR_INVALID, "weight_rows %d must be >= 0", weight_rows);
-    if ((weight_rows > 0) != (key_weight != nullptr)) return fail(RIS_ERR_INVALID, "key_weight goes with weight_rows > 0");
+    if (weight_rows == 0 && key_weight != nullptr) return fail(RIS_ERR_INVALID, "key_weight without weight_rows");
+    if (weight_rows > 0 && key_weight == nullptr && pack->k_total > 0) return fail(RIS_ERR_INVALID, "weight_rows without key_weight");
     if ((lse != nullptr && !aligned(lse, 16)) || (key_weight != nullptr && !aligned(key_weight, 16)))
         return fail(RIS_ERR_INVALID, "lse or key_weight is not 16-byte aligned");
     if (pack->q_total > 0) {
