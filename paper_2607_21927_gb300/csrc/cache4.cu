@@ -204,6 +204,13 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache4_append(const Cache4Ap
         }
 }
 
+__global__ void __launch_bounds__(kAppendThreads) k_cache4_start(const Cache4Args c, const int32_t *start)
+{
+    const int s = blockIdx.x * kAppendThreads + threadIdx.x;
+    after_last();
+    if (s < c.B) c.length[s] = (int32_t)max((int64_t)0, min((int64_t)start[s], c.cap));
+}
+
 // the two values of a byte
 __device__ __forceinline__ __half2 values2(uint32_t byte)
 {
@@ -988,6 +995,11 @@ cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStrea
                             : launch_chained(k_cache4_append<float, 64>, grid, block, 0, s, a);
     return a.c.D == 128 ? launch_chained(k_cache4_append<__nv_bfloat16, 128>, grid, block, 0, s, a)
                         : launch_chained(k_cache4_append<__nv_bfloat16, 64>, grid, block, 0, s, a);
+}
+
+cudaError_t launch_cache4_start(const Cache4Args &c, const int32_t *start, cudaStream_t s)
+{
+    return launch_chained(k_cache4_start, dim3((unsigned)((c.B + kAppendThreads - 1) / kAppendThreads)), dim3(kAppendThreads), 0, s, c, start);
 }
 
 cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_t count, float *k, float *v, cudaStream_t s)

@@ -108,6 +108,8 @@ struct Cache4AppendArgs {
     unsigned int *ticket;        // start null: CTAs done (0 between calls)
 };
 cudaError_t launch_cache4_append(const Cache4AppendArgs &a, int dtype, cudaStream_t s);
+// The lengths of an append without rows.
+cudaError_t launch_cache4_start(const Cache4Args &c, const int32_t *start, cudaStream_t s);
 cudaError_t launch_cache4_read(const Cache4Args &c, const int32_t *first, int64_t count, float *k, float *v, cudaStream_t s);
 
 struct Cache4AttendArgs {

@@ -504,7 +504,7 @@ ris_status ris_cache4_append(const ris_cache4 *cache, ris_pack_t pack, const voi
     if (start != nullptr && (!aligned(start, 4) || start == cache->length))
         return fail(RIS_ERR_INVALID, "start is misaligned or the cache's own lengths (pass NULL for those)");
     if (pack->q_total == 0) {
-        if (start != nullptr) RIS_CUDA(cudaMemcpyAsync(cache->length, start, sizeof(int32_t) * cache->batch, cudaMemcpyDeviceToDevice, reinterpret_cast<cudaStream_t>(stream)));
+        if (start != nullptr) RIS_CUDA(launch_cache4_start(cache_args(cache), start, reinterpret_cast<cudaStream_t>(stream)));
         return RIS_OK;
     }
     RIS_TRY(check_ptr(k, "k"));
