@@ -16,8 +16,8 @@
 // through to the end, TMEM is released and the CTA returns.
 //
 // Where a sequence's values of a KV head are not all finite (0 times an infinity is not 0, and a product over a tile multiplies
-// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the values as given: one warp per row
-// over exactly the keys it sees.
+// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the values as given, on the FP32
+// pipe, each over exactly the keys it sees.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -131,48 +131,117 @@ __device__ __forceinline__ void store_row(const PackedArgs &a, int h, int64_t ro
     if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l);
 }
 
-// Rows from the values as given: rows row .. row + BM - 1 of the item, warp `warp` of `warps` taking every warps-th, over the
-// keys that each sees. Outputs only: a row's maximum and sum do not depend on the values.
+// Rows from the values as given: rows row .. row + BM - 1 of the item on the FP32 pipe, warp `warp` of `warps` four of them at a
+// time over the keys that each sees (a lane per key for the scores, per channels for the outputs), through kGivenFloats of
+// shared memory per warp. Outputs only: a row's maximum and sum do not depend on the values. 8,192 tokens of one prompt, one of two
+// KV heads so: 8.3 ms (eight rows 5.5, but the row tiles then took 1.5 % more for their registers; a row by itself 120).
+constexpr int kGivenRows = 4;
+template <int D>
+constexpr int kGivenFloats = kGivenRows * D + 32 * kGivenRows;
 template <int DT, typename TOut>
-__device__ __noinline__ void rows_one_by_one(const PackedArgs &a, const PackItem &it, int row, int h, int warp, int warps)
+__device__ __noinline__ void rows_as_given(const PackedArgs &a, const PackItem &it, int row, int h, int warp, int warps, float *mem)
 {
-    constexpr int C = DT / 32;
-    const int lane = threadIdx.x & 31, g = h / a.G;
+    constexpr int R = kGivenRows, C = DT / 32;
+    const int lane = threadIdx.x & 31, g = h / a.G, shift = it.k_len - it.q_len;
     const __nv_bfloat16 *k = reinterpret_cast<const __nv_bfloat16 *>(a.k) + (int64_t)it.k_base * a.k_stride + g * DT;
-    const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(a.v) + (int64_t)it.k_base * a.v_stride + g * DT;
-    for (int i = row + warp; i < min(row + BM, it.q_len); i += warps) {
-        const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) + (int64_t)(it.q_base + i) * a.q_stride + h * DT;
-        const int n = min(it.k_len, i + it.k_len - it.q_len + 1);
-        float m = -INFINITY, l = 0.f, o[C] = {};
+    const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(a.v) + (int64_t)it.k_base * a.v_stride + g * DT + C * lane;
+    float *const qs = mem + warp * kGivenFloats<DT>, *const ps = qs + R * DT;  // [row][channel], [key][row]
+    auto value = [](uint32_t w, int e) { return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16)); };
+    for (int i0 = row + R * warp; i0 < min(row + BM, it.q_len); i0 += R * warps) {
+        const int rows = min(R, it.q_len - i0);
+        __syncwarp();
+        for (int t = lane; t < R * DT / 8; t += 32) {
+            const int r = t / (DT / 8), d = t % (DT / 8) * 8;
+            const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) + (int64_t)(it.q_base + i0 + min(r, rows - 1)) * a.q_stride + h * DT + d;
+            const uint4 x = *reinterpret_cast<const uint4 *>(q);
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) qs[r * DT + d + e] = value(w[e >> 1], e);
+        }
+        __syncwarp();
+        float m[R], l[R], o[R][C];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            m[r] = -INFINITY, l[r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[r][c] = 0.f;
+        }
+        const int n = min(it.k_len, i0 + rows + shift);  // keys that the last of the rows sees
         for (int j0 = 0; j0 < n; j0 += 32) {
             const int j = j0 + lane;
-            float s = -INFINITY;
-            if (j < n) {
-                s = 0.f;
-                for (int d = 0; d < DT; ++d) s = fmaf(__bfloat162float(q[d]), __bfloat162float(k[j * a.k_stride + d]), s);
-                s *= a.scale_log2;
+            const __nv_bfloat16 *kj = k + (int64_t)min(j, n - 1) * a.k_stride;
+            float s[R] = {};
+#pragma unroll 2
+            for (int d = 0; d < DT; d += 8) {
+                const uint4 x = *reinterpret_cast<const uint4 *>(kj + d);
+                const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float4 qa = *reinterpret_cast<const float4 *>(qs + r * DT + d), qb = *reinterpret_cast<const float4 *>(qs + r * DT + d + 4);
+                    s[r] = fmaf(qa.x, value(w[0], 0), fmaf(qa.y, value(w[0], 1), fmaf(qa.z, value(w[1], 0), fmaf(qa.w, value(w[1], 1), s[r]))));
+                    s[r] = fmaf(qb.x, value(w[2], 0), fmaf(qb.y, value(w[2], 1), fmaf(qb.z, value(w[3], 0), fmaf(qb.w, value(w[3], 1), s[r]))));
+                }
             }
-            const float nm = fmaxf(m, warp_max(s)), ref = nm == -INFINITY ? 0.f : nm;
-            const float p = exp2f(s - ref), al = exp2f(m - ref);
-            m = nm;
-            l = fmaf(l, al, warp_sum(j < n ? p : 0.f));
+            float p[R];
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] *= al;
-            for (int e = 0; e < min(32, n - j0); ++e) {
-                const float pe = __shfl_sync(0xFFFFFFFFu, p, e);
+            for (int r = 0; r < R; ++r) {
+                const float x = r < rows && j <= i0 + r + shift ? s[r] * a.scale_log2 : -INFINITY;
+                const float nm = fmaxf(m[r], warp_max(x)), ref = nm == -INFINITY ? 0.f : nm, al = exp2f(m[r] - ref);
+                p[r] = exp2f(x - ref);
+                m[r] = nm;
+                l[r] = fmaf(l[r], al, p[r]);  // this lane's part of the row's sum
 #pragma unroll
-                for (int c = 0; c < C; ++c) o[c] = fmaf(pe, __bfloat162float(v[(j0 + e) * a.v_stride + lane + 32 * c]), o[c]);
+                for (int c = 0; c < C; ++c) o[r][c] *= al;
             }
-        }
-        const int64_t r = it.q_base + i;
-        TOut *out = reinterpret_cast<TOut *>(a.out) + (r * a.Hq + h) * DT;
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const float x = l == 0.f ? 0.f : o[c] / l;
-            if constexpr (sizeof(TOut) == 4)
-                out[lane + 32 * c] = x;
+            for (int r = 0; r < R; r += 4) *reinterpret_cast<float4 *>(ps + lane * R + r) = make_float4(p[r], p[r + 1], p[r + 2], p[r + 3]);
+            __syncwarp();
+            // (a row takes only the keys that it sees: 0 times an infinity or NaN in a key's place is not 0)
+            auto add = [&](auto whole) {
+#pragma unroll 4
+                for (int e = 0; e < 32; ++e) {
+                    if (!decltype(whole)::value && j0 + e >= n) break;
+                    const __nv_bfloat16 *ve = v + (int64_t)(j0 + e) * a.v_stride;
+                    uint32_t w[C / 2];
+                    if constexpr (C == 4) {
+                        const uint2 x = *reinterpret_cast<const uint2 *>(ve);
+                        w[0] = x.x, w[1] = x.y;
+                    } else {
+                        w[0] = *reinterpret_cast<const uint32_t *>(ve);
+                    }
+                    float pe[R];
+#pragma unroll
+                    for (int r = 0; r < R; r += 4) {
+                        const float4 x = *reinterpret_cast<const float4 *>(ps + e * R + r);
+                        pe[r] = x.x, pe[r + 1] = x.y, pe[r + 2] = x.z, pe[r + 3] = x.w;
+                    }
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        if (!decltype(whole)::value && (r >= rows || j0 + e > i0 + r + shift)) continue;
+#pragma unroll
+                        for (int c = 0; c < C; ++c) o[r][c] = fmaf(pe[r], value(w[c / 2], c), o[r][c]);
+                    }
+                }
+            };
+            if (rows == R && j0 + 31 <= i0 + shift)
+                add(std::true_type{});
             else
-                out[lane + 32 * c] = __float2bfloat16_rn(x);
+                add(std::false_type{});
+            __syncwarp();
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float sum = warp_sum(l[r]);
+            if (r >= rows) continue;
+            TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + i0 + r) * a.Hq + h) * DT + C * lane;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const float x = sum == 0.f ? 0.f : o[r][c] / sum;
+                if constexpr (sizeof(TOut) == 4)
+                    out[c] = x;
+                else
+                    out[c] = __float2bfloat16_rn(x);
+            }
         }
     }
 }
@@ -287,7 +356,7 @@ struct Lay128 {
 // at 12 / 2 heads: 1.96 ms, 1.68 PFLOP/s (cuBLAS 1.89 in a burst and 1.70 under the power limit), the pipe 87 % busy from the
 // first CTA to the last.
 template <typename TOut>
-__global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+__global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant__ PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
     using L = Lay128;
     constexpr int NSK = L::NSK, NSV = L::NSV, DT = 128;
@@ -632,7 +701,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const PackedArgs a, c
                 __syncwarp();
                 rows_out<OC, TOut>(stage, out, (int64_t)a.Hq * DT, it.q_len - w0);
             } else {
-                rows_one_by_one<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps);
+                // (through the rings, as the outputs' way above)
+                static_assert(kSoftmaxWarps * kGivenFloats<DT> * 4 <= L::OFF_Q, "the rings hold every warp's part");
+                rows_as_given<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps, reinterpret_cast<float *>(smem));
             }
         }
     }
@@ -739,13 +810,13 @@ struct Units {
 
 // The units of this CTA whose rows are to be computed from the values as given.
 template <int D, typename TOut>
-__device__ __noinline__ void units_as_given(const PackedArgs &a, int warp)
+__device__ __noinline__ void units_as_given(const PackedArgs &a, int warp, float *mem)
 {
     Units units{(int64_t)a.n_items * a.Hq, -1};
     PackItem it;
     int h;
     while (units.next(a, it, h))
-        if (it.k_len > 0 && !(a.v_top[(int64_t)it.seq * a.Hkv + h / a.G] < INFINITY)) rows_one_by_one<D, TOut>(a, it, it.row, h, warp, kGroupWarps);
+        if (it.k_len > 0 && !(a.v_top[(int64_t)it.seq * a.Hkv + h / a.G] < INFINITY)) rows_as_given<D, TOut>(a, it, it.row, h, warp, kGroupWarps, mem);
 }
 
 // Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
@@ -765,7 +836,7 @@ __device__ __noinline__ void units_as_given(const PackedArgs &a, int warp)
 //   warp 6  S = Q K^T as soon as its columns are free, warp 7 O += P V;
 //   warps 0-3  the softmax, one thread per row.
 template <int D, typename TOut>
-__global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const PackedArgs a, const __grid_constant__ PackedMaps maps)
+__global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __grid_constant__ PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
     using L = LayRows<D>;
     constexpr int NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
@@ -1067,8 +1138,10 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const Pa
             }
             tc_fence_before();  // (O has been read before the next P is announced)
         }
-        // (after everything else: they take far longer than a wait of another role may)
-        if (ok && left) units_as_given<D, TOut>(a, warp);
+        // (after everything else: they take far longer than a wait of another role may; the rings are free by now, as this warp
+        // has seen the end of every product that read them)
+        static_assert(kGroupWarps * kGivenFloats<D> * 4 <= L::OFF_OUT, "the rings hold every warp's part");
+        if (ok && left) units_as_given<D, TOut>(a, warp, reinterpret_cast<float *>(smem));
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) atomicOr(&g_ris_packed_error, 2u);

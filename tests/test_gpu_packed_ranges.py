@@ -90,3 +90,25 @@ def test_values_of_zero():
     ref, _, _ = packed_plain(q, k, v, lens, lens, 1)
     assert (got[:130] == 0).all() and (got[330:389] == 0).all()
     check_bf16_path(to_np(got), ref.numpy(), out_bf16=True)
+
+
+@pytest.mark.parametrize("n,D", [(8192, 128), (2000, 128), (4000, 64)])
+def test_long_prompt_with_a_hidden_value(n, D):
+    """The rows of one KV head from the values as given, for a whole prompt: as from the tiles, in reasonable time."""
+    Hq, Hkv = 4, 2
+    q, k, v = inputs([n], [n], Hq, Hkv, D)
+    y = v.clone()
+    y[n - 1, 0, 3] = 1e12
+    with ris.ris_pack_create([n]) as pack:
+        good, = ris.ris_attention_packed(pack, q, k, v, out_dtype=F32)
+        ris.ris_attention_packed(pack, q, k, y, out_dtype=F32)
+        a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        a.record()
+        got, = ris.ris_attention_packed(pack, q, k, y, out_dtype=F32)
+        b.record()
+        ris.ris_device_status()
+    assert torch.equal(got[:, Hq // Hkv:], good[:, Hq // Hkv:])
+    check_bf16_path(to_np(got[:n - 1]), to_np(good[:n - 1]))
+    # pairs of rows and keys at a tenth of the FP32 pipe's rate, and a tile's own chain of steps (a row by itself took five times as long)
+    pairs = n * (n + 1) / 2 * Hq / Hkv
+    assert a.elapsed_time(b) <= 5.0 + 1e3 * pairs * 4 * D / 7e12
