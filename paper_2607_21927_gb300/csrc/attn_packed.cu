@@ -35,7 +35,7 @@
 
 namespace ris {
 
-// Device error word of this file (bit 1: a bounded wait gave up); read by read_packed_error.
+// Device error word of this file (bit 1: a bounded wait gave up); read by ris_device_status.
 __device__ unsigned int g_ris_packed_error;
 
 namespace {
@@ -1596,13 +1596,6 @@ cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s)
     }
 }
 
-// Read and clear this file's device error word (the caller has synchronised).
-unsigned int read_packed_error()
-{
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_ris_packed_error, sizeof(v)) != cudaSuccess) return 0;
-    if (v != 0) cudaMemcpyToSymbol(g_ris_packed_error, &zero, sizeof(zero));
-    return v;
-}
+cudaError_t packed_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_packed_error); }
 
 }  // namespace ris

@@ -96,7 +96,7 @@
 
 namespace ris {
 
-// Device error word of this kernel (bit 1: a bounded wait gave up); read by read_tile_error.
+// Device error word of this kernel (bit 1: a bounded wait gave up); read by ris_device_status.
 __device__ unsigned int g_ris_tile_error;
 
 namespace {
@@ -1318,14 +1318,7 @@ cudaError_t launch_t(const AttnArgs &a, const TileMaps &maps, cudaStream_t s)
 bool tile_design_available() { return encode_fn() != nullptr; }
 
 
-// Read and clear this kernel's device error word (the caller has synchronised).
-cudaError_t read_tile_error(unsigned int *out)
-{
-    cudaError_t e = cudaMemcpyFromSymbol(out, g_ris_tile_error, sizeof(unsigned int));
-    if (e != cudaSuccess || *out == 0u) return e;
-    const unsigned int zero = 0u;
-    return cudaMemcpyToSymbol(g_ris_tile_error, &zero, sizeof(unsigned int));
-}
+cudaError_t tile_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_tile_error); }
 
 // Q / K / V tensor maps of a call (the low parts only with split queries and keys; the values
 // as fp16). q_hi, q_lo: moved back by a.q_first rows, as the kernels' other row pointers.

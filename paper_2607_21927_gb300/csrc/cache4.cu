@@ -1024,12 +1024,6 @@ cudaError_t launch_cache4_attend(Cache4AttendArgs a, int dtype, int out_dtype, c
     return out_dtype == RIS_F32 ? launch_join<float>(a, s) : launch_join<__nv_bfloat16>(a, s);
 }
 
-unsigned int read_cache4_error()
-{
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_ris_cache4_error, sizeof(v)) != cudaSuccess) return 0;
-    if (v != 0) cudaMemcpyToSymbol(g_ris_cache4_error, &zero, sizeof(zero));
-    return v;
-}
+cudaError_t cache4_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_cache4_error); }
 
 }  // namespace ris

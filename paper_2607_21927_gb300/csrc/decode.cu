@@ -558,13 +558,7 @@ __global__ void __launch_bounds__(kCombineWarps * 32) k_decode_combine(const Dec
 
 }  // namespace
 
-unsigned int read_decode_error()
-{
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_ris_decode_error, sizeof(v)) != cudaSuccess) return 0;
-    if (v != 0) cudaMemcpyToSymbol(g_ris_decode_error, &zero, sizeof(zero));
-    return v;
-}
+cudaError_t decode_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_decode_error); }
 
 // Launch as a programmatic dependent of the previous kernel in the stream: it may be scheduled
 // while that kernel runs and waits for it (griddepcontrol.wait) before touching its results.

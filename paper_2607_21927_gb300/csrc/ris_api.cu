@@ -387,6 +387,19 @@ ris_status validate_attention(const void *q, const void *k, const void *v, void 
 
 namespace ris {
 void set_error_text(const char *msg) { t_err = msg; }
+
+// The error words of the kernels, taken (and cleared) by one small kernel so that ris_device_status needs one copy: four copies, with
+// ten microseconds each, took twice as long as the two there were before the serving kernels.
+constexpr int kErrorWords = 4;
+struct ErrorWords {
+    unsigned int *p[kErrorWords];
+};
+__device__ unsigned int g_ris_error_words[kErrorWords];
+__global__ void k_take_error_words(const ErrorWords at)
+{
+    if (threadIdx.x < kErrorWords) g_ris_error_words[threadIdx.x] = atomicExch(at.p[threadIdx.x], 0u);
+}
+std::mutex g_status_mu;
 int64_t debug_wait_limit() { return g_wait_limit.load(); }
 int32_t debug_no_loads() { return g_tile_no_loads.load(); }
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s)
@@ -918,11 +931,22 @@ int32_t ris_attention_design(ris_mask_t mask, int32_t dtype, int32_t head_dim)
 
 ris_status ris_device_status(void *stream)
 {
-    unsigned int word = 0, tile_word = 0;
-    RIS_CUDA(cudaStreamSynchronize(reinterpret_cast<cudaStream_t>(stream)));
-    RIS_CUDA(read_tile_error(&tile_word));
-    const unsigned int decode_word = read_decode_error(), cache_word = read_cache4_error();
-    word |= tile_word | (cache_word & 4u) | read_packed_error();
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    RIS_CUDA(cudaStreamSynchronize(s));
+    ErrorWords at;
+    RIS_CUDA(tile_error_word(&at.p[0]));
+    RIS_CUDA(packed_error_word(&at.p[1]));
+    RIS_CUDA(cache4_error_word(&at.p[2]));
+    RIS_CUDA(decode_error_word(&at.p[3]));
+    unsigned int w[kErrorWords] = {};
+    {
+        std::lock_guard<std::mutex> lk(g_status_mu);
+        k_take_error_words<<<1, 32, 0, s>>>(at);
+        RIS_CUDA(cudaGetLastError());
+        RIS_CUDA(cudaMemcpyFromSymbolAsync(w, g_ris_error_words, sizeof(w), 0, cudaMemcpyDeviceToHost, s));
+        RIS_CUDA(cudaStreamSynchronize(s));
+    }
+    const unsigned int word = w[0] | w[1] | (w[2] & 4u), cache_word = w[2], decode_word = w[3];
     if (word != 0u) return fail(RIS_ERR_DEVICE_TIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
     if (decode_word != 0u)
         return fail(RIS_ERR_INVALID, "a decode step read a position outside [t0, cache_len) from t_dev");

@@ -170,8 +170,8 @@ cudaError_t launch_mask_fill(const MaskFillArgs &a, cudaStream_t s);
 
 // Decode step: partial softmax per (chunk, KV head), then one combine per query head.
 cudaError_t launch_decode(const DecodeArgs &a, int dtype, int out_dtype, cudaStream_t s);
-// Reads and clears the decode error word (bit 1: a step's device-side t was out of range).
-unsigned int read_decode_error();
+// The decode error word on the current device (bit 1: a step's device-side t was out of range).
+cudaError_t decode_error_word(unsigned int **p);
 
 // dtype_in / dtype_out are ris_dtype values.
 cudaError_t launch_rope(const RopeArgs &a, int dtype_in, int dtype_out, cudaStream_t s);
@@ -229,6 +229,7 @@ cudaError_t launch_attention_tile(const AttnArgs &a, int D, const void *q_hi, co
                                   bool dense, cudaStream_t s);
 // The suffix pass of the dense-suffix split (a.part_o set): writes a.part_o / a.part_lse.
 cudaError_t launch_attention_tile_suffix(const AttnArgs &a, int D, const void *q_hi, const void *q_lo, cudaStream_t s);
-cudaError_t read_tile_error(unsigned int *out);
+// The tile kernel's error word on the current device (a bounded wait gave up).
+cudaError_t tile_error_word(unsigned int **p);
 
 }  // namespace ris

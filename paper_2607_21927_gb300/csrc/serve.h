@@ -143,10 +143,10 @@ struct Cache4EvictArgs {
 // holes: scratch [B * Hkv][budget]
 cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaStream_t s);
 
-// Reads and clears the error word of the cache's kernels (bit 1: tokens appended past the capacity).
-unsigned int read_cache4_error();
-// Reads and clears the error word of the packed attention's tile kernels (a bounded wait gave up).
-unsigned int read_packed_error();
+// The device error words of the cache's kernels (bit 1: tokens appended past the capacity, bit 2: a bounded wait gave up) and of
+// the packed attention's tile kernels (a bounded wait gave up), on the current device.
+cudaError_t cache4_error_word(unsigned int **p);
+cudaError_t packed_error_word(unsigned int **p);
 
 // What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked; whether loads are left out.
 int64_t debug_wait_limit();
