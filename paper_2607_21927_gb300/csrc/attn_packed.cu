@@ -52,9 +52,9 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
 // registers per thread: at launch, then after setmaxnreg of a softmax and of a loader / MMA thread
 constexpr int kRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(2 * kSoftmaxRegs + kOtherRegs == 3 * kRegs, "the shares of the three warpgroups add up to the launch's");
-// The reference maximum of a row moves only when its maximum grows by more than this (log2), so P
-// stays below 2^8.
-constexpr float kLazyLog2 = 8.f;
+// The reference m of a row moves only when its maximum grows by more than kLazyLog2. P = 2^(s - m + kAboveLog2) stays below 2^15 and
+// keeps fp16's 11 bits down to 2^-21 of the reference: rows whose weight goes to one key with next to no value are made of such.
+constexpr float kLazyLog2 = 7.f, kAboveLog2 = 7.f;
 constexpr uint32_t kTmemCols = 512;
 
 // Exponent E of the values' scale 2^-E: the largest magnitude lands in [2^13, 2^14).
@@ -88,11 +88,11 @@ __device__ __forceinline__ float row_max(const float (&sv)[BN])
     }
     return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
 }
-// P = 2^(s sc - mu) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the weights before they are rounded
+// P = 2^(s sc - mu + kAboveLog2) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the weights before they are rounded
 template <int C0 = 0, int C1 = BN>
 __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, float mu, uint32_t (&hw)[BN / 2])
 {
-    const uint64_t sc2 = f2_pack(sc, sc), nmu2 = f2_pack(-mu, -mu);
+    const uint64_t sc2 = f2_pack(sc, sc), nmu2 = f2_pack(kAboveLog2 - mu, kAboveLog2 - mu);
     uint64_t sum[2] = {0, 0};
 #pragma unroll
     for (int w = C0 / 2; w < C1 / 2; ++w) {
@@ -349,7 +349,7 @@ struct Lay128 {
 //   warps 0-7       two groups of four warps, one thread per row in each, on alternate key tiles:
 //                   scores from TMEM, causal cut (only where a warp's rows end inside the tile), maximum, fp32 online
 //                   softmax from the reference maximum that the other group hands over, O rescaled in
-//                   TMEM only when the maximum grew by more than 2^8, P into TMEM.
+//                   TMEM only when the maximum grew by more than 2^7, P into TMEM.
 // TMEM: S 2 x 128 columns, O 128, P 2 x 64: all 512.
 //
 // Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles. One prompt of 32,768 tokens
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
             const float m_fin = n_kt == 0 ? -INFINITY : ((n_kt - 1) & 1) ? mb.x : ma.x;
             const float lt = (ma.x == m_fin ? ma.y : ma.y * exp2f(ma.x - m_fin)) +
                              (mb.x == m_fin ? mb.y : mb.y * exp2f(mb.x - m_fin));
-            if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin, lt);
+            if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin - kAboveLog2, lt);
             // fp16 values were scaled by 2^-E for the value product
             if (v_top < INFINITY) {
                 const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_top)) / lt;
@@ -1100,7 +1100,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
             }
             if (ok && x.n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
             if (!ok) break;
-            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m, l);
+            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m - kAboveLog2, l);
             if (x.n > 0 && !(v_top < INFINITY)) {
                 left = true;
                 tc_fence_before();

@@ -127,3 +127,17 @@ def test_groups_of_zeros():
     v[0, :800, 0, 64:96] = 0.0
     for out in (F32, BF16):
         check(cache_of(k, v, [n]), randn(1, 4, D, seed=3, dtype=BF16, scale=2.0), [n], out)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("out", [F32, BF16])
+@pytest.mark.parametrize("size", [1e2, 1e4])
+def test_scores_of_millions(D, out, size):
+    """Each output is its best slot's value: fp32 scores of up to 1e9 stand further apart than they are off."""
+    n = 3000
+    k, v = randn(1, 3008, 1, D, seed=1) * size, randn(1, 3008, 1, D, seed=2)
+    cache, q = cache_of(k, v, [n]), (randn(1, 4, D, seed=3) * size).to(BF16)
+    got = ris.ris_cache4_attend(cache, q, out_dtype=out)
+    ris.ris_device_status()
+    ref, _, _ = attend_plain(cache, q, [n])
+    assert ((got.double().cpu() - ref).abs() <= 2.0 ** -8 * ref.abs() + 1e-6).all()

@@ -7,7 +7,7 @@ the largest value that the row sees. Rows of other sequences and of other KV hea
 import pytest
 import torch
 
-from helpers import check_bf16_path, to_np
+from helpers import check_bf16_path, rel_l2, to_np
 from paper_2607_21927_gb300 import ris
 from test_gpu_serving import BF16, F32, INF, LONG_KEYS, packed_plain, randn
 
@@ -112,3 +112,31 @@ def test_long_prompt_with_a_hidden_value(n, D):
     # pairs of rows and keys at a tenth of the FP32 pipe's rate, and a tile's own chain of steps (a row by itself took five times as long)
     pairs = n * (n + 1) / 2 * Hq / Hkv
     assert a.elapsed_time(b) <= 5.0 + 1e3 * pairs * 4 * D / 7e12
+
+
+@pytest.mark.parametrize("n,m", [([1500], [1500]), ([300, 40], [6000, 5000])])
+@pytest.mark.parametrize("Hq,Hkv,D", [(6, 2, 128), (4, 2, 64)])
+@pytest.mark.parametrize("nats", [8.0, 14.0, 17.0])
+def test_key_that_takes_nearly_all_weight_with_values_of_zero(n, m, Hq, Hkv, D, nats):
+    """The first key of each sequence stands `nats` above the others and holds zeros: the outputs are what the others add, each a
+    small part of the row's weight. Outputs by themselves at the bf16 path's bar, whatever their size: relative L2 5e-3."""
+    q, k, v = inputs(n, m, Hq, Hkv, D)
+    q, k = (q.float() * 0.3).to(BF16), (k.float() * 0.3).to(BF16)
+    q[..., 0] = 4.0
+    k[..., 0] = 0.0
+    at = 0
+    for x in m:
+        k[at, :, 0] = nats * D ** 0.5 / 4.0
+        v[at] = 0.0
+        at += x
+    with ris.ris_pack_create(n, m) as pack:
+        got, lse = ris.ris_attention_packed(pack, q, k, v, out_dtype=F32, return_lse=True)
+        ris.ris_device_status()
+    ref, rl, _ = packed_plain(q, k, v, n, m, 1)
+    at = 0
+    for x, y in zip(n, m):
+        first = max(0, 64 - (y - x))  # (rows of few keys are all their own)
+        for h in range(Hq):
+            assert rel_l2(to_np(got[at + first:at + x, h]), ref[at + first:at + x, h].numpy()) <= 5e-3
+        at += x
+    assert ((lse.double().cpu() - rl).abs() <= 2e-5 * (1 + rl.abs())).all()
