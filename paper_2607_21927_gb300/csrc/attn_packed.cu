@@ -16,8 +16,8 @@
 // through to the end, TMEM is released and the CTA returns.
 //
 // Where a sequence's values of a KV head are not all finite (0 times an infinity is not 0, and a product over a tile multiplies
-// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the values as given, on the FP32
-// pipe, each over exactly the keys it sees.
+// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the inputs as given, on the FP32
+// pipe, each over exactly the keys it sees; and so are rows of scores too large for P's range.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -55,6 +55,9 @@ static_assert(2 * kSoftmaxRegs + kOtherRegs == 3 * kRegs, "the shares of the thr
 // The reference m of a row moves only when its maximum grows by more than kLazyLog2. P = 2^(s - m + kAboveLog2) stays below 2^15 and
 // keeps fp16's 11 bits down to 2^-21 of the reference: rows whose weight goes to one key with next to no value are made of such.
 constexpr float kLazyLog2 = 7.f, kAboveLog2 = 7.f;
+// P's exponent is rounded once, the maximum behind m was rounded as a product: up to here they agree well enough for P's bound. Rows
+// that pass it (no model's do) are computed on the FP32 pipe, where products are rounded alike.
+constexpr float kFarLog2 = 0x1p23f;
 constexpr uint32_t kTmemCols = 512;
 
 // Exponent E of the values' scale 2^-E: the largest magnitude lands in [2^13, 2^14).
@@ -125,30 +128,44 @@ __device__ __forceinline__ void store16(void *dst, const float *x)
 }
 
 // A row's softmax as the other outputs: log-sum-exp, and (maximum, 1 / sum) for the key weights.
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : l; }
 __device__ __forceinline__ void store_row(const PackedArgs &a, int h, int64_t row, float m, float l)
 {
     if (a.lse != nullptr) a.lse[h * a.q_total + row] = (m + log2f(l)) * kLn2;
-    if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l);
+    if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, inverse_sum(l));
+}
+// The same of a row that is computed from the inputs as given: the key weights take their scores from tiles, so the maximum that
+// goes with them is the tiles' own (`top`), and only the sum the row's.
+__device__ __forceinline__ void store_top(const PackedArgs &a, int h, int64_t row, float top)
+{
+    if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row].x = top;
+}
+__device__ __forceinline__ void store_given(const PackedArgs &a, int h, int64_t row, float m, float l)
+{
+    if (a.lse != nullptr) a.lse[h * a.q_total + row] = (m + log2f(l)) * kLn2;
+    if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row].y = inverse_sum(l);
 }
 
-// Rows from the values as given: rows row .. row + BM - 1 of the item on the FP32 pipe, warp `warp` of `warps` four of them at a
-// time over the keys that each sees (a lane per key for the scores, per channels for the outputs), through kGivenFloats of
-// shared memory per warp. Outputs only: a row's maximum and sum do not depend on the values. 8,192 tokens of one prompt, one of two
-// KV heads so: 8.3 ms (eight rows 5.5, but the row tiles then took 1.5 % more for their registers; a row by itself 120).
+// Rows on the FP32 pipe from the inputs as given: kGivenRows of them from i0 on, then those `step` later, up to row i1 of the
+// item's sequence, by one warp over the keys that each sees (a lane per key for the scores, per channels for the outputs), through
+// kGivenFloats of shared memory. With `stats` the other outputs too, else those of the tiles stand: a row's maximum and sum do not
+// depend on the values. 8,192 tokens of one prompt, one of two KV heads so: 8.3 ms (eight rows together 5.5, but the row
+// tiles then took 1.5 % more for their registers; a row by itself 120).
 constexpr int kGivenRows = 4;
 template <int D>
 constexpr int kGivenFloats = kGivenRows * D + 32 * kGivenRows;
 template <int DT, typename TOut>
-__device__ __noinline__ void rows_as_given(const PackedArgs &a, const PackItem &it, int row, int h, int warp, int warps, float *mem)
+__device__ __noinline__ void rows_as_given(const PackedArgs &a, const PackItem &it, int i0, int i1, int step, int h, float *mem, bool stats)
 {
     constexpr int R = kGivenRows, C = DT / 32;
     const int lane = threadIdx.x & 31, g = h / a.G, shift = it.k_len - it.q_len;
     const __nv_bfloat16 *k = reinterpret_cast<const __nv_bfloat16 *>(a.k) + (int64_t)it.k_base * a.k_stride + g * DT;
     const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(a.v) + (int64_t)it.k_base * a.v_stride + g * DT + C * lane;
-    float *const qs = mem + warp * kGivenFloats<DT>, *const ps = qs + R * DT;  // [row][channel], [key][row]
+    float *const qs = mem, *const ps = qs + R * DT;  // [row][channel], [key][row]
     auto value = [](uint32_t w, int e) { return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16)); };
-    for (int i0 = row + R * warp; i0 < min(row + BM, it.q_len); i0 += R * warps) {
-        const int rows = min(R, it.q_len - i0);
+    i1 = min(i1, it.q_len);
+    for (; i0 < i1; i0 += step) {
+        const int rows = min(R, i1 - i0);
         __syncwarp();
         for (int t = lane; t < R * DT / 8; t += 32) {
             const int r = t / (DT / 8), d = t % (DT / 8) * 8;
@@ -185,7 +202,7 @@ __device__ __noinline__ void rows_as_given(const PackedArgs &a, const PackItem &
             float p[R];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float x = r < rows && j <= i0 + r + shift ? s[r] * a.scale_log2 : -INFINITY;
+                const float x = r < rows && j <= i0 + r + shift ? __fmul_rn(s[r], a.scale_log2) : -INFINITY;
                 const float nm = fmaxf(m[r], warp_max(x)), ref = nm == -INFINITY ? 0.f : nm, al = exp2f(m[r] - ref);
                 p[r] = exp2f(x - ref);
                 m[r] = nm;
@@ -233,6 +250,7 @@ __device__ __noinline__ void rows_as_given(const PackedArgs &a, const PackItem &
         for (int r = 0; r < R; ++r) {
             const float sum = warp_sum(l[r]);
             if (r >= rows) continue;
+            if (stats && lane == 0) store_given(a, h, it.q_base + i0 + r, m[r], sum);
             TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + i0 + r) * a.Hq + h) * DT + C * lane;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
@@ -315,7 +333,8 @@ struct Lay128 {
     static constexpr int OFF_END = OFF_TMEM + 4;     // ClosingNotes
     static constexpr int OFF_M = OFF_BARS + 256;     // float [BM]
     static constexpr int OFF_ML = OFF_M + BM * 4;    // float2 [2][BM]
-    static constexpr int BYTES = OFF_ML + 2 * BM * 8;
+    static constexpr int OFF_TOP = OFF_ML + 2 * BM * 8;  // float [2][BM]
+    static constexpr int BYTES = OFF_TOP + 2 * BM * 4;
     static_assert(BYTES <= 232448 && OFF_END + (int)sizeof(ClosingNotes) <= OFF_M, "shared memory of a CTA");
     // Barriers, one of each kind per ring stage or buffer, so that no waiter can fall two phases behind a
     // barrier it polls by parity:
@@ -349,7 +368,7 @@ struct Lay128 {
 //   warps 0-7       two groups of four warps, one thread per row in each, on alternate key tiles:
 //                   scores from TMEM, causal cut (only where a warp's rows end inside the tile), maximum, fp32 online
 //                   softmax from the reference maximum that the other group hands over, O rescaled in
-//                   TMEM only when the maximum grew by more than 2^7, P into TMEM.
+//                   TMEM only when the maximum grew by more than 2^8, P into TMEM.
 // TMEM: S 2 x 128 columns, O 128, P 2 x 64: all 512.
 //
 // Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles. One prompt of 32,768 tokens
@@ -365,6 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
     uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
     float *const m_sh = reinterpret_cast<float *>(smem + L::OFF_M);
     float2(*const ml_sh)[BM] = reinterpret_cast<float2(*)[BM]>(smem + L::OFF_ML);
+    float(*const top_sh)[BM] = reinterpret_cast<float(*)[BM]>(smem + L::OFF_TOP);
     volatile ClosingNotes *const notes = reinterpret_cast<ClosingNotes *>(smem + L::OFF_END);
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -584,6 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
         const int last_key = q0 + r + shift;          // last key that the row sees
         const int warp_sees = q0 + wq * 32 + shift;   // that every row of the warp sees (and those past the sequence's end)
         float l = 0.f, m_own = -INFINITY;  // row sum over this thread's tiles, relative to 2^m_own
+        float far = 0.f, top = -INFINITY;  // largest magnitude of m; largest score
         bool s_full = false;  // seen at the end of the last tile: a poll takes 200 cycles even if it succeeds
         for (int j = grp; j < n_kt; j += 2) {
             if (ok) {
@@ -611,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
 #pragma unroll
                 for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
             }
-            const float mx = row_max(sv) * sc;  // (the scale is positive)
+            const float mx = __fmul_rn(row_max(sv), sc);  // (the scale is positive)
             // The row's reference maximum moves on from tile to tile, handed to the other group. It moves, and
             // O is rescaled, only when the row max grows by more than kLazyLog2. The TMEM loads / stores are
             // warp-collective, so the whole warp runs them when any of its rows needs it.
@@ -621,7 +642,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
                 m_prev = m_sh[r];
             }
             const bool upd = mx > m_prev + kLazyLog2;
-            const float m_ref = upd ? mx : m_prev;
+            const float m_ref = upd ? mx : m_prev, mu = m_ref == -INFINITY ? 0.f : m_ref;
             // the value product of tile t is done (t < 0: nothing to wait for)
             auto pv_done = [&](int t) -> bool {
                 const uint32_t bar = sbase + BAR(L::B_PV_DONE + t % NSV);
@@ -630,12 +651,14 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
             const bool scale_o = upd && m_prev != -INFINITY;
             const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
             const float al = scale_o ? exp2f(m_prev - m_ref) : 1.f;
+            far = fmaxf(far, fabsf(mu));
+            top = fmaxf(top, mx);
             if (m_ref != m_own) {
                 l *= m_own == -INFINITY ? 0.f : exp2f(m_own - m_ref);
                 m_own = m_ref;
             }
             uint32_t hw[BN / 2];
-            const float lsum = weights_of(sv, sc, m_ref == -INFINITY ? 0.f : m_ref, hw);
+            const float lsum = weights_of(sv, sc, mu, hw);
             // Only now on to the other group: its exponentials (the other warp of this scheduler) run
             // while this warp stores P and takes the next tile's scores and maximum, and not
             // against this warp's own
@@ -679,7 +702,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
             if (lane == 0) arrive_lead(L::B_P_GO + j % NSV);
         }
         // the row's maximum and sum from both threads
-        ml_sh[grp][r] = make_float2(m_own, l);
+        top_sh[grp][r] = top;
+        ml_sh[grp][r] = make_float2(m_own, far > kFarLog2 && far < INFINITY ? INFINITY : l);  // (no sum of weights is infinite)
         ok = !pair_or(9 + wq, !ok);
         for (int t = max(0, n_kt - 2); t < n_kt && ok; ++t)  // in order, as above
             ok = __all_sync(0xFFFFFFFFu, mbar_wait<2>(sbase + BAR(L::B_PV_DONE + t % NSV), (t / NSV) & 1, gave_up));
@@ -690,9 +714,15 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
             const float m_fin = n_kt == 0 ? -INFINITY : ((n_kt - 1) & 1) ? mb.x : ma.x;
             const float lt = (ma.x == m_fin ? ma.y : ma.y * exp2f(ma.x - m_fin)) +
                              (mb.x == m_fin ? mb.y : mb.y * exp2f(mb.x - m_fin));
-            if (grp == 0 && q0 + r < it.q_len) store_row(a, h, it.q_base + q0 + r, m_fin - kAboveLog2, lt);
+            const bool too_far = __any_sync(0xFFFFFFFFu, ma.y == INFINITY || mb.y == INFINITY);
+            if (grp == 0 && q0 + r < it.q_len) {
+                if (too_far)
+                    store_top(a, h, it.q_base + q0 + r, fmaxf(top_sh[0][r], top_sh[1][r]));
+                else
+                    store_row(a, h, it.q_base + q0 + r, m_fin - kAboveLog2, lt);
+            }
             // fp16 values were scaled by 2^-E for the value product
-            if (v_top < INFINITY) {
+            if (v_top < INFINITY && !too_far) {
                 const float inv = lt == 0.f ? 0.f : pow2i(value_exp(v_top)) / lt;
                 const int w0 = q0 + 32 * wq;  // the warp's first row
                 TOut *out = reinterpret_cast<TOut *>(a.out) + ((int64_t)(it.q_base + w0) * a.Hq + h) * DT + OC * grp;
@@ -703,7 +733,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
             } else {
                 // (through the rings, as the outputs' way above)
                 static_assert(kSoftmaxWarps * kGivenFloats<DT> * 4 <= L::OFF_Q, "the rings hold every warp's part");
-                rows_as_given<DT, TOut>(a, it, q0, h, warp, kSoftmaxWarps, reinterpret_cast<float *>(smem));
+                // (the pair of warps takes its own 32 rows)
+                rows_as_given<DT, TOut>(a, it, q0 + 32 * wq + kGivenRows * grp, q0 + 32 * wq + 32, 2 * kGivenRows, h,
+                                        reinterpret_cast<float *>(smem) + warp * kGivenFloats<DT>, too_far);
             }
         }
     }
@@ -785,7 +817,7 @@ struct UnitInfo {
     int n;                  // key tiles, -1: no more units
     int h, row, shift;      // head; first row; key j is seen by row i when j <= i + shift
     int q_base, q_len, k_base, k_len;
-    int64_t top;            // its place in v_top
+    int64_t id, top;        // its number; its place in v_top
 };
 static_assert(sizeof(UnitInfo) <= 64, "the ring's slots");
 
@@ -794,7 +826,7 @@ static_assert(sizeof(UnitInfo) <= 64, "the ring's slots");
 struct Units {
     int64_t total;
     int round;
-    __device__ __forceinline__ bool next(const PackedArgs &a, PackItem &it, int &h)
+    __device__ __forceinline__ bool next(const PackedArgs &a, PackItem &it, int &h, int64_t &id)
     {
         for (;;) {
             const int64_t base = (int64_t)++round * gridDim.x;
@@ -803,20 +835,28 @@ struct Units {
             if (u >= total) continue;
             it = a.items[(int)u / a.Hq];
             h = (int)u % a.Hq;
+            id = u;
             return true;
         }
     }
 };
 
-// The units of this CTA whose rows are to be computed from the values as given.
+// The rows of this CTA's units that are to be computed from the inputs as given: all of a unit's where the values ask for it, a
+// warp's own 32 where their scores did (a.far).
 template <int D, typename TOut>
 __device__ __noinline__ void units_as_given(const PackedArgs &a, int warp, float *mem)
 {
     Units units{(int64_t)a.n_items * a.Hq, -1};
     PackItem it;
     int h;
-    while (units.next(a, it, h))
-        if (it.k_len > 0 && !(a.v_top[(int64_t)it.seq * a.Hkv + h / a.G] < INFINITY)) rows_as_given<D, TOut>(a, it, it.row, h, warp, kGroupWarps, mem);
+    int64_t id;
+    while (units.next(a, it, h, id)) {
+        if (it.k_len <= 0) continue;
+        const bool far = a.far[id * kGroupWarps + warp] != 0;
+        if (far) rows_as_given<D, TOut>(a, it, it.row + 32 * warp, it.row + 32 * warp + 32, kGivenRows, h, mem, true);
+        if (!(a.v_top[(int64_t)it.seq * a.Hkv + h / a.G] < INFINITY))
+            rows_as_given<D, TOut>(a, it, it.row + kGivenRows * warp, it.row + BM, kGivenRows * kGroupWarps, h, mem, false);
+    }
 }
 
 // Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
@@ -888,14 +928,15 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
                 for (int u = 0; more && ok; ++u) {
                     PackItem it;
                     int h = 0, n = -1;
-                    more = units.next(a, it, h);
+                    int64_t id = 0;
+                    more = units.next(a, it, h, id);
                     if (u >= NI) ok = mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up);
                     if (!ok) break;
                     UnitInfo &x = *reinterpret_cast<UnitInfo *>(smem + L::OFF_INFO + u % NI * 64);
                     if (more) {
                         const int shift = it.k_len - it.q_len;
                         n = (max(0, min(it.k_len, min(it.q_len, it.row + BM) + shift)) + BN - 1) / BN;  // tiles that the rows see
-                        x = UnitInfo{n, h, it.row, shift, it.q_base, it.q_len, it.k_base, it.k_len, (int64_t)it.seq * a.Hkv + h / a.G};
+                        x = UnitInfo{n, h, it.row, shift, it.q_base, it.q_len, it.k_base, it.k_len, id, (int64_t)it.seq * a.Hkv + h / a.G};
                     } else {
                         x.n = -1;
                     }
@@ -1022,7 +1063,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
         bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
         if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
         values_ready();
-        bool left = false;  // units whose rows are to be computed from the values as given
+        bool left = false;  // units of whose rows some are to be computed from the inputs as given
         for (int u = 0; ok; ++u) {
             UnitInfo x;
             ok = __all_sync(0xFFFFFFFFu, unit(u, x));
@@ -1032,7 +1073,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
             float v_top;  // (on its way from here on: it is asked for at the unit's end; undefined without keys)
             asm volatile("ld.global.f32 %0, [%1];" : "=f"(v_top) : "l"(a.v_top + x.top));
             const int last_key = x.row + r + x.shift, warp_sees = x.row + warp * 32 + x.shift;
-            float l = 0.f, m = -INFINITY;
+            float l = 0.f, m = -INFINITY, far = 0.f, top = -INFINITY;  // row sum, reference, its largest magnitude, largest score
             for (int j = 0; j < x.n; ++j, ++t) {
                 // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
                 if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL, t & 1);
@@ -1058,7 +1099,7 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
 #pragma unroll
                     for (int e = 0; e < BN; ++e) drop_unless(sv[e], cw[e >> 5], 1u << (e & 31));
                 }
-                const float mx = row_max(sv) * sc;
+                const float mx = __fmul_rn(row_max(sv), sc);
                 const bool upd = mx > m + kLazyLog2;
                 const bool scale_o = upd && m != -INFINITY;
                 const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
@@ -1066,6 +1107,8 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
                 l *= al;
                 m = upd ? mx : m;
                 const float mu = m == -INFINITY ? 0.f : m;
+                far = fmaxf(far, fabsf(mu));
+                top = fmaxf(top, mx);
                 uint32_t hw[BN / 2];
                 float sum = weights_of<0, 96>(sv, sc, mu, hw);
                 // polled here, the answers are there when the weights are
@@ -1100,8 +1143,15 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
             }
             if (ok && x.n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
             if (!ok) break;
-            if (r < x.q_len - x.row) store_row(a, x.h, x.q_base + x.row + r, m - kAboveLog2, l);
-            if (x.n > 0 && !(v_top < INFINITY)) {
+            const bool too_far = __any_sync(0xFFFFFFFFu, far > kFarLog2 && far < INFINITY);
+            if (lane == 0) a.far[x.id * kGroupWarps + warp] = too_far;
+            if (r < x.q_len - x.row) {
+                if (too_far)
+                    store_top(a, x.h, x.q_base + x.row + r, top);
+                else
+                    store_row(a, x.h, x.q_base + x.row + r, m - kAboveLog2, l);
+            }
+            if (too_far || (x.n > 0 && !(v_top < INFINITY))) {
                 left = true;
                 tc_fence_before();
                 continue;
@@ -1141,7 +1191,8 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
         // (after everything else: they take far longer than a wait of another role may; the rings are free by now, as this warp
         // has seen the end of every product that read them)
         static_assert(kGroupWarps * kGivenFloats<D> * 4 <= L::OFF_OUT, "the rings hold every warp's part");
-        if (ok && left) units_as_given<D, TOut>(a, warp, reinterpret_cast<float *>(smem));
+        __syncwarp();
+        if (ok && left) units_as_given<D, TOut>(a, warp, reinterpret_cast<float *>(smem) + warp * kGivenFloats<D>);
         if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
     }
     if (!ok) atomicOr(&g_ris_packed_error, 2u);
@@ -1409,32 +1460,42 @@ __global__ void __launch_bounds__(kWeightThreads, DT == 64 ? 4 : 2) k_packed_wei
             const int from = j - shift - i0;   // first row of the chunk that sees this thread's key
             const int rows = it.q_len - i0;    // rows of the chunk
             const bool whole = it.row + warp * 32 + 31 - shift <= i0 && rows >= RC;
+            // (a far row's maximum was rounded as a product, the others' sums came from exponents rounded once)
+            const bool far = __any_sync(0xFFFFFFFFu, fmaxf(fabsf(st[lane].x), fabsf(st[lane + 32].x)) > kFarLog2);
+            static_assert(RC == 64, "two rows to a lane");
             float part[4] = {};
+            auto add = [&](auto far_c) {
+                auto weight = [&](float x, float m) { return ex2(decltype(far_c)::value ? __fmul_rn(x, sc) - m : fmaf(x, sc, -m)); };
 #pragma unroll
-            for (int half = 0; half < RC; half += 32) {
-                float sv[32];
-                tmem_ld32(tmem + (s & 1) * RC + lane_off + half, sv);
-                if (half == RC - 32) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0 && s + 2 < steps) mbar_arrive(bar(L::B_S_FREE + (s & 1)));
-                }
-                if (whole) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float4 ml = *reinterpret_cast<const float4 *>(&st[half + e]);
-                        part[e & 2] = fmaf(ex2(fmaf(sv[e], sc, -ml.x)), ml.y, part[e & 2]);
-                        part[(e & 2) + 1] = fmaf(ex2(fmaf(sv[e + 1], sc, -ml.z)), ml.w, part[(e & 2) + 1]);
+                for (int half = 0; half < RC; half += 32) {
+                    float sv[32];
+                    tmem_ld32(tmem + (s & 1) * RC + lane_off + half, sv);
+                    if (half == RC - 32) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0 && s + 2 < steps) mbar_arrive(bar(L::B_S_FREE + (s & 1)));
                     }
-                } else {
+                    if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float2 ml = st[half + e];
-                        const float p = ex2(fmaf(sv[e], sc, -ml.x));
-                        if (half + e >= from && half + e < rows) part[e & 3] = fmaf(p, ml.y, part[e & 3]);
+                        for (int e = 0; e < 32; e += 2) {
+                            const float4 ml = *reinterpret_cast<const float4 *>(&st[half + e]);
+                            part[e & 2] = fmaf(weight(sv[e], ml.x), ml.y, part[e & 2]);
+                            part[(e & 2) + 1] = fmaf(weight(sv[e + 1], ml.z), ml.w, part[(e & 2) + 1]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) {
+                            const float2 ml = st[half + e];
+                            const float p = weight(sv[e], ml.x);
+                            if (half + e >= from && half + e < rows) part[e & 3] = fmaf(p, ml.y, part[e & 3]);
+                        }
                     }
                 }
-            }
+            };
+            if (far)
+                add(std::true_type{});
+            else
+                add(std::false_type{});
             w += (part[0] + part[1]) + (part[2] + part[3]);
         }
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -1531,12 +1592,13 @@ cudaError_t launch_rows(const PackedArgs &a, const PackedMaps &maps, cudaStream_
 
 }  // namespace
 
-// scratch: the bounds of the runs, the largest magnitudes, the values
+// scratch: the bounds of the runs, the largest magnitudes, the units' marks, the values
 static size_t scratch_part(const PackedArgs &a) { return (sizeof(uint32_t) * a.n_runs * a.Hkv + 255) & ~size_t(255); }
 static size_t scratch_top(const PackedArgs &a) { return (sizeof(float) * a.n_seqs * a.Hkv + 255) & ~size_t(255); }
+static size_t scratch_far(const PackedArgs &a) { return ((size_t)a.n_items * a.Hq * kGroupWarps + 255) & ~size_t(255); }
 size_t packed_scratch_bytes(const PackedArgs &a, int32_t head_dim)
 {
-    return scratch_part(a) + scratch_top(a) + (size_t)a.k_total * a.Hkv * head_dim * 2;
+    return scratch_part(a) + scratch_top(a) + scratch_far(a) + (size_t)a.k_total * a.Hkv * head_dim * 2;
 }
 
 cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s)
@@ -1544,7 +1606,8 @@ cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool cluster
     char *const mem = static_cast<char *>(scratch);
     uint32_t *const part = reinterpret_cast<uint32_t *>(mem);
     float *const top = reinterpret_cast<float *>(mem + scratch_part(a));
-    __half *const v16 = reinterpret_cast<__half *>(mem + scratch_part(a) + scratch_top(a));
+    a.far = reinterpret_cast<uint8_t *>(mem + scratch_part(a) + scratch_top(a));
+    __half *const v16 = reinterpret_cast<__half *>(mem + scratch_part(a) + scratch_top(a) + scratch_far(a));
     a.v_top = top;
     if (a.n_runs > 0) {
         const dim3 grid((unsigned)a.n_runs, (unsigned)a.Hkv);

@@ -73,6 +73,7 @@ struct PackedArgs {
     float2 *row_stat;          // scratch [Hq][q_total]: each row's (maximum in log2, 1 / sum); null without weights
     const PackRun *runs;
     int32_t n_runs, n_seqs;
+    uint8_t *far;              // tile kernels: [n_items][Hq][4] scratch, whose rows' scores passed what P's range allows
     const float *v_top;        // tile kernels: [n_seqs][Hkv] the largest |v|, or infinity where the rows are to be computed from
                                // the values as given (undefined for sequences without keys)
 };

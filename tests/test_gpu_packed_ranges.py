@@ -140,3 +140,22 @@ def test_key_that_takes_nearly_all_weight_with_values_of_zero(n, m, Hq, Hkv, D, 
             assert rel_l2(to_np(got[at + first:at + x, h]), ref[at + first:at + x, h].numpy()) <= 5e-3
         at += x
     assert ((lse.double().cpu() - rl).abs() <= 2e-5 * (1 + rl.abs())).all()
+
+
+@pytest.mark.parametrize("n,m", [([300, 77], [300, 77]), ([300, 40], [6000, 5000])])
+@pytest.mark.parametrize("Hq,Hkv,D", [(6, 2, 128), (4, 2, 64)])
+@pytest.mark.parametrize("size", [1e2, 1e4])
+def test_scores_of_millions(n, m, Hq, Hkv, D, size):
+    """Each row is its best key's value, or a mixture of very few: fp32 scores of up to 1e9 stand further apart than they are off. The
+    log-sum-exp is off by what fp32 leaves of it and of the products (2^-19), weights by that of a score of magnitude S (sums of
+    fp32 additions that cut off, 2^-23 S each, eight of them: 1e-6 S), one at most."""
+    q, k, v = inputs(n, m, Hq, Hkv, D)
+    q, k = (q.float() * size).to(BF16), (k.float() * size).to(BF16)
+    with ris.ris_pack_create(n, m) as pack:
+        got, lse, w = ris.ris_attention_packed(pack, q, k, v, out_dtype=F32, return_lse=True, weight_rows=50)
+        ris.ris_device_status()
+    ref, rl, rw = packed_plain(q, k, v, n, m, 50)
+    check_bf16_path(to_np(got), ref.numpy())
+    assert ((lse.double().cpu() - rl).abs() <= 2.0 ** -19 * rl.abs()).all()
+    off = 2e-5 + 1e-6 * float(rl[rl > -INF].abs().max())
+    assert (w.double().cpu() - rw).abs().max() <= min(off, 1e-2) * max(1.0, float(rw.max()))
