@@ -26,7 +26,8 @@ __device__ unsigned int g_ris_cache4_error;
 
 namespace {
 
-// N elements in a row as they lie in memory, N * sizeof(T) a multiple of 4 and the address aligned to it (up to 16)
+// N elements in a row as they lie in memory, N * sizeof(T) a multiple of 4 and the address aligned to it
+// (up to 16)
 template <typename T, int N>
 struct Raw {
     static constexpr int B = N * (int)sizeof(T), W = B >= 16 ? 16 : B;
@@ -73,10 +74,11 @@ __device__ __forceinline__ uint32_t code2(float a, float b)
     asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tcvt.u16.u8 %0, t;\n\t}" : "=h"(r) : "f"(b), "f"(a));
     return r;
 }
-// The codes of x / s, rounded to fp32 first as the format has it, without a division per value: with r = fl(1 / s), q = fl(x r)
-// and the exact remainder x - q s, fl(q + r (x - q s)) is the quotient but for a relative 2^-46 before its one
-// rounding (Markstein, IBM J. Res. Dev. 34, 1990). As the scale has 8 significant bits, a quotient that is no
-// fp32 number is at least 2^-33 of itself away from the middle of two, so the rounding is the division's own.
+// The codes of x / s, rounded to fp32 first as the format has it, without a division per value: with r =
+// fl(1 / s), q = fl(x r) and the exact remainder x - q s, fl(q + r (x - q s)) is the quotient but for a
+// relative 2^-46 before its one rounding (Markstein, IBM J. Res. Dev. 34, 1990). As the scale has 8
+// significant bits, a quotient that is no fp32 number is at least 2^-33 of itself away from the middle of
+// two, so the rounding is the division's own.
 struct Scale {
     float s, r;
     bool plain;  // the scale is outside the range where no step over- or underflows
@@ -98,11 +100,12 @@ struct Scale {
     }
 };
 
-// Four lanes to a row of keys and its row of values; each lane loads what it stores (16 or 8 bytes of codes in one
-// piece each), so rows are read and written in whole sectors; a group's maximum comes from its four lanes by shuffles.
-// Bound by the latency of a row's chain (load, maximum, scale, codes: 350 instructions a lane) at the 32 warps that its registers
-// leave an SM: 32,100 tokens of 2 heads of 128 take 11.5 us from L2, 15.5 from HBM, 8,028 CTAs over 8 heads 42 us at
-// 4.0 TB/s. More warps with fewer registers (51, 42 instead of 59) took 12.8 and 14.0 us, CTAs that stay and load ahead 14.4.
+// Four lanes to a row of keys and its row of values; each lane loads what it stores (16 or 8 bytes of codes
+// in one piece each), so rows are read and written in whole sectors; a group's maximum comes from its four
+// lanes by shuffles. Bound by the latency of a row's chain (load, maximum, scale, codes: 350 instructions a
+// lane) at the 32 warps that its registers leave an SM: 32,100 tokens of 2 heads of 128 take 11.5 us from
+// L2, 15.5 from HBM, 8,028 CTAs over 8 heads 42 us at 4.0 TB/s. More warps with fewer registers (51, 42
+// instead of 59) took 12.8 and 14.0 us, CTAs that stay and load ahead 14.4.
 constexpr int kAppendThreads = 128;
 
 template <typename T, int D>
@@ -219,8 +222,9 @@ __device__ __forceinline__ __half2 values2(uint32_t byte)
     return *reinterpret_cast<const __half2 *>(&r);
 }
 
-// One thread per four elements of a row of the output, kReadRows rows of a list to a CTA: two bytes in, 16 bytes out.
-// Bound by the fp32 rows that it writes: 21 us for the 98 MB of two times 4 x 2 lists of 12,000 slots of 128 (4.7 TB/s).
+// One thread per four elements of a row of the output, kReadRows rows of a list to a CTA: two bytes in, 16
+// bytes out. Bound by the fp32 rows that it writes: 21 us for the 98 MB of two times 4 x 2 lists of 12,000
+// slots of 128 (4.7 TB/s).
 constexpr int kReadThreads = 256, kReadRows = 64;
 template <int D>
 __global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c, const int32_t *first, int64_t count, int blocks,
@@ -264,8 +268,8 @@ __global__ void __launch_bounds__(kReadThreads) k_cache4_read(const Cache4Args c
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kTile = 16;                      // slots of a warp's product
 constexpr int kUnit = kCacheUnit;              // slots by which the work is shared out
-constexpr float kMostFactor = 0x1p118f;        // largest factor of a weight times value scale (a weight is 2^8 at most)
-constexpr float kMostHalf = 0x1p15f;           // what weight, scale and factor may come to as fp16
+constexpr int kMostFactor = 127 + 118;         // largest factor of a weight times value scale (a weight is 2^8 at most), its exponent
+constexpr int kMostHalf = 15;                  // what weight, scale and factor may come to as fp16 (log2)
 
 template <int D, bool SPLIT>
 struct Lay {
@@ -363,18 +367,21 @@ __device__ __forceinline__ uint32_t pack_rest(float x, float y, uint32_t hi)
     const float2 h = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
     return pack_half(x - h.x, y - h.y);
 }
+// 1 / f of a power of two, both normal numbers
+__device__ __forceinline__ float inverse2(float f) { return __uint_as_float((254u << 23) - __float_as_uint(f)); }
 __device__ __forceinline__ float bf16_at(uint32_t w, int e) { return __uint_as_float((e & 1) ? (w & 0xFFFF0000u) : (w << 16)); }
 
 // Slot of row r (0 .. 15) of a tile: the rows that a lane needs as pairs along the product's inner
-// dimension, 2 t, 2 t + 1, 2 t + 8 and 2 t + 9, are slots t, 4 + t, 8 + t and 12 + t, so that the four lanes t read
-// neighbouring rows of the values.
+// dimension, 2 t, 2 t + 1, 2 t + 8 and 2 t + 9, are slots t, 4 + t, 8 + t and 12 + t, so that the four
+// lanes t read neighbouring rows of the values.
 __device__ __forceinline__ int tile_slot(int r) { return ((r & 7) >> 1) + 4 * (r & 1) + (r & 8); }
 
 // How the slots in use are shared out. A list is a (sequence, KV head, block of 8 query heads) and holds
-// ceil(length / kUnit) units; the units of all lists, one list after another, are cut into as many equal runs as there are CTAs,
-// whatever the lengths are. CTA i's part of list l has partial number i + l: runs and lists advance together, so no
-// two parts share a number. Lists of a sequence are neighbours: list = b * per_seq + y. Every warp works this out for
-// itself, 32 sequences at a time by shuffles (with the block's barriers and 64-bit divisions it took 4 us).
+// ceil(length / kUnit) units; the units of all lists, one list after another, are cut into as many equal
+// runs as there are CTAs, whatever the lengths are. CTA i's part of list l has partial number i + l: runs
+// and lists advance together, so no two parts share a number. Lists of a sequence are neighbours: list = b
+// * per_seq + y. Every warp works this out for itself, 32 sequences at a time by shuffles (with the block's
+// barriers and 64-bit divisions it took 4 us).
 __device__ __forceinline__ int64_t slots_of(const Cache4AttendArgs &a, int b)
 {
     return max((int64_t)0, min((int64_t)a.c.length[b], a.reach));
@@ -395,10 +402,11 @@ __device__ __forceinline__ int64_t mul_div(int64_t x, int y, int z)
     return x < (1 << 20) && y < (1 << 11) ? (int64_t)((uint32_t)x * (uint32_t)y / (uint32_t)z) : x * y / z;
 }
 
-// Persistent CTAs of four warps; each CTA takes a run of units and the lists that it touches one after another. Its warps
-// take stages of 64 slots (32 for fp32 outputs, whose accumulators double; fewer where that leaves warps without any) in turn, each
-// with a softmax of its own over the slots that it saw and a ring of its own, filled by bulk copies (codes and scales are contiguous per KV head): no warp waits for another before a list's
-// end. A tile of 16 slots:
+// Persistent CTAs of four warps; each CTA takes a run of units and the lists that it touches one after
+// another. Its warps take stages of 64 slots (32 for fp32 outputs, whose accumulators double; fewer where
+// that leaves warps without any) in turn, each with a softmax of its own over the slots that it saw and a
+// ring of its own, filled by bulk copies (codes and scales are contiguous per KV head): no warp waits for
+// another before a list's end. A tile of 16 slots:
 //   S^T = K q^T  rows are slots, columns up to 8 query heads: the codes as fp16 (exact) straight from
 //                the lane's word, one accumulator per group of 32, which the group's scale then multiplies in
 //                fp32 (so the products are exact up to fp32 sums); the query as fp16 scaled by a power of
@@ -406,18 +414,20 @@ __device__ __forceinline__ int64_t mul_div(int64_t x, int y, int z)
 //   O^T += V^T P^T  the weights times the slot's scale, per group of 32, as fp16, transposed by
 //                movmatrix; with SPLIT a second fp16 of what the first leaves, for fp32 outputs; values as
 //                fp16 pairs of slots, paired as codes (half the instructions of pairing them as fp16).
-// The weights are p = 2^(s - m), m a whole number that moves only when a score exceeds it by more than 2^8; the row's sum is
-// that of p alone, whatever the values hold. fp16 gets u = f p scale with a factor f, a power of two, per query head and group
-// of 32 channels: it comes down when a u would pass 2^15, to where the largest of the stage is 16, and goes up with m, so
-// what a slot adds keeps fp16's 11 bits down to 2^-18 of the largest that any slot so far has added to that head and group,
-// and no group, slot or scale that is not finite takes bits from another group. O carries its group's f.
-// Slots past the length enter with score -infinity and scale 0, whatever lies there.
-// A list takes 8 query heads of its KV head, a product's columns.
-// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 54.6 us a call with the join, 4.7 of the 6.8 TB/s that a
-// copy reaches (one exponent for all groups and heads, which a scale that is not finite or one large slot spoils, took 49.7; fp32
-// outputs 82 and 73); unpacking keeps the ALU pipe and the issue slots half busy, so three CTAs' loads and arithmetic do not
-// overlap all the way. Smaller calls are latency: 24 sequences of 700 to 9,216 slots 12.5 us before the join, of which the
-// copies' first arrival and a warp's two stages are most.
+// The weights are p = 2^(s - m), m a whole number that moves only when a score exceeds it by more than 2^8;
+// the row's sum is that of p alone, whatever the values hold. fp16 gets u = f p scale with a factor f, a
+// power of two, per query head and group of 32 channels: it comes down when a u would pass 2^15, to where
+// the largest of the stage is 16, and goes up with m, so what a slot adds keeps fp16's 11 bits down to
+// 2^-18 of the largest that any slot so far has added to that head and group, and no group, slot or scale
+// that is not finite takes bits from another group. O carries its group's f. Slots past the length enter
+// with score -infinity and scale 0, whatever lies there. A list takes 8 query heads of its KV head, a
+// product's columns: where a KV head has more, its slots are copied and unpacked once per 8.
+// 16 sequences of 48,000 to 65,536 slots at 12 / 2 heads of 128, 258 MB: 52.0 us a call
+// with the join, 5.0 of the 6.8 TB/s that a copy reaches (one exponent for all groups and heads, which a
+// scale that is not finite or one large slot spoils, took 49.7; fp32 outputs 80 and 73); unpacking keeps
+// the ALU pipe and the issue slots half busy, so three CTAs' loads and arithmetic do not overlap all the
+// way. Smaller calls are latency: 24 sequences of 700 to 9,216 slots 16.3 us with the join (14.3
+// with one exponent), of which the copies' first arrival and a warp's two stages are most.
 constexpr float kLazyLog2 = 8.f;
 
 template <typename T, bool SPLIT, int D>
@@ -542,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
             m[0] = m[1] = -INFINITY;
             l[0] = l[1] = 0.f;
 #pragma unroll
-            for (int g = 0; g < NG; ++g) fac[0][g] = fac[1][g] = kMostFactor;
+            for (int g = 0; g < NG; ++g) fac[0][g] = fac[1][g] = __uint_as_float((uint32_t)kMostFactor << 23);
 #pragma unroll
             for (int e = 0; e < NM; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
         }
@@ -629,12 +639,12 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
 #pragma unroll
                     for (int i = 1; i < kWarpTiles; ++i) x[e] = fmaxf(x[e], fmaxf(s[i][e], s[i][e + 2]));
                     x[e] *= unscale[e];
-                    // no u of this lane is larger than its largest weight times its largest scales, all groups' together (NaN: not
-                    // known to be small)
+                    // no u of this lane is larger than its largest weight times its largest scales, all
+                    // groups' together (NaN: not known to be small)
                     float most = 0.f;
 #pragma unroll
                     for (int g = 0; g < NG; ++g) most = fmaf(fac[e][g], bf16_at(top[g / 2], g), most);
-                    moves = moves || x[e] > m[e] + kLazyLog2 || !(ex2(x[e] - m[e]) * most <= kMostHalf);
+                    moves = moves || x[e] > m[e] + kLazyLog2 || !(ex2(x[e] - m[e]) * most <= (float)(1 << kMostHalf));
                 }
                 if (__any_sync(0xFFFFFFFFu, moves)) {  // (in the first stages of a list, mostly)
 #pragma unroll
@@ -642,39 +652,45 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
 #pragma unroll
                         for (int w = 4; w < 32; w <<= 1) x[e] = fmaxf(x[e], __shfl_xor_sync(0xFFFFFFFFu, x[e], w));
                         const bool begun = m[e] != -INFINITY;  // (else O and l are 0, or NaN)
-                        float up = 1.f;
+                        int up = 0;
                         if (x[e] > m[e] + kLazyLog2) {
                             const float nm = ceilf(x[e]);
                             if (begun) {
-                                up = ex2(nm - m[e]);
                                 l[e] *= ex2(m[e] - nm);
+                                up = (int)fminf(nm - m[e], 1000.f);
                             }
                             m[e] = nm;
                         }
                         const float ref = m[e] == -INFINITY ? 0.f : m[e];
-                        float most[NG] = {};  // largest weight times scale, times 2^-8
+                        // largest weight times scale, times 2^-8, of two groups in a word: its power of two is what counts, which
+                        // bf16 gives (a NaN is passed over)
+                        __nv_bfloat162 most[NG / 2];
+#pragma unroll
+                        for (int g = 0; g < NG / 2; ++g) most[g] = __float2bfloat162_rn(0.f);
 #pragma unroll
                         for (int i = 0; i < kWarpTiles; ++i)
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
-                                const float p = ex2(fmaf(s[i][e + 2 * r], unscale[e], -ref)) * 0x1p-8f;
+                                const __nv_bfloat162 p = __float2bfloat162_rn(ex2(fmaf(s[i][e + 2 * r], unscale[e], -ref)) * 0x1p-8f);
 #pragma unroll
-                                for (int g = 0; g < NG; ++g) {
-                                    const float u = p * bf16_at(vsc[i][r][g / 2], g);
-                                    if (u < INFINITY) most[g] = fmaxf(most[g], u);
-                                }
+                                for (int g = 0; g < NG / 2; ++g)
+                                    most[g] = __hmax2(most[g], __hmul2(p, *reinterpret_cast<const __nv_bfloat162 *>(&vsc[i][r][g])));
                             }
 #pragma unroll
-                        for (int g = 0; g < NG; ++g) {
+                        for (int g = 0; g < NG / 2; ++g)
 #pragma unroll
-                            for (int w = 4; w < 32; w <<= 1) most[g] = fmaxf(most[g], __shfl_xor_sync(0xFFFFFFFFu, most[g], w));
-                            // O stays as it is where f goes up as the weights come down
-                            const float had = fac[e][g] * up;
-                            fac[e][g] = fminf(had, kMostFactor);
-                            if (most[g] * fac[e][g] > kMostHalf * 0x1p-8f)
-                                fac[e][g] = __uint_as_float((uint32_t)max(1, 127 - 4 - ((int)(__float_as_uint(most[g]) >> 23) - 127)) << 23);
-                            if (begun && fac[e][g] != had) {
-                                const float by = fac[e][g] / had;
+                            for (int w = 4; w < 32; w <<= 1) most[g] = __hmax2(most[g], __shfl_xor_sync(0xFFFFFFFFu, most[g], w));
+#pragma unroll
+                        for (int g = 0; g < NG; ++g) {
+                            // by exponents (of 127 + the power): the factor goes up as the weights come down, where O stays as it
+                            // is, and comes down to where the largest product is 16
+                            const int top = (int)(__float_as_uint(bf16_at(*reinterpret_cast<const uint32_t *>(&most[g / 2]), g)) >> 23);
+                            const int had = (int)(__float_as_uint(fac[e][g]) >> 23) + up;
+                            int now = min(had, kMostFactor);
+                            if (top + now - 2 * 127 >= kMostHalf - 8) now = max(1, 2 * 127 - 4 - top);
+                            fac[e][g] = __uint_as_float((uint32_t)now << 23);
+                            if (begun && now != had) {
+                                const float by = now - had < -126 ? 0.f : pow2i(now - had);
 #pragma unroll
                                 for (int t = 2 * g; t < 2 * g + 2; ++t) {
                                     o[t][e] *= by;
@@ -684,8 +700,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                         }
                     }
                 }
-                // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor pipe's
-                // additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
+                // fp32 outputs: the stage's products from zero, added to O in fp32 afterwards. (The tensor
+                // pipe's additions cut off: over thousands of slots in one accumulator 2e-6 of the result.)
                 [[maybe_unused]] float part[SPLIT ? NM : 1][4];
                 const float to[2] = {m[0] == -INFINITY ? 0.f : -m[0], m[1] == -INFINITY ? 0.f : -m[1]};  // exponent of a weight: s unscale + to
 #pragma unroll
@@ -722,8 +738,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
                     }
 #pragma unroll
                     for (int q4 = 0; q4 < NM / 4; ++q4) {
-                        // byte e of the words x (slots of rows 2 t, 2 t + 1) and y (2 t + 8, 2 t + 9): the pair of values
-                        // of element 2 g8 (index 0) or 2 g8 + 1 (1) of tile 4 q4 + e
+                        // byte e of the words x (slots of rows 2 t, 2 t + 1) and y (2 t + 8, 2 t + 9): the
+                        // pair of values of element 2 g8 (index 0) or 2 g8 + 1 (1) of tile 4 q4 + e
                         uint32_t x[2][4], y[2][4];
                         unpack4(low_halves(vw[0][q4], vw[1][q4]), x[0]);
                         unpack4(high_halves(vw[0][q4], vw[1][q4]), x[1]);
@@ -756,8 +772,8 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
         for (int s0 = warp * per; ok && s0 < n; s0 += s_step) {
             ok = __all_sync(0xFFFFFFFFu, mbar_wait(bars + 8 * used, phase, a.wait_limit));
             if (!ok) {
-                // the stages asked for, this one and the next of the ring, have landed before the ring is used for
-                // anything else, or the CTA ends
+                // the stages asked for, this one and the next of the ring, have landed before the ring is
+                // used for anything else, or the CTA ends
                 for (int i = 0; i < kStages && s0 < n && !a.debug_no_loads; ++i, s0 += s_step) {
                     mbar_wait(bars + 8 * used, phase);
                     if (++used == kStages) used = 0, phase ^= 1;
@@ -791,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
 #pragma unroll
             for (int tl = 0; tl < NM; ++tl)
                 *reinterpret_cast<float2 *>(so + (warp * 8 + h) * LO_ + 16 * tl + 2 * g8) =
-                    make_float2(o[tl][e] * inv * (1.f / fac[e][tl / 2]), o[tl][e + 2] * inv * (1.f / fac[e][tl / 2]));
+                    make_float2(o[tl][e] * inv * inverse2(fac[e][tl / 2]), o[tl][e + 2] * inv * inverse2(fac[e][tl / 2]));
         }
         __syncthreads();
         // one partial per head of the block: number cta + list
@@ -826,10 +842,10 @@ __global__ void __launch_bounds__(kThreads, 3) k_cache4_attend(const Cache4Atten
     if (!ok) atomicOr(&g_ris_cache4_error, 4u);  // (a copy that was given up: the outputs are undefined)
 }
 
-// Joins the parts of a list. The first CTAs: one per (query head, sequence), warps over its parts, a lane per
-// channels; then (weights) CTAs that add up what each slot got from the heads of its KV head, from the scores that
-// the first kernel left. Launched as its programmatic dependent. Latency: 8 us with the weights of 24 x 2 lists of 700 to 9,216
-// slots, 7 MB of scores.
+// Joins the parts of a list. The first CTAs: one per (query head, sequence), warps over its parts, a lane
+// per channels; then (weights) CTAs that add up what each slot got from the heads of its KV head, from the
+// scores that the first kernel left. Launched as its programmatic dependent. Latency: 8 us with the weights
+// of 24 x 2 lists of 700 to 9,216 slots, 7 MB of scores.
 constexpr int kJoinWarps = 4, kJoinThreads = 32 * kJoinWarps;
 constexpr int kWeightSlots = 4 * kJoinThreads;  // slots of a CTA
 
@@ -838,6 +854,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
 {
     constexpr int C = D / 32, block_heads = 8;
     __shared__ float so[kJoinWarps][D];
+    __shared__ float2 sml[kJoinWarps];
     extern __shared__ float2 stat[];  // [G], weights
     const int b = blockIdx.y, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per_seq = a.lists / a.c.B;
@@ -853,65 +870,51 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         i0 = len > 0 ? x.x : 0;
         i1 = len > 0 ? x.y : -1;
     };
-    // the maximum and sum of the parts together, a lane per part
-    auto whole = [&](int64_t p0, int i0, int i1) -> float2 {
-        float M = -INFINITY, sum = 0.f;
-        for (int i = i0 + lane; i <= i1; i += 32) {
-            const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
-            const float nm = fmaxf(M, ml.x);
-            sum = nm == -INFINITY ? sum + ml.y : sum * exp2f(M - nm) + ml.y * exp2f(ml.x - nm);
-            M = nm;
-        }
-        const float tm = warp_max(M);
-        return make_float2(tm, warp_sum(tm == -INFINITY ? sum : sum * exp2f(M - tm)));
-    };
     if ((int)blockIdx.x < a.Hq) {
         const int h = blockIdx.x, kvh = h / a.G, hb = (h % a.G) / block_heads, y = hb * a.c.Hkv + kvh;
         int i0, i1;
         parts(y, i0, i1);
         const int64_t p0 = ((int64_t)b * per_seq + y) * block_heads + h % a.G % block_heads;
-        // (each warp's first three parts are on their way while the sums are joined)
-        constexpr int AHEAD = 3;
-        float2 at[AHEAD];
-        float v[AHEAD][C];
-        auto fetch = [&](int i, float2 &ml, float(&o)[C]) {
+        // (averages, so that sums of values do not pass fp32's range, times sums of weights that may be as many as there
+        // are slots: scaled down)
+        constexpr float kDown = 0x1p-20f;
+        float M = -INFINITY, sum = 0.f, x[C] = {};
+#pragma unroll 4
+        for (int i = i0 + warp; i <= i1; i += kJoinWarps) {
             const int64_t p = p0 + (int64_t)i * block_heads;
-            ml = a.part_ml[p];
+            const float2 ml = a.part_ml[p];
+            float v[C];
 #pragma unroll
-            for (int c = 0; c < C; ++c) o[c] = a.part_o[p * D + lane + 32 * c];
-        };
+            for (int c = 0; c < C; ++c) v[c] = a.part_o[p * D + lane + 32 * c];
+            const float nm = fmaxf(M, ml.x);
+            const float f0 = M == -INFINITY ? 0.f : exp2f(M - nm), f1 = ml.y * (ml.x == -INFINITY ? 0.f : exp2f(ml.x - nm));
+            M = nm;
+            sum = fmaf(sum, f0, f1);
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n)
-            if (i0 + warp + kJoinWarps * n <= i1) fetch(i0 + warp + kJoinWarps * n, at[n], v[n]);
-        const float2 ml = whole(p0, i0, i1);
-        const float inv = 1.f / ml.y;
-        float x[C] = {};
-        auto add = [&](const float2 &part, const float(&o)[C]) {
-            const float share = part.y * (part.x == -INFINITY ? 0.f : exp2f(part.x - ml.x)) * inv;
-#pragma unroll
-            for (int c = 0; c < C; ++c) x[c] = fmaf(o[c], share, x[c]);
-        };
-#pragma unroll
-        for (int n = 0; n < AHEAD; ++n)
-            if (i0 + warp + kJoinWarps * n <= i1) add(at[n], v[n]);
-        for (int i = i0 + warp + kJoinWarps * AHEAD; i <= i1; i += kJoinWarps) {
-            fetch(i, at[0], v[0]);
-            add(at[0], v[0]);
+            for (int c = 0; c < C; ++c) x[c] = fmaf(x[c], f0, v[c] * (f1 * kDown));
         }
+        if (lane == 0) sml[warp] = make_float2(M, sum);
 #pragma unroll
         for (int c = 0; c < C; ++c) so[warp][lane + 32 * c] = x[c];
         __syncthreads();
         const int64_t row = (int64_t)b * a.Hq + h;
         const int d = threadIdx.x;
         if (d < D) {
-            float to = 0.f;  // (no slot: zeros)
+            float tm = -INFINITY, ts = 0.f, to = 0.f;
 #pragma unroll
-            for (int w = 0; w < kJoinWarps; ++w) to += so[w][d];
+            for (int w = 0; w < kJoinWarps; ++w) tm = fmaxf(tm, sml[w].x);
+#pragma unroll
+            for (int w = 0; w < kJoinWarps; ++w) {
+                const float f = sml[w].x == -INFINITY ? 0.f : exp2f(sml[w].x - tm);
+                ts = fmaf(sml[w].y, f, ts);
+                to = fmaf(so[w][d], f, to);
+            }
+            to = ts == 0.f ? 0.f : to / (ts * kDown);  // no slot: zeros
             if constexpr (sizeof(TO) == 4)
                 reinterpret_cast<float *>(a.out)[row * D + d] = to;
             else
                 reinterpret_cast<__nv_bfloat16 *>(a.out)[row * D + d] = __float2bfloat16_rn(to);
-            if (d == 0 && a.lse != nullptr) a.lse[row] = (ml.x + log2f(ml.y)) * kLn2;
+            if (d == 0 && a.lse != nullptr) a.lse[row] = (tm + log2f(ts)) * kLn2;
         }
         return;
     }
@@ -932,8 +935,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache4_join(const Cache4Attend
         int i0, i1;
         parts(yl, i0, i1);
         const int64_t p0 = ((int64_t)b * per_seq + yl) * block_heads + h % block_heads;
-        const float2 ml = whole(p0, i0, i1);
-        if (lane == 0) stat[h] = make_float2(ml.x, 1.f / ml.y);
+        float M = -INFINITY, sum = 0.f;
+        for (int i = i0 + lane; i <= i1; i += 32) {
+            const float2 ml = a.part_ml[p0 + (int64_t)i * block_heads];
+            const float nm = fmaxf(M, ml.x);
+            sum = nm == -INFINITY ? sum + ml.y : sum * exp2f(M - nm) + ml.y * exp2f(ml.x - nm);
+            M = nm;
+        }
+        const float tm = warp_max(M);
+        sum = warp_sum(tm == -INFINITY ? sum : sum * exp2f(M - tm));
+        if (lane == 0) stat[h] = make_float2(tm, 1.f / sum);
     }
     __syncthreads();
     for (int h0 = 0; h0 < a.G; h0 += 8) {
