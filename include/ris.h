@@ -414,14 +414,15 @@ ris_status ris_decode_step(ris_anchor_t anchor, const void *q, const void *k, co
  *
  * Pack: the plan of a call over n_seqs sequences whose tokens lie one after another. Sequence s has
  * q_lens[s] rows (new tokens) and k_lens[s] keys (HOST arrays; k_lens NULL: the same lengths). The rows
- * are the last of the sequence's positions: row i sees keys j <= i + k_lens[s] - q_lens[s], and a row that sees none
- * gets zeros and a log-sum-exp of -infinity. Lengths may be 0. Built once per batch
- * and kept for all layers and all calls of it, on any stream. Blocks (the
- * plan's copy); not during stream capture. Errors: RIS_ERR_INVALID (n_seqs outside [1, 65535], a negative length,
- * more than 2^31 - 65537 tokens), RIS_ERR_OOM, RIS_ERR_CUDA. On error *out is NULL.
- * ris_pack_info: any output may be NULL. ris_pack_free: gives the plan back on the stream it was built on, behind every call
- * with the pack that was queued before, on whatever stream. Calls captured into a graph are not among them: a graph must not be
- * replayed once a pack in it was freed, nor the pack freed before the last replay has finished. */
+ * are the last of the sequence's positions: row i sees keys j <= i + k_lens[s] - q_lens[s], and a row
+ * that sees none gets zeros and a log-sum-exp of -infinity. Lengths may be 0. Built once per batch and kept
+ * for all layers and all calls of it, on any stream. Blocks (the plan's copy); not during stream capture.
+ * Errors: RIS_ERR_INVALID (n_seqs outside [1, 65535], a negative length, more than 2^31 - 65537 tokens),
+ * RIS_ERR_OOM, RIS_ERR_CUDA. On error *out is NULL.
+ * ris_pack_info: any output may be NULL. ris_pack_free: gives the plan back on the stream it was built on,
+ * behind every call with the pack that was queued before, on whatever stream. Calls captured into a graph
+ * are not among them: a graph must not be replayed once a pack in it was freed, nor the pack freed before
+ * the last replay has finished. */
 typedef struct ris_pack_s *ris_pack_t;
 ris_status ris_pack_create(const int64_t *q_lens, const int64_t *k_lens, int32_t n_seqs, ris_pack_t *out, void *stream);
 ris_status ris_pack_info(ris_pack_t pack, int32_t *n_seqs, int64_t *q_total, int64_t *k_total, int64_t *q_longest,
@@ -451,10 +452,18 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
  * lse: optional [heads][q_total] natural-log sum of exp of the scaled scores.
  * weight_rows W > 0 with key_weight [kv_heads][k_total]: the attention weight that each key got from the
  * last W rows of its sequence (all rows where there are fewer), summed over the query heads of its KV head: what
- * ris_cache4_append takes as the first of a slot's accumulated weight. W = 0: key_weight NULL; it may be NULL where no sequence has a key.
- * head_dim in {64, 128}, any heads / kv_heads, fp32 or bf16. fp32 inputs never use a narrower product.
- * A key that a row does not see takes no part in it, whatever it holds.
- * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (more row tiles x heads than a grid holds), RIS_ERR_OOM, RIS_ERR_CUDA. */
+ * ris_cache4_append takes as the first of a slot's accumulated weight. W = 0: key_weight NULL; it may be
+ * NULL where no sequence has a key.
+ * head_dim in {64, 128}, any heads / kv_heads, fp32 or bf16. A key that a row does not see takes no part in
+ * it, whatever it holds, and no prompt or KV head takes bits from another.
+ * Precision: fp32 inputs never use a narrower product. bf16 inputs, whatever out_dtype is: exact products of
+ * q and k summed in fp32; softmax statistics in fp32; a weight as fp16, with its 11 bits down to 2^-21 of the
+ * row's largest; values as fp16 scaled by a power of two of their (sequence, KV head), exact down to 2^-30 of
+ * its largest, and to 2^-12 of the key's own largest where that lies lower. Where the keys' largest values of
+ * a (sequence, KV head) lie more than 2^26 apart or are not finite, and for rows of scores beyond 2^23, the
+ * rows are computed on the FP32 pipe instead: some 50 times slower.
+ * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (more row tiles x heads than a grid holds), RIS_ERR_OOM,
+ * RIS_ERR_CUDA. */
 ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, const void *v, void *out, int32_t heads,
                                 int32_t kv_heads, int32_t head_dim, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                                 int32_t dtype, int32_t out_dtype, float *lse, int32_t weight_rows, float *key_weight,
@@ -463,10 +472,10 @@ ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, c
 /* A K/V cache held in 4 bits: caller-owned DEVICE arrays, each 16-byte aligned. Sequence b holds the
  * slots 0 .. length[b] - 1 of every KV head; the slots of a head need not be in the order of their
  * positions, and after an eviction differ from head to head.
- *   A row of head_dim values is cut into groups of 32. A group's scale is bf16(max |x| * fl32(1/6)) (NaN where a
- *   value is not finite: the group then stands for NaN); a value is stored as the e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6, sign in bit 3)
- *   nearest to x / scale in fp32, ties to the even code, at most 6. Two codes make a byte, the even element in the
- *   low half. With i the byte's number in natural order, n = head_dim / 32 and m = head_dim / 16, it lies at
+ *   A row of head_dim values is cut into groups of 32. A group's scale is bf16(max |x| * fl32(1/6)) (NaN
+ *   where a value is not finite: the group then stands for NaN); a value is stored as the e2m1 code (0, 0.5,
+ *   1, 1.5, 2, 3, 4, 6, the value's sign in bit 3, also of -0) nearest to x / scale in fp32, ties to the even
+ *   code, at most 6. Two codes make a byte, the even element in the low half. With i the byte's number in natural order, n = head_dim / 32 and m = head_dim / 16, it lies at
  *     keys    4 (((i / 4) mod 4) n + i / 16) + i mod 4,      values  (i mod 8) m + i / 8.
  * capacity is a multiple of 16; slots at and past length[b] may hold anything. `sync` is zeroed by the
  * caller once; every call leaves it zero. Calls on one cache must be ordered on the GPU. */
@@ -485,9 +494,9 @@ typedef struct {
 } ris_cache4;
 
 /* Append the rows of a pack (its q side; sequence s to row s of the batch) to the cache: k and v
- * [q_total][kv_heads][head_dim], rotated, token strides in elements; positions: DEVICE int32 [q_total]; weight: optional
- * DEVICE [kv_heads][q_total] (else 0). Token i of sequence b goes to slot start[b] + i and length[b] becomes start[b] + q_lens[b];
- * start NULL: after the slots in use. start (DEVICE int32 [batch]) must not be the cache's length.
+ * [q_total][kv_heads][head_dim], rotated, token strides in elements; positions: DEVICE int32 [q_total];
+ * weight: optional DEVICE [kv_heads][q_total] (else 0). Token i of sequence b goes to slot start[b] + i and
+ * length[b] becomes start[b] + q_lens[b], cut to 0 .. capacity; start NULL: after the slots in use. start (DEVICE int32 [batch]) must not be the cache's length.
  * Tokens past the capacity (or at a negative slot) are left out and reported by ris_device_status as
  * RIS_ERR_INVALID. A pack of ones is a decode step's append. Errors: RIS_ERR_INVALID, RIS_ERR_CUDA. */
 ris_status ris_cache4_append(const ris_cache4 *cache, ris_pack_t pack, const void *k, const void *v, int64_t k_stride,
@@ -503,11 +512,16 @@ ris_status ris_cache4_read(const ris_cache4 *cache, const int32_t *first, int64_
  * longest: an upper bound of the lengths that the caller knows (slots past it take no part), 0 for the
  * capacity: it sizes the grid and the scratch, so nothing in the launch depends on the lengths and a
  * captured graph can be replayed as they grow.
- * weight_out (optional, [batch][kv_heads][capacity]): weight_in + the weights of this token, summed over the query
- * heads of the KV head, for every slot in use (others untouched); weight_in NULL counts as 0 and may be weight_out
- * (the cache's own weight array, to add up in place). fp32 outputs take the query (fp32 inputs) and the weights in two fp16 parts each, bf16
- * outputs the weights in one. Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (weights over more than 4096 query heads of a
- * KV head, batch x kv_heads past 2^24), RIS_ERR_OOM, RIS_ERR_CUDA. */
+ * weight_out (optional, [batch][kv_heads][capacity]): weight_in + the weights of this token, summed over
+ * the query heads of the KV head, for every slot in use (others untouched); weight_in NULL counts as 0 and
+ * may be weight_out (the cache's own weight array, to add up in place).
+ * Precision: the query as fp16 scaled by its head's largest element, in two parts for fp32 inputs (elements
+ * below 2^-26 of the largest lose bits); scores, weights and sums in fp32. Weight times value scale goes
+ * through one fp16 for bf16 outputs, two for fp32 outputs, with all bits down to 2^-18 of the largest that a
+ * slot adds to the same query head and group of 32 channels. A group that stands for NaN makes those channels
+ * NaN in its KV head's outputs; other groups, lse and weight_out do not depend on it.
+ * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (weights over more than 4096 query heads of a KV head, batch x
+ * kv_heads past 2^24), RIS_ERR_OOM, RIS_ERR_CUDA. */
 ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t heads, int32_t dtype, int32_t out_dtype,
                              int64_t longest, void *out, float *lse, const float *weight_in, float *weight_out, void *stream);
 

@@ -1,23 +1,25 @@
 // Causal attention over packed prompts on the 5th-generation tensor cores, bf16 inputs.
 //
-// S = Q K^T with bf16 operands (exact products, fp32 sums), one online softmax per row over the keys j <= i +
-// k_len - q_len of its own sequence, O = P V with P as fp16 (11 bits; a bf16 P would add as much error
+// S = Q K^T with bf16 operands (exact products, fp32 sums), one online softmax per row over the keys j <= i
+// + k_len - q_len of its own sequence, O = P V with P as fp16 (11 bits; a bf16 P would add as much error
 // again as the bf16 output's own rounding) against the values as fp16 scaled by a power of two of their
-// sequence and KV head (a bf16 value is exact there down to 2^-30 of the largest), the row's sum from the fp32 weights before they
-// are rounded. The values are converted by two passes over V ahead of the attention (bounds, then the values): a few
-// percent of a call where there are as many rows as keys, as V is read once per 128 rows of it anyway; most of one of
-// few rows behind many keys.
+// sequence and KV head (a bf16 value is exact there down to 2^-30 of the largest), the row's sum from the
+// fp32 weights before they are rounded. The values are converted by two passes over V ahead of the
+// attention (bounds, then the values): a few percent of a call where there are as many rows as keys, as V
+// is read once per 128 rows of it anyway; most of one of few rows behind many keys.
 //
 // A work item is a tile of 128 rows of a sequence, the ones with the most keys first. Two kernels:
-//   k_packed_rows  head dim 64, and short prompts at head dim 128: persistent, two CTAs to an SM, each with a row tile at a time
+//   k_packed_rows  head dim 64, and short prompts at head dim 128: persistent, two CTAs to an SM, each
+//                  with a row tile at a time
 //   k_packed128    long prompts at head dim 128: two CTAs of a cluster share every key and value tile
 //
 // Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls
 // through to the end, TMEM is released and the CTA returns.
 //
-// Where a sequence's values of a KV head are not all finite (0 times an infinity is not 0, and a product over a tile multiplies
-// keys that a row does not see by 0) or differ too much for fp16, its rows are computed from the inputs as given, on the FP32
-// pipe, each over exactly the keys it sees; and so are rows of scores too large for P's range.
+// Where a sequence's values of a KV head are not all finite (0 times an infinity is not 0, and a product
+// over a tile multiplies keys that a row does not see by 0) or differ too much for fp16, its rows are
+// computed from the inputs as given, on the FP32 pipe, each over exactly the keys it sees; and so are rows
+// of scores too large for P's range.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -52,11 +54,13 @@ constexpr int kThreads = 32 * (kSoftmaxWarps + 4);
 // registers per thread: at launch, then after setmaxnreg of a softmax and of a loader / MMA thread
 constexpr int kRegs = 168, kSoftmaxRegs = 200, kOtherRegs = 104;
 static_assert(2 * kSoftmaxRegs + kOtherRegs == 3 * kRegs, "the shares of the three warpgroups add up to the launch's");
-// The reference m of a row moves only when its maximum grows by more than kLazyLog2. P = 2^(s - m + kAboveLog2) stays below 2^15 and
-// keeps fp16's 11 bits down to 2^-21 of the reference: rows whose weight goes to one key with next to no value are made of such.
+// The reference m of a row moves only when its maximum grows by more than kLazyLog2. P = 2^(s - m +
+// kAboveLog2) stays below 2^15 and keeps fp16's 11 bits down to 2^-21 of the reference: rows whose weight
+// goes to one key with next to no value are made of such.
 constexpr float kLazyLog2 = 7.f, kAboveLog2 = 7.f;
-// P's exponent is rounded once, the maximum behind m was rounded as a product: up to here they agree well enough for P's bound. Rows
-// that pass it (no model's do) are computed on the FP32 pipe, where products are rounded alike.
+// P's exponent is rounded once, the maximum behind m was rounded as a product: up to here they agree well
+// enough for P's bound. Rows that pass it (no model's do) are computed on the FP32 pipe, where products are
+// rounded alike.
 constexpr float kFarLog2 = 0x1p23f;
 constexpr uint32_t kTmemCols = 512;
 
@@ -91,7 +95,8 @@ __device__ __forceinline__ float row_max(const float (&sv)[BN])
     }
     return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
 }
-// P = 2^(s sc - mu + kAboveLog2) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the weights before they are rounded
+// P = 2^(s sc - mu + kAboveLog2) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the
+// weights before they are rounded
 template <int C0 = 0, int C1 = BN>
 __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, float mu, uint32_t (&hw)[BN / 2])
 {
@@ -134,8 +139,8 @@ __device__ __forceinline__ void store_row(const PackedArgs &a, int h, int64_t ro
     if (a.lse != nullptr) a.lse[h * a.q_total + row] = (m + log2f(l)) * kLn2;
     if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row] = make_float2(m, inverse_sum(l));
 }
-// The same of a row that is computed from the inputs as given: the key weights take their scores from tiles, so the maximum that
-// goes with them is the tiles' own (`top`), and only the sum the row's.
+// The same of a row that is computed from the inputs as given: the key weights take their scores from
+// tiles, so the maximum that goes with them is the tiles' own (`top`), and only the sum the row's.
 __device__ __forceinline__ void store_top(const PackedArgs &a, int h, int64_t row, float top)
 {
     if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row].x = top;
@@ -146,11 +151,12 @@ __device__ __forceinline__ void store_given(const PackedArgs &a, int h, int64_t 
     if (a.row_stat != nullptr) a.row_stat[h * a.q_total + row].y = inverse_sum(l);
 }
 
-// Rows on the FP32 pipe from the inputs as given: kGivenRows of them from i0 on, then those `step` later, up to row i1 of the
-// item's sequence, by one warp over the keys that each sees (a lane per key for the scores, per channels for the outputs), through
-// kGivenFloats of shared memory. With `stats` the other outputs too, else those of the tiles stand: a row's maximum and sum do not
-// depend on the values. 8,192 tokens of one prompt, one of two KV heads so: 8.3 ms (eight rows together 5.5, but the row
-// tiles then took 1.5 % more for their registers; a row by itself 120).
+// Rows on the FP32 pipe from the inputs as given: kGivenRows of them from i0 on, then those `step` later,
+// up to row i1 of the item's sequence, by one warp over the keys that each sees (a lane per key for the
+// scores, per channels for the outputs), through kGivenFloats of shared memory. With `stats` the other
+// outputs too, else those of the tiles stand: a row's maximum and sum do not depend on the values. 8,192
+// tokens of one prompt, one of two KV heads so: 8.3 ms (eight rows together 5.5, but the row tiles then
+// took 1.5 % more for their registers; a row by itself 120).
 constexpr int kGivenRows = 4;
 template <int D>
 constexpr int kGivenFloats = kGivenRows * D + 32 * kGivenRows;
@@ -268,13 +274,14 @@ struct PackedMaps {
     CUtensorMap q, k, v, out;
 };
 
-// The kernels that lay out the values (k_values_f16) have finished. Ahead of it run the start-up and, as nothing before this
-// call is still running (see there), the copies of queries and keys and the first scores.
+// The kernels that lay out the values (k_values_f16) have finished. Ahead of it run the start-up and, as
+// nothing before this call is still running (see there), the copies of queries and keys and the first
+// scores.
 __device__ __forceinline__ void values_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // O of 32 rows (a warp's) x OC columns from TMEM, normalised, into the warp's part of shared memory, row by
-// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv 0) become zeros whatever
-// the columns hold.
+// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv
+// 0) become zeros whatever the columns hold.
 template <int OC, typename TOut>
 __device__ __forceinline__ void stage_out(unsigned char *stage, uint32_t t_o, float inv)
 {
@@ -366,14 +373,14 @@ struct Lay128 {
 //   warps 9, 10     (first CTA) issue tcgen05.mma: the score tile S into a double-buffered TMEM score
 //                   tile, and O += P V (A = P in TMEM, double-buffered) into the TMEM output tile;
 //   warps 0-7       two groups of four warps, one thread per row in each, on alternate key tiles:
-//                   scores from TMEM, causal cut (only where a warp's rows end inside the tile), maximum, fp32 online
-//                   softmax from the reference maximum that the other group hands over, O rescaled in
-//                   TMEM only when the maximum grew by more than 2^8, P into TMEM.
+//                   scores from TMEM, causal cut (only where a warp's rows end inside the tile),
+//                   maximum, fp32 online softmax from the reference maximum that the other group hands
+//                   over, O rescaled in TMEM only when the maximum grew by more than 2^7, P into TMEM.
 // TMEM: S 2 x 128 columns, O 128, P 2 x 64: all 512.
 //
-// Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles. One prompt of 32,768 tokens
-// at 12 / 2 heads: 1.96 ms, 1.68 PFLOP/s (cuBLAS 1.89 in a burst and 1.70 under the power limit), the pipe 87 % busy from the
-// first CTA to the last.
+// Bounded by the tensor pipe: a tile pair takes 16 products of 256 x 128 x 16, 1,024 cycles. One prompt of
+// 32,768 tokens at 12 / 2 heads: 1.96 ms, 1.68 PFLOP/s (cuBLAS 1.89 in a burst and 1.70 under the power
+// limit), the pipe 87 % busy from the first CTA to the last.
 template <typename TOut>
 __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant__ PackedArgs a, const __grid_constant__ PackedMaps maps)
 {
@@ -390,8 +397,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned int *const gave_up = &g_ris_packed_error;
 
-    // ---- the cluster's item: with an even group 128 rows of two heads, else 256 rows of one (rank 1 the second half,
-    // which may hold no rows)
+    // ---- the cluster's item: with an even group 128 rows of two heads, else 256 rows of one (rank 1 the
+    // second half, which may hold no rows)
     const int rank = (int)(blockIdx.x & 1);
     const bool head_pair = (a.G & 1) == 0;
     const unsigned n_h = (unsigned)(head_pair ? a.Hq / 2 : a.Hq), c = blockIdx.x / 2, r2 = c / n_h;
@@ -455,9 +462,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_packed128(const __grid_constant
         values_ready();
         if (lane == 0 && first_loads) {
             // (The query tile and the first keys were requested above.) Keys of tile j once the score
-            // products of tile j - NSK are done, values of tile j once the value product of tile j - NSV is: the loader
-            // waits on the barriers that announce those products (S_FULL, PV_DONE). The score
-            // products of tile t + 1 finish before the value product of tile t, so in this order no
+            // products of tile j - NSK are done, values of tile j once the value product of tile j - NSV
+            // is: the loader waits on the barriers that announce those products (S_FULL, PV_DONE). The
+            // score products of tile t + 1 finish before the value product of tile t, so in this order no
             // wait holds up a load that could go before it.
             int nk = 1, nv = 0;  // tiles whose keys / values were requested
             auto load_k = [&](int j) -> bool {
@@ -795,8 +802,8 @@ struct LayRows {
     //   K_FREE, V_FREE, Q_FREE  the products that read it are done
     //   I_FULL, I_FREE          a unit's description is there / every role has read it
     // and one phase per key tile:
-    //   S_GO    the last scores have been read out of their buffer (only where P has its own columns: else the value product
-    //           before has to be done, which says that too)
+    //   S_GO    the last scores have been read out of their buffer (only where P has its own columns:
+    //           else the value product before has to be done, which says that too)
     //   S_FULL  the next are there
     //   P_GO    P is written (and O rescaled where needed)
     //   PV_DONE O has settled, P's buffer is free
@@ -841,8 +848,8 @@ struct Units {
     }
 };
 
-// The rows of this CTA's units that are to be computed from the inputs as given: all of a unit's where the values ask for it, a
-// warp's own 32 where their scores did (a.far).
+// The rows of this CTA's units that are to be computed from the inputs as given: all of a unit's where the
+// values ask for it, a warp's own 32 where their scores did (a.far).
 template <int D, typename TOut>
 __device__ __noinline__ void units_as_given(const PackedArgs &a, int warp, float *mem)
 {
@@ -859,18 +866,19 @@ __device__ __noinline__ void units_as_given(const PackedArgs &a, int warp, float
     }
 }
 
-// Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns). A row tile of
-// few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and the two CTAs
-// fill each other's; the loaders and issuing warps run on into the next unit while the last one is finished; the outputs
-// leave by TMA. 64 prompts of 256 tokens take 40 us at 12 heads of 128, 57 at 32 heads of 64; with a CTA (head dim 128: a
-// cluster) per unit they took 96 and 111. At head dim 64 a key tile's products and its 16,384
-// exponentials each take 512 cycles; it takes 1,050 an SM over 16,384 tokens (issue slots 57 %, exponentials 49 %, tensor pipe 49 %
-// busy; 9 prompts of 16,233 tokens at 32 / 4 heads 188 us). It is the softmax warps' own chain at two warps
-// to a scheduler, 2,110 cycles a tile: 1,000 for the weights (512 of exponentials, the other warp's in between), 390 for the maximum, 310
-// for the tensor memory's loads and stores with their fences, 350 from the loop's end to the next scores; half the products' work would take
-// 1 % less time, no exponentials 18 %. Sixteen softmax warps to an SM instead of eight took 1,170, no maximum ahead of the
-// weights 1,090. At head dim 128 the products of a CTA
-// read as much shared memory as there is bandwidth, and long prompts go to k_packed128.
+// Persistent, two CTAs to an SM, each with one row tile at a time and one softmax group (TMEM 256 columns).
+// A row tile of few keys is a chain of waits (copies, scores, softmax, value product, outputs: 5 us), and
+// the two CTAs fill each other's; the loaders and issuing warps run on into the next unit while the last
+// one is finished; the outputs leave by TMA. 64 prompts of 256 tokens take 40 us at 12 heads of 128, 58 at
+// 32 heads of 64; with a CTA (head dim 128: a cluster) per unit they took 96 and 111. At head dim 64 a key
+// tile's products and its 16,384 exponentials each take 512 cycles; it takes 1,050 an SM over 16,384 tokens
+// (issue slots 57 %, exponentials 49 %, tensor pipe 49 % busy; 9 prompts of 16,233 tokens at 32 / 4 heads
+// 188 us). It is the softmax warps' own chain at two warps to a scheduler, 2,110 cycles a tile: 1,000 for
+// the weights (512 of exponentials, the other warp's in between), 390 for the maximum, 310 for the tensor
+// memory's loads and stores with their fences, 350 from the loop's end to the next scores; half the
+// products' work would take 1 % less time, no exponentials 18 %. Sixteen softmax warps to an SM instead of
+// eight took 1,170, no maximum ahead of the weights 1,090. At head dim 128 the products of a CTA read as
+// much shared memory as there is bandwidth, and long prompts go to k_packed128.
 //
 //   warp 4  the units, query and key tiles, warp 5 value tiles (TMA);
 //   warp 6  S = Q K^T as soon as its columns are free, warp 7 O += P V;
@@ -987,8 +995,9 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
                 for (int i = max(0, nv - NSV); i < nv; ++i) mbar_wait_own<1>(bar(L::B_V_FULL + i % NSV), (i / NSV) & 1);
             }
         } else if (ok) {
-            // The issuing warps, all lanes: trip counts and addresses come out of warp-wide reductions, which leave them in
-            // uniform registers; a product whose operands are in the lanes' registers costs more time to issue than to run.
+            // The issuing warps, all lanes: trip counts and addresses come out of warp-wide reductions,
+            // which leave them in uniform registers; a product whose operands are in the lanes' registers
+            // costs more time to issue than to run.
             const uint32_t tb = __reduce_max_sync(0xFFFFFFFFu, tmem);
             int t = 0, nq = 0;  // tiles; units with keys
             for (int u = 0;; ++u) {
@@ -1043,7 +1052,8 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
                 if (!ok) break;
                 ++nq;
             }
-            // every commit of this warp has arrived before the CTA ends (after a wait that gave up, those of the tiles issued)
+            // every commit of this warp has arrived before the CTA ends (after a wait that gave up, those
+            // of the tiles issued)
             if (lane == 0 && t > 0) {
                 const int done = warp == kScores ? L::B_S_FULL : L::B_PV_DONE, free = warp == kScores ? L::B_K_FREE : L::B_V_FREE;
                 const int ring = warp == kScores ? NSK : NSV;
@@ -1118,8 +1128,9 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
                     there = mbar_test<1>(bar(L::B_S_FULL), (t + 1) & 1);
                 }
                 l += sum + weights_of<96, BN>(sv, sc, mu, hw);
-                // P's buffer is free and O has settled once the last value product is done (where P takes the scores'
-                // place, the scores were computed after that; a unit's first tile: waited for at the end of the last unit)
+                // P's buffer is free and O has settled once the last value product is done (where P takes
+                // the scores' place, the scores were computed after that; a unit's first tile: waited for
+                // at the end of the last unit)
                 if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
                 tc_fence_after();
                 if (any_scale) {
@@ -1188,8 +1199,8 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
             }
             tc_fence_before();  // (O has been read before the next P is announced)
         }
-        // (after everything else: they take far longer than a wait of another role may; the rings are free by now, as this warp
-        // has seen the end of every product that read them)
+        // (after everything else: they take far longer than a wait of another role may; the rings are free
+        // by now, as this warp has seen the end of every product that read them)
         static_assert(kGroupWarps * kGivenFloats<D> * 4 <= L::OFF_OUT, "the rings hold every warp's part");
         __syncwarp();
         if (ok && left) units_as_given<D, TOut>(a, warp, reinterpret_cast<float *>(smem) + warp * kGivenFloats<D>);
@@ -1204,13 +1215,15 @@ __global__ void __launch_bounds__(LayRows<D>::THREADS, 2) k_packed_rows(const __
 }
 
 // ---------------------------------------------------------------- values as fp16
-// Two passes over V ahead of the attention, a CTA per (run of a sequence's keys, KV head). A row sees keys of its own
-// sequence and KV head only, so the scale is theirs: nothing that another prompt or head holds takes bits from these.
-// Within them fp16 holds a key's values to 2^-12 of its own largest (what P's rounding costs) where the keys' largest
-// values lie within 2^26 of one another. Where they do not (a key that most rows do not see may be that large), or are not
-// finite, the rows are computed from the values as given.
+// Two passes over V ahead of the attention, a CTA per (run of a sequence's keys, KV head). A row sees keys
+// of its own sequence and KV head only, so the scale is theirs: nothing that another prompt or head holds
+// takes bits from these. Within them fp16 holds a key's values to 2^-12 of its own largest (what P's
+// rounding costs) where the keys' largest values lie within 2^26 of one another. Where they do not (a key
+// that most rows do not see may be that large), or are not finite, the rows are computed from the values as
+// given.
 constexpr int kPrepThreads = 256, kPrepWarps = kPrepThreads / 32, kMostSpan = 26;
-// the pieces (16 bytes) of one head of a run's keys: this thread's piece of every kRows-th key from its first one
+// the pieces (16 bytes) of one head of a run's keys: this thread's piece of every kRows-th key from its
+// first one
 template <int D>
 struct HeadPieces {
     static constexpr int P = D / 8, kRows = kPrepThreads / P, kAhead = kPackKeys / kRows;  // (a short run's pieces at once)
@@ -1227,8 +1240,9 @@ struct HeadPieces {
         return i + row < n ? *reinterpret_cast<const uint4 *>(v + (int64_t)(i + row) * stride) : make_uint4(0u, 0u, 0u, 0u);
     }
 };
-// part[head][run] = the largest magnitude of the run's values (upper half, bf16 without the sign, so that an infinity or NaN wins)
-// and the smallest of its keys' largest ones that is not zero (lower half, 0xFFFF: every key is zero)
+// part[head][run] = the largest magnitude of the run's values (upper half, bf16 without the sign, so that
+// an infinity or NaN wins) and the smallest of its keys' largest ones that is not zero (lower half, 0xFFFF:
+// every key is zero)
 template <int D>
 __global__ void __launch_bounds__(kPrepThreads) k_values_bounds(const PackedArgs a, uint32_t *part)
 {
@@ -1265,8 +1279,9 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_bounds(const PackedArgs
         part[(int64_t)blockIdx.y * a.n_runs + blockIdx.x] = most | (least >> 16);
     }
 }
-// v16 = fp16(v 2^-E), E from the parts of the sequence's runs, and top[seq][head] as v_top. A programmatic dependent of the kernel
-// above; the attention is one of this kernel, allowed to start once every CTA here knows that nothing before this call is still running.
+// v16 = fp16(v 2^-E), E from the parts of the sequence's runs, and top[seq][head] as v_top. A programmatic
+// dependent of the kernel above; the attention is one of this kernel, allowed to start once every CTA here
+// knows that nothing before this call is still running.
 template <int D>
 __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a, const uint32_t *part, float *top, __half *v16)
 {
@@ -1297,7 +1312,8 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a,
     }
     const bool as_given = most >= 0x7F800000u || (least != 0xFFFFu && (int)(most >> 23) - (int)(least >> 7) > kMostSpan);
     if ((int)blockIdx.x == run.run0 && threadIdx.x == 0) top[(int64_t)run.seq * a.Hkv + head] = as_given ? INFINITY : __uint_as_float(most);
-    // (zeros where v16 is not to be used: a tile at a sequence's end reaches into the next one's, under weights of 0)
+    // (zeros where v16 is not to be used: a tile at a sequence's end reaches into the next one's, under
+    // weights of 0)
     const float s = as_given ? 0.f : pow2i(-value_exp(__uint_as_float(most)));
     __half *out = v16 + ((int64_t)run.first * a.Hkv + head) * D + (threadIdx.x % V::P) * 8;
     for (int i = 0;;) {
@@ -1321,12 +1337,12 @@ __global__ void __launch_bounds__(kPrepThreads) k_values_f16(const PackedArgs a,
 }
 
 // ---------------------------------------------------------------- key weights
-// What each key got from the last weight_rows rows of its sequence: w_j = sum over those rows i and the heads of its
-// KV head of 2^(s_ij - m_i) / l_i, with the maxima and sums that the attention left. One CTA per (128 keys,
-// KV head) holds the keys as the A operand and runs S^T = K Q^T over the group's heads and chunks of 64 rows: a
-// thread owns a key (a TMEM lane), so the sum over rows stays in its register. Bounded by the
-// latency of a few steps per CTA: 17 us for the last 64 rows of 9 prompts, 16,233 keys and 32 / 4 heads of 64, whose exponentials
-// alone take 3.6 (issue slots 34 % busy).
+// What each key got from the last weight_rows rows of its sequence: w_j = sum over those rows i and the
+// heads of its KV head of 2^(s_ij - m_i) / l_i, with the maxima and sums that the attention left. One CTA
+// per (128 keys, KV head) holds the keys as the A operand and runs S^T = K Q^T over the group's heads and
+// chunks of 64 rows: a thread owns a key (a TMEM lane), so the sum over rows stays in its register. Bounded
+// by the latency of a few steps per CTA: 17 us for the last 64 rows of 9 prompts, 16,233 keys and 32 / 4
+// heads of 64, whose exponentials alone take 3.6 (issue slots 34 % busy).
 //
 //   warps 0-3  one thread per key; warp 4 (TMA) the keys, then chunks of rows into a ring; warp 5 the products
 template <int DT>
@@ -1543,8 +1559,8 @@ constexpr CUtensorMapDataType kBf16 = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, kF16 = C
 
 using TileKernel = void (*)(PackedArgs, PackedMaps);
 
-// Once per kernel: its shared memory, and that its launch has the `regs` registers a thread that the softmax threads'
-// setmaxnreg would wait for.
+// Once per kernel: its shared memory, and that its launch has the `regs` registers a thread that the
+// softmax threads' setmaxnreg would wait for.
 cudaError_t prepare(TileKernel kern, int bytes, int regs)
 {
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);

@@ -1,16 +1,17 @@
 // Causal attention over packed prompts on the FP32 pipe: fp32 inputs, which never pass through a
 // narrower product, and the weight that each key got from a sequence's last rows.
 //
-// k_packed_f32: one CTA per (32 query rows, query head) walks the keys in tiles of 64 with a running maximum and
-// sum. Keys and values come row by row by cp.async into a buffer each, so that the next keys travel under the
-// value product and the next values under the scores; rows of 4 more elements than the head dim keep 16-byte reads of
-// eight neighbouring rows apart. S: a 4 x 4 patch per thread, 4 elements of d at a time as packed pairs (which leaves
-// two partial sums per score); the softmax over the 16 lanes that share a row; O += P V with a 4 x D/16
-// patch, P as pairs of the same weight in shared memory (two moves a weight otherwise).
-// Bound by the FMA pipe: 4 D flops per pair and head; shared memory reads fill three quarters of its
-// bandwidth beside it. 900 rows behind 301 keys at 12 / 2 heads of 128 take 133 us, 31 of 78 TFLOP/s: the pipe is 53 % busy while an
-// SM has work (two warps to a scheduler, each a patch of 212 registers), and a fifth of the time goes to the uneven ends. Tiles of 32 rows, because a short prompt has few of them and the one with the most keys is
-// the last to end.
+// k_packed_f32: one CTA per (32 query rows, query head) walks the keys in tiles of 64 with a running
+// maximum and sum. Keys and values come row by row by cp.async into a buffer each, so that the next keys
+// travel under the value product and the next values under the scores; rows of 4 more elements than the
+// head dim keep 16-byte reads of eight neighbouring rows apart. S: a 4 x 4 patch per thread, 4 elements of
+// d at a time as packed pairs (which leaves two partial sums per score); the softmax over the 16 lanes that
+// share a row; O += P V with a 4 x D/16 patch, P as pairs of the same weight in shared memory (two moves a
+// weight otherwise). Bound by the FMA pipe: 4 D flops per pair and head; shared memory reads fill three
+// quarters of its bandwidth beside it. 900 rows behind 301 keys at 12 / 2 heads of 128 take 133 us, 31 of
+// 78 TFLOP/s: the pipe is 53 % busy while an SM has work (two warps to a scheduler, each a patch of 212
+// registers), and a fifth of the time goes to the uneven ends. Tiles of 32 rows, because a short prompt has
+// few of them and the one with the most keys is the last to end.
 //
 // k_packed_weights: one thread per key holds the key's row in registers and walks the last rows of the
 // group's heads, broadcast from shared memory: w_j = sum_i,h exp2(s_ij - m_i) / l_i.
@@ -63,7 +64,8 @@ __device__ __forceinline__ float2 f2_get(uint64_t v)
     return r;
 }
 
-// R rows of one head from memory to rows of pitch D + 4 (PAD) or D in shared memory, asynchronously; rows past `rows` as zeros
+// R rows of one head from memory to rows of pitch D + 4 (PAD) or D in shared memory, asynchronously; rows
+// past `rows` as zeros
 template <int R, int D, bool PAD>
 __device__ __forceinline__ void fetch_rows(float *dst, const float *x, int64_t stride, int rows)
 {
@@ -88,8 +90,8 @@ __global__ void __launch_bounds__(kThreads, 2) k_packed_f32(const PackedArgs a)
     constexpr int LK = D + 4;
     extern __shared__ __align__(16) float sm[];
     float *const qs = sm, *const ks = qs + BM * LK, *const vs = ks + BN * LK, *const ps = vs + BN * D;
-    // (what follows is not let in early: its CTAs, in the places of those that end first, would upset the order by length of a
-    // next call's: 157 us instead of 135)
+    // (what follows is not let in early: its CTAs, in the places of those that end first, would upset the
+    // order by length of a next call's: 157 us instead of 135)
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int b = blockIdx.x, h = b % a.Hq, part = kParts - 1 - b / a.Hq % kParts;
     const PackItem it = a.items[b / a.Hq / kParts];

@@ -1,11 +1,10 @@
 // Cutting a cache back to a budget by accumulated attention weight.
 //
 // Of the slots of a (sequence, KV head) the `budget` first in this order stay: those of the newest
-// positions (within `recent` of the newest one), then by weight, then by slot. The keys are rotated and carry their
-// positions, so slots need no order: a kept slot below the budget stays where it is, and the i-th
-// kept one above it moves into the i-th freed one, which moves no more rows than have to move and
-// lets every row move at once, in place too (all sources lie at or above the budget, all targets
-// below it).
+// positions (within `recent` of the newest one), then by weight, then by slot. The keys are rotated and
+// carry their positions, so slots need no order: a kept slot below the budget stays where it is, and the
+// i-th kept one above it moves into the i-th freed one, which moves no more rows than have to move and lets
+// every row move at once, in place too (all sources lie at or above the budget, all targets below it).
 #include <cstdint>
 
 #include "serve.h"
@@ -80,13 +79,13 @@ __device__ __forceinline__ Pair block_scan(Pair v, Pair &total, Pair *part)
     return {(warp ? bx : 0) + inc.x - v.x, (warp ? by : 0) + inc.y - v.y};
 }
 
-// One cluster of `size` CTAs per (sequence, KV head), each with a run of its slots: the newest position, then the
-// threshold weight by three passes of a radix select (histograms in shared memory, summed over the cluster
-// by every CTA for itself), then the lists. A slot's order and position are read from memory once and
-// stay in shared memory (CACHED). Ties at the threshold go to the lowest slots: the last histogram says how many of
-// them each CTA holds. holes: [B * Hkv][budget] scratch, the freed slots in order. Bound by latency: seven
-// cluster barriers and about as many block scans, 31 us for 16 x 2 lists of 20,000 to 32,768 slots (7 MB). One
-// CTA to a list took 58 us (the atomics on one SM's shared memory).
+// One cluster of `size` CTAs per (sequence, KV head), each with a run of its slots: the newest position,
+// then the threshold weight by three passes of a radix select (histograms in shared memory, summed over the
+// cluster by every CTA for itself), then the lists. A slot's order and position are read from memory once
+// and stay in shared memory (CACHED). Ties at the threshold go to the lowest slots: the last histogram says
+// how many of them each CTA holds. holes: [B * Hkv][budget] scratch, the freed slots in order. Bound by
+// latency: seven cluster barriers and about as many block scans, 31 us for 16 x 2 lists of 20,000 to 32,768
+// slots (7 MB). One CTA to a list took 58 us (the atomics on one SM's shared memory).
 template <bool CACHED>
 __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs a, int32_t *holes, int size)
 {
@@ -170,8 +169,9 @@ __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs
             }
             cluster_sync();
         }
-        // The cluster's histogram: each CTA adds up its share of the bins over the CTAs, then takes all shares. (All of
-        // every CTA's bins by every CTA is size times the traffic: 8 CTAs of 4,096 slots 97 us instead of 31.)
+        // The cluster's histogram: each CTA adds up its share of the bins over the CTAs, then takes all
+        // shares. (All of every CTA's bins by every CTA is size times the traffic: 8 CTAs of 4,096 slots 97
+        // us instead of 31.)
         const int share = kBins / size;
         if (size > 1) {
             for (int i = tid; i < share; i += kThreads) {
@@ -258,10 +258,12 @@ __global__ void __launch_bounds__(kThreads) k_evict_select(const Cache4EvictArgs
     }
 }
 
-// Moves the rows: four lanes to a slot of the target. In place only what moves. Bound by HBM: a row's codes, scales, position and
-// weight are read once and written once, though the pieces of a row that is not next to the last one are parts of 32-byte sectors
-// (256 bytes fetched for 152 at head dim 128). One slot to a thread, so that the launch has threads enough to keep
-// the loads in flight: 51 us an eviction of 16 x 2 lists of 20,000 to 32,768 slots to 8,192, with two slots 53, with four 60.
+// Moves the rows: four lanes to a slot of the target. In place only what moves. Bound by HBM: a row's
+// codes, scales, position and weight are read once and written once, though the pieces of a row that is not
+// next to the last one are parts of 32-byte sectors (256 bytes fetched for 152 at head dim 128). One slot
+// to a thread, so that the launch has threads enough to keep the loads in flight: 54 us an eviction of 16 x
+// 2 lists of 20,000 to 32,768 slots to 8,192 (on a board where it took 51, two slots took 53, which is
+// within what boards differ, and four 60).
 constexpr int kMoveThreads = 256, kMoveSlots = kMoveThreads / 4;
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) k_evict_move(const Cache4EvictArgs a, int blocks)

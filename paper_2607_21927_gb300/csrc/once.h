@@ -7,8 +7,8 @@
 
 namespace ris {
 
-// Function attributes hold for the device that was current when they were set. Tried again where it failed; on devices
-// past the table every time.
+// Function attributes hold for the device that was current when they were set. Tried again where it failed;
+// on devices past the table every time.
 struct Once {
     static constexpr int kDevices = 64;
     std::atomic<bool> done[kDevices] = {};

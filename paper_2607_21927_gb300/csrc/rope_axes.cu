@@ -4,14 +4,14 @@
 // y_c = m (x_c cos a - x_{c+D/2} sin a), y_{c+D/2} = m (x_{c+D/2} cos a + x_c sin a) with a = f_c
 // pos[axis(c)][token]; the transposed rotation (inverse) turns by -a and is the gradient's.
 //
-// One thread takes V = 16 / sizeof(T) frequencies of a token (16-byte accesses of both halves of a
-// head), forms their sines and cosines once and turns every head of its slice. Angles are 64-bit fixed-point fractions of a
-// turn, as in the layer calls' rotation: exact at any int32 position, where a product in fp32 is off by
-// 1e-3 at position 30,000. Bound by HBM: each element read once and written once; the sines and cosines
-// (about 40 instructions each) are shared by the heads. The heads are sliced over CTAs only where the
-// tokens alone leave SMs without work, since every slice repeats the sines and cosines.
-// 30,011 tokens of 12 and 2 heads of 128 in bf16 on three axes take 37.7 us, 5.7 TB/s of the 6.8 that a copy reaches; 24 tokens
-// are a launch's latency.
+// One thread takes V = 16 / sizeof(T) frequencies of a token (16-byte accesses of both halves of a head),
+// forms their sines and cosines once and turns every head of its slice. Angles are 64-bit fixed-point
+// fractions of a turn, as in the layer calls' rotation: exact at any int32 position, where a product in
+// fp32 is off by 1e-3 at position 30,000. Bound by HBM: each element read once and written once; the sines
+// and cosines (about 40 instructions each) are shared by the heads. The heads are sliced over CTAs only
+// where the tokens alone leave SMs without work, since every slice repeats the sines and cosines. 30,011
+// tokens of 12 and 2 heads of 128 in bf16 on three axes take 37.7 us, 5.7 TB/s of the 6.8 that a copy
+// reaches; 24 tokens are a launch's latency.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -81,8 +81,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_rope_axes(const RopeAxesArgs a)
         const int64_t at = p * (out ? (int64_t)a.heads[w] * a.D : a.stride[w]) + (h - w * a.heads[0]) * a.D + c;
         return (out ? reinterpret_cast<T *>(a.y[w]) : reinterpret_cast<T *>(const_cast<void *>(a.x[w]))) + at;
     };
-    // kBatch heads' loads ahead of what is stored before them in time (which the compiler may not reorder: they may
-    // be in place), the first ahead of the sines and cosines
+    // kBatch heads' loads ahead of what is stored before them in time (which the compiler may not reorder:
+    // they may be in place), the first ahead of the sines and cosines
     Vec<T> u[kBatch], v[kBatch];
     auto load = [&](int h) {
 #pragma unroll

@@ -80,8 +80,8 @@ struct PackedArgs {
 // fp32 inputs: items of kPackRows rows.
 cudaError_t launch_packed_f32(const PackedArgs &a, int D, int out_dtype, cudaStream_t s);
 cudaError_t launch_packed_weights_f32(const PackedArgs &a, int D, cudaStream_t s);
-// bf16 inputs: items of kPackRows rows, or for clusters (head dim 128) with an odd group of 2 kPackRows; scratch
-// of packed_scratch_bytes, 256-byte aligned.
+// bf16 inputs: items of kPackRows rows, or for clusters (head dim 128) with an odd group of 2 kPackRows;
+// scratch of packed_scratch_bytes, 256-byte aligned.
 size_t packed_scratch_bytes(const PackedArgs &a, int32_t head_dim);
 cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s);
 cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s);
@@ -144,12 +144,13 @@ struct Cache4EvictArgs {
 // holes: scratch [B * Hkv][budget]
 cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaStream_t s);
 
-// The device error words of the cache's kernels (bit 1: tokens appended past the capacity, bit 2: a bounded wait gave up) and of
-// the packed attention's tile kernels (a bounded wait gave up), on the current device.
+// The device error words of the cache's kernels (bit 1: tokens appended past the capacity, bit 2: a bounded
+// wait gave up) and of the packed attention's tile kernels (a bounded wait gave up), on the current device.
 cudaError_t cache4_error_word(unsigned int **p);
 cudaError_t packed_error_word(unsigned int **p);
 
-// What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked; whether loads are left out.
+// What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked;
+// whether loads are left out.
 int64_t debug_wait_limit();
 int32_t debug_no_loads();
 
@@ -157,9 +158,10 @@ int32_t debug_no_loads();
 cudaError_t library_alloc(void **p, size_t bytes, cudaStream_t s);
 
 #ifdef __CUDACC__
-// The serving kernels are a few microseconds each, one after another: each is launched while the last one runs
-// (a programmatic dependent) and waits for it where it begins, so that only the launch itself overlaps: nothing is read
-// or written before `after_last` returns. Its own dependent may start from there on.
+// The serving kernels are a few microseconds each, one after another: each is launched while the last one
+// runs (a programmatic dependent) and waits for it where it begins, so that only the launch itself
+// overlaps: nothing is read or written before `after_last` returns. Its own dependent may start from there
+// on.
 __device__ __forceinline__ void after_last()
 {
     asm volatile("griddepcontrol.wait;" ::: "memory");

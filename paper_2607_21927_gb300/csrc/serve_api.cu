@@ -27,8 +27,8 @@ struct ris_pack_s {
     int32_t n_items = 0, n_pairs = 0, n_key_items = 0, n_runs = 0;
     int64_t key_tiles = 0;  // of 128 x 128 that the items of 128 rows see
     cudaStream_t stream = nullptr;
-    // Streams other than its own that calls with it were queued on, each with an event behind the last of them: its memory
-    // is given back behind these.
+    // Streams other than its own that calls with it were queued on, each with an event behind the last of
+    // them: its memory is given back behind these.
     std::mutex mu;
     std::vector<std::pair<cudaStream_t, cudaEvent_t>> used;
     bool unknown = false;  // a use could not be noted: the device is waited for
@@ -80,7 +80,8 @@ struct Scratch {
     }
 };
 
-// Notes that a call queues work with the pack on `s`, behind that work: when the call returns, whether it succeeds or not.
+// Notes that a call queues work with the pack on `s`, behind that work: when the call returns, whether it
+// succeeds or not.
 struct PackUse {
     ris_pack_s *pack;
     cudaStream_t s;
@@ -190,11 +191,11 @@ int64_t keys_of(const PackItem &it, int step)
     return std::max<int64_t>(0, std::min<int64_t>(last, it.k_len));
 }
 
-// Head dim 128, bf16: whether a pack's row tiles see so many key tiles (24 on average, about 6,000 tokens of one prompt)
-// that two CTAs sharing every key tile beat two independent ones on each SM, which finish a row tile and start the next
-// one with less delay. us a call of 16,384 to 18,432 tokens, clusters / rows: prompts of 256 tokens 86 / 41, of 1024 107 / 67,
-// of 4096 183 / 163, of 6144 254 / 259, of 8192 275 / 299, of 16384 465 / 565 (12 / 2 heads; 8 / 8 heads: of 4096 138 / 126, of
-// 8192 201 / 220).
+// Head dim 128, bf16: whether a pack's row tiles see so many key tiles (24 on average, about 6,000 tokens
+// of one prompt) that two CTAs sharing every key tile beat two independent ones on each SM, which finish a
+// row tile and start the next one with less delay. us a call of 16,384 to 18,432 tokens, clusters / rows:
+// prompts of 256 tokens 86 / 41, of 1024 107 / 67, of 4096 183 / 163, of 6144 254 / 259, of 8192 275 / 299,
+// of 16384 465 / 565 (12 / 2 heads; 8 / 8 heads: of 4096 138 / 126, of 8192 201 / 220).
 bool packed_by_clusters(const ris_pack_s *pack) { return pack->key_tiles >= 24LL * pack->n_items; }
 
 // The items of `step` rows (or keys) of every sequence; of rows, those with the most keys first, so that the
