@@ -461,7 +461,7 @@ ris_status ris_rope_axes(const void *q, const void *k, void *q_out, void *k_out,
  * row's largest; values as fp16 scaled by a power of two of their (sequence, KV head), exact down to 2^-30 of
  * its largest, and to 2^-12 of the key's own largest where that lies lower. Where the keys' largest values of
  * a (sequence, KV head) lie more than 2^26 apart or are not finite, and for rows of scores beyond 2^23, the
- * rows are computed on the FP32 pipe instead: some 50 times slower.
+ * rows are computed on the FP32 pipe instead: about a hundred times slower.
  * Errors: RIS_ERR_INVALID, RIS_ERR_UNSUPPORTED (more row tiles x heads than a grid holds), RIS_ERR_OOM,
  * RIS_ERR_CUDA. */
 ris_status ris_attention_packed(ris_pack_t pack, const void *q, const void *k, const void *v, void *out, int32_t heads,
