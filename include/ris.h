@@ -320,7 +320,8 @@ int32_t ris_attention_design(ris_mask_t mask, int32_t dtype, int32_t head_dim);
 
 /* Synchronise `stream` and report (then clear) the device error words: RIS_ERR_DEVICE_TIMEOUT
  * if a kernel's bounded wait gave up since the last call, RIS_ERR_INVALID if a decode step
- * read a position outside [t0, cache_len) from device memory or tokens did not fit a 4-bit cache, else RIS_OK. A kernel that sets
+ * read a position outside [t0, cache_len) from device memory, tokens did not fit a 4-bit cache, or tokens or keys
+ * lie outside a cache's pages, else RIS_OK. A kernel that sets
  * a word skips the rest of its work, so outputs of that launch are undefined. Blocks.
  * Errors: RIS_ERR_CUDA. */
 ris_status ris_device_status(void *stream);
@@ -534,6 +535,82 @@ ris_status ris_cache4_attend(const ris_cache4 *cache, const void *q, int32_t hea
  * 0 <= recent < budget. Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
 ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_t budget, int32_t recent, int32_t *kept,
                             void *stream);
+
+/* ---- Normed heads, and a cache in pages ---------------------------------------------------------
+ * The serving path of models that norm their queries and keys, and of servers that hand out memory by the
+ * page (the paper has no counterpart).
+ *
+ * RMS norm of every head of q [n][heads][head_dim] and k [n][kv_heads][head_dim] (k may be NULL with kv_heads
+ * 0), then the rotation to the token's position, in one pass: with r = (mean of the head's x^2 + eps)^-1/2,
+ * z = x r weight; of z's first rot_dim channels (a multiple of 16; 0: head_dim) the pairs (c, c + rot_dim / 2),
+ * or with pairs = 1 the neighbours (2c, 2c + 1), are turned by the angle of frequency c at positions[i] and
+ * scaled by the rope's mscale; the other channels are z. The frequencies are those of a head of rot_dim
+ * channels, their extension factor resolved for n_ctx tokens (ris_rope_freqs). q_weight, k_weight: DEVICE
+ * [head_dim] of `dtype`, NULL: that tensor is not normed. rope NULL or of kind NONE: no rotation (positions may
+ * be NULL, rot_dim is 0). positions: DEVICE int32 [n], of either sign. All strides are elements from token to
+ * token, as in ris_rope_axes; an output may be its input (with the same stride), so that rows of a fused
+ * projection are normed in place, and else must not overlap it.
+ * Statistics and products in fp32, angles exact at any position; bf16 results rounded once, to nearest even.
+ *
+ * The gradient: dq, dk of q_out, k_out; gq, gk of q, k (gq may be dq or q, with the same stride, gk alike); gq_weight,
+ * gk_weight fp32 [head_dim], for each weight that there is, summed over all tokens and heads in a fixed order (zeros
+ * for n = 0). q, k are the call's inputs as they were (not asked for where there is no weight).
+ * Errors: RIS_ERR_INVALID, RIS_ERR_OOM (gradient), RIS_ERR_CUDA. */
+ris_status ris_norm_rope(const void *q, const void *k, void *q_out, void *k_out, int32_t dtype, int64_t n, int32_t heads,
+                         int32_t kv_heads, int32_t head_dim, int64_t q_stride, int64_t k_stride, int64_t q_out_stride,
+                         int64_t k_out_stride, const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
+                         int32_t rot_dim, int32_t pairs, int64_t n_ctx, const ris_rope_cfg *rope, void *stream);
+ris_status ris_norm_rope_backward(const void *dq, const void *dk, const void *q, const void *k, void *gq, void *gk, float *gq_weight,
+                                  float *gk_weight, int32_t dtype, int64_t n, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                  int64_t dq_stride, int64_t dk_stride, int64_t q_stride, int64_t k_stride, int64_t gq_stride,
+                                  int64_t gk_stride, const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
+                                  int32_t rot_dim, int32_t pairs, int64_t n_ctx, const ris_rope_cfg *rope, void *stream);
+
+/* A K/V cache in pages of page_size slots: caller-owned DEVICE arrays. Slot t of sequence b, which is the
+ * sequence's token t, lies in page table[b][t / page_size], and its head g there at
+ *     k (v) + page * page_stride + g * head_stride + (t mod page_size) * slot_stride    (elements)
+ * so that [pages][kv_heads][page_size][head_dim], [pages][page_size][kv_heads][head_dim] and pools of keys
+ * and values side by side all do. Sequences may share pages that none of them writes. Entries of the table
+ * that a call does not reach may hold anything, and so may slots at and past length[b]. Calls on one cache
+ * must be ordered on the GPU. */
+typedef struct {
+    int32_t batch;      /* sequences, 1 .. 65535 */
+    int32_t kv_heads;   /* 1 .. 4096 */
+    int32_t head_dim;   /* 64 or 128 */
+    int32_t page_size;  /* a power of two, 16 .. 1024 */
+    int32_t dtype;      /* RIS_F32 or RIS_BF16 */
+    int32_t n_pages;    /* of the pools */
+    int32_t table_len;  /* pages that a sequence can have; table_len * page_size <= 2^30 */
+    int32_t reserved;   /* must be 0 */
+    int64_t page_stride, head_stride, slot_stride;  /* each at least head_dim and a multiple of 16 bytes */
+    void *k, *v;        /* 16-byte aligned */
+    const int32_t *table;  /* [batch][table_len] */
+    int32_t *length;    /* [batch] slots in use */
+} ris_paged;
+
+/* Append the rows of a pack (its q side; sequence s to row s of the batch): k and v [q_total][kv_heads]
+ * [head_dim] of the cache's dtype, token strides in elements. Token i of sequence b goes to slot start[b] + i and length[b]
+ * becomes start[b] + q_lens[b], cut to 0 .. the sequence's slots; start NULL: after the slots in use. start (DEVICE
+ * int32 [batch]) must not be the cache's length. Tokens at a negative slot, past the table or in an entry that is
+ * no page are left out and reported by ris_device_status as RIS_ERR_INVALID. A pack of ones is a decode step's append.
+ * Errors: RIS_ERR_INVALID, RIS_ERR_CUDA. */
+ris_status ris_paged_append(const ris_paged *cache, ris_pack_t pack, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                            const int32_t *start, void *stream);
+
+/* Attention of a pack's rows (its q side) over the pages: q [q_total][heads][head_dim] (rotated), token stride
+ * in elements; out [q_total][heads][head_dim] contiguous, both of the cache's dtype; lse optional
+ * [heads][q_total]; scores scaled by 1 / sqrt(head_dim). The rows are the last of their sequence's slots in use
+ * (append them first): row i of sequence b is at p = length[b] - q_lens[b] + i and sees the keys j <= p that
+ * have j > p - window or j < anchors; window 0: all of them (anchors is 0). Pages that no row sees are not
+ * read, nor are their table entries. A row that sees no key (p < 0) gets zeros and a log-sum-exp of -infinity.
+ * longest: an upper bound of the lengths that the caller knows (longer ones count as that long), 0 for the
+ * table's. Nothing in the launches depends on the lengths, so a captured graph can be replayed as they grow.
+ * One token, a few drafted ones and chunks of prompts may stand in one pack, any heads / kv_heads.
+ * An entry of the table that is needed and no page is reported by ris_device_status as RIS_ERR_INVALID (the rows
+ * that see it are then undefined). A key that a row does not see takes no part in it, whatever it holds.
+ * Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
+ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void *q, int64_t q_stride, int32_t heads, int32_t window,
+                            int32_t anchors, int64_t longest, void *out, float *lse, void *stream);
 
 /* ---- Measurement support (the paper has no counterpart) -------------------------------------
  * Small kernels that measure the ceilings the attention kernels are compared against, for the

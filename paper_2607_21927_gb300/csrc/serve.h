@@ -86,6 +86,88 @@ size_t packed_scratch_bytes(const PackedArgs &a, int32_t head_dim);
 cudaError_t launch_packed_tiles(PackedArgs a, int D, int out_dtype, bool clusters, void *scratch, cudaStream_t s);
 cudaError_t launch_packed_weights_tc(const PackedArgs &a, int D, cudaStream_t s);
 
+// Queries and keys normed per head and turned (norm_rope.cu): x into y, or backwards dy and x into y.
+struct NormRopeArgs {
+    const void *x[2];          // q and k (k may be null: heads[1] = 0)
+    const void *dy[2];
+    void *y[2];
+    int64_t x_stride[2], dy_stride[2], y_stride[2];  // elements from one token's heads to the next's
+    int32_t heads[2];
+    int64_t n;
+    const int32_t *pos;        // [n]
+    const void *weight[2];     // [D] of the inputs' type; null: no norm
+    float eps;
+    int32_t rot;               // channels that are turned, a multiple of 16
+    uint64_t turn[kMaxHeadDimHalf];  // rotation frequencies as fractions of a turn, in 2^-64
+    float mscale;
+    int32_t ctas[2];           // gradient: CTAs of q and of k
+    float *part;               // [ctas[0] + ctas[1]][D] scratch, their sums for the weights
+};
+cudaError_t launch_norm_rope(const NormRopeArgs &a, int dtype, int D, bool pairs, cudaStream_t s);
+void norm_rope_ctas(int dtype, int D, int64_t n, const int32_t (&heads)[2], int32_t (&ctas)[2]);
+cudaError_t launch_norm_rope_backward(const NormRopeArgs &a, int dtype, int D, bool pairs, float *gq, float *gk, cudaStream_t s);
+
+// A cache in pages (paged.cu).
+struct PagedArgs {
+    void *k, *v;               // pools of n_pages pages
+    int64_t page_stride, head_stride, slot_stride;  // elements
+    const int32_t *table;      // [B][table_len]
+    int32_t *length;           // [B]
+    int32_t B, Hkv, D, page_log2;
+    int32_t n_pages, table_len;
+};
+struct PagedAppendArgs {
+    PagedArgs c;
+    const void *k, *v;
+    int64_t k_stride, v_stride;
+    const int32_t *start;      // [B] or null: the cache's lengths
+    const int32_t *off, *seq_of;  // the pack's row offsets [B + 1] and sequence of each row
+    int64_t total;
+    int32_t rows;              // of a CTA
+};
+cudaError_t launch_paged_append(PagedAppendArgs a, int dtype, cudaStream_t s);
+
+// A row tile's part that a CTA leaves for the join: parts of CTAs first .. last, -1: none.
+struct PagedSplit {
+    int32_t first, last;
+    int32_t row0, tokens;      // its first row in q / out, its tokens
+    int32_t head0, heads;      // its query heads
+    int32_t pad[2];
+};
+struct PagedItem {
+    int32_t seq, tile;
+};
+struct PagedAttendArgs {
+    PagedArgs c;
+    const void *q;
+    void *out;                 // [q_total][Hq][D]
+    float *lse;                // [Hq][q_total] or null
+    int64_t q_stride, q_total;
+    const int32_t *off;        // the pack's row offsets [B + 1]
+    int32_t Hq, G;
+    int32_t block, blocks;     // query heads of a row tile; how many such blocks a KV head has
+    int32_t tokens;            // of a row tile
+    int32_t window, anchors;   // window 0: all
+    int32_t reach;             // lengths count up to here
+    float scale_log2;
+    // the sharing out of the work (attn_paged.cuh)
+    int32_t ctas, least;       // CTAs; key tiles of one at least
+    int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
+    int64_t *prefix;           // [max_items + 1] scratch: cost of the items before
+    PagedItem *items;          // [max_items]
+    int32_t *n_items;          // [1]
+    int32_t *seq_items;        // [B] first item of each sequence
+    PagedSplit *split;         // [ctas]
+    int32_t part_rows;         // rows of a part
+    float *part_o;             // [2 ctas][part_rows][D]
+    float2 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum)
+};
+constexpr int kPagedCtas = 2 * 152;
+constexpr int kPagedRows = 32, kPagedKeys = 64;  // of a row tile, of a key tile
+cudaError_t launch_paged_plan(const PagedAttendArgs &a, cudaStream_t s);
+cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);
+cudaError_t launch_paged_f32(const PagedAttendArgs &a, int dtype, cudaStream_t s);
+
 struct Cache4Args {
     uint8_t *k, *v;              // [B][Hkv][cap][D / 2]
     uint16_t *k_scale, *v_scale; // bf16 [B][Hkv][cap][D / 32]
@@ -148,6 +230,8 @@ cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaSt
 // wait gave up) and of the packed attention's tile kernels (a bounded wait gave up), on the current device.
 cudaError_t cache4_error_word(unsigned int **p);
 cudaError_t packed_error_word(unsigned int **p);
+// Of the paged cache's kernels (a token or key outside the pages).
+cudaError_t paged_error_word(unsigned int **p);
 
 // What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked;
 // whether loads are left out.

@@ -1,6 +1,7 @@
-// C ABI of the serving operators: packed prompts, positions on several axes and the 4-bit cache.
-// Argument checks, the plan of a pack, scratch and the launches; the work is in rope_axes.cu,
-// attn_packed.cu, attn_packed_f32.cu, cache4.cu and cache4_evict.cu.
+// C ABI of the serving operators: packed prompts, positions on several axes, the 4-bit cache, normed and
+// turned heads, and the cache in pages. Argument checks, the plan of a pack, scratch and the launches; the
+// work is in rope_axes.cu, norm_rope.cu, attn_packed.cu, attn_packed_f32.cu, cache4.cu, cache4_evict.cu and
+// paged.cu.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -238,6 +239,81 @@ std::vector<PackRun> runs_of(const std::vector<int32_t> &k_off)
         }
     }
     return v;
+}
+
+// What both directions of ris_norm_rope share: checks, and the arguments but for the tensors.
+ris_status norm_rope_args(NormRopeArgs &a, int32_t dtype, int64_t n, int32_t heads, int32_t kv_heads, int32_t head_dim, const int32_t *positions,
+                          const void *q_weight, const void *k_weight, float eps, int32_t rot_dim, int32_t pairs, int64_t n_ctx,
+                          const ris_rope_cfg *rope)
+{
+    RIS_TRY(check_dtype(dtype, "dtype"));
+    if (n < 0 || n > 2147483647LL) return fail(RIS_ERR_INVALID, "n=%lld outside [0, 2^31-1]", (long long)n);
+    if (heads < 1 || kv_heads < 0 || heads > 65535 || kv_heads > 65535)
+        return fail(RIS_ERR_INVALID, "heads must be in [1, 65535], kv_heads in [0, 65535]");
+    if (head_dim != 64 && head_dim != 128) return fail(RIS_ERR_INVALID, "head_dim %d not in {64, 128}", head_dim);
+    if (pairs != 0 && pairs != 1) return fail(RIS_ERR_INVALID, "pairs must be 0 or 1");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(RIS_ERR_INVALID, "eps must be finite and >= 0");
+    if (kv_heads == 0 && k_weight != nullptr) return fail(RIS_ERR_INVALID, "k_weight without k");
+    for (const void *w : {q_weight, k_weight})
+        if (w != nullptr && !aligned(w, 16)) return fail(RIS_ERR_INVALID, "a weight is not 16-byte aligned");
+    const bool turns = rope != nullptr && rope->kind != RIS_ROPE_NONE;
+    if (!turns) {
+        if (q_weight == nullptr && k_weight == nullptr) return fail(RIS_ERR_INVALID, "neither a weight nor a rotation");
+        if (rot_dim != 0) return fail(RIS_ERR_INVALID, "rot_dim %d without a rotation", rot_dim);
+    } else {
+        if (rot_dim == 0) rot_dim = head_dim;
+        if (rot_dim < 16 || rot_dim > head_dim || rot_dim % 16 != 0)
+            return fail(RIS_ERR_INVALID, "rot_dim %d must be a multiple of 16 in [16, head_dim]", rot_dim);
+        double f[kMaxHeadDimHalf], ms = 1.0;
+        RIS_TRY(ris_rope_freqs(rope, n_ctx, rot_dim, f, &ms));
+        if (n > 0 && (positions == nullptr || !aligned(positions, 4))) return fail(RIS_ERR_INVALID, "positions is NULL or misaligned");
+        for (int c = 0; c < rot_dim / 2; ++c)  // as fractions of a turn in 2^-64
+            a.turn[c] = (uint64_t)(f[c] * (18446744073709551616.0 / 6.283185307179586476925286766559));
+        a.mscale = (float)ms;
+    }
+    a.heads[0] = heads, a.heads[1] = kv_heads;
+    a.n = n;
+    a.pos = positions;
+    a.weight[0] = q_weight, a.weight[1] = k_weight;
+    a.eps = eps;
+    a.rot = rot_dim;
+    return RIS_OK;
+}
+
+ris_status check_paged(const ris_paged *c)
+{
+    if (c == nullptr) return fail(RIS_ERR_INVALID, "cache is NULL");
+    if (c->batch < 1 || c->batch > kMaxPackSeqs) return fail(RIS_ERR_INVALID, "batch %d outside [1, %d]", c->batch, kMaxPackSeqs);
+    if (c->kv_heads < 1 || c->kv_heads > 4096) return fail(RIS_ERR_INVALID, "kv_heads %d outside [1, 4096]", c->kv_heads);
+    if (c->head_dim != 64 && c->head_dim != 128) return fail(RIS_ERR_INVALID, "head_dim %d not in {64, 128}", c->head_dim);
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0)
+        return fail(RIS_ERR_INVALID, "page_size %d must be a power of two in [16, 1024]", c->page_size);
+    RIS_TRY(check_dtype(c->dtype, "dtype"));
+    if (c->n_pages < 1 || c->table_len < 1 || c->reserved != 0) return fail(RIS_ERR_INVALID, "n_pages and table_len must be positive, reserved 0");
+    if ((int64_t)c->table_len * c->page_size > (int64_t(1) << 30))
+        return fail(RIS_ERR_INVALID, "table_len x page_size = %lld slots, at most 2^30", (long long)c->table_len * c->page_size);
+    const int64_t unit = c->dtype == RIS_F32 ? 4 : 8;
+    for (int64_t x : {c->page_stride, c->head_stride, c->slot_stride})
+        if (x < c->head_dim || x % unit != 0 || x > (int64_t(1) << 36))
+            return fail(RIS_ERR_INVALID, "a stride of %lld must be at least head_dim, a multiple of 16 bytes and at most 2^36", (long long)x);
+    RIS_TRY(check_ptr(c->k, "k"));
+    RIS_TRY(check_ptr(c->v, "v"));
+    if (c->table == nullptr || !aligned(c->table, 4)) return fail(RIS_ERR_INVALID, "table is NULL or misaligned");
+    if (c->length == nullptr || !aligned(c->length, 4)) return fail(RIS_ERR_INVALID, "length is NULL or misaligned");
+    return RIS_OK;
+}
+
+PagedArgs paged_args(const ris_paged *c)
+{
+    PagedArgs a{};
+    a.k = c->k, a.v = c->v;
+    a.page_stride = c->page_stride, a.head_stride = c->head_stride, a.slot_stride = c->slot_stride;
+    a.table = c->table;
+    a.length = c->length;
+    a.B = c->batch, a.Hkv = c->kv_heads, a.D = c->head_dim;
+    while ((1 << a.page_log2) < c->page_size) ++a.page_log2;
+    a.n_pages = c->n_pages, a.table_len = c->table_len;
+    return a;
 }
 
 }  // namespace
@@ -629,6 +705,167 @@ ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_
     Scratch holes;
     RIS_CUDA(holes.alloc(sizeof(int32_t) * (size_t)src->batch * src->kv_heads * budget, s));
     RIS_CUDA(launch_cache4_evict(a, static_cast<int32_t *>(holes.p), s));
+    return RIS_OK;
+}
+
+// ---------------------------------------------------------------- normed and turned heads
+ris_status ris_norm_rope(const void *q, const void *k, void *q_out, void *k_out, int32_t dtype, int64_t n, int32_t heads,
+                         int32_t kv_heads, int32_t head_dim, int64_t q_stride, int64_t k_stride, int64_t q_out_stride,
+                         int64_t k_out_stride, const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
+                         int32_t rot_dim, int32_t pairs, int64_t n_ctx, const ris_rope_cfg *rope, void *stream)
+{
+    NormRopeArgs a{};
+    RIS_TRY(norm_rope_args(a, dtype, n, heads, kv_heads, head_dim, positions, q_weight, k_weight, eps, rot_dim, pairs, n_ctx, rope));
+    if (n == 0) return RIS_OK;
+    const void *const x[] = {q, k};
+    void *const y[] = {q_out, k_out};
+    const int64_t xs[] = {q_stride, k_stride}, ys[] = {q_out_stride, k_out_stride};
+    static const char *const name[2][4] = {{"q", "q_out", "q_stride", "q_out_stride"}, {"k", "k_out", "k_stride", "k_out_stride"}};
+    for (int w = 0; w < (kv_heads > 0 ? 2 : 1); ++w) {
+        RIS_TRY(check_ptr(x[w], name[w][0]));
+        RIS_TRY(check_ptr(y[w], name[w][1]));
+        RIS_TRY(check_stride(xs[w], (int64_t)a.heads[w] * head_dim, dtype, name[w][2]));
+        RIS_TRY(check_stride(ys[w], (int64_t)a.heads[w] * head_dim, dtype, name[w][3]));
+        if (x[w] == y[w] && xs[w] != ys[w]) return fail(RIS_ERR_INVALID, "%s in place with another stride", name[w][0]);
+        a.x[w] = x[w], a.y[w] = y[w];
+        a.x_stride[w] = xs[w], a.y_stride[w] = ys[w];
+    }
+    RIS_CUDA(launch_norm_rope(a, dtype, head_dim, pairs != 0, reinterpret_cast<cudaStream_t>(stream)));
+    return RIS_OK;
+}
+
+ris_status ris_norm_rope_backward(const void *dq, const void *dk, const void *q, const void *k, void *gq, void *gk, float *gq_weight,
+                                  float *gk_weight, int32_t dtype, int64_t n, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                  int64_t dq_stride, int64_t dk_stride, int64_t q_stride, int64_t k_stride, int64_t gq_stride,
+                                  int64_t gk_stride, const int32_t *positions, const void *q_weight, const void *k_weight, float eps,
+                                  int32_t rot_dim, int32_t pairs, int64_t n_ctx, const ris_rope_cfg *rope, void *stream)
+{
+    NormRopeArgs a{};
+    RIS_TRY(norm_rope_args(a, dtype, n, heads, kv_heads, head_dim, positions, q_weight, k_weight, eps, rot_dim, pairs, n_ctx, rope));
+    float *const gw[] = {gq_weight, gk_weight};
+    for (int w = 0; w < 2; ++w) {
+        if ((gw[w] != nullptr) != (a.weight[w] != nullptr)) return fail(RIS_ERR_INVALID, "a weight's gradient is wanted for each weight, and for no other");
+        if (gw[w] != nullptr && !aligned(gw[w], 4)) return fail(RIS_ERR_INVALID, "a weight's gradient is misaligned");
+    }
+    const void *const dy[] = {dq, dk}, *const x[] = {q, k};
+    void *const y[] = {gq, gk};
+    const int64_t ds[] = {dq_stride, dk_stride}, xs[] = {q_stride, k_stride}, ys[] = {gq_stride, gk_stride};
+    static const char *const name[2][6] = {{"dq", "q", "gq", "dq_stride", "q_stride", "gq_stride"}, {"dk", "k", "gk", "dk_stride", "k_stride", "gk_stride"}};
+    for (int w = 0; n > 0 && w < (kv_heads > 0 ? 2 : 1); ++w) {
+        const int64_t row = (int64_t)a.heads[w] * head_dim;
+        RIS_TRY(check_ptr(dy[w], name[w][0]));
+        RIS_TRY(check_ptr(y[w], name[w][2]));
+        RIS_TRY(check_stride(ds[w], row, dtype, name[w][3]));
+        RIS_TRY(check_stride(ys[w], row, dtype, name[w][5]));
+        if (dy[w] == y[w] && ds[w] != ys[w]) return fail(RIS_ERR_INVALID, "%s in place with another stride", name[w][0]);
+        if (a.weight[w] != nullptr) {  // (the rotation alone does not ask for its inputs)
+            RIS_TRY(check_ptr(x[w], name[w][1]));
+            RIS_TRY(check_stride(xs[w], row, dtype, name[w][4]));
+            if (x[w] == y[w] && xs[w] != ys[w]) return fail(RIS_ERR_INVALID, "%s in place with another stride", name[w][1]);
+        }
+        a.dy[w] = dy[w], a.x[w] = x[w], a.y[w] = y[w];
+        a.dy_stride[w] = ds[w], a.x_stride[w] = xs[w], a.y_stride[w] = ys[w];
+    }
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    norm_rope_ctas(dtype, head_dim, n, a.heads, a.ctas);
+    Scratch mem;
+    if (n > 0 && (gq_weight != nullptr || gk_weight != nullptr)) {
+        RIS_CUDA(mem.alloc(sizeof(float) * (size_t)(a.ctas[0] + a.ctas[1]) * head_dim, s));
+        a.part = static_cast<float *>(mem.p);
+    }
+    if (n > 0 || gq_weight != nullptr || gk_weight != nullptr) RIS_CUDA(launch_norm_rope_backward(a, dtype, head_dim, pairs != 0, gq_weight, gk_weight, s));
+    return RIS_OK;
+}
+
+// ---------------------------------------------------------------- the cache in pages
+ris_status ris_paged_append(const ris_paged *cache, ris_pack_t pack, const void *k, const void *v, int64_t k_stride, int64_t v_stride,
+                            const int32_t *start, void *stream)
+{
+    RIS_TRY(check_paged(cache));
+    if (pack == nullptr) return fail(RIS_ERR_INVALID, "pack is NULL");
+    if (pack->n_seqs != cache->batch)
+        return fail(RIS_ERR_INVALID, "the pack has %d sequences, the cache %d", pack->n_seqs, cache->batch);
+    if (start != nullptr && (!aligned(start, 4) || start == cache->length))
+        return fail(RIS_ERR_INVALID, "start is misaligned or the cache's own lengths (pass NULL for those)");
+    if (pack->q_total > 0) {
+        RIS_TRY(check_ptr(k, "k"));
+        RIS_TRY(check_ptr(v, "v"));
+        RIS_TRY(check_stride(k_stride, (int64_t)cache->kv_heads * cache->head_dim, cache->dtype, "k_stride"));
+        RIS_TRY(check_stride(v_stride, (int64_t)cache->kv_heads * cache->head_dim, cache->dtype, "v_stride"));
+    }
+    PagedAppendArgs a{};
+    a.c = paged_args(cache);
+    a.k = k, a.v = v;
+    a.k_stride = k_stride, a.v_stride = v_stride;
+    a.start = start;
+    a.off = pack->q_off;
+    a.seq_of = pack->seq_of;
+    a.total = pack->q_total;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const PackUse use{pack, s};
+    RIS_CUDA(launch_paged_append(a, cache->dtype, s));
+    return RIS_OK;
+}
+
+ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void *q, int64_t q_stride, int32_t heads, int32_t window,
+                            int32_t anchors, int64_t longest, void *out, float *lse, void *stream)
+{
+    RIS_TRY(check_paged(cache));
+    if (pack == nullptr) return fail(RIS_ERR_INVALID, "pack is NULL");
+    if (pack->n_seqs != cache->batch)
+        return fail(RIS_ERR_INVALID, "the pack has %d sequences, the cache %d", pack->n_seqs, cache->batch);
+    RIS_TRY(check_heads(heads, cache->kv_heads, cache->head_dim));
+    if (window < 0 || anchors < 0) return fail(RIS_ERR_INVALID, "window and anchors must be >= 0");
+    if (window == 0 && anchors != 0) return fail(RIS_ERR_INVALID, "anchors without a window");
+    const int64_t capacity = (int64_t)cache->table_len * cache->page_size;
+    if (longest < 0 || longest > capacity) return fail(RIS_ERR_INVALID, "longest %lld outside [0, %lld]", (long long)longest, (long long)capacity);
+    if (lse != nullptr && !aligned(lse, 16)) return fail(RIS_ERR_INVALID, "lse is not 16-byte aligned");
+    if (pack->q_total == 0) return RIS_OK;
+    RIS_TRY(check_ptr(q, "q"));
+    RIS_TRY(check_ptr(out, "out"));
+    RIS_TRY(check_stride(q_stride, (int64_t)heads * cache->head_dim, cache->dtype, "q_stride"));
+    PagedAttendArgs a{};
+    a.c = paged_args(cache);
+    a.q = q;
+    a.out = out;
+    a.lse = lse;
+    a.q_stride = q_stride;
+    a.q_total = pack->q_total;
+    a.off = pack->q_off;
+    a.Hq = heads;
+    a.G = heads / cache->kv_heads;
+    a.window = window;
+    a.anchors = anchors;
+    a.reach = (int32_t)(longest > 0 ? longest : capacity);
+    a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
+    a.least = 1;
+    a.block = std::min(a.G, kPagedRows);
+    a.blocks = (a.G + a.block - 1) / a.block;
+    a.tokens = kPagedRows / a.block;
+    a.part_rows = (int32_t)std::min<int64_t>(a.tokens, pack->q_longest) * a.block;
+    const int64_t items = pack->q_longest <= a.tokens ? pack->n_seqs : pack->q_total / a.tokens + pack->n_seqs;
+    if (pack->q_longest > a.tokens) a.max_items = (int32_t)items;
+    // no more CTAs than the longest line there can be has key tiles
+    const int64_t tiles = a.reach / kPagedKeys + 3, line = items * cache->kv_heads * a.blocks;
+    a.ctas = (int32_t)std::min<int64_t>(kPagedCtas, line > kPagedCtas ? line : line * tiles);
+    const bool plan = a.max_items > 0;
+    const size_t prefix_b = plan ? room(sizeof(int64_t) * (items + 1)) : 0, item_b = plan ? room(sizeof(PagedItem) * items) : 0,
+                 seq_b = plan ? room(sizeof(int32_t) * (pack->n_seqs + 1)) : 0, split_b = room(sizeof(PagedSplit) * a.ctas),
+                 ml_b = room(sizeof(float2) * 2 * a.ctas * a.part_rows), o_b = room(sizeof(float) * 2 * a.ctas * a.part_rows * cache->head_dim);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const PackUse use{pack, s};
+    Scratch mem;
+    RIS_CUDA(mem.alloc(prefix_b + item_b + seq_b + split_b + ml_b + o_b, s));
+    char *d = static_cast<char *>(mem.p);
+    a.prefix = reinterpret_cast<int64_t *>(d), d += prefix_b;
+    a.items = reinterpret_cast<PagedItem *>(d), d += item_b;
+    a.n_items = reinterpret_cast<int32_t *>(d), a.seq_items = a.n_items + 1, d += seq_b;
+    a.split = reinterpret_cast<PagedSplit *>(d), d += split_b;
+    a.part_ml = reinterpret_cast<float2 *>(d), d += ml_b;
+    a.part_o = reinterpret_cast<float *>(d);
+    if (plan) RIS_CUDA(launch_paged_plan(a, s));
+    RIS_CUDA(launch_paged_f32(a, cache->dtype, s));
+    if (a.ctas > 1) RIS_CUDA(launch_paged_join(a, cache->dtype, s));
     return RIS_OK;
 }
 

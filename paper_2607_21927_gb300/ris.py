@@ -137,6 +137,13 @@ _SIGS = {
                           ctypes.c_int64] + [ctypes.c_void_p] * 5,
     "ris_cache4_evict": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p,
                          ctypes.c_void_p],
+    "ris_norm_rope": [ctypes.c_void_p] * 4 + [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 3 + [ctypes.c_int64] * 4 +
+                     [ctypes.c_void_p] * 3 + [ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64] + [ctypes.c_void_p] * 2,
+    "ris_norm_rope_backward": [ctypes.c_void_p] * 8 + [ctypes.c_int32, ctypes.c_int64] + [ctypes.c_int32] * 3 + [ctypes.c_int64] * 6 +
+                              [ctypes.c_void_p] * 3 + [ctypes.c_float, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64] +
+                              [ctypes.c_void_p] * 2,
+    "ris_paged_append": [ctypes.c_void_p] * 4 + [ctypes.c_int64] * 2 + [ctypes.c_void_p] * 2,
+    "ris_paged_attend": [ctypes.c_void_p] * 3 + [ctypes.c_int64] + [ctypes.c_int32] * 3 + [ctypes.c_int64] + [ctypes.c_void_p] * 3,
     "ris_probe_l2_read": [ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p],
     "ris_probe_ffma": [ctypes.c_void_p, ctypes.c_void_p],
     "ris_probe_l2_bytes": [ctypes.c_void_p],
@@ -831,3 +838,148 @@ def ris_cache4_evict(src: Cache4, dst: Cache4, budget: int, recent: int, kept: O
     if st:
         _check("ris_cache4_evict", st)
     return kept
+
+
+# ----------------------------------------------------------------------------- normed and turned heads
+def _like(out, x: torch.Tensor, name: str):
+    """An output of x's shape [n, H, D] and type: (tensor, elements from token to token)."""
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        return out, x.shape[1] * x.shape[2]
+    if out.dtype != x.dtype or out.shape != x.shape:
+        raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}")
+    return out, _heads(out, name)[3]
+
+
+def _weight(w: Optional[torch.Tensor], x: torch.Tensor, name: str):
+    if w is None:
+        return None
+    if w.dtype != x.dtype or tuple(w.shape) != (x.shape[-1],) or not w.is_contiguous() or w.device != x.device:
+        raise ValueError(f"{name}: contiguous {x.dtype} [{x.shape[-1]}] on {x.device}")
+    return w.data_ptr()
+
+
+def _turning(positions, rope, n: int):
+    if rope is None or rope.kind == ROPE_NONE:
+        return None
+    if positions is None:
+        raise ValueError("positions: needed where there is a rotation")
+    return _ints(positions, n, "positions")
+
+
+def ris_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optional[torch.Tensor], n_ctx: int, rope: Optional[RopeCfg],
+                  q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  rot_dim: int = 0, pairs: bool = False, q_out=None, k_out=None, stream=None):
+    """q [n, Hq, D] and k [n, Hkv, D] (or None) normed per head (where there is a weight [D]) and turned at positions [n] (int32):
+    (q_out, k_out). An output may be its input, or rows of a wider tensor."""
+    n, Hq, D, qs = _heads(q, "q")
+    q_out, qos = _like(q_out, q, "q_out")
+    Hkv = ks = kos = 0
+    if k is not None:
+        m, Hkv, Dk, ks = _heads(k, "k")
+        assert m == n and Dk == D and k.dtype == q.dtype, "k: the tokens, head dim and type of q"
+        k_out, kos = _like(k_out, k, "k_out")
+    else:
+        k_out = None
+    st = lib().ris_norm_rope(q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), _code(q), n, Hq, Hkv, D, qs, ks, qos, kos,
+                             _turning(positions, rope, n), _weight(q_weight, q, "q_weight"), _weight(k_weight, q, "k_weight"), eps,
+                             rot_dim, int(pairs), n_ctx, _ref(rope), _raw_stream(stream, q))
+    if st:
+        _check("ris_norm_rope", st)
+    return q_out, k_out
+
+
+def ris_norm_rope_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                           positions: Optional[torch.Tensor], n_ctx: int, rope: Optional[RopeCfg],
+                           q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                           rot_dim: int = 0, pairs: bool = False, gq=None, gk=None, stream=None):
+    """The gradient of ris_norm_rope: dq, dk of its outputs, q, k as they went in (None where they are not normed).
+    Returns (gq, gk, gq_weight, gk_weight), the weights' in fp32; None for what there is not."""
+    n, Hq, D, dqs = _heads(dq, "dq")
+    gq, gqs = _like(gq, dq, "gq")
+    Hkv = dks = gks = qs = ks = 0
+    if dk is not None:
+        m, Hkv, Dk, dks = _heads(dk, "dk")
+        assert m == n and Dk == D and dk.dtype == dq.dtype, "dk: the tokens, head dim and type of dq"
+        gk, gks = _like(gk, dk, "gk")
+    else:
+        gk = None
+    for x, d, w, name in ((q, dq, q_weight, "q"), (k, dk, k_weight, "k")):
+        if w is not None and (x is None or d is None or x.shape != d.shape or x.dtype != d.dtype):
+            raise ValueError(f"{name}: the forward call's input, where it has a weight")
+    if q_weight is not None:
+        qs = _heads(q, "q")[3]
+    if k_weight is not None:
+        ks = _heads(k, "k")[3]
+    gw = [None if w is None else torch.empty(D, dtype=torch.float32, device=dq.device) for w in (q_weight, k_weight)]
+    st = lib().ris_norm_rope_backward(
+        dq.data_ptr(), _addr(dk), _addr(q), _addr(k), gq.data_ptr(), _addr(gk), _addr(gw[0]), _addr(gw[1]), _code(dq), n, Hq, Hkv, D,
+        dqs, dks, qs, ks, gqs, gks, _turning(positions, rope, n), _weight(q_weight, dq, "q_weight"), _weight(k_weight, dq, "k_weight"),
+        eps, rot_dim, int(pairs), n_ctx, _ref(rope), _raw_stream(stream, dq))
+    if st:
+        _check("ris_norm_rope_backward", st)
+    return gq, gk, gw[0], gw[1]
+
+
+# ----------------------------------------------------------------------------- the cache in pages
+class _PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "kv_heads", "head_dim", "page_size", "dtype", "n_pages", "table_len", "reserved")] + \
+               [(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "slot_stride")] + \
+               [(n, ctypes.c_void_p) for n in ("k", "v", "table", "length")]
+
+
+class PagedCache:
+    """A K/V cache in pages (ris_paged): the tensors, which the caller may read and set (in place), and their descriptor.
+    k and v [pages, Hkv, page_size, D], fp32 or bf16, of the same strides (a permuted [pages, page_size, Hkv, D] or the halves
+    of one pool do); table int32 [B, pages of a sequence], length int32 [B]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, length: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or not (k.is_cuda and v.is_cuda):
+            raise ValueError("k and v: alike, [pages, Hkv, page_size, D] on the GPU")
+        pages, H, page, D = k.shape
+        if k.stride(3) != 1 or any(k.stride(i) != v.stride(i) for i in range(3) if k.shape[i] > 1) or v.stride(3) != 1:
+            raise ValueError("k and v: the same strides, each head's channels side by side")
+        if table.dim() != 2 or length.dim() != 1 or length.shape[0] != table.shape[0]:
+            raise ValueError("table [B, pages of a sequence], length [B]")
+        for x, name in ((table, "table"), (length, "length")):
+            _ints(x, x.numel(), name)
+        # (the stride of an axis of one element says nothing: head_dim does for it)
+        st = [k.stride(i) if k.shape[i] > 1 else D for i in range(3)]
+        self.k, self.v, self.table, self.length = k, v, table, length
+        self.batch, self.kv_heads, self.head_dim, self.page_size = table.shape[0], H, D, page
+        self.capacity = table.shape[1] * page
+        self.desc = _PagedDesc(self.batch, H, D, page, _code(k), pages, table.shape[1], 0, st[0], st[1], st[2], k.data_ptr(),
+                               v.data_ptr(), table.data_ptr(), length.data_ptr())
+        self._ref = ctypes.byref(self.desc)
+
+
+def ris_paged_append(cache: PagedCache, pack: Pack, k: torch.Tensor, v: torch.Tensor, start: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """The pack's rows k, v [q_total, Hkv, D] into the cache's pages, after the slots in use or at start [B] (int32)."""
+    (n, H, D, ks), (nv, Hv, Dv, vs) = _heads(k, "k"), _heads(v, "v")
+    if n != pack.q_total or H != cache.kv_heads or D != cache.head_dim or (nv, Hv, Dv) != (n, H, D):
+        raise ValueError(f"k is {tuple(k.shape)}, v {tuple(v.shape)}, the pack has {pack.q_total} rows, the cache heads "
+                         f"{cache.kv_heads} x {cache.head_dim}")
+    assert k.dtype == v.dtype == cache.k.dtype, "k and v of the cache's type"
+    st = lib().ris_paged_append(cache._ref, pack.handle, k.data_ptr(), v.data_ptr(), ks, vs,
+                                None if start is None else _ints(start, cache.batch, "start"), _raw_stream(stream, cache.k))
+    if st:
+        _check("ris_paged_append", st)
+
+
+def ris_paged_attend(cache: PagedCache, pack: Pack, q: torch.Tensor, window: int = 0, anchors: int = 0, longest: int = 0,
+                     out: Optional[torch.Tensor] = None, return_lse: bool = False, stream=None):
+    """The pack's rows q [q_total, Hq, D], the last of their sequences' slots in use, over the pages, always a tuple: out
+    [q_total, Hq, D], then lse [Hq, q_total] (return_lse). window > 0: the last `window` keys and the first `anchors`."""
+    n, Hq, D, qs = _heads(q, "q")
+    if n != pack.q_total or D != cache.head_dim:
+        raise ValueError(f"q is {tuple(q.shape)}, the pack has {pack.q_total} rows, the cache heads of {cache.head_dim}")
+    assert q.dtype == cache.k.dtype, "q of the cache's type"
+    out = _out(out, (n, Hq, D), q.dtype, q.device)
+    assert out.dtype == q.dtype
+    lse = torch.empty((Hq, n), dtype=torch.float32, device=q.device) if return_lse else None
+    st = lib().ris_paged_attend(cache._ref, pack.handle, q.data_ptr(), qs, Hq, window, anchors, longest, out.data_ptr(), _addr(lse),
+                                _raw_stream(stream, q))
+    if st:
+        _check("ris_paged_attend", st)
+    return (out, lse) if return_lse else (out,)
