@@ -32,8 +32,8 @@
 #include <type_traits>
 
 #include "attn_common.cuh"
+#include "row_tiles.cuh"
 #include "serve.h"
-#include "tcgen05.cuh"
 
 namespace ris {
 
@@ -44,7 +44,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int BM = 128, BN = 128;  // query rows and keys of a tile
+constexpr int BM = kTileRows, BN = kTileKeys;
 static_assert(kPackRows == BM, "an item is a row tile");
 constexpr int kGroupWarps = 4;     // of a softmax group: one thread per row
 constexpr int kSoftmaxWarps = 2 * kGroupWarps;
@@ -70,31 +70,6 @@ __device__ __forceinline__ int value_exp(float vmax)
     return min(max((int)((__float_as_uint(vmax) >> 23) & 0xFF) - 127 - 13, -100), 114);
 }
 
-// kept keys of word e of a tile, as bits: those up to the row's last one (counted from the tile's start)
-__device__ __forceinline__ uint32_t causal_word(int last, int e)
-{
-    const int lim = min(31, max(-1, last - 32 * e));
-    return lim < 0 ? 0u : 0xFFFFFFFFu >> (31 - lim);
-}
-// x = -infinity unless the word has the bit: a predicated move
-__device__ __forceinline__ void drop_unless(float &x, uint32_t word, uint32_t bit)
-{
-    asm("{\n\t.reg .pred p;\n\t.reg .b32 t;\n\t"
-        "and.b32 t, %1, %2;\n\tsetp.eq.u32 p, t, 0;\n\t@p mov.b32 %0, 0xFF800000;\n\t}"
-        : "+f"(x)
-        : "r"(word), "r"(bit));
-}
-__device__ __forceinline__ float row_max(const float (&sv)[BN])
-{
-    float mx8[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        mx8[e] = fmaxf(sv[e], sv[e + 8]);
-#pragma unroll
-        for (int c = 16; c < BN; c += 16) mx8[e] = fmax3(mx8[e], sv[c + e], sv[c + 8 + e]);
-    }
-    return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
-}
 // P = 2^(s sc - mu + kAboveLog2) of columns C0 .. C1 - 1 as fp16, two keys to a word, and the sum of the
 // weights before they are rounded
 template <int C0 = 0, int C1 = BN>
@@ -115,21 +90,6 @@ __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, flo
     float a, b;
     f2_unpack(f2_add(sum[0], sum[1]), a, b);
     return a + b;
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t *>(&v);
-}
-// 16 bytes of outputs (four fp32 or eight bf16 values)
-template <typename TOut>
-__device__ __forceinline__ void store16(void *dst, const float *x)
-{
-    if constexpr (sizeof(TOut) == 4)
-        *reinterpret_cast<float4 *>(dst) = make_float4(x[0], x[1], x[2], x[3]);
-    else
-        *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
 // A row's softmax as the other outputs: log-sum-exp, and (maximum, 1 / sum) for the key weights.
@@ -279,27 +239,6 @@ struct PackedMaps {
 // scores.
 __device__ __forceinline__ void values_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// O of 32 rows (a warp's) x OC columns from TMEM, normalised, into the warp's part of shared memory, row by
-// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv
-// 0) become zeros whatever the columns hold.
-template <int OC, typename TOut>
-__device__ __forceinline__ void stage_out(unsigned char *stage, uint32_t t_o, float inv)
-{
-    constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;  // bytes and pieces of a row's part
-    const int lane = threadIdx.x & 31;
-#pragma unroll
-    for (int c0 = 0; c0 < OC; c0 += 32) {
-        float ov[32];
-        tmem_ld32(t_o + c0, ov);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) ov[c] = inv == 0.f ? 0.f : ov[c] * inv;
-#pragma unroll
-        for (int e = 0; e < 32 * (int)sizeof(TOut) / 16; ++e) {
-            const int piece = c0 * (int)sizeof(TOut) / 16 + e;
-            store16<TOut>(stage + lane * RB + ((piece ^ (lane & (NP - 1))) << 4), ov + e * (16 / (int)sizeof(TOut)));
-        }
-    }
-}
 // the first `rows` of those rows to memory, so that neighbouring lanes store neighbouring pieces of a row
 template <int OC, typename TOut>
 __device__ __forceinline__ void rows_out(const unsigned char *stage, TOut *out, int64_t pitch, int rows)
@@ -1526,20 +1465,6 @@ __global__ void __launch_bounds__(kWeightThreads, DT == 64 ? 4 : 2) k_packed_wei
 }
 
 // ---------------------------------------------------------------- host side
-PFN_cuTensorMapEncodeTiled_v12000 encode_fn()
-{
-    static std::once_flag once;
-    static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-    std::call_once(once, [] {
-        void *p = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
-            q == cudaDriverEntryPointSuccess)
-            fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-    });
-    return fn;
-}
-
 // n tokens of H heads of D values, `stride` elements from token to token, viewed as 3D (d, head, token); box =
 // 128 bytes of d x 1 head x `rows` tokens.
 bool make_map(CUtensorMap *m, CUtensorMapDataType type, const void *base, int64_t n, int H, int64_t stride, int rows, int D)

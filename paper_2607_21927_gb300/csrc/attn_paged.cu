@@ -1,0 +1,627 @@
+// Attention over pages on the 5th-generation tensor cores, bf16: from one token against a long cache to a
+// chunk of a prompt.
+//
+// S = Q K^T with bf16 operands (exact products, fp32 sums), one online softmax per row, O = P V with P
+// rounded to bf16 (2^-8 of a weight at most: as much as the bf16 output's own rounding, averaged over the
+// keys; values cannot be converted to fp16 ahead of a call, as that would read the whole cache) and the
+// row's sum from the fp32 weights. The heads of a KV head share a row tile (attn_paged.cuh), so few rows
+// read a key once for all of them.
+//
+// Persistent, two CTAs to an SM, each on its run of the line with one row tile at a time and one softmax
+// group (TMEM 256 columns); the two fill each other's waits:
+//   warp 4  the run's units, query and key tiles, warp 5 value tiles: TMA, a box for each page of a tile, the
+//           boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
+//           fills its place with zeros;
+//   warp 6  S = Q K^T as soon as its columns are free, warp 7 O += P V;
+//   warps 0-3  the softmax, one thread per row; a warp without a row only passes the tiles on.
+//
+// A product over a tile multiplies keys that a row does not see by 0, and 0 times an infinity is not 0. The
+// slots past the last row's own key, where a page may hold anything, are cleared in the tile by the softmax
+// warps. A row that comes out not finite all the same (a key of the sequence that only other rows see holds
+// an infinity or NaN, or one that it sees does) is computed again after everything else, on the FP32 pipe,
+// over exactly the keys that it sees.
+//
+// Every mbarrier wait is bounded; a wait that gives up sets the device error word, every role falls through
+// to the end, TMEM is released and the CTA returns.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "attn_common.cuh"
+#include "attn_paged.cuh"
+#include "row_tiles.cuh"
+
+namespace ris {
+
+// Device error words of this file, read by ris_device_status: a bounded wait gave up; a key outside the pages.
+__device__ unsigned int g_ris_paged_wait, g_ris_paged_page;
+
+namespace {
+
+using namespace tc;
+using namespace paged;
+
+constexpr int BM = kTileRows, BN = kTileKeys;
+static_assert(kPagedTileRows == BM && kPagedTileKeys == BN, "as the work is shared out");
+constexpr int kGroupWarps = 4;  // of the softmax group: one thread per row
+// The reference m of a row is its largest score so far: the weight of a key that takes nearly all is 1, which
+// bf16 holds. Up to here the exponent of a weight is rounded once, and that key's is within 2^-12 of 0 (the
+// reference was rounded as a product); scores beyond are rounded as products first, so that it is 0.
+constexpr float kFarLog2 = 0x1p12f;
+
+template <int D>
+struct Lay {
+    static constexpr int NB = D / 64;                      // 64-column blocks
+    static constexpr bool OVER = D == 128;                 // P takes the scores' columns
+    static constexpr int NSK = D == 64 ? 3 : 1, NSV = D == 64 ? 2 : 1, NI = 4;
+    static constexpr int BLK = 128 * 128, TILE = NB * BLK; // 128 rows or keys of D 16-bit values
+    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_OUT = OFF_Q + TILE,
+                         OFF_BARS = OFF_OUT + BLK, OFF_INFO = OFF_BARS + 192, OFF_RUN = OFF_INFO + NI * 64,
+                         OFF_TMEM = OFF_RUN + (int)sizeof(RunMem), BYTES = OFF_TMEM + 16;
+    // Barriers, of a ring stage:
+    //   K_FULL, V_FULL, Q_FULL  its keys / values / the query tile have landed
+    //   K_FREE, V_FREE, Q_FREE  the products that read it are done
+    //   I_FULL, I_FREE          a unit's description is there / every role has read it
+    // and one phase per key tile:
+    //   S_GO    the last scores have been read out of their buffer (only where P has its own columns:
+    //           else the value product before has to be done, which says that too)
+    //   S_FULL  the next are there
+    //   P_GO    P is written (and O rescaled where needed)
+    //   PV_DONE O has settled, P's buffer is free
+    static constexpr int B_K_FULL = 0, B_V_FULL = B_K_FULL + NSK, B_Q_FULL = B_V_FULL + NSV, B_K_FREE = B_Q_FULL + 1,
+                         B_V_FREE = B_K_FREE + NSK, B_Q_FREE = B_V_FREE + NSV, B_I_FULL = B_Q_FREE + 1, B_I_FREE = B_I_FULL + NI,
+                         B_S_GO = B_I_FREE + NI, B_S_FULL = B_S_GO + 1, B_P_GO = B_S_FULL + 1, B_PV_DONE = B_P_GO + 1,
+                         NBAR = B_PV_DONE + 1;
+    static_assert(NBAR <= 24 && 2 * (BYTES + 1024) <= 228 * 1024, "barriers; two CTAs of an SM");
+    static constexpr uint32_t COLS = 256, T_P = OVER ? 0 : BN, T_O = OVER ? BN : BN + BN / 2;  // TMEM; S at 0
+    static_assert(T_O + D <= COLS, "TMEM columns");
+    // registers per thread: at launch, then after setmaxnreg of a softmax and of another thread
+    static constexpr int THREADS = 256, REGS = 128, SOFTMAX_REGS = 200, OTHER_REGS = 56;
+    static_assert(SOFTMAX_REGS + OTHER_REGS == 2 * REGS, "the shares of the two warpgroups add up to the launch's");
+};
+
+// What the roles need to know of a unit.
+struct Info {
+    int n;              // key tiles of this part, -1: no more units
+    int j0, sinks, first;  // the first of them; which keys a tile holds (Sight)
+    int pos0, tokens, low, end;
+    int head0, heads, kv_head, seq, row0, part;
+    __device__ __forceinline__ int key(int j) const { return BN * (j0 + j < sinks ? j0 + j : first + j0 + j - sinks); }
+};
+static_assert(sizeof(Info) <= 64, "the ring's slots");
+
+// P = 2^(s sc - mu) of columns C0 .. C1 - 1 as bf16, two keys to a word, and the sum of the weights before they
+// are rounded
+template <int C0, int C1>
+__device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, float mu, uint32_t (&hw)[BN / 2])
+{
+    const uint64_t sc2 = f2_pack(sc, sc), nmu2 = f2_pack(-mu, -mu);
+    uint64_t sum[2] = {0, 0};
+#pragma unroll
+    for (int w = C0 / 2; w < C1 / 2; ++w) {
+        float x0, x1;
+        f2_unpack(f2_fma(f2_pack(sv[2 * w], sv[2 * w + 1]), sc2, nmu2), x0, x1);
+        x0 = ex2(x0);
+        x1 = ex2(x1);
+        sum[w & 1] = f2_add(sum[w & 1], f2_pack(x0, x1));
+        hw[w] = pack_bf16(x0, x1);
+    }
+    float a, b;
+    f2_unpack(f2_add(sum[0], sum[1]), a, b);
+    return a + b;
+}
+
+// Where box `box` of the tile from key k0 on lies: its page, or n_pages (past the pool's end) for one that no row
+// sees or whose entry is no page.
+__device__ __forceinline__ int box_page(const PagedAttendArgs &a, const Info &x, int k0, int box, int box_rows)
+{
+    const int j = k0 + box * box_rows;
+    if (j >= x.end || (j + box_rows <= x.low && j >= a.anchors)) return a.c.n_pages;
+    const int p = page_of(a.c, x.seq, j);
+    if (p < 0) atomicOr(&g_ris_paged_page, 1u);
+    return p < 0 ? a.c.n_pages : p;
+}
+
+// A row of a unit on the FP32 pipe, by one warp: over the unit's key tiles, 32 keys at a time (a lane per key for
+// the scores, D / 32 channels for the outputs), each key only where the row sees it.
+template <int D>
+__device__ __noinline__ void row_as_given(const PagedAttendArgs &a, const Unit &u, int tok, int head)
+{
+    constexpr int C = D / 32;
+    const int lane = threadIdx.x & 31, pos = u.sight.pos0 + tok, h = u.head0 + head;
+    const int64_t row = u.row0 + tok;
+    const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) + row * a.q_stride + (int64_t)h * D;
+    float m = -INFINITY, l = 0.f, o[C] = {};
+    for (int j = u.j0; j < u.j1; ++j)
+        for (int k0 = BN * u.sight.tile(j), e0 = 0; e0 < BN; e0 += 32) {
+            const int key = k0 + e0 + lane;
+            const int page = sees(a, pos, key) ? page_of(a.c, u.seq, key) : -1;
+            const int64_t at = page >= 0 ? slot_at(a.c, page, u.kv_head, key) : -1;
+            float s = -INFINITY;
+            if (at >= 0) {
+                const __nv_bfloat16 *k = reinterpret_cast<const __nv_bfloat16 *>(a.c.k) + at;
+                s = 0.f;
+                for (int d = 0; d < D; d += 2) {
+                    const float2 x = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(q + d)), y = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162 *>(k + d));
+                    s = fmaf(x.x, y.x, fmaf(x.y, y.y, s));
+                }
+                s = __fmul_rn(s, a.scale_log2);
+            }
+            const float top = fmaxf(m, warp_max(s)), ref = top == -INFINITY ? 0.f : top, al = exp2f(m - ref), p = at >= 0 ? exp2f(s - ref) : 0.f;
+            m = top;
+            l = fmaf(l, al, warp_sum(p));
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] *= al;
+            for (int e = 0; e < 32; ++e) {
+                const int64_t to = __shfl_sync(0xFFFFFFFFu, at, e);
+                const float pe = __shfl_sync(0xFFFFFFFFu, p, e);
+                if (to < 0) continue;
+                const __nv_bfloat16 *v = reinterpret_cast<const __nv_bfloat16 *>(a.c.v) + to + C * lane;
+#pragma unroll
+                for (int c = 0; c < C; ++c) o[c] = fmaf(pe, __bfloat162float(v[c]), o[c]);
+            }
+        }
+    if (u.part < 0) {
+        __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(a.out) + (row * a.Hq + h) * D + C * lane;
+        for (int c = 0; c < C; ++c) out[c] = __float2bfloat16_rn(l == 0.f ? 0.f : o[c] / l);
+        if (lane == 0 && a.lse != nullptr) a.lse[h * a.q_total + row] = (m + log2f(l)) * kLn2;
+    } else {
+        const int64_t at = (int64_t)u.part * a.part_rows + tok * a.block + head;
+        for (int c = 0; c < C; ++c) a.part_o[at * D + C * lane + c] = o[c];
+        if (lane == 0) a.part_ml[at] = make_float2(m, l);
+    }
+}
+
+// The rows of this warp (of each unit of the run) that came out not finite.
+template <int D>
+__device__ __noinline__ void rows_as_given(const PagedAttendArgs &a, const Run &run, int warp)
+{
+    constexpr int C = D / 32;
+    const int lane = threadIdx.x & 31;
+    Walk walk(run);
+    Unit u;
+    while (walk.next<BN>(a, run, u)) {
+        for (int r = 32 * warp; r < 32 * warp + 32; ++r) {
+            const int tok = r / a.block, head = r % a.block;
+            if (tok >= u.sight.tokens || head >= u.heads) continue;
+            bool bad = false;
+            const int64_t at = u.part < 0 ? ((int64_t)(u.row0 + tok) * a.Hq + u.head0 + head) * D : ((int64_t)u.part * a.part_rows + r) * D;
+            for (int c = 0; c < C; ++c) {
+                const int64_t e = at + C * lane + c;
+                bad = bad || !isfinite(u.part < 0 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16 *>(a.out)[e]) : a.part_o[e]);
+            }
+            if (__any_sync(0xFFFFFFFFu, bad)) row_as_given<D>(a, u, tok, head);
+        }
+    }
+}
+
+struct Maps {
+    CUtensorMap q, k, v;
+};
+
+template <int D>
+__global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid_constant__ PagedAttendArgs a, const __grid_constant__ Maps maps)
+{
+    using L = Lay<D>;
+    constexpr int NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
+    constexpr int kLoadQK = 4, kLoadV = 5, kScores = 6;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
+    const uint32_t sbase = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const unsigned int *const gave_up = &g_ris_paged_wait;
+    auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
+
+    if (warp == kLoadQK) {
+        if (lane < L::NBAR) {
+            const bool by_group = lane == L::B_S_GO || lane == L::B_P_GO, free = lane >= L::B_I_FREE && lane < L::B_I_FREE + NI;
+            mbar_init(bar(lane), by_group ? kGroupWarps : free ? kGroupWarps + 3 : 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+    } else if (warp == kScores) {
+        tmem_alloc<1, L::COLS>(smem_u32(&tmem_base_sh));
+    }
+    after_last();
+    {
+        RunMem &mem = *reinterpret_cast<RunMem *>(smem + L::OFF_RUN);
+        const Run r = run_of<BN, L::THREADS>(a, blockIdx.x, mem);
+        if (threadIdx.x == 0) mem.run = r;
+    }
+    const Run &run = reinterpret_cast<const RunMem *>(smem + L::OFF_RUN)->run;
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_base_sh;
+    bool ok = (sbase & 1023u) == 0u;
+    auto wait_all = [&](int i, int parity) -> bool {
+        const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+        tc_fence_after();
+        return got;
+    };
+    // description of unit u (a whole warp); its place is given back once every lane has it
+    auto unit = [&](int u, Info &x) -> bool {
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up))) return false;
+        x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
+        __syncwarp();
+        mbar_arrive_if(lane == 0, bar(L::B_I_FREE + u % NI));
+        return true;
+    };
+
+    if (warp >= kGroupWarps) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
+        const int box_rows = min(BN, 1 << a.c.page_log2), boxes = BN / box_rows;  // of a tile and 64-column block
+        const int box = lane % boxes, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;
+        if (warp == kLoadQK) {
+            const uint32_t q_bytes = (uint32_t)(a.block * a.tokens * 128 * NB);
+            int nq = 0, nk = 0;  // query and key tiles asked for
+            PagedSplit split{-1};
+            Walk walk(run);
+            Unit y;
+            bool more = walk.next<BN>(a, run, y);
+            for (int u = 0; ok; ++u) {
+                if (u >= NI) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up));
+                if (!ok) break;
+                const Info x{more ? y.j1 - y.j0 : -1, y.j0, y.sight.sinks, y.sight.first, y.sight.pos0, y.sight.tokens, y.sight.low, y.sight.end,
+                             y.head0, y.heads, y.kv_head, y.seq, y.row0, y.part};
+                if (lane == 0) {
+                    *reinterpret_cast<Info *>(smem + L::OFF_INFO + u % NI * 64) = x;
+                    mbar_arrive(bar(L::B_I_FULL + u % NI));
+                }
+                __syncwarp();
+                if (!more) break;
+                if (y.split.first >= 0) split = y.split;
+                for (int j = 0; j < x.n; ++j, ++nk) {
+                    const int st = nk % NSK, k0 = x.key(j);
+                    const int page = blk < NB ? box_page(a, x, k0, box, box_rows) : 0;
+                    if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + st), TILE);
+                    __syncwarp();
+                    if (blk < NB)
+                        tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + box * box_rows * 128, &maps.k, 64 * blk, (k0 + box * box_rows) & in_page,
+                                    x.kv_head, page, bar(L::B_K_FULL + st));
+                    if (j > 0) continue;
+                    if (nq > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up));
+                    if (!ok) {
+                        ++nk;
+                        break;
+                    }
+                    if (lane == 0) {
+                        mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL), q_bytes);
+                        for (int b = 0; b < NB; ++b) tma_load_3d<1>(sbase + L::OFF_Q + b * L::BLK, &maps.q, 64 * b, x.head0, x.row0, bar(L::B_Q_FULL));
+                    }
+                    ++nq;
+                    more = walk.next<BN>(a, run, y);  // (while these are on their way)
+                }
+                if (x.n == 0) more = walk.next<BN>(a, run, y);
+            }
+            if (lane == 0) {
+                a.split[blockIdx.x] = split;
+                // nothing of this warp's may still be on its way to shared memory when the CTA ends
+                if (nq > 0) mbar_wait_own<1>(bar(L::B_Q_FULL), (nq - 1) & 1);
+                for (int i = max(0, nk - NSK); i < nk; ++i) mbar_wait_own<1>(bar(L::B_K_FULL + i % NSK), (i / NSK) & 1);
+            }
+        } else if (warp == kLoadV) {
+            int nv = 0;
+            for (int u = 0; ok; ++u) {
+                Info x;
+                ok = unit(u, x);
+                if (!ok || x.n < 0) break;
+                for (int j = 0; j < x.n; ++j, ++nv) {
+                    const int st = nv % NSV, k0 = x.key(j);
+                    const int page = blk < NB ? box_page(a, x, k0, box, box_rows) : 0;
+                    if (nv >= NSV) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + st), TILE);
+                    __syncwarp();
+                    if (blk < NB)
+                        tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + box * box_rows * 128, &maps.v, 64 * blk, (k0 + box * box_rows) & in_page,
+                                    x.kv_head, page, bar(L::B_V_FULL + st));
+                }
+            }
+            if (lane == 0)
+                for (int i = max(0, nv - NSV); i < nv; ++i) mbar_wait_own<1>(bar(L::B_V_FULL + i % NSV), (i / NSV) & 1);
+        } else if (ok) {
+            // The issuing warps, all lanes: trip counts and addresses come out of warp-wide reductions,
+            // which leave them in uniform registers; a product whose operands are in the lanes' registers
+            // costs more time to issue than to run.
+            const uint32_t tb = __reduce_max_sync(0xFFFFFFFFu, tmem);
+            int t = 0, nq = 0;  // tiles; units with keys
+            for (int u = 0;; ++u) {
+                Info x;
+                ok = unit(u, x);
+                if (!ok) break;
+                const int n = __reduce_max_sync(0xFFFFFFFFu, x.n);
+                if (n < 0) break;
+                if (n == 0) continue;
+                if (warp == kScores) {
+                    constexpr uint32_t ID_S = idesc_bf16(BM, BN, false);
+                    ok = wait_all(L::B_Q_FULL, nq & 1);
+                    const uint32_t qd = desc_lo(sbase + L::OFF_Q, 16);
+                    for (int j = 0; j < n && ok; ++j, ++t) {
+                        const int st = t % NSK;
+                        ok = wait_all(L::B_K_FULL + st, (t / NSK) & 1);
+                        if (!L::OVER)
+                            ok = ok && wait_all(L::B_S_GO, t & 1);
+                        else if (t > 0)
+                            ok = ok && wait_all(L::B_PV_DONE, (t - 1) & 1);
+                        if (!ok) break;
+                        const uint32_t kd = desc_lo(sbase + L::OFF_K + st * TILE, 16);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks)
+                                tc_mma_ss<1>(tb, qd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), kd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), ID_S, ks > 0);
+                            tc_commit<1>(bar(L::B_S_FULL));
+                            tc_commit<1>(bar(L::B_K_FREE + st));
+                            if (j == n - 1) tc_commit<1>(bar(L::B_Q_FREE));
+                        }
+                        __syncwarp();
+                    }
+                } else {
+                    constexpr uint32_t ID_O = idesc_bf16(BM, D, true);
+                    for (int j = 0; j < n && ok; ++j, ++t) {
+                        const int st = t % NSV;
+                        ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO, t & 1);
+                        if (!ok) break;
+                        const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, L::BLK);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < BN / 16; ++ks)
+                                tc_mma_ts<1>(tb + L::T_O, tb + L::T_P + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
+                            tc_commit<1>(bar(L::B_PV_DONE));
+                            tc_commit<1>(bar(L::B_V_FREE + st));
+                        }
+                        __syncwarp();
+                    }
+                }
+                if (!ok) break;
+                ++nq;
+            }
+            // every commit of this warp has arrived before the CTA ends (after a wait that gave up, those
+            // of the tiles issued)
+            if (lane == 0 && t > 0) {
+                const int done = warp == kScores ? L::B_S_FULL : L::B_PV_DONE, free = warp == kScores ? L::B_K_FREE : L::B_V_FREE;
+                const int ring = warp == kScores ? NSK : NSV;
+                mbar_wait_own<1>(bar(done), (t - 1) & 1);
+                for (int i = max(0, t - ring); i < t; ++i) mbar_wait_own<1>(bar(free + i % ring), (i / ring) & 1);
+                if (warp == kScores && nq > 0) mbar_wait_own<1>(bar(L::B_Q_FREE), (nq - 1) & 1);
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
+        const int r = threadIdx.x;  // TMEM lane, row of the tile, key of a tile at the edges
+        const int tok = r / a.block, head = r - tok * a.block;
+        const int tok_first = warp * 32 / a.block, tok_last = (warp * 32 + 31) / a.block;  // of the warp
+        const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+        const uint32_t t_s = tmem + lane_off, t_p = tmem + L::T_P + lane_off, t_o = tmem + L::T_O + lane_off;
+        unsigned char *const stage = smem + L::OFF_OUT + warp * (L::BLK / kGroupWarps);
+        int t = 0;           // tiles
+        bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
+        bool left = false;   // rows of this warp came out not finite
+        if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
+        for (int u = 0; ok; ++u) {
+            // (its description stays in its place until the unit is done)
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up));
+            const Info &x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
+            const int n = x.n;
+            if (!ok || n < 0) break;
+            const bool valid = tok < x.tokens && head < x.heads;
+            const bool idle = !__any_sync(0xFFFFFFFFu, valid);
+            const int pos0 = x.pos0, pos = pos0 + tok, end = x.end;
+            int k0 = x.key(0), jump = x.sinks - x.j0;  // tiles up to the window's
+            bool far = false;
+            float l = 0.f, m = -INFINITY;  // row sum, reference
+            for (int j = 0; j < n; ++j, ++t, k0 = j == jump ? BN * x.first : k0 + BN) {
+                // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
+                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL, t & 1);
+                tc_fence_after();
+                if (idle) {
+                    there = false;
+                    if (!L::OVER) mbar_arrive_if(lane == 0, bar(L::B_S_GO));
+                    // (in step with the others: a wait for a phase tells nothing while the one before it is open, and
+                    // an arrival ahead of the others' would count for the last tile's P)
+                    if (!L::OVER && j > 0 && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+                } else {
+                    uint32_t su[2][64];
+                    tmem_issue64(t_s, su[0]);
+                    tmem_issue64(t_s + 64, su[1]);
+                    tmem_wait_ld();
+                    pin64(su[0]);
+                    pin64(su[1]);
+                    if (!L::OVER) {
+                        tc_fence_before();
+                        __syncwarp();
+                        mbar_arrive_if(lane == 0, bar(L::B_S_GO));
+                    }
+                    float sv[BN];
+#pragma unroll
+                    for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
+                    if (k0 + BN - 1 > pos0 + tok_first || (a.window != 0 && pos0 + tok_last - k0 >= a.window && a.anchors < k0 + BN)) {
+                        uint32_t cw[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            cw[e] = causal_word(pos - k0, e) &
+                                    (a.window == 0 ? 0xFFFFFFFFu : ~causal_word(pos - a.window - k0, e) | causal_word(a.anchors - 1 - k0, e));
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            // (an end of what the rows see lies in one or two of a warp's words)
+                            if (__all_sync(0xFFFFFFFFu, cw[w] == 0xFFFFFFFFu)) continue;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) drop_unless(sv[32 * w + e], cw[w], 1u << e);
+                        }
+                    }
+                    float sc = a.scale_log2;
+                    const float mx = valid ? __fmul_rn(row_max(sv), sc) : -INFINITY;
+                    const bool upd = mx > m;
+                    const bool scale_o = upd && m != -INFINITY;
+                    const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
+                    const float al = scale_o ? exp2f(m - mx) : 1.f;
+                    l *= al;
+                    m = upd ? mx : m;
+                    const float mu = m == -INFINITY ? 0.f : m;
+                    far = __any_sync(0xFFFFFFFFu, fabsf(mu) > kFarLog2);
+                    if (far) {
+#pragma unroll
+                        for (int e = 0; e < BN; ++e) sv[e] = __fmul_rn(sv[e], sc);
+                        sc = 1.f;
+                    }
+                    uint32_t hw[BN / 2];
+                    float sum = weights_of<0, 96>(sv, sc, mu, hw);
+                    // polled here, the answers are there when the weights are
+                    bool settled = true;
+                    if (!L::OVER) {
+                        settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
+                        there = mbar_test<1>(bar(L::B_S_FULL), (t + 1) & 1);
+                    }
+                    l += sum + weights_of<96, BN>(sv, sc, mu, hw);
+                    // P's buffer is free and O has settled once the last value product is done (where P takes
+                    // the scores' place, the scores were computed after that; a unit's first tile: waited for
+                    // at the end of the last unit)
+                    if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+                    tc_fence_after();
+                    if (any_scale) {
+#pragma unroll 1
+                        for (int c0 = 0; c0 < D; c0 += 32) {
+                            float ov[32];
+                            uint32_t ow[32];
+                            tmem_ld32(t_o + c0, ov);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) ow[e] = __float_as_uint(ov[e] * al);
+                            tmem_st32(t_o + c0, ow);
+                        }
+                    }
+                    tmem_st32(t_p, hw);
+                    tmem_st32(t_p + 32, hw + 32);
+                    tmem_wait_st();
+                }
+                if (k0 + BN > end) {  // (a thread takes a key)
+                    if (ok) ok = wait_all(L::B_V_FULL + t % NSV, (t / NSV) & 1);
+                    if (ok && k0 + r >= end) {
+                        unsigned char *const row = smem + L::OFF_V + t % NSV * TILE + r * 128;
+#pragma unroll
+                        for (int e = 0; e < 8 * NB; ++e)
+                            *reinterpret_cast<uint4 *>(row + (e >> 3) * L::BLK + (((e ^ r) & 7) << 4)) = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                tc_fence_before();
+                __syncwarp();
+                mbar_arrive_if(lane == 0, bar(L::B_P_GO));
+            }
+            if (ok && n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+            if (!ok) break;
+            const int part = x.part, head0 = x.head0, row0 = x.row0;
+            __syncwarp();
+            mbar_arrive_if(lane == 0, bar(L::B_I_FREE + u % NI));
+            if (idle) {
+                tc_fence_before();
+                continue;
+            }
+            // rows of OC columns by way of shared memory, so that neighbouring lanes store neighbouring pieces of a row
+            auto emit = [&](auto *base, float scale, int64_t mine) {
+                using TOut = std::remove_pointer_t<decltype(base)>;
+                constexpr int OC = 128 / (int)sizeof(TOut);
+#pragma unroll 1
+                for (int c0 = 0; c0 < D; c0 += OC) {
+                    __syncwarp();
+                    if (n > 0) {
+                        const float found = stage_out<OC, TOut, true>(stage, t_o + c0, scale);
+                        left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
+                    } else {  // rows without a key: zeros
+                        for (int e = lane; e < 256; e += 32) reinterpret_cast<uint4 *>(stage)[e] = make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int rr = 4 * e + (lane >> 3), piece = lane & 7;
+                        const int64_t to = __shfl_sync(0xFFFFFFFFu, mine, rr);
+                        const uint4 y = *reinterpret_cast<const uint4 *>(stage + rr * 128 + ((piece ^ (rr & 7)) << 4));
+                        if (to >= 0) *reinterpret_cast<uint4 *>(base + to + c0 + piece * (16 / (int)sizeof(TOut))) = y;
+                    }
+                }
+            };
+            if (part < 0) {
+                const int64_t row = row0 + tok;
+                if (valid && a.lse != nullptr) a.lse[(head0 + head) * a.q_total + row] = (m + log2f(l)) * kLn2;
+                emit(reinterpret_cast<__nv_bfloat16 *>(a.out), l == 0.f ? 0.f : 1.f / l, valid ? (row * a.Hq + head0 + head) * D : -1);
+            } else {
+                const int64_t at = (int64_t)part * a.part_rows + r;
+                if (valid) a.part_ml[at] = make_float2(m, l);
+                emit(a.part_o, l == 0.f ? 0.f : 1.f, valid ? at * D : -1);
+            }
+            tc_fence_before();  // (O has been read before the next P is announced)
+        }
+        // (after everything else: it takes far longer than a wait of another role may)
+        __syncwarp();
+        if (ok && left) rows_as_given<D>(a, run, warp);
+    }
+    if (!ok) atomicOr(&g_ris_paged_wait, 2u);
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == kScores) tmem_dealloc<1, L::COLS>(tmem);
+}
+
+// ---------------------------------------------------------------- host side
+bool encode(CUtensorMap *m, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box)
+{
+    auto fn = encode_fn();
+    if (fn == nullptr) return false;
+    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// the query rows as (channel, head, token): a box is the heads of a block of as many tokens as a row tile holds
+bool query_map(CUtensorMap *m, const PagedAttendArgs &a)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)a.c.D, (cuuint64_t)a.Hq, (cuuint64_t)a.q_total}, strides[2] = {(cuuint64_t)a.c.D * 2, (cuuint64_t)a.q_stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.block, (cuuint32_t)a.tokens};
+    return encode(m, a.q, 3, dims, strides, box);
+}
+// a pool as (channel, slot, head, page): a box is a page's slots, or a tile's
+bool pool_map(CUtensorMap *m, const PagedAttendArgs &a, const void *pool)
+{
+    const cuuint64_t dims[4] = {(cuuint64_t)a.c.D, (cuuint64_t)1 << a.c.page_log2, (cuuint64_t)a.c.Hkv, (cuuint64_t)a.c.n_pages},
+                     strides[3] = {(cuuint64_t)a.c.slot_stride * 2, (cuuint64_t)a.c.head_stride * 2, (cuuint64_t)a.c.page_stride * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(BN, 1 << a.c.page_log2), 1, 1};
+    return encode(m, pool, 4, dims, strides, box);
+}
+
+template <int D>
+cudaError_t launch(const PagedAttendArgs &a, const Maps &maps, cudaStream_t s)
+{
+    using L = Lay<D>;
+    static Once once;
+    const cudaError_t ready = once([] {
+        cudaError_t e = cudaFuncSetAttribute(k_paged_tiles<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+        cudaFuncAttributes fa;
+        if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, k_paged_tiles<D>);
+        // (setmaxnreg would wait forever on registers that the launch does not have)
+        return e != cudaSuccess ? e : (fa.numRegs + 7) / 8 * 8 < L::REGS ? cudaErrorInvalidConfiguration : cudaSuccess;
+    });
+    if (ready != cudaSuccess) return ready;
+    return launch_chained(k_paged_tiles<D>, dim3((unsigned)a.ctas), dim3(L::THREADS), L::BYTES, s, a, maps);
+}
+
+}  // namespace
+
+cudaError_t launch_paged_tiles(const PagedAttendArgs &a, cudaStream_t s)
+{
+    alignas(64) Maps maps;
+    if (!query_map(&maps.q, a) || !pool_map(&maps.k, a, a.c.k) || !pool_map(&maps.v, a, a.c.v)) return cudaErrorInvalidValue;
+    return a.c.D == 128 ? launch<128>(a, maps, s) : launch<64>(a, maps, s);
+}
+
+cudaError_t paged_tiles_error_words(unsigned int **wait, unsigned int **page)
+{
+    const cudaError_t e = cudaGetSymbolAddress(reinterpret_cast<void **>(wait), g_ris_paged_wait);
+    return e != cudaSuccess ? e : cudaGetSymbolAddress(reinterpret_cast<void **>(page), g_ris_paged_page);
+}
+
+}  // namespace ris

@@ -98,6 +98,7 @@ struct RunMem {
     int64_t sums[32];
     int64_t u0;
     int item;
+    Run run;  // (a place for the caller's copy)
 };
 template <int BN, int THREADS>
 __device__ __forceinline__ Run run_of(const PagedAttendArgs &a, int cta, RunMem &mem)

@@ -1,6 +1,6 @@
 // A cache in pages: writing rows into it, the plan of an attention call whose sequences have several row
 // tiles, the join of row tiles that several CTAs worked on, and attention in fp32 (the FP32 pipe; inputs
-// never pass through a narrower product).
+// never pass through a narrower product). bf16: attn_paged.cu.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -212,15 +212,10 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
 // scores. S: a 4 x 4 patch per thread, 4 elements at a time as packed pairs; the softmax over the 16 lanes
 // that share a row; O += P V with a 4 x D / 16 patch, P as pairs of the same weight in shared memory. Bound by
 // the FMA pipe: 4 D flops per row and key.
-constexpr int BM = kPagedRows, BN = kPagedKeys, LP = 2 * BN + 4;  // rows and keys of a tile, pitch of P
+constexpr int BM = kPagedF32Rows, BN = kPagedF32Keys, LP = 2 * BN + 4;  // rows and keys of a tile, pitch of P
 constexpr int kThreads = 4 * BM;
 
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
-__device__ __forceinline__ void store4(__nv_bfloat16 *p, float4 x)
-{
-    const __nv_bfloat162 a = __floats2bfloat162_rn(x.x, x.y), b = __floats2bfloat162_rn(x.z, x.w);
-    *reinterpret_cast<uint2 *>(p) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
-}
 __device__ __forceinline__ uint64_t f2(float x, float y)
 {
     uint64_t d;
@@ -245,16 +240,11 @@ __device__ __forceinline__ float2 f2_get(uint64_t v)
     asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
     return r;
 }
-// four elements to shared memory as fp32, or zeros
-__device__ __forceinline__ void copy4(float *dst, const float *src, bool there)
+// 16 bytes to shared memory, or zeros
+__device__ __forceinline__ void copy16(float *dst, const float *src, bool there)
 {
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy4(float *dst, const __nv_bfloat16 *src, bool there)
-{
-    const uint2 w = there ? *reinterpret_cast<const uint2 *>(src) : make_uint2(0u, 0u);
-    *reinterpret_cast<uint4 *>(dst) = make_uint4(w.x << 16, w.x & 0xFFFF0000u, w.y << 16, w.y & 0xFFFF0000u);
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -265,14 +255,14 @@ __device__ __forceinline__ void copied_but()  // all but the last N groups
 
 // The keys (or values) of a tile that some row of the unit sees, the others as zeros, into rows of pitch
 // D + 4 or D
-template <typename T, int D, bool PAD>
+template <int D, bool PAD>
 __device__ __forceinline__ void fetch_keys(const PagedAttendArgs &a, const Unit &u, float *dst, const void *pool, int k0)
 {
 #pragma unroll 4
     for (int e = 0; e < BN * (D / 4) / kThreads; ++e) {
         const int t = threadIdx.x + e * kThreads, r = t / (D / 4), d = t % (D / 4) * 4, j = k0 + r;
         bool there = j < u.sight.end && (j >= u.sight.low || j < a.anchors);
-        const T *src = reinterpret_cast<const T *>(pool);
+        const float *src = reinterpret_cast<const float *>(pool);
         if (there) {
             const int page = page_of(a.c, u.seq, j);
             there = page >= 0;
@@ -281,12 +271,12 @@ __device__ __forceinline__ void fetch_keys(const PagedAttendArgs &a, const Unit 
             else
                 atomicOr(&g_ris_paged_error, 1u);
         }
-        copy4(dst + r * (PAD ? D + 4 : D) + d, src, there);
+        copy16(dst + r * (PAD ? D + 4 : D) + d, src, there);
     }
     copies_end();
 }
 
-template <typename T, int D>
+template <int D>
 __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant__ PagedAttendArgs a)
 {
     constexpr int LK = D + 4, C = D / 16;  // columns of O of a thread
@@ -306,12 +296,12 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
         for (int e = 0; e < BM * (D / 4) / kThreads && u.j0 < u.j1; ++e) {
             const int t = threadIdx.x + e * kThreads, r = t / (D / 4), d = t % (D / 4) * 4, tok = r / a.block, h = r % a.block;
             const bool there = tok < u.sight.tokens && h < u.heads;
-            const T *q = reinterpret_cast<const T *>(a.q) + (there ? (int64_t)(u.row0 + tok) * a.q_stride + (u.head0 + h) * D + d : 0);
-            copy4(qs + r * LK + d, q, there);
+            const float *q = reinterpret_cast<const float *>(a.q) + (there ? (int64_t)(u.row0 + tok) * a.q_stride + (u.head0 + h) * D + d : 0);
+            copy16(qs + r * LK + d, q, there);
         }
         if (u.j0 < u.j1) {
-            fetch_keys<T, D, true>(a, u, ks, a.c.k, BN * u.sight.tile(u.j0));
-            fetch_keys<T, D, false>(a, u, vs, a.c.v, BN * u.sight.tile(u.j0));
+            fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.tile(u.j0));
+            fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.tile(u.j0));
         }
         int pos[4];  // of each row; one that is not there sees nothing
 #pragma unroll
@@ -348,7 +338,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
             }
             __syncthreads();  // the keys' buffer is free
             if (more)
-                fetch_keys<T, D, true>(a, u, ks, a.c.k, BN * u.sight.tile(t + 1));
+                fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.tile(t + 1));
             else
                 copies_end();
 #pragma unroll
@@ -411,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
                 values(std::true_type{});
             __syncthreads();  // the values' buffer and P's are free
             if (more)
-                fetch_keys<T, D, false>(a, u, vs, a.c.v, BN * u.sight.tile(t + 1));
+                fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.tile(t + 1));
             else
                 copies_end();
         }
@@ -426,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
             const int64_t row = u.row0 + tok;
             if (u.part < 0) {
                 const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // no key: zeros; NaN stays
-                T *out = reinterpret_cast<T *>(a.out) + (row * a.Hq + u.head0 + h) * D;
+                float *out = reinterpret_cast<float *>(a.out) + (row * a.Hq + u.head0 + h) * D;
                 if (tx == 0 && a.lse != nullptr) a.lse[(u.head0 + h) * a.q_total + row] = (m[i] + log2f(sum)) * kLn2;
 #pragma unroll
                 for (int c = 0; c < C / 4; ++c) {
@@ -447,14 +437,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
     if (threadIdx.x == 0) a.split[blockIdx.x] = split;
 }
 
-template <typename T, int D>
+template <int D>
 cudaError_t launch_f32(const PagedAttendArgs &a, cudaStream_t s)
 {
     constexpr int bytes = ((BM + BN) * (D + 4) + BN * D + BM * LP) * (int)sizeof(float);
     static Once once;
-    const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_paged_f32<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_paged_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
-    return launch_chained(k_paged_f32<T, D>, dim3((unsigned)a.ctas), dim3(kThreads), bytes, s, a);
+    return launch_chained(k_paged_f32<D>, dim3((unsigned)a.ctas), dim3(kThreads), bytes, s, a);
 }
 
 template <typename T, int D>
@@ -486,9 +476,9 @@ cudaError_t launch_paged_append(PagedAppendArgs a, int dtype, cudaStream_t s)
     return launch_chained(k_paged_lengths, dim3((unsigned)std::min<int64_t>(16, (a.c.B + kAppendThreads - 1) / kAppendThreads)), dim3(kAppendThreads), 0, s, a);
 }
 
-cudaError_t launch_paged_plan(const PagedAttendArgs &a, cudaStream_t s)
+cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s)
 {
-    return launch_chained(k_paged_plan<BN>, dim3(1), dim3(kPlanThreads), 0, s, a);
+    return launch_chained(dtype == RIS_F32 ? k_paged_plan<kPagedF32Keys> : k_paged_plan<kPagedTileKeys>, dim3(1), dim3(kPlanThreads), 0, s, a);
 }
 
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s)
@@ -497,11 +487,7 @@ cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t 
     return a.c.D == 128 ? launch_join<__nv_bfloat16, 128>(a, s) : launch_join<__nv_bfloat16, 64>(a, s);
 }
 
-cudaError_t launch_paged_f32(const PagedAttendArgs &a, int dtype, cudaStream_t s)
-{
-    if (dtype == RIS_F32) return a.c.D == 128 ? launch_f32<float, 128>(a, s) : launch_f32<float, 64>(a, s);
-    return a.c.D == 128 ? launch_f32<__nv_bfloat16, 128>(a, s) : launch_f32<__nv_bfloat16, 64>(a, s);
-}
+cudaError_t launch_paged_f32(const PagedAttendArgs &a, cudaStream_t s) { return a.c.D == 128 ? launch_f32<128>(a, s) : launch_f32<64>(a, s); }
 
 cudaError_t paged_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_paged_error); }
 

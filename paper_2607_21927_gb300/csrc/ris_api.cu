@@ -390,7 +390,7 @@ void set_error_text(const char *msg) { t_err = msg; }
 
 // The error words of the kernels, taken (and cleared) by one small kernel so that ris_device_status needs one copy: four copies, with
 // ten microseconds each, took twice as long as the two there were before the serving kernels.
-constexpr int kErrorWords = 5;
+constexpr int kErrorWords = 7;
 struct ErrorWords {
     unsigned int *p[kErrorWords];
 };
@@ -939,6 +939,7 @@ ris_status ris_device_status(void *stream)
     RIS_CUDA(cache4_error_word(&at.p[2]));
     RIS_CUDA(decode_error_word(&at.p[3]));
     RIS_CUDA(paged_error_word(&at.p[4]));
+    RIS_CUDA(paged_tiles_error_words(&at.p[5], &at.p[6]));
     unsigned int w[kErrorWords] = {};
     {
         std::lock_guard<std::mutex> lk(g_status_mu);
@@ -947,7 +948,7 @@ ris_status ris_device_status(void *stream)
         RIS_CUDA(cudaMemcpyFromSymbolAsync(w, g_ris_error_words, sizeof(w), 0, cudaMemcpyDeviceToHost, s));
         RIS_CUDA(cudaStreamSynchronize(s));
     }
-    const unsigned int word = w[0] | w[1] | (w[2] & 4u), cache_word = w[2], decode_word = w[3], paged_word = w[4];
+    const unsigned int word = w[0] | w[1] | (w[2] & 4u) | w[5], cache_word = w[2], decode_word = w[3], paged_word = w[4] | w[6];
     if (word != 0u) return fail(RIS_ERR_DEVICE_TIMEOUT, "a device-side wait gave up (error word 0x%x)", word);
     if (decode_word != 0u)
         return fail(RIS_ERR_INVALID, "a decode step read a position outside [t0, cache_len) from t_dev");

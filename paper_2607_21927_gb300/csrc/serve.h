@@ -107,7 +107,7 @@ cudaError_t launch_norm_rope(const NormRopeArgs &a, int dtype, int D, bool pairs
 void norm_rope_ctas(int dtype, int D, int64_t n, const int32_t (&heads)[2], int32_t (&ctas)[2]);
 cudaError_t launch_norm_rope_backward(const NormRopeArgs &a, int dtype, int D, bool pairs, float *gq, float *gk, cudaStream_t s);
 
-// A cache in pages (paged.cu).
+// A cache in pages (paged.cu, attn_paged.cu).
 struct PagedArgs {
     void *k, *v;               // pools of n_pages pages
     int64_t page_stride, head_stride, slot_stride;  // elements
@@ -163,10 +163,12 @@ struct PagedAttendArgs {
     float2 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum)
 };
 constexpr int kPagedCtas = 2 * 152;
-constexpr int kPagedRows = 32, kPagedKeys = 64;  // of a row tile, of a key tile
-cudaError_t launch_paged_plan(const PagedAttendArgs &a, cudaStream_t s);
+// rows of a row tile and keys of a key tile, fp32 and bf16
+constexpr int kPagedF32Rows = 32, kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128;
+cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);
-cudaError_t launch_paged_f32(const PagedAttendArgs &a, int dtype, cudaStream_t s);
+cudaError_t launch_paged_f32(const PagedAttendArgs &a, cudaStream_t s);
+cudaError_t launch_paged_tiles(const PagedAttendArgs &a, cudaStream_t s);
 
 struct Cache4Args {
     uint8_t *k, *v;              // [B][Hkv][cap][D / 2]
@@ -230,8 +232,10 @@ cudaError_t launch_cache4_evict(const Cache4EvictArgs &a, int32_t *holes, cudaSt
 // wait gave up) and of the packed attention's tile kernels (a bounded wait gave up), on the current device.
 cudaError_t cache4_error_word(unsigned int **p);
 cudaError_t packed_error_word(unsigned int **p);
-// Of the paged cache's kernels (a token or key outside the pages).
+// Of the paged cache's kernels: a token or key outside the pages; of its tile kernel alone: a bounded wait gave
+// up, a key outside the pages.
 cudaError_t paged_error_word(unsigned int **p);
+cudaError_t paged_tiles_error_words(unsigned int **wait, unsigned int **page);
 
 // What ris_debug_tile_stall asks for (ris_api.cu): cycles that a wait may take, 0 where nothing is asked;
 // whether loads are left out.

@@ -1,7 +1,7 @@
 // C ABI of the serving operators: packed prompts, positions on several axes, the 4-bit cache, normed and
 // turned heads, and the cache in pages. Argument checks, the plan of a pack, scratch and the launches; the
-// work is in rope_axes.cu, norm_rope.cu, attn_packed.cu, attn_packed_f32.cu, cache4.cu, cache4_evict.cu and
-// paged.cu.
+// work is in rope_axes.cu, norm_rope.cu, attn_packed.cu, attn_packed_f32.cu, cache4.cu, cache4_evict.cu, paged.cu
+// and attn_paged.cu.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -834,20 +834,22 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.off = pack->q_off;
     a.Hq = heads;
     a.G = heads / cache->kv_heads;
-    a.window = window;
-    a.anchors = anchors;
+    a.window = std::min(window, 1 << 30);  // (no sequence is longer)
+    a.anchors = std::min(anchors, 1 << 30);
     a.reach = (int32_t)(longest > 0 ? longest : capacity);
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
     a.least = 1;
-    a.block = std::min(a.G, kPagedRows);
+    const bool tiles = cache->dtype == RIS_BF16;
+    const int32_t tile_rows = tiles ? kPagedTileRows : kPagedF32Rows;
+    a.block = std::min(a.G, tile_rows);
     a.blocks = (a.G + a.block - 1) / a.block;
-    a.tokens = kPagedRows / a.block;
+    a.tokens = tile_rows / a.block;
     a.part_rows = (int32_t)std::min<int64_t>(a.tokens, pack->q_longest) * a.block;
     const int64_t items = pack->q_longest <= a.tokens ? pack->n_seqs : pack->q_total / a.tokens + pack->n_seqs;
     if (pack->q_longest > a.tokens) a.max_items = (int32_t)items;
     // no more CTAs than the longest line there can be has key tiles
-    const int64_t tiles = a.reach / kPagedKeys + 3, line = items * cache->kv_heads * a.blocks;
-    a.ctas = (int32_t)std::min<int64_t>(kPagedCtas, line > kPagedCtas ? line : line * tiles);
+    const int64_t most = a.reach / (tiles ? kPagedTileKeys : kPagedF32Keys) + 3, line = items * cache->kv_heads * a.blocks;
+    a.ctas = (int32_t)std::min<int64_t>(kPagedCtas, line > kPagedCtas ? line : line * most);
     const bool plan = a.max_items > 0;
     const size_t prefix_b = plan ? room(sizeof(int64_t) * (items + 1)) : 0, item_b = plan ? room(sizeof(PagedItem) * items) : 0,
                  seq_b = plan ? room(sizeof(int32_t) * (pack->n_seqs + 1)) : 0, split_b = room(sizeof(PagedSplit) * a.ctas),
@@ -863,8 +865,8 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.split = reinterpret_cast<PagedSplit *>(d), d += split_b;
     a.part_ml = reinterpret_cast<float2 *>(d), d += ml_b;
     a.part_o = reinterpret_cast<float *>(d);
-    if (plan) RIS_CUDA(launch_paged_plan(a, s));
-    RIS_CUDA(launch_paged_f32(a, cache->dtype, s));
+    if (plan) RIS_CUDA(launch_paged_plan(a, cache->dtype, s));
+    RIS_CUDA(tiles ? launch_paged_tiles(a, s) : launch_paged_f32(a, s));
     if (a.ctas > 1) RIS_CUDA(launch_paged_join(a, cache->dtype, s));
     return RIS_OK;
 }
