@@ -47,10 +47,11 @@ using namespace paged;
 constexpr int BM = kTileRows, BN = kTileKeys;
 static_assert(kPagedTileRows == BM && kPagedTileKeys == BN, "as the work is shared out");
 constexpr int kGroupWarps = 4;  // of the softmax group: one thread per row
-// The reference m of a row is its largest score so far: the weight of a key that takes nearly all is 1, which
-// bf16 holds. Up to here the exponent of a weight is rounded once, and that key's is within 2^-12 of 0 (the
-// reference was rounded as a product); scores beyond are rounded as products first, so that it is 0.
-constexpr float kFarLog2 = 0x1p12f;
+// The reference m of a row moves only when its largest score grows by more than this: P stays below 2^7.
+constexpr float kLazyLog2 = 7.f;
+// The exponent of a weight is rounded once, the reference behind it was rounded as a product: rows that pass
+// this (no model's do) are computed from the inputs as given, where both are rounded alike.
+constexpr float kFarLog2 = 0x1p28f;
 
 template <int D>
 struct Lay {
@@ -171,7 +172,7 @@ __device__ __noinline__ void row_as_given(const PagedAttendArgs &a, const Unit &
     } else {
         const int64_t at = (int64_t)u.part * a.part_rows + tok * a.block + head;
         for (int c = 0; c < C; ++c) a.part_o[at * D + C * lane + c] = o[c];
-        if (lane == 0) a.part_ml[at] = make_float2(m, l);
+        if (lane == 0) a.part_ml[at] = make_float4(m, l, l, 0.f);
     }
 }
 
@@ -414,8 +415,9 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
             const bool idle = !__any_sync(0xFFFFFFFFu, valid);
             const int pos0 = x.pos0, pos = pos0 + tok, end = x.end;
             int k0 = x.key(0), jump = x.sinks - x.j0;  // tiles up to the window's
-            bool far = false;
-            float l = 0.f, m = -INFINITY;  // row sum, reference
+            // row sum, reference, largest score; by how much the largest score's weight is rounded up: the outputs
+            // are divided by the sum with that weight as rounded, so that a row whose weight goes to one key is that key's values
+            float l = 0.f, m = -INFINITY, top = -INFINITY, up = 0.f;
             for (int j = 0; j < n; ++j, ++t, k0 = j == jump ? BN * x.first : k0 + BN) {
                 // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
                 if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL, t & 1);
@@ -455,30 +457,26 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                             for (int e = 0; e < 32; ++e) drop_unless(sv[32 * w + e], cw[w], 1u << e);
                         }
                     }
-                    float sc = a.scale_log2;
-                    const float mx = valid ? __fmul_rn(row_max(sv), sc) : -INFINITY;
-                    const bool upd = mx > m;
+                    const float raw = valid ? row_max(sv) : -INFINITY, mx = __fmul_rn(raw, a.scale_log2);
+                    const bool upd = mx > m + kLazyLog2;
                     const bool scale_o = upd && m != -INFINITY;
                     const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
                     const float al = scale_o ? exp2f(m - mx) : 1.f;
                     l *= al;
                     m = upd ? mx : m;
                     const float mu = m == -INFINITY ? 0.f : m;
-                    far = __any_sync(0xFFFFFFFFu, fabsf(mu) > kFarLog2);
-                    if (far) {
-#pragma unroll
-                        for (int e = 0; e < BN; ++e) sv[e] = __fmul_rn(sv[e], sc);
-                        sc = 1.f;
-                    }
                     uint32_t hw[BN / 2];
-                    float sum = weights_of<0, 96>(sv, sc, mu, hw);
+                    float sum = weights_of<0, 96>(sv, a.scale_log2, mu, hw);
                     // polled here, the answers are there when the weights are
                     bool settled = true;
                     if (!L::OVER) {
                         settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
                         there = mbar_test<1>(bar(L::B_S_FULL), (t + 1) & 1);
                     }
-                    l += sum + weights_of<96, BN>(sv, sc, mu, hw);
+                    l += sum + weights_of<96, BN>(sv, a.scale_log2, mu, hw);
+                    const float w = ex2(fmaf(raw, a.scale_log2, -mu));
+                    up = mx > top ? __bfloat162float(__float2bfloat16_rn(w)) - w : up * al;
+                    top = fmaxf(top, mx);
                     // P's buffer is free and O has settled once the last value product is done (where P takes
                     // the scores' place, the scores were computed after that; a unit's first tile: waited for
                     // at the end of the last unit)
@@ -545,14 +543,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                     }
                 }
             };
+            const float by = l + up, far = fabsf(m) > kFarLog2 && fabsf(m) < INFINITY ? NAN : 1.f;
             if (part < 0) {
                 const int64_t row = row0 + tok;
                 if (valid && a.lse != nullptr) a.lse[(head0 + head) * a.q_total + row] = (m + log2f(l)) * kLn2;
-                emit(reinterpret_cast<__nv_bfloat16 *>(a.out), l == 0.f ? 0.f : 1.f / l, valid ? (row * a.Hq + head0 + head) * D : -1);
+                emit(reinterpret_cast<__nv_bfloat16 *>(a.out), l == 0.f ? 0.f : far / by, valid ? (row * a.Hq + head0 + head) * D : -1);
             } else {
                 const int64_t at = (int64_t)part * a.part_rows + r;
-                if (valid) a.part_ml[at] = make_float2(m, l);
-                emit(a.part_o, l == 0.f ? 0.f : 1.f, valid ? at * D : -1);
+                if (valid) a.part_ml[at] = make_float4(m, l, by, 0.f);
+                emit(a.part_o, l == 0.f ? 0.f : far, valid ? at * D : -1);
             }
             tc_fence_before();  // (O has been read before the next P is announced)
         }

@@ -129,15 +129,16 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
 }
 
 // ---------------------------------------------------------------- the join
-// out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) l_p over the parts of a row, in their order. CTAs (run that
-// began the row tile, group of rows); W warps take every W-th part of a row and are added up in order.
+// out = sum_p 2^(m_p - m) O_p / sum_p 2^(m_p - m) n_p over the parts of a row, in their order, and its log-sum-exp from
+// the sums l_p (n_p is l_p, or with a weight as it was rounded). CTAs (run that began the row tile, group of rows);
+// W warps take every W-th part of a row and are added up in order.
 constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32;
 
 template <typename T, int D, int W>
 __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_constant__ PagedAttendArgs a)
 {
     constexpr int C = D / 32, ROWS = kJoinWarps / W;
-    __shared__ float2 ml[kJoinWarps];
+    __shared__ float4 ml[kJoinWarps];
     __shared__ float os[kJoinWarps][D];
     after_last();
     const PagedSplit sp = a.split[blockIdx.x];
@@ -145,16 +146,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % W;
     const int r = blockIdx.y * ROWS + warp / W, token = r / a.block, head = r % a.block;
     const bool there = token < sp.tokens && head < sp.heads;
-    float m = -INFINITY, l = 0.f, o[C] = {};
+    float m = -INFINITY, l = 0.f, n = 0.f, o[C] = {};
     if (there) {
         auto place = [&](int c) { return (int64_t)(2 * c + (c == sp.first ? 1 : 0)) * a.part_rows + r; };
-        for (int c = sp.first + wr; c <= sp.last; c += W) {
-            m = fmaxf(m, a.part_ml[place(c)].x);
-        }
+        // (a lane looks at every 32nd of the warp's parts)
+        for (int c = sp.first + wr + W * lane; c <= sp.last; c += 32 * W) m = fmaxf(m, a.part_ml[place(c)].x);
+        m = warp_max(m);
         const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll 4
         for (int c = sp.first + wr; c <= sp.last; c += W) {
-            const float2 y = a.part_ml[place(c)];
+            const float4 y = a.part_ml[place(c)];
             const float *p = a.part_o + place(c) * D + C * lane;
             float z[C];
             if constexpr (C == 4) {
@@ -167,37 +168,38 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
             // (a part without a visible key adds nothing, whatever its product holds)
             const float f = y.y == 0.f ? 0.f : exp2f(y.x - ref);
             l = fmaf(y.y, f, l);
+            n = fmaf(y.z, f, n);
 #pragma unroll
             for (int e = 0; e < C; ++e) o[e] = y.y == 0.f ? o[e] : fmaf(z[e], f, o[e]);
         }
     }
     if constexpr (W > 1) {
-        if (lane == 0) ml[warp] = make_float2(m, l);
+        if (lane == 0) ml[warp] = make_float4(m, l, n, 0.f);
 #pragma unroll
         for (int e = 0; e < C; ++e) os[warp][C * lane + e] = o[e];
         __syncthreads();
         if (wr != 0) return;
         for (int i = 0; i < W; ++i) m = fmaxf(m, ml[warp + i].x);
         const float ref = m == -INFINITY ? 0.f : m;
-        l = 0.f;
+        l = n = 0.f;
 #pragma unroll
         for (int e = 0; e < C; ++e) o[e] = 0.f;
         for (int i = 0; i < W; ++i) {
-            const float2 y = ml[warp + i];
+            const float4 y = ml[warp + i];
             if (y.y == 0.f) continue;
             const float f = exp2f(y.x - ref);
             l = fmaf(y.y, f, l);
+            n = fmaf(y.z, f, n);
 #pragma unroll
             for (int e = 0; e < C; ++e) o[e] = fmaf(os[warp + i][C * lane + e], f, o[e]);
         }
     }
     if (!there) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
     const int64_t row = sp.row0 + token;
     T *out = reinterpret_cast<T *>(a.out) + (row * a.Hq + sp.head0 + head) * D + C * lane;
 #pragma unroll
     for (int e = 0; e < C; ++e) {
-        const float x = l == 0.f ? 0.f : o[e] * inv;
+        const float x = l == 0.f ? 0.f : o[e] / n;
         if constexpr (sizeof(T) == 4)
             out[e] = x;
         else
@@ -425,7 +427,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
                 }
             } else {
                 const int64_t at = (int64_t)u.part * a.part_rows + r;
-                if (tx == 0) a.part_ml[at] = make_float2(m[i], sum);
+                if (tx == 0) a.part_ml[at] = make_float4(m[i], sum, sum, 0.f);
 #pragma unroll
                 for (int c = 0; c < C / 4; ++c) {
                     const float2 x = f2_get(o[i][2 * c]), y = f2_get(o[i][2 * c + 1]);

@@ -160,7 +160,7 @@ struct PagedAttendArgs {
     PagedSplit *split;         // [ctas]
     int32_t part_rows;         // rows of a part
     float *part_o;             // [2 ctas][part_rows][D]
-    float2 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum)
+    float4 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum, what the outputs are divided by)
 };
 constexpr int kPagedCtas = 2 * 152;
 // rows of a row tile and keys of a key tile, fp32 and bf16

@@ -853,7 +853,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     const bool plan = a.max_items > 0;
     const size_t prefix_b = plan ? room(sizeof(int64_t) * (items + 1)) : 0, item_b = plan ? room(sizeof(PagedItem) * items) : 0,
                  seq_b = plan ? room(sizeof(int32_t) * (pack->n_seqs + 1)) : 0, split_b = room(sizeof(PagedSplit) * a.ctas),
-                 ml_b = room(sizeof(float2) * 2 * a.ctas * a.part_rows), o_b = room(sizeof(float) * 2 * a.ctas * a.part_rows * cache->head_dim);
+                 ml_b = room(sizeof(float4) * 2 * a.ctas * a.part_rows), o_b = room(sizeof(float) * 2 * a.ctas * a.part_rows * cache->head_dim);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const PackUse use{pack, s};
     Scratch mem;
@@ -863,7 +863,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.items = reinterpret_cast<PagedItem *>(d), d += item_b;
     a.n_items = reinterpret_cast<int32_t *>(d), a.seq_items = a.n_items + 1, d += seq_b;
     a.split = reinterpret_cast<PagedSplit *>(d), d += split_b;
-    a.part_ml = reinterpret_cast<float2 *>(d), d += ml_b;
+    a.part_ml = reinterpret_cast<float4 *>(d), d += ml_b;
     a.part_o = reinterpret_cast<float *>(d);
     if (plan) RIS_CUDA(launch_paged_plan(a, cache->dtype, s));
     RIS_CUDA(tiles ? launch_paged_tiles(a, s) : launch_paged_f32(a, s));
