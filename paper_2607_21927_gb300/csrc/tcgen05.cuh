@@ -377,8 +377,8 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Two fp32 values in one 64-bit register, and their packed fused multiply-add (each half
-// rounded as the scalar operation).
+// Two fp32 values in one 64-bit register, and their packed operations (each half rounded as the scalar
+// operation).
 __device__ __forceinline__ uint64_t f2_pack(float x, float y)
 {
     uint64_t d;
@@ -395,7 +395,12 @@ __device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
     return d;
 }
-
+__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ uint64_t f2_add(uint64_t a, uint64_t b)
 {
     uint64_t d;

@@ -844,8 +844,8 @@ def ris_cache4_evict(src: Cache4, dst: Cache4, budget: int, recent: int, kept: O
 def _like(out, x: torch.Tensor, name: str):
     """An output of x's shape [n, H, D] and type: (tensor, elements from token to token)."""
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        return out, x.shape[1] * x.shape[2]
+        n, H, D = x.shape
+        return x.new_empty((n, H, D)), H * D
     if out.dtype != x.dtype or out.shape != x.shape:
         raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}")
     return out, _heads(out, name)[3]
@@ -854,7 +854,7 @@ def _like(out, x: torch.Tensor, name: str):
 def _weight(w: Optional[torch.Tensor], x: torch.Tensor, name: str):
     if w is None:
         return None
-    if w.dtype != x.dtype or tuple(w.shape) != (x.shape[-1],) or not w.is_contiguous() or w.device != x.device:
+    if w.dtype != x.dtype or w.shape != x.shape[2:] or not w.is_contiguous() or w.get_device() != x.get_device():
         raise ValueError(f"{name}: contiguous {x.dtype} [{x.shape[-1]}] on {x.device}")
     return w.data_ptr()
 

@@ -5,7 +5,7 @@ a normed channel by less than that of itself (the sum of squares: 128 terms of r
 the root 2^-22; two products): 4e-6 of the pair's norm in all; bf16 results add half a step, 2^-8 of the result. Backwards
 dx = r (u - h mean(u h)): u is off by 3e-6 of the head's largest, the mean by 6e-6 of the mean of |u h|, r and h by 1e-6:
 1e-5 r (max |u| + |h| mean |u h|). A weight's gradient: each of its terms by 1e-5 of (pair's norm of g) |h|, the sums by less than
-another 1e-5 of the sum of these (40 sequential additions at most in these sizes)."""
+another 1e-5 of the sum of these (100 sequential additions at most in these sizes: 100 x 2^-24 = 6e-6)."""
 import pytest
 import torch
 
@@ -56,6 +56,8 @@ CASES = [
     (19, 5, 0, 64, 64, False, BF16, 1, (True, False)),
     (70, 2, 1, 128, 0, False, BF16, 0, (True, True)),   # the norm alone
     (70, 2, 1, 64, 0, False, F32, 0, (False, True)),
+    (10007, 1, 1, 128, 128, False, F32, 1, (True, True)),  # a CTA takes several groups of tokens
+    (9001, 1, 2, 64, 32, True, BF16, 1, (True, True)),
 ]
 
 
