@@ -9,6 +9,7 @@
 
 #include "attn_common.cuh"
 #include "attn_paged.cuh"
+#include "tcgen05.cuh"
 
 namespace ris {
 
@@ -209,39 +210,25 @@ __global__ void __launch_bounds__(kJoinThreads) k_paged_join(const __grid_consta
 }
 
 // ---------------------------------------------------------------- attention in fp32
-// A CTA walks its run of (32 rows x 64 keys) tiles with a running maximum and sum. Keys and values come row by
+// A CTA walks its run of tiles of 8 R rows and 64 keys with a running maximum and sum. Keys and values come row by
 // row by cp.async into a buffer each, the next keys under the value product and the next values under the
-// scores. S: a 4 x 4 patch per thread, 4 elements at a time as packed pairs; the softmax over the 16 lanes
-// that share a row; O += P V with a 4 x D / 16 patch, P as pairs of the same weight in shared memory. Bound by
-// the FMA pipe: 4 D flops per row and key.
-constexpr int BM = kPagedF32Rows, BN = kPagedF32Keys, LP = 2 * BN + 4;  // rows and keys of a tile, pitch of P
-constexpr int kThreads = 4 * BM;
+// scores; two CTAs of an SM fill each other's phases. S: a patch of R x 4 per thread, 4 elements at a time as packed
+// pairs; the softmax over the 16 lanes that share a row; O += P V with a patch of R x D / 16. Rows of Q, K and P lie in
+// 16-byte pieces swizzled by the row's low three bits, so that the rows that a warp reads at once lie in different banks.
+// 4 D flops per row and key on the FMA pipe, which runs at 45% of its rate in long chunks (35 TFLOP/s; 900 tokens behind
+// 301 at 12 / 2 heads of 128: 156 us): the rest goes to operands. A patch of 4 x 4 in tiles of 32 rows took 208 us, 4 x 4
+// with twice the threads on 64 rows 167. Tiles of 8 rows (R = 1) are for single tokens: 16 of them behind 8,000 keys
+// take 124 us (2.1 TB/s) instead of 150 in tiles of 32.
+constexpr int BN = kPagedF32Keys;
+constexpr int kF32Threads = 128, TY = kF32Threads / 16;  // (rows ty + TY i, keys tx + 16 j)
+static_assert(TY == 8 && BN == 64, "the swizzle; a thread's four keys");
+
+using tc::f2_fma;
+using tc::f2_mul;
+using tc::f2_pack;
+using tc::f2_unpack;
 
 __device__ __forceinline__ void store4(float *p, float4 x) { *reinterpret_cast<float4 *>(p) = x; }
-__device__ __forceinline__ uint64_t f2(float x, float y)
-{
-    uint64_t d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(x), "f"(y));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_fma(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t f2_mul(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-__device__ __forceinline__ float2 f2_get(uint64_t v)
-{
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-    return r;
-}
 // 16 bytes to shared memory, or zeros
 __device__ __forceinline__ void copy16(float *dst, const float *src, bool there)
 {
@@ -255,39 +242,39 @@ __device__ __forceinline__ void copied_but()  // all but the last N groups
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// The keys (or values) of a tile that some row of the unit sees, the others as zeros, into rows of pitch
-// D + 4 or D
-template <int D, bool PAD>
+// The keys (or values) of a tile that some row of the unit sees, the others as zeros
+template <int D, bool SWIZZLE>
 __device__ __forceinline__ void fetch_keys(const PagedAttendArgs &a, const Unit &u, float *dst, const void *pool, int k0)
 {
-#pragma unroll 4
-    for (int e = 0; e < BN * (D / 4) / kThreads; ++e) {
-        const int t = threadIdx.x + e * kThreads, r = t / (D / 4), d = t % (D / 4) * 4, j = k0 + r;
-        bool there = j < u.sight.end && (j >= u.sight.low || j < a.anchors);
-        const float *src = reinterpret_cast<const float *>(pool);
-        if (there) {
-            const int page = page_of(a.c, u.seq, j);
-            there = page >= 0;
-            if (there)
-                src += slot_at(a.c, page, u.kv_head, j) + d;
-            else
-                atomicOr(&g_ris_paged_error, 1u);
+    constexpr int AT_ONCE = kF32Threads / (D / 4);  // rows
+    const int w = threadIdx.x / (D / 4), d = threadIdx.x % (D / 4);
+#pragma unroll 2
+    for (int r0 = 0; r0 < BN; r0 += 16) {  // (16 keys of a tile lie in one page)
+        const int j0 = k0 + r0;
+        const bool wanted = j0 < u.sight.end && (j0 + 15 >= u.sight.low || j0 < a.anchors);
+        const int page = wanted ? page_of(a.c, u.seq, j0) : -1;
+        if (wanted && page < 0) atomicOr(&g_ris_paged_error, 1u);
+        const float *src = reinterpret_cast<const float *>(pool) + (page >= 0 ? slot_at(a.c, page, u.kv_head, j0 + w) + 4 * d : 0);
+        const int64_t step = page >= 0 ? AT_ONCE * a.c.slot_stride : 0;
+#pragma unroll
+        for (int e = 0; e < 16 / AT_ONCE; ++e, src += step) {
+            const int r = r0 + e * AT_ONCE + w, j = k0 + r;
+            copy16(dst + r * D + 4 * (SWIZZLE ? d ^ (r & 7) : d), src, page >= 0 && j < u.sight.end && (j >= u.sight.low || j < a.anchors));
         }
-        copy16(dst + r * (PAD ? D + 4 : D) + d, src, there);
     }
     copies_end();
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant__ PagedAttendArgs a)
+template <int D, int R>
+__global__ void __launch_bounds__(kF32Threads, 2) k_paged_f32(const __grid_constant__ PagedAttendArgs a)
 {
-    constexpr int LK = D + 4, C = D / 16;  // columns of O of a thread
+    constexpr int BM = TY * R, C = D / 16;  // columns of O of a thread
     extern __shared__ __align__(16) float sm[];
-    float *const qs = sm, *const ks = qs + BM * LK, *const vs = ks + BN * LK, *const ps = vs + BN * D;
+    float *const qs = sm, *const ks = qs + BM * D, *const vs = ks + BN * D, *const ps = vs + BN * D;
     __shared__ RunMem mem;
     after_last();
-    const Run run = run_of<BN, kThreads>(a, blockIdx.x, mem);
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;  // rows 4 ty + i; keys tx + 16 j; columns 4 tx + 64 c
+    const Run run = run_of<BN, kF32Threads>(a, blockIdx.x, mem);
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;  // rows ty + TY i; keys tx + 16 j; columns 4 tx + 64 c
     PagedSplit split{-1};
     Walk walk(run);
     Unit u;
@@ -295,26 +282,26 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
         if (u.split.first >= 0) split = u.split;
         __syncthreads();  // the last unit's buffers are free
         // the query rows: token r / block, head r % block; zeros for rows that there are not
-        for (int e = 0; e < BM * (D / 4) / kThreads && u.j0 < u.j1; ++e) {
-            const int t = threadIdx.x + e * kThreads, r = t / (D / 4), d = t % (D / 4) * 4, tok = r / a.block, h = r % a.block;
+        for (int t = threadIdx.x; t < BM * (D / 4) && u.j0 < u.j1; t += kF32Threads) {
+            const int r = t / (D / 4), d = t % (D / 4), tok = r / a.block, h = r % a.block;
             const bool there = tok < u.sight.tokens && h < u.heads;
-            const float *q = reinterpret_cast<const float *>(a.q) + (there ? (int64_t)(u.row0 + tok) * a.q_stride + (u.head0 + h) * D + d : 0);
-            copy16(qs + r * LK + d, q, there);
+            const float *q = reinterpret_cast<const float *>(a.q) + (there ? (int64_t)(u.row0 + tok) * a.q_stride + (u.head0 + h) * D + 4 * d : 0);
+            copy16(qs + r * D + 4 * (d ^ (r & 7)), q, there);
         }
         if (u.j0 < u.j1) {
             fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.tile(u.j0));
             fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.tile(u.j0));
         }
-        int pos[4];  // of each row; one that is not there sees nothing
+        int pos[R];  // of each row; one that is not there sees nothing
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = 4 * ty + i, tok = r / a.block;
+        for (int i = 0; i < R; ++i) {
+            const int r = ty + TY * i, tok = r / a.block;
             pos[i] = tok < u.sight.tokens && r % a.block < u.heads ? u.sight.pos0 + tok : -1;
         }
-        uint64_t o[4][C / 2] = {};
-        float m[4], l[4];
+        uint64_t o[R][C / 2] = {};
+        float m[R], l[R];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = -INFINITY, l[i] = 0.f;
+        for (int i = 0; i < R; ++i) m[i] = -INFINITY, l[i] = 0.f;
         for (int t = u.j0; t < u.j1; ++t) {
             const int k0 = BN * u.sight.tile(t);
             const bool more = t + 1 < u.j1;
@@ -322,21 +309,20 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
             const bool whole = k0 + BN - 1 <= u.sight.pos0 && (k0 + BN <= a.anchors || a.window == 0 || u.sight.pos0 + u.sight.tokens - 1 - k0 < a.window);
             copied_but<1>();  // (the values' copy may still be on its way)
             __syncthreads();
-            uint64_t s2[4][4] = {};  // two partial sums of each score: of the even and of the odd elements
-#pragma unroll 4
-            for (int d = 0; d < D; d += 4) {
-                ulonglong2 qa[4], kb[4];
+            uint64_t s2[R][4] = {};  // two partial sums of each score: of the even and of the odd elements
+#pragma unroll 2
+            for (int d = 0; d < D / 4; ++d) {
+                ulonglong2 kb[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qa[i] = *reinterpret_cast<const ulonglong2 *>(qs + (4 * ty + i) * LK + d);
+                for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const ulonglong2 *>(ks + (tx + 16 * j) * D + 4 * (d ^ (tx & 7)));
 #pragma unroll
-                for (int j = 0; j < 4; ++j) kb[j] = *reinterpret_cast<const ulonglong2 *>(ks + (tx + 16 * j) * LK + d);
+                for (int i = 0; i < R; ++i) {
+                    const ulonglong2 qa = *reinterpret_cast<const ulonglong2 *>(qs + (ty + TY * i) * D + 4 * (d ^ ty));
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                    for (int j = 0; j < 4; ++j) s2[i][j] = f2_fma(qa.x, kb[j].x, s2[i][j]);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        s2[i][j] = f2_fma(qa[i].x, kb[j].x, s2[i][j]);
-                        s2[i][j] = f2_fma(qa[i].y, kb[j].y, s2[i][j]);
-                    }
+                    for (int j = 0; j < 4; ++j) s2[i][j] = f2_fma(qa.y, kb[j].y, s2[i][j]);
+                }
             }
             __syncthreads();  // the keys' buffer is free
             if (more)
@@ -344,12 +330,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
             else
                 copies_end();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < R; ++i) {
                 float s[4], mx = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float2 x = f2_get(s2[i][j]);
-                    s[j] = sees(a, pos[i], k0 + tx + 16 * j) ? (x.x + x.y) * a.scale_log2 : -INFINITY;
+                    float x, y;
+                    f2_unpack(s2[i][j], x, y);
+                    s[j] = (x + y) * a.scale_log2;
+                    if (!whole && !sees(a, pos[i], k0 + tx + 16 * j)) s[j] = -INFINITY;
                     mx = fmaxf(mx, s[j]);
                 }
 #pragma unroll
@@ -358,14 +346,15 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
                 const float al = exp2f(m[i] - ref);
                 m[i] = nm;
                 float sum = 0.f;
+                float *const p = ps + (ty + TY * i) * BN + (tx & 3);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     s[j] = exp2f(s[j] - ref);
                     sum += s[j];
-                    *reinterpret_cast<uint64_t *>(ps + (4 * ty + i) * LP + 2 * (tx + 16 * j)) = f2(s[j], s[j]);
+                    p[4 * ((tx / 4 + 4 * j) ^ ty)] = s[j];
                 }
                 l[i] = fmaf(l[i], al, sum);  // this lane's part of the row's sum
-                const uint64_t al2 = f2(al, al);
+                const uint64_t al2 = f2_pack(al, al);
 #pragma unroll
                 for (int c = 0; c < C / 2; ++c) o[i][c] = f2_mul(o[i][c], al2);
             }
@@ -374,20 +363,21 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
             // O += P V; where some row does not see the whole tile, a row takes only the keys that it sees (0 times
             // an infinity or NaN in a key's place is not 0)
             auto values = [&](auto masked) {
-#pragma unroll 4
-                for (int j = 0; j < BN; j += 2) {
-                    ulonglong2 pa[4];
+#pragma unroll 2
+                for (int j = 0; j < BN; j += 4) {
+                    float4 p4[R];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pa[i] = *reinterpret_cast<const ulonglong2 *>(ps + (4 * ty + i) * LP + 2 * j);
+                    for (int i = 0; i < R; ++i) p4[i] = *reinterpret_cast<const float4 *>(ps + (ty + TY * i) * BN + 4 * ((j / 4) ^ ty));
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
+                    for (int e = 0; e < 4; ++e) {
                         ulonglong2 vb[C / 4];
 #pragma unroll
                         for (int c = 0; c < C / 4; ++c) vb[c] = *reinterpret_cast<const ulonglong2 *>(vs + (j + e) * D + 64 * c + 4 * tx);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
+                        for (int i = 0; i < R; ++i) {
                             if (decltype(masked)::value && !sees(a, pos[i], k0 + j + e)) continue;
-                            const uint64_t pp = e == 0 ? pa[i].x : pa[i].y;
+                            const float p = e == 0 ? p4[i].x : e == 1 ? p4[i].y : e == 2 ? p4[i].z : p4[i].w;
+                            const uint64_t pp = f2_pack(p, p);
 #pragma unroll
                             for (int c = 0; c < C / 4; ++c) {
                                 o[i][2 * c] = f2_fma(pp, vb[c].x, o[i][2 * c]);
@@ -409,44 +399,44 @@ __global__ void __launch_bounds__(kThreads, 2) k_paged_f32(const __grid_constant
         }
         copied_but<0>();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < R; ++i) {
             float sum = l[i];
 #pragma unroll
             for (int x = 8; x > 0; x >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-            const int r = 4 * ty + i, tok = r / a.block, h = r % a.block;
+            const int r = ty + TY * i, tok = r / a.block, h = r % a.block;
             if (tok >= u.sight.tokens || h >= u.heads) continue;
             const int64_t row = u.row0 + tok;
+            const float inv = u.part >= 0 ? 1.f : sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // no key: zeros; NaN stays
+            float *to;
             if (u.part < 0) {
-                const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // no key: zeros; NaN stays
-                float *out = reinterpret_cast<float *>(a.out) + (row * a.Hq + u.head0 + h) * D;
+                to = reinterpret_cast<float *>(a.out) + (row * a.Hq + u.head0 + h) * D;
                 if (tx == 0 && a.lse != nullptr) a.lse[(u.head0 + h) * a.q_total + row] = (m[i] + log2f(sum)) * kLn2;
-#pragma unroll
-                for (int c = 0; c < C / 4; ++c) {
-                    const float2 x = f2_get(o[i][2 * c]), y = f2_get(o[i][2 * c + 1]);
-                    store4(out + 64 * c + 4 * tx, make_float4(x.x * inv, x.y * inv, y.x * inv, y.y * inv));
-                }
             } else {
                 const int64_t at = (int64_t)u.part * a.part_rows + r;
+                to = a.part_o + at * D;
                 if (tx == 0) a.part_ml[at] = make_float4(m[i], sum, sum, 0.f);
+            }
 #pragma unroll
-                for (int c = 0; c < C / 4; ++c) {
-                    const float2 x = f2_get(o[i][2 * c]), y = f2_get(o[i][2 * c + 1]);
-                    store4(a.part_o + at * D + 64 * c + 4 * tx, make_float4(x.x, x.y, y.x, y.y));
-                }
+            for (int c = 0; c < C / 4; ++c) {
+                float4 y;
+                f2_unpack(o[i][2 * c], y.x, y.y);
+                f2_unpack(o[i][2 * c + 1], y.z, y.w);
+                store4(to + 64 * c + 4 * tx, make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv));
             }
         }
     }
     if (threadIdx.x == 0) a.split[blockIdx.x] = split;
 }
 
-template <int D>
+template <int D, int R>
 cudaError_t launch_f32(const PagedAttendArgs &a, cudaStream_t s)
 {
-    constexpr int bytes = ((BM + BN) * (D + 4) + BN * D + BM * LP) * (int)sizeof(float);
+    constexpr int bytes = ((TY * R + 2 * BN) * D + TY * R * BN) * (int)sizeof(float);
+    static_assert(2 * (bytes + (int)sizeof(RunMem) + 1024) <= 228 * 1024, "two CTAs of an SM");
     static Once once;
-    const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_paged_f32<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_paged_f32<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
-    return launch_chained(k_paged_f32<D>, dim3((unsigned)a.ctas), dim3(kThreads), bytes, s, a);
+    return launch_chained(k_paged_f32<D, R>, dim3((unsigned)a.ctas), dim3(kF32Threads), bytes, s, a);
 }
 
 template <typename T, int D>
@@ -489,7 +479,15 @@ cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t 
     return a.c.D == 128 ? launch_join<__nv_bfloat16, 128>(a, s) : launch_join<__nv_bfloat16, 64>(a, s);
 }
 
-cudaError_t launch_paged_f32(const PagedAttendArgs &a, cudaStream_t s) { return a.c.D == 128 ? launch_f32<128>(a, s) : launch_f32<64>(a, s); }
+// Rows of a row tile: the smallest that takes the most that a sequence has of them.
+int32_t paged_f32_rows(int64_t rows) { return rows <= 8 ? 8 : rows <= 32 ? 32 : 64; }
+
+cudaError_t launch_paged_f32(const PagedAttendArgs &a, int32_t rows, cudaStream_t s)
+{
+    if (rows == 8) return a.c.D == 128 ? launch_f32<128, 1>(a, s) : launch_f32<64, 1>(a, s);
+    if (rows == 32) return a.c.D == 128 ? launch_f32<128, 4>(a, s) : launch_f32<64, 4>(a, s);
+    return a.c.D == 128 ? launch_f32<128, 8>(a, s) : launch_f32<64, 8>(a, s);
+}
 
 cudaError_t paged_error_word(unsigned int **p) { return cudaGetSymbolAddress(reinterpret_cast<void **>(p), g_ris_paged_error); }
 

@@ -163,11 +163,12 @@ struct PagedAttendArgs {
     float4 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum, what the outputs are divided by)
 };
 constexpr int kPagedCtas = 2 * 152;
-// rows of a row tile and keys of a key tile, fp32 and bf16
-constexpr int kPagedF32Rows = 32, kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128;
+// keys of a key tile and rows of a row tile, fp32 (by the most rows that a sequence has) and bf16
+constexpr int kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128;
+int32_t paged_f32_rows(int64_t rows);
 cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);
-cudaError_t launch_paged_f32(const PagedAttendArgs &a, cudaStream_t s);
+cudaError_t launch_paged_f32(const PagedAttendArgs &a, int32_t rows, cudaStream_t s);
 cudaError_t launch_paged_tiles(const PagedAttendArgs &a, cudaStream_t s);
 
 struct Cache4Args {

@@ -840,7 +840,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
     a.least = 1;
     const bool tiles = cache->dtype == RIS_BF16;
-    const int32_t tile_rows = tiles ? kPagedTileRows : kPagedF32Rows;
+    const int32_t tile_rows = tiles ? kPagedTileRows : paged_f32_rows((int64_t)pack->q_longest * a.G);
     a.block = std::min(a.G, tile_rows);
     a.blocks = (a.G + a.block - 1) / a.block;
     a.tokens = tile_rows / a.block;
@@ -866,7 +866,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.part_ml = reinterpret_cast<float4 *>(d), d += ml_b;
     a.part_o = reinterpret_cast<float *>(d);
     if (plan) RIS_CUDA(launch_paged_plan(a, cache->dtype, s));
-    RIS_CUDA(tiles ? launch_paged_tiles(a, s) : launch_paged_f32(a, s));
+    RIS_CUDA(tiles ? launch_paged_tiles(a, s) : launch_paged_f32(a, tile_rows, s));
     if (a.ctas > 1) RIS_CUDA(launch_paged_join(a, cache->dtype, s));
     return RIS_OK;
 }
