@@ -7,8 +7,13 @@
 // row's sum from the fp32 weights. The heads of a KV head share a row tile (attn_paged.cuh), so few rows
 // read a key once for all of them.
 //
-// Persistent, two CTAs to an SM, each on its run of the line with one row tile at a time and one softmax
-// group (TMEM 256 columns); the two fill each other's waits:
+// Persistent, each CTA on its run of the line, one row tile at a time with one softmax group:
+//   head dim 128  one CTA to an SM and two buffers of scores (TMEM 512 columns): the scores of the next tile and the value
+//                 product of the last run under a tile's softmax. Two CTAs with a buffer each, whose scores wait
+//                 for the value product before, took 1,130 us instead of 1,046 for 8,192 rows behind 24,576 keys at 12 / 2
+//                 heads (1.38 PFLOP/s) and 36 instead of 28 for 24 sequences' four rows through a window of 4,096.
+//   head dim 64   two CTAs to an SM (TMEM 256 columns), weights beside the scores; the products are half as
+//                 long, and one softmax group does not fill an SM: 1,108 us instead of 1,650 for 16,384 rows at 32 / 4 heads.
 //   warp 4  the run's units, query and key tiles, warp 5 value tiles: TMA, a box for each page of a tile, the
 //           boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
 //           fills its place with zeros;
@@ -55,32 +60,39 @@ constexpr float kFarLog2 = 0x1p28f;
 
 template <int D>
 struct Lay {
+    static constexpr int CTAS = paged_tile_ctas(D);        // of an SM
     static constexpr int NB = D / 64;                      // 64-column blocks
-    static constexpr bool OVER = D == 128;                 // P takes the scores' columns
-    static constexpr int NSK = D == 64 ? 3 : 1, NSV = D == 64 ? 2 : 1, NI = 4;
-    static constexpr int BLK = 128 * 128, TILE = NB * BLK; // 128 rows or keys of D 16-bit values
-    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_OUT = OFF_Q + TILE,
-                         OFF_BARS = OFF_OUT + BLK, OFF_INFO = OFF_BARS + 192, OFF_RUN = OFF_INFO + NI * 64,
+    // NS buffers of scores; a tile's weights take the place of its scores, or one place beside them
+    static constexpr int NS = D == 64 ? 1 : 2;
+    static constexpr bool OVER = D == 128;
+    static constexpr int NSK = D == 64 ? 4 : 3, NSV = 2, NI = 4;
+    static constexpr int BLK = 128 * 128, TILE = NB * BLK;  // 128 rows or keys of D 16-bit values
+    static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_BARS = OFF_Q + TILE,
+                         OFF_INFO = OFF_BARS + 256, OFF_RUN = OFF_INFO + NI * 64,
                          OFF_TMEM = OFF_RUN + (int)sizeof(RunMem), BYTES = OFF_TMEM + 16;
     // Barriers, of a ring stage:
     //   K_FULL, V_FULL, Q_FULL  its keys / values / the query tile have landed
     //   K_FREE, V_FREE, Q_FREE  the products that read it are done
     //   I_FULL, I_FREE          a unit's description is there / every role has read it
-    // and one phase per key tile:
+    // and one phase per key tile, of its buffer (tile mod NS):
     //   S_GO    the last scores have been read out of their buffer (only where P has its own columns:
     //           else the value product before has to be done, which says that too)
     //   S_FULL  the next are there
     //   P_GO    P is written (and O rescaled where needed)
     //   PV_DONE O has settled, P's buffer is free
+    // No phase of a barrier is completed before everyone has seen the one before it: scores into a buffer wait for the value
+    // product over its last weights, and these for every softmax warp.
     static constexpr int B_K_FULL = 0, B_V_FULL = B_K_FULL + NSK, B_Q_FULL = B_V_FULL + NSV, B_K_FREE = B_Q_FULL + 1,
                          B_V_FREE = B_K_FREE + NSK, B_Q_FREE = B_V_FREE + NSV, B_I_FULL = B_Q_FREE + 1, B_I_FREE = B_I_FULL + NI,
-                         B_S_GO = B_I_FREE + NI, B_S_FULL = B_S_GO + 1, B_P_GO = B_S_FULL + 1, B_PV_DONE = B_P_GO + 1,
-                         NBAR = B_PV_DONE + 1;
-    static_assert(NBAR <= 24 && 2 * (BYTES + 1024) <= 228 * 1024, "barriers; two CTAs of an SM");
-    static constexpr uint32_t COLS = 256, T_P = OVER ? 0 : BN, T_O = OVER ? BN : BN + BN / 2;  // TMEM; S at 0
+                         B_S_GO = B_I_FREE + NI, B_S_FULL = B_S_GO + 1, B_P_GO = B_S_FULL + NS, B_PV_DONE = B_P_GO + NS,
+                         NBAR = B_PV_DONE + NS;
+    static_assert(8 * NBAR <= OFF_INFO - OFF_BARS && CTAS * (BYTES + 1024) <= 228 * 1024, "barriers; the CTAs of an SM");
+    static constexpr uint32_t COLS = 512 / CTAS, T_P = OVER ? 0 : BN, T_O = NS * BN + (OVER ? 0 : BN / 2);  // TMEM; S at 0
     static_assert(T_O + D <= COLS, "TMEM columns");
-    // registers per thread: at launch, then after setmaxnreg of a softmax and of another thread
-    static constexpr int THREADS = 256, REGS = 128, SOFTMAX_REGS = 200, OTHER_REGS = 56;
+    // Registers per thread: at launch, then after setmaxnreg of a softmax and of another thread. Shared memory leaves
+    // next to no L1, so what a loader spills comes from L2: with 56 instead of 64 (head dim 128: 152) for them, single tokens
+    // against long caches ran at 5.3 TB/s instead of 6.3.
+    static constexpr int THREADS = 256, REGS = CTAS == 2 ? 128 : 192, SOFTMAX_REGS = CTAS == 2 ? 192 : 232, OTHER_REGS = 2 * REGS - SOFTMAX_REGS;
     static_assert(SOFTMAX_REGS + OTHER_REGS == 2 * REGS, "the shares of the two warpgroups add up to the launch's");
 };
 
@@ -204,10 +216,10 @@ struct Maps {
 };
 
 template <int D>
-__global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid_constant__ PagedAttendArgs a, const __grid_constant__ Maps maps)
+__global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(const __grid_constant__ PagedAttendArgs a, const __grid_constant__ Maps maps)
 {
     using L = Lay<D>;
-    constexpr int NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
+    constexpr int NS = L::NS, NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
     constexpr int kLoadQK = 4, kLoadV = 5, kScores = 6;
     extern __shared__ __align__(1024) unsigned char smem[];
     uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
@@ -217,12 +229,12 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
     auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
 
     if (warp == kLoadQK) {
-        if (lane < L::NBAR) {
-            const bool by_group = lane == L::B_S_GO || lane == L::B_P_GO, free = lane >= L::B_I_FREE && lane < L::B_I_FREE + NI;
-            mbar_init(bar(lane), by_group ? kGroupWarps : free ? kGroupWarps + 3 : 1);
-            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (int i = lane; i < L::NBAR; i += 32) {
+            const bool by_group = i == L::B_S_GO || (i >= L::B_P_GO && i < L::B_P_GO + NS), free = i >= L::B_I_FREE && i < L::B_I_FREE + NI;
+            mbar_init(bar(i), by_group ? kGroupWarps : free ? kGroupWarps + 3 : 1);
         }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     } else if (warp == kScores) {
         tmem_alloc<1, L::COLS>(smem_u32(&tmem_base_sh));
     }
@@ -260,23 +272,26 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
         if (warp == kLoadQK) {
             const uint32_t q_bytes = (uint32_t)(a.block * a.tokens * 128 * NB);
             int nq = 0, nk = 0;  // query and key tiles asked for
-            PagedSplit split{-1};
+            if (lane == 0) a.split[blockIdx.x].first = -1;
             Walk walk(run);
             Unit y;
             bool more = walk.next<BN>(a, run, y);
             for (int u = 0; ok; ++u) {
                 if (u >= NI) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up));
                 if (!ok) break;
-                const Info x{more ? y.j1 - y.j0 : -1, y.j0, y.sight.sinks, y.sight.first, y.sight.pos0, y.sight.tokens, y.sight.low, y.sight.end,
+                const Info z{more ? y.j1 - y.j0 : -1, y.j0, y.sight.sinks, y.sight.first, y.sight.pos0, y.sight.tokens, y.sight.low, y.sight.end,
                              y.head0, y.heads, y.kv_head, y.seq, y.row0, y.part};
                 if (lane == 0) {
-                    *reinterpret_cast<Info *>(smem + L::OFF_INFO + u % NI * 64) = x;
+                    *reinterpret_cast<Info *>(smem + L::OFF_INFO + u % NI * 64) = z;
+                    if (more && y.split.first >= 0) a.split[blockIdx.x] = y.split;
                     mbar_arrive(bar(L::B_I_FULL + u % NI));
                 }
                 __syncwarp();
                 if (!more) break;
-                if (y.split.first >= 0) split = y.split;
-                for (int j = 0; j < x.n; ++j, ++nk) {
+                // (read from there, to need fewer registers)
+                const Info &x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
+                const int n = x.n;
+                for (int j = 0; j < n; ++j, ++nk) {
                     const int st = nk % NSK, k0 = x.key(j);
                     const int page = blk < NB ? box_page(a, x, k0, box, box_rows) : 0;
                     if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up));
@@ -299,10 +314,9 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                     ++nq;
                     more = walk.next<BN>(a, run, y);  // (while these are on their way)
                 }
-                if (x.n == 0) more = walk.next<BN>(a, run, y);
+                if (n == 0) more = walk.next<BN>(a, run, y);
             }
             if (lane == 0) {
-                a.split[blockIdx.x] = split;
                 // nothing of this warp's may still be on its way to shared memory when the CTA ends
                 if (nq > 0) mbar_wait_own<1>(bar(L::B_Q_FULL), (nq - 1) & 1);
                 for (int i = max(0, nk - NSK); i < nk; ++i) mbar_wait_own<1>(bar(L::B_K_FULL + i % NSK), (i / NSK) & 1);
@@ -349,15 +363,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                         ok = wait_all(L::B_K_FULL + st, (t / NSK) & 1);
                         if (!L::OVER)
                             ok = ok && wait_all(L::B_S_GO, t & 1);
-                        else if (t > 0)
-                            ok = ok && wait_all(L::B_PV_DONE, (t - 1) & 1);
+                        else if (t >= NS)
+                            ok = ok && wait_all(L::B_PV_DONE + t % NS, (t / NS - 1) & 1);
                         if (!ok) break;
                         const uint32_t kd = desc_lo(sbase + L::OFF_K + st * TILE, 16);
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < D / 16; ++ks)
-                                tc_mma_ss<1>(tb, qd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), kd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), ID_S, ks > 0);
-                            tc_commit<1>(bar(L::B_S_FULL));
+                                tc_mma_ss<1>(tb + t % NS * BN, qd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), kd + dstep((ks >> 2) * L::BLK + (ks & 3) * 32), ID_S, ks > 0);
+                            tc_commit<1>(bar(L::B_S_FULL + t % NS));
                             tc_commit<1>(bar(L::B_K_FREE + st));
                             if (j == n - 1) tc_commit<1>(bar(L::B_Q_FREE));
                         }
@@ -367,14 +381,14 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                     constexpr uint32_t ID_O = idesc_bf16(BM, D, true);
                     for (int j = 0; j < n && ok; ++j, ++t) {
                         const int st = t % NSV;
-                        ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO, t & 1);
+                        ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO + t % NS, (t / NS) & 1);
                         if (!ok) break;
                         const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, L::BLK);
                         if (elect_one()) {
 #pragma unroll
                             for (int ks = 0; ks < BN / 16; ++ks)
-                                tc_mma_ts<1>(tb + L::T_O, tb + L::T_P + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
-                            tc_commit<1>(bar(L::B_PV_DONE));
+                                tc_mma_ts<1>(tb + L::T_O, tb + L::T_P + t % NS * BN + 8 * ks, vd + dstep(ks * 2048), ID_O, ks > 0 || j > 0);
+                            tc_commit<1>(bar(L::B_PV_DONE + t % NS));
                             tc_commit<1>(bar(L::B_V_FREE + st));
                         }
                         __syncwarp();
@@ -388,7 +402,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
             if (lane == 0 && t > 0) {
                 const int done = warp == kScores ? L::B_S_FULL : L::B_PV_DONE, free = warp == kScores ? L::B_K_FREE : L::B_V_FREE;
                 const int ring = warp == kScores ? NSK : NSV;
-                mbar_wait_own<1>(bar(done), (t - 1) & 1);
+                for (int i = max(0, t - NS); i < t; ++i) mbar_wait_own<1>(bar(done + i % NS), (i / NS) & 1);
                 for (int i = max(0, t - ring); i < t; ++i) mbar_wait_own<1>(bar(free + i % ring), (i / ring) & 1);
                 if (warp == kScores && nq > 0) mbar_wait_own<1>(bar(L::B_Q_FREE), (nq - 1) & 1);
             }
@@ -399,8 +413,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
         const int tok = r / a.block, head = r - tok * a.block;
         const int tok_first = warp * 32 / a.block, tok_last = (warp * 32 + 31) / a.block;  // of the warp
         const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
-        const uint32_t t_s = tmem + lane_off, t_p = tmem + L::T_P + lane_off, t_o = tmem + L::T_O + lane_off;
-        unsigned char *const stage = smem + L::OFF_OUT + warp * (L::BLK / kGroupWarps);
+        const uint32_t t_o = tmem + L::T_O + lane_off;
         int t = 0;           // tiles
         bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
         bool left = false;   // rows of this warp came out not finite
@@ -414,14 +427,16 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
             const bool valid = tok < x.tokens && head < x.heads;
             const bool idle = !__any_sync(0xFFFFFFFFu, valid);
             const int pos0 = x.pos0, pos = pos0 + tok, end = x.end;
-            int k0 = x.key(0), jump = x.sinks - x.j0;  // tiles up to the window's
+            int k0 = x.key(0);
+            const int jump = x.sinks - x.j0, after_jump = BN * x.first;  // tiles up to the window's, where those begin
             // row sum, reference, largest score; by how much the largest score's weight is rounded up: the outputs
             // are divided by the sum with that weight as rounded, so that a row whose weight goes to one key is that key's values
             float l = 0.f, m = -INFINITY, top = -INFINITY, up = 0.f;
-            for (int j = 0; j < n; ++j, ++t, k0 = j == jump ? BN * x.first : k0 + BN) {
+            for (int j = 0; j < n; ++j, ++t, k0 = j == jump ? after_jump : k0 + BN) {
                 // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
-                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL, t & 1);
+                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL + t % NS, (t / NS) & 1);
                 tc_fence_after();
+                const uint32_t t_s = tmem + lane_off + t % NS * BN, t_p = t_s + L::T_P;
                 if (idle) {
                     there = false;
                     if (!L::OVER) mbar_arrive_if(lane == 0, bar(L::B_S_GO));
@@ -444,13 +459,13 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
 #pragma unroll
                     for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
                     if (k0 + BN - 1 > pos0 + tok_first || (a.window != 0 && pos0 + tok_last - k0 >= a.window && a.anchors < k0 + BN)) {
-                        uint32_t cw[4];
+                        uint32_t cw[BN / 32];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
+                        for (int e = 0; e < BN / 32; ++e)
                             cw[e] = causal_word(pos - k0, e) &
                                     (a.window == 0 ? 0xFFFFFFFFu : ~causal_word(pos - a.window - k0, e) | causal_word(a.anchors - 1 - k0, e));
 #pragma unroll
-                        for (int w = 0; w < 4; ++w) {
+                        for (int w = 0; w < BN / 32; ++w) {
                             // (an end of what the rows see lies in one or two of a warp's words)
                             if (__all_sync(0xFFFFFFFFu, cw[w] == 0xFFFFFFFFu)) continue;
 #pragma unroll
@@ -466,21 +481,20 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                     m = upd ? mx : m;
                     const float mu = m == -INFINITY ? 0.f : m;
                     uint32_t hw[BN / 2];
-                    float sum = weights_of<0, 96>(sv, a.scale_log2, mu, hw);
+                    float sum = weights_of<0, BN * 3 / 4>(sv, a.scale_log2, mu, hw);
                     // polled here, the answers are there when the weights are
                     bool settled = true;
-                    if (!L::OVER) {
-                        settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
-                        there = mbar_test<1>(bar(L::B_S_FULL), (t + 1) & 1);
-                    }
-                    l += sum + weights_of<96, BN>(sv, a.scale_log2, mu, hw);
+                    if (!L::OVER) settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
+                    if (!L::OVER || NS > 1) there = mbar_test<1>(bar(L::B_S_FULL + (t + 1) % NS), ((t + 1) / NS) & 1);
+                    l += sum + weights_of<BN * 3 / 4, BN>(sv, a.scale_log2, mu, hw);
                     const float w = ex2(fmaf(raw, a.scale_log2, -mu));
                     up = mx > top ? __bfloat162float(__float2bfloat16_rn(w)) - w : up * al;
                     top = fmaxf(top, mx);
-                    // P's buffer is free and O has settled once the last value product is done (where P takes
-                    // the scores' place, the scores were computed after that; a unit's first tile: waited for
-                    // at the end of the last unit)
-                    if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+                    // P's buffer is free and O has settled once the last value product is done (where P takes its own
+                    // scores' place, only a change of O waits for that; a unit's first tile: waited for at the end
+                    // of the last unit)
+                    if (L::OVER) settled = !any_scale || j == 0;
+                    if (!__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE + (t - 1) % NS, ((t - 1) / NS) & 1);
                     tc_fence_after();
                     if (any_scale) {
 #pragma unroll 1
@@ -509,9 +523,9 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                 }
                 tc_fence_before();
                 __syncwarp();
-                mbar_arrive_if(lane == 0, bar(L::B_P_GO));
+                mbar_arrive_if(lane == 0, bar(L::B_P_GO + t % NS));
             }
-            if (ok && n > 0) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
+            if (ok && n > 0) ok = wait_all(L::B_PV_DONE + (t - 1) % NS, ((t - 1) / NS) & 1);
             if (!ok) break;
             const int part = x.part, head0 = x.head0, row0 = x.row0;
             __syncwarp();
@@ -520,38 +534,36 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, 2) k_paged_tiles(const __grid
                 tc_fence_before();
                 continue;
             }
-            // rows of OC columns by way of shared memory, so that neighbouring lanes store neighbouring pieces of a row
-            auto emit = [&](auto *base, float scale, int64_t mine) {
-                using TOut = std::remove_pointer_t<decltype(base)>;
-                constexpr int OC = 128 / (int)sizeof(TOut);
+            // a thread's row; rows with no weight (scale 0) become zeros whatever the columns hold
+            auto emit = [&](auto *to, float scale) {
+                using TOut = std::remove_pointer_t<decltype(to)>;
+                constexpr int E = 16 / (int)sizeof(TOut);
+                float found = 0.f;  // NaN where a value is not finite
 #pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += OC) {
-                    __syncwarp();
-                    if (n > 0) {
-                        const float found = stage_out<OC, TOut, true>(stage, t_o + c0, scale);
-                        left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
-                    } else {  // rows without a key: zeros
-                        for (int e = lane; e < 256; e += 32) reinterpret_cast<uint4 *>(stage)[e] = make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    __syncwarp();
+                for (int c0 = 0; c0 < D; c0 += 32) {
+                    float x[32];
+                    tmem_ld32(t_o + c0, x);  // (of no use where there is no tile)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int rr = 4 * e + (lane >> 3), piece = lane & 7;
-                        const int64_t to = __shfl_sync(0xFFFFFFFFu, mine, rr);
-                        const uint4 y = *reinterpret_cast<const uint4 *>(stage + rr * 128 + ((piece ^ (rr & 7)) << 4));
-                        if (to >= 0) *reinterpret_cast<uint4 *>(base + to + c0 + piece * (16 / (int)sizeof(TOut))) = y;
+                    for (int e = 0; e < 32; ++e) {
+                        x[e] = scale == 0.f ? 0.f : x[e] * scale;
+                        found = fmaf(x[e], 0.f, found);
+                    }
+                    if (valid) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += E) store16<TOut>(to + c0 + e, x + e);
                     }
                 }
+                left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
             };
             const float by = l + up, far = fabsf(m) > kFarLog2 && fabsf(m) < INFINITY ? NAN : 1.f;
             if (part < 0) {
                 const int64_t row = row0 + tok;
                 if (valid && a.lse != nullptr) a.lse[(head0 + head) * a.q_total + row] = (m + log2f(l)) * kLn2;
-                emit(reinterpret_cast<__nv_bfloat16 *>(a.out), l == 0.f ? 0.f : far / by, valid ? (row * a.Hq + head0 + head) * D : -1);
+                emit(reinterpret_cast<__nv_bfloat16 *>(a.out) + (row * a.Hq + head0 + head) * D, l == 0.f ? 0.f : far / by);
             } else {
                 const int64_t at = (int64_t)part * a.part_rows + r;
                 if (valid) a.part_ml[at] = make_float4(m, l, by, 0.f);
-                emit(a.part_o, l == 0.f ? 0.f : far, valid ? at * D : -1);
+                emit(a.part_o + at * D, l == 0.f ? 0.f : far);
             }
             tc_fence_before();  // (O has been read before the next P is announced)
         }
@@ -605,7 +617,7 @@ cudaError_t launch(const PagedAttendArgs &a, const Maps &maps, cudaStream_t s)
         return e != cudaSuccess ? e : (fa.numRegs + 7) / 8 * 8 < L::REGS ? cudaErrorInvalidConfiguration : cudaSuccess;
     });
     if (ready != cudaSuccess) return ready;
-    return launch_chained(k_paged_tiles<D>, dim3((unsigned)a.ctas), dim3(L::THREADS), L::BYTES, s, a, maps);
+    return launch_chained(k_paged_tiles<D>, dim3((unsigned)a.runs), dim3(L::THREADS), L::BYTES, s, a, maps);
 }
 
 }  // namespace

@@ -3,7 +3,9 @@
 // A row tile is a sequence's next `tokens` new tokens x a block of the query heads of a KV head (row r is
 // token r / block, head r % block), so that a token's heads share every key they read. It sees the keys
 // from the first that its first row sees up to its last row's own, and the first `anchors`; in tiles of BN
-// keys these are n of them, and the row tile costs n + 1. The row tiles of all sequences, heads innermost,
+// keys these are n of them, and the row tile costs n + 4, in fp32 n + 1: beginning and ending it takes as long as so
+// many tiles (bf16 at n + 1: the CTAs that have the short row tiles came last, 714 us instead of 635 for 16,384 rows at 12 / 2
+// heads of 128; fp32 at n + 4: 186 instead of 156 for 900). The row tiles of all sequences, heads innermost,
 // laid one after another make a line of that length, which is cut into as many equal runs as there are
 // CTAs: one row against 60,000 keys and 8,000 rows against 30,000 are spread over the SMs alike, whatever
 // the lengths, which only the device knows. A row tile that lies in one run is finished there; of the
@@ -17,6 +19,9 @@
 
 namespace ris {
 namespace paged {
+
+template <int BN>
+constexpr int kUnitCost = BN == kPagedTileKeys ? kPagedTileUnitCost : kPagedF32UnitCost;
 
 // 0 <= length <= reach
 __device__ __forceinline__ int length_of(const PagedAttendArgs &a, int seq) { return min(max(a.c.length[seq], 0), a.reach); }
@@ -54,7 +59,7 @@ template <int BN>
 __device__ __forceinline__ int seq_cost(const PagedAttendArgs &a, int seq)
 {
     const int rows = a.off[seq + 1] - a.off[seq];
-    return rows > 0 ? sight_of<BN>(a, length_of(a, seq), rows, 0).n + 1 : 0;
+    return rows > 0 ? sight_of<BN>(a, length_of(a, seq), rows, 0).n + kUnitCost<BN> : 0;
 }
 
 __device__ __forceinline__ int64_t warp_scan(int64_t x)
@@ -107,7 +112,7 @@ __device__ __forceinline__ Run run_of(const PagedAttendArgs &a, int cta, RunMem 
     const int units = a.c.Hkv * a.blocks;  // row tiles of an item
     auto use = [&](int64_t cost) {
         r.total = cost * units;
-        r.runs = (int)min((int64_t)a.ctas, max((int64_t)1, r.total / a.least));
+        r.runs = (int)min((int64_t)a.runs, max((int64_t)1, r.total / a.least));
         if (cta < r.runs && r.total > 0) r.v0 = r.begin(cta), r.v1 = r.begin(cta + 1);
     };
     if (a.max_items > 0) {
@@ -178,7 +183,7 @@ struct Walk {
                     continue;
                 }
                 sight = sight_of<BN>(a, length_of(a, it.seq), rows, it.tile);
-                cost = sight.n + 1;
+                cost = sight.n + kUnitCost<BN>;
                 seq = it.seq;
                 row0 = off + it.tile * a.tokens;
                 unit = 0;
@@ -195,7 +200,7 @@ struct Walk {
             x.seq = seq;
             x.row0 = row0;
             if (last_of_item) cost = 0, ++item;
-            if (n > 0 && j0 >= j1) continue;
+            if (n > 0 ? j0 >= j1 : j0 > 0) continue;
             x.j0 = j0;
             x.j1 = max(j0, j1);
             x.kv_head = u / a.blocks;

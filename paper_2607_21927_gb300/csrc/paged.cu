@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
             }
             const PagedItem it{lo, i - a.seq_items[lo]};
             a.items[i] = it;
-            cost = sight_of<KEYS>(a, length_of(a, lo), a.off[lo + 1] - a.off[lo], it.tile).n + 1;
+            cost = sight_of<KEYS>(a, length_of(a, lo), a.off[lo + 1] - a.off[lo], it.tile).n + kUnitCost<KEYS>;
         }
         const int64_t at = before + block_scan<kPlanThreads>(cost, mem, all);
         if (i < n) a.prefix[i] = at;
@@ -436,15 +436,15 @@ cudaError_t launch_f32(const PagedAttendArgs &a, cudaStream_t s)
     static Once once;
     const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_paged_f32<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
     if (ready != cudaSuccess) return ready;
-    return launch_chained(k_paged_f32<D, R>, dim3((unsigned)a.ctas), dim3(kF32Threads), bytes, s, a);
+    return launch_chained(k_paged_f32<D, R>, dim3((unsigned)a.runs), dim3(kF32Threads), bytes, s, a);
 }
 
 template <typename T, int D>
 cudaError_t launch_join(const PagedAttendArgs &a, cudaStream_t s)
 {
     // few rows: every warp of a CTA on the parts of one row, else a row for each
-    if (a.part_rows <= 32) return launch_chained(k_paged_join<T, D, kJoinWarps>, dim3((unsigned)a.ctas, (unsigned)a.part_rows), dim3(kJoinThreads), 0, s, a);
-    return launch_chained(k_paged_join<T, D, 1>, dim3((unsigned)a.ctas, (unsigned)((a.part_rows + kJoinWarps - 1) / kJoinWarps)), dim3(kJoinThreads), 0, s, a);
+    if (a.part_rows <= 32) return launch_chained(k_paged_join<T, D, kJoinWarps>, dim3((unsigned)a.runs, (unsigned)a.part_rows), dim3(kJoinThreads), 0, s, a);
+    return launch_chained(k_paged_join<T, D, 1>, dim3((unsigned)a.runs, (unsigned)((a.part_rows + kJoinWarps - 1) / kJoinWarps)), dim3(kJoinThreads), 0, s, a);
 }
 
 }  // namespace
@@ -455,7 +455,7 @@ cudaError_t launch_paged_append(PagedAppendArgs a, int dtype, cudaStream_t s)
     constexpr int64_t full = kAppendThreads * kAppendPieces;  // of a CTA
     // one CTA where it can take everything, else full ones, or two on every SM
     const int64_t most = std::max<int64_t>(1, full / pieces);
-    a.rows = (int)(a.total * pieces <= full ? a.total : std::min<int64_t>(most, std::max<int64_t>(1, a.total / kPagedCtas)));
+    a.rows = (int)(a.total * pieces <= full ? a.total : std::min<int64_t>(most, std::max<int64_t>(1, a.total / 2 * kPagedSMs)));
     int64_t blocks = 0;
     if (a.total > 0) {
         blocks = (a.total + a.rows - 1) / a.rows;

@@ -43,14 +43,15 @@ __device__ __forceinline__ void drop_unless(float &x, uint32_t word, uint32_t bi
         : "+f"(x)
         : "r"(word), "r"(bit));
 }
-__device__ __forceinline__ float row_max(const float (&sv)[kTileKeys])
+template <int BN>
+__device__ __forceinline__ float row_max(const float (&sv)[BN])
 {
     float mx8[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         mx8[e] = fmaxf(sv[e], sv[e + 8]);
 #pragma unroll
-        for (int c = 16; c < kTileKeys; c += 16) mx8[e] = fmax3(mx8[e], sv[c + e], sv[c + 8 + e]);
+        for (int c = 16; c < BN; c += 16) mx8[e] = fmax3(mx8[e], sv[c + e], sv[c + 8 + e]);
     }
     return fmax3(fmax3(mx8[0], mx8[1], mx8[2]), fmax3(mx8[3], mx8[4], mx8[5]), fmaxf(mx8[6], mx8[7]));
 }

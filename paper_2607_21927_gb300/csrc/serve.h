@@ -127,7 +127,7 @@ struct PagedAppendArgs {
 };
 cudaError_t launch_paged_append(PagedAppendArgs a, int dtype, cudaStream_t s);
 
-// A row tile's part that a CTA leaves for the join: parts of CTAs first .. last, -1: none.
+// A row tile's part that a run leaves for the join: parts of runs first .. last, -1: none.
 struct PagedSplit {
     int32_t first, last;
     int32_t row0, tokens;      // its first row in q / out, its tokens
@@ -151,21 +151,24 @@ struct PagedAttendArgs {
     int32_t reach;             // lengths count up to here
     float scale_log2;
     // the sharing out of the work (attn_paged.cuh)
-    int32_t ctas, least;       // CTAs; key tiles of one at least
+    int32_t runs, least;       // runs of the line, one for each CTA; key tiles of one at least
     int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
     int64_t *prefix;           // [max_items + 1] scratch: cost of the items before
     PagedItem *items;          // [max_items]
     int32_t *n_items;          // [1]
     int32_t *seq_items;        // [B] first item of each sequence
-    PagedSplit *split;         // [ctas]
+    PagedSplit *split;         // [runs]
     int32_t part_rows;         // rows of a part
-    float *part_o;             // [2 ctas][part_rows][D]
-    float4 *part_ml;           // [2 ctas][part_rows] (reference in log2, sum, what the outputs are divided by)
+    float *part_o;             // [2 runs][part_rows][D]
+    float4 *part_ml;           // [2 runs][part_rows] (reference in log2, sum, what the outputs are divided by)
 };
-constexpr int kPagedCtas = 2 * 152;
+constexpr int kPagedSMs = 152;
 // keys of a key tile and rows of a row tile, fp32 (by the most rows that a sequence has) and bf16
 constexpr int kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128;
 int32_t paged_f32_rows(int64_t rows);
+// what a row tile costs besides its key tiles
+constexpr int kPagedF32UnitCost = 1, kPagedTileUnitCost = 4;
+constexpr int paged_tile_ctas(int D) { return D == 128 ? 1 : 2; }
 cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_f32(const PagedAttendArgs &a, int32_t rows, cudaStream_t s);

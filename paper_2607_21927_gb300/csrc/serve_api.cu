@@ -845,15 +845,17 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.blocks = (a.G + a.block - 1) / a.block;
     a.tokens = tile_rows / a.block;
     a.part_rows = (int32_t)std::min<int64_t>(a.tokens, pack->q_longest) * a.block;
+    const int32_t keys = tiles ? kPagedTileKeys : kPagedF32Keys;  // of a tile
+    const int32_t places = kPagedSMs * (tiles ? paged_tile_ctas(cache->head_dim) : 2);  // of CTAs
     const int64_t items = pack->q_longest <= a.tokens ? pack->n_seqs : pack->q_total / a.tokens + pack->n_seqs;
     if (pack->q_longest > a.tokens) a.max_items = (int32_t)items;
     // no more CTAs than the longest line there can be has key tiles
-    const int64_t most = a.reach / (tiles ? kPagedTileKeys : kPagedF32Keys) + 3, line = items * cache->kv_heads * a.blocks;
-    a.ctas = (int32_t)std::min<int64_t>(kPagedCtas, line > kPagedCtas ? line : line * most);
+    const int64_t most = a.reach / keys + 2 + (tiles ? kPagedTileUnitCost : kPagedF32UnitCost), line = items * cache->kv_heads * a.blocks;
+    a.runs = (int32_t)std::min<int64_t>(places, line > places ? line : line * most);
     const bool plan = a.max_items > 0;
     const size_t prefix_b = plan ? room(sizeof(int64_t) * (items + 1)) : 0, item_b = plan ? room(sizeof(PagedItem) * items) : 0,
-                 seq_b = plan ? room(sizeof(int32_t) * (pack->n_seqs + 1)) : 0, split_b = room(sizeof(PagedSplit) * a.ctas),
-                 ml_b = room(sizeof(float4) * 2 * a.ctas * a.part_rows), o_b = room(sizeof(float) * 2 * a.ctas * a.part_rows * cache->head_dim);
+                 seq_b = plan ? room(sizeof(int32_t) * (pack->n_seqs + 1)) : 0, split_b = room(sizeof(PagedSplit) * a.runs),
+                 ml_b = room(sizeof(float4) * 2 * a.runs * a.part_rows), o_b = room(sizeof(float) * 2 * a.runs * a.part_rows * cache->head_dim);
     cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
     const PackUse use{pack, s};
     Scratch mem;
@@ -867,7 +869,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.part_o = reinterpret_cast<float *>(d);
     if (plan) RIS_CUDA(launch_paged_plan(a, cache->dtype, s));
     RIS_CUDA(tiles ? launch_paged_tiles(a, s) : launch_paged_f32(a, tile_rows, s));
-    if (a.ctas > 1) RIS_CUDA(launch_paged_join(a, cache->dtype, s));
+    if (a.runs > 1) RIS_CUDA(launch_paged_join(a, cache->dtype, s));
     return RIS_OK;
 }
 

@@ -124,6 +124,10 @@ ATTEND = [
     ([130, 0, 1], [300, 4, 70], 12, 2, 128, 16, 0, 0, F32, "tokens"),
     ([130, 9, 1], [300, 4, 700], 32, 4, 64, 64, 100, 5, F32, "joint"),
     ([6], [90], 70, 1, 64, 16, 0, 0, F32, "heads"),
+    ([4, 5], [300, 40], 12, 2, 128, 32, 64, 4, F32, "joint"),
+    ([1, 1], [900, 131], 8, 1, 128, 16, 200, 20, F32, "tokens"),
+    ([700], [0], 12, 2, 128, 16, 0, 0, BF16, "heads"),      # CTAs with many short row tiles
+    ([900], [50], 4, 4, 64, 32, 100, 10, BF16, "tokens"),
     ([1] * 40, [37 * i % 900 for i in range(40)], 8, 8, 64, 32, 0, 0, F32, "heads"),
 ]
 
