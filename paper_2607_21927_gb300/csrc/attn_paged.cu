@@ -49,7 +49,7 @@ namespace {
 using namespace tc;
 using namespace paged;
 
-constexpr int BM = kTileRows, BN = kTileKeys;
+constexpr int BM = kTileRows, BN = kTileKeys, GR = kPagedGranule;
 static_assert(kPagedTileRows == BM && kPagedTileKeys == BN, "as the work is shared out");
 constexpr int kGroupWarps = 4;  // of the softmax group: one thread per row
 // The reference m of a row moves only when its largest score grows by more than this: P stays below 2^7.
@@ -99,10 +99,15 @@ struct Lay {
 // What the roles need to know of a unit.
 struct Info {
     int n;              // key tiles of this part, -1: no more units
-    int j0, sinks, first;  // the first of them; which keys a tile holds (Sight)
+    int j0, sinks, first;  // the first of them; which keys the granules hold (Sight)
     int pos0, tokens, low, end;
     int head0, heads, kv_head, seq, row0, part;
-    __device__ __forceinline__ int key(int j) const { return BN * (j0 + j < sinks ? j0 + j : first + j0 + j - sinks); }
+    // the key of a column of the part's tile j
+    __device__ __forceinline__ int key(int j, int col) const
+    {
+        const int g = BN / GR * (j0 + j) + col / GR;
+        return GR * (g < sinks ? g : first + g - sinks) + col % GR;
+    }
 };
 static_assert(sizeof(Info) <= 64, "the ring's slots");
 
@@ -127,12 +132,11 @@ __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, flo
     return a + b;
 }
 
-// Where box `box` of the tile from key k0 on lies: its page, or n_pages (past the pool's end) for one that no row
-// sees or whose entry is no page.
-__device__ __forceinline__ int box_page(const PagedAttendArgs &a, const Info &x, int k0, int box, int box_rows)
+// Where the box from key j on lies: its page, or n_pages (past the pool's end) for one that no row sees or whose entry is
+// no page.
+__device__ __forceinline__ int box_page(const PagedAttendArgs &a, const Info &x, int j)
 {
-    const int j = k0 + box * box_rows;
-    if (j >= x.end || (j + box_rows <= x.low && j >= a.anchors)) return a.c.n_pages;
+    if (j >= x.end || (j + a.box_rows <= x.low && j >= a.anchors)) return a.c.n_pages;
     const int p = page_of(a.c, x.seq, j);
     if (p < 0) atomicOr(&g_ris_paged_page, 1u);
     return p < 0 ? a.c.n_pages : p;
@@ -149,8 +153,8 @@ __device__ __noinline__ void row_as_given(const PagedAttendArgs &a, const Unit &
     const __nv_bfloat16 *q = reinterpret_cast<const __nv_bfloat16 *>(a.q) + row * a.q_stride + (int64_t)h * D;
     float m = -INFINITY, l = 0.f, o[C] = {};
     for (int j = u.j0; j < u.j1; ++j)
-        for (int k0 = BN * u.sight.tile(j), e0 = 0; e0 < BN; e0 += 32) {
-            const int key = k0 + e0 + lane;
+        for (int e = 0; e < BN / 32; ++e) {
+            const int key = GR * u.sight.granule(BN / GR * j + e) + lane;
             const int page = sees(a, pos, key) ? page_of(a.c, u.seq, key) : -1;
             const int64_t at = page >= 0 ? slot_at(a.c, page, u.kv_head, key) : -1;
             float s = -INFINITY;
@@ -267,8 +271,8 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
 
     if (warp >= kGroupWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
-        const int box_rows = min(BN, 1 << a.c.page_log2), boxes = BN / box_rows;  // of a tile and 64-column block
-        const int box = lane % boxes, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;
+        const int boxes = BN / a.box_rows;  // of a tile and 64-column block
+        const int col = lane % boxes * a.box_rows, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;
         if (warp == kLoadQK) {
             const uint32_t q_bytes = (uint32_t)(a.block * a.tokens * 128 * NB);
             int nq = 0, nk = 0;  // query and key tiles asked for
@@ -292,15 +296,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 const Info &x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
                 const int n = x.n;
                 for (int j = 0; j < n; ++j, ++nk) {
-                    const int st = nk % NSK, k0 = x.key(j);
-                    const int page = blk < NB ? box_page(a, x, k0, box, box_rows) : 0;
+                    const int st = nk % NSK, key = x.key(j, col);
+                    const int page = blk < NB ? box_page(a, x, key) : 0;
                     if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up));
                     if (!ok) break;
                     if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + st), TILE);
                     __syncwarp();
                     if (blk < NB)
-                        tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + box * box_rows * 128, &maps.k, 64 * blk, (k0 + box * box_rows) & in_page,
-                                    x.kv_head, page, bar(L::B_K_FULL + st));
+                        tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + col * 128, &maps.k, 64 * blk, key & in_page, x.kv_head, page,
+                                    bar(L::B_K_FULL + st));
                     if (j > 0) continue;
                     if (nq > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up));
                     if (!ok) {
@@ -328,15 +332,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 ok = unit(u, x);
                 if (!ok || x.n < 0) break;
                 for (int j = 0; j < x.n; ++j, ++nv) {
-                    const int st = nv % NSV, k0 = x.key(j);
-                    const int page = blk < NB ? box_page(a, x, k0, box, box_rows) : 0;
+                    const int st = nv % NSV, key = x.key(j, col);
+                    const int page = blk < NB ? box_page(a, x, key) : 0;
                     if (nv >= NSV) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up));
                     if (!ok) break;
                     if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + st), TILE);
                     __syncwarp();
                     if (blk < NB)
-                        tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + box * box_rows * 128, &maps.v, 64 * blk, (k0 + box * box_rows) & in_page,
-                                    x.kv_head, page, bar(L::B_V_FULL + st));
+                        tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + col * 128, &maps.v, 64 * blk, key & in_page, x.kv_head, page,
+                                    bar(L::B_V_FULL + st));
                 }
             }
             if (lane == 0)
@@ -427,12 +431,13 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
             const bool valid = tok < x.tokens && head < x.heads;
             const bool idle = !__any_sync(0xFFFFFFFFu, valid);
             const int pos0 = x.pos0, pos = pos0 + tok, end = x.end;
-            int k0 = x.key(0);
-            const int jump = x.sinks - x.j0, after_jump = BN * x.first;  // tiles up to the window's, where those begin
+            // A tile's keys follow one another from k0 on, but for granules of the anchors, which the first `mixed` have.
+            int k0 = GR * (x.first - x.sinks) + BN * x.j0;
+            const int mixed = (x.sinks + BN / GR - 1) / (BN / GR) - x.j0;
             // row sum, reference, largest score; by how much the largest score's weight is rounded up: the outputs
             // are divided by the sum with that weight as rounded, so that a row whose weight goes to one key is that key's values
             float l = 0.f, m = -INFINITY, top = -INFINITY, up = 0.f;
-            for (int j = 0; j < n; ++j, ++t, k0 = j == jump ? after_jump : k0 + BN) {
+            for (int j = 0; j < n; ++j, ++t, k0 += BN) {
                 // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
                 if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL + t % NS, (t / NS) & 1);
                 tc_fence_after();
@@ -458,12 +463,14 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     float sv[BN];
 #pragma unroll
                     for (int e = 0; e < BN; ++e) sv[e] = __uint_as_float(su[e >> 6][e & 63]);
-                    if (k0 + BN - 1 > pos0 + tok_first || (a.window != 0 && pos0 + tok_last - k0 >= a.window && a.anchors < k0 + BN)) {
+                    if (j < mixed || k0 + BN - 1 > pos0 + tok_first || (a.window != 0 && pos0 + tok_last - k0 >= a.window)) {
                         uint32_t cw[BN / 32];
 #pragma unroll
-                        for (int e = 0; e < BN / 32; ++e)
-                            cw[e] = causal_word(pos - k0, e) &
-                                    (a.window == 0 ? 0xFFFFFFFFu : ~causal_word(pos - a.window - k0, e) | causal_word(a.anchors - 1 - k0, e));
+                        for (int e = 0; e < BN / 32; ++e) {
+                            const int k = j < mixed ? x.key(j, 32 * e) : k0 + 32 * e;
+                            cw[e] = causal_word(pos - k, 0) &
+                                    (a.window == 0 ? 0xFFFFFFFFu : ~causal_word(pos - a.window - k, 0) | causal_word(a.anchors - 1 - k, 0));
+                        }
 #pragma unroll
                         for (int w = 0; w < BN / 32; ++w) {
                             // (an end of what the rows see lies in one or two of a warp's words)
@@ -511,9 +518,9 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     tmem_st32(t_p + 32, hw + 32);
                     tmem_wait_st();
                 }
-                if (k0 + BN > end) {  // (a thread takes a key)
+                if (j < mixed || k0 + BN > end) {  // (a thread takes a key)
                     if (ok) ok = wait_all(L::B_V_FULL + t % NSV, (t / NSV) & 1);
-                    if (ok && k0 + r >= end) {
+                    if (ok && (j < mixed ? x.key(j, r) : k0 + r) >= end) {
                         unsigned char *const row = smem + L::OFF_V + t % NSV * TILE + r * 128;
 #pragma unroll
                         for (int e = 0; e < 8 * NB; ++e)
@@ -600,7 +607,7 @@ bool pool_map(CUtensorMap *m, const PagedAttendArgs &a, const void *pool)
 {
     const cuuint64_t dims[4] = {(cuuint64_t)a.c.D, (cuuint64_t)1 << a.c.page_log2, (cuuint64_t)a.c.Hkv, (cuuint64_t)a.c.n_pages},
                      strides[3] = {(cuuint64_t)a.c.slot_stride * 2, (cuuint64_t)a.c.head_stride * 2, (cuuint64_t)a.c.page_stride * 2};
-    const cuuint32_t box[4] = {64, (cuuint32_t)std::min(BN, 1 << a.c.page_log2), 1, 1};
+    const cuuint32_t box[4] = {64, (cuuint32_t)a.box_rows, 1, 1};
     return encode(m, pool, 4, dims, strides, box);
 }
 
@@ -622,8 +629,9 @@ cudaError_t launch(const PagedAttendArgs &a, const Maps &maps, cudaStream_t s)
 
 }  // namespace
 
-cudaError_t launch_paged_tiles(const PagedAttendArgs &a, cudaStream_t s)
+cudaError_t launch_paged_tiles(PagedAttendArgs a, cudaStream_t s)
 {
+    a.box_rows = std::min(a.window == 0 ? BN : GR, 1 << a.c.page_log2);
     alignas(64) Maps maps;
     if (!query_map(&maps.q, a) || !pool_map(&maps.k, a, a.c.k) || !pool_map(&maps.v, a, a.c.v)) return cudaErrorInvalidValue;
     return a.c.D == 128 ? launch<128>(a, maps, s) : launch<64>(a, maps, s);

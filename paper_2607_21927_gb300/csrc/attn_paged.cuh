@@ -2,8 +2,8 @@
 //
 // A row tile is a sequence's next `tokens` new tokens x a block of the query heads of a KV head (row r is
 // token r / block, head r % block), so that a token's heads share every key they read. It sees the keys
-// from the first that its first row sees up to its last row's own, and the first `anchors`; in tiles of BN
-// keys these are n of them, and the row tile costs n + 4, in fp32 n + 1: beginning and ending it takes as long as so
+// from the first that its first row sees up to its last row's own, and the first `anchors`: a list of granules
+// (32 keys; in fp32 a tile), those of the anchors first, cut into n tiles of BN keys, and the row tile costs n + 4, in fp32 n + 1: beginning and ending it takes as long as so
 // many tiles (bf16 at n + 1: the CTAs that have the short row tiles came last, 714 us instead of 635 for 16,384 rows at 12 / 2
 // heads of 128; fp32 at n + 4: 186 instead of 156 for 900). The row tiles of all sequences, heads innermost,
 // laid one after another make a line of that length, which is cut into as many equal runs as there are
@@ -26,13 +26,15 @@ constexpr int kUnitCost = BN == kPagedTileKeys ? kPagedTileUnitCost : kPagedF32U
 // 0 <= length <= reach
 __device__ __forceinline__ int length_of(const PagedAttendArgs &a, int seq) { return min(max(a.c.length[seq], 0), a.reach); }
 
-// What a row tile sees, of BN-key tiles: `sinks` from key 0 on, then those from tile `first` up to key `end`.
+// What a row tile sees, in granules: `sinks` from key 0 on, then those from granule `first` up to key `end`; n tiles.
+template <int BN>
+constexpr int kGranule = BN == kPagedTileKeys ? kPagedGranule : BN;
 struct Sight {
     int pos0;   // position of its first row (negative: it is before the sequence's first slot)
     int tokens;
     int low, end;  // keys [low, end) and [0, anchors) are seen by some row
     int sinks, first, n;
-    __device__ __forceinline__ int tile(int j) const { return j < sinks ? j : first + j - sinks; }
+    __device__ __forceinline__ int granule(int g) const { return g < sinks ? g : first + g - sinks; }
 };
 template <int BN>
 __device__ __forceinline__ Sight sight_of(const PagedAttendArgs &a, int length, int rows, int tile)
@@ -43,9 +45,10 @@ __device__ __forceinline__ Sight sight_of(const PagedAttendArgs &a, int length, 
     s.pos0 = length - rows + t0;
     s.end = max(0, s.pos0 + s.tokens);
     s.low = a.window == 0 ? 0 : max(0, max(s.pos0, 0) - (a.window - 1));
-    s.first = s.low / BN;
-    s.sinks = s.end > 0 ? min((min(a.anchors, s.end) + BN - 1) / BN, s.first) : 0;
-    s.n = s.end > 0 ? s.sinks + (s.end + BN - 1) / BN - s.first : 0;
+    constexpr int GR = kGranule<BN>, OF = BN / GR;  // of a tile
+    s.first = s.low / GR;
+    s.sinks = s.end > 0 ? min((min(a.anchors, s.end) + GR - 1) / GR, s.first) : 0;
+    s.n = s.end > 0 ? (s.sinks + (s.end + GR - 1) / GR - s.first + OF - 1) / OF : 0;
     return s;
 }
 // whether the row at `pos` sees key j

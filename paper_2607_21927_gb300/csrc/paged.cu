@@ -289,8 +289,8 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_paged_f32(const __grid_const
             copy16(qs + r * D + 4 * (d ^ (r & 7)), q, there);
         }
         if (u.j0 < u.j1) {
-            fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.tile(u.j0));
-            fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.tile(u.j0));
+            fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.granule(u.j0));
+            fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.granule(u.j0));
         }
         int pos[R];  // of each row; one that is not there sees nothing
 #pragma unroll
@@ -303,7 +303,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_paged_f32(const __grid_const
 #pragma unroll
         for (int i = 0; i < R; ++i) m[i] = -INFINITY, l[i] = 0.f;
         for (int t = u.j0; t < u.j1; ++t) {
-            const int k0 = BN * u.sight.tile(t);
+            const int k0 = BN * u.sight.granule(t);
             const bool more = t + 1 < u.j1;
             // whether every row sees the whole tile
             const bool whole = k0 + BN - 1 <= u.sight.pos0 && (k0 + BN <= a.anchors || a.window == 0 || u.sight.pos0 + u.sight.tokens - 1 - k0 < a.window);
@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_paged_f32(const __grid_const
             }
             __syncthreads();  // the keys' buffer is free
             if (more)
-                fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.tile(t + 1));
+                fetch_keys<D, true>(a, u, ks, a.c.k, BN * u.sight.granule(t + 1));
             else
                 copies_end();
 #pragma unroll
@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(kF32Threads, 2) k_paged_f32(const __grid_const
                 values(std::true_type{});
             __syncthreads();  // the values' buffer and P's are free
             if (more)
-                fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.tile(t + 1));
+                fetch_keys<D, false>(a, u, vs, a.c.v, BN * u.sight.granule(t + 1));
             else
                 copies_end();
         }

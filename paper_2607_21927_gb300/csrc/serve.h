@@ -150,6 +150,7 @@ struct PagedAttendArgs {
     int32_t window, anchors;   // window 0: all
     int32_t reach;             // lengths count up to here
     float scale_log2;
+    int32_t box_rows;          // tile kernel: keys of a TMA box
     // the sharing out of the work (attn_paged.cuh)
     int32_t runs, least;       // runs of the line, one for each CTA; key tiles of one at least
     int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
@@ -164,7 +165,7 @@ struct PagedAttendArgs {
 };
 constexpr int kPagedSMs = 152;
 // keys of a key tile and rows of a row tile, fp32 (by the most rows that a sequence has) and bf16
-constexpr int kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128;
+constexpr int kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128, kPagedGranule = 32;
 int32_t paged_f32_rows(int64_t rows);
 // what a row tile costs besides its key tiles
 constexpr int kPagedF32UnitCost = 1, kPagedTileUnitCost = 4;
@@ -172,7 +173,7 @@ constexpr int paged_tile_ctas(int D) { return D == 128 ? 1 : 2; }
 cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_f32(const PagedAttendArgs &a, int32_t rows, cudaStream_t s);
-cudaError_t launch_paged_tiles(const PagedAttendArgs &a, cudaStream_t s);
+cudaError_t launch_paged_tiles(PagedAttendArgs a, cudaStream_t s);
 
 struct Cache4Args {
     uint8_t *k, *v;              // [B][Hkv][cap][D / 2]
