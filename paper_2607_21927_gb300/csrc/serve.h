@@ -152,6 +152,7 @@ struct PagedAttendArgs {
     float scale_log2;
     int32_t box_rows;          // tile kernel: keys of a TMA box
     // the sharing out of the work (attn_paged.cuh)
+    int64_t line;              // row tiles of the line (at most)
     int32_t runs, least;       // runs of the line, one for each CTA; key tiles of one at least
     int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
     int64_t *prefix;           // [max_items + 1] scratch: cost of the items before

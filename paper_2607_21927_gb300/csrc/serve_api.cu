@@ -851,6 +851,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     if (pack->q_longest > a.tokens) a.max_items = (int32_t)items;
     // no more CTAs than the longest line there can be has key tiles
     const int64_t most = a.reach / keys + 2 + (tiles ? kPagedTileUnitCost : kPagedF32UnitCost), line = items * cache->kv_heads * a.blocks;
+    a.line = line;
     a.runs = (int32_t)std::min<int64_t>(places, line > places ? line : line * most);
     const bool plan = a.max_items > 0;
     const size_t prefix_b = plan ? room(sizeof(int64_t) * (items + 1)) : 0, item_b = plan ? room(sizeof(PagedItem) * items) : 0,
