@@ -844,8 +844,8 @@ def ris_cache4_evict(src: Cache4, dst: Cache4, budget: int, recent: int, kept: O
 def _like(out, x: torch.Tensor, name: str):
     """An output of x's shape [n, H, D] and type: (tensor, elements from token to token)."""
     if out is None:
-        n, H, D = x.shape
-        return x.new_empty((n, H, D)), H * D
+        # (dense, tokens first, heads side by side, as x is: the cheapest of torch's ways to allocate)
+        return torch.empty_like(x), x.shape[1] * x.shape[2]
     if out.dtype != x.dtype or out.shape != x.shape:
         raise ValueError(f"{name}: {x.dtype} {tuple(x.shape)}")
     return out, _heads(out, name)[3]
@@ -975,8 +975,11 @@ def ris_paged_attend(cache: PagedCache, pack: Pack, q: torch.Tensor, window: int
     if n != pack.q_total or D != cache.head_dim:
         raise ValueError(f"q is {tuple(q.shape)}, the pack has {pack.q_total} rows, the cache heads of {cache.head_dim}")
     assert q.dtype == cache.k.dtype, "q of the cache's type"
-    out = _out(out, (n, Hq, D), q.dtype, q.device)
-    assert out.dtype == q.dtype
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        out = _out(out, (n, Hq, D), q.dtype, q.device)
+        assert out.dtype == q.dtype
     lse = torch.empty((Hq, n), dtype=torch.float32, device=q.device) if return_lse else None
     st = lib().ris_paged_attend(cache._ref, pack.handle, q.data_ptr(), qs, Hq, window, anchors, longest, out.data_ptr(), _addr(lse),
                                 _raw_stream(stream, q))
