@@ -148,6 +148,21 @@ def test_attend(q_lens, prior, Hq, Hkv, D, page, window, anchors, dtype, layout)
     ris.ris_device_status()
 
 
+@pytest.mark.parametrize("dtype,D,page", [(BF16, 128, 16), (BF16, 64, 64), (F32, 64, 16)])
+def test_windows_and_anchors(dtype, D, page):
+    """Ends of windows and of the first tokens in all places of a granule and of a tile, apart, side by side and one over the other."""
+    q_lens, prior = [70, 1, 5], [330, 401, 3]
+    lengths = [n + p for n, p in zip(q_lens, prior)]
+    cache, keys, values = make(lengths, 1, D, page, dtype, seed=2)
+    q = randn(sum(q_lens), 3, D, seed=3, dtype=dtype)
+    with ris.ris_pack_create(q_lens) as pack:
+        for window in (1, 31, 33, 100, 128, 300):
+            for anchors in (0, 1, 32, 33, 129, 250, 10 ** 9):
+                out, lse = ris.ris_paged_attend(cache, pack, q, window, anchors, return_lse=True)
+                check(out, lse, plain(q, keys, values, q_lens, window, anchors), dtype)
+    ris.ris_device_status()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_sequences(dtype):
     """More sequences than a CTA has threads, with and without several row tiles, some without rows or keys."""
