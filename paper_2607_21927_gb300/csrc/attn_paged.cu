@@ -57,19 +57,31 @@ constexpr float kLazyLog2 = 7.f;
 // The exponent of a weight is rounded once, the reference behind it was rounded as a product: rows that pass
 // this (no model's do) are computed from the inputs as given, where both are rounded alike.
 constexpr float kFarLog2 = 0x1p28f;
+// Two groups: a row's reference is its largest score in the first tile where it sees a key, and stays. Weights may grow by 2^100
+// above it (bf16 and fp32 hold that); rows that pass this are computed from the inputs as given too.
+constexpr float kGrowthLog2 = 100.f;
+
+// What two softmax groups tell each other.
+struct Share {
+    float ref[kTileRows];                          // the rows' references
+    int done[2][kGroupWarps];                      // each warp's tiles whose references are settled
+    float4 sums[2][2][kTileRows];                  // [unit mod 2][group]: sum, its correction, largest score, reference
+    int left[kGroupWarps];
+};
 
 template <int D>
 struct Lay {
     static constexpr int CTAS = paged_tile_ctas(D);        // of an SM
     static constexpr int NB = D / 64;                      // 64-column blocks
-    // NS buffers of scores; a tile's weights take the place of its scores, or one place beside them
-    static constexpr int NS = D == 64 ? 1 : 2;
+    // NG softmax groups, which take the tiles of a part in turn; NS buffers of scores; a tile's weights take the place of its
+    // scores, or one place beside them
+    static constexpr int NG = D == 64 ? 1 : 2, NS = D == 64 ? 1 : 3;
     static constexpr bool OVER = D == 128;
     static constexpr int NSK = D == 64 ? 4 : 3, NSV = 2, NI = 4;
     static constexpr int BLK = 128 * 128, TILE = NB * BLK;  // 128 rows or keys of D 16-bit values
     static constexpr int OFF_K = 0, OFF_V = OFF_K + NSK * TILE, OFF_Q = OFF_V + NSV * TILE, OFF_BARS = OFF_Q + TILE,
                          OFF_INFO = OFF_BARS + 256, OFF_RUN = OFF_INFO + NI * 64,
-                         OFF_TMEM = OFF_RUN + (int)sizeof(RunMem), BYTES = OFF_TMEM + 16;
+                         OFF_TMEM = OFF_RUN + (int)sizeof(RunMem), OFF_SHARE = (OFF_TMEM + 4 + 15) / 16 * 16, BYTES = OFF_SHARE + (NG == 1 ? 0 : (int)sizeof(Share));
     // Barriers, of a ring stage:
     //   K_FULL, V_FULL, Q_FULL  its keys / values / the query tile have landed
     //   K_FREE, V_FREE, Q_FREE  the products that read it are done
@@ -80,20 +92,23 @@ struct Lay {
     //   S_FULL  the next are there
     //   P_GO    P is written (and O rescaled where needed)
     //   PV_DONE O has settled, P's buffer is free
+    // and, of two groups, one phase per unit with keys:
+    //   SUMS    every softmax warp has left its rows' sums for the other group
+    //   O_FREE  every softmax warp has read its part of O
     // No phase of a barrier is completed before everyone has seen the one before it: scores into a buffer wait for the value
     // product over its last weights, and these for every softmax warp.
     static constexpr int B_K_FULL = 0, B_V_FULL = B_K_FULL + NSK, B_Q_FULL = B_V_FULL + NSV, B_K_FREE = B_Q_FULL + 1,
                          B_V_FREE = B_K_FREE + NSK, B_Q_FREE = B_V_FREE + NSV, B_I_FULL = B_Q_FREE + 1, B_I_FREE = B_I_FULL + NI,
                          B_S_GO = B_I_FREE + NI, B_S_FULL = B_S_GO + 1, B_P_GO = B_S_FULL + NS, B_PV_DONE = B_P_GO + NS,
-                         NBAR = B_PV_DONE + NS;
+                         B_SUMS = B_PV_DONE + NS, B_O_FREE = B_SUMS + 1, NBAR = B_PV_DONE + NS + (NG == 1 ? 0 : 2);
     static_assert(8 * NBAR <= OFF_INFO - OFF_BARS && CTAS * (BYTES + 1024) <= 228 * 1024, "barriers; the CTAs of an SM");
     static constexpr uint32_t COLS = 512 / CTAS, T_P = OVER ? 0 : BN, T_O = NS * BN + (OVER ? 0 : BN / 2);  // TMEM; S at 0
     static_assert(T_O + D <= COLS, "TMEM columns");
     // Registers per thread: at launch, then after setmaxnreg of a softmax and of another thread. Shared memory leaves
     // next to no L1, so what a loader spills comes from L2: with 56 instead of 64 (head dim 128: 152) for them, single tokens
     // against long caches ran at 5.3 TB/s instead of 6.3.
-    static constexpr int THREADS = 256, REGS = CTAS == 2 ? 128 : 192, SOFTMAX_REGS = CTAS == 2 ? 192 : 232, OTHER_REGS = 2 * REGS - SOFTMAX_REGS;
-    static_assert(SOFTMAX_REGS + OTHER_REGS == 2 * REGS, "the shares of the two warpgroups add up to the launch's");
+    static constexpr int THREADS = 32 * kGroupWarps * (NG + 1), REGS = NG == 1 ? 128 : 168, SOFTMAX_REGS = 192, OTHER_REGS = (NG + 1) * REGS - NG * SOFTMAX_REGS;
+    static_assert(OTHER_REGS % 8 == 0 && THREADS * REGS * CTAS <= 64 * 1024, "the shares of the warpgroups add up to the launch's, within the SM's");
 };
 
 // What the roles need to know of a unit.
@@ -223,8 +238,8 @@ template <int D>
 __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(const __grid_constant__ PagedAttendArgs a, const __grid_constant__ Maps maps)
 {
     using L = Lay<D>;
-    constexpr int NS = L::NS, NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
-    constexpr int kLoadQK = 4, kLoadV = 5, kScores = 6;
+    constexpr int NG = L::NG, NS = L::NS, NSK = L::NSK, NSV = L::NSV, NI = L::NI, NB = L::NB, TILE = L::TILE;
+    constexpr int kSoftmaxWarps = NG * kGroupWarps, kLoadQK = kSoftmaxWarps, kLoadV = kLoadQK + 1, kScores = kLoadV + 1;
     extern __shared__ __align__(1024) unsigned char smem[];
     uint32_t &tmem_base_sh = *reinterpret_cast<uint32_t *>(smem + L::OFF_TMEM);
     const uint32_t sbase = smem_u32(smem);
@@ -235,12 +250,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
     if (warp == kLoadQK) {
         for (int i = lane; i < L::NBAR; i += 32) {
             const bool by_group = i == L::B_S_GO || (i >= L::B_P_GO && i < L::B_P_GO + NS), free = i >= L::B_I_FREE && i < L::B_I_FREE + NI;
-            mbar_init(bar(i), by_group ? kGroupWarps : free ? kGroupWarps + 3 : 1);
+            mbar_init(bar(i), by_group ? kGroupWarps : free ? kSoftmaxWarps + 3 : NG > 1 && i >= L::B_SUMS ? kSoftmaxWarps : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     } else if (warp == kScores) {
         tmem_alloc<1, L::COLS>(smem_u32(&tmem_base_sh));
+    } else if (NG > 1 && warp == kLoadV && lane < 3 * kGroupWarps) {
+        Share &share = *reinterpret_cast<Share *>(smem + L::OFF_SHARE);
+        (lane < 2 * kGroupWarps ? &share.done[0][0] + lane : share.left + lane - 2 * kGroupWarps)[0] = 0;
     }
     after_last();
     {
@@ -260,6 +278,20 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
         tc_fence_after();
         return got;
     };
+    // a count in shared memory, and a bounded wait until it is `least` (what was written before it was stored is there)
+    auto store_count = [&](int *word, int x) { asm volatile("st.release.cta.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(word)), "r"(x) : "memory"); };
+    auto wait_count = [&](const int *word, int least) -> bool {
+        const uint32_t at = smem_u32(word);
+        const long long since = clock64();
+        while (true) {
+            int x;
+            asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
+            if (__all_sync(0xFFFFFFFFu, x >= least)) return true;
+            const long long waited = clock64() - since;
+            const bool over = waited > (1LL << 31) || (waited > (1LL << 20) && *reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u);
+            if (__any_sync(0xFFFFFFFFu, over)) return false;
+        }
+    };
     // description of unit u (a whole warp); its place is given back once every lane has it
     auto unit = [&](int u, Info &x) -> bool {
         if (!__all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up))) return false;
@@ -269,7 +301,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
         return true;
     };
 
-    if (warp >= kGroupWarps) {
+    if (warp >= kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
         const int boxes = BN / a.box_rows;  // of a tile and 64-column block
         const int col = lane % boxes * a.box_rows, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;
@@ -383,6 +415,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     }
                 } else {
                     constexpr uint32_t ID_O = idesc_bf16(BM, D, true);
+                    if (NG > 1 && nq > 0) ok = wait_all(L::B_O_FREE, (nq - 1) & 1);
                     for (int j = 0; j < n && ok; ++j, ++t) {
                         const int st = t % NSV;
                         ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO + t % NS, (t / NS) & 1);
@@ -413,12 +446,15 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(L::SOFTMAX_REGS));
-        const int r = threadIdx.x;  // TMEM lane, row of the tile, key of a tile at the edges
+        const int group = warp / kGroupWarps, quarter = warp % kGroupWarps;
+        const int r = threadIdx.x % BM;  // TMEM lane, row of the tile, key of a tile at the edges
         const int tok = r / a.block, head = r - tok * a.block;
-        const int tok_first = warp * 32 / a.block, tok_last = (warp * 32 + 31) / a.block;  // of the warp
-        const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
+        const int tok_first = quarter * 32 / a.block, tok_last = (quarter * 32 + 31) / a.block;  // of the warp
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
         const uint32_t t_o = tmem + L::T_O + lane_off;
-        int t = 0;           // tiles
+        Share &share = *reinterpret_cast<Share *>(smem + L::OFF_SHARE);
+        int t0 = 0;          // tiles of the units before
+        int keyed = 0;       // units with keys
         bool there = false;  // the next scores, seen under the last exponentials: a poll takes 200 cycles and more even if they are
         bool left = false;   // rows of this warp came out not finite
         if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
@@ -432,16 +468,17 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
             const bool idle = !__any_sync(0xFFFFFFFFu, valid);
             const int pos0 = x.pos0, pos = pos0 + tok, end = x.end;
             // A tile's keys follow one another from k0 on, but for granules of the anchors, which the first `mixed` have.
-            int k0 = GR * (x.first - x.sinks) + BN * x.j0;
+            int k0 = GR * (x.first - x.sinks) + BN * (x.j0 + group);
             const int mixed = (x.sinks + BN / GR - 1) / (BN / GR) - x.j0;
             // row sum, reference, largest score; by how much the largest score's weight is rounded up: the outputs
             // are divided by the sum with that weight as rounded, so that a row whose weight goes to one key is that key's values
             float l = 0.f, m = -INFINITY, top = -INFINITY, up = 0.f;
-            for (int j = 0; j < n; ++j, ++t, k0 += BN) {
+            for (int j = group; j < n; j += NG, k0 += NG * BN) {
+                const int t = t0 + j, buf = (unsigned)t % NS;
                 // (after a wait that gave up the loop runs on without waiting: fewer branches in it)
-                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL + t % NS, (t / NS) & 1);
+                if (!__all_sync(0xFFFFFFFFu, there) && ok) ok = wait_all(L::B_S_FULL + buf, (unsigned)t / NS & 1);
                 tc_fence_after();
-                const uint32_t t_s = tmem + lane_off + t % NS * BN, t_p = t_s + L::T_P;
+                const uint32_t t_s = tmem + lane_off + buf * BN, t_p = t_s + L::T_P;
                 if (idle) {
                     there = false;
                     if (!L::OVER) mbar_arrive_if(lane == 0, bar(L::B_S_GO));
@@ -480,30 +517,43 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                         }
                     }
                     const float raw = valid ? row_max(sv) : -INFINITY, mx = __fmul_rn(raw, a.scale_log2);
-                    const bool upd = mx > m + kLazyLog2;
-                    const bool scale_o = upd && m != -INFINITY;
-                    const bool any_scale = __any_sync(0xFFFFFFFFu, scale_o);
-                    const float al = scale_o ? exp2f(m - mx) : 1.f;
-                    l *= al;
-                    m = upd ? mx : m;
+                    bool any_scale = false;
+                    float al = 1.f;
+                    if constexpr (NG == 1) {
+                        const bool upd = mx > m + kLazyLog2, scale_o = upd && m != -INFINITY;
+                        any_scale = __any_sync(0xFFFFFFFFu, scale_o);
+                        al = scale_o ? exp2f(m - mx) : 1.f;
+                        m = upd ? mx : m;
+                    } else {
+                        // (the groups' weights add up in one O: a row without a reference waits for the other group's last tile)
+                        if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {
+                            if (j > 0) {
+                                if (ok) ok = wait_count(&share.done[1 - group][quarter], t);
+                                m = share.ref[r];
+                            }
+                            if (m == -INFINITY) m = mx;
+                            share.ref[r] = m;
+                        }
+                        __syncwarp();
+                        if (lane == 0) store_count(&share.done[group][quarter], t + 1);
+                    }
                     const float mu = m == -INFINITY ? 0.f : m;
                     uint32_t hw[BN / 2];
-                    float sum = weights_of<0, BN * 3 / 4>(sv, a.scale_log2, mu, hw);
+                    float sum = weights_of<0, 96>(sv, a.scale_log2, mu, hw);
                     // polled here, the answers are there when the weights are
                     bool settled = true;
                     if (!L::OVER) settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
-                    if (!L::OVER || NS > 1) there = mbar_test<1>(bar(L::B_S_FULL + (t + 1) % NS), ((t + 1) / NS) & 1);
-                    l += sum + weights_of<BN * 3 / 4, BN>(sv, a.scale_log2, mu, hw);
+                    there = (NG == 1 || j + NG < n) && mbar_test<1>(bar(L::B_S_FULL + (unsigned)(t + NG) % NS), (unsigned)(t + NG) / NS & 1);
+                    sum += weights_of<96, BN>(sv, a.scale_log2, mu, hw);
+                    l = NG == 1 ? fmaf(l, al, sum) : l + sum;
                     const float w = ex2(fmaf(raw, a.scale_log2, -mu));
                     up = mx > top ? __bfloat162float(__float2bfloat16_rn(w)) - w : up * al;
                     top = fmaxf(top, mx);
                     // P's buffer is free and O has settled once the last value product is done (where P takes its own
-                    // scores' place, only a change of O waits for that; a unit's first tile: waited for at the end
-                    // of the last unit)
-                    if (L::OVER) settled = !any_scale || j == 0;
-                    if (!__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE + (t - 1) % NS, ((t - 1) / NS) & 1);
+                    // scores' place, O is not looked at; a unit's first tile: waited for at the end of the last unit)
+                    if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
                     tc_fence_after();
-                    if (any_scale) {
+                    if (NG == 1 && any_scale) {
 #pragma unroll 1
                         for (int c0 = 0; c0 < D; c0 += 32) {
                             float ov[32];
@@ -530,53 +580,83 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 }
                 tc_fence_before();
                 __syncwarp();
-                mbar_arrive_if(lane == 0, bar(L::B_P_GO + t % NS));
+                mbar_arrive_if(lane == 0, bar(L::B_P_GO + buf));
             }
-            if (ok && n > 0) ok = wait_all(L::B_PV_DONE + (t - 1) % NS, ((t - 1) / NS) & 1);
+            if (ok && n > 0) ok = wait_all(L::B_PV_DONE + (unsigned)(t0 + n - 1) % NS, (unsigned)(t0 + n - 1) / NS & 1);
+            bool grown = false;
+            if constexpr (NG > 1) {
+                there = false;
+                grown = top > m + kGrowthLog2;
+                if (n > 0) {
+                    float4 *const sums = share.sums[u & 1][0];
+                    sums[BM * group + r] = make_float4(l, up, top, m);
+                    __syncwarp();
+                    mbar_arrive_if(lane == 0, bar(L::B_SUMS));
+                    if (ok) ok = wait_all(L::B_SUMS, keyed & 1);
+                    const float4 y = sums[r], z = sums[BM + r];  // of either group, in this order in both
+                    l = y.x + z.x;
+                    up = y.z >= z.z ? y.y : z.y;
+                    top = fmaxf(y.z, z.z);
+                    m = fmaxf(y.w, z.w);  // (the same, or one of them saw no key)
+                    grown = top > m + kGrowthLog2;
+                    ++keyed;
+                }
+            }
+            t0 += max(n, 0);
             if (!ok) break;
             const int part = x.part, head0 = x.head0, row0 = x.row0;
             __syncwarp();
             mbar_arrive_if(lane == 0, bar(L::B_I_FREE + u % NI));
-            if (idle) {
-                tc_fence_before();
-                continue;
-            }
-            // a thread's row; rows with no weight (scale 0) become zeros whatever the columns hold
-            auto emit = [&](auto *to, float scale) {
-                using TOut = std::remove_pointer_t<decltype(to)>;
-                constexpr int E = 16 / (int)sizeof(TOut);
-                float found = 0.f;  // NaN where a value is not finite
+            if (!idle) {
+                // a thread's row (of two groups: each half of the columns); rows with no weight (scale 0) become zeros whatever
+                // the columns hold
+                auto emit = [&](auto *to, float scale) {
+                    using TOut = std::remove_pointer_t<decltype(to)>;
+                    constexpr int E = 16 / (int)sizeof(TOut);
+                    float found = 0.f;  // NaN where a value is not finite
 #pragma unroll 1
-                for (int c0 = 0; c0 < D; c0 += 32) {
-                    float x[32];
-                    tmem_ld32(t_o + c0, x);  // (of no use where there is no tile)
+                    for (int c0 = D / NG * group; c0 < D / NG * (group + 1); c0 += 32) {
+                        float y[32];
+                        tmem_ld32(t_o + c0, y);  // (of no use where there is no tile)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        x[e] = scale == 0.f ? 0.f : x[e] * scale;
-                        found = fmaf(x[e], 0.f, found);
-                    }
-                    if (valid) {
+                        for (int e = 0; e < 32; ++e) {
+                            y[e] = scale == 0.f ? 0.f : y[e] * scale;
+                            found = fmaf(y[e], 0.f, found);
+                        }
+                        if (valid) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += E) store16<TOut>(to + c0 + e, x + e);
+                            for (int e = 0; e < 32; e += E) store16<TOut>(to + c0 + e, y + e);
+                        }
                     }
+                    left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
+                };
+                const float by = l + up, far = grown || (fabsf(m) > kFarLog2 && fabsf(m) < INFINITY) ? NAN : 1.f;
+                if (part < 0) {
+                    const int64_t row = row0 + tok;
+                    if (group == 0 && valid && a.lse != nullptr) a.lse[(head0 + head) * a.q_total + row] = (m + log2f(l)) * kLn2;
+                    emit(reinterpret_cast<__nv_bfloat16 *>(a.out) + (row * a.Hq + head0 + head) * D, l == 0.f ? 0.f : far / by);
+                } else {
+                    const int64_t at = (int64_t)part * a.part_rows + r;
+                    if (group == 0 && valid) a.part_ml[at] = make_float4(m, l, by, 0.f);
+                    emit(a.part_o + at * D, l == 0.f ? 0.f : far);
                 }
-                left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
-            };
-            const float by = l + up, far = fabsf(m) > kFarLog2 && fabsf(m) < INFINITY ? NAN : 1.f;
-            if (part < 0) {
-                const int64_t row = row0 + tok;
-                if (valid && a.lse != nullptr) a.lse[(head0 + head) * a.q_total + row] = (m + log2f(l)) * kLn2;
-                emit(reinterpret_cast<__nv_bfloat16 *>(a.out) + (row * a.Hq + head0 + head) * D, l == 0.f ? 0.f : far / by);
-            } else {
-                const int64_t at = (int64_t)part * a.part_rows + r;
-                if (valid) a.part_ml[at] = make_float4(m, l, by, 0.f);
-                emit(a.part_o + at * D, l == 0.f ? 0.f : far);
             }
-            tc_fence_before();  // (O has been read before the next P is announced)
+            tc_fence_before();  // (O has been read before the next P, or O_FREE, is announced)
+            if (NG > 1 && n > 0) {
+                __syncwarp();
+                mbar_arrive_if(lane == 0, bar(L::B_O_FREE));
+            }
         }
         // (after everything else: it takes far longer than a wait of another role may)
         __syncwarp();
-        if (ok && left) rows_as_given<D>(a, run, warp);
+        if constexpr (NG > 1) {  // the first group computes both's
+            if (ok && left && lane == 0 && group == 1) share.left[quarter] = 1;
+            __syncwarp();
+            mbar_arrive_if(lane == 0, bar(L::B_SUMS));
+            if (ok) ok = wait_all(L::B_SUMS, keyed & 1);
+            left = group == 0 && (left || share.left[quarter] != 0);
+        }
+        if (ok && left) rows_as_given<D>(a, run, quarter);
     }
     if (!ok) atomicOr(&g_ris_paged_wait, 2u);
     __syncwarp();
