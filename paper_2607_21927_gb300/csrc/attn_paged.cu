@@ -65,7 +65,7 @@ constexpr float kGrowthLog2 = 100.f;
 struct Share {
     float ref[kTileRows];                          // the rows' references
     int done[2][kGroupWarps];                      // each warp's tiles whose references are settled
-    float4 sums[2][2][kTileRows];                  // [unit mod 2][group]: sum, its correction, largest score, reference
+    float4 sums[2][2][kTileRows];                  // [unit with keys mod 2][group]: sum, its correction, largest score, reference
     int left[kGroupWarps];
 };
 
@@ -569,6 +569,10 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     tmem_wait_st();
                 }
                 if (j < mixed || k0 + BN > end) {  // (a thread takes a key)
+                    // (the values before in this place have been used: the scores came without waiting for that, and the wait for
+                    // the values' phase tells nothing while the one before it is open)
+                    static_assert(NG == 1 || NSV == 2, "which ones those are");
+                    if (NG > 1 && t >= 2 && ok) ok = wait_all(L::B_PV_DONE + (unsigned)(t - 2) % NS, (unsigned)(t - 2) / NS & 1);
                     if (ok) ok = wait_all(L::B_V_FULL + t % NSV, (t / NSV) & 1);
                     if (ok && (j < mixed ? x.key(j, r) : k0 + r) >= end) {
                         unsigned char *const row = smem + L::OFF_V + t % NSV * TILE + r * 128;
@@ -588,7 +592,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 there = false;
                 grown = top > m + kGrowthLog2;
                 if (n > 0) {
-                    float4 *const sums = share.sums[u & 1][0];
+                    float4 *const sums = share.sums[keyed & 1][0];
                     sums[BM * group + r] = make_float4(l, up, top, m);
                     __syncwarp();
                     mbar_arrive_if(lane == 0, bar(L::B_SUMS));

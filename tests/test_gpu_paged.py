@@ -163,6 +163,23 @@ def test_windows_and_anchors(dtype, D, page):
     ris.ris_device_status()
 
 
+@pytest.mark.parametrize("D,Hq,Hkv", [(128, 12, 2), (64, 8, 1)])
+def test_few_rows_behind_many_keys(D, Hq, Hkv):
+    """Several tiles to a CTA, most of a row tile's warps without a row, the last tile cut off anywhere; the same bits each time."""
+    q_lens = [1, 4, 1, 2, 1, 1, 7, 1]
+    lengths = [9001 + 77 * i for i in range(8)]
+    cache, keys, values = make(lengths, Hkv, D, 64, BF16, seed=4, fill=3.0)
+    q = randn(sum(q_lens), Hq, D, seed=5, dtype=BF16)
+    with ris.ris_pack_create(q_lens) as pack:
+        for window, anchors in ((0, 0), (5000, 4)):
+            out, lse = ris.ris_paged_attend(cache, pack, q, window, anchors, return_lse=True)
+            check(out, lse, plain(q, keys, values, q_lens, window, anchors), BF16)
+            for _ in range(20):
+                again, = ris.ris_paged_attend(cache, pack, q, window, anchors)
+                assert torch.equal(out, again)
+    ris.ris_device_status()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_many_sequences(dtype):
     """More sequences than a CTA has threads, with and without several row tiles, some without rows or keys."""
