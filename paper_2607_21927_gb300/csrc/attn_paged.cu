@@ -7,18 +7,20 @@
 // row's sum from the fp32 weights. The heads of a KV head share a row tile (attn_paged.cuh), so few rows
 // read a key once for all of them.
 //
-// Persistent, each CTA on its run of the line, one row tile at a time with one softmax group:
-//   head dim 128  one CTA to an SM and two buffers of scores (TMEM 512 columns): the scores of the next tile and the value
-//                 product of the last run under a tile's softmax. Two CTAs with a buffer each, whose scores wait
-//                 for the value product before, took 1,130 us instead of 1,046 for 8,192 rows behind 24,576 keys at 12 / 2
-//                 heads (1.38 PFLOP/s) and 36 instead of 28 for 24 sequences' four rows through a window of 4,096.
-//   head dim 64   two CTAs to an SM (TMEM 256 columns), weights beside the scores; the products are half as
-//                 long, and one softmax group does not fill an SM: 1,108 us instead of 1,650 for 16,384 rows at 32 / 4 heads.
-//   warp 4  the run's units, query and key tiles, warp 5 value tiles: TMA, a box for each page of a tile, the
-//           boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
-//           fills its place with zeros;
-//   warp 6  S = Q K^T as soon as its columns are free, warp 7 O += P V;
-//   warps 0-3  the softmax, one thread per row; a warp without a row only passes the tiles on.
+// Persistent, each CTA on its run of the line, one row tile at a time:
+//   head dim 128  one CTA to an SM (TMEM 512 columns), two softmax groups that take the row tile's key tiles in turn and add
+//                 their weights up in one O, three buffers of scores. 8,192 rows behind 24,576 keys at 12 / 2 heads take 900 us
+//                 (1.6 PFLOP/s; 990 in a long row of calls, at the power limit): a tile takes 1,350 cycles, of which shared
+//                 memory is busy for 1,280 (Q and K read for the scores, V for the outputs, 64 KB written by TMA). With one group and two
+//                 buffers 1,015, with two CTAs of a group and a buffer each 1,130. 16 single tokens behind 48 to 64 thousand keys: 140 us, 95%
+//                 of the copy rate.
+//   head dim 64   two CTAs to an SM (TMEM 256 columns) with a group each, weights beside the scores; nothing is full, a softmax warp's
+//                 chain of 2,450 cycles a tile sets the time: 16,384 rows at 32 / 4 heads take 1,105 us; one CTA took 1,650.
+// The first warps (a group's four) do the softmax, one thread per row; a warp without a row only passes the tiles on. Then
+//   kLoadQK   the run's units, query and key tiles, kLoadV value tiles: TMA, a box for each page of a tile, the
+//             boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
+//             fills its place with zeros;
+//   kScores   S = Q K^T as soon as its columns are free, and the last warp O += P V.
 //
 // A product over a tile multiplies keys that a row does not see by 0, and 0 times an infinity is not 0. The
 // slots past the last row's own key, where a page may hold anything, are cleared in the tile by the softmax
@@ -105,8 +107,8 @@ struct Lay {
     static constexpr uint32_t COLS = 512 / CTAS, T_P = OVER ? 0 : BN, T_O = NS * BN + (OVER ? 0 : BN / 2);  // TMEM; S at 0
     static_assert(T_O + D <= COLS, "TMEM columns");
     // Registers per thread: at launch, then after setmaxnreg of a softmax and of another thread. Shared memory leaves
-    // next to no L1, so what a loader spills comes from L2: with 56 instead of 64 (head dim 128: 152) for them, single tokens
-    // against long caches ran at 5.3 TB/s instead of 6.3.
+    // next to no L1, so what a loader spills comes from L2: with 56 for them, single tokens against long caches ran at 5.3
+    // TB/s instead of 6.5.
     static constexpr int THREADS = 32 * kGroupWarps * (NG + 1), REGS = NG == 1 ? 128 : 168, SOFTMAX_REGS = 192, OTHER_REGS = (NG + 1) * REGS - NG * SOFTMAX_REGS;
     static_assert(OTHER_REGS % 8 == 0 && THREADS * REGS * CTAS <= 64 * 1024, "the shares of the warpgroups add up to the launch's, within the SM's");
 };

@@ -5,7 +5,7 @@
 // from the first that its first row sees up to its last row's own, and the first `anchors`: a list of granules
 // (32 keys; in fp32 a tile), those of the anchors first, cut into n tiles of BN keys, and the row tile costs n + 4, in fp32 n + 1: beginning and ending it takes as long as so
 // many tiles (bf16 at n + 1: the CTAs that have the short row tiles came last, 714 us instead of 635 for 16,384 rows at 12 / 2
-// heads of 128; fp32 at n + 4: 186 instead of 156 for 900). The row tiles of all sequences, heads innermost,
+// heads of 128 with one softmax group; fp32 at n + 4: 186 instead of 156 for 900). The row tiles of all sequences, heads innermost,
 // laid one after another make a line of that length, which is cut into as many equal runs as there are
 // CTAs: one row against 60,000 keys and 8,000 rows against 30,000 are spread over the SMs alike, whatever
 // the lengths, which only the device knows. A row tile that lies in one run is finished there; of the
