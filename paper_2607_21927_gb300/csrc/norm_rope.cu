@@ -11,7 +11,7 @@
 // thread keeps its V angles for all heads of its token. Arithmetic and statistics are fp32 (two values to an
 // instruction), angles 64-bit fractions of a turn (rows.cuh). Bound by HBM, each element read once and written
 // once: 30,011 tokens of 12 / 2 heads of 128 in bf16 take 37 us (215 MB, 86% of the copy rate); the gradient
-// at 32 / 4 heads of 64 takes 75 us (415 MB, 82%).
+// at 32 / 4 heads of 64 takes 70.5 us (415 MB, 87%; 75 without the hint that the next 256 bytes follow).
 #include <algorithm>
 #include <cstdint>
 
@@ -31,7 +31,7 @@ using tc::f2_unpack;
 
 constexpr int kThreads = 256, kSMs = 152;
 // CTAs of an SM and stages of the ring. Four CTAs (64 registers) took 41 us instead of 37 forwards, three (84) 111 instead
-// of 75 backwards; rings of 3 or 6 stages instead of 4 1 us more, of 4 instead of 3 2 us.
+// of 77 backwards; rings of 3 or 6 stages instead of 4 1 us more, of 4 instead of 3 2 us.
 constexpr int kForwardCtas = 3, kForwardStages = 4, kBackwardCtas = 2, kBackwardStages = 3;
 
 // The pairs of a thread: lane l of a head's D / 2V.
@@ -141,7 +141,7 @@ struct Ring {
     __device__ __forceinline__ uint4 *at(int64_t step, int piece) const { return mine + ((int)(step % S) * P + piece) * kThreads; }
     __device__ __forceinline__ void ask(int64_t step, int piece, const void *src) const
     {
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(at(step, piece))), "l"(src) : "memory");
+        asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(at(step, piece))), "l"(src) : "memory");
     }
     static __device__ __forceinline__ void close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory"); }  // for the oldest of S - 1
