@@ -15,7 +15,7 @@
 //                 buffers 1,015, with two CTAs of a group and a buffer each 1,130. 16 single tokens behind 48 to 64 thousand keys: 140 us, 95%
 //                 of the copy rate.
 //   head dim 64   two CTAs to an SM (TMEM 256 columns) with a group each, weights beside the scores; nothing is full, a softmax warp's
-//                 chain of 2,450 cycles a tile sets the time: 16,384 rows at 32 / 4 heads take 1,105 us; one CTA took 1,650.
+//                 chain of 2,370 cycles a tile sets the time: 16,384 rows at 32 / 4 heads take 1,070 us; one CTA took 1,650.
 // The first warps (a group's four) do the softmax, one thread per row; a warp without a row only passes the tiles on. Then
 //   kLoadQK   the run's units, query and key tiles, kLoadV value tiles: TMA, a box for each page of a tile, the
 //             boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
@@ -54,13 +54,13 @@ using namespace paged;
 constexpr int BM = kTileRows, BN = kTileKeys, GR = kPagedGranule;
 static_assert(kPagedTileRows == BM && kPagedTileKeys == BN, "as the work is shared out");
 constexpr int kGroupWarps = 4;  // of the softmax group: one thread per row
-// The reference m of a row moves only when its largest score grows by more than this: P stays below 2^7.
-constexpr float kLazyLog2 = 7.f;
 // The exponent of a weight is rounded once, the reference behind it was rounded as a product: rows that pass
 // this (no model's do) are computed from the inputs as given, where both are rounded alike.
 constexpr float kFarLog2 = 0x1p28f;
-// Two groups: a row's reference is its largest score in the first tile where it sees a key, and stays. Weights may grow by 2^100
-// above it (bf16 and fp32 hold that); rows that pass this are computed from the inputs as given too.
+// A row's reference is its largest score in the first tile of the part where it sees a key, and stays: O is never rescaled, and two
+// groups can add to one. Weights may grow by 2^100 above it, which bf16 and fp32 hold with values up to 2^20; rows that pass this are computed
+// from the inputs as given too. A reference that followed the largest score (by 2^7 at most behind) took 220 us instead of 211
+// for the 16,233 ragged rows at 32 / 4 heads of 64 through a window, although it moved in few tiles.
 constexpr float kGrowthLog2 = 100.f;
 
 // What two softmax groups tell each other.
@@ -92,7 +92,7 @@ struct Lay {
     //   S_GO    the last scores have been read out of their buffer (only where P has its own columns:
     //           else the value product before has to be done, which says that too)
     //   S_FULL  the next are there
-    //   P_GO    P is written (and O rescaled where needed)
+    //   P_GO    P is written
     //   PV_DONE O has settled, P's buffer is free
     // and, of two groups, one phase per unit with keys:
     //   SUMS    every softmax warp has left its rows' sums for the other group
@@ -519,13 +519,8 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                         }
                     }
                     const float raw = valid ? row_max(sv) : -INFINITY, mx = __fmul_rn(raw, a.scale_log2);
-                    bool any_scale = false;
-                    float al = 1.f;
                     if constexpr (NG == 1) {
-                        const bool upd = mx > m + kLazyLog2, scale_o = upd && m != -INFINITY;
-                        any_scale = __any_sync(0xFFFFFFFFu, scale_o);
-                        al = scale_o ? exp2f(m - mx) : 1.f;
-                        m = upd ? mx : m;
+                        m = m == -INFINITY ? mx : m;
                     } else {
                         // (the groups' weights add up in one O: a row without a reference waits for the other group's last tile)
                         if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {
@@ -547,25 +542,14 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     if (!L::OVER) settled = j == 0 || mbar_test<1>(bar(L::B_PV_DONE), (t - 1) & 1);
                     there = (NG == 1 || j + NG < n) && mbar_test<1>(bar(L::B_S_FULL + (unsigned)(t + NG) % NS), (unsigned)(t + NG) / NS & 1);
                     sum += weights_of<96, BN>(sv, a.scale_log2, mu, hw);
-                    l = NG == 1 ? fmaf(l, al, sum) : l + sum;
+                    l += sum;
                     const float w = ex2(fmaf(raw, a.scale_log2, -mu));
-                    up = mx > top ? __bfloat162float(__float2bfloat16_rn(w)) - w : up * al;
+                    up = mx > top ? __bfloat162float(__float2bfloat16_rn(w)) - w : up;
                     top = fmaxf(top, mx);
-                    // P's buffer is free and O has settled once the last value product is done (where P takes its own
-                    // scores' place, O is not looked at; a unit's first tile: waited for at the end of the last unit)
+                    // P's buffer is free once the last value product is done (a unit's first tile: waited for at the end of the
+                    // last unit)
                     if (!L::OVER && !__all_sync(0xFFFFFFFFu, settled) && ok) ok = wait_all(L::B_PV_DONE, (t - 1) & 1);
                     tc_fence_after();
-                    if (NG == 1 && any_scale) {
-#pragma unroll 1
-                        for (int c0 = 0; c0 < D; c0 += 32) {
-                            float ov[32];
-                            uint32_t ow[32];
-                            tmem_ld32(t_o + c0, ov);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) ow[e] = __float_as_uint(ov[e] * al);
-                            tmem_st32(t_o + c0, ow);
-                        }
-                    }
                     tmem_st32(t_p, hw);
                     tmem_st32(t_p + 32, hw + 32);
                     tmem_wait_st();
@@ -589,10 +573,8 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 mbar_arrive_if(lane == 0, bar(L::B_P_GO + buf));
             }
             if (ok && n > 0) ok = wait_all(L::B_PV_DONE + (unsigned)(t0 + n - 1) % NS, (unsigned)(t0 + n - 1) / NS & 1);
-            bool grown = false;
             if constexpr (NG > 1) {
                 there = false;
-                grown = top > m + kGrowthLog2;
                 if (n > 0) {
                     float4 *const sums = share.sums[keyed & 1][0];
                     sums[BM * group + r] = make_float4(l, up, top, m);
@@ -604,7 +586,6 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     up = y.z >= z.z ? y.y : z.y;
                     top = fmaxf(y.z, z.z);
                     m = fmaxf(y.w, z.w);  // (the same, or one of them saw no key)
-                    grown = top > m + kGrowthLog2;
                     ++keyed;
                 }
             }
@@ -636,6 +617,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                     }
                     left = left || __any_sync(0xFFFFFFFFu, valid && found != found);
                 };
+                const bool grown = top > m + kGrowthLog2;
                 const float by = l + up, far = grown || (fabsf(m) > kFarLog2 && fabsf(m) < INFINITY) ? NAN : 1.f;
                 if (part < 0) {
                     const int64_t row = row0 + tok;

@@ -260,6 +260,25 @@ def test_large_scores(dtype):
     check(out, lse, plain(q, keys, values, [70]), dtype)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_that_grow(D):
+    """Keys from the fourth tile on with scores 2^60, 2^90, 2^130 or 2^400 above the first ones': a row's reference stays behind them,
+    or the row is computed another way. Many rows, and a few behind many keys."""
+    for rows, length in ((70, 700), (3, 9000)):
+        cache, _, values = make([length], 1, D, 32, BF16, seed=1, fill=0.0)
+        q = randn(rows, 4, D, seed=2, dtype=BF16)
+        start = torch.zeros(1, dtype=torch.int32, device="cuda")
+        for f in (12.0, 18.0, 26.0, 80.0):
+            k = randn(length, 1, D, seed=3)
+            k[384:] *= f
+            k = k.to(BF16)
+            with ris.ris_pack_create([length]) as pack:
+                ris.ris_paged_append(cache, pack, k, values[0], start=start)
+            with ris.ris_pack_create([rows]) as pack:
+                out, lse = ris.ris_paged_attend(cache, pack, q, return_lse=True)
+            check(out, lse, plain(q, [k], values, [rows]), BF16)
+
+
 def test_longest_cuts_the_lengths():
     cache, keys, values = make([500, 90], 2, 64, 16, BF16, seed=1)
     q = randn(8, 4, 64, seed=2, dtype=BF16)
