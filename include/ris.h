@@ -608,6 +608,9 @@ ris_status ris_paged_append(const ris_paged *cache, ris_pack_t pack, const void 
  * One token, a few drafted ones and chunks of prompts may stand in one pack, any heads / kv_heads.
  * An entry of the table that is needed and no page is reported by ris_device_status as RIS_ERR_INVALID (the rows
  * that see it are then undefined). A key that a row does not see takes no part in it, whatever it holds.
+ * fp32: products and sums in fp32. bf16: exact products, fp32 sums, each weight rounded once. bf16 rows that cannot be had so (a value that
+ * is not finite beside them in a tile, a weight more than 2^100 times those of the first 128 keys) are computed a second time in fp32: right,
+ * but slow.
  * Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
 ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void *q, int64_t q_stride, int32_t heads, int32_t window,
                             int32_t anchors, int64_t longest, void *out, float *lse, void *stream);
