@@ -11,7 +11,7 @@
 // thread keeps its V angles for all heads of its token. Arithmetic and statistics are fp32 (two values to an
 // instruction), angles 64-bit fractions of a turn (rows.cuh). Bound by HBM, each element read once and written
 // once: 30,011 tokens of 12 / 2 heads of 128 in bf16 take 37 us (215 MB, 86% of the copy rate); the gradient
-// at 32 / 4 heads of 64 takes 70.5 us (415 MB, 87%; 75 without the hint that the next 256 bytes follow).
+// at 32 / 4 heads of 64 takes 69 us (415 MB, 89%; 73 without the hint that the next 256 bytes follow).
 #include <algorithm>
 #include <cstdint>
 
@@ -22,7 +22,7 @@
 namespace ris {
 namespace {
 
-using rows::sincos_turns;
+using rows::sincos_half_turns;
 using rows::Vec;
 using tc::f2_fma;
 using tc::f2_mul;
@@ -160,8 +160,8 @@ struct Turn {
             if (!lane.turns[4 * j / V]) continue;
             const uint64_t *const f = a.turn + lane.f[4 * j / V] + 2 * j % (V / 2);
             float s0, s1, c0, c1;
-            sincos_turns(pos, f[0], &s0, &c0);
-            sincos_turns(pos, f[1], &s1, &c1);
+            sincos_half_turns(pos, f[0], &s0, &c0);
+            sincos_half_turns(pos, f[1], &s1, &c1);
             cs[j] = f2_pack(c0 * a.mscale, c1 * a.mscale);
             sn[j] = f2_pack(s0 * a.mscale, s1 * a.mscale);
         }
