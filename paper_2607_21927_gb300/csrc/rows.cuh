@@ -49,7 +49,7 @@ __device__ __forceinline__ void sincos_turns(int32_t p, uint64_t turn, float *sn
     sincosf(fmaf(top, A, fmaf(top, A_LO, rest * B)), sn, cs);
 }
 
-// The same with the fraction's top 32 bits as half turns, rounded to 24 bits (3 2^-25 radians at most, like the rounding of
+// The same with the fraction's top 32 bits as half turns, rounded to 24 bits (pi 2^-25 radians at most, like the rounding of
 // an angle in fp32): fewer instructions, 3.0 instead of 3.5 us where a call is one chain of latencies.
 __device__ __forceinline__ void sincos_half_turns(int32_t p, uint64_t turn, float *sn, float *cs)
 {

@@ -851,12 +851,22 @@ def _like(out, x: torch.Tensor, name: str):
     return out, _heads(out, name)[3]
 
 
-def _weight(w: Optional[torch.Tensor], x: torch.Tensor, name: str):
+def _weight(w: Optional[torch.Tensor], D: int, x: torch.Tensor, name: str):
     if w is None:
         return None
-    if w.dtype != x.dtype or w.shape != x.shape[2:] or not w.is_contiguous() or w.get_device() != x.get_device():
-        raise ValueError(f"{name}: contiguous {x.dtype} [{x.shape[-1]}] on {x.device}")
+    if w.dtype != x.dtype or w.dim() != 1 or w.numel() != D or not w.is_contiguous() or w.get_device() != x.get_device():
+        raise ValueError(f"{name}: contiguous {x.dtype} [{D}] on {x.device}")
     return w.data_ptr()
+
+
+def _normed(x: Optional[torch.Tensor], d: Optional[torch.Tensor], shape, name: str) -> int:
+    """The token stride of an input of the forward call, of the shape and type of its output's gradient."""
+    if x is None or d is None or x.dtype != d.dtype or x.dim() != 3:
+        raise ValueError(f"{name}: the forward call's input, where it has a weight")
+    *its, stride = _heads(x, name)
+    if tuple(its) != shape:
+        raise ValueError(f"{name}: the forward call's input, where it has a weight")
+    return stride
 
 
 def _turning(positions, rope, n: int):
@@ -882,7 +892,7 @@ def ris_norm_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: Optiona
     else:
         k_out = None
     st = lib().ris_norm_rope(q.data_ptr(), _addr(k), q_out.data_ptr(), _addr(k_out), _code(q), n, Hq, Hkv, D, qs, ks, qos, kos,
-                             _turning(positions, rope, n), _weight(q_weight, q, "q_weight"), _weight(k_weight, q, "k_weight"), eps,
+                             _turning(positions, rope, n), _weight(q_weight, D, q, "q_weight"), _weight(k_weight, D, q, "k_weight"), eps,
                              rot_dim, int(pairs), n_ctx, _ref(rope), _raw_stream(stream, q))
     if st:
         _check("ris_norm_rope", st)
@@ -904,21 +914,21 @@ def ris_norm_rope_backward(dq: torch.Tensor, dk: Optional[torch.Tensor], q: Opti
         gk, gks = _like(gk, dk, "gk")
     else:
         gk = None
-    for x, d, w, name in ((q, dq, q_weight, "q"), (k, dk, k_weight, "k")):
-        if w is not None and (x is None or d is None or x.shape != d.shape or x.dtype != d.dtype):
-            raise ValueError(f"{name}: the forward call's input, where it has a weight")
+    gqw = gkw = qw = kw = None
     if q_weight is not None:
-        qs = _heads(q, "q")[3]
+        qs = _normed(q, dq, (n, Hq, D), "q")
+        qw = _weight(q_weight, D, dq, "q_weight")
+        gqw = torch.empty(D, dtype=torch.float32, device=dq.device)
     if k_weight is not None:
-        ks = _heads(k, "k")[3]
-    gw = [None if w is None else torch.empty(D, dtype=torch.float32, device=dq.device) for w in (q_weight, k_weight)]
+        ks = _normed(k, dk, (n, Hkv, D), "k")
+        kw = _weight(k_weight, D, dq, "k_weight")
+        gkw = torch.empty(D, dtype=torch.float32, device=dq.device)
     st = lib().ris_norm_rope_backward(
-        dq.data_ptr(), _addr(dk), _addr(q), _addr(k), gq.data_ptr(), _addr(gk), _addr(gw[0]), _addr(gw[1]), _code(dq), n, Hq, Hkv, D,
-        dqs, dks, qs, ks, gqs, gks, _turning(positions, rope, n), _weight(q_weight, dq, "q_weight"), _weight(k_weight, dq, "k_weight"),
-        eps, rot_dim, int(pairs), n_ctx, _ref(rope), _raw_stream(stream, dq))
+        dq.data_ptr(), _addr(dk), _addr(q), _addr(k), gq.data_ptr(), _addr(gk), _addr(gqw), _addr(gkw), _code(dq), n, Hq, Hkv, D,
+        dqs, dks, qs, ks, gqs, gks, _turning(positions, rope, n), qw, kw, eps, rot_dim, int(pairs), n_ctx, _ref(rope), _raw_stream(stream, dq))
     if st:
         _check("ris_norm_rope_backward", st)
-    return gq, gk, gw[0], gw[1]
+    return gq, gk, gqw, gkw
 
 
 # ----------------------------------------------------------------------------- the cache in pages

@@ -202,3 +202,20 @@ def test_on_another_stream():
     ris.ris_norm_rope(q, k, pos, n, rope, w, w, q_out=out[0], k_out=out[1], stream=side)
     side.synchronize()
     assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
+
+
+def test_binding_refuses():
+    """Weights and forward inputs that do not fit, before anything is launched."""
+    q, d, w = randn(5, 4, 64), randn(5, 4, 64), randn(64)
+    before = ris.ris_launch_count()
+    for bad in (randn(128), w[None], w.to(BF16), randn(128)[::2], w.cpu()):
+        with pytest.raises(ValueError):
+            ris.ris_norm_rope(q, None, None, 1, None, bad)
+        with pytest.raises(ValueError):
+            ris.ris_norm_rope_backward(d, None, q, None, None, 1, None, bad)
+    for bad in (None, randn(5, 4, 128)[..., :64], randn(6, 4, 64), randn(5, 2, 64), q.to(BF16), q[0]):
+        with pytest.raises(ValueError):
+            ris.ris_norm_rope_backward(d, None, bad, None, None, 1, None, w)
+    with pytest.raises(ValueError):
+        ris.ris_norm_rope_backward(d, None, q, q, None, 1, None, w, w)  # k has a weight and no gradient
+    assert ris.ris_launch_count() == before
