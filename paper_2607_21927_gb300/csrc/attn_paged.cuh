@@ -3,9 +3,10 @@
 // A row tile is a sequence's next `tokens` new tokens x a block of the query heads of a KV head (row r is
 // token r / block, head r % block), so that a token's heads share every key they read. It sees the keys
 // from the first that its first row sees up to its last row's own, and the first `anchors`: a list of granules
-// (32 keys; in fp32 a tile), those of the anchors first, cut into n tiles of BN keys, and the row tile costs n + 4, in fp32 n + 1: beginning and ending it takes as long as so
-// many tiles (bf16 at n + 1: the CTAs that have the short row tiles came last, 714 us instead of 635 for 16,384 rows at 12 / 2
-// heads of 128 with one softmax group; fp32 at n + 4: 186 instead of 156 for 900). The row tiles of all sequences, heads innermost,
+// (32 keys; in fp32 a tile), those of the anchors first, cut into n tiles of BN keys, and the row tile costs n and
+// as many tiles more as beginning and ending it take: 5 in bf16 at head dim 128 (16,384 rows at 12 / 2 heads: 556 us,
+// with 4 580, with 3 643, as the CTAs that have the short row tiles come last), 3 at 64 (16,384 rows at 32 / 4 heads:
+// 1,064 us, with 5 1,074), 1 in fp32 (900 rows: 156 us, with 4 186). The row tiles of all sequences, heads innermost,
 // laid one after another make a line of that length, which is cut into as many equal runs as there are
 // CTAs: one row against 60,000 keys and 8,000 rows against 30,000 are spread over the SMs alike, whatever
 // the lengths, which only the device knows. A row tile that lies in one run is finished there; of the
@@ -19,9 +20,6 @@
 
 namespace ris {
 namespace paged {
-
-template <int BN>
-constexpr int kUnitCost = BN == kPagedTileKeys ? kPagedTileUnitCost : kPagedF32UnitCost;
 
 // 0 <= length <= reach
 __device__ __forceinline__ int length_of(const PagedAttendArgs &a, int seq) { return min(max(a.c.length[seq], 0), a.reach); }
@@ -62,7 +60,7 @@ template <int BN>
 __device__ __forceinline__ int seq_cost(const PagedAttendArgs &a, int seq)
 {
     const int rows = a.off[seq + 1] - a.off[seq];
-    return rows > 0 ? sight_of<BN>(a, length_of(a, seq), rows, 0).n + kUnitCost<BN> : 0;
+    return rows > 0 ? sight_of<BN>(a, length_of(a, seq), rows, 0).n + a.unit_cost : 0;
 }
 
 __device__ __forceinline__ int64_t warp_scan(int64_t x)
@@ -186,7 +184,7 @@ struct Walk {
                     continue;
                 }
                 sight = sight_of<BN>(a, length_of(a, it.seq), rows, it.tile);
-                cost = sight.n + kUnitCost<BN>;
+                cost = sight.n + a.unit_cost;
                 seq = it.seq;
                 row0 = off + it.tile * a.tokens;
                 unit = 0;

@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_paged_plan(const __grid_consta
             }
             const PagedItem it{lo, i - first[lo]};
             a.items[i] = it;
-            cost = sight_of<KEYS>(a, length_of(a, lo), a.off[lo + 1] - a.off[lo], it.tile).n + kUnitCost<KEYS>;
+            cost = sight_of<KEYS>(a, length_of(a, lo), a.off[lo + 1] - a.off[lo], it.tile).n + a.unit_cost;
         }
         const int64_t at = before + block_scan<kPlanThreads>(cost, mem, all);
         if (i < n) a.prefix[i] = at;

@@ -153,6 +153,7 @@ struct PagedAttendArgs {
     int32_t box_rows;          // tile kernel: keys of a TMA box
     // the sharing out of the work (attn_paged.cuh)
     int64_t line;              // row tiles of the line (at most)
+    int32_t unit_cost;         // what a row tile costs besides its key tiles
     int32_t runs, least;       // runs of the line, one for each CTA; key tiles of one at least
     int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
     int64_t *prefix;           // [max_items + 1] scratch: cost of the items before
@@ -168,8 +169,8 @@ constexpr int kPagedSMs = 152;
 // keys of a key tile and rows of a row tile, fp32 (by the most rows that a sequence has) and bf16
 constexpr int kPagedF32Keys = 64, kPagedTileRows = 128, kPagedTileKeys = 128, kPagedGranule = 32;
 int32_t paged_f32_rows(int64_t rows);
-// what a row tile costs besides its key tiles
-constexpr int kPagedF32UnitCost = 1, kPagedTileUnitCost = 4;
+// in key tiles, what a row tile costs besides them
+constexpr int paged_unit_cost(bool tiles, int D) { return !tiles ? 1 : D == 128 ? 5 : 3; }
 constexpr int paged_tile_ctas(int D) { return D == 128 ? 1 : 2; }
 cudaError_t launch_paged_plan(const PagedAttendArgs &a, int dtype, cudaStream_t s);
 cudaError_t launch_paged_join(const PagedAttendArgs &a, int dtype, cudaStream_t s);

@@ -840,6 +840,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
     a.least = 1;
     const bool tiles = cache->dtype == RIS_BF16;
+    a.unit_cost = paged_unit_cost(tiles, cache->head_dim);
     const int32_t tile_rows = tiles ? kPagedTileRows : paged_f32_rows((int64_t)pack->q_longest * a.G);
     a.block = std::min(a.G, tile_rows);
     a.blocks = (a.G + a.block - 1) / a.block;
@@ -850,7 +851,7 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     const int64_t items = pack->q_longest <= a.tokens ? pack->n_seqs : pack->q_total / a.tokens + pack->n_seqs;
     if (pack->q_longest > a.tokens) a.max_items = (int32_t)items;
     // no more CTAs than the longest line there can be has key tiles
-    const int64_t most = a.reach / keys + 2 + (tiles ? kPagedTileUnitCost : kPagedF32UnitCost), line = items * cache->kv_heads * a.blocks;
+    const int64_t most = a.reach / keys + 2 + a.unit_cost, line = items * cache->kv_heads * a.blocks;
     a.line = line;
     a.runs = (int32_t)std::min<int64_t>(places, line > places ? line : line * most);
     const bool plan = a.max_items > 0;
