@@ -149,15 +149,23 @@ __device__ __forceinline__ float weights_of(const float (&sv)[BN], float sc, flo
     return a + b;
 }
 
-// Where the box from key j on lies: its page, or n_pages (past the pool's end) for one that no row sees or whose entry is
-// no page.
-__device__ __forceinline__ int box_page(const PagedAttendArgs &a, const Info &x, int j)
-{
-    if (j >= x.end || (j + a.box_rows <= x.low && j >= a.anchors)) return a.c.n_pages;
-    const int p = page_of(a.c, x.seq, j);
-    if (p < 0) atomicOr(&g_ris_paged_page, 1u);
-    return p < 0 ? a.c.n_pages : p;
-}
+// A lane's box of a tile and the table's entry for it.
+struct Box {
+    int key, entry;
+    bool seen;  // by some row
+    __device__ __forceinline__ Box(const PagedAttendArgs &a, const Info &x, int j, int col, bool mine) : key(x.key(j, col)), entry(-1)
+    {
+        seen = mine && key < x.end && (key + a.box_rows > x.low || key < a.anchors);
+        if (seen) entry = a.c.table[(int64_t)x.seq * a.c.table_len + (key >> a.c.page_log2)];
+    }
+    // its page, or n_pages (past the pool's end) for one that no row sees or whose entry is no page
+    __device__ __forceinline__ int page(const PagedAttendArgs &a) const
+    {
+        const bool is = entry >= 0 && entry < a.c.n_pages;
+        if (seen && !is) atomicOr(&g_ris_paged_page, 1u);
+        return seen && is ? entry : a.c.n_pages;
+    }
+};
 
 // A row of a unit on the FP32 pipe, by one warp: over the unit's key tiles, 32 keys at a time (a lane per key for
 // the scores, D / 32 channels for the outputs), each key only where the row sees it.
@@ -305,6 +313,9 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
 
     if (warp >= kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
+        // table entries are asked for a tile ahead where there are registers for it (pages of 16 slots at 12 / 2 heads of 128:
+        // 16,384 rows in 725 us instead of 772; at head dim 64 spilled registers cost 2%)
+        constexpr bool AHEAD = D == 128;
         const int boxes = BN / a.box_rows;  // of a tile and 64-column block
         const int col = lane % boxes * a.box_rows, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;
         if (warp == kLoadQK) {
@@ -329,15 +340,17 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 // (read from there, to need fewer registers)
                 const Info &x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
                 const int n = x.n;
+                Box next(a, x, 0, col, AHEAD && blk < NB && n > 0);
                 for (int j = 0; j < n; ++j, ++nk) {
-                    const int st = nk % NSK, key = x.key(j, col);
-                    const int page = blk < NB ? box_page(a, x, key) : 0;
+                    const int st = nk % NSK;
+                    const Box at = AHEAD ? next : Box(a, x, j, col, blk < NB);
+                    if (AHEAD && j + 1 < n) next = Box(a, x, j + 1, col, blk < NB);
                     if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up));
                     if (!ok) break;
                     if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + st), TILE);
                     __syncwarp();
                     if (blk < NB)
-                        tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + col * 128, &maps.k, 64 * blk, key & in_page, x.kv_head, page,
+                        tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + col * 128, &maps.k, 64 * blk, at.key & in_page, x.kv_head, at.page(a),
                                     bar(L::B_K_FULL + st));
                     if (j > 0) continue;
                     if (nq > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up));
@@ -365,15 +378,17 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 Info x;
                 ok = unit(u, x);
                 if (!ok || x.n < 0) break;
+                Box next(a, x, 0, col, AHEAD && blk < NB && x.n > 0);
                 for (int j = 0; j < x.n; ++j, ++nv) {
-                    const int st = nv % NSV, key = x.key(j, col);
-                    const int page = blk < NB ? box_page(a, x, key) : 0;
+                    const int st = nv % NSV;
+                    const Box at = AHEAD ? next : Box(a, x, j, col, blk < NB);
+                    if (AHEAD && j + 1 < x.n) next = Box(a, x, j + 1, col, blk < NB);
                     if (nv >= NSV) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up));
                     if (!ok) break;
                     if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + st), TILE);
                     __syncwarp();
                     if (blk < NB)
-                        tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + col * 128, &maps.v, 64 * blk, key & in_page, x.kv_head, page,
+                        tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + col * 128, &maps.v, 64 * blk, at.key & in_page, x.kv_head, at.page(a),
                                     bar(L::B_V_FULL + st));
                 }
             }
