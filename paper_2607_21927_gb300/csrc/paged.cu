@@ -488,7 +488,7 @@ cudaError_t launch_paged_append(PagedAppendArgs a, int dtype, cudaStream_t s)
         if (e != cudaSuccess) return e;
     }
     if (blocks == 1 || (blocks > 0 && a.start != nullptr)) return cudaSuccess;
-    if (blocks == 0 && a.start == nullptr) return cudaSuccess;
+    // (without rows too: lengths outside the slots are cut)
     return launch_chained(k_paged_lengths, dim3((unsigned)std::min<int64_t>(16, (a.c.B + kAppendThreads - 1) / kAppendThreads)), dim3(kAppendThreads), 0, s, a);
 }
 
