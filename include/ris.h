@@ -550,7 +550,8 @@ ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_
  * be NULL, rot_dim is 0). positions: DEVICE int32 [n], of either sign. All strides are elements from token to
  * token, as in ris_rope_axes; an output may be its input (with the same stride), so that rows of a fused
  * projection are normed in place, and else must not overlap it.
- * Statistics and products in fp32, angles exact at any position; bf16 results rounded once, to nearest even.
+ * Statistics and products in fp32, angles good to 2^-51 of themselves at any position (64-bit fractions of a turn); bf16 results rounded
+ * once, to nearest even.
  *
  * The gradient: dq, dk of q_out, k_out; gq, gk of q, k (gq may be dq or q, with the same stride, gk alike); gq_weight,
  * gk_weight fp32 [head_dim], for each weight that there is, summed over all tokens and heads in a fixed order (zeros
