@@ -265,6 +265,61 @@ __global__ void __launch_bounds__(kThreads, kForwardCtas) k_norm_rope(const __gr
     }
 }
 
+// s + c += x, what the addition drops kept in c
+__device__ __forceinline__ void add_exactly(float &s, float &c, float x)
+{
+    const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
+    c = __fadd_rn(c, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
+    s = t;
+}
+
+// A thread's sums of a weight's gradient. fp32 additions one after another would be off by up to 2^-24 of the sum each, all the same way where
+// the terms are alike (a thousand equal ones: 1e-5): a thread adds up kSumSteps of them in its registers, then these go to pairs of fp32 in its
+// column of shared memory, and everything after that is added in pairs.
+constexpr int kSumSteps = 64;
+template <int V, int LANES>
+struct Sums {
+    static constexpr int PITCH = kThreads + LANES;  // (the lanes' columns of different channels in different banks)
+    static constexpr int BYTES = 2 * V * PITCH * (int)sizeof(float2);
+    float2 *mem;
+    __device__ __forceinline__ void add(uint64_t (&a)[V / 2], uint64_t (&b)[V / 2], bool first) const
+    {
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) {
+            float x[4];
+            f2_unpack(a[j], x[0], x[1]);
+            f2_unpack(b[j], x[2], x[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float2 *const p = mem + (4 * j + i) * PITCH + threadIdx.x;
+                float2 y = first ? make_float2(0.f, 0.f) : *p;
+                add_exactly(y.x, y.y, x[i]);
+                *p = y;
+            }
+            a[j] = b[j] = 0;
+        }
+    }
+    // over the block's threads of lane l, in a fixed order
+    __device__ __forceinline__ float2 of(int l, int row) const
+    {
+        float s[4] = {}, c[4] = {};
+        for (int g = 0; g < kThreads / LANES; g += 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 y = mem[row * PITCH + (g + i) * LANES + l];
+                add_exactly(s[i], c[i], y.x);
+                c[i] += y.y;
+            }
+        }
+#pragma unroll
+        for (int i = 1; i < 4; ++i) {
+            add_exactly(s[0], c[0], s[i]);
+            c[0] += c[i];
+        }
+        return make_float2(s[0], c[0]);
+    }
+};
+
 // The gradient. A CTA belongs to q or to k (the sums of a weight's gradient stay in its threads' registers)
 // and takes every step-th group of tokens of it; what its threads summed is added up in a fixed order here
 // and over the CTAs in k_weight_sums, so that no result depends on the order in which they run.
@@ -275,11 +330,9 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) k_norm_rope_backward(
     using R = Ring<kBackwardStages, 4>;
     constexpr int V = L::V, LANES = D / (2 * V), TOKENS = kThreads / LANES;
     extern __shared__ __align__(16) uint4 mem[];
-    float (*const part)[D + 1] = reinterpret_cast<float (*)[D + 1]>(mem);  // (once the ring is done with)
-    static_assert(sizeof(float) * TOKENS * (D + 1) <= R::BYTES, "the sums' place");
-    const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
-    const L lane(l, a.rot);
+    const L lane(threadIdx.x % LANES, a.rot);
     const R ring(mem);
+    const Sums<V, LANES> sums{reinterpret_cast<float2 *>(mem + R::BYTES / 16)};
     const int w = (int)blockIdx.x >= a.ctas[0], heads = a.heads[w];
     after_last();
     const T *const weight = reinterpret_cast<const T *>(a.weight[w]);
@@ -346,38 +399,23 @@ __global__ void __launch_bounds__(kThreads, kBackwardCtas) k_norm_rope_backward(
         }
         if (here.there) L::put(reinterpret_cast<T *>(a.y[w]) + here.row * a.y_stride[w] + here.head * D, lane.at, ua, ub);
         moved = here.next(heads, a.n) && lane.any();
+        if (weight != nullptr && (s - run.first) % kSumSteps == kSumSteps - 1) sums.add(ga, gb, s - run.first == kSumSteps - 1);
     }
     if (weight == nullptr) return;
-    __syncthreads();  // (every thread has read its last pieces; its last groups are empty)
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-        const int ca = PAIRS ? 2 * e : e, cb = PAIRS ? 2 * e + 1 : V + e;
-        float y[2], z[2];
-        f2_unpack(ga[e / 2], y[0], y[1]);
-        f2_unpack(gb[e / 2], z[0], z[1]);
-        part[group][lane.at[ca / V] + ca % V] = y[e % 2];
-        part[group][lane.at[cb / V] + cb % V] = z[e % 2];
-    }
+    sums.add(ga, gb, run.end - run.first < kSumSteps);
     __syncthreads();
-    for (int c = threadIdx.x; c < D; c += kThreads) {
-        float s = 0.f;
-        for (int i = 0; i < TOKENS; ++i) s += part[i][c];
-        a.part[(int64_t)blockIdx.x * D + c] = s;
-    }
-}
-
-// s + c += x, what the addition drops kept in c
-__device__ __forceinline__ void add_exactly(float &s, float &c, float x)
-{
-    const float t = __fadd_rn(s, x), y = __fsub_rn(t, s);
-    c = __fadd_rn(c, __fadd_rn(__fsub_rn(s, __fsub_rn(t, y)), __fsub_rn(x, y)));
-    s = t;
+    if (threadIdx.x >= D) return;
+    // (row of a channel: as Sums::add has them)
+    const int row = threadIdx.x / LANES, e = row / 4 * 2 + row % 2, b = row / 2 % 2;
+    const L of(threadIdx.x % LANES, a.rot);
+    const int p = PAIRS ? 2 * e + b : V * b + e, c = (p < V ? of.at[0] : of.at[1]) + p % V;
+    a.part[(int64_t)blockIdx.x * D + c] = sums.of(threadIdx.x % LANES, row);
 }
 
 // dw of q (blockIdx.y 0) and k (1), 32 channels to a CTA: the CTAs' sums, a warp on every 32nd of them, then a warp's
 // lanes on a channel's. In pairs of fp32: as fp64 additions, of which an SM has few, the same sums took 15 us.
 constexpr int kSumWarps = 32;
-__global__ void __launch_bounds__(32 * kSumWarps) k_weight_sums(const float *part, int D, int ctas_q, int ctas_k, float *gq, float *gk)
+__global__ void __launch_bounds__(32 * kSumWarps) k_weight_sums(const float2 *part, int D, int ctas_q, int ctas_k, float *gq, float *gk)
 {
     __shared__ float2 sums[32][kSumWarps + 1];
     const int w = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = w ? ctas_k : ctas_q, c0 = 32 * blockIdx.x;
@@ -387,7 +425,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_weight_sums(const float *par
     part += (int64_t)(w ? ctas_q : 0) * D + c0 + lane;
     float s = 0.f, c = 0.f;
 #pragma unroll 8
-    for (int i = warp; i < n; i += kSumWarps) add_exactly(s, c, part[(int64_t)i * D]);
+    for (int i = warp; i < n; i += kSumWarps) {
+        const float2 x = part[(int64_t)i * D];
+        add_exactly(s, c, x.x);
+        c += x.y;
+    }
     sums[lane][warp] = make_float2(s, c);
     __syncthreads();
     const float2 y = sums[warp][lane];
@@ -413,7 +455,7 @@ template <typename T, bool PAIRS, int D>
 cudaError_t backward(const NormRopeArgs &a, float *gq, float *gk, cudaStream_t s)
 {
     if (a.n > 0) {
-        constexpr int bytes = Ring<kBackwardStages, 4>::BYTES;
+        constexpr int V = Vec<T>::V, bytes = Ring<kBackwardStages, 4>::BYTES + Sums<V, D / (2 * V)>::BYTES;
         static Once once;
         const cudaError_t ready = once([] { return cudaFuncSetAttribute(k_norm_rope_backward<T, PAIRS, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes); });
         if (ready != cudaSuccess) return ready;
@@ -422,7 +464,7 @@ cudaError_t backward(const NormRopeArgs &a, float *gq, float *gk, cudaStream_t s
     }
     if (gq == nullptr && gk == nullptr) return cudaSuccess;
     const int n0 = a.n > 0 ? a.ctas[0] : 0, n1 = a.n > 0 ? a.ctas[1] : 0;
-    return launch_chained(k_weight_sums, dim3(D / 32, 2), dim3(32 * kSumWarps), 0, s, static_cast<const float *>(a.part), D, n0, n1, gq, gk);
+    return launch_chained(k_weight_sums, dim3(D / 32, 2), dim3(32 * kSumWarps), 0, s, static_cast<const float2 *>(a.part), D, n0, n1, gq, gk);
 }
 
 }  // namespace

@@ -101,7 +101,7 @@ struct NormRopeArgs {
     uint64_t turn[kMaxHeadDimHalf];  // rotation frequencies as fractions of a turn, in 2^-64
     float mscale;
     int32_t ctas[2];           // gradient: CTAs of q and of k
-    float *part;               // [ctas[0] + ctas[1]][D] scratch, their sums for the weights
+    float2 *part;              // [ctas[0] + ctas[1]][D] scratch, their sums for the weights (value, what is left of it)
 };
 cudaError_t launch_norm_rope(const NormRopeArgs &a, int dtype, int D, bool pairs, cudaStream_t s);
 void norm_rope_ctas(int dtype, int D, int64_t n, const int32_t (&heads)[2], int32_t (&ctas)[2]);

@@ -770,8 +770,8 @@ ris_status ris_norm_rope_backward(const void *dq, const void *dk, const void *q,
     norm_rope_ctas(dtype, head_dim, n, a.heads, a.ctas);
     Scratch mem;
     if (n > 0 && (gq_weight != nullptr || gk_weight != nullptr)) {
-        RIS_CUDA(mem.alloc(sizeof(float) * (size_t)(a.ctas[0] + a.ctas[1]) * head_dim, s));
-        a.part = static_cast<float *>(mem.p);
+        RIS_CUDA(mem.alloc(sizeof(float2) * (size_t)(a.ctas[0] + a.ctas[1]) * head_dim, s));
+        a.part = static_cast<float2 *>(mem.p);
     }
     if (n > 0 || gq_weight != nullptr || gk_weight != nullptr) RIS_CUDA(launch_norm_rope_backward(a, dtype, head_dim, pairs != 0, gq_weight, gk_weight, s));
     return RIS_OK;
