@@ -550,8 +550,8 @@ ris_status ris_cache4_evict(const ris_cache4 *src, const ris_cache4 *dst, int32_
  * be NULL, rot_dim is 0). positions: DEVICE int32 [n], of either sign. All strides are elements from token to
  * token, as in ris_rope_axes; an output may be its input (with the same stride), so that rows of a fused
  * projection are normed in place, and else must not overlap it.
- * Statistics and products in fp32, angles good to 2^-51 of themselves at any position (64-bit fractions of a turn); bf16 results rounded
- * once, to nearest even.
+ * Statistics and products in fp32, angles good to 2^-51 of themselves and 2^-30 radians at any position (64-bit fractions of a turn); bf16
+ * results rounded once, to nearest even.
  *
  * The gradient: dq, dk of q_out, k_out; gq, gk of q, k (gq may be dq or q, with the same stride, gk alike); gq_weight,
  * gk_weight fp32 [head_dim], for each weight that there is, summed over all tokens and heads in a fixed order (zeros
@@ -609,9 +609,10 @@ ris_status ris_paged_append(const ris_paged *cache, ris_pack_t pack, const void 
  * One token, a few drafted ones and chunks of prompts may stand in one pack, any heads / kv_heads.
  * An entry of the table that is needed and no page is reported by ris_device_status as RIS_ERR_INVALID (the rows
  * that see it are then undefined). A key that a row does not see takes no part in it, whatever it holds.
- * fp32: products and sums in fp32. bf16: exact products, fp32 sums, each weight rounded once. bf16 rows that cannot be had so (a value that
- * is not finite beside them in a tile, a weight more than 2^100 times those of the first 128 keys) are computed a second time in fp32: right,
- * but slow.
+ * fp32: products and sums in fp32. bf16: exact products, fp32 sums, each weight rounded once. Where a row sees a value that is not finite, or another
+ * row of its tile does, or its largest weight is more than 2^100 times that of the first keys it is given (of its window, or of a share of its keys:
+ * that can be one), a thread block does its share of the call twice; rows of scores past 2^28 are computed in fp32, slowly. Rows without such a value
+ * or score come out the same, whatever stands beside them in the call.
  * Errors: RIS_ERR_INVALID, RIS_ERR_OOM, RIS_ERR_CUDA. */
 ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void *q, int64_t q_stride, int32_t heads, int32_t window,
                             int32_t anchors, int64_t longest, void *out, float *lse, void *stream);

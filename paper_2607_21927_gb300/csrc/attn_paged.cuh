@@ -169,6 +169,7 @@ struct Walk {
     int item, unit, cost;  // cost 0: the item has not been looked at
     int seq, row0;
     Sight sight;
+    Walk() = default;
     __device__ __forceinline__ explicit Walk(const Run &r) : v(r.v0), u0(r.u0), item(r.item), unit(0), cost(0), seq(0), row0(0) {}
     template <int BN>
     __device__ __forceinline__ bool next(const PagedAttendArgs &a, const Run &r, Unit &x)
