@@ -476,6 +476,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
     const uint32_t sbase = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const unsigned int *const gave_up = &g_ris_paged_wait;
+    const long long limit = a.wait_limit;
     auto bar = [&](int i) { return sbase + (uint32_t)(L::OFF_BARS + 8 * i); };
 
     // 1: a second pass is needed, 2: something is left to do after it, 4: a wait gave up, 8: it is the second pass, 16: rows
@@ -512,7 +513,13 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
     const uint32_t tmem = tmem_base_sh;
     bool ok = (sbase & 1023u) == 0u;
     auto wait_all = [&](int i, int parity) -> bool {
-        const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up));
+        const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(i), parity, gave_up, limit));
+        tc_fence_after();
+        return got;
+    };
+    // The same by looking at the barrier where a test asks for short waits: of one role, as every wait would cost short row tiles 8%.
+    auto look_all = [&](int i, int parity) -> bool {
+        const bool got = __all_sync(0xFFFFFFFFu, mbar_wait<1, false, true>(bar(i), parity, gave_up, limit));
         tc_fence_after();
         return got;
     };
@@ -526,13 +533,13 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
             asm volatile("ld.acquire.cta.shared::cta.b32 %0, [%1];" : "=r"(x) : "r"(at) : "memory");
             if (__all_sync(0xFFFFFFFFu, x >= least)) return true;
             const long long waited = clock64() - since;
-            const bool over = waited > (1LL << 31) || (waited > (1LL << 20) && *reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u);
+            const bool over = waited > limit || (waited > (1LL << 20) && *reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u);
             if (__any_sync(0xFFFFFFFFu, over)) return false;
         }
     };
     // description of unit u (a whole warp); its place is given back once every lane has it
     auto unit = [&](int u, Info &x) -> bool {
-        if (!__all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up))) return false;
+        if (!__all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up, limit))) return false;
         x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
         __syncwarp();
         mbar_arrive_if(lane == 0, bar(L::B_I_FREE + u % NI));
@@ -579,7 +586,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                 Unit y;
                 bool more = walk.next<BN>(a, run, y);
                 for (int u = 0; ok; ++u) {
-                    if (u >= NI) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up));
+                    if (u >= NI) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FREE + u % NI), (u / NI - 1) & 1, gave_up, limit));
                     if (!ok) break;
                     const Info z{more ? y.j1 - y.j0 : -1, y.j0, y.sight.sinks, y.sight.first, y.sight.pos0, y.sight.tokens, y.sight.low, y.sight.end,
                                  y.head0, y.heads, y.kv_head, y.seq, y.row0, y.part};
@@ -598,29 +605,29 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                         const int st = nk % NSK;
                         const Box at = AHEAD ? next : Box(a, x, j, col, blk < NB);
                         if (AHEAD && j + 1 < n) next = Box(a, x, j + 1, col, blk < NB);
-                        if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up));
+                        if (nk >= NSK) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_K_FREE + st), (nk / NSK - 1) & 1, gave_up, limit));
                         if (!ok) break;
                         if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_K_FULL + st), TILE);
                         __syncwarp();
-                        if (blk < NB)
+                        if (blk < NB && a.debug_no_loads == 0)
                             tma_load_4d(sbase + L::OFF_K + st * TILE + blk * L::BLK + col * 128, &maps.k, 64 * blk, at.key & in_page, x.kv_head, at.page(a),
                                         bar(L::B_K_FULL + st));
                         if (j > 0) continue;
-                        if (nq > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up));
+                        if (nq > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_Q_FREE), (nq - 1) & 1, gave_up, limit));
                         if (!ok) {
                             ++nk;
                             break;
                         }
                         if (lane == 0) {
                             mbar_arrive_expect_tx<1>(bar(L::B_Q_FULL), q_bytes);
-                            for (int b = 0; b < NB; ++b) tma_load_3d<1>(sbase + L::OFF_Q + b * L::BLK, &maps.q, 64 * b, x.head0, x.row0, bar(L::B_Q_FULL));
+                            for (int b = 0; b < NB && a.debug_no_loads == 0; ++b) tma_load_3d<1>(sbase + L::OFF_Q + b * L::BLK, &maps.q, 64 * b, x.head0, x.row0, bar(L::B_Q_FULL));
                         }
                         ++nq;
                         more = walk.next<BN>(a, run, y);  // (while these are on their way)
                     }
                     if (n == 0) more = walk.next<BN>(a, run, y);
                 }
-                if (lane == 0) {
+                if (lane == 0 && a.debug_no_loads == 0) {
                     // nothing of this warp's may still be on its way to shared memory when the CTA ends
                     if (nq > 0) mbar_wait_own<1>(bar(L::B_Q_FULL), (nq - 1) & 1);
                     for (int i = max(0, nk - NSK); i < nk; ++i) mbar_wait_own<1>(bar(L::B_K_FULL + i % NSK), (i / NSK) & 1);
@@ -636,16 +643,16 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                         const int st = nv % NSV;
                         const Box at = AHEAD ? next : Box(a, x, j, col, blk < NB);
                         if (AHEAD && j + 1 < x.n) next = Box(a, x, j + 1, col, blk < NB);
-                        if (nv >= NSV) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up));
+                        if (nv >= NSV) ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_V_FREE + st), (nv / NSV - 1) & 1, gave_up, limit));
                         if (!ok) break;
                         if (lane == 0) mbar_arrive_expect_tx<1>(bar(L::B_V_FULL + st), TILE);
                         __syncwarp();
-                        if (blk < NB)
+                        if (blk < NB && a.debug_no_loads == 0)
                             tma_load_4d(sbase + L::OFF_V + st * TILE + blk * L::BLK + col * 128, &maps.v, 64 * blk, at.key & in_page, x.kv_head, at.page(a),
                                         bar(L::B_V_FULL + st));
                     }
                 }
-                if (lane == 0)
+                if (lane == 0 && a.debug_no_loads == 0)
                     for (int i = max(0, nv - NSV); i < nv; ++i) mbar_wait_own<1>(bar(L::B_V_FULL + i % NSV), (i / NSV) & 1);
             } else if (ok) {
                 // The issuing warps, all lanes: trip counts and addresses come out of warp-wide reductions,
@@ -685,10 +692,10 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
                         }
                     } else {
                         constexpr uint32_t ID_O = idesc_bf16(BM, D, true);
-                        if (NG > 1 && nq > 0) ok = wait_all(L::B_O_FREE, (nq - 1) & 1);
+                        if (NG > 1 && nq > 0) ok = look_all(L::B_O_FREE, (nq - 1) & 1);
                         for (int j = 0; j < n && ok; ++j, ++t) {
                             const int st = t % NSV;
-                            ok = wait_all(L::B_V_FULL + st, (t / NSV) & 1) && wait_all(L::B_P_GO + t % NS, (t / NS) & 1);
+                            ok = look_all(L::B_V_FULL + st, (t / NSV) & 1) && look_all(L::B_P_GO + t % NS, (t / NS) & 1);
                             if (!ok) break;
                             const uint32_t vd = desc_lo(sbase + L::OFF_V + st * TILE, L::BLK);
                             if (elect_one()) {
@@ -732,7 +739,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
             if (!L::OVER && lane == 0) mbar_arrive(bar(L::B_S_GO));
             for (int u = 0; ok; ++u) {
                 // (its description stays in its place until the unit is done)
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up));
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait<1>(bar(L::B_I_FULL + u % NI), (u / NI) & 1, gave_up, limit));
                 const Info &x = *reinterpret_cast<const Info *>(smem + L::OFF_INFO + u % NI * 64);
                 const int n = x.n;
                 if (!ok || n < 0) break;

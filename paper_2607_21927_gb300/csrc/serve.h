@@ -151,6 +151,8 @@ struct PagedAttendArgs {
     int32_t reach;             // lengths count up to here
     float scale_log2;
     int32_t box_rows;          // tile kernel: keys of a TMA box
+    int64_t wait_limit;        // tile kernel: cycles that a wait may take
+    int32_t debug_no_loads;    // tile kernel, tests only: no copies are issued, so the first wait on them gives up
     // the sharing out of the work (attn_paged.cuh)
     int64_t line;              // row tiles of the line (at most)
     int32_t unit_cost;         // what a row tile costs besides its key tiles

@@ -839,6 +839,8 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.reach = (int32_t)(longest > 0 ? longest : capacity);
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
     a.least = 1;
+    a.wait_limit = debug_wait_limit() > 0 ? debug_wait_limit() : int64_t(1) << 31;
+    a.debug_no_loads = debug_no_loads();
     const bool tiles = cache->dtype == RIS_BF16;
     a.unit_cost = paged_unit_cost(tiles, cache->head_dim);
     const int32_t tile_rows = tiles ? kPagedTileRows : paged_f32_rows((int64_t)pack->q_longest * a.G);

@@ -139,18 +139,21 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity)
     return ok != 0;
 }
 
-// Bounded wait (about 2^31 cycles); false if the phase did not complete in time or another CTA
+// Bounded wait (about 2^31 cycles; a test may ask for less); false if the phase did not complete in time or another CTA
 // already gave up (*gave_up, the device error word).
-template <int CG, bool TMEM = false>
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const unsigned int *gave_up)
+// POLL: where less is asked for, by looking at the barrier (an attempt at a wait may sleep for longer than that).
+constexpr long long kWaitCycles = 1LL << 31;
+template <int CG, bool TMEM = false, bool POLL = false>
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const unsigned int *gave_up, long long limit = kWaitCycles)
 {
-    if (mbar_try_wait<CG, TMEM>(bar, parity)) return true;
+    auto there = [&]() -> bool { return !POLL || limit >= kWaitCycles ? mbar_try_wait<CG, TMEM>(bar, parity) : mbar_test<CG, TMEM>(bar, parity); };
+    if (there()) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait<CG, TMEM>(bar, parity)) {
+    while (!there()) {
         // (the error word only once the wait is far beyond what it ever takes: a poll that reads it first sees the
         // barrier a memory latency late)
         const long long waited = clock64() - t0;
-        if (waited > (1LL << 31)) return false;
+        if (waited > limit) return false;
         if (waited > (1LL << 20) && *reinterpret_cast<const volatile unsigned int *>(gave_up) != 0u) return false;
     }
     return true;

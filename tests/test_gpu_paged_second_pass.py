@@ -63,8 +63,7 @@ def test_a_poisoned_key_costs_little(D, Hq, Hkv, window, anchors):
                     hit |= pos >= first
                 hit = torch.cat([hit, torch.tensor([False, False])]).cuda()
                 assert not torch.isfinite(out[hit]).any()
-                # (the others may be computed another way, at the same precision)
-                assert torch.isfinite(out[~hit]).all() and ((out[~hit].float() - clean[~hit].float()).abs() <= 2.0 ** -6).all()
+                assert torch.equal(out[~hit], clean[~hit])
                 times.append(_us(call))
     print(f"{D}, {Hq} / {Hkv}, window {window}: " + ", ".join(f"{t:.0f}" for t in times) + " us")
     assert max(times[1:]) <= 4 * times[0] + 20, times
