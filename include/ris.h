@@ -599,7 +599,7 @@ ris_status ris_paged_append(const ris_paged *cache, ris_pack_t pack, const void 
                             const int32_t *start, void *stream);
 
 /* Attention of a pack's rows (its q side) over the pages: q [q_total][heads][head_dim] (rotated), token stride
- * in elements; out [q_total][heads][head_dim] contiguous, both of the cache's dtype; lse optional
+ * in elements; out [q_total][heads][head_dim] contiguous and apart from q, both of the cache's dtype; lse optional
  * [heads][q_total]; scores scaled by 1 / sqrt(head_dim). The rows are the last of their sequence's slots in use
  * (append them first): row i of sequence b is at p = length[b] - q_lens[b] + i and sees the keys j <= p that
  * have j > p - window or j < anchors; window 0: all of them (anchors is 0). Pages that no row sees are not

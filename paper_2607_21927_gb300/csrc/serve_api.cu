@@ -824,6 +824,11 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     RIS_TRY(check_ptr(q, "q"));
     RIS_TRY(check_ptr(out, "out"));
     RIS_TRY(check_stride(q_stride, (int64_t)heads * cache->head_dim, cache->dtype, "q_stride"));
+    {  // (a second pass reads the queries again, after outputs have been written)
+        const uintptr_t row = (uintptr_t)heads * cache->head_dim, esz = cache->dtype == RIS_F32 ? 4 : 2, n = (uintptr_t)pack->q_total;
+        const uintptr_t q0 = reinterpret_cast<uintptr_t>(q), o0 = reinterpret_cast<uintptr_t>(out);
+        if (q0 < o0 + n * row * esz && o0 < q0 + ((n - 1) * (uintptr_t)q_stride + row) * esz) return fail(RIS_ERR_INVALID, "out overlaps q");
+    }
     PagedAttendArgs a{};
     a.c = paged_args(cache);
     a.q = q;

@@ -29,6 +29,9 @@ def test_refused(mem):  # noqa: F811
         a = dict(ok, **c)
         refused(ris, L.ris_paged_attend(d, a["pack"].handle, a["q"], a["qs"], a["heads"], a["window"], a["anchors"], a["longest"], a["out"],
                                         a["lse"], None))
+    for at in (p, p + 16, p + 5 * 1024 - 16):  # (outputs over the queries, which are read again after outputs have been written)
+        refused(ris, L.ris_paged_attend(d, pack.handle, p, 512, 4, 0, 0, 0, at, None, None))
+        refused(ris, L.ris_paged_attend(d, pack.handle, at, 512, 4, 0, 0, 0, p, None, None))
     assert L.ris_paged_attend(d, none.handle, None, 0, 4, 0, 0, 0, None, None, None) == ris.RIS_OK  # (no rows: nothing to do)
     assert ris.ris_launch_count() == before
 
@@ -43,6 +46,8 @@ def test_binding_refuses():
                 ris.ris_paged_attend(cache, pack, bad)
         with pytest.raises(AssertionError):
             ris.ris_paged_attend(cache, pack, q.float())
+        with pytest.raises(ris.RisError):
+            ris.ris_paged_attend(cache, pack, q, out=q)
         with pytest.raises(AssertionError):
             ris.ris_paged_attend(cache, pack, q, out=torch.empty(5, 4, 64, device="cuda"))
         with pytest.raises(AssertionError):
