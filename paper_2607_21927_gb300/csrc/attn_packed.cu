@@ -239,6 +239,27 @@ struct PackedMaps {
 // scores.
 __device__ __forceinline__ void values_ready() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// O of 32 rows (a warp's) x OC columns from TMEM, normalised, into the warp's part of shared memory, row by
+// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv
+// 0) become zeros whatever the columns hold.
+template <int OC, typename TOut>
+__device__ __forceinline__ void stage_out(unsigned char *stage, uint32_t t_o, float inv)
+{
+    constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;  // bytes and pieces of a row's part
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c0 = 0; c0 < OC; c0 += 32) {
+        float ov[32];
+        tmem_ld32(t_o + c0, ov);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) ov[c] = inv == 0.f ? 0.f : ov[c] * inv;
+#pragma unroll
+        for (int e = 0; e < 32 * (int)sizeof(TOut) / 16; ++e) {
+            const int piece = c0 * (int)sizeof(TOut) / 16 + e;
+            store16<TOut>(stage + lane * RB + ((piece ^ (lane & (NP - 1))) << 4), ov + e * (16 / (int)sizeof(TOut)));
+        }
+    }
+}
 // the first `rows` of those rows to memory, so that neighbouring lanes store neighbouring pieces of a row
 template <int OC, typename TOut>
 __device__ __forceinline__ void rows_out(const unsigned char *stage, TOut *out, int64_t pitch, int rows)

@@ -113,7 +113,7 @@ __device__ __forceinline__ Run run_of(const PagedAttendArgs &a, int cta, RunMem 
     const int units = a.c.Hkv * a.blocks;  // row tiles of an item
     auto use = [&](int64_t cost) {
         r.total = cost * units;
-        r.runs = (int)min((int64_t)a.runs, max((int64_t)1, r.total / a.least));
+        r.runs = (int)min((int64_t)a.runs, max((int64_t)1, r.total));
         if (cta < r.runs && r.total > 0) r.v0 = r.begin(cta), r.v1 = r.begin(cta + 1);
     };
     if (a.max_items > 0) {

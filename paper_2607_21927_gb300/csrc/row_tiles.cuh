@@ -71,34 +71,5 @@ __device__ __forceinline__ void store16(void *dst, const float *x)
         *reinterpret_cast<uint4 *>(dst) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
 }
 
-// O of 32 rows (a warp's) x OC columns from TMEM, normalised, into the warp's part of shared memory, row by
-// row in 16-byte pieces swizzled by the row (128-byte rows: as TMA reads a box). Rows with no weight (inv
-// 0) become zeros whatever the columns hold. CHECK: returns 0, or NaN where one of the thread's values is not
-// finite.
-template <int OC, typename TOut, bool CHECK = false>
-__device__ __forceinline__ float stage_out(unsigned char *stage, uint32_t t_o, float inv)
-{
-    constexpr int RB = OC * (int)sizeof(TOut), NP = RB / 16;  // bytes and pieces of a row's part
-    const int lane = threadIdx.x & 31;
-    float found = 0.f;
-#pragma unroll
-    for (int c0 = 0; c0 < OC; c0 += 32) {
-        float ov[32];
-        tmem_ld32(t_o + c0, ov);
-#pragma unroll
-        for (int c = 0; c < 32; ++c) ov[c] = inv == 0.f ? 0.f : ov[c] * inv;
-        if constexpr (CHECK) {
-#pragma unroll
-            for (int c = 0; c < 32; ++c) found = fmaf(ov[c], 0.f, found);
-        }
-#pragma unroll
-        for (int e = 0; e < 32 * (int)sizeof(TOut) / 16; ++e) {
-            const int piece = c0 * (int)sizeof(TOut) / 16 + e;
-            store16<TOut>(stage + lane * RB + ((piece ^ (lane & (NP - 1))) << 4), ov + e * (16 / (int)sizeof(TOut)));
-        }
-    }
-    return found;
-}
-
 }  // namespace tc
 }  // namespace ris

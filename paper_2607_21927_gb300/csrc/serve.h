@@ -156,7 +156,7 @@ struct PagedAttendArgs {
     // the sharing out of the work (attn_paged.cuh)
     int64_t line;              // row tiles of the line (at most)
     int32_t unit_cost;         // what a row tile costs besides its key tiles
-    int32_t runs, least;       // runs of the line, one for each CTA; key tiles of one at least
+    int32_t runs;              // of the line, one for each CTA
     int32_t max_items;         // 0: a row tile per sequence, else as many items as the plan has room for
     int64_t *prefix;           // [max_items + 1] scratch: cost of the items before
     PagedItem *items;          // [max_items]

@@ -843,7 +843,6 @@ ris_status ris_paged_attend(const ris_paged *cache, ris_pack_t pack, const void 
     a.anchors = std::min(anchors, 1 << 30);
     a.reach = (int32_t)(longest > 0 ? longest : capacity);
     a.scale_log2 = (float)log2e_over_sqrt(cache->head_dim);
-    a.least = 1;
     a.wait_limit = debug_wait_limit() > 0 ? debug_wait_limit() : int64_t(1) << 31;
     a.debug_no_loads = debug_no_loads();
     const bool tiles = cache->dtype == RIS_BF16;
