@@ -9,13 +9,13 @@
 //
 // Persistent, each CTA on its run of the line, one row tile at a time:
 //   head dim 128  one CTA to an SM (TMEM 512 columns), two softmax groups that take the row tile's key tiles in turn and add
-//                 their weights up in one O, three buffers of scores. 8,192 rows behind 24,576 keys at 12 / 2 heads take 900 us
-//                 (1.6 PFLOP/s; 990 in a long row of calls, at the power limit): a tile takes 1,350 cycles, of which shared
+//                 their weights up in one O, three buffers of scores. 8,192 rows behind 24,576 keys at 12 / 2 heads take 885 us
+//                 (1.6 PFLOP/s; 985 in a long row of calls, at the power limit): a tile takes 1,350 cycles, of which shared
 //                 memory is busy for 1,280 (Q and K read for the scores, V for the outputs, 64 KB written by TMA). With one group and two
-//                 buffers 1,015, with two CTAs of a group and a buffer each 1,130. 16 single tokens behind 48 to 64 thousand keys: 140 us, 95%
+//                 buffers 1,015, with two CTAs of a group and a buffer each 1,130. 16 single tokens behind 48 to 64 thousand keys: 138 us, 96%
 //                 of the copy rate.
 //   head dim 64   two CTAs to an SM (TMEM 256 columns) with a group each, weights beside the scores; nothing is full, a softmax warp's
-//                 chain of 2,370 cycles a tile sets the time: 16,384 rows at 32 / 4 heads take 1,070 us; one CTA took 1,650.
+//                 chain of 2,370 cycles a tile sets the time: 16,384 rows at 32 / 4 heads take 1,056 us; one CTA took 1,650.
 // The first warps (a group's four) do the softmax, one thread per row; a warp without a row only passes the tiles on. Then
 //   kLoadQK   the run's units, query and key tiles, kLoadV value tiles: TMA, a box for each page of a tile, the
 //             boxes of a tile issued by as many lanes; a page that no row sees is asked for past the pool's end, which
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(Lay<D>::THREADS, Lay<D>::CTAS) k_paged_tiles(c
     if (warp >= kSoftmaxWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(L::OTHER_REGS));
         // table entries are asked for a tile ahead where there are registers for it (pages of 16 slots at 12 / 2 heads of 128:
-        // 16,384 rows in 725 us instead of 772; at head dim 64 spilled registers cost 2%)
+        // 16,384 rows in 725 us instead of 772 when it was built, 699 now; at head dim 64 spilled registers cost 2%)
         constexpr bool AHEAD = D == 128;
         const int boxes = BN / a.box_rows;  // of a tile and 64-column block
         const int col = lane % boxes * a.box_rows, blk = lane / boxes, in_page = (1 << a.c.page_log2) - 1;

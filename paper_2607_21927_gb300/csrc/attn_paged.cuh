@@ -4,9 +4,9 @@
 // token r / block, head r % block), so that a token's heads share every key they read. It sees the keys
 // from the first that its first row sees up to its last row's own, and the first `anchors`: a list of granules
 // (32 keys; in fp32 a tile), those of the anchors first, cut into n tiles of BN keys, and the row tile costs n and
-// as many tiles more as beginning and ending it take: 5 in bf16 at head dim 128 (16,384 rows at 12 / 2 heads: 556 us,
-// with 4 580, with 3 643, as the CTAs that have the short row tiles come last), 3 at 64 (16,384 rows at 32 / 4 heads:
-// 1,064 us, with 5 1,074), 1 in fp32 (900 rows: 156 us, with 4 186). The row tiles of all sequences, heads innermost,
+// as many tiles more as beginning and ending it take: 5 in bf16 at head dim 128 (16,384 rows at 12 / 2 heads: 556 us when it
+// was chosen, 542 now; with 4 580, with 3 643, as the CTAs that have the short row tiles come last), 3 at 64 (16,384 rows at 32 / 4
+// heads: 1,064 us, now 1,056; with 5 1,074), 1 in fp32 (900 rows: 156 us, with 4 186). The row tiles of all sequences, heads innermost,
 // laid one after another make a line of that length, which is cut into as many equal runs as there are
 // CTAs: one row against 60,000 keys and 8,000 rows against 30,000 are spread over the SMs alike, whatever
 // the lengths, which only the device knows. A row tile that lies in one run is finished there; of the

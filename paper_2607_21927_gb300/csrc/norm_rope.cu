@@ -10,8 +10,8 @@
 // the turn needs no other lane: D / 2V lanes make a head, and its sums take log2 of that many exchanges. A
 // thread keeps its V angles for all heads of its token. Arithmetic and statistics are fp32 (two values to an
 // instruction), angles 64-bit fractions of a turn (rows.cuh). Bound by HBM, each element read once and written
-// once: 30,011 tokens of 12 / 2 heads of 128 in bf16 take 37 us (215 MB, 86% of the copy rate); the gradient
-// at 32 / 4 heads of 64 takes 69 us (415 MB, 89%; 73 without the hint that the next 256 bytes follow).
+// once: 30,011 tokens of 12 / 2 heads of 128 in bf16 take 38 us (215 MB, 83% of the copy rate); the gradient
+// at 32 / 4 heads of 64 takes 69.5 us (415 MB, 88%; 4 more without the hint that the next 256 bytes follow).
 #include <algorithm>
 #include <cstdint>
 
