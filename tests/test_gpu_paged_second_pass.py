@@ -155,3 +155,39 @@ def test_scores_past_all_bounds(D, Hq, window, anchors):
         assert ((y[a:a + n] - w @ v).abs() <= 2.0 ** -8 * (w @ v).abs() + 700 * 2.0 ** -24 * (w @ v.abs())).all()
         a += n
     ris.ris_device_status()
+
+
+def test_a_captured_call_meets_a_poisoned_key():
+    """A graph captured over finite keys, replayed before, with and after a NaN in one of them, twice in a row and beside another stream's."""
+    lengths, q_lens = [900, 40, 2000], [130, 1, 4]
+    cache, keys, values = make(lengths, 2, 128, 32, BF16, seed=1)
+    q = randn(135, 12, 128, seed=2, dtype=BF16)
+    packs, streams, outs, graphs = [], [], [], []
+    for _ in range(2):
+        pack, stream, out = ris.ris_pack_create(q_lens), torch.cuda.Stream(), torch.empty_like(q)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            ris.ris_paged_attend(cache, pack, q, out=out)
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                ris.ris_paged_attend(cache, pack, q, out=out)
+        packs.append(pack), streams.append(stream), outs.append(out), graphs.append(graph)
+    at = (int(cache.table[0, 850 // 32]), 1, 850 % 32, 7)
+    was = cache.v[at].clone()
+    for what in (None, NAN, INF, None):
+        cache.v[at] = was if what is None else what
+        values[0][850, 1, 7] = was if what is None else what
+        torch.cuda.synchronize()
+        for stream, graph in zip(streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+                graph.replay()
+        torch.cuda.synchronize()
+        ref = plain(q, keys, values, q_lens)
+        for out in outs:
+            y = out.double().cpu()
+            assert torch.equal(y.isnan(), ref[0].isnan()) and torch.equal(y == INF, ref[0] == INF)
+            check(out, None, ref, BF16)
+    ris.ris_device_status()
+    graphs.clear()
