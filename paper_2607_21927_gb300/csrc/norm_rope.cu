@@ -439,7 +439,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) k_weight_sums(const float2 *pa
         add_exactly(s, c, s2);
         c += c2;
     }
-    if (lane == 0) out[c0 + warp] = s + c;
+    if (lane == 0) out[c0 + warp] = fabsf(s) < INFINITY ? s + c : s;  // (what an infinity leaves is NaN)
 }
 
 template <typename T, bool PAIRS, int D>

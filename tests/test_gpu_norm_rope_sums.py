@@ -21,3 +21,24 @@ def test_gradient_of_a_weight_over_thousands_of_terms():
     _, _, gw, _ = ris.ris_norm_rope_backward(d, None, x, None, None, 1, None, w, eps=0.0, gq=d)
     want = dy.double() * (n * H)
     assert ((gw.double() - want).abs() <= (63 * 2.0 ** -24 + 2.0 ** -22 + 2.0 ** -23) * want).all(), float(((gw.double() - want).abs() / want).max())
+
+
+@pytest.mark.parametrize("n", [1, 3000])
+def test_an_infinite_term(n):
+    """An infinity among the terms of a channel: its sum is that, NaN with both signs or a NaN, and the other channels' are as without it."""
+    D, H = 64, 2
+    g = torch.Generator().manual_seed(n)
+    x, d = (torch.randn(n, H, D, generator=g).cuda() for _ in range(2))
+    x = x.abs() + 0.5
+    w = torch.ones(D, device="cuda")
+
+    def call(dy):
+        return ris.ris_norm_rope_backward(dy, None, x, None, None, 1, None, w)[2]
+
+    clean, bad = call(d), d.clone()
+    inf, nan = float("inf"), float("nan")
+    bad[n // 2, 0, 3], bad[n // 2, 1, 5], bad[0, 0, 7], bad[0, 0, 9], bad[n - 1, 1, 9] = inf, -inf, nan, inf, -inf
+    got = call(bad)
+    assert got[3] == inf and got[5] == -inf and got[7].isnan() and got[9].isnan()
+    rest = [c for c in range(D) if c not in (3, 5, 7, 9)]
+    assert torch.equal(got[rest], clean[rest])
